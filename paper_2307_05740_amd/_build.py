@@ -30,7 +30,9 @@ CALL_LIB = os.path.join(PKG_DIR, "tensor_call.so")
 ORACLE_LIB = os.path.join(REPO_DIR, "oracle", "liboracle.so")
 
 HIP_SOURCES = ["csrc/decompose.cpp", "csrc/layout.cpp", "csrc/abi.cpp", "csrc/kernels.hip", "csrc/sddmm.hip",
-               "csrc/csf3.cpp", "csrc/mttkrp.hip", "csrc/probe.hip", "csrc/static_scratch.hip"]
+               "csrc/csf3.cpp", "csrc/mttkrp.hip", "csrc/probe.hip", "csrc/static_scratch.hip",
+               "csrc/attention.cpp", "csrc/attention.hip", "csrc/attention_grad.hip", "csrc/attention_decode.hip",
+               "csrc/embedding.cpp", "csrc/embedding.hip"]
 
 
 def _run(cmd: list[str]) -> None:

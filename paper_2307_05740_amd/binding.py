@@ -32,6 +32,9 @@ EXPORTED = [
     "arrow_destroy",
     "csf3_build", "csf3_device_bytes", "csf3_upload", "csf3_workspace_bytes", "csf3_set_workspace",
     "csf3_mttkrp", "csf3_info", "csf3_form", "csf3_set_profiling", "csf3_get_profile", "csf3_last_error", "csf3_destroy",
+    "arrow_attention_forward", "arrow_attention_workspace_bytes", "arrow_attention_backward", "arrow_cache_append",
+    "arrow_attention_decode_workspace_bytes", "arrow_attention_decode",
+    "arrow_embedding_forward", "arrow_embedding_workspace_bytes", "arrow_embedding_backward",
 ]
 
 
@@ -84,6 +87,34 @@ class csf3_info_t(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int64) for name in
                 ("I", "J", "K", "nnz", "slices", "fibers", "segments", "items", "split_rows", "partials",
                  "distinct_j", "distinct_k")] + [("build_seconds", ctypes.c_double)]
+
+
+ARROW_F32, ARROW_BF16, ARROW_F16 = 0, 1, 2
+
+
+class arrow_strides_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("sequence", "token", "head")]
+
+
+class arrow_attention_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("dtype", "batch", "q_heads", "kv_heads", "dim", "q_len", "k_len", "window", "sinks")] + \
+               [("scale", ctypes.c_float), ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
+                ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64)] + \
+               [(name, arrow_strides_t) for name in ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")]
+
+
+class arrow_cache_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "batch", "q_heads", "kv_heads", "dim", "window", "sinks")] + \
+               [("scale", ctypes.c_float), ("page", ctypes.c_int32), ("columns", ctypes.c_int32)] + \
+               [(name, ctypes.c_int64) for name in
+                ("pages", "max_len", "k_page", "k_token", "k_head", "v_page", "v_token", "v_head")] + \
+               [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
+
+
+class arrow_embedding_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "grad_dtype", "id_bytes", "columns")] + \
+               [(name, ctypes.c_int64) for name in ("rows", "tokens", "w_stride", "y_stride")] + [("scale", ctypes.c_float)]
 
 
 def lib():
@@ -184,6 +215,26 @@ def lib():
     L.csf3_last_error.argtypes = []
     L.csf3_destroy.restype = None
     L.csf3_destroy.argtypes = [vp]
+    attention, cache, embedding, st = (ctypes.POINTER(arrow_attention_t), ctypes.POINTER(arrow_cache_t),
+                                       ctypes.POINTER(arrow_embedding_t), arrow_strides_t)
+    L.arrow_attention_forward.restype = ctypes.c_int
+    L.arrow_attention_forward.argtypes = [attention, vp, vp, vp, vp, vp, vp]
+    L.arrow_attention_workspace_bytes.restype = sz
+    L.arrow_attention_workspace_bytes.argtypes = [attention]
+    L.arrow_attention_backward.restype = ctypes.c_int
+    L.arrow_attention_backward.argtypes = [attention] + [vp] * 10 + [sz, vp]
+    L.arrow_cache_append.restype = ctypes.c_int
+    L.arrow_cache_append.argtypes = [cache, i32, vp, vp, st, st, vp, vp, vp]
+    L.arrow_attention_decode_workspace_bytes.restype = sz
+    L.arrow_attention_decode_workspace_bytes.argtypes = [cache]
+    L.arrow_attention_decode.restype = ctypes.c_int
+    L.arrow_attention_decode.argtypes = [cache, vp, st, vp, vp, st, st, vp, vp, vp, st, vp, sz, vp]
+    L.arrow_embedding_forward.restype = ctypes.c_int
+    L.arrow_embedding_forward.argtypes = [embedding, vp, vp, vp, vp]
+    L.arrow_embedding_workspace_bytes.restype = sz
+    L.arrow_embedding_workspace_bytes.argtypes = [embedding]
+    L.arrow_embedding_backward.restype = ctypes.c_int
+    L.arrow_embedding_backward.argtypes = [embedding, vp, vp, vp, vp, sz, vp]
     _lib = L
     return L
 

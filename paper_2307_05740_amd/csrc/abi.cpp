@@ -54,6 +54,11 @@ struct Span {
 
 }  // namespace
 
+namespace arrow {
+// The same for entries in other files (attention_internal.h).
+int fail_text(int code, const char* text) { return fail(code, "%s", text); }
+}  // namespace arrow
+
 struct arrow_handle {
   int64_t n = 0, nnz = 0;
   int32_t b = 0;

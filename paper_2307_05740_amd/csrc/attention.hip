@@ -1,0 +1,193 @@
+// Attention under an arrow-shaped mask, forward (include/arrow_attention.h).
+//
+// A wavefront holds 32 queries and goes through tiles of 64 keys.  It computes the scores transposed, S^T = K Q^T, so that a
+// lane has one query's scores in its registers: the running maximum and sum of the softmax need one exchange, between lane halves, and
+// the probabilities are at once the B operand of O^T += V^T P^T.
+#include "attention_common.h"
+
+namespace arrow {
+namespace {
+
+constexpr int kStep = 64;   // keys of a tile
+
+// One row of the result in plain steps, the wavefront's lanes over its columns, by the row's own visible keys alone.  Matrix
+// instructions multiply what a query does not see by a probability of 0, and that is no zero where a value there is infinite or NaN:
+// the rows that this may have touched come here.
+template <typename T>
+__device__ __noinline__ void plain_row(const T* q, const char* k, const char* v, T* o, int64_t k_token, int64_t v_token, int dim, int p, int window,
+                                       int sinks, float scale, float lse) {
+  const int lane = threadIdx.x & 63, d = 2 * lane;
+  const bool mine = d < dim;
+  const float q0 = mine ? (float)q[d] : 0.f, q1 = mine ? (float)q[d + 1] : 0.f;
+  float a0 = 0.f, a1 = 0.f;
+  for (int j = 0; j <= p; ++j) {
+    if (window && j >= sinks && j <= p - window) { j = p - window; continue; }
+    const T* kj = (const T*)(k + 2 * (int64_t)j * k_token);
+    const T* vj = (const T*)(v + 2 * (int64_t)j * v_token);
+    float s = mine ? q0 * (float)kj[d] + q1 * (float)kj[d + 1] : 0.f;
+    for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m, 64);
+    const float w = exp2f((s * scale - lse) * kLog2e);
+    if (mine) { a0 += w * (float)vj[d]; a1 += w * (float)vj[d + 1]; }
+  }
+  if (mine) { o[d] = (T)a0; o[d + 1] = (T)a1; }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a, int tiles) {
+  using Tl = Tile<D>;
+  __shared__ __align__(1024) unsigned char smem[4][kStep * Tl::kRowBytes];   // keys and values, two tiles each
+  const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
+  // query heads of one key head next to each other, then tiles of queries: they read the same keys
+  int id = blockIdx.x;
+  const int g = id % a.group; id /= a.group;
+  const int tile = tiles - 1 - id % tiles; id /= tiles;       // the longest rows of a triangle first
+  const int kv = id % a.kv_heads, b = id / a.kv_heads, head = kv * a.group + g;
+  const bool ragged = a.q_offsets != nullptr;
+  const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
+  const int first = tile * kQueryTile;
+  if (first >= sq.count) return;
+  const int shift = sk.count - sq.count;                      // position of query 0
+  const int row = first + wave * 32 + (lane & 31);            // this lane's query
+  const bool there = row < sq.count;
+  const int p = row + shift;
+  const char* q = rows_of(a.q, ragged, b, sq.first, head);
+  const char* k = rows_of(a.k, ragged, b, sk.first, kv);
+  const char* v = rows_of(a.v, ragged, b, sk.first, kv);
+
+  x8<T> qf[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const int d = 16 * s + 8 * half;
+    x8<T> z = {};
+    qf[s] = there && d < a.dim ? *(const x8<T>*)(q + 2 * ((int64_t)row * a.q.token + d)) : z;
+  }
+
+  const int last = min(first + kQueryTile, sq.count) - 1 + shift;
+  const SeenTiles seen = seen_tiles<kStep>(max(first + shift, 0), last, a.window, a.sinks);
+  // of this wavefront's queries
+  const int low = first + wave * 32 + shift, high = min(low + 31, sk.count - 1);
+
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m) acc[m] = (f32x16)(0.f);
+  const float c = a.scale * kLog2e;
+  float top = minus_infinity(), total = 0.f;                  // of c times the scores; of this lane's keys
+
+  const Loader<D, kStep, 4> lk(wave, lane, a.k.token, a.dim), lv(wave, lane, a.v.token, a.dim);
+  lds_byte* base = (lds_byte*)smem;
+  auto load = [&](int t, int to) {
+    const int k0 = seen.at(t) * kStep;
+    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * (kStep * Tl::kRowBytes), wave);
+    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * (kStep * Tl::kRowBytes), wave);
+  };
+  if (seen.total > 0) load(0, 0);
+  for (int t = 0; t < seen.total; ++t) {
+    wait_for_tiles();
+    if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
+    const lds_byte* kt = base + (2 * (t & 1)) * (kStep * Tl::kRowBytes);
+    const lds_byte* vt = kt + kStep * Tl::kRowBytes;
+    const int k0 = seen.at(t) * kStep;
+    // no query of this wavefront sees the tile
+    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
+
+    f32x16 s[kStep / 32];
+#pragma unroll
+    for (int n = 0; n < kStep / 32; ++n) {
+      s[n] = (f32x16)(0.f);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        s[n] = mma32(lds_rows<T>(kt + n * 32 * Tl::kRowBytes + Tl::rows_at(lane, i)), qf[i], s[n]);
+    }
+    // every query sees every key: nothing to mask
+    const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
+    if (!whole) {
+      const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
+      const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
+#pragma unroll
+      for (int n = 0; n < kStep / 32; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = n * 32 + 8 * (i / 4) + i % 4;
+          const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
+          s[n][i] = visible ? s[n][i] : minus_infinity();
+        }
+    }
+    float most = s[0][0];
+#pragma unroll
+    for (int n = 0; n < kStep / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
+    most = max_halves(most) * c;
+    // The maximum is only raised where a score is more than 2^8 times the terms' scale: until then they stay within what the sums and
+    // both types hold, and the sums are left as they are.
+    if (__any(most > top + 8.f)) {
+      const float now = most > top + 8.f ? most : top;
+      const float by = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+      top = now;
+      total *= by;
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m) acc[m] *= by;
+    }
+    const float off = top == minus_infinity() ? 0.f : top;
+    x8<T> pf[kStep / 16];
+#pragma unroll
+    for (int n = 0; n < kStep / 32; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -off));
+        total += s[n][i];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        pf[2 * n + u] = round8<T>(s[n][8 * u], s[n][8 * u + 1], s[n][8 * u + 2], s[n][8 * u + 3], s[n][8 * u + 4], s[n][8 * u + 5],
+                                  s[n][8 * u + 6], s[n][8 * u + 7]);
+    }
+#pragma unroll
+    for (int u = 0; u < kStep / 16; ++u)
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m)
+        acc[m] = mma32(lds_columns<T>(vt + 16 * u * Tl::kRowBytes + Tl::columns_at(lane, m, 0), vt + 16 * u * Tl::kRowBytes + Tl::columns_at(lane, m, 1)),
+                       pf[u], acc[m]);
+  }
+
+  total = add_halves(total);
+  const float by = total > 0.f || total != total ? 1.f / total : 0.f;
+  const float lse = total == 0.f ? minus_infinity() : (top + __log2f(total)) * kLn2;
+  const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
+  if (a.lse && there && half == 0) a.lse[stat] = lse;
+  float test = 0.f;                                           // NaN where a result is not finite
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { acc[m][i] *= by; test = fmaf(acc[m][i], 0.f, test); }
+  const bool finite_lse = lse - lse == 0.f;
+  uint64_t odd = __ballot(there && finite_lse && test != test);
+  odd = (odd | odd >> 32) & 0xffffffffu;
+  T* o = (T*)rows_of(a.o, ragged, b, sq.first, head);
+  // (all lanes take part in the exchange; whether a row is stored is the same in both halves)
+  if (there && !(odd >> (lane & 31) & 1)) store_columns<T, D>(acc, o + (int64_t)row * a.o.token, half, a.dim);
+  while (odd) {
+    const int r = __builtin_ctzll(odd);
+    odd &= odd - 1;
+    const int at = first + wave * 32 + r;
+    plain_row<T>((const T*)q + (int64_t)at * a.q.token, k, v, o + (int64_t)at * a.o.token, a.k.token, a.v.token, a.dim, at + shift, a.window, a.sinks,
+                 a.scale, __shfl(lse, r, 64));
+  }
+}
+
+template <typename T, int D>
+int forward(const AttentionArgs& a, void* stream) {
+  const int64_t tiles = (a.q_len + (int64_t)kQueryTile - 1) / kQueryTile, blocks = tiles * a.q_heads * a.batch;
+  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  attention_forward_kernel<T, D><<<dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream>>>(a, (int)tiles);
+  return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream) {
+  if (dtype == ARROW_BF16) return a.dim <= 64 ? forward<__bf16, 64>(a, stream) : forward<__bf16, 128>(a, stream);
+  return a.dim <= 64 ? forward<_Float16, 64>(a, stream) : forward<_Float16, 128>(a, stream);
+}
+
+}  // namespace arrow

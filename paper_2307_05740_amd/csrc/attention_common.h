@@ -1,0 +1,200 @@
+// Helpers shared by the attention kernels: 16-bit types and their matrix instructions, tiles of rows in LDS.
+// Everything has internal linkage; include inside a .hip file only.
+//
+// Matrix instructions.  D = A B + C over 32 x 32 with 16 inner steps; lane l holds row (A) or column (B) l % 32 at inner
+// steps 8 (l / 32) + 0..7, and of C and D column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 for i = 0..15.  A product whose inner steps
+// run over the rows of an earlier result takes that result as its B operand without any exchange between lanes: the inner steps may come
+// in any order as long as A has the same one, so lane half h = l / 32 simply holds rows 4 h + 0..3 and 8 + 4 h + 0..3 of each 16.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "attention_internal.h"
+
+namespace arrow {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <typename T> struct Wide;
+template <> struct Wide<__bf16> {
+  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 x4 __attribute__((ext_vector_type(4)));
+  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+};
+template <> struct Wide<_Float16> {
+  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 x4 __attribute__((ext_vector_type(4)));
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+};
+template <typename T> using x8 = typename Wide<T>::x8;
+template <typename T> using x4 = typename Wide<T>::x4;
+template <typename T> using x2 = typename Wide<T>::x2;
+
+__device__ __forceinline__ f32x16 mma32(x8<__bf16> a, x8<__bf16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(x8<_Float16> a, x8<_Float16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma16(x8<__bf16> a, x8<__bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma16(x8<_Float16> a, x8<_Float16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float minus_infinity() { return -__builtin_inff(); }
+
+// max / sum of a value and that of the lane 32 further on, in both.
+__device__ __forceinline__ float max_halves(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Eight values rounded to T, to nearest even.
+template <typename T>
+__device__ __forceinline__ x8<T> round8(float a, float b, float c, float d, float e, float f, float g, float h) {
+  x8<T> r;
+  r[0] = (T)a; r[1] = (T)b; r[2] = (T)c; r[3] = (T)d; r[4] = (T)e; r[5] = (T)f; r[6] = (T)g; r[7] = (T)h;
+  return r;
+}
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// A tile of rows of D 16-bit elements in LDS, in pieces of 16 bytes.  Piece c of row r lies at place c ^ turn(r) of the row, so
+// that both ways of reading it touch every bank once: 16 rows' pieces of one number (`rows`, an operand whose inner steps run
+// along the rows), and four rows' runs of 64 bytes (`columns`, one whose inner steps run across them, transposed on the way).
+template <int D>
+struct Tile {
+  static constexpr int kPieces = D / 8;
+  static constexpr int kRowBytes = 2 * D;
+  static constexpr int kRowsOfKiB = 1024 / kRowBytes;
+  __device__ static int turn(int r) {
+    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+  // Where in a tile lane l finds its part of A or B for rows row0 + l % 32 and columns 16 s + 8 (l / 32) + 0..7 (row0 a multiple of 32).
+  __device__ static int rows_at(int l, int s) { return (l & 31) * kRowBytes + (((2 * s + (l >> 5)) ^ turn(l & 31)) << 4); }
+  // The same for A = the transposed tile: columns 32 m + l % 32 as its rows, inner steps 8 u + 4 (l / 32) + 0..3 of rows row0 + 0..15
+  // (row0 a multiple of 16), four values for u = 0 and 1 each.
+  __device__ static int columns_at(int l, int m, int u) {
+    const int g = l >> 4, i = l & 15, row = 8 * u + 4 * (g >> 1) + (i >> 2), piece = 4 * m + 2 * (g & 1) + ((i & 3) >> 1);
+    return row * kRowBytes + ((piece ^ turn(row)) << 4) + ((i & 1) << 3);
+  }
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+template <typename T>
+__device__ __forceinline__ x8<T> lds_rows(const lds_byte* p) { return *(const __attribute__((address_space(3))) x8<T>*)p; }
+template <typename T>
+__device__ __forceinline__ x8<T> lds_columns(const lds_byte* __restrict p0, const lds_byte* __restrict p1) {
+  union { i16x4 half[2]; x8<T> all; } r;
+  r.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p0);
+  r.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p1);
+  return r.all;
+}
+
+// Copies ROWS rows of an operand into a Tile, straight to LDS, WAVES wavefronts together.  Rows that are not there and columns from `dim` on
+// become 0: the buffer descriptor ends with the last row.
+template <int D, int ROWS, int WAVES>
+struct Loader {
+  static constexpr int kSteps = ROWS / (WAVES * Tile<D>::kRowsOfKiB);
+  static_assert(kSteps * WAVES * Tile<D>::kRowsOfKiB == ROWS && (WAVES * Tile<D>::kRowsOfKiB) % 16 == 0, "whole steps, one turn");
+  uint32_t offset, step;
+  bool inside;
+  int dim_bytes, stride_bytes;
+  __device__ __forceinline__ Loader(int wave, int lane, int64_t stride, int dim) {
+    const int row = wave * Tile<D>::kRowsOfKiB + lane / Tile<D>::kPieces, piece = (lane % Tile<D>::kPieces) ^ Tile<D>::turn(row);
+    stride_bytes = (int)(stride * 2);
+    dim_bytes = dim * 2;
+    offset = (uint32_t)(row * stride_bytes + piece * 16);
+    step = (uint32_t)(WAVES * Tile<D>::kRowsOfKiB * stride_bytes);
+    inside = piece * 8 < dim;
+  }
+  // base: the tile's first row (the same in all lanes); rows: those that are there, any number
+  __device__ __forceinline__ void load(const void* base, int rows, lds_byte* tile, int wave) const {
+    rows = min(rows, ROWS);
+    const int bytes = rows > 0 ? (rows - 1) * stride_bytes + dim_bytes : 0;
+    auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (i * WAVES + wave) * 1024), 16,
+                                               inside ? offset + i * step : 0xfffffff0u, 0, 0, 0);
+  }
+};
+
+// Tokens of one sequence: where they start in its operands, and how many there are.
+struct Span { int64_t first; int count; };
+__device__ __forceinline__ Span span_of(const int32_t* offsets, int b, int64_t tokens, int len) {
+  if (!offsets) return {0, len};
+  int64_t first = offsets[b], end = offsets[b + 1];
+  first = first < 0 ? 0 : first > tokens ? tokens : first;
+  end = end < first ? first : end > tokens ? tokens : end;
+  const int64_t n = end - first;
+  return {first, (int)(n < len ? n : len)};
+}
+__device__ __forceinline__ const char* rows_of(const Operand& m, bool ragged, int b, int64_t first, int64_t head) {
+  return (const char*)m.at + 2 * (head * m.head + (ragged ? first * m.token : b * m.sequence));
+}
+
+// Which tiles of K keys the queries at positions low .. high see: the first `sinks` ones, then those of the window.
+struct SeenTiles {
+  int lead, rest, total;
+  __device__ __forceinline__ int at(int t) const { return t < lead ? t : t - lead + rest; }
+};
+template <int K>
+__device__ __forceinline__ SeenTiles seen_tiles(int low, int high, int window, int sinks) {
+  SeenTiles s{0, 0, 0};
+  if (high < 0) return s;
+  const int last = high / K;
+  const int64_t begin = (int64_t)low - window + 1;
+  s.rest = window && begin > 0 ? (int)(begin / K) : 0;
+  s.lead = window ? min((int)(((int64_t)sinks + K - 1) / K), s.rest) : 0;
+  s.total = s.lead + last - s.rest + 1;
+  return s;
+}
+
+// A transposed result of D rows (columns of the operand) and 32 columns (its rows, this lane's at `to`), rounded and stored.  A lane has
+// columns 32 m + 16 u + 4 half + 0..3 and + 8..11; with the other half's it gets eight in a row.
+template <typename T, int D>
+__device__ __forceinline__ void store_columns(const f32x16* acc, T* to, int half, int dim) {
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      union { x8<T> all; uint32_t w[4]; } r, x;
+      r.all = round8<T>(acc[m][8 * u], acc[m][8 * u + 1], acc[m][8 * u + 2], acc[m][8 * u + 3], acc[m][8 * u + 4], acc[m][8 * u + 5],
+                        acc[m][8 * u + 6], acc[m][8 * u + 7]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        auto y = __builtin_amdgcn_permlane32_swap(r.w[i], r.w[2 + i], false, false);
+        x.w[i] = y[0];
+        x.w[2 + i] = y[1];
+      }
+      const int d = 32 * m + 16 * u + 8 * half;
+      if (d < dim) *(x8<T>*)(to + d) = x.all;
+    }
+}
+
+// Where the sums of a part of a key tile lie in the workspace, counted in pairs (dk, dv): only tiles in several parts have places.
+__device__ __forceinline__ int64_t part_place(const AttentionArgs& a, int tiles, int64_t unit, int tile, int part) {
+  const int lead = a.sink_parts > 1 ? a.sink_tiles * a.sink_parts : 0;
+  const int per_unit = lead + (a.tile_parts > 1 ? (tiles - a.sink_tiles) * a.tile_parts : 0);
+  return unit * per_unit + (tile < a.sink_tiles ? tile * a.sink_parts : lead + (tile - a.sink_tiles) * a.tile_parts) + part;
+}
+
+__device__ __forceinline__ void wait_for_tiles() {
+  // (the builtins of loads to LDS count as vector memory)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
+}  // namespace
+}  // namespace arrow

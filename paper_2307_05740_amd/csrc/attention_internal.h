@@ -1,0 +1,53 @@
+// What the entries of arrow_attention.h hand to their kernels.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "arrow_attention.h"
+
+namespace arrow {
+
+// Sets the calling thread's arrow_last_error() text and returns `code` (abi.cpp).
+int fail_text(int code, const char* text);
+
+struct Operand {
+  const void* at;
+  int64_t sequence, token, head;   // steps in elements
+};
+
+struct AttentionArgs {
+  Operand q, k, v, o, d_o, dq, dk, dv;
+  const float* lse_in;             // backward
+  float* lse;                      // forward, may be null
+  float* delta;                    // backward: <do_i, o_i>, laid out as lse
+  float* parts;                    // backward: sums of the parts of a key tile, dk then dv of each
+  const int32_t *q_offsets, *k_offsets;
+  int64_t q_tokens, k_tokens;
+  int32_t batch, q_heads, kv_heads, group, dim, q_len, k_len, window, sinks;
+  float scale;
+  // backward, keys: tiles of keys that some query sees for good (the first ones, with a window), and into how many parts
+  // the work of those and of the others is cut
+  int32_t sink_tiles, sink_parts, tile_parts;
+};
+
+struct CacheArgs {
+  arrow_cache_t c;
+  Operand q, k, v, o;              // the new token's (k, v may be null)
+  void *k_pool, *v_pool;
+  int32_t group, splits, page_log, tokens;
+  float* parts;                    // splits x batch x q_heads x (dim + 2)
+};
+
+// Launchers: 0 or a hipError_t.
+int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream);
+int launch_attention_backward(const AttentionArgs& a, int32_t dtype, void* stream);
+int launch_cache_append(const CacheArgs& a, void* stream);
+int launch_attention_decode(const CacheArgs& a, void* stream);
+
+constexpr int kQueryTile = 128;    // queries of a workgroup, forward and dq
+constexpr int kKeyTile = 128;      // keys of a workgroup, dk and dv
+constexpr int kQueryStep = 64;     // queries that it goes through at a time
+constexpr int kHeadTile = 16;      // query heads of a workgroup, single tokens
+
+}  // namespace arrow

@@ -1,0 +1,392 @@
+"""Attention under an arrow-shaped mask against the 64-bit oracle: forward, gradients, single tokens over a cache in pages.  The bounds are the oracle's:
+what the roundings of the operands' type may do."""
+import math
+
+import pytest
+
+from oracle import attention_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ("bfloat16", "float16")
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: these tests need a real MI355X")
+    return torch
+
+
+@pytest.fixture(scope="module")
+def Attention(torch):
+    from paper_2307_05740_amd.attention import ArrowAttention
+    return ArrowAttention
+
+
+def normal(torch, seed, dtype, *shape, by=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * by).to(getattr(torch, dtype)).cuda()
+
+
+def within(torch, name, got, want, bound):
+    got = got.double()
+    same = (got == want) | ((got - want).abs() <= bound)
+    if not bool(same.all()):
+        off = torch.where(same, 0.0, torch.nan_to_num((got - want).abs() / bound.clamp(min=1e-300), nan=math.inf, posinf=math.inf))
+        at = int(off.argmax())
+        raise AssertionError(f"{name}: {int((~same).sum())} of {same.numel()} values off, the worst {float(off.max()):.3g} times the bound: "
+                             f"{float(got.flatten()[at])} for {float(want.flatten()[at])} at {at}")
+
+
+def check_sequence(torch, got, q, k, v, window, sinks, scale=None, d_o=None):
+    """One sequence, (tokens, heads, dim): got holds o, lse (heads, tokens) and the gradients there are."""
+    heads, kv = q.shape[1], k.shape[1]
+    grads = {}
+    for h in range(heads):
+        want, bound = oracle.attention(q[:, h], k[:, h * kv // heads], v[:, h * kv // heads], window, sinks, scale, None if d_o is None else d_o[:, h])
+        within(torch, f"o of head {h}", got["o"][:, h], want["o"], bound["o"])
+        within(torch, f"lse of head {h}", got["lse"][h], want["lse"], bound["lse"])
+        if d_o is not None:
+            within(torch, f"dq of head {h}", got["dq"][:, h], want["dq"], bound["dq"])
+            for n in ("dk", "dv"):
+                a, b = grads.setdefault((n, h * kv // heads), [0, 0])
+                grads[n, h * kv // heads] = [a + want[n], b + bound[n]]
+    for (n, h), (a, b) in grads.items():
+        within(torch, f"{n} of head {h}", got[n][:, h], a, b + oracle.UNIT[q.dtype] * a.abs())
+
+
+def run(torch, op, q, k, v, d_o=None, **ragged):
+    o, lse = op.forward(q, k, v, o=torch.full_like(q, math.nan), **ragged)
+    got = {"o": o, "lse": lse}
+    if d_o is not None:
+        nan = [torch.full_like(t, math.nan) for t in (q, k, v)]
+        got["dq"], got["dk"], got["dv"] = op.backward(d_o, q, k, v, o, lse, *nan, **ragged)
+    return got
+
+
+# queries, keys: one token to several tiles and odd numbers of them; more queries than keys leave rows empty
+LENGTHS = [(1, 1), (1, 64), (1, 300), (2, 2), (31, 31), (33, 33), (64, 64), (65, 65), (127, 130), (128, 128), (129, 129), (200, 200), (257, 321),
+           (300, 300), (7, 0), (50, 20), (300, 130), (3, 700)]
+MASKS = [(0, 0), (1, 0), (1, 1), (17, 0), (64, 4), (100, 65), (128, 200), (1000, 5)]
+
+
+@pytest.mark.parametrize("queries,keys", LENGTHS)
+@pytest.mark.parametrize("window,sinks", MASKS)
+def test_lengths_and_masks(torch, Attention, queries, keys, window, sinks):
+    dtype = TYPES[(queries + window) % 2]
+    q, d_o = (normal(torch, s, dtype, 1, queries, 2, 64, by=b) for s, b in ((1, 2.0), (4, 1.0)))
+    k, v = (normal(torch, s, dtype, 1, keys, 1, 64) for s in (2, 3))
+    got = run(torch, Attention(window, sinks), q, k, v, d_o)
+    check_sequence(torch, {n: t[0] for n, t in got.items()}, q[0], k[0], v[0], window, sinks, d_o=d_o[0])
+    if keys < queries:
+        empty = queries - keys
+        assert bool((got["o"][0, :empty] == 0).all()) and bool((got["lse"][0, :, :empty] == -math.inf).all()) and bool((got["dq"][0, :empty] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [8, 24, 64, 72, 80, 96, 128])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (6, 2), (8, 1)])
+def test_head_layouts(torch, Attention, dtype, dim, heads, kv):
+    q, d_o = (normal(torch, s, dtype, 2, 150, heads, dim) for s in (1, 4))
+    k, v = (normal(torch, s, dtype, 2, 170, kv, dim) for s in (2, 3))
+    for window, sinks in ((0, 0), (70, 3)):
+        got = run(torch, Attention(window, sinks, scale=0.2), q, k, v, d_o)
+        for b in range(2):
+            check_sequence(torch, {n: t[b] for n, t in got.items()}, q[b], k[b], v[b], window, sinks, 0.2, d_o[b])
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 4), (64, 300)])
+def test_long_sequences_in_parts(torch, Attention, window, sinks):
+    """Enough tiles for keys that all queries see to be cut into parts, and for the loads to go round both halves of their room."""
+    q, d_o = (normal(torch, s, "bfloat16", 1, 1500, 4, 128) for s in (1, 4))
+    k, v = (normal(torch, s, "bfloat16", 1, 1700, 2, 128) for s in (2, 3))
+    got = run(torch, Attention(window, sinks), q, k, v, d_o)
+    check_sequence(torch, {n: t[0] for n, t in got.items()}, q[0], k[0], v[0], window, sinks, d_o=d_o[0])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ragged_batches(torch, Attention, dtype):
+    lengths, keys = [5, 0, 1, 200, 64, 0, 131], [5, 0, 90, 210, 64, 33, 100]
+    nq, nk = sum(lengths) + 9, sum(keys) + 4                     # some tokens belong to no sequence
+    q, d_o = (normal(torch, s, dtype, nq, 4, 64) for s in (1, 4))
+    k, v = (normal(torch, s, dtype, nk, 2, 64) for s in (2, 3))
+    offsets = {n: torch.tensor([sum(x[:i]) for i in range(len(x) + 1)], dtype=torch.int32, device="cuda") for n, x in (("q_offsets", lengths), ("k_offsets", keys))}
+    for window, sinks in ((0, 0), (40, 3)):
+        for limits in ({}, {"q_len": 200, "k_len": 210}):
+            got = run(torch, Attention(window, sinks), q, k, v, d_o, **offsets, **limits)
+            a = b = 0
+            for n, m in zip(lengths, keys):
+                one = {x: got[x][a:a + n] for x in ("o", "dq")}
+                one.update({x: got[x][b:b + m] for x in ("dk", "dv")}, lse=got["lse"][:, a:a + n])
+                check_sequence(torch, one, q[a:a + n], k[b:b + m], v[b:b + m], window, sinks, d_o=d_o[a:a + n])
+                a, b = a + n, b + m
+            assert bool(got["o"][a:].isnan().all()) and bool(got["dq"][a:].isnan().all()) and bool(got["dk"][b:].isnan().all()), "no sequence's"
+
+
+def test_offsets_that_lie_are_cut_to_what_there_is(torch, Attention):
+    q, k, v = (normal(torch, s, "bfloat16", 40, 2, 64) for s in (1, 2, 3))
+    offsets = torch.tensor([-5, 20, 10, 4000], dtype=torch.int32, device="cuda")
+    o, _ = Attention().forward(q, k, v, q_offsets=offsets, k_offsets=offsets)
+    want, bound = oracle.attention(q[:20, 0], k[:20, 0], v[:20, 0])
+    within(torch, "o", o[:20, 0].double()[:10], want["o"][:10], bound["o"][:10])      # (sequence 2 begins at 10)
+
+
+def test_strides(torch, Attention):
+    """Operands and results within larger tensors: one for queries, keys and values together, heads before tokens, heads that are one head."""
+    both = normal(torch, 1, "bfloat16", 2, 100, 3, 4, 64)
+    q, k, v = both.unbind(2)
+    d_o = normal(torch, 2, "bfloat16", 2, 4, 100, 64).transpose(1, 2)
+    out = torch.full_like(both, math.nan)
+    op = Attention(30, 2)
+    o = torch.empty_strided(q.shape, (100 * 4 * 64, 64, 100 * 64, 1), dtype=q.dtype, device="cuda")
+    o, lse = op.forward(q, k, v, o=o)
+    dq, dk, dv = op.backward(d_o, q, k, v, o, lse, *out.unbind(2))
+    for b in range(2):
+        got = {"o": o[b], "lse": lse[b], "dq": out[b, :, 0], "dk": out[b, :, 1], "dv": out[b, :, 2]}
+        check_sequence(torch, got, q[b], k[b], v[b], 30, 2, d_o=d_o[b])
+    one_k, one_v = k[:, :, :1].expand(-1, -1, 4, -1), v[:, :, :1].expand(-1, -1, 4, -1)
+    o1, _ = op.forward(q, one_k, one_v)
+    o2, _ = op.forward(q, k[:, :, :1], v[:, :, :1])
+    assert torch.equal(o1, o2)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_what_is_not_seen_does_not_count(torch, Attention, bad):
+    """NaN and infinities in keys and values ahead of a query, behind its window, and beyond a sequence's end."""
+    q, k, v = (normal(torch, s, "bfloat16", 1, 300, 1, 64) for s in (1, 2, 3))
+    window, sinks = 50, 4
+    want, bound = oracle.attention(q[0, :, 0], k[0, :, 0], v[0, :, 0], window, sinks)
+    k[0, 100:102], v[0, 100:102] = bad, bad
+    o, lse = Attention(window, sinks).forward(q, k, v)
+    rows = [i for i in range(300) if not (100 <= i < 151)]
+    within(torch, "o", o[0, rows, 0], want["o"][rows], bound["o"][rows])
+    within(torch, "lse", lse[0, 0, rows], want["lse"][rows], bound["lse"][rows])
+    offsets = torch.tensor([0, 100], dtype=torch.int32, device="cuda")
+    o, _ = Attention(window, sinks).forward(q[0], k[0], v[0], q_offsets=offsets, k_offsets=offsets)
+    within(torch, "o of a sequence that ends there", o[:100, 0], want["o"][:100], bound["o"][:100])
+
+
+def test_large_scores(torch, Attention):
+    """Scores far beyond what exp holds, and rows whose maximum comes last."""
+    q = normal(torch, 1, "bfloat16", 1, 200, 1, 64, by=30.0)
+    k, v = (normal(torch, s, "bfloat16", 1, 200, 1, 64) for s in (2, 3))
+    k[0] *= torch.linspace(0.1, 8, 200, device="cuda")[:, None, None].to(k.dtype)
+    got = run(torch, Attention(), q, k, v)
+    check_sequence(torch, {n: t[0] for n, t in got.items()}, q[0], k[0], v[0], 0, 0)
+
+
+def test_gradients_against_differences(torch, Attention):
+    """Central differences of <o, d_o> in 64 bits along random directions; the gradient may be off by what its bound allows along them."""
+    q, k, v, d_o = (normal(torch, s, "float16", 1, 90, 2 if s in (1, 4) else 1, 64) for s in (1, 2, 3, 4))
+    window, sinks = 33, 2
+    got = run(torch, Attention(window, sinks), q, k, v, d_o)
+
+    def loss(q, k, v):
+        p = 0.0
+        for h in range(2):
+            s = (q[:, h] @ k[:, 0].T / 8.0).masked_fill(~oracle.visible(90, 90, window, sinks, "cuda"), -math.inf)
+            p = p + ((torch.softmax(s, -1) @ v[:, 0]) * d_o[0, :, h].double()).sum()
+        return float(p)
+
+    x = {"q": q[0].double(), "k": k[0].double(), "v": v[0].double()}
+    for name in x:
+        g = torch.Generator().manual_seed(9)
+        to = torch.randn(x[name].shape, generator=g).cuda().double()
+        eps = 1e-5
+        diff = (loss(**{**x, name: x[name] + eps * to}) - loss(**{**x, name: x[name] - eps * to})) / (2 * eps)
+        along = float((got["d" + name][0].double() * to).sum())
+        room = 0.0
+        for h in range(2):
+            _, bound = oracle.attention(q[0, :, h], k[0, :, 0], v[0, :, 0], window, sinks, None, d_o[0, :, h])
+            room += float((bound["d" + name] * (to[:, h] if name == "q" else to[:, 0]).abs()).sum())
+        assert abs(along - diff) <= room + 1e-6 * abs(diff), (name, along, diff, room)
+
+
+def test_results_are_the_same_every_time(torch, Attention):
+    q, d_o = (normal(torch, s, "bfloat16", 1, 1000, 4, 64) for s in (1, 4))
+    k, v = (normal(torch, s, "bfloat16", 1, 1000, 2, 64) for s in (2, 3))
+    op = Attention(100, 4)
+    first = run(torch, op, q, k, v, d_o)
+    for _ in range(3):
+        again = run(torch, op, q, k, v, d_o)
+        assert all(torch.equal(first[n], again[n]) for n in first)
+
+
+def test_captured_and_on_another_stream(torch, Attention):
+    q, d_o = (normal(torch, s, "bfloat16", 1, 500, 4, 64) for s in (1, 4))
+    k, v = (normal(torch, s, "bfloat16", 1, 500, 2, 64) for s in (2, 3))
+    op = Attention(100, 4)
+    want = run(torch, op, q, k, v, d_o)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        there = run(torch, op, q, k, v, d_o)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(want[n], there[n]) for n in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = op.forward(q, k, v)
+        grads = op.backward(d_o, q, k, v, o, lse)
+    for seed in (7, 8, 9):
+        q.copy_(normal(torch, seed, "bfloat16", 1, 500, 4, 64))
+        graph.replay()
+        want = run(torch, op, q, k, v, d_o)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want["o"]) and all(torch.equal(a, want[n]) for a, n in zip(grads, ("dq", "dk", "dv")))
+
+
+# ---- a cache in pages --------------------------------------------------------------------------------------------------------------
+def paged(torch, dtype, lengths, page, kv, dim, spare=3, columns=None, fill=math.nan):
+    """Pools whose unwritten places hold `fill`, a table in which pages lie in any order (-1 where there is none), and the keys and values of
+    each sequence."""
+    columns = max(1, max(-(-n // page) for n in lengths)) if columns is None else columns
+    need = sum(-(-n // page) for n in lengths)
+    g = torch.Generator().manual_seed(5)
+    order = torch.randperm(need + spare, generator=g).tolist()
+    table = torch.full((len(lengths), columns), -1, dtype=torch.int32)
+    pools = [torch.full((need + spare, page, kv, dim), fill, dtype=getattr(torch, dtype), device="cuda") for _ in range(2)]
+    rows = []
+    for b, n in enumerate(lengths):
+        own = [normal(torch, 100 * b + s, dtype, n, kv, dim) for s in (1, 2)]
+        rows.append(own)
+        for c in range(-(-n // page)):
+            table[b, c] = order.pop()
+            for pool, x in zip(pools, own):
+                part = x[c * page:(c + 1) * page]
+                pool[table[b, c], :part.shape[0]] = part
+    return pools, table.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda"), rows
+
+
+def check_tokens(torch, o, q, rows, window, sinks, scale=None):
+    for b, (k, v) in enumerate(rows):
+        if k.shape[0] == 0:
+            assert bool((o[b] == 0).all())
+            continue
+        for h in range(q.shape[1]):
+            kv = h * k.shape[1] // q.shape[1]
+            want, bound = oracle.attention(q[b, h][None], k[:, kv], v[:, kv], window, sinks, scale)
+            within(torch, f"o of sequence {b}, head {h}", o[b, h][None], want["o"], bound["o"])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page", [1, 8, 16, 64, 256])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (50, 4), (33, 70), (128, 1)])
+def test_single_tokens(torch, Attention, dtype, page, window, sinks):
+    lengths = [1, 0, 31, 32, 33, 200, 700]
+    (kp, vp), table, n, rows = paged(torch, dtype, lengths, page, 2, 64)
+    q = normal(torch, 3, dtype, len(lengths), 6, 64, by=2.0)
+    o = Attention(window, sinks).decode(q, kp, vp, table, n, max(lengths), o=torch.full_like(q, math.nan))
+    check_tokens(torch, o, q, rows, window, sinks)
+
+
+@pytest.mark.parametrize("dim", [8, 72, 96, 128])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (16, 1), (17, 1), (40, 1), (12, 4)])
+def test_single_tokens_head_layouts(torch, Attention, dim, heads, kv):
+    lengths = [5, 300]
+    (kp, vp), table, n, rows = paged(torch, "bfloat16", lengths, 16, kv, dim)
+    q = normal(torch, 3, "bfloat16", 2, heads, dim)
+    for max_len in (None, 300, 1, 100000):                       # whatever is said of the longest
+        o = Attention(scale=0.3).decode(q, kp, vp, table, n, max_len)
+        check_tokens(torch, o, q, rows, 0, 0, 0.3)
+
+
+def test_single_tokens_over_a_long_cache(torch, Attention):
+    lengths = [9000, 4097, 1]
+    (kp, vp), table, n, rows = paged(torch, "bfloat16", lengths, 64, 2, 128)
+    q = normal(torch, 3, "bfloat16", 3, 16, 128)
+    for window, sinks in ((0, 0), (3000, 100)):
+        o = Attention(window, sinks).decode(q, kp, vp, table, n, 9000)
+        check_tokens(torch, o, q, rows, window, sinks)
+
+
+@pytest.mark.parametrize("heads", [4, 40])
+def test_the_new_token_is_written_first(torch, Attention, heads):
+    lengths = [1, 0, 32, 33, 500]
+    (kp, vp), table, n, rows = paged(torch, "bfloat16", lengths, 16, 2, 64)
+    q, k, v = normal(torch, 3, "bfloat16", 5, heads, 64), *(normal(torch, s, "bfloat16", 5, 2, 64) for s in (4, 5))
+    want_k, want_v = kp.clone(), vp.clone()
+    for b, m in enumerate(lengths):
+        if m:
+            rows[b][0][-1], rows[b][1][-1] = k[b], v[b]
+            want_k[table[b, (m - 1) // 16], (m - 1) % 16] = k[b]
+            want_v[table[b, (m - 1) // 16], (m - 1) % 16] = v[b]
+    o = Attention(40, 3).decode(q, kp, vp, table, n, 500, k=k, v=v)
+    check_tokens(torch, o, q, rows, 40, 3)
+    assert torch.equal(kp.view(torch.int16), want_k.view(torch.int16)) and torch.equal(vp.view(torch.int16), want_v.view(torch.int16)), "nothing else is written"
+
+
+def test_pages_that_are_not_there_are_not_seen(torch, Attention):
+    """Entries outside the pool, and lengths beyond the table: neither read nor written."""
+    lengths = [100]
+    (kp, vp), table, n, rows = paged(torch, "float16", lengths, 16, 1, 64)
+    table[0, 1], table[0, 3] = -1, 10_000
+    gone = [i for i in range(100) if i // 16 in (1, 3)]
+    q, k, v = normal(torch, 3, "float16", 1, 2, 64), *(normal(torch, s, "float16", 1, 1, 64) for s in (4, 5))
+    seen = torch.ones(1, 100, dtype=torch.bool, device="cuda")
+    seen[0, gone] = False
+    o = Attention().decode(q, kp, vp, table, n, 100)
+    for h in range(2):
+        want, bound = oracle.attention(q[0, h][None], rows[0][0][:, 0], rows[0][1][:, 0], seen=seen)
+        within(torch, "o", o[0, h][None], want["o"], bound["o"])
+    before = kp.clone()
+    o = Attention().decode(q, kp, vp, table, torch.tensor([20], dtype=torch.int32, device="cuda"), 100, k=k, v=v)
+    assert torch.equal(kp.view(torch.int16), before.view(torch.int16))
+    o = Attention().decode(q, kp, vp, table, torch.tensor([2_000_000_000], dtype=torch.int32, device="cuda"), 100)
+    assert o.shape == q.shape
+    o = Attention().decode(q, kp, vp, table, torch.tensor([-3], dtype=torch.int32, device="cuda"), 100)
+    assert bool((o == 0).all())
+
+
+def test_prompts_are_appended(torch, Attention):
+    lengths = [40, 3, 0, 17]
+    (kp, vp), table, n, rows = paged(torch, "bfloat16", lengths, 8, 2, 72)
+    blank = [torch.zeros_like(kp), torch.zeros_like(vp)]
+    new = [normal(torch, s, "bfloat16", 4, 20, 2, 72) for s in (7, 8)]
+    Attention().append(*new, *blank, table, n)
+    for pool, x in zip(blank, new):
+        want = torch.zeros_like(pool)
+        for b, m in enumerate(lengths):
+            for t in range(20):
+                j = m - 20 + t
+                if j >= 0:
+                    want[table[b, j // 8], j % 8] = x[b, t]
+        assert torch.equal(pool, want)
+
+
+def test_pools_of_heads_before_tokens(torch, Attention):
+    lengths = [50, 9]
+    (kp, vp), table, n, rows = paged(torch, "bfloat16", lengths, 16, 2, 64)
+    q = normal(torch, 3, "bfloat16", 2, 4, 64)
+    want = Attention().decode(q, kp, vp, table, n)
+    other = [p.transpose(1, 2).contiguous().transpose(1, 2) for p in (kp, vp)]
+    assert torch.equal(Attention().decode(q, *other, table, n), want)
+
+
+def test_single_tokens_agree_with_whole_sequences(torch, Attention):
+    """The last row of the forward call, and a captured step that is replayed as the sequence grows."""
+    op = Attention(60, 4)
+    k, v = (normal(torch, s, "bfloat16", 1, 120, 2, 64) for s in (1, 2))
+    q = normal(torch, 3, "bfloat16", 1, 120, 4, 64)
+    whole, _ = op.forward(q, k, v)
+    pools = [torch.zeros(8, 16, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.arange(8, dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    n = torch.zeros(1, dtype=torch.int32, device="cuda")
+    now = [torch.empty(1, t.shape[2], 64, dtype=torch.bfloat16, device="cuda") for t in (q, k, v)]
+    now[0].zero_()
+    out = torch.empty_like(now[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        n.add_(1)
+        op.decode(now[0], *pools, table, n, 120, k=now[1], v=now[2], o=out)
+    n.zero_()
+    for t in range(120):
+        for to, x in zip(now, (q, k, v)):
+            to.copy_(x[:, t])
+        graph.replay()
+        if t % 13 == 0 or t == 119:
+            for h in range(4):
+                want, bound = oracle.attention(q[0, t, h][None], k[0, :t + 1, h // 2], v[0, :t + 1, h // 2], 60, 4)
+                within(torch, "o", out[0, h][None], want["o"], bound["o"])
+                within(torch, "o of the whole", whole[0, t, h][None], want["o"], bound["o"])
