@@ -83,15 +83,21 @@ AttentionArgs plan(const arrow_attention_t* a) {
   p.dim = a->dim; p.q_len = a->q_len; p.k_len = a->k_len; p.scale = a->scale;
   p.window = a->window < a->k_len ? a->window : 0;   // one as long as any sequence hides nothing
   p.sinks = p.window ? std::min(a->sinks, a->k_len) : 0;
-  // Keys that every later query sees have far more work than the others; it is cut into parts of about the others' work.
-  const int64_t tiles = ceil_div(a->k_len, kKeyTile), steps = ceil_div(a->q_len, kQueryStep) * p.group;
+  // Gradients of keys: a workgroup has the queries that see a tile of keys, in steps of 64 queries of a head.
+  const int64_t tiles = ceil_div(a->k_len, kKeyTile), all = ceil_div(a->q_len, kQueryStep) * p.group;
+  const int64_t usual = p.window ? std::min(all, (ceil_div((int64_t)p.window + kKeyTile, kQueryStep) + 1) * p.group) : all;
   p.sink_tiles = (int32_t)std::min(tiles, ceil_div(p.sinks, kKeyTile));
-  const int64_t usual = p.window ? std::min(steps, (ceil_div((int64_t)p.window + kKeyTile, kQueryStep) + 1) * p.group) : steps;
-  p.sink_parts = p.sink_tiles ? (int32_t)std::min<int64_t>(64, std::max<int64_t>(1, ceil_div(steps, std::max<int64_t>(usual, 16)))) : 1;
-  // Few tiles of keys leave most of the chip empty: the others are cut as well, down to eight steps each.
-  const int64_t items = std::max<int64_t>(1, tiles * a->kv_heads * a->batch);
-  p.tile_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({16, ceil_div(512, items), usual / 8}));
-  p.sink_parts = std::max(p.sink_parts, p.tile_parts);
+  // A tile is cut into parts where that fills the chip better: the time goes by the rounds of workgroups that it holds at once, and a
+  // part costs about as much as kPartSteps steps more, for its sums on their way through memory.
+  constexpr int64_t kSlots = 512, kPartSteps = 10;
+  const int64_t items = std::max<int64_t>(1, (tiles - p.sink_tiles) * a->kv_heads * a->batch);
+  int64_t best = INT64_MAX;
+  for (int32_t n = 1; n <= 16 && (n == 1 || usual / n >= 4); ++n) {
+    const int64_t time = ceil_div(items * n, kSlots) * (ceil_div(usual, n) + (n > 1 ? kPartSteps : 0));
+    if (time < best) { best = time; p.tile_parts = n; }
+  }
+  // Keys that every later query sees have far more queries than the others.  Their parts are small and come last, to fill what others leave.
+  p.sink_parts = p.sink_tiles ? (int32_t)std::max<int64_t>(p.tile_parts, std::min<int64_t>(64, ceil_div(all, std::max<int64_t>(8, usual / 4)))) : 1;
   return p;
 }
 
@@ -104,7 +110,7 @@ int64_t pairs_of(const AttentionArgs& p) {
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
-size_t delta_bytes(const arrow_attention_t* a) {
+size_t rows_bytes(const arrow_attention_t* a) {
   const int64_t rows = a->q_offsets ? a->q_tokens * a->q_heads : (int64_t)a->batch * a->q_heads * a->q_len;
   return align_up((size_t)rows * 4);
 }
@@ -172,7 +178,7 @@ int arrow_attention_forward(const arrow_attention_t* a, const void* q, const voi
 
 size_t arrow_attention_workspace_bytes(const arrow_attention_t* a) {
   if (check(a)) return 0;
-  return delta_bytes(a) + align_up((size_t)pairs_of(plan(a)) * 2 * kKeyTile * a->dim * 4);
+  return 2 * rows_bytes(a) + align_up((size_t)pairs_of(plan(a)) * 2 * kKeyTile * a->dim * 4);
 }
 
 int arrow_attention_backward(const arrow_attention_t* a, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -198,8 +204,9 @@ int arrow_attention_backward(const arrow_attention_t* a, const void* q, const vo
   p.q = operand(q, a->q); p.k = operand(k, a->k); p.v = operand(v, a->v); p.o = operand(o, a->o); p.d_o = operand(d_o, a->d_o);
   p.dq = operand(dq, a->dq); p.dk = operand(dk, a->dk); p.dv = operand(dv, a->dv);
   p.lse_in = lse;
-  p.delta = (float*)ws;
-  p.parts = (float*)((char*)ws + delta_bytes(a));
+  p.off = (float*)ws;
+  p.delta = (float*)((char*)ws + rows_bytes(a));
+  p.parts = (float*)((char*)ws + 2 * rows_bytes(a));
   return launched("attention backward", launch_attention_backward(p, a->dtype, stream));
 }
 

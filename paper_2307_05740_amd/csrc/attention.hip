@@ -75,6 +75,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 
   const Loader<D, kStep, 4> lk(wave, lane, a.k.token, a.dim), lv(wave, lane, a.v.token, a.dim);
   lds_byte* base = (lds_byte*)smem;
+  const TileReads<D> my(lane);
   auto load = [&](int t, int to) {
     const int k0 = seen.at(t) * kStep;
     lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * (kStep * Tl::kRowBytes), wave);
@@ -84,8 +85,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
   for (int t = 0; t < seen.total; ++t) {
     wait_for_tiles();
     if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
-    const lds_byte* kt = base + (2 * (t & 1)) * (kStep * Tl::kRowBytes);
-    const lds_byte* vt = kt + kStep * Tl::kRowBytes;
+    const uint32_t kt = lds_address(base) + (2 * (t & 1)) * (kStep * Tl::kRowBytes), vt = kt + kStep * Tl::kRowBytes;
     const int k0 = seen.at(t) * kStep;
     // no query of this wavefront sees the tile
     if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       s[n] = (f32x16)(0.f);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
-        s[n] = mma32(lds_rows<T>(kt + n * 32 * Tl::kRowBytes + Tl::rows_at(lane, i)), qf[i], s[n]);
+        s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
     }
     // every query sees every key: nothing to mask
     const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
@@ -146,8 +146,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     for (int u = 0; u < kStep / 16; ++u)
 #pragma unroll
       for (int m = 0; m < D / 32; ++m)
-        acc[m] = mma32(lds_columns<T>(vt + 16 * u * Tl::kRowBytes + Tl::columns_at(lane, m, 0), vt + 16 * u * Tl::kRowBytes + Tl::columns_at(lane, m, 1)),
-                       pf[u], acc[m]);
+        acc[m] = mma32(read_columns<T, D>(vt + my.columns, m, 16 * u * Tl::kRowBytes), pf[u], acc[m]);
   }
 
   total = add_halves(total);

@@ -76,26 +76,43 @@ struct Tile {
   __device__ static int turn(int r) {
     return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   }
-  // Where in a tile lane l finds its part of A or B for rows row0 + l % 32 and columns 16 s + 8 (l / 32) + 0..7 (row0 a multiple of 32).
-  __device__ static int rows_at(int l, int s) { return (l & 31) * kRowBytes + (((2 * s + (l >> 5)) ^ turn(l & 31)) << 4); }
-  // The same for A = the transposed tile: columns 32 m + l % 32 as its rows, inner steps 8 u + 4 (l / 32) + 0..3 of rows row0 + 0..15
-  // (row0 a multiple of 16), four values for u = 0 and 1 each.
-  __device__ static int columns_at(int l, int m, int u) {
-    const int g = l >> 4, i = l & 15, row = 8 * u + 4 * (g >> 1) + (i >> 2), piece = 4 * m + 2 * (g & 1) + ((i & 3) >> 1);
-    return row * kRowBytes + ((piece ^ turn(row)) << 4) + ((i & 1) << 3);
-  }
 };
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
 template <typename T>
-__device__ __forceinline__ x8<T> lds_rows(const lds_byte* p) { return *(const __attribute__((address_space(3))) x8<T>*)p; }
+__device__ __forceinline__ x8<T> lds_read8(uint32_t at) { return *(const __attribute__((address_space(3))) x8<T>*)(uintptr_t)at; }
+__device__ __forceinline__ f32x4 lds_read4(uint32_t at) { return *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)at; }
+// (`restrict` tells these reads apart from the loads to LDS that are on their way to other tiles, for which they would wait otherwise;
+// so does that a kernel has all its LDS in one array)
+__device__ __forceinline__ i16x4 lds_transposed(const lds_byte* __restrict p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+}
+__device__ __forceinline__ uint32_t lds_address(const lds_byte* p) { return (uint32_t)(uintptr_t)p; }
+
+// This lane's places in the tile at an address whose low byte is 0.  Those of other inner steps and columns differ by an exclusive
+// or of a constant, which costs an instruction each and no registers from tile to tile.
+template <int D>
+struct TileReads {
+  uint32_t rows, columns;
+  __device__ __forceinline__ explicit TileReads(int l) {
+    const int g = l >> 4, i = l & 15, row = 4 * (g >> 1) + (i >> 2), piece = 2 * (g & 1) + ((i & 3) >> 1);
+    rows = (l & 31) * Tile<D>::kRowBytes + (((l >> 5) ^ Tile<D>::turn(l & 31)) << 4);
+    columns = row * Tile<D>::kRowBytes + ((piece ^ Tile<D>::turn(row)) << 4) + ((i & 1) << 3);
+  }
+};
+// A or B of a tile's rows (32 from a multiple of 32 on, `skip` bytes into the tile) and its columns 16 s .. 16 s + 15: lane l has row l % 32,
+// columns 16 s + 8 (l / 32) + 0..7.  at: the tile's address + TileReads::rows.
 template <typename T>
-__device__ __forceinline__ x8<T> lds_columns(const lds_byte* __restrict p0, const lds_byte* __restrict p1) {
+__device__ __forceinline__ x8<T> read_rows(uint32_t at, int s, int skip) { return lds_read8<T>((at ^ (s << 5)) + skip); }
+// A of the transposed tile: its rows are the tile's columns 32 m .. 32 m + 31, its inner steps 16 rows of the tile (from a multiple of 16 on, `skip` bytes into
+// it) in the order of an earlier result's.  at: the tile's address + TileReads::columns.
+template <typename T, int D>
+__device__ __forceinline__ x8<T> read_columns(uint32_t at, int m, int skip) {
   union { i16x4 half[2]; x8<T> all; } r;
-  r.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p0);
-  r.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p1);
+  r.half[0] = lds_transposed((const lds_byte*)(uintptr_t)((at ^ (m << 6)) + skip));
+  r.half[1] = lds_transposed((const lds_byte*)(uintptr_t)((at ^ (m << 6 | 32)) + skip + 8 * Tile<D>::kRowBytes));
   return r.all;
 }
 

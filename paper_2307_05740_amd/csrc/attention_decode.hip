@@ -168,7 +168,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_decode_kernel(CacheA
 #pragma unroll
     for (int m = 0; m < D / 16; ++m) {
       const lds_byte* at = vt + tr_byte + (((2 * m + tr_piece) ^ tr_turn) << 4);
-      acc[m] = mma16(lds_columns<T>(at, at + 16 * Tl::kRowBytes), pf, acc[m]);
+      union { i16x4 half[2]; x8<T> all; } vr;
+      vr.half[0] = lds_transposed(at);
+      vr.half[1] = lds_transposed(at + 16 * Tl::kRowBytes);
+      acc[m] = mma16(vr.all, pf, acc[m]);
     }
   }
   total = add_quarters(total);

@@ -11,11 +11,18 @@ namespace {
 
 constexpr int kStep = 64;   // keys of a tile (dq)
 
-// dq, and <do_i, o_i> for the other kernel.  As the forward kernel: a wavefront holds 32 queries, scores and their gradients are
-// transposed, dS^T is at once the B operand of dQ^T += K^T dS^T.
+// dq, and D_i = sum_j P(i,j) <do_i, v_j> for the other kernel.  As the forward kernel: a wavefront holds 32 queries, scores and their gradients
+// are transposed, dS^T is at once the B operand of dQ^T += K^T dS^T.
+//
+// D is <do_i, o_i> as well, but o has been rounded, and where a row has one large probability dS is a small difference of <do_i, v_j>
+// and D: the sum over the row's keys is exact to 32 bits.  Two ways to have it, both measured (TODO):
+//  - heads of up to 64: dS is formed with <do_i, o_i>, whose error e = -sum_j dS(i,j) comes out with the row, and dq is put right
+//    with e sum_j P(i,j) k_j, one product more;
+//  - larger heads, whose sums leave no registers for those of P K: the row is gone through twice, first for D alone.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
+  constexpr bool kTwice = D > 64;
   __shared__ __align__(1024) unsigned char smem[4][kStep * Tl::kRowBytes];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   int id = blockIdx.x;
@@ -45,71 +52,113 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
     const bool in = there && d < a.dim;
     qf[s] = in ? *(const x8<T>*)(q + 2 * ((int64_t)row * a.q.token + d)) : z;
     df[s] = in ? *(const x8<T>*)(d_o + 2 * ((int64_t)row * a.d_o.token + d)) : z;
-    const x8<T> of = in ? *(const x8<T>*)(o + 2 * ((int64_t)row * a.o.token + d)) : z;
+    if constexpr (!kTwice) {
+      const x8<T> of = in ? *(const x8<T>*)(o + 2 * ((int64_t)row * a.o.token + d)) : z;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) delta = fmaf((float)df[s][i], (float)of[i], delta);
+      for (int i = 0; i < 8; ++i) delta = fmaf((float)df[s][i], (float)of[i], delta);
+    }
   }
-  delta = add_halves(delta);
+  if constexpr (!kTwice) delta = add_halves(delta);
   const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
-  if (there && half == 0) a.delta[stat] = delta;
   // of a row that sees nothing, -infinity: its probabilities are masked
-  const float lse = there ? a.lse_in[stat] * kLog2e : 0.f;
+  const float off = there ? -a.lse_in[stat] / a.scale : 0.f;
 
   const int last = min(first + kQueryTile, sq.count) - 1 + shift;
   const SeenTiles seen = seen_tiles<kStep>(max(first + shift, 0), last, a.window, a.sinks);
   const int low = first + wave * 32 + shift, high = min(low + 31, sk.count - 1);
-  f32x16 acc[D / 32];
-#pragma unroll
-  for (int m = 0; m < D / 32; ++m) acc[m] = (f32x16)(0.f);
   const float c = a.scale * kLog2e;
 
   const Loader<D, kStep, 4> lk(wave, lane, a.k.token, a.dim), lv(wave, lane, a.v.token, a.dim);
   lds_byte* base = (lds_byte*)smem;
+  const TileReads<D> my(lane);
   auto load = [&](int t, int to) {
     const int k0 = seen.at(t) * kStep;
     lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * (kStep * Tl::kRowBytes), wave);
     lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * (kStep * Tl::kRowBytes), wave);
   };
-  if (seen.total > 0) load(0, 0);
-  for (int t = 0; t < seen.total; ++t) {
-    wait_for_tiles();
-    if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
-    const lds_byte* kt = base + (2 * (t & 1)) * (kStep * Tl::kRowBytes);
-    const lds_byte* vt = kt + kStep * Tl::kRowBytes;
-    const int k0 = seen.at(t) * kStep;
-    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
-    const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
-    const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
-    const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
+  // over all tiles, for 32 keys at a time: each(where their tile's columns are read, how far into it they begin, P^T, (<do, v> - delta)^T)
+  auto all_tiles = [&](auto&& each) {
+    if (seen.total > 0) load(0, 0);
+    for (int t = 0; t < seen.total; ++t) {
+      wait_for_tiles();
+      if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
+      const uint32_t kt = lds_address(base) + (2 * (t & 1)) * (kStep * Tl::kRowBytes), vt = kt + kStep * Tl::kRowBytes;
+      const int k0 = seen.at(t) * kStep;
+      if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
+      const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
+      const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
+      const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
 #pragma unroll
-    for (int n = 0; n < kStep / 32; ++n) {
-      f32x16 s = (f32x16)(0.f), e = (f32x16)(0.f);
+      for (int n = 0; n < kStep / 32; ++n) {
+        f32x16 s = (f32x16)(off), e = (f32x16)(-delta);       // the products begin with what is taken off them
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        s = mma32(lds_rows<T>(kt + n * 32 * Tl::kRowBytes + Tl::rows_at(lane, i)), qf[i], s);
-        e = mma32(lds_rows<T>(vt + n * 32 * Tl::kRowBytes + Tl::rows_at(lane, i)), df[i], e);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (e[i] - delta);
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = n * 32 + 8 * (i / 4) + i % 4;
-          const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
-          s[i] = visible ? s[i] : 0.f;
+        for (int i = 0; i < D / 16; ++i) {
+          s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s);
+          e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
         }
-      }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const x8<T> ds = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
-        const lds_byte* at = kt + (n * 32 + 16 * u) * Tl::kRowBytes;
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
+        if (!whole) {
 #pragma unroll
-        for (int m = 0; m < D / 32; ++m)
-          acc[m] = mma32(lds_columns<T>(at + Tl::columns_at(lane, m, 0), at + Tl::columns_at(lane, m, 1)), ds, acc[m]);
+          for (int i = 0; i < 16; ++i) {
+            const int j = n * 32 + 8 * (i / 4) + i % 4;
+            const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
+            s[i] = visible ? s[i] : 0.f;
+            e[i] = visible ? e[i] : 0.f;
+          }
+        }
+        each(kt + my.columns, n * 32 * Tl::kRowBytes, s, e);
       }
     }
-  }
+  };
 
+  float rest = 0.f;                                           // of this lane's keys: sum of dS, or D
+  if constexpr (kTwice) {
+    all_tiles([&](uint32_t, int, const f32x16& s, const f32x16& e) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) rest = fmaf(s[i], e[i], rest);
+    });
+    delta = add_halves(rest);
+    __syncthreads();                                          // the next loads go where the last tiles are read
+  }
+  f32x16 acc[D / 32], pk[kTwice ? 1 : D / 32];
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m) {
+    acc[m] = (f32x16)(0.f);
+    if constexpr (!kTwice) pk[m] = (f32x16)(0.f);
+  }
+  all_tiles([&](uint32_t kt, int skip, const f32x16& s, f32x16& e) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      e[i] *= s[i];
+      if constexpr (!kTwice) rest += e[i];
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
+      x8<T> pf;
+      if constexpr (!kTwice) pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m) {
+        const x8<T> kf = read_columns<T, D>(kt, m, skip + 16 * u * Tl::kRowBytes);
+        acc[m] = mma32(kf, ds, acc[m]);
+        if constexpr (!kTwice) pk[m] = mma32(kf, pf, pk[m]);
+      }
+    }
+  });
+
+  if constexpr (!kTwice) {
+    rest = add_halves(rest);
+    delta += rest;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[m][i] = fmaf(-rest, pk[m][i], acc[m][i]);
+  }
+  if (there && half == 0) {
+    a.off[stat] = off;
+    a.delta[stat] = -delta;
+  }
   T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
 #pragma unroll
   for (int m = 0; m < D / 32; ++m) acc[m] *= a.scale;
@@ -122,20 +171,22 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
 // Parts: part i of n takes the steps (64 queries of one head) from i / n to (i + 1) / n of the tile's; with n > 1 their sums go
 // to the workspace and attention_join_kernel adds them up in order.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
-  constexpr int kBytes = kQueryStep * Tl::kRowBytes;
-  __shared__ __align__(1024) unsigned char smem[4][kBytes];      // q and do, two tiles each
-  __shared__ float stats[2][2][kQueryStep];                      // lse and delta
+  constexpr bool kKeysInLds = D > 64;
+  constexpr int kQ = kKeysInLds ? 32 : 64, kBytes = kQ * Tl::kRowBytes;   // queries of a step
+  // q and do, two tiles each; the keys; what the dq kernel noted of each query, two steps'
+  constexpr int kKeysAt = 4 * kBytes, kStatsAt = kKeysAt + (kKeysInLds ? kKeyTile * Tl::kRowBytes : 0);
+  __shared__ __align__(1024) unsigned char smem[kStatsAt + 2 * 2 * 4 * kQ];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
-  int id = blockIdx.x;
-  const int per_head = a.sink_tiles * a.sink_parts + (tiles - a.sink_tiles) * a.tile_parts;
-  const int item = id % per_head; id /= per_head;
-  const int kv = id % a.kv_heads, b = id / a.kv_heads;
-  const int sink_items = a.sink_tiles * a.sink_parts;
-  const int parts = item < sink_items ? a.sink_parts : a.tile_parts;
-  const int tile = item < sink_items ? item / parts : a.sink_tiles + (item - sink_items) / parts;
-  const int part = (item < sink_items ? item : item - sink_items) % parts;
+  // an item of every head and sequence in turn; the longest first, and last the small parts of keys that all queries see
+  const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;
+  const int kv = unit % a.kv_heads, b = unit / a.kv_heads;
+  const int usual = (tiles - a.sink_tiles) * a.tile_parts;
+  const bool sink = item >= usual;
+  const int parts = sink ? a.sink_parts : a.tile_parts;
+  const int tile = sink ? (item - usual) / parts : a.sink_tiles + item / parts;
+  const int part = (sink ? item - usual : item) % parts;
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
   const int first = tile * kKeyTile;
@@ -145,13 +196,15 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionArgs a, 
   const bool there = key < sk.count;
   const char* k = rows_of(a.k, ragged, b, sk.first, kv);
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
-  x8<T> kf[D / 16], vf[D / 16];
+  x8<T> kf[kKeysInLds ? 1 : D / 16], vf[D / 16];
+  if constexpr (kKeysInLds)                                      // (waited for with the first step's tiles)
+    Loader<D, kKeyTile, 4>(wave, lane, a.k.token, a.dim).load(k + 2 * (int64_t)first * a.k.token, sk.count - first, (lds_byte*)smem + kKeysAt, wave);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
     const int d = 16 * s + 8 * half;
     const x8<T> z = {};
     const bool in = there && d < a.dim;
-    kf[s] = in ? *(const x8<T>*)(k + 2 * ((int64_t)key * a.k.token + d)) : z;
+    if constexpr (!kKeysInLds) kf[s] = in ? *(const x8<T>*)(k + 2 * ((int64_t)key * a.k.token + d)) : z;
     vf[s] = in ? *(const x8<T>*)(v + 2 * ((int64_t)key * a.v.token + d)) : z;
   }
   f32x16 dk[D / 32], dv[D / 32];
@@ -162,73 +215,85 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionArgs a, 
   const int tile_end = min(first + kKeyTile, sk.count) - 1;
   int end = sk.count - 1;
   if (a.window && first >= a.sinks) end = (int)min((int64_t)end, (int64_t)tile_end + a.window - 1);
-  const int q_begin = max(first - shift, 0) / kQueryStep;
-  const int q_steps = end - shift < 0 || first - shift >= sq.count ? 0 : (end - shift) / kQueryStep + 1 - q_begin;
+  const int q_begin = max(first - shift, 0) / kQ;
+  const int q_steps = end - shift < 0 || first - shift >= sq.count ? 0 : (end - shift) / kQ + 1 - q_begin;
   const int steps = max(q_steps, 0) * a.group;
   const int step0 = (int)((int64_t)steps * part / parts), step1 = (int)((int64_t)steps * (part + 1) / parts);
   const float c = a.scale * kLog2e;
 
-  const Loader<D, kQueryStep, 4> lq(wave, lane, a.q.token, a.dim), ld(wave, lane, a.d_o.token, a.dim);
+  const Loader<D, kQ, 4> lq(wave, lane, a.q.token, a.dim), ld(wave, lane, a.d_o.token, a.dim);
   lds_byte* base = (lds_byte*)smem;
-  float held = 0.f;                                              // lse or delta on its way to LDS, threads 0..127
-  auto load = [&](int t, int to) {
-    const int head = kv * a.group + t / q_steps, q0 = (q_begin + t % q_steps) * kQueryStep;
+  const TileReads<D> my(lane);
+  auto load = [&](int head, int q0, int to) {
     const char* q = rows_of(a.q, ragged, b, sq.first, head);
     const char* d_o = rows_of(a.d_o, ragged, b, sq.first, head);
     lq.load(q + 2 * (int64_t)q0 * a.q.token, sq.count - q0, base + (2 * to) * kBytes, wave);
     ld.load(d_o + 2 * (int64_t)q0 * a.d_o.token, sq.count - q0, base + (2 * to + 1) * kBytes, wave);
     const int64_t stat = ragged ? head * a.q_tokens + sq.first + q0 : ((int64_t)b * a.q_heads + head) * a.q_len + q0;
-    const int i = threadIdx.x & 63;
-    if (wave < 2) held = q0 + i < sq.count ? (wave == 0 ? a.lse_in : a.delta)[stat + i] : 0.f;
+    if (wave < 2 && lane < kQ) {
+      const float* from = (wave == 0 ? a.off : a.delta) + stat;
+      auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, 4 * min(max(sq.count - q0, 0), kQ), 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(base + kStatsAt + (2 * to + wave) * 4 * kQ), 4, 4 * lane, 0, 0, 0);
+    }
   };
-  if (step0 < step1) load(step0, 0);
+  int head = kv * a.group, q_at = q_begin;                       // of the step that is loaded next
+  if (step0 < step1) {
+    head += step0 / q_steps;
+    q_at += step0 % q_steps;
+  }
+  int q0 = q_at * kQ;
+  auto next = [&] { if (++q_at == q_begin + q_steps) { q_at = q_begin; ++head; } };
+  if (step0 < step1) { load(head, q0, 0); next(); }
   for (int t = step0; t < step1; ++t) {
     const int now = (t - step0) & 1;
-    if (wave < 2) stats[now][wave][threadIdx.x & 63] = wave == 0 ? held * kLog2e : held;
     wait_for_tiles();
-    if (t + 1 < step1) load(t + 1, now ^ 1);
-    const lds_byte* qt = base + (2 * now) * kBytes;
-    const lds_byte* dt = qt + kBytes;
-    const int q0 = (q_begin + t % q_steps) * kQueryStep;
+    const int q_now = q0;
+    if (t + 1 < step1) { q0 = q_at * kQ; load(head, q0, now ^ 1); next(); }
+    const uint32_t qt = lds_address(base) + (2 * now) * kBytes;
+    const uint32_t kt = lds_address(base) + kKeysAt + wave * 32 * Tl::kRowBytes;
+    const uint32_t stat = lds_address(base) + kStatsAt + now * (2 * 4 * kQ) + 16 * half;
     const int low = first + wave * 32, high = min(low + 31, sk.count - 1);   // this wavefront's keys
 #pragma unroll
-    for (int n = 0; n < kQueryStep / 32; ++n) {
-      const int p0 = q0 + n * 32 + shift;                        // position of the first of 32 queries
-      if (q0 + n * 32 >= sq.count || p0 + 31 < low || (a.window && low >= a.sinks && p0 - a.window >= high)) continue;
-      f32x16 s = (f32x16)(0.f), e = (f32x16)(0.f);
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        s = mma32(lds_rows<T>(qt + n * 32 * Tl::kRowBytes + Tl::rows_at(lane, i)), kf[i], s);
-        e = mma32(lds_rows<T>(dt + n * 32 * Tl::kRowBytes + Tl::rows_at(lane, i)), vf[i], e);
-      }
-      const bool whole = p0 >= low + 31 && q0 + n * 32 + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
-      const int ahead = p0 + 4 * half - key;                     // how far the first of this lane's queries is ahead of its key
-      const uint32_t window = a.window && key >= a.sinks ? (uint32_t)a.window : 0x80000000u;
+    for (int n = 0; n < kQ / 32; ++n) {
+      const int p0 = q_now + n * 32 + shift;                     // position of the first of 32 queries
+      if (q_now + n * 32 >= sq.count || p0 + 31 < low || (a.window && low >= a.sinks && p0 - a.window >= high)) continue;
+      f32x16 s, e;                                               // the products begin with what is taken off them
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
-        const f32x4 lse = *(const f32x4*)&stats[now][0][n * 32 + 2 * i + 4 * half], delta = *(const f32x4*)&stats[now][1][n * 32 + 2 * i + 4 * half];
+        const f32x4 x = lds_read4(stat + 4 * (n * 32 + 2 * i)), y = lds_read4(stat + 4 * (kQ + n * 32 + 2 * i));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x = __builtin_amdgcn_exp2f(fmaf(s[i + j], c, -lse[j])), y = x * (e[i + j] - delta[j]);
-          if (!whole) {
-            const bool visible = (uint32_t)(ahead + 2 * i + j) < window && q0 + n * 32 + 2 * i + 4 * half + j < sq.count;
-            x = visible ? x : 0.f;
-            y = visible ? y : 0.f;
-          }
-          s[i + j] = x;
-          e[i + j] = y;
+        for (int j = 0; j < 4; ++j) { s[i + j] = x[j]; e[i + j] = y[j]; }
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), kKeysInLds ? read_rows<T>(kt + my.rows, i, 0) : kf[kKeysInLds ? 0 : i], s);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
+      const bool whole = p0 >= low + 31 && q_now + n * 32 + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
+      if (!whole) {
+        const int ahead = p0 + 4 * half - key;                   // how far the first of this lane's queries is ahead of its key
+        const int left = sq.count - (q_now + n * 32 + 4 * half);
+        const uint32_t window = a.window && key >= a.sinks ? (uint32_t)a.window : 0x80000000u;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = 8 * (i / 4) + i % 4;
+          const bool visible = ((uint32_t)(ahead + j) < window) & (j < left);
+          s[i] = visible ? s[i] : 0.f;
+          e[i] = visible ? e[i] : 0.f;
         }
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[i] *= s[i];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
         const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
-        const lds_byte* at = dt + (n * 32 + 16 * u) * Tl::kRowBytes;
-        const lds_byte* qat = qt + (n * 32 + 16 * u) * Tl::kRowBytes;
 #pragma unroll
         for (int m = 0; m < D / 32; ++m) {
-          dv[m] = mma32(lds_columns<T>(at + Tl::columns_at(lane, m, 0), at + Tl::columns_at(lane, m, 1)), pf, dv[m]);
-          dk[m] = mma32(lds_columns<T>(qat + Tl::columns_at(lane, m, 0), qat + Tl::columns_at(lane, m, 1)), ds, dk[m]);
+          dv[m] = mma32(read_columns<T, D>(qt + my.columns, m, kBytes + (n * 32 + 16 * u) * Tl::kRowBytes), pf, dv[m]);
+          dk[m] = mma32(read_columns<T, D>(qt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes), ds, dk[m]);
         }
       }
     }

@@ -20,7 +20,7 @@ struct AttentionArgs {
   Operand q, k, v, o, d_o, dq, dk, dv;
   const float* lse_in;             // backward
   float* lse;                      // forward, may be null
-  float* delta;                    // backward: <do_i, o_i>, laid out as lse
+  float *off, *delta;              // backward, laid out as lse: -lse_i / scale and -sum_j P(i,j) <do_i, v_j>
   float* parts;                    // backward: sums of the parts of a key tile, dk then dv of each
   const int32_t *q_offsets, *k_offsets;
   int64_t q_tokens, k_tokens;
