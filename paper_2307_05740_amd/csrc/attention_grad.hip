@@ -9,21 +9,19 @@
 namespace arrow {
 namespace {
 
-constexpr int kStep = 64;   // keys of a tile (dq)
-
 // dq, and D_i = sum_j P(i,j) <do_i, v_j> for the other kernel.  As the forward kernel: a wavefront holds 32 queries, scores and their gradients
 // are transposed, dS^T is at once the B operand of dQ^T += K^T dS^T.
 //
 // D is <do_i, o_i> as well, but o has been rounded, and where a row has one large probability dS is a small difference of <do_i, v_j>
-// and D: the sum over the row's keys is exact to 32 bits.  Two ways to have it, both measured (TODO):
-//  - heads of up to 64: dS is formed with <do_i, o_i>, whose error e = -sum_j dS(i,j) comes out with the row, and dq is put right
-//    with e sum_j P(i,j) k_j, one product more;
-//  - larger heads, whose sums leave no registers for those of P K: the row is gone through twice, first for D alone.
+// and D.  dS is formed with <do_i, o_i>; its error e = -sum_j dS(i,j) comes out with the row, in 32 bits, and dq is put right with
+// e sum_j P(i,j) k_j, one product more.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
-  constexpr bool kTwice = D > 64;
-  __shared__ __align__(1024) unsigned char smem[4][kStep * Tl::kRowBytes];
+  constexpr bool kQueriesInLds = D > 64;                         // no registers are left for them
+  constexpr int kStep = kQueriesInLds ? 32 : 64, kBytes = kStep * Tl::kRowBytes;   // keys of a tile
+  constexpr int kQueriesAt = 4 * kBytes;                         // k and v, two tiles each; the queries
+  __shared__ __align__(1024) unsigned char smem[kQueriesAt + (kQueriesInLds ? kQueryTile * Tl::kRowBytes : 0)];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   int id = blockIdx.x;
   const int g = id % a.group; id /= a.group;
@@ -42,25 +40,26 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
   const char* o = rows_of(a.o, ragged, b, sq.first, head);
   const char* d_o = rows_of(a.d_o, ragged, b, sq.first, head);
+  lds_byte* base = (lds_byte*)smem;
 
-  x8<T> qf[D / 16], df[D / 16];
+  x8<T> qf[kQueriesInLds ? 1 : D / 16], df[D / 16];
+  if constexpr (kQueriesInLds)                                   // (waited for with the first tiles)
+    Loader<D, kQueryTile, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, base + kQueriesAt, wave);
   float delta = 0.f;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
     const int d = 16 * s + 8 * half;
     const x8<T> z = {};
     const bool in = there && d < a.dim;
-    qf[s] = in ? *(const x8<T>*)(q + 2 * ((int64_t)row * a.q.token + d)) : z;
+    if constexpr (!kQueriesInLds) qf[s] = in ? *(const x8<T>*)(q + 2 * ((int64_t)row * a.q.token + d)) : z;
     df[s] = in ? *(const x8<T>*)(d_o + 2 * ((int64_t)row * a.d_o.token + d)) : z;
-    if constexpr (!kTwice) {
-      const x8<T> of = in ? *(const x8<T>*)(o + 2 * ((int64_t)row * a.o.token + d)) : z;
+    const x8<T> of = in ? *(const x8<T>*)(o + 2 * ((int64_t)row * a.o.token + d)) : z;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) delta = fmaf((float)df[s][i], (float)of[i], delta);
-    }
+    for (int i = 0; i < 8; ++i) delta = fmaf((float)df[s][i], (float)of[i], delta);
   }
-  if constexpr (!kTwice) delta = add_halves(delta);
+  delta = add_halves(delta);
   const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
-  // of a row that sees nothing, -infinity: its probabilities are masked
+  // of a row that sees nothing, infinity: its probabilities are masked
   const float off = there ? -a.lse_in[stat] / a.scale : 0.f;
 
   const int last = min(first + kQueryTile, sq.count) - 1 + shift;
@@ -69,99 +68,74 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
   const float c = a.scale * kLog2e;
 
   const Loader<D, kStep, 4> lk(wave, lane, a.k.token, a.dim), lv(wave, lane, a.v.token, a.dim);
-  lds_byte* base = (lds_byte*)smem;
   const TileReads<D> my(lane);
   auto load = [&](int t, int to) {
     const int k0 = seen.at(t) * kStep;
-    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * (kStep * Tl::kRowBytes), wave);
-    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * (kStep * Tl::kRowBytes), wave);
+    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * kBytes, wave);
+    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, wave);
   };
-  // over all tiles, for 32 keys at a time: each(where their tile's columns are read, how far into it they begin, P^T, (<do, v> - delta)^T)
-  auto all_tiles = [&](auto&& each) {
-    if (seen.total > 0) load(0, 0);
-    for (int t = 0; t < seen.total; ++t) {
-      wait_for_tiles();
-      if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
-      const uint32_t kt = lds_address(base) + (2 * (t & 1)) * (kStep * Tl::kRowBytes), vt = kt + kStep * Tl::kRowBytes;
-      const int k0 = seen.at(t) * kStep;
-      if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
-      const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
-      const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
-      const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
+  f32x16 acc[D / 32], pk[D / 32];                             // dS K and P K
 #pragma unroll
-      for (int n = 0; n < kStep / 32; ++n) {
-        f32x16 s = (f32x16)(off), e = (f32x16)(-delta);       // the products begin with what is taken off them
+  for (int m = 0; m < D / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
+  float rest = 0.f;                                           // sum of dS of this lane's keys
+  if (seen.total > 0) load(0, 0);
+  for (int t = 0; t < seen.total; ++t) {
+    wait_for_tiles();
+    if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
+    const uint32_t kt = lds_address(base) + (2 * (t & 1)) * kBytes, vt = kt + kBytes, qt = lds_address(base) + kQueriesAt + wave * 32 * Tl::kRowBytes;
+    const int k0 = seen.at(t) * kStep;
+    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
+    const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
+    const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
+    const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s);
-          e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
+    for (int n = 0; n < kStep / 32; ++n) {
+      f32x16 s = (f32x16)(off), e = (f32x16)(-delta);         // the products begin with what is taken off them
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt + my.rows, i, 0) : qf[kQueriesInLds ? 0 : i], s);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = n * 32 + 8 * (i / 4) + i % 4;
+          const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
+          s[i] = visible ? s[i] : 0.f;
+          e[i] = visible ? e[i] : 0.f;
         }
+      }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
-        if (!whole) {
+      for (int i = 0; i < 16; ++i) {
+        e[i] *= s[i];
+        rest += e[i];
+      }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = n * 32 + 8 * (i / 4) + i % 4;
-            const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
-            s[i] = visible ? s[i] : 0.f;
-            e[i] = visible ? e[i] : 0.f;
-          }
+      for (int u = 0; u < 2; ++u) {
+        const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
+        const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) {
+          const x8<T> kf = read_columns<T, D>(kt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes);
+          acc[m] = mma32(kf, ds, acc[m]);
+          pk[m] = mma32(kf, pf, pk[m]);
         }
-        each(kt + my.columns, n * 32 * Tl::kRowBytes, s, e);
       }
     }
-  };
+  }
 
-  float rest = 0.f;                                           // of this lane's keys: sum of dS, or D
-  if constexpr (kTwice) {
-    all_tiles([&](uint32_t, int, const f32x16& s, const f32x16& e) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) rest = fmaf(s[i], e[i], rest);
-    });
-    delta = add_halves(rest);
-    __syncthreads();                                          // the next loads go where the last tiles are read
-  }
-  f32x16 acc[D / 32], pk[kTwice ? 1 : D / 32];
-#pragma unroll
-  for (int m = 0; m < D / 32; ++m) {
-    acc[m] = (f32x16)(0.f);
-    if constexpr (!kTwice) pk[m] = (f32x16)(0.f);
-  }
-  all_tiles([&](uint32_t kt, int skip, const f32x16& s, f32x16& e) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      e[i] *= s[i];
-      if constexpr (!kTwice) rest += e[i];
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
-      x8<T> pf;
-      if constexpr (!kTwice) pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
-#pragma unroll
-      for (int m = 0; m < D / 32; ++m) {
-        const x8<T> kf = read_columns<T, D>(kt, m, skip + 16 * u * Tl::kRowBytes);
-        acc[m] = mma32(kf, ds, acc[m]);
-        if constexpr (!kTwice) pk[m] = mma32(kf, pf, pk[m]);
-      }
-    }
-  });
-
-  if constexpr (!kTwice) {
-    rest = add_halves(rest);
-    delta += rest;
-#pragma unroll
-    for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[m][i] = fmaf(-rest, pk[m][i], acc[m][i]);
-  }
+  rest = add_halves(rest);
   if (there && half == 0) {
     a.off[stat] = off;
-    a.delta[stat] = -delta;
+    a.delta[stat] = -(delta + rest);
   }
   T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m) acc[m] *= a.scale;
+  for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-rest, pk[m][i], acc[m][i]);
   if (there) store_columns<T, D>(acc, dq, half, a.dim);
 }
 
