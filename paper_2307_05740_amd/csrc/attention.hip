@@ -98,6 +98,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       for (int i = 0; i < D / 16; ++i)
         s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
     }
+    reads_ahead<6, (kStep / 32) * (D / 16), 1>();
     // every query sees every key: nothing to mask
     const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
     if (!whole) {
@@ -147,6 +148,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 #pragma unroll
       for (int m = 0; m < D / 32; ++m)
         acc[m] = mma32(read_columns<T, D>(vt + my.columns, m, 16 * u * Tl::kRowBytes), pf[u], acc[m]);
+    reads_ahead<8, (kStep / 16) * (D / 32), 2>();
   }
 
   total = add_halves(total);

@@ -205,6 +205,24 @@ __device__ __forceinline__ int64_t part_place(const AttentionArgs& a, int tiles,
   return unit * per_unit + (tile < a.sink_tiles ? tile * a.sink_parts : lead + (tile - a.sink_tiles) * a.tile_parts) + part;
 }
 
+// The order of a block's instructions: kAhead LDS reads first, then kPer of them for each of kProducts matrix instructions, and the same for a second
+// kind of products, so that a product's operands are on their way while earlier ones run.  (By itself the compiler reads one operand
+// at a time and waits for it.)
+template <int kAhead, int kProducts, int kPer, int kProducts2 = 0, int kPer2 = 0>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int kReads = kProducts * kPer + kProducts2 * kPer2;
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < kProducts + kProducts2; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    const int done = kAhead + (i < kProducts ? i * kPer : kProducts * kPer + (i - kProducts) * kPer2);
+    if (done < kReads) {
+      if (i < kProducts) __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);
+      else __builtin_amdgcn_sched_group_barrier(0x100, kPer2, 0);
+    }
+  }
+}
+
 __device__ __forceinline__ void wait_for_tiles() {
   // (the builtins of loads to LDS count as vector memory)
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");

@@ -96,6 +96,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
         s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt + my.rows, i, 0) : qf[kQueriesInLds ? 0 : i], s);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
+      reads_ahead<4, D / 16, kQueriesInLds ? 2 : 1, D / 16, 1>();
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
       if (!whole) {
@@ -123,6 +124,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
           pk[m] = mma32(kf, pf, pk[m]);
         }
       }
+      reads_ahead<4, 4 * (D / 32), 1>();
     }
   }
 
@@ -243,6 +245,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
         s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), kKeysInLds ? read_rows<T>(kt + my.rows, i, 0) : kf[kKeysInLds ? 0 : i], s);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
+      reads_ahead<kKeysInLds ? 16 : 12, D / 16, kKeysInLds ? 2 : 1, D / 16, 1>();   // (eight of those ahead: what the products begin with)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
       const bool whole = p0 >= low + 31 && q_now + n * 32 + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
@@ -270,6 +273,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
           dk[m] = mma32(read_columns<T, D>(qt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes), ds, dk[m]);
         }
       }
+      reads_ahead<kKeysInLds ? 8 : 4, 4 * (D / 32), 2>();
     }
   }
 
