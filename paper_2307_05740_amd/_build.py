@@ -89,7 +89,7 @@ def build_call() -> str:
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", sysconfig.get_paths()["include"],
           "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-          "-isystem", rocm_inc, os.path.join(PKG_DIR, "csrc", "tensor_call.cpp"), "-L", os.path.join(root, "lib"),
+          "-isystem", rocm_inc, "-I", os.path.join(REPO_DIR, "include"), os.path.join(PKG_DIR, "csrc", "tensor_call.cpp"), "-L", os.path.join(root, "lib"),
           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-o", CALL_LIB])
     return CALL_LIB
 

@@ -26,6 +26,13 @@ def _address(t) -> int:
     return t.data_ptr() if t is not None else 0
 
 
+def _results(done):
+    """What a native call gave: results, or the library's error code."""
+    if type(done) is int:
+        binding._check(done)
+    return done
+
+
 class ArrowAttention:
     """A mask (``window`` keys back, 0 = all earlier ones, and the first ``sinks`` keys) and a scale of the scores, by
     default 1 / sqrt(size of a head)."""
@@ -37,6 +44,15 @@ class ArrowAttention:
         self.window, self.sinks, self.scale = int(window), int(sinks), scale
         if self.window < 0 or self.sinks < 0:
             raise ValueError("window and sinks are not negative")
+        # The plain case, tensors that are what they have to be, is looked over and started in native code (csrc/tensor_call.cpp); it
+        # says None to anything else, which then goes the way below and is reported there.
+        self._call = binding._tensor_call(self.device)
+        mask = (self.device.index, min(self.window, 2**31 - 1), min(self.sinks, 2**31 - 1), -1.0 if scale is None else max(0.0, float(scale)))
+        address = lambda name: binding._address(getattr(lib(), name))   # noqa: E731
+        if self._call is not None:
+            self._forward = (address("arrow_attention_forward"), *mask)
+            self._backward = (address("arrow_attention_backward"), address("arrow_attention_workspace_bytes"), *mask)
+            self._decode = (address("arrow_attention_decode"), address("arrow_attention_decode_workspace_bytes"), *mask)
 
     def _stream(self) -> int:
         return binding._current_stream(self._torch, self.device)
@@ -106,6 +122,10 @@ class ArrowAttention:
         """``(o, lse)``.  q: (batch, tokens, heads, dim), k and v: (batch, keys, key heads, dim); or, with int32 offsets of
         batch + 1 values each, (tokens of all sequences, heads, dim), of which no sequence has more than q_len (k_len).
         lse: float32, (batch, heads, tokens), or (heads, tokens of all sequences)."""
+        if self._call is not None:
+            done = self._call.attention_forward(*self._forward, q, k, v, o, lse, q_offsets, k_offsets, q_len, k_len)
+            if done is not None:
+                return _results(done)
         torch = self._torch
         a = self._describe(q, k, v, q_offsets, k_offsets, q_len, k_len)
         if o is None:
@@ -123,6 +143,10 @@ class ArrowAttention:
 
     def backward(self, d_o, q, k, v, o, lse, dq=None, dk=None, dv=None, q_offsets=None, k_offsets=None, q_len=None, k_len=None):
         """``(dq, dk, dv)`` for the gradient d_o of the o that ``forward`` gave for these arguments together with lse."""
+        if self._call is not None:
+            done = self._call.attention_backward(*self._backward, d_o, q, k, v, o, lse, dq, dk, dv, q_offsets, k_offsets, q_len, k_len)
+            if done is not None:
+                return _results(done)
         torch = self._torch
         a = self._describe(q, k, v, q_offsets, k_offsets, q_len, k_len)
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
@@ -187,6 +211,10 @@ class ArrowAttention:
         """o of one query per sequence, q: (batch, heads, dim), at the last of its lengths[b] positions (0: an idle sequence).  k and v,
         (batch, key heads, dim): the new token's, written to their place first; without them they are there already.
         max_len: the longest length; only how the work is split goes by it."""
+        if self._call is not None:
+            done = self._call.attention_decode(*self._decode, q, k_cache, v_cache, table, lengths, max_len, k, v, o)
+            if done is not None:
+                return _results(done)
         torch = self._torch
         if q.dim() != 3:
             raise ValueError(f"q {tuple(q.shape)}: (batch, heads, dim) expected")

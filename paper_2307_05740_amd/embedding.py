@@ -10,6 +10,7 @@ import ctypes
 import math
 
 from . import binding
+from .attention import _results
 from .binding import arrow_embedding_t, lib
 
 
@@ -23,6 +24,12 @@ class ArrowEmbedding:
         self.rows, self.scale = int(rows), float(scale)
         if self.rows < 1:
             raise ValueError("a table has rows")
+        # the plain case goes by native code, as in attention.py
+        self._call = binding._tensor_call(self.device)
+        if self._call is not None:
+            address = lambda name: binding._address(getattr(lib(), name))   # noqa: E731
+            self._forward = (address("arrow_embedding_forward"), self.device.index, self.rows, self.scale)
+            self._backward = (address("arrow_embedding_backward"), address("arrow_embedding_workspace_bytes"), self.device.index, self.rows, self.scale)
         self._dtypes = {torch.float32: binding.ARROW_F32, torch.bfloat16: binding.ARROW_BF16, torch.float16: binding.ARROW_F16}
 
     def _stream(self) -> int:
@@ -55,6 +62,10 @@ class ArrowEmbedding:
 
     def forward(self, W, ids, Y=None):
         """Y, (shape of ids, columns), of W (rows, columns)."""
+        if self._call is not None:
+            done = self._call.embedding_forward(*self._forward, W, ids, Y)
+            if done is not None:
+                return _results(done)
         torch = self._torch
         shape = (*ids.shape, W.shape[-1])
         Y = torch.empty(shape, dtype=W.dtype, device=W.device) if Y is None else Y
@@ -68,6 +79,10 @@ class ArrowEmbedding:
 
     def backward(self, dY, ids, dW=None, dtype=None):
         """dW, (rows, columns), of dY (shape of ids, columns): every row is written.  dtype: dY's (the default) or float32."""
+        if self._call is not None and dtype is None:
+            done = self._call.embedding_backward(*self._backward, dY, ids, dW)
+            if done is not None:
+                return _results(done)
         torch = self._torch
         if tuple(dY.shape[:-1]) != tuple(ids.shape) or dY.dim() < 2:
             raise ValueError(f"dY {tuple(dY.shape)} of ids {tuple(ids.shape)}")
