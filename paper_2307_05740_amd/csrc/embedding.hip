@@ -163,6 +163,115 @@ __global__ __launch_bounds__(64) void sort_move_kernel(SortArgs s) {
   }
 }
 
+// The sort of a digit in one launch, for few tokens: every workgroup counts all of them, those before its own 1024 in the upper half of
+// a word, and so knows where its tokens go.  16,384 tokens of 32,000 rows: TODO us, where the three launches above take TODO, twice.
+constexpr int kSortBlock = 1024;
+
+__global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32_t* row_begin, uint32_t* row_end) {
+  __shared__ __align__(16) uint32_t bins[1 << kWideDigitBits];
+  __shared__ uint32_t sums[kSortBlock / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, values = 1 << s.bits, mask = values - 1;
+  // four values to a place; threads that go through neighbouring places do not meet in a bank
+  auto place = [](uint32_t b) { return b ^ ((b >> 5 & 7) << 2); };
+  for (int i = 4 * threadIdx.x; i < values; i += 4 * kSortBlock) *(uint4*)&bins[i] = uint4{0, 0, 0, 0};
+  const int n = (int)s.n, own = (int)blockIdx.x * kSortBlock, t = own + threadIdx.x;
+  const bool in = t < n;
+  uint32_t key = 0;
+  constexpr int kBatch = 8;
+  for (int begin = 0; begin < n; begin += kBatch * kSortBlock) {     // (as often for every thread: there is a barrier in it)
+    const int t0 = begin + threadIdx.x;
+    uint32_t x[kBatch];
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) x[r] = t0 + r * kSortBlock < n ? key_at(s, t0 + r * kSortBlock) : 0;
+    if (begin == 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      const int at = t0 + r * kSortBlock;
+      if (at < n) atomicAdd(&bins[place((x[r] >> s.shift) & mask)], at < own ? 0x10001u : 1u);
+      if (at == t) key = x[r];
+    }
+  }
+  __syncthreads();
+  // where each value begins: all tokens of smaller ones, and its own before this workgroup's
+  const int each = (values + kSortBlock - 1) / kSortBlock, first = threadIdx.x * each;
+  uint32_t count = 0;
+  if (each < 4) {
+    for (int i = first; i < first + each && i < values; ++i) count += bins[place(i)] & 0xffff;
+  } else {
+#pragma unroll 4
+    for (int i = first; i < first + each; i += 4) {
+      const uint4 x = *(const uint4*)&bins[place(i)];
+      count += (x.x & 0xffff) + (x.y & 0xffff) + (x.z & 0xffff) + (x.w & 0xffff);
+    }
+  }
+  uint32_t upto = count;
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint32_t x = __shfl_up(upto, m, 64);
+    if (lane >= m) upto += x;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  uint32_t base = upto - count;
+  for (int w = 0; w < wave; ++w) base += sums[w];
+  const bool note = row_begin && threadIdx.x % gridDim.x == blockIdx.x;   // the only digit: a value is a row
+  if (each < 4) {
+    for (int i = first; i < first + each && i < values; ++i) {
+      const uint32_t x = bins[place(i)];
+      if (note && i < s.rows) { row_begin[i] = base; row_end[i] = base + (x & 0xffff); }
+      bins[place(i)] = base + (x >> 16);
+      base += x & 0xffff;
+    }
+  } else {
+    for (int i = first; i < first + each; i += 4) {
+      const uint4 x = *(const uint4*)&bins[place(i)];
+      const uint4 at = {base, base + (x.x & 0xffff), base + (x.x & 0xffff) + (x.y & 0xffff), base + (x.x & 0xffff) + (x.y & 0xffff) + (x.z & 0xffff)};
+      base = at.w + (x.w & 0xffff);
+      *(uint4*)&bins[place(i)] = uint4{at.x + (x.x >> 16), at.y + (x.y >> 16), at.z + (x.z >> 16), at.w + (x.w >> 16)};
+      if (!note) continue;
+      if (i + 3 < s.rows) {
+        *(uint4*)&row_begin[i] = at;
+        *(uint4*)&row_end[i] = uint4{at.y, at.z, at.w, base};
+      } else {
+        const uint32_t b[5] = {at.x, at.y, at.z, at.w, base};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (i + j < s.rows) { row_begin[i + j] = b[j]; row_end[i + j] = b[j + 1]; }
+      }
+    }
+  }
+  __syncthreads();
+  // this workgroup's tokens, in order: the lanes of a wavefront with one value, one wavefront after the other
+  const uint32_t digit = (key >> s.shift) & mask;
+  uint64_t same = __ballot(in);
+  for (int b = 0; b < s.bits; ++b) {
+    const uint64_t set = __ballot(digit >> b & 1);
+    same &= digit >> b & 1 ? set : ~set;
+  }
+  const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
+  uint32_t at = 0;
+  for (int w = 0; w < kSortBlock / 64 && own + w * 64 < n; ++w) {
+    if (w == wave && in) {
+      at = bins[place(digit)];
+      if (before == 0) bins[place(digit)] = at + __popcll(same);
+    }
+    __syncthreads();
+  }
+  if (in) {
+    s.to_keys[at + before] = key;
+    s.to_tokens[at + before] = s.tokens ? s.tokens[t] : (uint32_t)t;
+  }
+}
+
+// Where rows begin and end among the sorted tokens.
+__global__ __launch_bounds__(256) void sort_rows_kernel(const uint32_t* keys, int64_t n, int64_t rows, uint32_t* begin, uint32_t* end) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const uint32_t key = keys[i];
+  if (key >= rows) return;
+  if (i == 0 || keys[i - 1] != key) begin[key] = (uint32_t)i;
+  if (i + 1 == n || keys[i + 1] != key) end[key] = (uint32_t)(i + 1);
+}
+
 // ---- sums ----
 
 struct SumArgs {
@@ -174,41 +283,34 @@ struct SumArgs {
   int columns, pieces, lanes_log;
 };
 
-// Adds up the rows of dY of the sorted tokens lo .. hi - 1, one piece of columns; four rows on their way at a time.
+// Adds up the rows of dY of the sorted tokens lo .. hi - 1, one piece of columns, in order; eight rows on their way at a time.
 template <typename T, int VEC>
 __device__ __forceinline__ void add_rows(const SumArgs& a, const T* dY, int64_t lo, int64_t hi, int c, float (&sum)[VEC]) {
-  int64_t i = lo;
-  for (; i + 4 <= hi; i += 4) {
-    float x[4][VEC];
+  constexpr int kAhead = 8;
+  for (int64_t i = lo; i < hi; i += kAhead) {
+    typename Columns<T, VEC>::type x[kAhead];
+    const int64_t last = hi - 1;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) load<T, VEC>(dY + a.tokens[i + r] * a.y_stride + c, x[r]);
+    for (int r = 0; r < kAhead; ++r) x[r] = *(const typename Columns<T, VEC>::type*)(dY + a.tokens[i + r < hi ? i + r : last] * a.y_stride + c);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < kAhead; ++r)
+      if (i + r < hi) {
+        if constexpr (VEC == 1) sum[0] += (float)x[r];
+        else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[j] += x[r][j];
-  }
-  for (; i < hi; ++i) {
-    float x[VEC];
-    load<T, VEC>(dY + a.tokens[i] * a.y_stride + c, x);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] += x[j];
+          for (int j = 0; j < VEC; ++j) sum[j] += (float)x[r][j];
+        }
+      }
   }
 }
 
-// Chunk i, columns 256 VEC of it: notes where rows begin and end among the sorted tokens, and sums its part of rows that go on
-// beyond it, one that began before it into partial row 2 i, one that begins in it into 2 i + 1.
+// Chunk i of the sorted tokens, 256 VEC columns of it: sums its part of rows that go on beyond it, one that began before it into partial row
+// 2 i, one that begins in it into 2 i + 1.
 template <typename T, int VEC>
-__global__ __launch_bounds__(256) void embedding_chunk_kernel(SumArgs a, const T* dY) {
-  const int64_t lo = blockIdx.x * a.chunk, hi = lo + a.chunk < a.n ? lo + a.chunk : a.n;
-  if (blockIdx.y == 0)
-    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
-      const uint32_t key = a.keys[i];
-      if (key >= a.rows) continue;
-      if (i == 0 || a.keys[i - 1] != key) a.begin[key] = (uint32_t)i;
-      if (i + 1 == a.n || a.keys[i + 1] != key) a.end[key] = (uint32_t)(i + 1);
-    }
+__device__ __forceinline__ void add_chunk(const SumArgs& a, const T* dY, int64_t chunk, int slice) {
+  const int64_t lo = chunk * a.chunk, hi = lo + a.chunk < a.n ? lo + a.chunk : a.n;
   const uint32_t first = a.keys[lo], last = a.keys[hi - 1];
-  const int piece = blockIdx.y * 256 + threadIdx.x;
+  const int piece = slice * 256 + threadIdx.x;
   if (piece >= a.pieces) return;
   const int c = VEC == 1 ? piece : min(piece * VEC, a.columns - VEC);
   if (first < a.rows && lo > 0 && a.keys[lo - 1] == first) {        // began before: up to where it ends, or the chunk does
@@ -221,7 +323,7 @@ __global__ __launch_bounds__(256) void embedding_chunk_kernel(SumArgs a, const T
     float sum[VEC] = {};
     add_rows<T, VEC>(a, dY, lo, to, c, sum);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) a.parts[(2 * (int64_t)blockIdx.x) * a.padded + piece * VEC + j] = sum[j];
+    for (int j = 0; j < VEC; ++j) a.parts[2 * chunk * a.padded + piece * VEC + j] = sum[j];
   }
   const bool began_before = lo > 0 && a.keys[lo - 1] == last;
   if (last < a.rows && hi < a.n && a.keys[hi] == last && !began_before) {
@@ -230,51 +332,82 @@ __global__ __launch_bounds__(256) void embedding_chunk_kernel(SumArgs a, const T
     float sum[VEC] = {};
     add_rows<T, VEC>(a, dY, l, hi, c, sum);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) a.parts[(2 * (int64_t)blockIdx.x + 1) * a.padded + piece * VEC + j] = sum[j];
+    for (int j = 0; j < VEC; ++j) a.parts[(2 * chunk + 1) * a.padded + piece * VEC + j] = sum[j];
   }
 }
 
-constexpr int kTableRows = 8;      // rows of dW of a lane group
+constexpr int kTableRows = 8;      // rows of dW of a lane group, four on their way at a time
 
-// Every row of dW: zero, the sum of its tokens' rows, or of its partial rows.  begin[] and end[] hold what they will for
-// rows without tokens: a row has tokens only where the sorted ids say so.
-template <typename T, typename G, int VEC>
-__global__ __launch_bounds__(256) void embedding_rows_kernel(SumArgs a, const T* dY, G* dW) {
+// The rows of dW that lie within a chunk: zero, or the sum of their tokens' rows; and, by the first workgroups, the parts of the others.
+// kNoted: begin[] and end[] hold what they will for rows without tokens, and a row has some only where the sorted ids say so.
+template <typename T, typename G, int VEC, bool kNoted>
+__global__ __launch_bounds__(256) void embedding_rows_kernel(SumArgs a, const T* dY, G* dW, int chunk_blocks, int slices) {
+  if ((int)blockIdx.x < chunk_blocks) return add_chunk<T, VEC>(a, dY, blockIdx.x / slices, blockIdx.x % slices);
   __shared__ uint32_t begins[256 * kTableRows], ends[256 * kTableRows];
   const int lane = threadIdx.x & ((1 << a.lanes_log) - 1), in = threadIdx.x >> a.lanes_log, abreast = 256 >> a.lanes_log;
-  const int64_t row0 = (int64_t)blockIdx.x * abreast * kTableRows;
+  const int64_t row0 = (int64_t)(blockIdx.x - chunk_blocks) * abreast * kTableRows;
   for (int r = threadIdx.x; r < abreast * kTableRows; r += 256) {
     const int64_t row = row0 + r;
     uint32_t lo = 0, hi = 0;
     if (row < a.rows && a.n > 0) {
-      const uint32_t at = a.begin[row];
-      if (at < a.n && a.keys[at] == (uint32_t)row && (at == 0 || a.keys[at - 1] != (uint32_t)row)) { lo = at; hi = a.end[row]; }
+      lo = a.begin[row];
+      hi = a.end[row];
+      if (!kNoted && !(lo < a.n && a.keys[lo] == (uint32_t)row && (lo == 0 || a.keys[lo - 1] != (uint32_t)row))) hi = lo = 0;
     }
     begins[r] = lo;
     ends[r] = hi;
   }
   __syncthreads();
-  for (int r = in; r < abreast * kTableRows; r += abreast) {
-    const int64_t row = row0 + r;
-    if (row >= a.rows) return;
-    const int64_t lo = begins[r], hi = ends[r], c0 = lo / a.chunk, c1 = hi > lo ? (hi - 1) / a.chunk : c0;
+  for (int r0 = in; r0 < abreast * kTableRows; r0 += 4 * abreast) {
+    int64_t lo[4], hi[4], first[4];
+    bool mine[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      lo[r] = begins[r0 + r * abreast];
+      hi[r] = ends[r0 + r * abreast];
+      mine[r] = row0 + r0 + r * abreast < a.rows && (lo[r] == hi[r] || lo[r] / a.chunk == (hi[r] - 1) / a.chunk);
+      first[r] = mine[r] && lo[r] < hi[r] ? (int64_t)a.tokens[lo[r]] * a.y_stride : -1;
+    }
     for (int piece = lane; piece < a.pieces; piece += 1 << a.lanes_log) {
       const int c = VEC == 1 ? piece : min(piece * VEC, a.columns - VEC);
-      float sum[VEC] = {};
-      if (c0 == c1) {
-        add_rows<T, VEC>(a, dY, lo, hi, c, sum);
-      } else {
-        for (int64_t i = c0; i <= c1; ++i) {
-          const float* from = a.parts + (2 * i + (i == c0)) * a.padded + piece * VEC;
+      float sum[4][VEC] = {};
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) sum[j] += from[j];
-        }
+      for (int r = 0; r < 4; ++r)
+        if (first[r] >= 0) load<T, VEC>(dY + first[r] + c, sum[r]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (!mine[r]) continue;
+        if (hi[r] - lo[r] > 1) add_rows<T, VEC>(a, dY, lo[r] + 1, hi[r], c, sum[r]);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[r][j] *= a.scale;
+        store<G, VEC>(dW + (row0 + r0 + r * abreast) * a.w_stride + c, sum[r]);
       }
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[j] *= a.scale;
-      store<G, VEC>(dW + row * a.w_stride + c, sum);
     }
   }
+}
+
+// The rows that go over the end of a chunk, each by the end that it goes over first: their partial rows added up in order.
+template <typename G, int VEC>
+__global__ __launch_bounds__(64) void embedding_join_kernel(SumArgs a, G* dW) {
+  const int64_t chunk = blockIdx.x, edge = (chunk + 1) * a.chunk;    // (there is a token at the edge)
+  const uint32_t row = a.keys[edge];
+  if (row >= a.rows || a.keys[edge - 1] != row) return;
+  const int64_t lo = a.begin[row], last = (a.end[row] - 1) / a.chunk;
+  if (lo < chunk * a.chunk) return;
+  const int piece = blockIdx.y * 64 + threadIdx.x;
+  if (piece >= a.pieces) return;
+  const int c = VEC == 1 ? piece : min(piece * VEC, a.columns - VEC);
+  float sum[VEC] = {};
+  const float* from = a.parts + piece * VEC;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] = from[(2 * chunk + 1) * a.padded + j];
+#pragma unroll 8
+  for (int64_t i = chunk + 1; i <= last; ++i)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += from[2 * i * a.padded + j];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] *= a.scale;
+  store<G, VEC>(dW + row * a.w_stride + c, sum);
 }
 
 int log2_up(int64_t x, int most) {
@@ -295,6 +428,7 @@ template <typename T, typename G, int VEC>
 int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY, const void* ids, void* dW, void* ws, hipStream_t s) {
   auto at = [&](size_t offset) { return (uint32_t*)((char*)ws + offset); };
   int now = 0;
+  const bool noted = p.few && p.passes == 1;
   for (int i = 0; i < p.passes && e.tokens; ++i) {
     SortArgs a{};
     a.ids = i == 0 ? ids : nullptr;
@@ -307,6 +441,10 @@ int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY,
     a.counts = at(p.counts);
     a.n = e.tokens; a.block_tokens = p.block_tokens; a.blocks = p.blocks; a.rows = e.rows;
     a.shift = i * p.bits; a.bits = p.bits;
+    if (p.few) {
+      sort_few_kernel<<<dim3((unsigned)((e.tokens + kSortBlock - 1) / kSortBlock)), dim3(kSortBlock), 0, s>>>(a, noted ? at(p.begin) : nullptr, at(p.end));
+      continue;
+    }
     sort_count_kernel<<<dim3((unsigned)p.blocks), dim3(64), 0, s>>>(a);
     sort_scan_kernel<<<dim3(1), dim3(1024), 0, s>>>(a.counts, p.blocks << p.bits);
     sort_move_kernel<<<dim3((unsigned)p.blocks), dim3(64), 0, s>>>(a);
@@ -317,9 +455,15 @@ int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY,
   a.parts = (float*)at(p.parts);
   a.n = e.tokens; a.chunk = p.chunk; a.padded = p.padded; a.rows = e.rows; a.w_stride = e.w_stride; a.y_stride = e.y_stride;
   a.scale = e.scale; a.columns = e.columns; a.pieces = (e.columns + VEC - 1) / VEC; a.lanes_log = log2_up(a.pieces, 8);
-  if (e.tokens) embedding_chunk_kernel<T, VEC><<<dim3((unsigned)p.chunks, (unsigned)((a.pieces + 255) / 256)), dim3(256), 0, s>>>(a, (const T*)dY);
-  const int64_t rows = (256 >> a.lanes_log) * kTableRows, blocks = (e.rows + rows - 1) / rows;
-  embedding_rows_kernel<T, G, VEC><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, (const T*)dY, (G*)dW);
+  if (e.tokens && !noted) sort_rows_kernel<<<dim3((unsigned)((e.tokens + 255) / 256)), dim3(256), 0, s>>>(a.keys, a.n, a.rows, a.begin, a.end);
+  const int slices = (a.pieces + 255) / 256;
+  const int64_t chunk_blocks = p.chunks > 1 ? p.chunks * slices : 0;
+  const int64_t rows = (256 >> a.lanes_log) * kTableRows, blocks = chunk_blocks + (e.rows + rows - 1) / rows;
+  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  if (noted) embedding_rows_kernel<T, G, VEC, true><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, (const T*)dY, (G*)dW, (int)chunk_blocks, slices);
+  else embedding_rows_kernel<T, G, VEC, false><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, (const T*)dY, (G*)dW, (int)chunk_blocks, slices);
+  if (p.chunks > 1)
+    embedding_join_kernel<G, VEC><<<dim3((unsigned)(p.chunks - 1), (unsigned)((a.pieces + 63) / 64)), dim3(64), 0, s>>>(a, (G*)dW);
   return (int)hipGetLastError();
 }
 

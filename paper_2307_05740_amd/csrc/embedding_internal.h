@@ -8,19 +8,22 @@
 
 namespace arrow {
 
-constexpr int kDigitBits = 9;        // of the sort by id, at most
-constexpr int kSortTokens = 256;     // of a wavefront of the sort, at least
-constexpr int kChunkTokens = 64;     // sorted tokens that a workgroup of the sums goes through, at least
+constexpr int kDigitBits = 9;        // of the sort by id of many tokens, at most
+constexpr int kSortTokens = 256;     // of a wavefront of it, at least
+constexpr int kWideDigitBits = 15;   // of the sort of few tokens, at most
+constexpr int kFewTokens = 65535;    // they are counted in 16 bits
+constexpr int kChunkTokens = 32;     // sorted tokens that a workgroup of the sums goes through, at least
 
 // How the gradient of a call is carried out, and where its workspace keeps what.
 struct EmbeddingPlan {
+  bool few;                        // tokens: each workgroup of the sort counts them all
   int32_t passes, bits;            // of the sort by id: digits, and bits of each
   int64_t blocks, block_tokens;    // its workgroups, and the tokens of each
   int64_t chunk, chunks;           // sorted tokens of a workgroup of the sums, and how many of those
   int64_t padded;                  // columns of a row of partial sums
   size_t keys[2], tokens[2];       // sorted ids and the tokens they stand at, two of each
   size_t counts;                   // digits x blocks
-  size_t begin, end;               // per row of the table; holds nothing for rows without tokens
+  size_t begin, end;               // per row of the table, its sorted tokens; after a sort of several digits nothing for rows without any
   size_t parts;                    // two rows of partial sums per chunk
   size_t bytes;
 };
