@@ -3,7 +3,7 @@
 // Both are bound by the rows that they move.  The gradient is the product of a transposed one-hot matrix with dY: the tokens
 // are sorted by id (a stable radix sort, so that a row's tokens keep their order), then each row of dW is the sum of its
 // tokens' rows.  A few ids have a large part of all tokens: the sorted tokens are cut into chunks, rows that reach over a chunk's end
-// are summed chunk by chunk into partial rows, and a row's own workgroup adds those up.
+// are summed chunk by chunk into partial rows, which a last kernel adds up.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -283,107 +283,95 @@ struct SumArgs {
   int columns, pieces, lanes_log;
 };
 
-// Adds up the rows of dY of the sorted tokens lo .. hi - 1, one piece of columns, in order; eight rows on their way at a time.
-template <typename T, int VEC>
-__device__ __forceinline__ void add_rows(const SumArgs& a, const T* dY, int64_t lo, int64_t hi, int c, float (&sum)[VEC]) {
+// One piece of columns of chunk `chunk` of the sorted tokens: a row whose tokens all lie in it goes to dW, the part of one that began
+// before it to partial row 2 chunk, of one that begins in it and goes on to 2 chunk + 1.  Eight tokens' rows are on their way at a time, whichever
+// rows of dW they belong to.
+template <typename T, typename G, int VEC>
+__device__ __forceinline__ void add_chunk(const SumArgs& a, const T* dY, G* dW, int64_t chunk, int piece) {
   constexpr int kAhead = 8;
+  static_assert(kChunkTokens % kAhead == 0, "keys are read eight at a time");
+  const int64_t lo = chunk * a.chunk, hi = lo + a.chunk < a.n ? lo + a.chunk : a.n;
+  const int c = VEC == 1 ? piece : min(piece * VEC, a.columns - VEC);
+  constexpr uint32_t kNone = 0xffffffffu;
+  const uint32_t before = lo > 0 ? a.keys[lo - 1] : kNone, after = hi < a.n ? a.keys[hi] : kNone;
+  struct Eight { uint4 lo, hi; };                                   // (the arrays have room for the last eight)
+  auto eight = [](const uint32_t* p) { return Eight{*(const uint4*)p, *(const uint4*)(p + 4)}; };
+  auto spread = [](const Eight& e, uint32_t (&x)[kAhead]) {
+    x[0] = e.lo.x; x[1] = e.lo.y; x[2] = e.lo.z; x[3] = e.lo.w; x[4] = e.hi.x; x[5] = e.hi.y; x[6] = e.hi.z; x[7] = e.hi.w;
+  };
+  Eight keys = eight(a.keys + lo), tokens = eight(a.tokens + lo);
+  bool began_before = keys.lo.x == before;
+  float sum[VEC] = {};
+  uint32_t key[kAhead], token[kAhead], now = kNone;
   for (int64_t i = lo; i < hi; i += kAhead) {
+    spread(keys, key);
+    spread(tokens, token);
     typename Columns<T, VEC>::type x[kAhead];
-    const int64_t last = hi - 1;
-#pragma unroll
-    for (int r = 0; r < kAhead; ++r) x[r] = *(const typename Columns<T, VEC>::type*)(dY + a.tokens[i + r < hi ? i + r : last] * a.y_stride + c);
 #pragma unroll
     for (int r = 0; r < kAhead; ++r)
-      if (i + r < hi) {
-        if constexpr (VEC == 1) sum[0] += (float)x[r];
-        else {
+      if (i + r < hi && key[r] < a.rows) x[r] = *(const typename Columns<T, VEC>::type*)(dY + (int64_t)token[r] * a.y_stride + c);
+    const bool more = i + kAhead < hi;
+    if (more) { keys = eight(a.keys + i + kAhead); tokens = eight(a.tokens + i + kAhead); }
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) sum[j] += (float)x[r][j];
-        }
+    for (int r = 0; r < kAhead; ++r) {
+      if (i + r >= hi || key[r] >= a.rows) continue;
+      now = key[r];
+      if constexpr (VEC == 1) sum[0] += (float)x[r];
+      else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[j] += (float)x[r][j];
       }
-  }
-}
-
-// Chunk i of the sorted tokens, 256 VEC columns of it: sums its part of rows that go on beyond it, one that began before it into partial row
-// 2 i, one that begins in it into 2 i + 1.
-template <typename T, int VEC>
-__device__ __forceinline__ void add_chunk(const SumArgs& a, const T* dY, int64_t chunk, int slice) {
-  const int64_t lo = chunk * a.chunk, hi = lo + a.chunk < a.n ? lo + a.chunk : a.n;
-  const uint32_t first = a.keys[lo], last = a.keys[hi - 1];
-  const int piece = slice * 256 + threadIdx.x;
-  if (piece >= a.pieces) return;
-  const int c = VEC == 1 ? piece : min(piece * VEC, a.columns - VEC);
-  if (first < a.rows && lo > 0 && a.keys[lo - 1] == first) {        // began before: up to where it ends, or the chunk does
-    int64_t to = hi;
-    if (last != first) {                                             // first place of another key
-      int64_t l = lo, h = hi - 1;
-      while (l < h) { const int64_t m = (l + h) / 2; if (a.keys[m] == first) l = m + 1; else h = m; }
-      to = l;
+      const uint32_t next = i + r + 1 == hi ? after : r + 1 < kAhead ? key[r + 1 < kAhead ? r + 1 : 0] : keys.lo.x;
+      if (next == now) continue;
+      if (began_before) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) a.parts[2 * chunk * a.padded + piece * VEC + j] = sum[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[j] *= a.scale;
+        store<G, VEC>(dW + (int64_t)now * a.w_stride + c, sum);
+      }
+      began_before = false;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
     }
-    float sum[VEC] = {};
-    add_rows<T, VEC>(a, dY, lo, to, c, sum);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) a.parts[2 * chunk * a.padded + piece * VEC + j] = sum[j];
   }
-  const bool began_before = lo > 0 && a.keys[lo - 1] == last;
-  if (last < a.rows && hi < a.n && a.keys[hi] == last && !began_before) {
-    int64_t l = lo, h = hi - 1;                                      // its first place
-    while (l < h) { const int64_t m = (l + h) / 2; if (a.keys[m] < last) l = m + 1; else h = m; }
-    float sum[VEC] = {};
-    add_rows<T, VEC>(a, dY, l, hi, c, sum);
+  if (after != kNone && now == after) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) a.parts[(2 * chunk + 1) * a.padded + piece * VEC + j] = sum[j];
+    for (int j = 0; j < VEC; ++j) a.parts[(2 * chunk + !began_before) * a.padded + piece * VEC + j] = sum[j];
   }
 }
 
-constexpr int kTableRows = 8;      // rows of dW of a lane group, four on their way at a time
+constexpr int kTableRows = 8;      // rows of dW that a lane group looks over
 
-// The rows of dW that lie within a chunk: zero, or the sum of their tokens' rows; and, by the first workgroups, the parts of the others.
-// kNoted: begin[] and end[] hold what they will for rows without tokens, and a row has some only where the sorted ids say so.
+// The first workgroups add up the chunks, `slices` of them per 256 >> lanes_log chunks; the others clear the rows of dW that have no tokens.
+// kNoted: begin[] and end[] say which those are; otherwise they hold what they will for such rows, and a row has tokens only where the sorted ids say so.
 template <typename T, typename G, int VEC, bool kNoted>
-__global__ __launch_bounds__(256) void embedding_rows_kernel(SumArgs a, const T* dY, G* dW, int chunk_blocks, int slices) {
-  if ((int)blockIdx.x < chunk_blocks) return add_chunk<T, VEC>(a, dY, blockIdx.x / slices, blockIdx.x % slices);
-  __shared__ uint32_t begins[256 * kTableRows], ends[256 * kTableRows];
+__global__ __launch_bounds__(256) void embedding_rows_kernel(SumArgs a, const T* dY, G* dW, int64_t chunks, int chunk_blocks, int slices) {
   const int lane = threadIdx.x & ((1 << a.lanes_log) - 1), in = threadIdx.x >> a.lanes_log, abreast = 256 >> a.lanes_log;
+  if ((int)blockIdx.x < chunk_blocks) {
+    const int64_t chunk = (int64_t)(blockIdx.x / slices) * abreast + in;
+    const int piece = (blockIdx.x % slices << a.lanes_log) + lane;
+    if (chunk < chunks && piece < a.pieces) add_chunk<T, G, VEC>(a, dY, dW, chunk, piece);
+    return;
+  }
+  __shared__ bool empty[256 * kTableRows];
   const int64_t row0 = (int64_t)(blockIdx.x - chunk_blocks) * abreast * kTableRows;
   for (int r = threadIdx.x; r < abreast * kTableRows; r += 256) {
     const int64_t row = row0 + r;
-    uint32_t lo = 0, hi = 0;
-    if (row < a.rows && a.n > 0) {
-      lo = a.begin[row];
-      hi = a.end[row];
-      if (!kNoted && !(lo < a.n && a.keys[lo] == (uint32_t)row && (lo == 0 || a.keys[lo - 1] != (uint32_t)row))) hi = lo = 0;
+    bool none = row < a.rows;
+    if (none && a.n > 0) {
+      const uint32_t at = a.begin[row];
+      none = kNoted ? at == a.end[row] : !(at < a.n && a.keys[at] == (uint32_t)row && (at == 0 || a.keys[at - 1] != (uint32_t)row));
     }
-    begins[r] = lo;
-    ends[r] = hi;
+    empty[r] = none;
   }
   __syncthreads();
-  for (int r0 = in; r0 < abreast * kTableRows; r0 += 4 * abreast) {
-    int64_t lo[4], hi[4], first[4];
-    bool mine[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      lo[r] = begins[r0 + r * abreast];
-      hi[r] = ends[r0 + r * abreast];
-      mine[r] = row0 + r0 + r * abreast < a.rows && (lo[r] == hi[r] || lo[r] / a.chunk == (hi[r] - 1) / a.chunk);
-      first[r] = mine[r] && lo[r] < hi[r] ? (int64_t)a.tokens[lo[r]] * a.y_stride : -1;
-    }
-    for (int piece = lane; piece < a.pieces; piece += 1 << a.lanes_log) {
-      const int c = VEC == 1 ? piece : min(piece * VEC, a.columns - VEC);
-      float sum[4][VEC] = {};
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (first[r] >= 0) load<T, VEC>(dY + first[r] + c, sum[r]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (!mine[r]) continue;
-        if (hi[r] - lo[r] > 1) add_rows<T, VEC>(a, dY, lo[r] + 1, hi[r], c, sum[r]);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) sum[r][j] *= a.scale;
-        store<G, VEC>(dW + (row0 + r0 + r * abreast) * a.w_stride + c, sum[r]);
-      }
-    }
-  }
+  const float zero[VEC] = {};
+  for (int r = in; r < abreast * kTableRows; r += abreast)
+    if (empty[r])
+      for (int piece = lane; piece < a.pieces; piece += 1 << a.lanes_log)
+        store<G, VEC>(dW + (row0 + r) * a.w_stride + (VEC == 1 ? piece : min(piece * VEC, a.columns - VEC)), zero);
 }
 
 // The rows that go over the end of a chunk, each by the end that it goes over first: their partial rows added up in order.
@@ -456,12 +444,15 @@ int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY,
   a.n = e.tokens; a.chunk = p.chunk; a.padded = p.padded; a.rows = e.rows; a.w_stride = e.w_stride; a.y_stride = e.y_stride;
   a.scale = e.scale; a.columns = e.columns; a.pieces = (e.columns + VEC - 1) / VEC; a.lanes_log = log2_up(a.pieces, 8);
   if (e.tokens && !noted) sort_rows_kernel<<<dim3((unsigned)((e.tokens + 255) / 256)), dim3(256), 0, s>>>(a.keys, a.n, a.rows, a.begin, a.end);
-  const int slices = (a.pieces + 255) / 256;
-  const int64_t chunk_blocks = p.chunks > 1 ? p.chunks * slices : 0;
-  const int64_t rows = (256 >> a.lanes_log) * kTableRows, blocks = chunk_blocks + (e.rows + rows - 1) / rows;
+  const int abreast = 256 >> a.lanes_log, slices = (a.pieces + (1 << a.lanes_log) - 1) >> a.lanes_log;
+  const int64_t chunk_blocks = (p.chunks + abreast - 1) / abreast * slices;
+  const int64_t rows = abreast * kTableRows, blocks = chunk_blocks + (e.rows + rows - 1) / rows;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
-  if (noted) embedding_rows_kernel<T, G, VEC, true><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, (const T*)dY, (G*)dW, (int)chunk_blocks, slices);
-  else embedding_rows_kernel<T, G, VEC, false><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, (const T*)dY, (G*)dW, (int)chunk_blocks, slices);
+  auto sums = [&](auto is_noted) {
+    embedding_rows_kernel<T, G, VEC, decltype(is_noted)::value>
+        <<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, (const T*)dY, (G*)dW, p.chunks, (int)chunk_blocks, slices);
+  };
+  if (noted) sums(std::true_type{}); else sums(std::false_type{});
   if (p.chunks > 1)
     embedding_join_kernel<G, VEC><<<dim3((unsigned)(p.chunks - 1), (unsigned)((a.pieces + 63) / 64)), dim3(64), 0, s>>>(a, (G*)dW);
   return (int)hipGetLastError();
