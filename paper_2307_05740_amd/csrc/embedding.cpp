@@ -70,14 +70,15 @@ EmbeddingPlan plan_embedding(const arrow_embedding_t& e) {
   p.bits = (bits + p.passes - 1) / p.passes;
   p.block_tokens = std::max<int64_t>(kSortTokens, ceil_div(ceil_div(e.tokens, 1024), 64) * 64);
   p.blocks = ceil_div(e.tokens, p.block_tokens);
-  p.chunk = kChunkTokens * std::max<int64_t>(1, ceil_div(e.tokens, 4096 * kChunkTokens));
+  const int64_t eights = std::max<int64_t>(1, ceil_div(e.tokens, 512 * kChunkTokens));
+  p.chunk = kChunkTokens * std::max(std::min<int64_t>(4, eights), ceil_div(e.tokens, 16384 * kChunkTokens));
   p.chunks = ceil_div(e.tokens, p.chunk);
   p.padded = ceil_div(e.columns, 8) * 8;
   size_t at = 0;
   auto room = [&](int64_t n) { const size_t was = at; at += ((size_t)n * 4 + 255) / 256 * 256; return was; };
   for (int i = 0; i < 2; ++i) { p.keys[i] = room(e.tokens); p.tokens[i] = room(e.tokens); }
   p.counts = p.few ? at : room(((int64_t)1 << p.bits) * p.blocks);
-  p.begin = room(e.rows);
+  p.begin = room(e.rows + 1);
   p.end = room(e.rows);
   p.parts = room(2 * p.chunks * p.padded);
   p.bytes = at;

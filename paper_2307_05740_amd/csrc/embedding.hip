@@ -163,20 +163,21 @@ __global__ __launch_bounds__(64) void sort_move_kernel(SortArgs s) {
   }
 }
 
-// The sort of a digit in one launch, for few tokens: every workgroup counts all of them, those before its own 1024 in the upper half of
-// a word, and so knows where its tokens go.  16,384 tokens of 32,000 rows: TODO us, where the three launches above take TODO, twice.
+// The sort of a digit in one launch, for few tokens: every workgroup counts all of them, those before its own ones in the upper half of
+// a word, and so knows where its own go: block_tokens of them, whole wavefronts' and at most as many as it has threads.  16,384 tokens of 32,000
+// rows: TODO us, where the three launches above take TODO, twice.
 constexpr int kSortBlock = 1024;
 
-__global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32_t* row_begin, uint32_t* row_end) {
+__global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32_t* row_begin) {
   __shared__ __align__(16) uint32_t bins[1 << kWideDigitBits];
   __shared__ uint32_t sums[kSortBlock / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, values = 1 << s.bits, mask = values - 1;
   // four values to a place; threads that go through neighbouring places do not meet in a bank
-  auto place = [](uint32_t b) { return b ^ ((b >> 5 & 7) << 2); };
+  auto place = [](uint32_t b) { return b ^ ((b >> 6 & 7) << 2); };
   for (int i = 4 * threadIdx.x; i < values; i += 4 * kSortBlock) *(uint4*)&bins[i] = uint4{0, 0, 0, 0};
-  const int n = (int)s.n, own = (int)blockIdx.x * kSortBlock, t = own + threadIdx.x;
-  const bool in = t < n;
-  uint32_t key = 0;
+  const int n = (int)s.n, own = (int)(blockIdx.x * s.block_tokens), t = own + threadIdx.x;
+  const bool in = threadIdx.x < s.block_tokens && t < n;
+  uint32_t key = in ? key_at(s, t) : 0;
   constexpr int kBatch = 8;
   for (int begin = 0; begin < n; begin += kBatch * kSortBlock) {     // (as often for every thread: there is a barrier in it)
     const int t0 = begin + threadIdx.x;
@@ -188,7 +189,6 @@ __global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32
     for (int r = 0; r < kBatch; ++r) {
       const int at = t0 + r * kSortBlock;
       if (at < n) atomicAdd(&bins[place((x[r] >> s.shift) & mask)], at < own ? 0x10001u : 1u);
-      if (at == t) key = x[r];
     }
   }
   __syncthreads();
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32
   if (each < 4) {
     for (int i = first; i < first + each && i < values; ++i) count += bins[place(i)] & 0xffff;
   } else {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = first; i < first + each; i += 4) {
       const uint4 x = *(const uint4*)&bins[place(i)];
       count += (x.x & 0xffff) + (x.y & 0xffff) + (x.z & 0xffff) + (x.w & 0xffff);
@@ -211,36 +211,32 @@ __global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32
   }
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
-  uint32_t base = upto - count;
-  for (int w = 0; w < wave; ++w) base += sums[w];
-  const bool note = row_begin && threadIdx.x % gridDim.x == blockIdx.x;   // the only digit: a value is a row
+  uint32_t base = lane < wave ? sums[lane] : 0;                      // (at most 15 wavefronts before)
+  for (int m = 1; m < 16; m <<= 1) base += __shfl_xor(base, m, 64);
+  base = __shfl(base, 0, 64) + upto - count;
+  // the only digit: a value is a row; every workgroup notes a part of them
+  const bool note = row_begin && threadIdx.x % gridDim.x == blockIdx.x;
   if (each < 4) {
     for (int i = first; i < first + each && i < values; ++i) {
       const uint32_t x = bins[place(i)];
-      if (note && i < s.rows) { row_begin[i] = base; row_end[i] = base + (x & 0xffff); }
+      if (note && i <= s.rows) row_begin[i] = base;
       bins[place(i)] = base + (x >> 16);
       base += x & 0xffff;
     }
   } else {
+#pragma unroll 8
     for (int i = first; i < first + each; i += 4) {
       const uint4 x = *(const uint4*)&bins[place(i)];
-      const uint4 at = {base, base + (x.x & 0xffff), base + (x.x & 0xffff) + (x.y & 0xffff), base + (x.x & 0xffff) + (x.y & 0xffff) + (x.z & 0xffff)};
-      base = at.w + (x.w & 0xffff);
-      *(uint4*)&bins[place(i)] = uint4{at.x + (x.x >> 16), at.y + (x.y >> 16), at.z + (x.z >> 16), at.w + (x.w >> 16)};
-      if (!note) continue;
-      if (i + 3 < s.rows) {
-        *(uint4*)&row_begin[i] = at;
-        *(uint4*)&row_end[i] = uint4{at.y, at.z, at.w, base};
-      } else {
-        const uint32_t b[5] = {at.x, at.y, at.z, at.w, base};
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (i + j < s.rows) { row_begin[i + j] = b[j]; row_end[i + j] = b[j + 1]; }
-      }
+      const uint32_t a = base + (x.x & 0xffff), b = a + (x.y & 0xffff), c = b + (x.z & 0xffff);
+      *(uint4*)&bins[place(i)] = uint4{base + (x.x >> 16), a + (x.y >> 16), b + (x.z >> 16), c + (x.w >> 16)};
+      if (note && i <= s.rows) *(uint4*)&row_begin[i] = uint4{base, a, b, c};   // (there is room for the last four)
+      base = c + (x.w & 0xffff);
     }
   }
   __syncthreads();
   // this workgroup's tokens, in order: the lanes of a wavefront with one value, one wavefront after the other
+  const int waves = (int)(s.block_tokens + 63) / 64;
+  if (waves == 1 && wave > 0) return;                                // (no barrier below is one of several wavefronts then)
   const uint32_t digit = (key >> s.shift) & mask;
   uint64_t same = __ballot(in);
   for (int b = 0; b < s.bits; ++b) {
@@ -249,12 +245,12 @@ __global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32
   }
   const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
   uint32_t at = 0;
-  for (int w = 0; w < kSortBlock / 64 && own + w * 64 < n; ++w) {
+  for (int w = 0; w < waves; ++w) {
     if (w == wave && in) {
       at = bins[place(digit)];
       if (before == 0) bins[place(digit)] = at + __popcll(same);
     }
-    __syncthreads();
+    if (waves > 1) __syncthreads();
   }
   if (in) {
     s.to_keys[at + before] = key;
@@ -430,7 +426,9 @@ int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY,
     a.n = e.tokens; a.block_tokens = p.block_tokens; a.blocks = p.blocks; a.rows = e.rows;
     a.shift = i * p.bits; a.bits = p.bits;
     if (p.few) {
-      sort_few_kernel<<<dim3((unsigned)((e.tokens + kSortBlock - 1) / kSortBlock)), dim3(kSortBlock), 0, s>>>(a, noted ? at(p.begin) : nullptr, at(p.end));
+      a.block_tokens = 64 * ((e.tokens + 64 * 256 - 1) / (64 * 256));   // a workgroup for every compute unit
+      a.blocks = (e.tokens + a.block_tokens - 1) / a.block_tokens;
+      sort_few_kernel<<<dim3((unsigned)a.blocks), dim3(kSortBlock), 0, s>>>(a, noted ? at(p.begin) : nullptr);
       continue;
     }
     sort_count_kernel<<<dim3((unsigned)p.blocks), dim3(64), 0, s>>>(a);
@@ -439,7 +437,7 @@ int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY,
   }
   SumArgs a{};
   a.keys = at(p.keys[now]); a.tokens = at(p.tokens[now]);
-  a.begin = at(p.begin); a.end = at(p.end);
+  a.begin = at(p.begin); a.end = noted ? a.begin + 1 : at(p.end);
   a.parts = (float*)at(p.parts);
   a.n = e.tokens; a.chunk = p.chunk; a.padded = p.padded; a.rows = e.rows; a.w_stride = e.w_stride; a.y_stride = e.y_stride;
   a.scale = e.scale; a.columns = e.columns; a.pieces = (e.columns + VEC - 1) / VEC; a.lanes_log = log2_up(a.pieces, 8);

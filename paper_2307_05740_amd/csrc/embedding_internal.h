@@ -12,7 +12,8 @@ constexpr int kDigitBits = 9;        // of the sort by id of many tokens, at mos
 constexpr int kSortTokens = 256;     // of a wavefront of it, at least
 constexpr int kWideDigitBits = 15;   // of the sort of few tokens, at most
 constexpr int kFewTokens = 65535;    // they are counted in 16 bits
-constexpr int kChunkTokens = 32;     // sorted tokens that a workgroup of the sums goes through, at least
+constexpr int kChunkTokens = 8;      // sorted tokens that a lane group of the sums goes through, a multiple of this: a row's load or two for few
+                                     // tokens, and four where there are enough to fill the chip
 
 // How the gradient of a call is carried out, and where its workspace keeps what.
 struct EmbeddingPlan {
@@ -23,7 +24,8 @@ struct EmbeddingPlan {
   int64_t padded;                  // columns of a row of partial sums
   size_t keys[2], tokens[2];       // sorted ids and the tokens they stand at, two of each
   size_t counts;                   // digits x blocks
-  size_t begin, end;               // per row of the table, its sorted tokens; after a sort of several digits nothing for rows without any
+  size_t begin, end;               // per row of the table, its sorted tokens: begin up to the next row's after a sort of one digit; after others both,
+                                   // and nothing for rows without any
   size_t parts;                    // two rows of partial sums per chunk
   size_t bytes;
 };

@@ -198,3 +198,11 @@ def test_classes_refuse_tensors():
         ArrowEmbedding(4).forward(torch.zeros(4, 8), torch.zeros(3, dtype=torch.int16))
     with pytest.raises(TypeError):
         ArrowEmbedding(4).forward(torch.zeros(4, 8, dtype=torch.float64), torch.zeros(3, dtype=torch.int64))
+
+
+def test_workspaces_of_any_number_of_tokens(L):
+    """None, one, and those around the sizes at which the sort or the chunks of the sums change."""
+    for tokens in (0, 1, 7, 8, 9, 4096, 4097, 65535, 65536, 1_000_000, 1 << 30):
+        for rows in (1, 2, 32767, 32768, 2**31 - 2):
+            e = embedding(tokens=tokens, rows=rows)
+            assert L.arrow_embedding_workspace_bytes(ctypes.byref(e)) >= 4 * (rows + 4 * tokens)
