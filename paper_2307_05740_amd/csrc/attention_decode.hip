@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a cache in pages, and writes into it (include/arrow_attention.h).
 //
 // What bounds it is the cache: every visible key and value is read once, for all query heads that share it.  A workgroup takes
-// the up to 16 query heads of a key head and a stretch of the visible keys; its wavefronts take tiles of 32 keys in turn, each with
+// the up to 16 query heads of a key head and a stretch of the visible keys; its wavefronts take tiles of 16 keys in turn, each with
 // a running maximum and sum of its own, and are joined in LDS.  Long caches are cut into several stretches; their results go to the
 // workspace and a second kernel joins them.
 //
@@ -12,9 +12,20 @@ namespace arrow {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kKeys = 32;    // keys of a tile
+constexpr int kKeys = 16;    // keys of a tile
 
-// 16 x 16 with 32 inner steps: lane l holds row / column l % 16 at inner steps 8 (l / 16) + 0..7; of C and D column l % 16, rows 4 (l / 16) + 0..3.
+// Scores: 16 x 16 with 32 inner steps; lane l holds row / column l % 16 at inner steps 8 (l / 16) + 0..7; of C and D column l % 16, rows
+// 4 (l / 16) + 0..3.  Values: 16 x 16 with 16 inner steps, 4 (l / 16) + 0..3 in lane l: a result's rows as they come.
+__device__ __forceinline__ f32x4 mma_values(i16x4 a, x4<__bf16> b, f32x4 c) {
+  union { x4<__bf16> t; i16x4 i; } u;
+  u.t = b;
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, u.i, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma_values(i16x4 a, x4<_Float16> b, f32x4 c) {
+  union { x4<_Float16> t; i16x4 i; } u;
+  u.i = a;
+  return __builtin_amdgcn_mfma_f32_16x16x16f16(u.t, b, c, 0, 0, 0);
+}
 
 // max / sum over the four lanes that have one l % 16
 __device__ __forceinline__ float max_quarters(float x) {
@@ -32,11 +43,12 @@ struct Row {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void attention_decode_kernel(CacheArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheArgs a) {
   using Tl = Tile<D>;
   constexpr int kPer = D / 32;                                   // pieces of 16 bytes of a row that a lane loads
-  __shared__ __align__(1024) unsigned char smem[kWaves][kKeys * Tl::kRowBytes];
-  __shared__ float tops[kWaves][16], totals[kWaves][16];
+  constexpr int kRoom = 16 * D * 4;                              // of a wavefront: its sums, and before them a tile of values
+  static_assert(kKeys * Tl::kRowBytes <= kRoom, "room for a tile of values");
+  __shared__ __align__(1024) unsigned char smem[kWaves * kRoom + kWaves * 2 * 16 * 4];
   const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
   const arrow_cache_t& c = a.c;
   int id = blockIdx.x;
@@ -68,49 +80,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_decode_kernel(CacheA
                 ? *(const x8<T>*)((const char*)a.q.at + 2 * (b * a.q.sequence + (int64_t)(kv * a.group + head0 + col) * a.q.head + d)) : z;
   }
 
-  auto row_of = [&](int i) {
-    Row r{nullptr, nullptr, -1, -1};
-    if (i >= seen) return r;
-    const int j = i < lead ? i : i - lead + begin;
-    const int page = table[j >> a.page_log];
-    if (page < 0 || page >= c.pages) return r;
-    const int slot = j & (c.page - 1);
-    const int64_t at_k = page * c.k_page + slot * c.k_token, at_v = page * c.v_page + slot * c.v_token;
-    r.k = k_pool + 2 * at_k;
-    r.v = v_pool + 2 * at_v;
-    if (fresh && j == length - 1) { r.to_k = at_k; r.to_v = at_v; r.k = k_new; r.v = v_new; }
-    return r;
-  };
-  // A tile on its way: of rows col and 16 + col, the pieces 4 s + quarter
-  x8<T> kf[2][kPer], vf[2][kPer];
-  uint32_t visible = 0;                                          // of the tile's keys, the same in all lanes
-  auto load = [&](int tile) {
-    const Row r[2] = {row_of(tile * kKeys + col), row_of(tile * kKeys + 16 + col)};
-    visible = (uint32_t)(__ballot(r[0].k != nullptr) & 0xffff) | (uint32_t)(__ballot(r[1].k != nullptr) & 0xffff) << 16;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int s = 0; s < kPer; ++s) {
-        const int d = 32 * s + 8 * quarter;
-        const x8<T> z = {};
-        const bool in = r[n].k != nullptr && d < c.dim;
-        kf[n][s] = in ? *(const x8<T>*)(r[n].k + 2 * d) : z;
-        vf[n][s] = in ? *(const x8<T>*)(r[n].v + 2 * d) : z;
-      }
-    if (fresh && head_tile == 0) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-        if (r[n].to_k >= 0) {
-#pragma unroll
-          for (int s = 0; s < kPer; ++s) {
-            const int d = 32 * s + 8 * quarter;
-            if (d < c.dim) {
-              *(x8<T>*)((char*)k_pool + 2 * (r[n].to_k + d)) = kf[n][s];
-              *(x8<T>*)((char*)v_pool + 2 * (r[n].to_v + d)) = vf[n][s];
-            }
-          }
-        }
+  // the new token to its place, by the last stretch
+  if (fresh && head_tile == 0 && split == a.splits - 1 && wave == kWaves - 1 && length > 0) {
+    const int page = table[(length - 1) >> a.page_log], slot = (length - 1) & (c.page - 1), d = 8 * lane;
+    if (page >= 0 && page < c.pages && d < c.dim) {
+      *(x8<T>*)((char*)k_pool + 2 * (page * c.k_page + slot * c.k_token + d)) = *(const x8<T>*)(k_new + 2 * d);
+      *(x8<T>*)((char*)v_pool + 2 * (page * c.v_page + slot * c.v_token + d)) = *(const x8<T>*)(v_new + 2 * d);
     }
+  }
+
+  // A tile on its way: of key col, the pieces 4 s + quarter of its row.  Nothing here branches: the loads of one tile are to be on their way while
+  // another's are waited for.  Pieces beyond the row are read as its last one, where zeros of q and unused sums meet them; keys that are not
+  // visible as q, whose scores are masked and whose values are cleared below.
+  x8<T> kf[kPer], vf[kPer];
+  uint32_t visible = 0;                                          // of the tile's keys, the same in all lanes
+  int offset[kPer];
+#pragma unroll
+  for (int s = 0; s < kPer; ++s) offset[s] = min(64 * s + 16 * quarter, 2 * c.dim - 16);
+  const char* nothing = (const char*)a.q.at + 2 * (b * a.q.sequence + (int64_t)kv * a.group * a.q.head);
+  auto key_of = [&](int i) { return i < lead ? i : i - lead + begin; };
+  auto page_of = [&](int tile) { return table[key_of(min(tile * kKeys + col, seen - 1)) >> a.page_log]; };
+  int page = 0;                                                  // of the tile that is loaded next, looked up a tile ahead
+  auto load = [&](int tile) {
+    const int i = tile * kKeys + col, j = key_of(i), slot = j & (c.page - 1);
+    const bool in = i < seen && page >= 0 && page < c.pages, newest = fresh && j == length - 1;
+    const char* k = !in ? nothing : newest ? k_new : k_pool + 2 * (page * c.k_page + slot * c.k_token);
+    const char* v = !in ? nothing : newest ? v_new : v_pool + 2 * (page * c.v_page + slot * c.v_token);
+    visible = (uint32_t)__ballot(in) & 0xffff;
+    page = page_of(tile + kWaves);
+#pragma unroll
+    for (int s = 0; s < kPer; ++s) kf[s] = *(const x8<T>*)(k + offset[s]);
+#pragma unroll
+    for (int s = 0; s < kPer; ++s) vf[s] = *(const x8<T>*)(v + offset[s]);
   };
 
   f32x4 acc[D / 16];
@@ -118,124 +119,129 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_decode_kernel(CacheA
   for (int m = 0; m < D / 16; ++m) acc[m] = (f32x4)(0.f);
   const float scale = c.scale * kLog2e;
   float top = minus_infinity(), total = 0.f;
-  lds_byte* vt = (lds_byte*)smem[wave];
-  // the transposed read: rows 16 u + 4 quarter + 0..3, columns 16 m + col
-  const int tr_row = 4 * quarter + (col >> 2), tr_turn = Tl::turn(tr_row), tr_byte = tr_row * Tl::kRowBytes + ((col & 1) << 3), tr_piece = (col & 3) >> 1;
+  lds_byte* vt = (lds_byte*)smem + wave * kRoom;
+  lds_byte* to = vt + col * Tl::kRowBytes;
+  const int turn = Tl::turn(col);
+  // the transposed read: rows 4 quarter + 0..3, columns 16 m + col
+  const int row = 4 * quarter + (col >> 2), row_turn = Tl::turn(row), piece = (col & 3) >> 1;
+  const lds_byte* from = vt + row * Tl::kRowBytes + ((col & 1) << 3);
 
   int tile = tile0 + wave;
-  if (tile < tile1) load(tile);
+  if (tile < tile1) {
+    page = page_of(tile);
+    load(tile);
+  }
   while (tile < tile1) {
-    f32x4 s[2];
+    f32x4 s = (f32x4)(0.f);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      s[n] = (f32x4)(0.f);
+    for (int i = 0; i < kPer; ++i) s = mma16(kf[i], qf[i], s);
+    if (visible != 0xffff) {
+      const x8<T> z = {};
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) s[n] = mma16(kf[n][i], qf[i], s[n]);
+      for (int i = 0; i < kPer; ++i) vf[i] = visible >> col & 1 ? vf[i] : z;
     }
     // (the tile is this wavefront's own: no barrier)
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        *(__attribute__((address_space(3))) x8<T>*)(vt + (16 * n + col) * Tl::kRowBytes + (((4 * i + quarter) ^ Tl::turn(16 * n + col)) << 4)) = vf[n][i];
-    const uint32_t now = visible;
+    for (int i = 0; i < kPer; ++i) *(__attribute__((address_space(3))) x8<T>*)(to + (((4 * i + quarter) ^ turn) << 4)) = vf[i];
+    const uint32_t now = visible >> (4 * quarter);
     tile += kWaves;
     if (tile < tile1) load(tile);
 
     float most = minus_infinity();
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[n][i] = now >> (16 * n + 4 * quarter + i) & 1 ? s[n][i] : minus_infinity();
-        most = fmaxf(most, s[n][i]);
-      }
+    for (int i = 0; i < 4; ++i) {
+      s[i] = now >> i & 1 ? s[i] : minus_infinity();
+      most = fmaxf(most, s[i]);
+    }
     most = max_quarters(most) * scale;
     const float next = fmaxf(top, most), off = next == minus_infinity() ? 0.f : next;
     const float by = __builtin_amdgcn_exp2f(top - off);
     top = next;
     total *= by;
+    x4<T> pf;
 #pragma unroll
-    for (int m = 0; m < D / 16; ++m) acc[m] *= by;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], scale, -off));
-        total += s[n][i];
-      }
-    const x8<T> pf = round8<T>(s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]);
-#pragma unroll
-    for (int m = 0; m < D / 16; ++m) {
-      const lds_byte* at = vt + tr_byte + (((2 * m + tr_piece) ^ tr_turn) << 4);
-      union { i16x4 half[2]; x8<T> all; } vr;
-      vr.half[0] = lds_transposed(at);
-      vr.half[1] = lds_transposed(at + 16 * Tl::kRowBytes);
-      acc[m] = mma16(vr.all, pf, acc[m]);
+    for (int i = 0; i < 4; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -off));
+      total += s[i];
+      pf[i] = (T)s[i];
     }
+#pragma unroll
+    for (int m = 0; m < D / 16; ++m) acc[m] = mma_values(lds_transposed(from + (((2 * m + piece) ^ row_turn) << 4)), pf, acc[m] * by);
+    reads_ahead<D / 16, D / 16, 1>();
   }
   total = add_quarters(total);
 
-  // the wavefronts' results, sums first: column d of head h at [d][h], 16 floats to a row (the tiles are done with)
+  // the wavefronts' results: column d of head h at [d][h], 16 floats to a row (the tiles are done with)
   __syncthreads();
-  float* mine = (float*)smem[wave];
-  static_assert(kKeys * Tl::kRowBytes >= 16 * D * 4, "room for a wavefront's sums");
+  float* mine = (float*)(smem + wave * kRoom);
+  float *tops = (float*)(smem + kWaves * kRoom), *totals = tops + kWaves * 16;
 #pragma unroll
   for (int m = 0; m < D / 16; ++m)
 #pragma unroll
     for (int i = 0; i < 4; ++i) mine[(16 * m + 4 * quarter + i) * 16 + col] = acc[m][i];
-  if (quarter == 0) { tops[wave][col] = top; totals[wave][col] = total; }
+  if (quarter == 0) { tops[wave * 16 + col] = top; totals[wave * 16 + col] = total; }
   __syncthreads();
   for (int e = threadIdx.x; e < heads * c.dim; e += 64 * kWaves) {
     const int h = e / c.dim, d = e % c.dim;
-    float all = tops[0][h];
+    float all = tops[h];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w][h]);
+    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w * 16 + h]);
     const float off = all == minus_infinity() ? 0.f : all;
     float sum = 0.f, weight = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float by = __builtin_amdgcn_exp2f(tops[w][h] - off);
-      sum = fmaf(by, ((const float*)smem[w])[d * 16 + h], sum);
-      weight = fmaf(by, totals[w][h], weight);
+      const float by = __builtin_amdgcn_exp2f(tops[w * 16 + h] - off);
+      sum = fmaf(by, ((const float*)(smem + w * kRoom))[d * 16 + h], sum);
+      weight = fmaf(by, totals[w * 16 + h], weight);
     }
     const int head = kv * a.group + head0 + h;
     if (a.splits == 1) {
       ((T*)a.o.at)[b * a.o.sequence + head * a.o.head + d] = (T)(weight > 0.f || weight != weight ? sum / weight : 0.f);
     } else {
-      float* to = a.parts + ((int64_t)(b * c.q_heads + head) * a.splits + split) * (c.dim + 2);
-      to[d] = sum;
-      if (d == 0) { to[c.dim] = all; to[c.dim + 1] = weight; }
+      float* part = a.parts + ((int64_t)(b * c.q_heads + head) * a.splits + split) * (c.dim + 2);
+      part[d] = sum;
+      if (d == 0) { part[c.dim] = all; part[c.dim + 1] = weight; }
     }
   }
 }
 
-// The results of the stretches of one query head, joined: a wavefront, two columns per lane.
+// The results of the stretches of one query head, joined: two columns per lane, every fourth stretch per wavefront.
 template <typename T>
-__global__ __launch_bounds__(64) void attention_decode_join_kernel(CacheArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void attention_decode_join_kernel(CacheArgs a) {
+  __shared__ float weights[kMostSplits];
+  __shared__ float2 sums[kWaves][64];
   const arrow_cache_t& c = a.c;
-  const int row = blockIdx.x, b = row / c.q_heads, head = row % c.q_heads, step = c.dim + 2, lane = threadIdx.x, d = 2 * lane;
+  const int row = blockIdx.x, b = row / c.q_heads, head = row % c.q_heads, step = c.dim + 2, lane = threadIdx.x & 63, wave = wave_id(), d = 2 * lane;
   const float* from = a.parts + (int64_t)row * a.splits * step;
   float all = minus_infinity();
   for (int i = lane; i < a.splits; i += 64) all = fmaxf(all, from[(int64_t)i * step + c.dim]);
   for (int m = 32; m; m >>= 1) all = fmaxf(all, __shfl_xor(all, m, 64));
   const float off = all == minus_infinity() ? 0.f : all;
-  float s0 = 0.f, s1 = 0.f, weight = 0.f;
-  for (int i = 0; i < a.splits; ++i, from += step) {
-    const float by = __builtin_amdgcn_exp2f(from[c.dim] - off);
-    weight = fmaf(by, from[c.dim + 1], weight);
-    if (d < c.dim) {
-      const float2 x = *(const float2*)(from + d);
-      s0 = fmaf(by, x.x, s0);
-      s1 = fmaf(by, x.y, s1);
-    }
+  float total = 0.f;
+  for (int i = lane; i < a.splits; i += 64) {
+    const float by = __builtin_amdgcn_exp2f(from[(int64_t)i * step + c.dim] - off);
+    if (wave == 0) weights[i] = by;
+    total = fmaf(by, from[(int64_t)i * step + c.dim + 1], total);
   }
-  const float over = weight > 0.f || weight != weight ? 1.f / weight : 0.f;
-  if (d < c.dim) {
-    T* to = (T*)a.o.at + b * a.o.sequence + head * a.o.head + d;
-    to[0] = (T)(s0 * over);
-    to[1] = (T)(s1 * over);
+  for (int m = 32; m; m >>= 1) total += __shfl_xor(total, m, 64);
+  __syncthreads();
+  float2 sum = {0.f, 0.f};
+#pragma unroll 4
+  for (int i = wave; i < a.splits; i += kWaves) {
+    const float2 x = d < c.dim ? *(const float2*)(from + (int64_t)i * step + d) : float2{0.f, 0.f};
+    sum.x = fmaf(weights[i], x.x, sum.x);
+    sum.y = fmaf(weights[i], x.y, sum.y);
   }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave > 0 || d >= c.dim) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) { sum.x += sums[w][lane].x; sum.y += sums[w][lane].y; }
+  const float over = total > 0.f || total != total ? 1.f / total : 0.f;
+  x2<T> r;
+  r[0] = (T)(sum.x * over);
+  r[1] = (T)(sum.y * over);
+  *(x2<T>*)((T*)a.o.at + b * a.o.sequence + head * a.o.head + d) = r;
 }
 
 // One piece of 16 bytes per thread.
@@ -267,7 +273,7 @@ int decode(const CacheArgs& a, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (c.dim <= 64) attention_decode_kernel<T, 64><<<dim3((unsigned)blocks), dim3(64 * kWaves), 0, s>>>(a);
   else attention_decode_kernel<T, 128><<<dim3((unsigned)blocks), dim3(64 * kWaves), 0, s>>>(a);
-  if (a.splits > 1) attention_decode_join_kernel<T><<<dim3((unsigned)rows), dim3(64), 0, s>>>(a);
+  if (a.splits > 1) attention_decode_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kWaves), 0, s>>>(a);
   return (int)hipGetLastError();
 }
 

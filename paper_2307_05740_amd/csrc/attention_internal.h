@@ -48,6 +48,7 @@ int launch_attention_decode(const CacheArgs& a, void* stream);
 constexpr int kQueryTile = 128;    // queries of a workgroup, forward and dq
 constexpr int kKeyTile = 128;      // keys of a workgroup, dk and dv
 constexpr int kQueryStep = 64;     // queries that it goes through at a time
+constexpr int kMostSplits = 256;   // stretches of a cache
 constexpr int kHeadTile = 16;      // query heads of a workgroup, single tokens
 
 }  // namespace arrow
