@@ -151,7 +151,7 @@ CacheArgs plan(const arrow_cache_t* c) {
   int64_t seen = std::min(c->max_len, room);
   if (p.c.window) seen = std::min(seen, (int64_t)p.c.window + p.c.sinks);
   const int64_t rows = std::max<int64_t>(1, (int64_t)c->batch * c->kv_heads * ceil_div(p.group, kHeadTile));
-  p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({kMostSplits, ceil_div(1024, rows), ceil_div(seen, 64)}));
+  p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({kMostSplits, ceil_div(4096, rows), ceil_div(seen, 64)}));
   return p;
 }
 

@@ -92,12 +92,11 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 
     f32x16 s[kStep / 32];
 #pragma unroll
-    for (int n = 0; n < kStep / 32; ++n) {
-      s[n] = (f32x16)(0.f);
+    for (int n = 0; n < kStep / 32; ++n) s[n] = (f32x16)(0.f);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-        s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
-    }
+    for (int i = 0; i < D / 16; ++i)                          // (in turn: a product waits for the last one on the same sums)
+#pragma unroll
+      for (int n = 0; n < kStep / 32; ++n) s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
     reads_ahead<6, (kStep / 32) * (D / 16), 1>();
     // every query sees every key: nothing to mask
     const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);

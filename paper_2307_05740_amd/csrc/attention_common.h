@@ -124,19 +124,19 @@ struct Loader {
   static_assert(kSteps * WAVES * Tile<D>::kRowsOfKiB == ROWS && (WAVES * Tile<D>::kRowsOfKiB) % 16 == 0, "whole steps, one turn");
   uint32_t offset, step;
   bool inside;
-  int dim_bytes, stride_bytes;
+  int dim_bytes, stride_bytes, tile_bytes;                       // (of a tile whose rows are all there)
   __device__ __forceinline__ Loader(int wave, int lane, int64_t stride, int dim) {
     const int row = wave * Tile<D>::kRowsOfKiB + lane / Tile<D>::kPieces, piece = (lane % Tile<D>::kPieces) ^ Tile<D>::turn(row);
     stride_bytes = (int)(stride * 2);
     dim_bytes = dim * 2;
+    tile_bytes = (ROWS - 1) * stride_bytes + dim_bytes;
     offset = (uint32_t)(row * stride_bytes + piece * 16);
     step = (uint32_t)(WAVES * Tile<D>::kRowsOfKiB * stride_bytes);
     inside = piece * 8 < dim;
   }
   // base: the tile's first row (the same in all lanes); rows: those that are there, any number
   __device__ __forceinline__ void load(const void* base, int rows, lds_byte* tile, int wave) const {
-    rows = min(rows, ROWS);
-    const int bytes = rows > 0 ? (rows - 1) * stride_bytes + dim_bytes : 0;
+    const int bytes = rows >= ROWS ? tile_bytes : rows > 0 ? (rows - 1) * stride_bytes + dim_bytes : 0;
     auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)

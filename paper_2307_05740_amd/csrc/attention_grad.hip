@@ -200,31 +200,45 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
   const Loader<D, kQ, 4> lq(wave, lane, a.q.token, a.dim), ld(wave, lane, a.d_o.token, a.dim);
   lds_byte* base = (lds_byte*)smem;
   const TileReads<D> my(lane);
-  auto load = [&](int head, int q0, int to) {
-    const char* q = rows_of(a.q, ragged, b, sq.first, head);
-    const char* d_o = rows_of(a.d_o, ragged, b, sq.first, head);
-    lq.load(q + 2 * (int64_t)q0 * a.q.token, sq.count - q0, base + (2 * to) * kBytes, wave);
-    ld.load(d_o + 2 * (int64_t)q0 * a.d_o.token, sq.count - q0, base + (2 * to + 1) * kBytes, wave);
-    const int64_t stat = ragged ? head * a.q_tokens + sq.first + q0 : ((int64_t)b * a.q_heads + head) * a.q_len + q0;
+  // the step that is loaded next: a head's queries from q_next on, and where they lie
+  const int64_t q_step = 2 * kQ * a.q.token, d_step = 2 * kQ * a.d_o.token;
+  int head = kv * a.group, q_next = 0;
+  const char *q_at = nullptr, *d_at = nullptr;
+  const float* stat_at = nullptr;
+  auto begin = [&](int from) {
+    q_next = from * kQ;
+    q_at = rows_of(a.q, ragged, b, sq.first, head) + from * q_step;
+    d_at = rows_of(a.d_o, ragged, b, sq.first, head) + from * d_step;
+    stat_at = (wave == 0 ? a.off : a.delta) + (ragged ? head * a.q_tokens + sq.first : ((int64_t)b * a.q_heads + head) * a.q_len) + q_next;
+  };
+  auto load = [&](int to) {
+    lq.load(q_at, sq.count - q_next, base + (2 * to) * kBytes, wave);
+    ld.load(d_at, sq.count - q_next, base + (2 * to + 1) * kBytes, wave);
     if (wave < 2 && lane < kQ) {
-      const float* from = (wave == 0 ? a.off : a.delta) + stat;
-      auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, 4 * min(max(sq.count - q0, 0), kQ), 0x00020000);
+      auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(stat_at), 0, 4 * min(max(sq.count - q_next, 0), kQ), 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(base + kStatsAt + (2 * to + wave) * 4 * kQ), 4, 4 * lane, 0, 0, 0);
     }
+    q_next += kQ;
+    if (q_next < (q_begin + q_steps) * kQ) {
+      q_at += q_step;
+      d_at += d_step;
+      stat_at += kQ;
+    } else if (++head < (kv + 1) * a.group) {
+      begin(q_begin);
+    }
   };
-  int head = kv * a.group, q_at = q_begin;                       // of the step that is loaded next
+  int q_loaded = 0;
   if (step0 < step1) {
     head += step0 / q_steps;
-    q_at += step0 % q_steps;
+    begin(q_begin + step0 % q_steps);
+    q_loaded = q_next;
+    load(0);
   }
-  int q0 = q_at * kQ;
-  auto next = [&] { if (++q_at == q_begin + q_steps) { q_at = q_begin; ++head; } };
-  if (step0 < step1) { load(head, q0, 0); next(); }
   for (int t = step0; t < step1; ++t) {
     const int now = (t - step0) & 1;
     wait_for_tiles();
-    const int q_now = q0;
-    if (t + 1 < step1) { q0 = q_at * kQ; load(head, q0, now ^ 1); next(); }
+    const int q_now = q_loaded;
+    if (t + 1 < step1) { q_loaded = q_next; load(now ^ 1); }
     const uint32_t qt = lds_address(base) + (2 * now) * kBytes;
     const uint32_t kt = lds_address(base) + kKeysAt + wave * 32 * Tl::kRowBytes;
     const uint32_t stat = lds_address(base) + kStatsAt + now * (2 * 4 * kQ) + 16 * half;
