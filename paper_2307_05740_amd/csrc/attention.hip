@@ -3,12 +3,24 @@
 // A wavefront holds 32 queries and goes through tiles of 64 keys.  It computes the scores transposed, S^T = K Q^T, so that a
 // lane has one query's scores in its registers: the running maximum and sum of the softmax need one exchange, between lane halves, and
 // the probabilities are at once the B operand of O^T += V^T P^T.
+//
+// Four wavefronts share the tiles and have 128 queries together.  Where that gives too few workgroups to fill the chip, the four have the
+// same 32 queries, tiles of 32 keys in turn and of their own, and join their results in LDS.
+#include <algorithm>
+
 #include "attention_common.h"
 
 namespace arrow {
 namespace {
 
-constexpr int kStep = 64;   // keys of a tile
+// Whether workgroups of 32 queries are faster than `blocks` of 128: up to 64 of those, 128 for small heads, and twice as many where a row
+// sees 2000 keys or more, whose tiles the four wavefronts go through four times as fast (us, of 128 -> of 32 queries):
+//   heads of 64:   8 blocks  7.2 ->  5.8, 64 blocks 11.4 ->  7.2, 128 blocks 11.7 ->  9.6, 256 blocks 17.0 -> 22.1, of 4000 keys 56.8 -> 40.9
+//   heads of 128:  8 blocks  8.6 ->  7.1, 64 blocks 13.8 -> 10.0, 128 blocks 15.5 -> 20.6, of 2000 keys 39.5 -> 27.3, 256 of 4000 73.8 -> 78.1
+bool few_blocks(int64_t blocks, const AttentionArgs& a) {
+  const int64_t seen = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks, a.k_len) : a.k_len;
+  return blocks <= (a.dim <= 64 ? 128 : 64) * (seen >= 2000 ? 2 : 1);
+}
 
 // One row of the result in plain steps, the wavefront's lanes over its columns, by the row's own visible keys alone.  Matrix
 // instructions multiply what a query does not see by a probability of 0, and that is no zero where a value there is infinite or NaN:
@@ -32,10 +44,16 @@ __device__ __noinline__ void plain_row(const T* q, const char* k, const char* v,
   if (mine) { o[d] = (T)a0; o[d + 1] = (T)a1; }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a, int tiles) {
+template <typename T, int D, bool kShare>
+__global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
-  __shared__ __align__(1024) unsigned char smem[4][kStep * Tl::kRowBytes];   // keys and values, two tiles each
+  constexpr int kStep = kShare ? 64 : 32;                     // keys of a tile
+  constexpr int kTurns = kShare ? 1 : 4;                      // a wavefront has every kTurns-th tile
+  constexpr int kBytes = kStep * Tl::kRowBytes;
+  // keys and values, two tiles each, of all wavefronts or of each one; joined afterwards: the sums of each, its maxima and totals
+  constexpr int kRoom = 4 * kTurns * kBytes;
+  static_assert(kShare || kRoom >= 4 * D * 32 * 4, "room for the sums");
+  __shared__ __align__(1024) unsigned char smem[kRoom + (kShare ? 0 : 4 * (2 * 64 * 4 + 8))];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   // query heads of one key head next to each other, then tiles of queries: they read the same keys
   int id = blockIdx.x;
@@ -44,10 +62,12 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
   const int kv = id % a.kv_heads, b = id / a.kv_heads, head = kv * a.group + g;
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
-  const int first = tile * kQueryTile;
+  constexpr int kRows = kShare ? kQueryTile : 32;
+  const int first = tile * kRows;
   if (first >= sq.count) return;
+  const int mine = first + (kShare ? wave * 32 : 0);          // the first of this wavefront's queries
   const int shift = sk.count - sq.count;                      // position of query 0
-  const int row = first + wave * 32 + (lane & 31);            // this lane's query
+  const int row = mine + (lane & 31);                         // this lane's query
   const bool there = row < sq.count;
   const int p = row + shift;
   const char* q = rows_of(a.q, ragged, b, sq.first, head);
@@ -62,10 +82,10 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     qf[s] = there && d < a.dim ? *(const x8<T>*)(q + 2 * ((int64_t)row * a.q.token + d)) : z;
   }
 
-  const int last = min(first + kQueryTile, sq.count) - 1 + shift;
+  const int last = min(first + kRows, sq.count) - 1 + shift;
   const SeenTiles seen = seen_tiles<kStep>(max(first + shift, 0), last, a.window, a.sinks);
   // of this wavefront's queries
-  const int low = first + wave * 32 + shift, high = min(low + 31, sk.count - 1);
+  const int low = mine + shift, high = min(low + 31, sk.count - 1);
 
   f32x16 acc[D / 32];
 #pragma unroll
@@ -73,19 +93,22 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
   const float c = a.scale * kLog2e;
   float top = minus_infinity(), total = 0.f;                  // of c times the scores; of this lane's keys
 
-  const Loader<D, kStep, 4> lk(wave, lane, a.k.token, a.dim), lv(wave, lane, a.v.token, a.dim);
-  lds_byte* base = (lds_byte*)smem;
+  const int sharer = kShare ? wave : 0;
+  const Loader<D, kStep, 4 / kTurns> lk(sharer, lane, a.k.token, a.dim), lv(sharer, lane, a.v.token, a.dim);
+  lds_byte* base = (lds_byte*)smem + (kShare ? 0 : wave * 4 * kBytes);
   const TileReads<D> my(lane);
   auto load = [&](int t, int to) {
     const int k0 = seen.at(t) * kStep;
-    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * (kStep * Tl::kRowBytes), wave);
-    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * (kStep * Tl::kRowBytes), wave);
+    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + 2 * to * kBytes, sharer);
+    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, sharer);
   };
-  if (seen.total > 0) load(0, 0);
-  for (int t = 0; t < seen.total; ++t) {
-    wait_for_tiles();
-    if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
-    const uint32_t kt = lds_address(base) + (2 * (t & 1)) * (kStep * Tl::kRowBytes), vt = kt + kStep * Tl::kRowBytes;
+  const int t0 = kShare ? 0 : wave;
+  if (t0 < seen.total) load(t0, 0);
+  for (int t = t0, now = 0; t < seen.total; t += kTurns, now ^= 1) {
+    if constexpr (kShare) wait_for_tiles();
+    else wait_for_own_tiles();
+    if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
+    const uint32_t kt = lds_address(base) + 2 * now * kBytes, vt = kt + kBytes;
     const int k0 = seen.at(t) * kStep;
     // no query of this wavefront sees the tile
     if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
@@ -151,35 +174,87 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
   }
 
   total = add_halves(total);
-  const float by = total > 0.f || total != total ? 1.f / total : 0.f;
-  const float lse = total == 0.f ? minus_infinity() : (top + __log2f(total)) * kLn2;
-  const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
-  if (a.lse && there && half == 0) a.lse[stat] = lse;
-  float test = 0.f;                                           // NaN where a result is not finite
-#pragma unroll
-  for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) { acc[m][i] *= by; test = fmaf(acc[m][i], 0.f, test); }
-  const bool finite_lse = lse - lse == 0.f;
-  uint64_t odd = __ballot(there && finite_lse && test != test);
-  odd = (odd | odd >> 32) & 0xffffffffu;
   T* o = (T*)rows_of(a.o, ragged, b, sq.first, head);
-  // (all lanes take part in the exchange; whether a row is stored is the same in both halves)
-  if (there && !(odd >> (lane & 31) & 1)) store_columns<T, D>(acc, o + (int64_t)row * a.o.token, half, a.dim);
-  while (odd) {
-    const int r = __builtin_ctzll(odd);
-    odd &= odd - 1;
-    const int at = first + wave * 32 + r;
-    plain_row<T>((const T*)q + (int64_t)at * a.q.token, k, v, o + (int64_t)at * a.o.token, a.k.token, a.v.token, a.dim, at + shift, a.window, a.sinks,
-                 a.scale, __shfl(lse, r, 64));
+  const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
+  // 1 / total, 0 for a row that sees nothing; the lanes that hold a result that is not finite though the row's sum is
+  auto over = [](float total) { return total > 0.f || total != total ? 1.f / total : 0.f; };
+  auto lse_of = [](float top, float total) { return total == 0.f ? minus_infinity() : (top + __log2f(total)) * kLn2; };
+  auto odd_rows = [&](float test, float lse) {
+    const uint64_t odd = __ballot(there && lse - lse == 0.f && test != test);
+    return (odd | odd >> 32) & 0xffffffffu;
+  };
+  auto plain_rows = [&](uint64_t odd, float lse) {
+    while (odd) {
+      const int r = __builtin_ctzll(odd), at = mine + r;
+      odd &= odd - 1;
+      plain_row<T>((const T*)q + (int64_t)at * a.q.token, k, v, o + (int64_t)at * a.o.token, a.k.token, a.v.token, a.dim, at + shift, a.window, a.sinks,
+                   a.scale, __shfl(lse, r, 64));
+    }
+  };
+  if constexpr (kShare) {
+    const float by = over(total), lse = lse_of(top, total);
+    if (a.lse && there && half == 0) a.lse[stat] = lse;
+    float test = 0.f;                                         // NaN where a result is not finite
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) { acc[m][i] *= by; test = fmaf(acc[m][i], 0.f, test); }
+    const uint64_t odd = odd_rows(test, lse);
+    // (all lanes take part in the exchange; whether a row is stored is the same in both halves)
+    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, D>(acc, o + (int64_t)row * a.o.token, half, a.dim);
+    plain_rows(odd, lse);
+  } else {
+    float *sums = (float*)smem, *tops = (float*)(smem + kRoom), *totals = tops + 4 * 64;
+    uint64_t* odds = (uint64_t*)(totals + 4 * 64);
+    __syncthreads();                                          // the tiles are done with
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[((wave * (D / 32) + m) * 16 + i) * 64 + lane] = acc[m][i];
+    tops[wave * 64 + lane] = top;
+    totals[wave * 64 + lane] = total;
+    __syncthreads();
+    float all = tops[lane], share[4];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) all = fmaxf(all, tops[w * 64 + lane]);
+    const float off = all == minus_infinity() ? 0.f : all;
+    total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      share[w] = __builtin_amdgcn_exp2f(tops[w * 64 + lane] - off);
+      total = fmaf(share[w], totals[w * 64 + lane], total);
+    }
+    const float by = over(total), lse = lse_of(all, total);
+    if (a.lse && there && half == 0 && wave == 0) a.lse[stat] = lse;
+    // a wavefront joins 32 columns
+    f32x16 r = (f32x16)(0.f);
+    float test = 0.f;
+    if (wave < D / 32) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[i] = fmaf(share[w], sums[((w * (D / 32) + wave) * 16 + i) * 64 + lane], r[i]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) { r[i] *= by; test = fmaf(r[i], 0.f, test); }
+    }
+    uint64_t odd = odd_rows(test, lse);
+    if (lane == 0) odds[wave] = odd;
+    __syncthreads();
+    odd = odds[0] | odds[1] | odds[2] | odds[3];
+    if (wave < D / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, o + (int64_t)row * a.o.token, half, a.dim);
+    if (wave == 0) plain_rows(odd, lse);
   }
 }
 
 template <typename T, int D>
 int forward(const AttentionArgs& a, void* stream) {
-  const int64_t tiles = (a.q_len + (int64_t)kQueryTile - 1) / kQueryTile, blocks = tiles * a.q_heads * a.batch;
+  const int64_t heads = (int64_t)a.q_heads * a.batch, tiles = ((int64_t)a.q_len + kQueryTile - 1) / kQueryTile;
+  const bool share = !few_blocks(tiles * heads, a);
+  const int64_t rows = share ? tiles : ((int64_t)a.q_len + 31) / 32, blocks = rows * heads;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
-  attention_forward_kernel<T, D><<<dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream>>>(a, (int)tiles);
+  const dim3 grid((unsigned)blocks), block(256);
+  if (share) attention_forward_kernel<T, D, true><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  else attention_forward_kernel<T, D, false><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
   return (int)hipGetLastError();
 }
 

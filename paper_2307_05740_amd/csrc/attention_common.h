@@ -120,28 +120,31 @@ __device__ __forceinline__ x8<T> read_columns(uint32_t at, int m, int skip) {
 // become 0: the buffer descriptor ends with the last row.
 template <int D, int ROWS, int WAVES>
 struct Loader {
-  static constexpr int kSteps = ROWS / (WAVES * Tile<D>::kRowsOfKiB);
-  static_assert(kSteps * WAVES * Tile<D>::kRowsOfKiB == ROWS && (WAVES * Tile<D>::kRowsOfKiB) % 16 == 0, "whole steps, one turn");
-  uint32_t offset, step;
-  bool inside;
-  int dim_bytes, stride_bytes, tile_bytes;                       // (of a tile whose rows are all there)
-  __device__ __forceinline__ Loader(int wave, int lane, int64_t stride, int dim) {
-    const int row = wave * Tile<D>::kRowsOfKiB + lane / Tile<D>::kPieces, piece = (lane % Tile<D>::kPieces) ^ Tile<D>::turn(row);
+  static constexpr int kStepRows = WAVES * Tile<D>::kRowsOfKiB, kSteps = ROWS / kStepRows;
+  static_assert(kSteps * kStepRows == ROWS, "whole steps");
+  // what step i changes of a row's turn
+  __device__ static constexpr int turn_of(int i) { return (D == 128 ? i * WAVES : 2 * i * WAVES) & 3; }
+  uint32_t offset;                                               // of this lane's row
+  int piece, dim;
+  int stride_bytes, tile_bytes;                                  // (of a tile whose rows are all there)
+  __device__ __forceinline__ Loader(int wave, int lane, int64_t stride, int dim_) {
+    const int row = wave * Tile<D>::kRowsOfKiB + lane / Tile<D>::kPieces;
+    piece = (lane % Tile<D>::kPieces) ^ Tile<D>::turn(row);
     stride_bytes = (int)(stride * 2);
-    dim_bytes = dim * 2;
-    tile_bytes = (ROWS - 1) * stride_bytes + dim_bytes;
-    offset = (uint32_t)(row * stride_bytes + piece * 16);
-    step = (uint32_t)(WAVES * Tile<D>::kRowsOfKiB * stride_bytes);
-    inside = piece * 8 < dim;
+    dim = dim_;
+    tile_bytes = (ROWS - 1) * stride_bytes + 2 * dim;
+    offset = (uint32_t)(row * stride_bytes);
   }
   // base: the tile's first row (the same in all lanes); rows: those that are there, any number
   __device__ __forceinline__ void load(const void* base, int rows, lds_byte* tile, int wave) const {
-    const int bytes = rows >= ROWS ? tile_bytes : rows > 0 ? (rows - 1) * stride_bytes + dim_bytes : 0;
+    const int bytes = rows >= ROWS ? tile_bytes : rows > 0 ? (rows - 1) * stride_bytes + 2 * dim : 0;
     auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i) {
+      const int p = piece ^ turn_of(i);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (i * WAVES + wave) * 1024), 16,
-                                               inside ? offset + i * step : 0xfffffff0u, 0, 0, 0);
+                                               8 * p < dim ? offset + (uint32_t)(i * kStepRows * stride_bytes + 16 * p) : 0xfffffff0u, 0, 0, 0);
+    }
   }
 };
 
@@ -176,26 +179,28 @@ __device__ __forceinline__ SeenTiles seen_tiles(int low, int high, int window, i
   return s;
 }
 
-// A transposed result of D rows (columns of the operand) and 32 columns (its rows, this lane's at `to`), rounded and stored.  A lane has
-// columns 32 m + 16 u + 4 half + 0..3 and + 8..11; with the other half's it gets eight in a row.
+// 32 rows (columns 32 m on of the operand) of a transposed result and 32 columns (the operand's rows, this lane's at `to`), rounded and stored.  A lane
+// has columns 32 m + 16 u + 4 half + 0..3 and + 8..11; with the other half's it gets eight in a row.
+template <typename T>
+__device__ __forceinline__ void store_block(const f32x16& acc, int m, T* to, int half, int dim) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    union { x8<T> all; uint32_t w[4]; } r, x;
+    r.all = round8<T>(acc[8 * u], acc[8 * u + 1], acc[8 * u + 2], acc[8 * u + 3], acc[8 * u + 4], acc[8 * u + 5], acc[8 * u + 6], acc[8 * u + 7]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      auto y = __builtin_amdgcn_permlane32_swap(r.w[i], r.w[2 + i], false, false);
+      x.w[i] = y[0];
+      x.w[2 + i] = y[1];
+    }
+    const int d = 32 * m + 16 * u + 8 * half;
+    if (d < dim) *(x8<T>*)(to + d) = x.all;
+  }
+}
 template <typename T, int D>
 __device__ __forceinline__ void store_columns(const f32x16* acc, T* to, int half, int dim) {
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      union { x8<T> all; uint32_t w[4]; } r, x;
-      r.all = round8<T>(acc[m][8 * u], acc[m][8 * u + 1], acc[m][8 * u + 2], acc[m][8 * u + 3], acc[m][8 * u + 4], acc[m][8 * u + 5],
-                        acc[m][8 * u + 6], acc[m][8 * u + 7]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        auto y = __builtin_amdgcn_permlane32_swap(r.w[i], r.w[2 + i], false, false);
-        x.w[i] = y[0];
-        x.w[2 + i] = y[1];
-      }
-      const int d = 32 * m + 16 * u + 8 * half;
-      if (d < dim) *(x8<T>*)(to + d) = x.all;
-    }
+  for (int m = 0; m < D / 32; ++m) store_block<T>(acc[m], m, to, half, dim);
 }
 
 // Where the sums of a part of a key tile lie in the workspace, counted in pairs (dk, dv): only tiles in several parts have places.
@@ -229,6 +234,13 @@ __device__ __forceinline__ void wait_for_tiles() {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
+// The same for tiles that only this wavefront loads and reads.
+__device__ __forceinline__ void wait_for_own_tiles() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 }  // namespace

@@ -97,6 +97,19 @@ def test_head_layouts(torch, Attention, dtype, dim, heads, kv):
             check_sequence(torch, {n: t[b] for n, t in got.items()}, q[b], k[b], v[b], window, sinks, 0.2, d_o[b])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [40, 64, 80, 128])
+@pytest.mark.parametrize("queries,keys", [(400, 400), (385, 700), (430, 250)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 1), (90, 5), (200, 130)])
+def test_many_heads(torch, Attention, dtype, dim, queries, keys, window, sinks):
+    """Enough rows for wavefronts to share tiles of keys."""
+    q, d_o = (normal(torch, s, dtype, 3, queries, 12, dim, by=b) for s, b in ((1, 2.0), (4, 1.0)))
+    k, v = (normal(torch, s, dtype, 3, keys, 4, dim) for s in (2, 3))
+    got = run(torch, Attention(window, sinks), q, k, v, d_o)
+    for b in range(3):
+        check_sequence(torch, {n: t[b] for n, t in got.items()}, q[b], k[b], v[b], window, sinks, d_o=d_o[b])
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (150, 4), (64, 300)])
 def test_long_sequences_in_parts(torch, Attention, window, sinks):
     """Enough tiles for keys that all queries see to be cut into parts, and for the loads to go round both halves of their room."""
@@ -166,6 +179,21 @@ def test_what_is_not_seen_does_not_count(torch, Attention, bad):
     offsets = torch.tensor([0, 100], dtype=torch.int32, device="cuda")
     o, _ = Attention(window, sinks).forward(q[0], k[0], v[0], q_offsets=offsets, k_offsets=offsets)
     within(torch, "o of a sequence that ends there", o[:100, 0], want["o"][:100], bound["o"][:100])
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_is_not_seen_does_not_count_for_many_heads(torch, Attention, bad):
+    """The same where wavefronts share tiles of keys; a row is the same for every head."""
+    q, k, v = (normal(torch, s, "bfloat16", 1, 300, 1, 64) for s in (1, 2, 3))
+    window, sinks = 50, 4
+    want, bound = oracle.attention(q[0, :, 0], k[0, :, 0], v[0, :, 0], window, sinks)
+    k[0, 100:102], v[0, 100:102] = bad, bad
+    o, lse = Attention(window, sinks).forward(q.expand(-1, -1, 60, -1), k, v)
+    rows = [i for i in range(300) if not (100 <= i < 151)]
+    for h in (0, 59):
+        within(torch, "o", o[0, rows, h], want["o"][rows], bound["o"][rows])
+        within(torch, "lse", lse[0, h, rows], want["lse"][rows], bound["lse"][rows])
+    assert all(torch.equal(o[:, :, 0].view(torch.int16), o[:, :, h].view(torch.int16)) for h in range(60))
 
 
 def test_large_scores(torch, Attention):
