@@ -166,6 +166,10 @@ class ArrowAttention:
                 _address(dv), _address(ws), ws.numel(), self._stream()))
         return dq, dk, dv
 
+    def __call__(self, q, k, v, q_offsets=None, k_offsets=None, q_len=None, k_len=None):
+        """o as ``forward`` gives it, with its gradient for torch's autograd."""
+        return _attention_function().apply(self, q, k, v, q_offsets, k_offsets, q_len, k_len)
+
     # ---- a cache in pages ---------------------------------------------------------------------------------------------
     def _cache(self, k_cache, v_cache, table, lengths, q_heads: int, max_len) -> arrow_cache_t:
         torch = self._torch
@@ -236,3 +240,31 @@ class ArrowAttention:
                                                         _address(k_cache), _address(v_cache), _address(o), steps[3], _address(ws), ws.numel(),
                                                         self._stream()))
         return o
+
+
+_function = None
+
+
+def _attention_function():
+    """The call as a node of torch's autograd."""
+    global _function
+    if _function is None:
+        import torch
+
+        class Attention(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, op, q, k, v, *lengths):
+                o, lse = op.forward(q, k, v, None, None, *lengths)
+                ctx.save_for_backward(q, k, v, o, lse, *lengths[:2])
+                ctx.op, ctx.limits = op, lengths[2:]
+                return o
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, d_o):
+                q, k, v, o, lse, *offsets = ctx.saved_tensors
+                d_o = d_o if d_o.stride(-1) == 1 and all(s % 8 == 0 for s in d_o.stride()[:-1]) else d_o.contiguous()
+                return None, *ctx.op.backward(d_o, q, k, v, o, lse, None, None, None, *offsets, *ctx.limits), None, None, None, None
+
+        _function = Attention
+    return _function

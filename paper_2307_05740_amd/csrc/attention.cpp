@@ -86,6 +86,13 @@ AttentionArgs plan(const arrow_attention_t* a) {
   // Gradients of keys: a workgroup has the queries that see a tile of keys, in steps of 64 queries of a head.
   const int64_t tiles = ceil_div(a->k_len, kKeyTile), all = ceil_div(a->q_len, kQueryStep) * p.group;
   const int64_t usual = p.window ? std::min(all, (ceil_div((int64_t)p.window + kKeyTile, kQueryStep) + 1) * p.group) : all;
+  // Workgroups of 32 keys, whose wavefronts take the steps in turn, are faster than ones of 128 where there are few of those and each has
+  // few steps (gradients in us, of 128 -> of 32 keys, heads of 64 and of 128):
+  //   32 workgroups of 8 steps 28 -> 24, 47 -> 36;  64 of 7 steps 36 -> 31, 58 -> 48;  64 of 32 steps 40 -> 42, 69 -> 69
+  //   128 of 7 steps 38 -> 45, 63 -> 68;  16 of 32 steps, cut into parts, 33 -> 38, 55 -> 57
+  p.tile_parts = p.sink_parts = 1;
+  p.few_keys = tiles * a->kv_heads * a->batch <= 64 && usual > 1 && usual <= 16;
+  if (p.few_keys) return p;
   p.sink_tiles = (int32_t)std::min(tiles, ceil_div(p.sinks, kKeyTile));
   // A tile is cut into parts where that fills the chip better: the time goes by the rounds of workgroups that it holds at once, and a
   // part costs about as much as kPartSteps steps more, for its sums on their way through memory.

@@ -15,13 +15,18 @@ namespace {
 // D is <do_i, o_i> as well, but o has been rounded, and where a row has one large probability dS is a small difference of <do_i, v_j>
 // and D.  dS is formed with <do_i, o_i>; its error e = -sum_j dS(i,j) comes out with the row, in 32 bits, and dq is put right with
 // e sum_j P(i,j) k_j, one product more.
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, int tiles) {
+//
+// kShare: as in the forward kernel, wavefronts of 32 queries each share tiles of keys, or have the same 32 and every fourth tile.
+template <typename T, int D, bool kShare>
+__global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
   constexpr bool kQueriesInLds = D > 64;                         // no registers are left for them
-  constexpr int kStep = kQueriesInLds ? 32 : 64, kBytes = kStep * Tl::kRowBytes;   // keys of a tile
-  constexpr int kQueriesAt = 4 * kBytes;                         // k and v, two tiles each; the queries
-  __shared__ __align__(1024) unsigned char smem[kQueriesAt + (kQueriesInLds ? kQueryTile * Tl::kRowBytes : 0)];
+  constexpr int kStep = kQueriesInLds || !kShare ? 32 : 64, kBytes = kStep * Tl::kRowBytes;   // keys of a tile
+  constexpr int kTurns = kShare ? 1 : 4, kRows = kShare ? kQueryTile : 32;
+  // k and v, two tiles each, of all wavefronts or of each one, or their sums to be joined; the queries; sums of dS to be joined
+  constexpr int kQueriesAt = 4 * kTurns * kBytes, kRestAt = kQueriesAt + (kQueriesInLds ? kRows * Tl::kRowBytes : 0);
+  static_assert(kShare || kQueriesAt >= 4 * 2 * D * 32 * 4, "room for the sums");
+  __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 4 * 64 * 4)];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   int id = blockIdx.x;
   const int g = id % a.group; id /= a.group;
@@ -29,10 +34,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
   const int kv = id % a.kv_heads, b = id / a.kv_heads, head = kv * a.group + g;
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
-  const int first = tile * kQueryTile;
+  const int first = tile * kRows;
   if (first >= sq.count) return;
   const int shift = sk.count - sq.count;
-  const int row = first + wave * 32 + (lane & 31);
+  const int mine = first + (kShare ? wave * 32 : 0);
+  const int row = mine + (lane & 31);
   const bool there = row < sq.count;
   const int p = row + shift;
   const char* q = rows_of(a.q, ragged, b, sq.first, head);
@@ -40,11 +46,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
   const char* o = rows_of(a.o, ragged, b, sq.first, head);
   const char* d_o = rows_of(a.d_o, ragged, b, sq.first, head);
-  lds_byte* base = (lds_byte*)smem;
+  lds_byte *room = (lds_byte*)smem, *base = room + (kShare ? 0 : wave * 4 * kBytes);
 
   x8<T> qf[kQueriesInLds ? 1 : D / 16], df[D / 16];
   if constexpr (kQueriesInLds)                                   // (waited for with the first tiles)
-    Loader<D, kQueryTile, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, base + kQueriesAt, wave);
+    Loader<D, kRows, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, room + kQueriesAt, wave);
   float delta = 0.f;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
@@ -62,27 +68,32 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
   // of a row that sees nothing, infinity: its probabilities are masked
   const float off = there ? -a.lse_in[stat] / a.scale : 0.f;
 
-  const int last = min(first + kQueryTile, sq.count) - 1 + shift;
+  const int last = min(first + kRows, sq.count) - 1 + shift;
   const SeenTiles seen = seen_tiles<kStep>(max(first + shift, 0), last, a.window, a.sinks);
-  const int low = first + wave * 32 + shift, high = min(low + 31, sk.count - 1);
+  const int low = mine + shift, high = min(low + 31, sk.count - 1);
   const float c = a.scale * kLog2e;
 
-  const Loader<D, kStep, 4> lk(wave, lane, a.k.token, a.dim), lv(wave, lane, a.v.token, a.dim);
+  const int sharer = kShare ? wave : 0;
+  const Loader<D, kStep, 4 / kTurns> lk(sharer, lane, a.k.token, a.dim), lv(sharer, lane, a.v.token, a.dim);
   const TileReads<D> my(lane);
   auto load = [&](int t, int to) {
     const int k0 = seen.at(t) * kStep;
-    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * kBytes, wave);
-    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, wave);
+    lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * kBytes, sharer);
+    lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, sharer);
   };
   f32x16 acc[D / 32], pk[D / 32];                             // dS K and P K
 #pragma unroll
   for (int m = 0; m < D / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
   float rest = 0.f;                                           // sum of dS of this lane's keys
-  if (seen.total > 0) load(0, 0);
-  for (int t = 0; t < seen.total; ++t) {
-    wait_for_tiles();
-    if (t + 1 < seen.total) load(t + 1, (t + 1) & 1);
-    const uint32_t kt = lds_address(base) + (2 * (t & 1)) * kBytes, vt = kt + kBytes, qt = lds_address(base) + kQueriesAt + wave * 32 * Tl::kRowBytes;
+  const int t0 = kShare ? 0 : wave;
+  if (t0 < seen.total) load(t0, 0);
+  if constexpr (!kShare && kQueriesInLds) wait_for_tiles();     // (all wavefronts' queries)
+  for (int t = t0, now = 0; t < seen.total; t += kTurns, now ^= 1) {
+    if constexpr (kShare) wait_for_tiles();
+    else wait_for_own_tiles();
+    if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
+    const uint32_t kt = lds_address(base) + 2 * now * kBytes, vt = kt + kBytes;
+    const uint32_t qt = lds_address(room) + kQueriesAt + sharer * 32 * Tl::kRowBytes;
     const int k0 = seen.at(t) * kStep;
     if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
     const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
@@ -129,16 +140,48 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
   }
 
   rest = add_halves(rest);
-  if (there && half == 0) {
-    a.off[stat] = off;
-    a.delta[stat] = -(delta + rest);
-  }
   T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
+  if constexpr (kShare) {
+    if (there && half == 0) {
+      a.off[stat] = off;
+      a.delta[stat] = -(delta + rest);
+    }
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < D / 32; ++m)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-rest, pk[m][i], acc[m][i]);
-  if (there) store_columns<T, D>(acc, dq, half, a.dim);
+      for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-rest, pk[m][i], acc[m][i]);
+    if (there) store_columns<T, D>(acc, dq, half, a.dim);
+  } else {
+    float *sums = (float*)smem, *rests = (float*)(smem + kRestAt);
+    __syncthreads();                                            // the tiles are done with
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sums[((wave * (D / 32) + m) * 32 + i) * 64 + lane] = acc[m][i];
+        sums[((wave * (D / 32) + m) * 32 + 16 + i) * 64 + lane] = pk[m][i];
+      }
+    rests[wave * 64 + lane] = rest;
+    __syncthreads();
+    rest = rests[lane] + rests[64 + lane] + rests[128 + lane] + rests[192 + lane];
+    if (there && half == 0 && wave == 0) {
+      a.off[stat] = off;
+      a.delta[stat] = -(delta + rest);
+    }
+    if (wave >= D / 32) return;
+    f32x16 r;                                                   // a wavefront joins 32 columns
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x = 0.f, y = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        x += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
+        y += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+      }
+      r[i] = a.scale * fmaf(-rest, y, x);
+    }
+    if (there) store_block<T>(r, wave, dq, half, a.dim);
+  }
 }
 
 // dk and dv of 128 keys, 32 per wavefront, over the queries of all heads that share them.  Scores are not transposed here: a lane
@@ -146,14 +189,18 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a, i
 //
 // Parts: part i of n takes the steps (64 queries of one head) from i / n to (i + 1) / n of the tile's; with n > 1 their sums go
 // to the workspace and attention_join_kernel adds them up in order.
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, int tiles) {
+//
+// kShare: wavefronts of 32 keys each share steps, or have the same 32 and every fourth step; tiles are in one part then.
+template <typename T, int D, bool kShare>
+__global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
   constexpr bool kKeysInLds = D > 64;
-  constexpr int kQ = kKeysInLds ? 32 : 64, kBytes = kQ * Tl::kRowBytes;   // queries of a step
-  // q and do, two tiles each; the keys; what the dq kernel noted of each query, two steps'
-  constexpr int kKeysAt = 4 * kBytes, kStatsAt = kKeysAt + (kKeysInLds ? kKeyTile * Tl::kRowBytes : 0);
-  __shared__ __align__(1024) unsigned char smem[kStatsAt + 2 * 2 * 4 * kQ];
+  constexpr int kQ = kKeysInLds || !kShare ? 32 : 64, kBytes = kQ * Tl::kRowBytes;   // queries of a step
+  constexpr int kTurns = kShare ? 1 : 4, kKeys = kShare ? kKeyTile : 32;
+  // q and do, two tiles each, of all wavefronts or of each one, or their sums to be joined; the keys; what the dq kernel noted of each query, two steps'
+  constexpr int kKeysAt = 4 * kTurns * kBytes, kStatsAt = kKeysAt + (kKeysInLds ? kKeys * Tl::kRowBytes : 0), kStatsBytes = 2 * 2 * 4 * kQ;
+  static_assert(kShare || kKeysAt >= 4 * 2 * D * 32 * 4, "room for the sums");
+  __shared__ __align__(1024) unsigned char smem[kStatsAt + kTurns * kStatsBytes];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   // an item of every head and sequence in turn; the longest first, and last the small parts of keys that all queries see
   const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;
@@ -165,16 +212,17 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
   const int part = (sink ? item - usual : item) % parts;
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
-  const int first = tile * kKeyTile;
+  const int first = tile * kKeys;
   if (first >= sk.count) return;
   const int shift = sk.count - sq.count;
-  const int key = first + wave * 32 + (lane & 31);
+  const int mine = first + (kShare ? wave * 32 : 0);
+  const int key = mine + (lane & 31);
   const bool there = key < sk.count;
   const char* k = rows_of(a.k, ragged, b, sk.first, kv);
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
   x8<T> kf[kKeysInLds ? 1 : D / 16], vf[D / 16];
   if constexpr (kKeysInLds)                                      // (waited for with the first step's tiles)
-    Loader<D, kKeyTile, 4>(wave, lane, a.k.token, a.dim).load(k + 2 * (int64_t)first * a.k.token, sk.count - first, (lds_byte*)smem + kKeysAt, wave);
+    Loader<D, kKeys, 4>(wave, lane, a.k.token, a.dim).load(k + 2 * (int64_t)first * a.k.token, sk.count - first, (lds_byte*)smem + kKeysAt, wave);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
     const int d = 16 * s + 8 * half;
@@ -188,7 +236,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
   for (int m = 0; m < D / 32; ++m) { dk[m] = (f32x16)(0.f); dv[m] = (f32x16)(0.f); }
 
   // queries that see one of the tile's keys: positions first .. end
-  const int tile_end = min(first + kKeyTile, sk.count) - 1;
+  const int tile_end = min(first + kKeys, sk.count) - 1;
   int end = sk.count - 1;
   if (a.window && first >= a.sinks) end = (int)min((int64_t)end, (int64_t)tile_end + a.window - 1);
   const int q_begin = max(first - shift, 0) / kQ;
@@ -197,52 +245,64 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
   const int step0 = (int)((int64_t)steps * part / parts), step1 = (int)((int64_t)steps * (part + 1) / parts);
   const float c = a.scale * kLog2e;
 
-  const Loader<D, kQ, 4> lq(wave, lane, a.q.token, a.dim), ld(wave, lane, a.d_o.token, a.dim);
-  lds_byte* base = (lds_byte*)smem;
+  const int sharer = kShare ? wave : 0;
+  const Loader<D, kQ, 4 / kTurns> lq(sharer, lane, a.q.token, a.dim), ld(sharer, lane, a.d_o.token, a.dim);
+  lds_byte *room = (lds_byte*)smem, *base = room + (kShare ? 0 : wave * 4 * kBytes);
+  lds_byte* stats = room + kStatsAt + (kShare ? 0 : wave * kStatsBytes);
   const TileReads<D> my(lane);
   // the step that is loaded next: a head's queries from q_next on, and where they lie
   const int64_t q_step = 2 * kQ * a.q.token, d_step = 2 * kQ * a.d_o.token;
   int head = kv * a.group, q_next = 0;
   const char *q_at = nullptr, *d_at = nullptr;
-  const float* stat_at = nullptr;
+  int64_t stat_at = 0;
   auto begin = [&](int from) {
     q_next = from * kQ;
     q_at = rows_of(a.q, ragged, b, sq.first, head) + from * q_step;
     d_at = rows_of(a.d_o, ragged, b, sq.first, head) + from * d_step;
-    stat_at = (wave == 0 ? a.off : a.delta) + (ragged ? head * a.q_tokens + sq.first : ((int64_t)b * a.q_heads + head) * a.q_len) + q_next;
+    stat_at = (ragged ? head * a.q_tokens + sq.first : ((int64_t)b * a.q_heads + head) * a.q_len) + q_next;
+  };
+  auto load_stats = [&](const float* from, lds_byte* at) {
+    auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, 4 * min(max(sq.count - q_next, 0), kQ), 0x00020000);
+    if (lane < kQ) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)at, 4, 4 * lane, 0, 0, 0);
   };
   auto load = [&](int to) {
-    lq.load(q_at, sq.count - q_next, base + (2 * to) * kBytes, wave);
-    ld.load(d_at, sq.count - q_next, base + (2 * to + 1) * kBytes, wave);
-    if (wave < 2 && lane < kQ) {
-      auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(stat_at), 0, 4 * min(max(sq.count - q_next, 0), kQ), 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(base + kStatsAt + (2 * to + wave) * 4 * kQ), 4, 4 * lane, 0, 0, 0);
-    }
-    q_next += kQ;
-    if (q_next < (q_begin + q_steps) * kQ) {
-      q_at += q_step;
-      d_at += d_step;
-      stat_at += kQ;
-    } else if (++head < (kv + 1) * a.group) {
-      begin(q_begin);
+    lq.load(q_at, sq.count - q_next, base + (2 * to) * kBytes, sharer);
+    ld.load(d_at, sq.count - q_next, base + (2 * to + 1) * kBytes, sharer);
+    if (!kShare || wave == 0) load_stats(a.off + stat_at, stats + 2 * to * 4 * kQ);
+    if (!kShare || wave == 1) load_stats(a.delta + stat_at, stats + (2 * to + 1) * 4 * kQ);
+    if constexpr (kShare) {
+      q_next += kQ;
+      if (q_next < (q_begin + q_steps) * kQ) {
+        q_at += q_step;
+        d_at += d_step;
+        stat_at += kQ;
+      } else if (++head < (kv + 1) * a.group) {
+        begin(q_begin);
+      }
+    } else {
+      int from = q_next / kQ + kTurns;
+      while (from >= q_begin + q_steps) { from -= q_steps; ++head; }
+      if (head < (kv + 1) * a.group) begin(from);
     }
   };
+  const int mine0 = step0 + (kShare ? 0 : wave);                 // this wavefront's first step
   int q_loaded = 0;
-  if (step0 < step1) {
-    head += step0 / q_steps;
-    begin(q_begin + step0 % q_steps);
+  if (mine0 < step1) {
+    head += mine0 / q_steps;
+    begin(q_begin + mine0 % q_steps);
     q_loaded = q_next;
     load(0);
   }
-  for (int t = step0; t < step1; ++t) {
-    const int now = (t - step0) & 1;
-    wait_for_tiles();
+  if constexpr (!kShare) wait_for_tiles();                       // (all wavefronts' keys)
+  for (int t = mine0, now = 0; t < step1; t += kTurns, now ^= 1) {
+    if constexpr (kShare) wait_for_tiles();
+    else wait_for_own_tiles();
     const int q_now = q_loaded;
-    if (t + 1 < step1) { q_loaded = q_next; load(now ^ 1); }
+    if (t + kTurns < step1) { q_loaded = q_next; load(now ^ 1); }
     const uint32_t qt = lds_address(base) + (2 * now) * kBytes;
-    const uint32_t kt = lds_address(base) + kKeysAt + wave * 32 * Tl::kRowBytes;
-    const uint32_t stat = lds_address(base) + kStatsAt + now * (2 * 4 * kQ) + 16 * half;
-    const int low = first + wave * 32, high = min(low + 31, sk.count - 1);   // this wavefront's keys
+    const uint32_t kt = lds_address(room) + kKeysAt + sharer * 32 * Tl::kRowBytes;
+    const uint32_t stat = lds_address(stats) + now * (2 * 4 * kQ) + 16 * half;
+    const int low = mine, high = min(low + 31, sk.count - 1);   // this wavefront's keys
 #pragma unroll
     for (int n = 0; n < kQ / 32; ++n) {
       const int p0 = q_now + n * 32 + shift;                     // position of the first of 32 queries
@@ -291,6 +351,33 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a, 
     }
   }
 
+  if constexpr (!kShare) {
+    float* sums = (float*)smem;
+    __syncthreads();                                             // the tiles are done with
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sums[((wave * (D / 32) + m) * 32 + i) * 64 + lane] = dk[m][i];
+        sums[((wave * (D / 32) + m) * 32 + 16 + i) * 64 + lane] = dv[m][i];
+      }
+    __syncthreads();
+    if (wave >= D / 32) return;
+    f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);                 // a wavefront joins 32 columns
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        x[i] += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
+        y[i] += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+      }
+      x[i] *= a.scale;
+    }
+    if (!there) return;
+    store_block<T>(x, wave, (T*)rows_of(a.dk, ragged, b, sk.first, kv) + (int64_t)key * a.dk.token, half, a.dim);
+    store_block<T>(y, wave, (T*)rows_of(a.dv, ragged, b, sk.first, kv) + (int64_t)key * a.dv.token, half, a.dim);
+    return;
+  }
 #pragma unroll
   for (int m = 0; m < D / 32; ++m) dk[m] *= a.scale;
   if (parts == 1) {
@@ -342,18 +429,27 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
       round8<T>(sum[0], sum[1], sum[2], sum[3], sum[4], sum[5], sum[6], sum[7]);
 }
 
+// Up to so many workgroups of 128 queries, those of 32 are faster (gradients in us, of 128 -> of 32 queries, heads of 64 and of 128):
+//   32 blocks 28 -> 25, 47 -> 39;  128 blocks, window of 256, 38 -> 37, 63 -> 62, no window 76 -> 61, 134 -> 97;  256 blocks 44 -> 52, 72 -> 94
+constexpr int64_t kFewQueryBlocks = 128;
+
 template <typename T, int D>
 int backward(const AttentionArgs& a, void* stream) {
-  const int64_t q_tiles = (a.q_len + (int64_t)kQueryTile - 1) / kQueryTile, q_blocks = q_tiles * a.q_heads * a.batch;
-  const int64_t k_tiles = (a.k_len + (int64_t)kKeyTile - 1) / kKeyTile;
-  const int64_t k_blocks = (a.sink_tiles * (int64_t)a.sink_parts + (k_tiles - a.sink_tiles) * a.tile_parts) * a.kv_heads * a.batch;
+  const int64_t q_heads = (int64_t)a.q_heads * a.batch, kv_heads = (int64_t)a.kv_heads * a.batch;
+  auto tiles_of = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
+  const bool q_share = tiles_of(a.q_len, kQueryTile) * q_heads > kFewQueryBlocks || a.k_len <= 64;   // (one tile or two)
+  const int64_t q_tiles = tiles_of(a.q_len, q_share ? kQueryTile : 32), k_tiles = tiles_of(a.k_len, a.few_keys ? 32 : kKeyTile);
+  const int64_t q_blocks = q_tiles * q_heads, k_blocks = (a.sink_tiles * (int64_t)a.sink_parts + (k_tiles - a.sink_tiles) * a.tile_parts) * kv_heads;
   const int first_cut = a.sink_parts > 1 ? 0 : a.sink_tiles, cut = (int)((a.tile_parts > 1 ? k_tiles : a.sink_tiles) - first_cut);
-  const int64_t join_blocks = cut > 0 ? ((int64_t)cut * a.kv_heads * a.batch * kKeyTile * (a.dim / 8) * 2 + 255) / 256 : 0;
+  const int64_t join_blocks = cut > 0 ? (cut * kv_heads * kKeyTile * (a.dim / 8) * 2 + 255) / 256 : 0;
   if (q_blocks > 0x7fffffff || k_blocks > 0x7fffffff || join_blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   hipStream_t s = (hipStream_t)stream;
-  if (q_blocks) attention_dq_kernel<T, D><<<dim3((unsigned)q_blocks), dim3(256), 0, s>>>(a, (int)q_tiles);
-  if (k_blocks) attention_dkv_kernel<T, D><<<dim3((unsigned)k_blocks), dim3(256), 0, s>>>(a, (int)k_tiles);
-  if (join_blocks) attention_join_kernel<T><<<dim3((unsigned)join_blocks), dim3(256), 0, s>>>(a, (int)k_tiles, cut, first_cut);
+  const dim3 q_grid((unsigned)q_blocks), k_grid((unsigned)k_blocks), block(256);
+  if (q_blocks && q_share) attention_dq_kernel<T, D, true><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  else if (q_blocks) attention_dq_kernel<T, D, false><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  if (k_blocks && !a.few_keys) attention_dkv_kernel<T, D, true><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
+  else if (k_blocks) attention_dkv_kernel<T, D, false><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
+  if (join_blocks) attention_join_kernel<T><<<dim3((unsigned)join_blocks), block, 0, s>>>(a, (int)k_tiles, cut, first_cut);
   return (int)hipGetLastError();
 }
 

@@ -29,6 +29,7 @@ struct AttentionArgs {
   // backward, keys: tiles of keys that some query sees for good (the first ones, with a window), and into how many parts
   // the work of those and of the others is cut
   int32_t sink_tiles, sink_parts, tile_parts;
+  bool few_keys;                   // workgroups of 32 keys, not 128; no tile is cut
 };
 
 struct CacheArgs {

@@ -38,8 +38,8 @@ class ArrowEmbedding:
     def _describe(self, ids, table, rows, grad_dtype=None) -> arrow_embedding_t:
         """`table`: W or dW, `rows`: Y or dY as (tokens, columns)."""
         torch = self._torch
-        if ids.dtype not in (torch.int32, torch.int64) or not ids.is_contiguous():
-            raise ValueError(f"ids are contiguous int32 or int64, not {ids.dtype}")
+        if ids.dtype not in (torch.int32, torch.int64):
+            raise ValueError(f"ids are int32 or int64, not {ids.dtype}")
         if rows.dtype not in self._dtypes:
             raise TypeError(f"embedding takes float32, bfloat16 and float16 tensors, not {rows.dtype}")
         if table.dim() != 2 or table.shape[0] != self.rows or rows.shape != (ids.numel(), table.shape[1]) or table.shape[1] < 1:
@@ -67,6 +67,7 @@ class ArrowEmbedding:
             if done is not None:
                 return _results(done)
         torch = self._torch
+        ids = ids.contiguous()
         shape = (*ids.shape, W.shape[-1])
         Y = torch.empty(shape, dtype=W.dtype, device=W.device) if Y is None else Y
         if Y.dtype != W.dtype or tuple(Y.shape) != shape:
@@ -77,6 +78,10 @@ class ArrowEmbedding:
             binding._check(lib().arrow_embedding_forward(ctypes.byref(e), W.data_ptr(), ids.data_ptr(), Y.data_ptr(), self._stream()))
         return Y
 
+    def __call__(self, W, ids):
+        """Y as ``forward`` gives it, with its gradient for torch's autograd."""
+        return _embedding_function().apply(self, W, ids)
+
     def backward(self, dY, ids, dW=None, dtype=None):
         """dW, (rows, columns), of dY (shape of ids, columns): every row is written.  dtype: dY's (the default) or float32."""
         if self._call is not None and dtype is None:
@@ -84,6 +89,7 @@ class ArrowEmbedding:
             if done is not None:
                 return _results(done)
         torch = self._torch
+        ids = ids.contiguous()
         if tuple(dY.shape[:-1]) != tuple(ids.shape) or dY.dim() < 2:
             raise ValueError(f"dY {tuple(dY.shape)} of ids {tuple(ids.shape)}")
         flat = dY if dY.dim() == 2 else dY.reshape(math.prod(ids.shape), dY.shape[-1])
@@ -97,3 +103,28 @@ class ArrowEmbedding:
             binding._check(lib().arrow_embedding_backward(ctypes.byref(e), flat.data_ptr(), ids.data_ptr(), dW.data_ptr(), ws.data_ptr(), ws.numel(),
                                                           self._stream()))
         return dW
+
+
+_function = None
+
+
+def _embedding_function():
+    """The call as a node of torch's autograd."""
+    global _function
+    if _function is None:
+        import torch
+
+        class Embedding(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, op, W, ids):
+                ctx.save_for_backward(ids)
+                ctx.op = op
+                return op.forward(W, ids)
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, dY):
+                return None, ctx.op.backward(dY.contiguous(), ctx.saved_tensors[0]), None
+
+        _function = Embedding
+    return _function
