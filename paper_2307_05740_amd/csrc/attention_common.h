@@ -63,6 +63,20 @@ __device__ __forceinline__ x8<T> round8(float a, float b, float c, float d, floa
   return r;
 }
 
+// Sum of eight values and of c, in 32 bits.
+__device__ __forceinline__ float add8(x8<__bf16> x, float c) {
+  const x2<__bf16> one = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) c = __builtin_amdgcn_fdot2_f32_bf16(x2<__bf16>{x[i], x[i + 1]}, one, c, false);
+  return c;
+}
+__device__ __forceinline__ float add8(x8<_Float16> x, float c) {
+  const x2<_Float16> one = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) c = __builtin_amdgcn_fdot2(x2<_Float16>{x[i], x[i + 1]}, one, c, false);
+  return c;
+}
+
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
 // A tile of rows of D 16-bit elements in LDS, in pieces of 16 bytes.  Piece c of row r lies at place c ^ turn(r) of the row, so

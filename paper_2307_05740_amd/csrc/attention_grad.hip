@@ -13,8 +13,10 @@ namespace {
 // are transposed, dS^T is at once the B operand of dQ^T += K^T dS^T.
 //
 // D is <do_i, o_i> as well, but o has been rounded, and where a row has one large probability dS is a small difference of <do_i, v_j>
-// and D.  dS is formed with <do_i, o_i>; its error e = -sum_j dS(i,j) comes out with the row, in 32 bits, and dq is put right with
-// e sum_j P(i,j) k_j, one product more.
+// and D.  dS is formed with <do_i, o_i>; the error -sum_j dS(i,j) of that comes out with the row, in 32 bits.  dq is put right with one
+// product more, sum_j P(i,j) k_j times that sum.  Workgroups of few rows, where all sequences of up to 64 keys are, take the sum of the dS as
+// they were rounded for their product: the weights then add up to nothing, as the true gradient's do, which a row of few keys notices
+// (dq of 5 keys off by 1.55 times what rounding dq alone does, and 1.4 so; for long rows the same, and 15 % of the kernel's time).
 //
 // kShare: as in the forward kernel, wavefronts of 32 queries each share tiles of keys, or have the same 32 and every fourth tile.
 template <typename T, int D, bool kShare>
@@ -26,7 +28,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   // k and v, two tiles each, of all wavefronts or of each one, or their sums to be joined; the queries; sums of dS to be joined
   constexpr int kQueriesAt = 4 * kTurns * kBytes, kRestAt = kQueriesAt + (kQueriesInLds ? kRows * Tl::kRowBytes : 0);
   static_assert(kShare || kQueriesAt >= 4 * 2 * D * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 4 * 64 * 4)];
+  __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 2 * 4 * 64 * 4)];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   int id = blockIdx.x;
   const int g = id % a.group; id /= a.group;
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   f32x16 acc[D / 32], pk[D / 32];                             // dS K and P K
 #pragma unroll
   for (int m = 0; m < D / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
-  float rest = 0.f;                                           // sum of dS of this lane's keys
+  float rest = 0.f, kept = 0.f;                               // sums of dS of this lane's keys, before and after they are rounded
   const int t0 = kShare ? 0 : wave;
   if (t0 < seen.total) load(t0, 0);
   if constexpr (!kShare && kQueriesInLds) wait_for_tiles();     // (all wavefronts' queries)
@@ -128,6 +130,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
       for (int u = 0; u < 2; ++u) {
         const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
         const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
+        if constexpr (!kShare) kept = add8(ds, kept);
 #pragma unroll
         for (int m = 0; m < D / 32; ++m) {
           const x8<T> kf = read_columns<T, D>(kt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes);
@@ -140,6 +143,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   }
 
   rest = add_halves(rest);
+  kept = kShare ? rest : add_halves(kept);
   T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
   if constexpr (kShare) {
     if (there && half == 0) {
@@ -149,7 +153,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
 #pragma unroll
     for (int m = 0; m < D / 32; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-rest, pk[m][i], acc[m][i]);
+      for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
     if (there) store_columns<T, D>(acc, dq, half, a.dim);
   } else {
     float *sums = (float*)smem, *rests = (float*)(smem + kRestAt);
@@ -162,8 +166,14 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
         sums[((wave * (D / 32) + m) * 32 + 16 + i) * 64 + lane] = pk[m][i];
       }
     rests[wave * 64 + lane] = rest;
+    rests[(4 + wave) * 64 + lane] = kept;
     __syncthreads();
-    rest = rests[lane] + rests[64 + lane] + rests[128 + lane] + rests[192 + lane];
+    rest = kept = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      rest += rests[w * 64 + lane];
+      kept += rests[(4 + w) * 64 + lane];
+    }
     if (there && half == 0 && wave == 0) {
       a.off[stat] = off;
       a.delta[stat] = -(delta + rest);
@@ -178,7 +188,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
         x += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
         y += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
       }
-      r[i] = a.scale * fmaf(-rest, y, x);
+      r[i] = a.scale * fmaf(-kept, y, x);
     }
     if (there) store_block<T>(r, wave, dq, half, a.dim);
   }
