@@ -116,6 +116,12 @@ struct TileReads {
     columns = row * Tile<D>::kRowBytes + ((piece ^ Tile<D>::turn(row)) << 4) + ((i & 1) << 3);
   }
 };
+// The same value, computed where it stands: what is derived from it is not kept in registers from one round of a loop to the next.
+template <typename X>
+__device__ __forceinline__ X here(X x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 // A or B of a tile's rows (32 from a multiple of 32 on, `skip` bytes into the tile) and its columns 16 s .. 16 s + 15: lane l has row l % 32,
 // columns 16 s + 8 (l / 32) + 0..7.  at: the tile's address + TileReads::rows.
 template <typename T>

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
     else wait_for_own_tiles();
     if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
     const uint32_t kt = lds_address(base) + 2 * now * kBytes, vt = kt + kBytes;
-    const uint32_t qt = lds_address(room) + kQueriesAt + sharer * 32 * Tl::kRowBytes;
+    const uint32_t qt = kQueriesInLds ? here(lds_address(room) + kQueriesAt + sharer * 32 * Tl::kRowBytes + my.rows) : 0;
     const int k0 = seen.at(t) * kStep;
     if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
     const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
@@ -103,10 +103,11 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
     const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
 #pragma unroll
     for (int n = 0; n < kStep / 32; ++n) {
-      f32x16 s = (f32x16)(off), e = (f32x16)(-delta);         // the products begin with what is taken off them
+      // the products begin with what is taken off them (which is in one register each, not in 16 ready for that, where those are needed)
+      f32x16 s = (f32x16)(kQueriesInLds ? here(off) : off), e = (f32x16)(kQueriesInLds ? here(-delta) : -delta);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
-        s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt + my.rows, i, 0) : qf[kQueriesInLds ? 0 : i], s);
+        s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt, i, 0) : qf[kQueriesInLds ? 0 : i], s);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
       reads_ahead<4, D / 16, kQueriesInLds ? 2 : 1, D / 16, 1>();
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dkv_kernel(Atte
     const int q_now = q_loaded;
     if (t + kTurns < step1) { q_loaded = q_next; load(now ^ 1); }
     const uint32_t qt = lds_address(base) + (2 * now) * kBytes;
-    const uint32_t kt = lds_address(room) + kKeysAt + sharer * 32 * Tl::kRowBytes;
+    const uint32_t kt = lds_address(room) + kKeysAt + sharer * 32 * Tl::kRowBytes + my.rows;
     const uint32_t stat = lds_address(stats) + now * (2 * 4 * kQ) + 16 * half;
     const int low = mine, high = min(low + 31, sk.count - 1);   // this wavefront's keys
 #pragma unroll
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dkv_kernel(Atte
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
-        s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), kKeysInLds ? read_rows<T>(kt + my.rows, i, 0) : kf[kKeysInLds ? 0 : i], s);
+        s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), kKeysInLds ? read_rows<T>(kt, i, 0) : kf[kKeysInLds ? 0 : i], s);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
       reads_ahead<kKeysInLds ? 16 : 12, D / 16, kKeysInLds ? 2 : 1, D / 16, 1>();   // (eight of those ahead: what the products begin with)
