@@ -30,10 +30,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   static_assert(kShare || kQueriesAt >= 4 * 2 * D * 32 * 4, "room for the sums");
   __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 2 * 4 * 64 * 4)];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
-  int id = blockIdx.x;
-  const int g = id % a.group; id /= a.group;
-  const int tile = tiles - 1 - id % tiles; id /= tiles;
-  const int kv = id % a.kv_heads, b = id / a.kv_heads, head = kv * a.group + g;
+  const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;   // as in the forward kernel
+  const int g = item % a.group, tile = tiles - 1 - item / a.group;
+  const int kv = unit % a.kv_heads, b = unit / a.kv_heads, head = kv * a.group + g;
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
   const int first = tile * kRows;
