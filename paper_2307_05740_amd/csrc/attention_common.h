@@ -146,24 +146,24 @@ struct Loader {
   __device__ static constexpr int turn_of(int i) { return (D == 128 ? i * WAVES : 2 * i * WAVES) & 3; }
   uint32_t offset;                                               // of this lane's row
   int piece, dim;
-  int stride_bytes, tile_bytes;                                  // (of a tile whose rows are all there)
+  uint32_t stride_bytes, tile_bytes;                             // (of a tile whose rows are all there; 127 of the longest steps are below 2^32)
   __device__ __forceinline__ Loader(int wave, int lane, int64_t stride, int dim_) {
     const int row = wave * Tile<D>::kRowsOfKiB + lane / Tile<D>::kPieces;
     piece = (lane % Tile<D>::kPieces) ^ Tile<D>::turn(row);
-    stride_bytes = (int)(stride * 2);
+    stride_bytes = (uint32_t)(stride * 2);
     dim = dim_;
     tile_bytes = (ROWS - 1) * stride_bytes + 2 * dim;
-    offset = (uint32_t)(row * stride_bytes);
+    offset = row * stride_bytes;
   }
   // base: the tile's first row (the same in all lanes); rows: those that are there, any number
   __device__ __forceinline__ void load(const void* base, int rows, lds_byte* tile, int wave) const {
-    const int bytes = rows >= ROWS ? tile_bytes : rows > 0 ? (rows - 1) * stride_bytes + 2 * dim : 0;
-    auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+    const uint32_t bytes = rows >= ROWS ? tile_bytes : rows > 0 ? (rows - 1) * stride_bytes + 2 * dim : 0;
+    auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       const int p = piece ^ turn_of(i);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (i * WAVES + wave) * 1024), 16,
-                                               8 * p < dim ? offset + (uint32_t)(i * kStepRows * stride_bytes + 16 * p) : 0xfffffff0u, 0, 0, 0);
+                                               8 * p < dim ? offset + i * kStepRows * stride_bytes + 16 * p : 0xfffffff0u, 0, 0, 0);
     }
   }
 };

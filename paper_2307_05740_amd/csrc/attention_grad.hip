@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   // k and v, two tiles each, of all wavefronts or of each one, or their sums to be joined; the queries; sums of dS to be joined
   constexpr int kQueriesAt = 4 * kTurns * kBytes, kRestAt = kQueriesAt + (kQueriesInLds ? kRows * Tl::kRowBytes : 0);
   static_assert(kShare || kQueriesAt >= 4 * 2 * D * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 2 * 4 * 64 * 4)];
+  __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 2 * 4 * 64 * 4 + 4 * 8)];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;   // as in the forward kernel
   const int g = item % a.group, tile = tiles - 1 - item / a.group;
@@ -145,6 +145,36 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   rest = add_halves(rest);
   kept = kShare ? rest : add_halves(kept);
   T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
+  // Rows to be done in plain steps, as in the forward kernel: with a result that is not finite, though what they see may be
+  auto odd_rows = [&](float test) {
+    const uint64_t odd = __ballot(there && off == off && delta == delta && test != test);
+    return (odd | odd >> 32) & 0xffffffffu;
+  };
+  auto plain_rows = [&](uint64_t odd) {
+    const int d = 2 * lane;
+    const bool in = d < a.dim;
+    while (odd) {
+      const int r = __builtin_ctzll(odd), at = mine + r, pr = at + shift;
+      odd &= odd - 1;
+      const T *qr = (const T*)q + (int64_t)at * a.q.token + d, *gr = (const T*)d_o + (int64_t)at * a.d_o.token + d;
+      const float q0 = in ? (float)qr[0] : 0.f, q1 = in ? (float)qr[1] : 0.f, g0 = in ? (float)gr[0] : 0.f, g1 = in ? (float)gr[1] : 0.f;
+      const float plus = __shfl(off, r, 64), less = __shfl(delta + rest, r, 64);
+      float x0 = 0.f, x1 = 0.f;
+      for (int j = 0; j <= pr; ++j) {
+        if (a.window && j >= a.sinks && j <= pr - a.window) { j = pr - a.window; continue; }
+        const T *kj = (const T*)k + (int64_t)j * a.k.token + d, *vj = (const T*)v + (int64_t)j * a.v.token + d;
+        const float k0 = in ? (float)kj[0] : 0.f, k1 = in ? (float)kj[1] : 0.f;
+        float s = q0 * k0 + q1 * k1, e = in ? g0 * (float)vj[0] + g1 * (float)vj[1] : 0.f;
+        for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); e += __shfl_xor(e, m, 64); }
+        const float ds = exp2f((s + plus) * c) * (e - less);
+        x0 = fmaf(ds, k0, x0);
+        x1 = fmaf(ds, k1, x1);
+      }
+      T* to = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)at * a.dq.token + d;
+      if (in) { to[0] = (T)(a.scale * x0); to[1] = (T)(a.scale * x1); }
+    }
+  };
+  float test = 0.f;                                           // NaN where a result is not finite
   if constexpr (kShare) {
     if (there && half == 0) {
       a.off[stat] = off;
@@ -153,8 +183,13 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
 #pragma unroll
     for (int m = 0; m < D / 32; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
-    if (there) store_columns<T, D>(acc, dq, half, a.dim);
+      for (int i = 0; i < 16; ++i) {
+        acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
+        test = fmaf(acc[m][i], 0.f, test);
+      }
+    const uint64_t odd = odd_rows(test);
+    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, D>(acc, dq, half, a.dim);
+    plain_rows(odd);
   } else {
     float *sums = (float*)smem, *rests = (float*)(smem + kRestAt);
     __syncthreads();                                            // the tiles are done with
@@ -178,19 +213,26 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
       a.off[stat] = off;
       a.delta[stat] = -(delta + rest);
     }
-    if (wave >= D / 32) return;
-    f32x16 r;                                                   // a wavefront joins 32 columns
+    f32x16 r = (f32x16)(0.f);                                   // a wavefront joins 32 columns
+    if (wave < D / 32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x = 0.f, y = 0.f;
+      for (int i = 0; i < 16; ++i) {
+        float x = 0.f, y = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        x += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
-        y += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+        for (int w = 0; w < 4; ++w) {
+          x += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
+          y += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+        }
+        r[i] = a.scale * fmaf(-kept, y, x);
+        test = fmaf(r[i], 0.f, test);
       }
-      r[i] = a.scale * fmaf(-kept, y, x);
     }
-    if (there) store_block<T>(r, wave, dq, half, a.dim);
+    uint64_t odd = odd_rows(test), *odds = (uint64_t*)(rests + 2 * 4 * 64);
+    if (lane == 0) odds[wave] = odd;
+    __syncthreads();
+    odd = odds[0] | odds[1] | odds[2] | odds[3];
+    if (wave < D / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, dq, half, a.dim);
+    if (wave == 0) plain_rows(odd);
   }
 }
 
@@ -202,7 +244,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
 //
 // kShare: wavefronts of 32 keys each share steps, or have the same 32 and every fourth step; tiles are in one part then.
 template <typename T, int D, bool kShare>
-__global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
+__global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
   using Tl = Tile<D>;
   constexpr bool kKeysInLds = D > 64;
   constexpr int kQ = kKeysInLds || !kShare ? 32 : 64, kBytes = kQ * Tl::kRowBytes;   // queries of a step
@@ -361,8 +403,64 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dkv_kernel(Atte
     }
   }
 
+  T *dk_to = (T*)rows_of(a.dk, ragged, b, sk.first, kv), *dv_to = (T*)rows_of(a.dv, ragged, b, sk.first, kv);
+  // parts in the workspace: [sequence, head][item][dk, dv][key][dim]; items of tiles in one part have no place there
+  float* part_to = nullptr;
+  if (parts > 1) part_to = a.parts + part_place(a, tiles, ((int64_t)b * a.kv_heads + kv), tile, part) * 2 * kKeyTile * a.dim + (int64_t)(mine - first) * a.dim;
+  // Keys to be done in plain steps, as rows in the forward kernel: with a result that is not finite, which may come from a query that does
+  // not see them.  A key whose gradients are NaN throughout is done.
+  auto odd_keys = [&](float test) {
+    const uint64_t odd = __ballot(there && test != test);
+    return (odd | odd >> 32) & 0xffffffffu;
+  };
+  auto plain_keys = [&](uint64_t odd) {
+    const int d = 2 * lane;
+    const bool in = d < a.dim;
+    while (odd) {
+      const int r = __builtin_ctzll(odd), j = mine + r;
+      odd &= odd - 1;
+      const T *kj = (const T*)k + (int64_t)j * a.k.token + d, *vj = (const T*)v + (int64_t)j * a.v.token + d;
+      const float k0 = in ? (float)kj[0] : 0.f, k1 = in ? (float)kj[1] : 0.f, v0 = in ? (float)vj[0] : 0.f, v1 = in ? (float)vj[1] : 0.f;
+      float x0 = 0.f, x1 = 0.f, y0 = 0.f, y1 = 0.f;
+      bool done = false;
+      for (int t = step0; t < step1 && !done; ++t) {
+        const int from = (q_begin + t % q_steps) * kQ, h = kv * a.group + t / q_steps;
+        const T *qh = (const T*)rows_of(a.q, ragged, b, sq.first, h) + d, *gh = (const T*)rows_of(a.d_o, ragged, b, sq.first, h) + d;
+        const int64_t stat = ragged ? h * a.q_tokens + sq.first : ((int64_t)b * a.q_heads + h) * a.q_len;
+        for (int i = from; i < min(from + kQ, sq.count) && !done; ++i) {
+          const int p = i + shift;
+          if (j > p || (a.window && j >= a.sinks && j <= p - a.window)) continue;
+          const T *qi = qh + (int64_t)i * a.q.token, *gi = gh + (int64_t)i * a.d_o.token;
+          const float q0 = in ? (float)qi[0] : 0.f, q1 = in ? (float)qi[1] : 0.f, g0 = in ? (float)gi[0] : 0.f, g1 = in ? (float)gi[1] : 0.f;
+          float s = q0 * k0 + q1 * k1, e = g0 * v0 + g1 * v1;
+          for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); e += __shfl_xor(e, m, 64); }
+          const float w = exp2f((s + a.off[stat + i]) * c), ds = w * (e + a.delta[stat + i]);
+          x0 = fmaf(ds, q0, x0);
+          x1 = fmaf(ds, q1, x1);
+          y0 = fmaf(w, g0, y0);
+          y1 = fmaf(w, g1, y1);
+          done = __all(!in || (x0 != x0 && x1 != x1 && y0 != y0 && y1 != y1));
+        }
+      }
+      if (in && parts > 1) {
+        float* to = part_to + (int64_t)r * a.dim + d;
+        to[0] = a.scale * x0;
+        to[1] = a.scale * x1;
+        to[kKeyTile * a.dim] = y0;
+        to[kKeyTile * a.dim + 1] = y1;
+      } else if (in) {
+        T *x = dk_to + (int64_t)j * a.dk.token + d, *y = dv_to + (int64_t)j * a.dv.token + d;
+        x[0] = (T)(a.scale * x0);
+        x[1] = (T)(a.scale * x1);
+        y[0] = (T)y0;
+        y[1] = (T)y1;
+      }
+    }
+  };
+  float test = 0.f;                                              // NaN where a result is not finite
   if constexpr (!kShare) {
     float* sums = (float*)smem;
+    uint64_t* odds = (uint64_t*)(smem + kStatsAt);
     __syncthreads();                                             // the tiles are done with
 #pragma unroll
     for (int m = 0; m < D / 32; ++m)
@@ -372,43 +470,56 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dkv_kernel(Atte
         sums[((wave * (D / 32) + m) * 32 + 16 + i) * 64 + lane] = dv[m][i];
       }
     __syncthreads();
-    if (wave >= D / 32) return;
     f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);                 // a wavefront joins 32 columns
+    if (wave < D / 32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 16; ++i) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        x[i] += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
-        y[i] += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+        for (int w = 0; w < 4; ++w) {
+          x[i] += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
+          y[i] += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+        }
+        x[i] *= a.scale;
+        test = fmaf(x[i], 0.f, fmaf(y[i], 0.f, test));
       }
-      x[i] *= a.scale;
     }
-    if (!there) return;
-    store_block<T>(x, wave, (T*)rows_of(a.dk, ragged, b, sk.first, kv) + (int64_t)key * a.dk.token, half, a.dim);
-    store_block<T>(y, wave, (T*)rows_of(a.dv, ragged, b, sk.first, kv) + (int64_t)key * a.dv.token, half, a.dim);
+    uint64_t odd = odd_keys(test);
+    if (lane == 0) odds[wave] = odd;
+    __syncthreads();
+    odd = odds[0] | odds[1] | odds[2] | odds[3];
+    if (wave < D / 32 && there && !(odd >> (lane & 31) & 1)) {
+      store_block<T>(x, wave, dk_to + (int64_t)key * a.dk.token, half, a.dim);
+      store_block<T>(y, wave, dv_to + (int64_t)key * a.dv.token, half, a.dim);
+    }
+    if (wave == 0) plain_keys(odd);
     return;
   }
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m) dk[m] *= a.scale;
+  for (int m = 0; m < D / 32; ++m) {
+    dk[m] *= a.scale;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) test = fmaf(dk[m][i], 0.f, fmaf(dv[m][i], 0.f, test));
+  }
+  const uint64_t odd = odd_keys(test);
   if (parts == 1) {
-    if (!there) return;
-    store_columns<T, D>(dk, (T*)rows_of(a.dk, ragged, b, sk.first, kv) + (int64_t)key * a.dk.token, half, a.dim);
-    store_columns<T, D>(dv, (T*)rows_of(a.dv, ragged, b, sk.first, kv) + (int64_t)key * a.dv.token, half, a.dim);
-    return;
-  }
-  // parts in the workspace: [sequence, head][item][dk, dv][key][dim]; items of tiles in one part have no place there
-  const int64_t pair = part_place(a, tiles, ((int64_t)b * a.kv_heads + kv), tile, part);
-  float* to = a.parts + pair * 2 * kKeyTile * a.dim + (int64_t)(wave * 32 + (lane & 31)) * a.dim;
-#pragma unroll
-  for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d = 32 * m + 2 * i + 4 * half;
-      if (d < a.dim) {
-        *(f32x4*)(to + d) = f32x4{dk[m][i], dk[m][i + 1], dk[m][i + 2], dk[m][i + 3]};
-        *(f32x4*)(to + kKeyTile * a.dim + d) = f32x4{dv[m][i], dv[m][i + 1], dv[m][i + 2], dv[m][i + 3]};
-      }
+    if (there && !(odd >> (lane & 31) & 1)) {
+      store_columns<T, D>(dk, dk_to + (int64_t)key * a.dk.token, half, a.dim);
+      store_columns<T, D>(dv, dv_to + (int64_t)key * a.dv.token, half, a.dim);
     }
+  } else if (!(odd >> (lane & 31) & 1)) {
+    float* to = part_to + (int64_t)(lane & 31) * a.dim;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * m + 2 * i + 4 * half;
+        if (d < a.dim) {
+          *(f32x4*)(to + d) = f32x4{dk[m][i], dk[m][i + 1], dk[m][i + 2], dk[m][i + 3]};
+          *(f32x4*)(to + kKeyTile * a.dim + d) = f32x4{dv[m][i], dv[m][i + 1], dv[m][i + 2], dv[m][i + 3]};
+        }
+      }
+  }
+  plain_keys(odd);
 }
 
 // Adds up the parts of tiles that were cut, eight columns of a key per thread, dk and dv.

@@ -418,3 +418,74 @@ def test_single_tokens_agree_with_whole_sequences(torch, Attention):
                 want, bound = oracle.attention(q[0, t, h][None], k[0, :t + 1, h // 2], v[0, :t + 1, h // 2], 60, 4)
                 within(torch, "o", out[0, h][None], want["o"], bound["o"])
                 within(torch, "o of the whole", whole[0, t, h][None], want["o"], bound["o"])
+
+
+def test_offsets_beyond_32_bits(torch, Attention):
+    """Sequences 2^31 elements apart, heads 2^31 elements apart, and pages whose places pass 2^32 bytes and 2^31 elements."""
+    far = 1 << 31
+    room = torch.empty(far + 40_000, dtype=torch.bfloat16, device="cuda")
+    q, k, v = (torch.as_strided(room, (2, 100, 1, 64), (far, 64, 0, 1), 8000 * i) for i in range(3))
+    d_o = normal(torch, 5, "bfloat16", 2, 100, 1, 64)
+    for i, t in enumerate((q, k, v)):
+        t.copy_(normal(torch, i, "bfloat16", 2, 100, 1, 64))
+    op = Attention(30, 2)
+    o, lse = op.forward(q, k, v)
+    grads = op.backward(d_o, q, k, v, o, lse)
+    for b in range(2):
+        got = dict(zip(("dq", "dk", "dv"), (g[b] for g in grads)), o=o[b], lse=lse[b])
+        check_sequence(torch, got, q[b], k[b], v[b], 30, 2, d_o=d_o[b])
+    q = torch.as_strided(room, (1, 100, 2, 64), (0, 64, far, 1))
+    o, lse = op.forward(q, q, q)
+    check_sequence(torch, {"o": o[0], "lse": lse[0]}, q[0], q[0], q[0], 30, 2)
+    del room, q, k, v
+    pages, page = 280_000, 16                                    # 2.3 G elements, 4.6 GB
+    pools = [torch.empty(pages, page, 8, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.tensor([[pages - 1, 0, pages - 7, 263_000]], dtype=torch.int32, device="cuda")
+    rows = [[normal(torch, s, "bfloat16", 60, 8, 64) for s in (1, 2)]]
+    n = torch.tensor([60], dtype=torch.int32, device="cuda")
+    op = Attention()
+    op.append(*(x[None] for x in rows[0]), *pools, table, n)
+    q = normal(torch, 3, "bfloat16", 1, 8, 64)
+    check_tokens(torch, op.decode(q, *pools, table, n, 60), q, rows, 0, 0)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("heads,kv,dim,window,sinks", [(1, 1, 64, 50, 4), (60, 1, 64, 50, 4), (1, 1, 128, 0, 0), (60, 1, 128, 50, 4), (60, 60, 64, 0, 0),
+                                                       (60, 60, 128, 20, 0), (8, 2, 72, 100, 100)])
+def test_gradients_of_what_is_not_seen(torch, Attention, heads, kv, dim, window, sinks, bad):
+    """Keys and values that are not finite leave the gradients of queries that do not see them alone, and queries and gradients of results that
+    are not finite those of keys that they do not see.  The rest is as it would be without them."""
+    n, last = 300, heads // kv
+    q, d_o = (normal(torch, s, "bfloat16", n, heads, dim) for s in (1, 4))
+    k, v = (normal(torch, s, "bfloat16", n, kv, dim) for s in (2, 3))
+    op = Attention(window, sinks)
+    seen = oracle.visible(n, n, window, sinks)
+    want = [oracle.attention(q[:, h], k[:, -1], v[:, -1], window, sinks, d_o=d_o[:, h]) for h in range(heads - last, heads)]    # of the last key head
+
+    def check_keys(got, name, keys, columns):
+        total, bound = (sum(w[i][name] for w in want) for i in (0, 1))
+        bound = bound + oracle.UNIT[q.dtype] * total.abs()
+        within(torch, name, got[name][0, :, -1][keys][:, columns], total[keys][:, columns], bound[keys][:, columns])
+
+    at = [150, 151]
+    bad_k, bad_v = k.clone(), v.clone()
+    bad_k[at], bad_v[at] = bad, bad
+    got = run(torch, op, q[None], bad_k[None], bad_v[None], d_o[None])
+    rows = [i for i in range(n) if not seen[i, at].any()]
+    assert len(rows) >= 148
+    for h in (0, -1):
+        within(torch, "dq", got["dq"][0, rows, heads - last if h == 0 else -1], want[h][0]["dq"][rows], want[h][1]["dq"][rows])
+
+    bad_q, bad_do = q.clone(), d_o.clone()
+    bad_q[at[0]], bad_do[at] = bad, bad
+    got = run(torch, op, bad_q[None], k[None], v[None], bad_do[None])
+    keys = [j for j in range(n) if not seen[at, j].any()]
+    assert len(keys) >= 148
+    for name in ("dk", "dv"):
+        check_keys(got, name, keys, list(range(dim)))
+
+    bad_do = d_o.clone()                                         # one column of a gradient that some keys do see
+    bad_do[at[0], -1, 5] = bad
+    got = run(torch, op, q[None], k[None], v[None], bad_do[None])
+    check_keys(got, "dv", list(range(n)), [i for i in range(dim) if i != 5])
+    assert torch.equal(torch.isfinite(got["dv"][0, :, -1, 5]).cpu(), ~seen[at[0]])
