@@ -37,7 +37,7 @@ int arrow_embedding_forward(const arrow_embedding_t *e, const void *W, const voi
 
 /*
  * dW = scale E^T dY: every row of dW is written (rows without tokens become 0); it must not overlap dY.
- * ws: DEVICE, 256-byte aligned, at least arrow_embedding_workspace_bytes(e); written, holds nothing between calls.
+ * ws: DEVICE, 256-byte aligned, at least arrow_embedding_workspace_bytes(e); written (not by calls of few tokens), holds nothing between calls.
  * Errors: EINVAL, ETOOSMALL, EHIP.
  */
 size_t arrow_embedding_workspace_bytes(const arrow_embedding_t *e);

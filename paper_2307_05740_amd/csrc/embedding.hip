@@ -3,9 +3,10 @@
 // Both are bound by the rows that they move.  The gradient is the product of a transposed one-hot matrix with dY: the tokens
 // are sorted by id (a stable radix sort, so that a row's tokens keep their order), then each row of dW is the sum of its
 // tokens' rows.  A few ids have a large part of all tokens: the sorted tokens are cut into chunks, rows that reach over a chunk's end
-// are summed chunk by chunk into partial rows, which a last kernel adds up.
+// are summed chunk by chunk into partial rows, which a last kernel adds up.  For few tokens one kernel does all of that, its workgroups by themselves.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "embedding_internal.h"
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(64) void sort_move_kernel(SortArgs s) {
 
 // The sort of a digit in one launch, for few tokens: every workgroup counts all of them, those before its own ones in the upper half of
 // a word, and so knows where its own go: block_tokens of them, whole wavefronts' and at most as many as it has threads.  16,384 tokens of 32,000
-// rows: TODO us, where the three launches above take TODO, twice.
+// rows: 17 us, of which the 32 Ki counts in LDS are about 6, where the three launches above take some 20, twice.
 constexpr int kSortBlock = 1024;
 
 __global__ __launch_bounds__(kSortBlock) void sort_few_kernel(SortArgs s, uint32_t* row_begin) {
@@ -394,6 +395,137 @@ __global__ __launch_bounds__(64) void embedding_join_kernel(SumArgs a, G* dW) {
   store<G, VEC>(dW + row * a.w_stride + c, sum);
 }
 
+// ---- the whole gradient in one launch, for few tokens ----
+
+// A workgroup has one slice of the columns of every 2^step_log-th row of dW, at most kDirectRows of them (frequent ids often have numbers next to each
+// other).  It goes through all ids for those that are its own, sorts them by row in LDS (each wavefront a quarter of the tokens, in
+// order), and 16 groups of 16 lanes add up equal parts of what it found; rows that reach over a part's end are joined in LDS, in order.
+//
+// What bounds it: of few tokens, the launch and three loads that wait for each other; of large tables, the rows that are written.  Up to kDirectTokens it is
+// faster than the launches it replaces (us, those -> this; ids as in text, of columns in bfloat16; "one": the same id for all):
+//   128 tokens:   32,000 x 512 20 -> 10, 32,000 x 4096 65 -> 52, 1000 x 4096 12 -> 6, 50 x 64 11 -> 5
+//   2048 tokens:  32,000 x 512 23 -> 14, 32,000 x 4096 67 -> 64, 1000 x 4096 18 -> 14, 50 x 64 13 -> 12; one: 40 -> 32, 87 -> 51, 35 -> 35, 28 -> 30
+//   4096 tokens:  32,000 x 512 24 -> 21, 32,000 x 4096 73 -> 126, 1000 x 4096 25 -> 23, 50 x 64 16 -> 19; one: 61 -> 57, 112 -> 88, 58 -> 71, 46 -> 56
+constexpr int kDirectRows = 64, kDirectLanes = 16, kDirectBlocks = 1024;
+
+template <typename T, typename G, int VEC>
+__global__ __launch_bounds__(256) void embedding_direct_kernel(arrow_embedding_t e, const T* dY, const void* ids, G* dW, int step_log, int slices, int pieces) {
+  constexpr int kSteps = kDirectTokens / 256, kGroups = 256 / kDirectLanes, kAhead = 8;
+  constexpr uint32_t kNone = 0xffffffffu;
+  static_assert(kDirectRows * 4 == 256 && kDirectTokens <= 65536, "a thread for every row and wavefront; tokens of 16 bits");
+  __shared__ uint32_t next[kDirectRows * 4];       // per row and wavefront: its tokens, then where they go
+  __shared__ uint32_t list[kDirectTokens];         // token, row << 16
+  __shared__ uint32_t sums[4];
+  __shared__ float parts[2 * kGroups][kDirectLanes * VEC];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tokens = (int)e.tokens;
+  const int slice = blockIdx.x % slices;
+  const int64_t row0 = blockIdx.x / slices, step = (int64_t)1 << step_log;   // its rows: row0 + r step
+  const int rows = (int)((e.rows - row0 + step - 1) >> step_log);
+  next[threadIdx.x] = 0;
+  const int steps = (tokens + 255) / 256, t0 = wave * steps * 64 + lane;
+  uint32_t row[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int t = t0 + 64 * i;
+    const int64_t id = i < steps && t < tokens ? id_at(ids, t, e.id_bytes == 8) : -1;
+    row[i] = id >= 0 && id < e.rows && (id & (step - 1)) == row0 ? (uint32_t)(id >> step_log) : kNone;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (row[i] != kNone) atomicAdd(&next[4 * row[i] + wave], 1u);
+  __syncthreads();
+  const uint32_t count = next[threadIdx.x];
+  uint32_t upto = count;
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint32_t x = __shfl_up(upto, m, 64);
+    if (lane >= m) upto += x;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  uint32_t base = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) base += sums[w];
+    all += sums[w];
+  }
+  next[threadIdx.x] = base + upto - count;
+  __syncthreads();
+  // (a wavefront's places are its own: its steps go one after the other, and lanes with one row in the order of lanes)
+  volatile uint32_t* place = next;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const bool in = row[i] != kNone;
+    uint64_t same = __ballot(in);
+    if (same == 0) continue;
+    for (int b = 0; b < 6; ++b) {
+      const uint64_t set = __ballot(row[i] >> b & 1);
+      same &= row[i] >> b & 1 ? set : ~set;
+    }
+    if (in) {
+      const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
+      const uint32_t at = place[4 * row[i] + wave];
+      if (before == 0) place[4 * row[i] + wave] = at + __popcll(same);
+      list[at + before] = (uint32_t)(t0 + 64 * i) | row[i] << 16;
+    }
+  }
+  __syncthreads();
+  // now row r has the places from the end of the one before, next[4 r - 1], to next[4 r + 3]
+  const int group = threadIdx.x / kDirectLanes, in = threadIdx.x % kDirectLanes, piece = slice * kDirectLanes + in;
+  const bool there = piece < pieces;
+  const int c = min(piece * VEC, e.columns - VEC);
+  const float zero[VEC] = {};
+  for (int r = group; r < rows; r += kGroups)
+    if (there && next[4 * r + 3] == (r ? next[4 * r - 1] : 0)) store<G, VEC>(dW + (row0 + r * step) * e.w_stride + c, zero);
+  const int n = (int)all, each = max(1, (n + kGroups - 1) / kGroups), lo = group * each, hi = min(n, lo + each);
+  bool began_before = lo > 0 && lo < hi && list[lo] >> 16 == list[lo - 1] >> 16;
+  float sum[VEC] = {};
+  for (int i = lo; i < hi; i += kAhead) {
+    uint32_t entry[kAhead + 1];
+    typename Columns<T, VEC>::type x[kAhead];
+#pragma unroll
+    for (int r = 0; r <= kAhead; ++r) entry[r] = list[min(i + r, n - 1)];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r)                            // (without branches: some lanes load what they do not need)
+      x[r] = *(const typename Columns<T, VEC>::type*)(dY + (int64_t)(entry[r] & 0xffff) * e.y_stride + c);
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      if (i + r >= hi) continue;
+      if constexpr (VEC == 1) sum[0] += (float)x[r];
+      else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[j] += (float)x[r][j];
+      }
+      const bool goes_on = i + r + 1 < n && entry[r] >> 16 == entry[r + 1] >> 16;
+      if (goes_on && i + r + 1 < hi) continue;
+      if (began_before || goes_on) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) parts[2 * group + !began_before][in * VEC + j] = sum[j];
+      } else if (there) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[j] *= e.scale;
+        store<G, VEC>(dW + (row0 + (entry[r] >> 16) * step) * e.w_stride + c, sum);
+      }
+      began_before = false;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+    }
+  }
+  __syncthreads();
+  if (lo >= hi || hi >= n || !there) return;
+  const int r = list[hi - 1] >> 16, begin = r ? next[4 * r - 1] : 0;
+  if ((int)(list[hi] >> 16) != r || begin < lo) return;
+  const int last = (int)(next[4 * r + 3] - 1) / each;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] = parts[2 * group + 1][in * VEC + j];
+  for (int g = group + 1; g <= last; ++g)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += parts[2 * g][in * VEC + j];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] *= e.scale;
+  store<G, VEC>(dW + (row0 + r * step) * e.w_stride + c, sum);
+}
+
 int log2_up(int64_t x, int most) {
   int r = 0;
   while (r < most && ((int64_t)1 << r) < x) ++r;
@@ -410,6 +542,14 @@ int forward(const arrow_embedding_t& e, const void* W, const void* ids, void* Y,
 
 template <typename T, typename G, int VEC>
 int backward(const arrow_embedding_t& e, const EmbeddingPlan& p, const void* dY, const void* ids, void* dW, void* ws, hipStream_t s) {
+  if (p.direct) {
+    const int pieces = (e.columns + VEC - 1) / VEC, slices = (pieces + kDirectLanes - 1) / kDirectLanes;
+    const int step_log = log2_up(std::max<int64_t>(kDirectBlocks / slices, (e.rows + kDirectRows - 1) / kDirectRows), 31);
+    const int64_t blocks = std::min<int64_t>(e.rows, (int64_t)1 << step_log) * slices;
+    if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+    embedding_direct_kernel<T, G, VEC><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(e, (const T*)dY, ids, (G*)dW, step_log, slices, pieces);
+    return (int)hipGetLastError();
+  }
   auto at = [&](size_t offset) { return (uint32_t*)((char*)ws + offset); };
   int now = 0;
   const bool noted = p.few && p.passes == 1;

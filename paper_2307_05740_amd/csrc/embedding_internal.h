@@ -12,11 +12,13 @@ constexpr int kDigitBits = 9;        // of the sort by id of many tokens, at mos
 constexpr int kSortTokens = 256;     // of a wavefront of it, at least
 constexpr int kWideDigitBits = 15;   // of the sort of few tokens, at most
 constexpr int kFewTokens = 65535;    // they are counted in 16 bits
+constexpr int kDirectTokens = 2048;  // of a gradient in one launch, at most
 constexpr int kChunkTokens = 8;      // sorted tokens that a lane group of the sums goes through, a multiple of this: a row's load or two for few
                                      // tokens, and four where there are enough to fill the chip
 
 // How the gradient of a call is carried out, and where its workspace keeps what.
 struct EmbeddingPlan {
+  bool direct;                     // one launch does it all; the rest is not used
   bool few;                        // tokens: each workgroup of the sort counts them all
   int32_t passes, bits;            // of the sort by id: digits, and bits of each
   int64_t blocks, block_tokens;    // its workgroups, and the tokens of each

@@ -148,3 +148,16 @@ def test_gradient_against_differences(torch, Embedding):
     right = float((op.backward(dY, ids).double() * E.double()).sum())
     room = 2.0 ** -22 * 3.0 * float((dY.double().abs().sum()) * (W.abs().max() + E.abs().max())) + 2.0 ** -20 * abs(right)
     assert abs(left - right) <= room, (left, right, room)
+
+
+@pytest.mark.parametrize("n", [17, 511, 2047, 2048, 2049])
+@pytest.mark.parametrize("rows,columns", [(1, 130), (64, 1), (65, 1100), (1025, 5), (20_001, 260)])
+@pytest.mark.parametrize("kind", ["one", "text", "even"])
+def test_few_tokens_and_slices_of_columns(torch, Embedding, n, rows, columns, kind):
+    """Around the number of tokens that a gradient takes in one launch; rows that reach over several of its groups of lanes."""
+    dY, ids = normal(torch, 2, "bfloat16", n, columns), tokens(torch, 3, n, rows, kind)
+    op = Embedding(rows, 1.5)
+    check_grad(torch, op.backward(dY, ids, torch.full((rows, columns), math.nan, dtype=torch.bfloat16, device="cuda")), dY, ids, rows, 1.5)
+    again = op.backward(dY, ids.int(), dtype=torch.float32)
+    check_grad(torch, again, dY, ids, rows, 1.5)
+    assert torch.equal(again, op.backward(dY, ids, dtype=torch.float32))
