@@ -44,8 +44,9 @@ __device__ __noinline__ void plain_row(const T* q, const char* k, const char* v,
   if (mine) { o[d] = (T)a0; o[d + 1] = (T)a1; }
 }
 
-template <typename T, int D, bool kShare>
+template <typename T, int C, bool kShare>
 __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
+  constexpr int D = columns_of_tile(C);
   using Tl = Tile<D>;
   constexpr int kStep = kShare ? 64 : 32;                     // keys of a tile
   constexpr int kTurns = kShare ? 1 : 4;                      // a wavefront has every kTurns-th tile
@@ -74,9 +75,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
   const char* k = rows_of(a.k, ragged, b, sk.first, kv);
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
 
-  x8<T> qf[D / 16];
+  x8<T> qf[C / 16];
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
+  for (int s = 0; s < C / 16; ++s) {
     const int d = 16 * s + 8 * half;
     x8<T> z = {};
     qf[s] = there && d < a.dim ? *(const x8<T>*)(q + 2 * ((int64_t)row * a.q.token + d)) : z;
@@ -87,9 +88,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
   // of this wavefront's queries
   const int low = mine + shift, high = min(low + 31, sk.count - 1);
 
-  f32x16 acc[D / 32];
+  f32x16 acc[C / 32];
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m) acc[m] = (f32x16)(0.f);
+  for (int m = 0; m < C / 32; ++m) acc[m] = (f32x16)(0.f);
   const float c = a.scale * kLog2e;
   float top = minus_infinity(), total = 0.f;                  // of c times the scores; of this lane's keys
 
@@ -117,10 +118,10 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
 #pragma unroll
     for (int n = 0; n < kStep / 32; ++n) s[n] = (f32x16)(0.f);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i)                          // (in turn: a product waits for the last one on the same sums)
+    for (int i = 0; i < C / 16; ++i)                          // (in turn: a product waits for the last one on the same sums)
 #pragma unroll
       for (int n = 0; n < kStep / 32; ++n) s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
-    reads_ahead<6, (kStep / 32) * (D / 16), 1>();
+    reads_ahead<6, (kStep / 32) * (C / 16), 1>();
     // every query sees every key: nothing to mask
     const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
     if (!whole) {
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
       top = now;
       total *= by;
 #pragma unroll
-      for (int m = 0; m < D / 32; ++m) acc[m] *= by;
+      for (int m = 0; m < C / 32; ++m) acc[m] *= by;
     }
     const float off = top == minus_infinity() ? 0.f : top;
     x8<T> pf[kStep / 16];
@@ -168,9 +169,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
 #pragma unroll
     for (int u = 0; u < kStep / 16; ++u)
 #pragma unroll
-      for (int m = 0; m < D / 32; ++m)
+      for (int m = 0; m < C / 32; ++m)
         acc[m] = mma32(read_columns<T, D>(vt + my.columns, m, 16 * u * Tl::kRowBytes), pf[u], acc[m]);
-    reads_ahead<8, (kStep / 16) * (D / 32), 2>();
+    reads_ahead<8, (kStep / 16) * (C / 32), 2>();
   }
 
   total = add_halves(total);
@@ -196,21 +197,21 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
     if (a.lse && there && half == 0) a.lse[stat] = lse;
     float test = 0.f;                                         // NaN where a result is not finite
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < C / 32; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) { acc[m][i] *= by; test = fmaf(acc[m][i], 0.f, test); }
     const uint64_t odd = odd_rows(test, lse);
     // (all lanes take part in the exchange; whether a row is stored is the same in both halves)
-    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, D>(acc, o + (int64_t)row * a.o.token, half, a.dim);
+    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, C>(acc, o + (int64_t)row * a.o.token, half, a.dim);
     plain_rows(odd, lse);
   } else {
     float *sums = (float*)smem, *tops = (float*)(smem + kRoom), *totals = tops + 4 * 64;
     uint64_t* odds = (uint64_t*)(totals + 4 * 64);
     __syncthreads();                                          // the tiles are done with
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < C / 32; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sums[((wave * (D / 32) + m) * 16 + i) * 64 + lane] = acc[m][i];
+      for (int i = 0; i < 16; ++i) sums[((wave * (C / 32) + m) * 16 + i) * 64 + lane] = acc[m][i];
     tops[wave * 64 + lane] = top;
     totals[wave * 64 + lane] = total;
     __syncthreads();
@@ -229,11 +230,11 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
     // a wavefront joins 32 columns
     f32x16 r = (f32x16)(0.f);
     float test = 0.f;
-    if (wave < D / 32) {
+    if (wave < C / 32) {
 #pragma unroll
       for (int w = 0; w < 4; ++w)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) r[i] = fmaf(share[w], sums[((w * (D / 32) + wave) * 16 + i) * 64 + lane], r[i]);
+        for (int i = 0; i < 16; ++i) r[i] = fmaf(share[w], sums[((w * (C / 32) + wave) * 16 + i) * 64 + lane], r[i]);
 #pragma unroll
       for (int i = 0; i < 16; ++i) { r[i] *= by; test = fmaf(r[i], 0.f, test); }
     }
@@ -241,28 +242,33 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
     if (lane == 0) odds[wave] = odd;
     __syncthreads();
     odd = odds[0] | odds[1] | odds[2] | odds[3];
-    if (wave < D / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, o + (int64_t)row * a.o.token, half, a.dim);
+    if (wave < C / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, o + (int64_t)row * a.o.token, half, a.dim);
     if (wave == 0) plain_rows(odd, lse);
   }
 }
 
-template <typename T, int D>
+template <typename T, int C>
 int forward(const AttentionArgs& a, void* stream) {
   const int64_t heads = (int64_t)a.q_heads * a.batch, tiles = ((int64_t)a.q_len + kQueryTile - 1) / kQueryTile;
   const bool share = !few_blocks(tiles * heads, a);
   const int64_t rows = share ? tiles : ((int64_t)a.q_len + 31) / 32, blocks = rows * heads;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(256);
-  if (share) attention_forward_kernel<T, D, true><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
-  else attention_forward_kernel<T, D, false><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  if (share) attention_forward_kernel<T, C, true><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  else attention_forward_kernel<T, C, false><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
   return (int)hipGetLastError();
+}
+
+template <typename T>
+int by_columns(const AttentionArgs& a, void* stream) {
+  return a.dim <= 64 ? forward<T, 64>(a, stream) : a.dim <= 96 ? forward<T, 96>(a, stream) : forward<T, 128>(a, stream);
 }
 
 }  // namespace
 
 int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream) {
-  if (dtype == ARROW_BF16) return a.dim <= 64 ? forward<__bf16, 64>(a, stream) : forward<__bf16, 128>(a, stream);
-  return a.dim <= 64 ? forward<_Float16, 64>(a, stream) : forward<_Float16, 128>(a, stream);
+  if (dtype == ARROW_BF16) return by_columns<__bf16>(a, stream);
+  return by_columns<_Float16>(a, stream);
 }
 
 }  // namespace arrow

@@ -92,6 +92,10 @@ struct Tile {
   }
 };
 
+// Columns of the tiles in which heads of up to C = 64, 96 or 128 columns lie.  Products leave out those from C on (training over 1531 tokens, heads
+// of 96: 155 us with all 128, 141 without the last ones).
+constexpr int columns_of_tile(int C) { return C <= 64 ? 64 : 128; }
+
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 

@@ -19,8 +19,9 @@ namespace {
 // (dq of 5 keys off by 1.55 times what rounding dq alone does, and 1.4 so; for long rows the same, and 15 % of the kernel's time).
 //
 // kShare: as in the forward kernel, wavefronts of 32 queries each share tiles of keys, or have the same 32 and every fourth tile.
-template <typename T, int D, bool kShare>
+template <typename T, int C, bool kShare>
 __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(AttentionArgs a, int tiles) {
+  constexpr int D = columns_of_tile(C);
   using Tl = Tile<D>;
   constexpr bool kQueriesInLds = D > 64;                         // no registers are left for them
   constexpr int kStep = kQueriesInLds || !kShare ? 32 : 64, kBytes = kStep * Tl::kRowBytes;   // keys of a tile
@@ -49,12 +50,12 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   const char* d_o = rows_of(a.d_o, ragged, b, sq.first, head);
   lds_byte *room = (lds_byte*)smem, *base = room + (kShare ? 0 : wave * 4 * kBytes);
 
-  x8<T> qf[kQueriesInLds ? 1 : D / 16], df[D / 16];
+  x8<T> qf[kQueriesInLds ? 1 : C / 16], df[C / 16];
   if constexpr (kQueriesInLds)                                   // (waited for with the first tiles)
     Loader<D, kRows, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, room + kQueriesAt, wave);
   float delta = 0.f;
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
+  for (int s = 0; s < C / 16; ++s) {
     const int d = 16 * s + 8 * half;
     const x8<T> z = {};
     const bool in = there && d < a.dim;
@@ -82,9 +83,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
     lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * kBytes, sharer);
     lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, sharer);
   };
-  f32x16 acc[D / 32], pk[D / 32];                             // dS K and P K
+  f32x16 acc[C / 32], pk[C / 32];                             // dS K and P K
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
+  for (int m = 0; m < C / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
   float rest = 0.f, kept = 0.f;                               // sums of dS of this lane's keys, before and after they are rounded
   const int t0 = kShare ? 0 : wave;
   if (t0 < seen.total) load(t0, 0);
@@ -105,11 +106,11 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
       // the products begin with what is taken off them (which is in one register each, not in 16 ready for that, where those are needed)
       f32x16 s = (f32x16)(kQueriesInLds ? here(off) : off), e = (f32x16)(kQueriesInLds ? here(-delta) : -delta);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
+      for (int i = 0; i < C / 16; ++i)
         s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt, i, 0) : qf[kQueriesInLds ? 0 : i], s);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
-      reads_ahead<4, D / 16, kQueriesInLds ? 2 : 1, D / 16, 1>();
+      for (int i = 0; i < C / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
+      reads_ahead<4, C / 16, kQueriesInLds ? 2 : 1, C / 16, 1>();
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
       if (!whole) {
@@ -132,13 +133,13 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
         const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
         if constexpr (!kShare) kept = add8(ds, kept);
 #pragma unroll
-        for (int m = 0; m < D / 32; ++m) {
+        for (int m = 0; m < C / 32; ++m) {
           const x8<T> kf = read_columns<T, D>(kt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes);
           acc[m] = mma32(kf, ds, acc[m]);
           pk[m] = mma32(kf, pf, pk[m]);
         }
       }
-      reads_ahead<4, 4 * (D / 32), 1>();
+      reads_ahead<4, 4 * (C / 32), 1>();
     }
   }
 
@@ -181,24 +182,24 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
       a.delta[stat] = -(delta + rest);
     }
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < C / 32; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
         test = fmaf(acc[m][i], 0.f, test);
       }
     const uint64_t odd = odd_rows(test);
-    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, D>(acc, dq, half, a.dim);
+    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, C>(acc, dq, half, a.dim);
     plain_rows(odd);
   } else {
     float *sums = (float*)smem, *rests = (float*)(smem + kRestAt);
     __syncthreads();                                            // the tiles are done with
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < C / 32; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        sums[((wave * (D / 32) + m) * 32 + i) * 64 + lane] = acc[m][i];
-        sums[((wave * (D / 32) + m) * 32 + 16 + i) * 64 + lane] = pk[m][i];
+        sums[((wave * (C / 32) + m) * 32 + i) * 64 + lane] = acc[m][i];
+        sums[((wave * (C / 32) + m) * 32 + 16 + i) * 64 + lane] = pk[m][i];
       }
     rests[wave * 64 + lane] = rest;
     rests[(4 + wave) * 64 + lane] = kept;
@@ -214,14 +215,14 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
       a.delta[stat] = -(delta + rest);
     }
     f32x16 r = (f32x16)(0.f);                                   // a wavefront joins 32 columns
-    if (wave < D / 32) {
+    if (wave < C / 32) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float x = 0.f, y = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          x += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
-          y += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+          x += sums[((w * (C / 32) + wave) * 32 + i) * 64 + lane];
+          y += sums[((w * (C / 32) + wave) * 32 + 16 + i) * 64 + lane];
         }
         r[i] = a.scale * fmaf(-kept, y, x);
         test = fmaf(r[i], 0.f, test);
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
     if (lane == 0) odds[wave] = odd;
     __syncthreads();
     odd = odds[0] | odds[1] | odds[2] | odds[3];
-    if (wave < D / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, dq, half, a.dim);
+    if (wave < C / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, dq, half, a.dim);
     if (wave == 0) plain_rows(odd);
   }
 }
@@ -243,8 +244,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
 // to the workspace and attention_join_kernel adds them up in order.
 //
 // kShare: wavefronts of 32 keys each share steps, or have the same 32 and every fourth step; tiles are in one part then.
-template <typename T, int D, bool kShare>
-__global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
+template <typename T, int C, bool kShare>
+__global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
+  constexpr int D = columns_of_tile(C);
   using Tl = Tile<D>;
   constexpr bool kKeysInLds = D > 64;
   constexpr int kQ = kKeysInLds || !kShare ? 32 : 64, kBytes = kQ * Tl::kRowBytes;   // queries of a step
@@ -272,20 +274,20 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
   const bool there = key < sk.count;
   const char* k = rows_of(a.k, ragged, b, sk.first, kv);
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
-  x8<T> kf[kKeysInLds ? 1 : D / 16], vf[D / 16];
+  x8<T> kf[kKeysInLds ? 1 : C / 16], vf[C / 16];
   if constexpr (kKeysInLds)                                      // (waited for with the first step's tiles)
     Loader<D, kKeys, 4>(wave, lane, a.k.token, a.dim).load(k + 2 * (int64_t)first * a.k.token, sk.count - first, (lds_byte*)smem + kKeysAt, wave);
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
+  for (int s = 0; s < C / 16; ++s) {
     const int d = 16 * s + 8 * half;
     const x8<T> z = {};
     const bool in = there && d < a.dim;
     if constexpr (!kKeysInLds) kf[s] = in ? *(const x8<T>*)(k + 2 * ((int64_t)key * a.k.token + d)) : z;
     vf[s] = in ? *(const x8<T>*)(v + 2 * ((int64_t)key * a.v.token + d)) : z;
   }
-  f32x16 dk[D / 32], dv[D / 32];
+  f32x16 dk[C / 32], dv[C / 32];
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m) { dk[m] = (f32x16)(0.f); dv[m] = (f32x16)(0.f); }
+  for (int m = 0; m < C / 32; ++m) { dk[m] = (f32x16)(0.f); dv[m] = (f32x16)(0.f); }
 
   // queries that see one of the tile's keys: positions first .. end
   const int tile_end = min(first + kKeys, sk.count) - 1;
@@ -367,11 +369,11 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
         for (int j = 0; j < 4; ++j) { s[i + j] = x[j]; e[i + j] = y[j]; }
       }
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
+      for (int i = 0; i < C / 16; ++i)
         s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), kKeysInLds ? read_rows<T>(kt, i, 0) : kf[kKeysInLds ? 0 : i], s);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
-      reads_ahead<kKeysInLds ? 16 : 12, D / 16, kKeysInLds ? 2 : 1, D / 16, 1>();   // (eight of those ahead: what the products begin with)
+      for (int i = 0; i < C / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
+      reads_ahead<kKeysInLds ? 16 : 12, C / 16, kKeysInLds ? 2 : 1, C / 16, 1>();   // (eight of those ahead: what the products begin with)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
       const bool whole = p0 >= low + 31 && q_now + n * 32 + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
@@ -394,12 +396,12 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
         const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
         const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
 #pragma unroll
-        for (int m = 0; m < D / 32; ++m) {
+        for (int m = 0; m < C / 32; ++m) {
           dv[m] = mma32(read_columns<T, D>(qt + my.columns, m, kBytes + (n * 32 + 16 * u) * Tl::kRowBytes), pf, dv[m]);
           dk[m] = mma32(read_columns<T, D>(qt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes), ds, dk[m]);
         }
       }
-      reads_ahead<kKeysInLds ? 8 : 4, 4 * (D / 32), 2>();
+      reads_ahead<kKeysInLds ? 8 : 4, 4 * (C / 32), 2>();
     }
   }
 
@@ -463,21 +465,21 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
     uint64_t* odds = (uint64_t*)(smem + kStatsAt);
     __syncthreads();                                             // the tiles are done with
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < C / 32; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        sums[((wave * (D / 32) + m) * 32 + i) * 64 + lane] = dk[m][i];
-        sums[((wave * (D / 32) + m) * 32 + 16 + i) * 64 + lane] = dv[m][i];
+        sums[((wave * (C / 32) + m) * 32 + i) * 64 + lane] = dk[m][i];
+        sums[((wave * (C / 32) + m) * 32 + 16 + i) * 64 + lane] = dv[m][i];
       }
     __syncthreads();
     f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);                 // a wavefront joins 32 columns
-    if (wave < D / 32) {
+    if (wave < C / 32) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          x[i] += sums[((w * (D / 32) + wave) * 32 + i) * 64 + lane];
-          y[i] += sums[((w * (D / 32) + wave) * 32 + 16 + i) * 64 + lane];
+          x[i] += sums[((w * (C / 32) + wave) * 32 + i) * 64 + lane];
+          y[i] += sums[((w * (C / 32) + wave) * 32 + 16 + i) * 64 + lane];
         }
         x[i] *= a.scale;
         test = fmaf(x[i], 0.f, fmaf(y[i], 0.f, test));
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
     if (lane == 0) odds[wave] = odd;
     __syncthreads();
     odd = odds[0] | odds[1] | odds[2] | odds[3];
-    if (wave < D / 32 && there && !(odd >> (lane & 31) & 1)) {
+    if (wave < C / 32 && there && !(odd >> (lane & 31) & 1)) {
       store_block<T>(x, wave, dk_to + (int64_t)key * a.dk.token, half, a.dim);
       store_block<T>(y, wave, dv_to + (int64_t)key * a.dv.token, half, a.dim);
     }
@@ -495,7 +497,7 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
     return;
   }
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m) {
+  for (int m = 0; m < C / 32; ++m) {
     dk[m] *= a.scale;
 #pragma unroll
     for (int i = 0; i < 16; ++i) test = fmaf(dk[m][i], 0.f, fmaf(dv[m][i], 0.f, test));
@@ -503,13 +505,13 @@ __global__ __launch_bounds__(256, kShare ? (D <= 64 ? 3 : 2) : 1) void attention
   const uint64_t odd = odd_keys(test);
   if (parts == 1) {
     if (there && !(odd >> (lane & 31) & 1)) {
-      store_columns<T, D>(dk, dk_to + (int64_t)key * a.dk.token, half, a.dim);
-      store_columns<T, D>(dv, dv_to + (int64_t)key * a.dv.token, half, a.dim);
+      store_columns<T, C>(dk, dk_to + (int64_t)key * a.dk.token, half, a.dim);
+      store_columns<T, C>(dv, dv_to + (int64_t)key * a.dv.token, half, a.dim);
     }
   } else if (!(odd >> (lane & 31) & 1)) {
     float* to = part_to + (int64_t)(lane & 31) * a.dim;
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < C / 32; ++m)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int d = 32 * m + 2 * i + 4 * half;
@@ -554,7 +556,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 //   32 blocks 28 -> 25, 47 -> 39;  128 blocks, window of 256, 38 -> 37, 63 -> 62, no window 76 -> 61, 134 -> 97;  256 blocks 44 -> 52, 72 -> 94
 constexpr int64_t kFewQueryBlocks = 128;
 
-template <typename T, int D>
+template <typename T, int C>
 int backward(const AttentionArgs& a, void* stream) {
   const int64_t q_heads = (int64_t)a.q_heads * a.batch, kv_heads = (int64_t)a.kv_heads * a.batch;
   auto tiles_of = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
@@ -566,19 +568,24 @@ int backward(const AttentionArgs& a, void* stream) {
   if (q_blocks > 0x7fffffff || k_blocks > 0x7fffffff || join_blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   hipStream_t s = (hipStream_t)stream;
   const dim3 q_grid((unsigned)q_blocks), k_grid((unsigned)k_blocks), block(256);
-  if (q_blocks && q_share) attention_dq_kernel<T, D, true><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
-  else if (q_blocks) attention_dq_kernel<T, D, false><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
-  if (k_blocks && !a.few_keys) attention_dkv_kernel<T, D, true><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
-  else if (k_blocks) attention_dkv_kernel<T, D, false><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
+  if (q_blocks && q_share) attention_dq_kernel<T, C, true><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  else if (q_blocks) attention_dq_kernel<T, C, false><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  if (k_blocks && !a.few_keys) attention_dkv_kernel<T, C, true><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
+  else if (k_blocks) attention_dkv_kernel<T, C, false><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
   if (join_blocks) attention_join_kernel<T><<<dim3((unsigned)join_blocks), block, 0, s>>>(a, (int)k_tiles, cut, first_cut);
   return (int)hipGetLastError();
+}
+
+template <typename T>
+int by_columns(const AttentionArgs& a, void* stream) {
+  return a.dim <= 64 ? backward<T, 64>(a, stream) : a.dim <= 96 ? backward<T, 96>(a, stream) : backward<T, 128>(a, stream);
 }
 
 }  // namespace
 
 int launch_attention_backward(const AttentionArgs& a, int32_t dtype, void* stream) {
-  if (dtype == ARROW_BF16) return a.dim <= 64 ? backward<__bf16, 64>(a, stream) : backward<__bf16, 128>(a, stream);
-  return a.dim <= 64 ? backward<_Float16, 64>(a, stream) : backward<_Float16, 128>(a, stream);
+  if (dtype == ARROW_BF16) return by_columns<__bf16>(a, stream);
+  return by_columns<_Float16>(a, stream);
 }
 
 }  // namespace arrow
