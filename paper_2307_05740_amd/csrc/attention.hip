@@ -4,8 +4,8 @@
 // lane has one query's scores in its registers: the running maximum and sum of the softmax need one exchange, between lane halves, and
 // the probabilities are at once the B operand of O^T += V^T P^T.
 //
-// Four wavefronts share the tiles and have 128 queries together.  Where that gives too few workgroups to fill the chip, the four have the
-// same 32 queries, tiles of 32 keys in turn and of their own, and join their results in LDS.
+// Four wavefronts share the tiles and have 128 queries together.  Where that gives too few workgroups to fill the chip, they have 64 queries, half of every tile
+// each, or the same 32 queries and every fourth tile, of 32 keys and its own, and join their results in LDS.
 #include <algorithm>
 
 #include "attention_common.h"
@@ -13,13 +13,17 @@
 namespace arrow {
 namespace {
 
-// Whether workgroups of 32 queries are faster than `blocks` of 128: up to 64 of those, 128 for small heads, and twice as many where a row
-// sees 2000 keys or more, whose tiles the four wavefronts go through four times as fast (us, of 128 -> of 32 queries):
-//   heads of 64:   8 blocks  7.2 ->  5.8, 64 blocks 11.4 ->  7.2, 128 blocks 11.7 ->  9.6, 256 blocks 17.0 -> 22.1, of 4000 keys 56.8 -> 40.9
-//   heads of 128:  8 blocks  8.6 ->  7.1, 64 blocks 13.8 -> 10.0, 128 blocks 15.5 -> 20.6, of 2000 keys 39.5 -> 27.3, 256 of 4000 73.8 -> 78.1
-bool few_blocks(int64_t blocks, const AttentionArgs& a) {
+// How many groups of 32 queries a workgroup has, by `blocks`, the workgroups of four groups that there would be.  One up to 64 of those, 128 for small heads, and
+// twice as many where a row sees 2000 keys or more; two up to 256 of them, 384 without a window, whose workgroups are half as long on average, and 512 for
+// small heads (us, of one / two / four groups):
+//   heads of 64:   128 blocks, window 256, 8.9 / 9.1 / 12.1, no window, 2048 keys, 19.0 / 25.0 / 32.5;  256 blocks 15.9 / 11.0 / 12.6, 27.1 / 26.1 / 33.1
+//                  512 blocks 27.2 / 16.8 / 16.7, 46.2 / 30.2 / 34.6;  768 blocks 40.3 / 23.2 / 22.5, 70.5 / 44.3 / 41.2
+//   heads of 128:  64 blocks 9.6 / 11.4 / 14.6, 21.2 / 31.1 / 40.1;  128 blocks 17.4 / 11.8 / 15.3, 28.9 / 33.1 / 41.2;  256 blocks 32.6 / 16.2 / 16.4,
+//                  52.6 / 36.1 / 42.3;  384 blocks 49.3 / 25.4 / 23.2, 76.6 / 42.1 / 46.0;  512 blocks 62.9 / 31.0 / 24.8, 100 / 53.0 / 49.9
+int query_groups(int64_t blocks, const AttentionArgs& a) {
   const int64_t seen = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks, a.k_len) : a.k_len;
-  return blocks <= (a.dim <= 64 ? 128 : 64) * (seen >= 2000 ? 2 : 1);
+  if (blocks <= (a.dim <= 64 ? 128 : 64) * (seen >= 2000 ? 2 : 1)) return 1;
+  return blocks <= (a.dim <= 64 ? 512 : a.window == 0 && seen >= 1000 ? 384 : 256) ? 2 : 4;
 }
 
 // One row of the result in plain steps, the wavefront's lanes over its columns, by the row's own visible keys alone.  Matrix
@@ -44,17 +48,20 @@ __device__ __noinline__ void plain_row(const T* q, const char* k, const char* v,
   if (mine) { o[d] = (T)a0; o[d + 1] = (T)a1; }
 }
 
-template <typename T, int C, bool kShare>
-__global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
+// kGroups: how many groups of 32 queries the four wavefronts have.
+template <typename T, int C, int kGroups>
+__global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
   constexpr int D = columns_of_tile(C);
   using Tl = Tile<D>;
-  constexpr int kStep = kShare ? 64 : 32;                     // keys of a tile
-  constexpr int kTurns = kShare ? 1 : 4;                      // a wavefront has every kTurns-th tile
+  constexpr bool kShare = kGroups > 1;                        // tiles
+  constexpr int kStep = kShare ? 64 : 32, kTurns = kShare ? 1 : 4;   // keys of a tile; a wavefront has every kTurns-th tile
+  constexpr int kMine = kGroups == 4 ? 64 : 32;               // and so many of its keys
+  constexpr int kParts = 4 / kGroups;                         // wavefronts with the same queries
   constexpr int kBytes = kStep * Tl::kRowBytes;
   // keys and values, two tiles each, of all wavefronts or of each one; joined afterwards: the sums of each, its maxima and totals
   constexpr int kRoom = 4 * kTurns * kBytes;
-  static_assert(kShare || kRoom >= 4 * D * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kRoom + (kShare ? 0 : 4 * (2 * 64 * 4 + 8))];
+  static_assert(kParts == 1 || kRoom >= 4 * C * 32 * 4, "room for the sums");
+  __shared__ __align__(1024) unsigned char smem[kRoom + (kParts == 1 ? 0 : 4 * (2 * 64 * 4 + 8))];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   // Workgroups next to each other go to different dies: an item of every sequence and key head in turn, so that a die has the same keys again
   // and again (8192 queries, 32/8 heads of 128: 300 -> 270 us); of one, the longest rows of a triangle first.
@@ -63,10 +70,11 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
   const int kv = unit % a.kv_heads, b = unit / a.kv_heads, head = kv * a.group + g;
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
-  constexpr int kRows = kShare ? kQueryTile : 32;
+  constexpr int kRows = 32 * kGroups;
   const int first = tile * kRows;
   if (first >= sq.count) return;
-  const int mine = first + (kShare ? wave * 32 : 0);          // the first of this wavefront's queries
+  const int group = wave % kGroups, part = wave / kGroups;
+  const int mine = first + group * 32;                        // the first of this wavefront's queries
   const int shift = sk.count - sq.count;                      // position of query 0
   const int row = mine + (lane & 31);                         // this lane's query
   const bool there = row < sq.count;
@@ -109,26 +117,27 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
     if constexpr (kShare) wait_for_tiles();
     else wait_for_own_tiles();
     if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
-    const uint32_t kt = lds_address(base) + 2 * now * kBytes, vt = kt + kBytes;
-    const int k0 = seen.at(t) * kStep;
+    const int skip = kMine < kStep ? part * kMine : 0;        // (keys of the tile that are another wavefront's)
+    const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
+    const int k0 = seen.at(t) * kStep + skip;
     // no query of this wavefront sees the tile
-    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
+    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kMine - 1 <= low - a.window)) continue;
 
-    f32x16 s[kStep / 32];
+    f32x16 s[kMine / 32];
 #pragma unroll
-    for (int n = 0; n < kStep / 32; ++n) s[n] = (f32x16)(0.f);
+    for (int n = 0; n < kMine / 32; ++n) s[n] = (f32x16)(0.f);
 #pragma unroll
     for (int i = 0; i < C / 16; ++i)                          // (in turn: a product waits for the last one on the same sums)
 #pragma unroll
-      for (int n = 0; n < kStep / 32; ++n) s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
-    reads_ahead<6, (kStep / 32) * (C / 16), 1>();
+      for (int n = 0; n < kMine / 32; ++n) s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
+    reads_ahead<6, (kMine / 32) * (C / 16), 1>();
     // every query sees every key: nothing to mask
-    const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
+    const bool whole = k0 + kMine - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kMine <= a.sinks);
     if (!whole) {
       const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
       const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
 #pragma unroll
-      for (int n = 0; n < kStep / 32; ++n)
+      for (int n = 0; n < kMine / 32; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = n * 32 + 8 * (i / 4) + i % 4;
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
     }
     float most = s[0][0];
 #pragma unroll
-    for (int n = 0; n < kStep / 32; ++n)
+    for (int n = 0; n < kMine / 32; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
     most = max_halves(most) * c;
@@ -153,9 +162,9 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
       for (int m = 0; m < C / 32; ++m) acc[m] *= by;
     }
     const float off = top == minus_infinity() ? 0.f : top;
-    x8<T> pf[kStep / 16];
+    x8<T> pf[kMine / 16];
 #pragma unroll
-    for (int n = 0; n < kStep / 32; ++n) {
+    for (int n = 0; n < kMine / 32; ++n) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -off));
@@ -167,11 +176,11 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
                                   s[n][8 * u + 6], s[n][8 * u + 7]);
     }
 #pragma unroll
-    for (int u = 0; u < kStep / 16; ++u)
+    for (int u = 0; u < kMine / 16; ++u)
 #pragma unroll
       for (int m = 0; m < C / 32; ++m)
         acc[m] = mma32(read_columns<T, D>(vt + my.columns, m, 16 * u * Tl::kRowBytes), pf[u], acc[m]);
-    reads_ahead<8, (kStep / 16) * (C / 32), 2>();
+    reads_ahead<8, (kMine / 16) * (C / 32), 2>();
   }
 
   total = add_halves(total);
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
                    a.scale, __shfl(lse, r, 64));
     }
   };
-  if constexpr (kShare) {
+  if constexpr (kParts == 1) {
     const float by = over(total), lse = lse_of(top, total);
     if (a.lse && there && half == 0) a.lse[stat] = lse;
     float test = 0.f;                                         // NaN where a result is not finite
@@ -215,47 +224,58 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_forward_kernel(
     tops[wave * 64 + lane] = top;
     totals[wave * 64 + lane] = total;
     __syncthreads();
-    float all = tops[lane], share[4];
+    float all = minus_infinity(), share[kParts];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) all = fmaxf(all, tops[w * 64 + lane]);
+    for (int w = 0; w < kParts; ++w) all = fmaxf(all, tops[(group + kGroups * w) * 64 + lane]);
     const float off = all == minus_infinity() ? 0.f : all;
     total = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      share[w] = __builtin_amdgcn_exp2f(tops[w * 64 + lane] - off);
-      total = fmaf(share[w], totals[w * 64 + lane], total);
+    for (int w = 0; w < kParts; ++w) {
+      share[w] = __builtin_amdgcn_exp2f(tops[(group + kGroups * w) * 64 + lane] - off);
+      total = fmaf(share[w], totals[(group + kGroups * w) * 64 + lane], total);
     }
     const float by = over(total), lse = lse_of(all, total);
-    if (a.lse && there && half == 0 && wave == 0) a.lse[stat] = lse;
-    // a wavefront joins 32 columns
-    f32x16 r = (f32x16)(0.f);
+    if (a.lse && there && half == 0 && part == 0) a.lse[stat] = lse;
+    // a wavefront joins every kParts-th block of 32 columns
+    constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
+    f32x16 r[kJoined];
     float test = 0.f;
-    if (wave < C / 32) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
+    for (int n = 0; n < kJoined; ++n) {
+      const int m = part + n * kParts;
+      r[n] = (f32x16)(0.f);
+      if (m >= kBlocks) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) r[i] = fmaf(share[w], sums[((w * (C / 32) + wave) * 16 + i) * 64 + lane], r[i]);
+      for (int w = 0; w < kParts; ++w)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) { r[i] *= by; test = fmaf(r[i], 0.f, test); }
+        for (int i = 0; i < 16; ++i) r[n][i] = fmaf(share[w], sums[(((group + kGroups * w) * kBlocks + m) * 16 + i) * 64 + lane], r[n][i]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) { r[n][i] *= by; test = fmaf(r[n][i], 0.f, test); }
     }
     uint64_t odd = odd_rows(test, lse);
     if (lane == 0) odds[wave] = odd;
     __syncthreads();
-    odd = odds[0] | odds[1] | odds[2] | odds[3];
-    if (wave < C / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, o + (int64_t)row * a.o.token, half, a.dim);
-    if (wave == 0) plain_rows(odd, lse);
+#pragma unroll
+    for (int w = 0; w < kParts; ++w) odd |= odds[group + kGroups * w];
+#pragma unroll
+    for (int n = 0; n < kJoined; ++n) {
+      const int m = part + n * kParts;
+      if (m < kBlocks && there && !(odd >> (lane & 31) & 1)) store_block<T>(r[n], m, o + (int64_t)row * a.o.token, half, a.dim);
+    }
+    if (part == 0) plain_rows(odd, lse);
   }
 }
 
 template <typename T, int C>
 int forward(const AttentionArgs& a, void* stream) {
   const int64_t heads = (int64_t)a.q_heads * a.batch, tiles = ((int64_t)a.q_len + kQueryTile - 1) / kQueryTile;
-  const bool share = !few_blocks(tiles * heads, a);
-  const int64_t rows = share ? tiles : ((int64_t)a.q_len + 31) / 32, blocks = rows * heads;
+  const int groups = query_groups(tiles * heads, a);
+  const int64_t rows = ((int64_t)a.q_len + 32 * groups - 1) / (32 * groups), blocks = rows * heads;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(256);
-  if (share) attention_forward_kernel<T, C, true><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
-  else attention_forward_kernel<T, C, false><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  if (groups == 4) attention_forward_kernel<T, C, 4><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  else if (groups == 2) attention_forward_kernel<T, C, 2><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  else attention_forward_kernel<T, C, 1><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
   return (int)hipGetLastError();
 }
 

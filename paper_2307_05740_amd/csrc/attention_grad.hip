@@ -14,22 +14,25 @@ namespace {
 //
 // D is <do_i, o_i> as well, but o has been rounded, and where a row has one large probability dS is a small difference of <do_i, v_j>
 // and D.  dS is formed with <do_i, o_i>; the error -sum_j dS(i,j) of that comes out with the row, in 32 bits.  dq is put right with one
-// product more, sum_j P(i,j) k_j times that sum.  Workgroups of few rows, where all sequences of up to 64 keys are, take the sum of the dS as
-// they were rounded for their product: the weights then add up to nothing, as the true gradient's do, which a row of few keys notices
+// product more, sum_j P(i,j) k_j times that sum.  Workgroups whose wavefronts share queries, where all sequences of up to 64 keys are, take the
+// sum of the dS as they were rounded for their product: the weights then add up to nothing, as the true gradient's do, which a row of few keys notices
 // (dq of 5 keys off by 1.55 times what rounding dq alone does, and 1.4 so; for long rows the same, and 15 % of the kernel's time).
 //
-// kShare: as in the forward kernel, wavefronts of 32 queries each share tiles of keys, or have the same 32 and every fourth tile.
-template <typename T, int C, bool kShare>
-__global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(AttentionArgs a, int tiles) {
+// kGroups: as in the forward kernel, how many groups of 32 queries the four wavefronts have.
+template <typename T, int C, int kGroups>
+__global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(AttentionArgs a, int tiles) {
   constexpr int D = columns_of_tile(C);
   using Tl = Tile<D>;
+  constexpr bool kShare = kGroups > 1;                           // tiles
   constexpr bool kQueriesInLds = D > 64;                         // no registers are left for them
-  constexpr int kStep = kQueriesInLds || !kShare ? 32 : 64, kBytes = kStep * Tl::kRowBytes;   // keys of a tile
-  constexpr int kTurns = kShare ? 1 : 4, kRows = kShare ? kQueryTile : 32;
-  // k and v, two tiles each, of all wavefronts or of each one, or their sums to be joined; the queries; sums of dS to be joined
-  constexpr int kQueriesAt = 4 * kTurns * kBytes, kRestAt = kQueriesAt + (kQueriesInLds ? kRows * Tl::kRowBytes : 0);
-  static_assert(kShare || kQueriesAt >= 4 * 2 * D * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kRestAt + (kShare ? 0 : 2 * 4 * 64 * 4 + 4 * 8)];
+  constexpr int kMine = kQueriesInLds || kGroups < 4 ? 32 : 64;  // keys of a tile that a wavefront takes
+  constexpr int kStep = kGroups == 2 ? 64 : kMine, kBytes = kStep * Tl::kRowBytes;   // keys of a tile
+  constexpr int kTurns = kShare ? 1 : 4, kRows = 32 * kGroups, kParts = 4 / kGroups;
+  // k and v, two tiles each, of all wavefronts or of each one, or their sums to be joined; the queries, afterwards the sums of dS to be joined
+  constexpr int kQueriesAt = 4 * kTurns * kBytes, kQueriesBytes = kQueriesInLds ? kRows * Tl::kRowBytes : 0;
+  constexpr int kRestBytes = kParts == 1 ? 0 : 2 * 4 * 64 * 4 + 4 * 8;
+  static_assert(kParts == 1 || kQueriesAt >= 4 * C * 32 * 4, "room for the sums");
+  __shared__ __align__(1024) unsigned char smem[kQueriesAt + (kQueriesBytes > kRestBytes ? kQueriesBytes : kRestBytes)];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;   // as in the forward kernel
   const int g = item % a.group, tile = tiles - 1 - item / a.group;
@@ -39,7 +42,8 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   const int first = tile * kRows;
   if (first >= sq.count) return;
   const int shift = sk.count - sq.count;
-  const int mine = first + (kShare ? wave * 32 : 0);
+  const int group = wave % kGroups, split = wave / kGroups;
+  const int mine = first + group * 32;
   const int row = mine + (lane & 31);
   const bool there = row < sq.count;
   const int p = row + shift;
@@ -94,15 +98,16 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
     if constexpr (kShare) wait_for_tiles();
     else wait_for_own_tiles();
     if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
-    const uint32_t kt = lds_address(base) + 2 * now * kBytes, vt = kt + kBytes;
-    const uint32_t qt = kQueriesInLds ? here(lds_address(room) + kQueriesAt + sharer * 32 * Tl::kRowBytes + my.rows) : 0;
-    const int k0 = seen.at(t) * kStep;
-    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kStep - 1 <= low - a.window)) continue;
-    const bool whole = k0 + kStep - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kStep <= a.sinks);
+    const int skip = kMine < kStep ? split * kMine : 0;
+    const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
+    const uint32_t qt = kQueriesInLds ? here(lds_address(room) + kQueriesAt + group * 32 * Tl::kRowBytes + my.rows) : 0;
+    const int k0 = seen.at(t) * kStep + skip;
+    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kMine - 1 <= low - a.window)) continue;
+    const bool whole = k0 + kMine - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kMine <= a.sinks);
     const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
     const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
 #pragma unroll
-    for (int n = 0; n < kStep / 32; ++n) {
+    for (int n = 0; n < kMine / 32; ++n) {
       // the products begin with what is taken off them (which is in one register each, not in 16 ready for that, where those are needed)
       f32x16 s = (f32x16)(kQueriesInLds ? here(off) : off), e = (f32x16)(kQueriesInLds ? here(-delta) : -delta);
 #pragma unroll
@@ -131,7 +136,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
       for (int u = 0; u < 2; ++u) {
         const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
         const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
-        if constexpr (!kShare) kept = add8(ds, kept);
+        if constexpr (kParts > 1) kept = add8(ds, kept);
 #pragma unroll
         for (int m = 0; m < C / 32; ++m) {
           const x8<T> kf = read_columns<T, D>(kt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes);
@@ -144,7 +149,7 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
   }
 
   rest = add_halves(rest);
-  kept = kShare ? rest : add_halves(kept);
+  kept = kParts == 1 ? rest : add_halves(kept);
   T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
   // Rows to be done in plain steps, as in the forward kernel: with a result that is not finite, though what they see may be
   auto odd_rows = [&](float test) {
@@ -176,64 +181,68 @@ __global__ __launch_bounds__(256, kShare ? 2 : 1) void attention_dq_kernel(Atten
     }
   };
   float test = 0.f;                                           // NaN where a result is not finite
-  if constexpr (kShare) {
-    if (there && half == 0) {
-      a.off[stat] = off;
-      a.delta[stat] = -(delta + rest);
-    }
-#pragma unroll
-    for (int m = 0; m < C / 32; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
-        test = fmaf(acc[m][i], 0.f, test);
-      }
-    const uint64_t odd = odd_rows(test);
-    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, C>(acc, dq, half, a.dim);
-    plain_rows(odd);
-  } else {
-    float *sums = (float*)smem, *rests = (float*)(smem + kRestAt);
-    __syncthreads();                                            // the tiles are done with
-#pragma unroll
-    for (int m = 0; m < C / 32; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sums[((wave * (C / 32) + m) * 32 + i) * 64 + lane] = acc[m][i];
-        sums[((wave * (C / 32) + m) * 32 + 16 + i) * 64 + lane] = pk[m][i];
-      }
+  uint64_t* odds = (uint64_t*)(smem + kQueriesAt + 2 * 4 * 64 * 4);
+  if constexpr (kParts > 1) {
+    float* rests = (float*)(smem + kQueriesAt);
+    wait_for_tiles();                                           // the tiles and queries are done with, or there and not needed
     rests[wave * 64 + lane] = rest;
     rests[(4 + wave) * 64 + lane] = kept;
     __syncthreads();
     rest = kept = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      rest += rests[w * 64 + lane];
-      kept += rests[(4 + w) * 64 + lane];
+    for (int w = 0; w < kParts; ++w) {
+      rest += rests[(group + kGroups * w) * 64 + lane];
+      kept += rests[(4 + group + kGroups * w) * 64 + lane];
     }
-    if (there && half == 0 && wave == 0) {
-      a.off[stat] = off;
-      a.delta[stat] = -(delta + rest);
-    }
-    f32x16 r = (f32x16)(0.f);                                   // a wavefront joins 32 columns
-    if (wave < C / 32) {
+  }
+  if (there && half == 0 && split == 0) {
+    a.off[stat] = off;
+    a.delta[stat] = -(delta + rest);
+  }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float x = 0.f, y = 0.f;
+  for (int m = 0; m < C / 32; ++m)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          x += sums[((w * (C / 32) + wave) * 32 + i) * 64 + lane];
-          y += sums[((w * (C / 32) + wave) * 32 + 16 + i) * 64 + lane];
-        }
-        r[i] = a.scale * fmaf(-kept, y, x);
-        test = fmaf(r[i], 0.f, test);
-      }
+    for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
+  if constexpr (kParts == 1) {
+#pragma unroll
+    for (int m = 0; m < C / 32; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) test = fmaf(acc[m][i], 0.f, test);
+    const uint64_t odd = odd_rows(test);
+    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, C>(acc, dq, half, a.dim);
+    plain_rows(odd);
+  } else {
+    float* sums = (float*)smem;
+    constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
+#pragma unroll
+    for (int m = 0; m < kBlocks; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[((wave * kBlocks + m) * 16 + i) * 64 + lane] = acc[m][i];
+    __syncthreads();
+    f32x16 r[kJoined];                                          // a wavefront joins every kParts-th block of 32 columns
+#pragma unroll
+    for (int n = 0; n < kJoined; ++n) {
+      const int m = split + n * kParts;
+      r[n] = (f32x16)(0.f);
+      if (m >= kBlocks) continue;
+#pragma unroll
+      for (int w = 0; w < kParts; ++w)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[n][i] += sums[(((group + kGroups * w) * kBlocks + m) * 16 + i) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) test = fmaf(r[n][i], 0.f, test);
     }
-    uint64_t odd = odd_rows(test), *odds = (uint64_t*)(rests + 2 * 4 * 64);
+    uint64_t odd = odd_rows(test);
     if (lane == 0) odds[wave] = odd;
     __syncthreads();
-    odd = odds[0] | odds[1] | odds[2] | odds[3];
-    if (wave < C / 32 && there && !(odd >> (lane & 31) & 1)) store_block<T>(r, wave, dq, half, a.dim);
-    if (wave == 0) plain_rows(odd);
+#pragma unroll
+    for (int w = 0; w < kParts; ++w) odd |= odds[group + kGroups * w];
+#pragma unroll
+    for (int n = 0; n < kJoined; ++n) {
+      const int m = split + n * kParts;
+      if (m < kBlocks && there && !(odd >> (lane & 31) & 1)) store_block<T>(r[n], m, dq, half, a.dim);
+    }
+    if (split == 0) plain_rows(odd);
   }
 }
 
@@ -552,24 +561,34 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
       round8<T>(sum[0], sum[1], sum[2], sum[3], sum[4], sum[5], sum[6], sum[7]);
 }
 
-// Up to so many workgroups of 128 queries, those of 32 are faster (gradients in us, of 128 -> of 32 queries, heads of 64 and of 128):
-//   32 blocks 28 -> 25, 47 -> 39;  128 blocks, window of 256, 38 -> 37, 63 -> 62, no window 76 -> 61, 134 -> 97;  256 blocks 44 -> 52, 72 -> 94
-constexpr int64_t kFewQueryBlocks = 128;
+// How many groups of 32 queries a workgroup of the dq kernel has, by `blocks`, the workgroups of four groups that there would be: as in the forward kernel, with other
+// limits (all three kernels' us, of one / two / four groups):
+//   heads of 64:   64 blocks, window 256, 28.1 / 29.1 / 33.0, no window, 2048 keys, 49.4 / 54.8 / 65.4;  128 blocks 37.9 / 36.0 / 40.1, 60.0 / 62.7 / 72.3
+//                  256 blocks 53.4 / 46.0 / 46.8, 85.6 / 77.7 / 83.2;  384 blocks 63.5 / 53.4 / 52.5, 109 / 92.5 / 98.2;  512 blocks 73.5 / 61.5 / 57.5, 124 / 104 / 102
+//   heads of 128:  64 blocks 37.4 / 38.4 / 44.6, 71.3 / 77.4 / 103;  128 blocks 61.1 / 51.3 / 57.4, 91.7 / 89.2 / 113;  256 blocks 92.6 / 63.7 / 64.0,
+//                  154 / 119 / 137;  384 blocks 118 / 76.8 / 76.6, 211 / 150 / 160;  512 blocks 160 / 105 / 98, 254 / 177 / 175
+// Up to 64 keys two, which are all queries of such a sequence as a rule, for what the kernel says of rows of few keys.
+int query_groups(int64_t blocks, const AttentionArgs& a) {
+  if (a.k_len <= 64) return 2;
+  if (blocks <= 64) return 1;
+  return blocks <= (a.window == 0 && a.k_len >= 1000 ? 384 : 256) ? 2 : 4;
+}
 
 template <typename T, int C>
 int backward(const AttentionArgs& a, void* stream) {
   const int64_t q_heads = (int64_t)a.q_heads * a.batch, kv_heads = (int64_t)a.kv_heads * a.batch;
   auto tiles_of = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
-  const bool q_share = tiles_of(a.q_len, kQueryTile) * q_heads > kFewQueryBlocks || a.k_len <= 64;   // (one tile or two)
-  const int64_t q_tiles = tiles_of(a.q_len, q_share ? kQueryTile : 32), k_tiles = tiles_of(a.k_len, a.few_keys ? 32 : kKeyTile);
+  const int groups = query_groups(tiles_of(a.q_len, kQueryTile) * q_heads, a);
+  const int64_t q_tiles = tiles_of(a.q_len, 32 * groups), k_tiles = tiles_of(a.k_len, a.few_keys ? 32 : kKeyTile);
   const int64_t q_blocks = q_tiles * q_heads, k_blocks = (a.sink_tiles * (int64_t)a.sink_parts + (k_tiles - a.sink_tiles) * a.tile_parts) * kv_heads;
   const int first_cut = a.sink_parts > 1 ? 0 : a.sink_tiles, cut = (int)((a.tile_parts > 1 ? k_tiles : a.sink_tiles) - first_cut);
   const int64_t join_blocks = cut > 0 ? (cut * kv_heads * kKeyTile * (a.dim / 8) * 2 + 255) / 256 : 0;
   if (q_blocks > 0x7fffffff || k_blocks > 0x7fffffff || join_blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   hipStream_t s = (hipStream_t)stream;
   const dim3 q_grid((unsigned)q_blocks), k_grid((unsigned)k_blocks), block(256);
-  if (q_blocks && q_share) attention_dq_kernel<T, C, true><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
-  else if (q_blocks) attention_dq_kernel<T, C, false><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  if (q_blocks && groups == 4) attention_dq_kernel<T, C, 4><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  else if (q_blocks && groups == 2) attention_dq_kernel<T, C, 2><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
+  else if (q_blocks) attention_dq_kernel<T, C, 1><<<q_grid, block, 0, s>>>(a, (int)q_tiles);
   if (k_blocks && !a.few_keys) attention_dkv_kernel<T, C, true><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
   else if (k_blocks) attention_dkv_kernel<T, C, false><<<k_grid, block, 0, s>>>(a, (int)k_tiles);
   if (join_blocks) attention_join_kernel<T><<<dim3((unsigned)join_blocks), block, 0, s>>>(a, (int)k_tiles, cut, first_cut);
