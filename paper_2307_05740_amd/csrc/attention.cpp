@@ -90,8 +90,10 @@ AttentionArgs plan(const arrow_attention_t* a) {
   // few steps (gradients in us, of 128 -> of 32 keys, heads of 64 and of 128):
   //   32 workgroups of 8 steps 28 -> 24, 47 -> 36;  64 of 7 steps 36 -> 31, 58 -> 48;  64 of 32 steps 40 -> 42, 69 -> 69
   //   128 of 7 steps 38 -> 45, 63 -> 68;  16 of 32 steps, cut into parts, 33 -> 38, 55 -> 57
+  // They are not cut into parts, and keys that all queries see have more steps than the others (4 sinks, window of 256):
+  //   16 steps 33 -> 28, 45 -> 38;  32 steps 34 -> 41, 46 -> 55;  64 steps 35 -> 66, 51 -> 93
   p.tile_parts = p.sink_parts = 1;
-  p.few_keys = tiles * a->kv_heads * a->batch <= 64 && usual > 1 && usual <= 16;
+  p.few_keys = tiles * a->kv_heads * a->batch <= 64 && usual > 1 && usual <= 16 && (p.sinks == 0 || all <= 24);
   if (p.few_keys) return p;
   p.sink_tiles = (int32_t)std::min(tiles, ceil_div(p.sinks, kKeyTile));
   // A tile is cut into parts where that fills the chip better: the time goes by the rounds of workgroups that it holds at once, and a
