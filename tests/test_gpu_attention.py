@@ -489,3 +489,32 @@ def test_gradients_of_what_is_not_seen(torch, Attention, heads, kv, dim, window,
     got = run(torch, op, q[None], k[None], v[None], bad_do[None])
     check_keys(got, "dv", list(range(n)), [i for i in range(dim) if i != 5])
     assert torch.equal(torch.isfinite(got["dv"][0, :, -1, 5]).cpu(), ~seen[at[0]])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [64, 80, 96, 128])
+@pytest.mark.parametrize("queries,keys,window,sinks", [(300, 300, 0, 0), (290, 333, 70, 5), (300, 130, 64, 0), (65, 257, 100, 100)])
+def test_workgroups_of_128_queries(torch, Attention, dtype, dim, queries, keys, window, sinks):
+    """So many heads that no tile is shared out further; three query heads to a key head, of which the first, the last and one in between are checked."""
+    heads, kv = 600, 200
+    q, d_o = (normal(torch, s, dtype, 1, queries, heads, dim) for s in (1, 4))
+    k, v = (normal(torch, s, dtype, 1, keys, kv, dim) for s in (2, 3))
+    got = run(torch, Attention(window, sinks), q, k, v, d_o)
+    for g in (0, 77, kv - 1):
+        of, at = slice(3 * g, 3 * g + 3), slice(g, g + 1)
+        part = {n: got[n][0, :, of] for n in ("o", "dq")} | {n: got[n][0, :, at] for n in ("dk", "dv")} | {"lse": got["lse"][0, of]}
+        check_sequence(torch, part, q[0, :, of], k[0, :, at], v[0, :, at], window, sinks, d_o=d_o[0, :, of])
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dim,window,sinks", [(64, 50, 4), (96, 0, 0), (128, 50, 4)])
+def test_what_is_not_seen_by_workgroups_of_128_queries(torch, Attention, dim, window, sinks, bad):
+    test_gradients_of_what_is_not_seen(torch, Attention, 240, 240, dim, window, sinks, bad)
+    q, k, v = (normal(torch, s, "bfloat16", 1, 300, 1, dim) for s in (1, 2, 3))
+    want, bound = oracle.attention(q[0, :, 0], k[0, :, 0], v[0, :, 0], window, sinks)
+    k[0, 100:102], v[0, 100:102] = bad, bad
+    o, lse = Attention(window, sinks).forward(q.expand(-1, -1, 240, -1), k, v)
+    rows = [i for i in range(300) if not oracle.visible(300, 300, window, sinks)[i, 100:102].any()]
+    for h in (0, 239):
+        within(torch, "o", o[0, rows, h], want["o"][rows], bound["o"][rows])
+        within(torch, "lse", lse[0, h, rows], want["lse"][rows], bound["lse"][rows])
