@@ -62,7 +62,7 @@ namespace arrow {
 
 EmbeddingPlan plan_embedding(const arrow_embedding_t& e) {
   EmbeddingPlan p{};
-  p.direct = e.tokens <= kDirectTokens;
+  p.direct = e.tokens <= kDirectTokens && (e.rows <= kDirectTable || e.columns * size_of(e.dtype) >= 256);
   int bits = 1;
   while ((int64_t)1 << bits <= e.rows) ++bits;                 // ids 0 .. rows, the last one for those outside the table
   p.few = e.tokens <= kFewTokens;

@@ -405,6 +405,8 @@ __global__ __launch_bounds__(64) void embedding_join_kernel(SumArgs a, G* dW) {
 // faster than the launches it replaces (us, those -> this; ids as in text, of columns in bfloat16; "one": the same id for all):
 //   128 tokens:   32,000 x 512 20 -> 10, 32,000 x 4096 65 -> 52, 1000 x 4096 12 -> 6, 50 x 64 11 -> 5
 //   2048 tokens:  32,000 x 512 23 -> 14, 32,000 x 4096 67 -> 64, 1000 x 4096 18 -> 14, 50 x 64 13 -> 12; one: 40 -> 32, 87 -> 51, 35 -> 35, 28 -> 30
+// and of rows shorter than a slice, which leave lanes idle, up to kDirectTable of them (512 tokens): 75,000 x 32 18 -> 8, 150,000 x 32 18 -> 12, 300,000 x 32 20 -> 19,
+// 600,000 x 32 21 -> 32, 600,000 x 128 41 -> 33.  Beyond kDirectTokens:
 //   4096 tokens:  32,000 x 512 24 -> 21, 32,000 x 4096 73 -> 126, 1000 x 4096 25 -> 23, 50 x 64 16 -> 19; one: 61 -> 57, 112 -> 88, 58 -> 71, 46 -> 56
 constexpr int kDirectRows = 64, kDirectLanes = 16, kDirectBlocks = 1024;
 

@@ -13,6 +13,7 @@ constexpr int kSortTokens = 256;     // of a wavefront of it, at least
 constexpr int kWideDigitBits = 15;   // of the sort of few tokens, at most
 constexpr int kFewTokens = 65535;    // they are counted in 16 bits
 constexpr int kDirectTokens = 2048;  // of a gradient in one launch, at most
+constexpr int kDirectTable = 1 << 18;   // rows of one whose columns fill no slice of 256 bytes, at most
 constexpr int kChunkTokens = 8;      // sorted tokens that a lane group of the sums goes through, a multiple of this: a row's load or two for few
                                      // tokens, and four where there are enough to fill the chip
 

@@ -161,3 +161,11 @@ def test_few_tokens_and_slices_of_columns(torch, Embedding, n, rows, columns, ki
     again = op.backward(dY, ids.int(), dtype=torch.float32)
     check_grad(torch, again, dY, ids, rows, 1.5)
     assert torch.equal(again, op.backward(dY, ids, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("columns", [3, 127, 128, 200])
+def test_few_tokens_of_a_large_table(torch, Embedding, columns):
+    """Rows shorter and longer than a slice, of more rows than one launch takes of the former, and of some fewer."""
+    for rows in (262_144, 262_145, 300_001):
+        dY, ids = normal(torch, 2, "bfloat16", 500, columns), tokens(torch, 3, 500, rows, "text")
+        check_grad(torch, Embedding(rows).backward(dY, ids, torch.full((rows, columns), math.nan, dtype=torch.bfloat16, device="cuda")), dY, ids, rows, 1.0)
