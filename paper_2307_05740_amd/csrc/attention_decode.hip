@@ -5,6 +5,10 @@
 // a running maximum and sum of its own, and are joined in LDS.  Long caches are cut into several stretches; their results go to the
 // workspace and a second kernel joins them.
 //
+// 32 sequences of 4000 to 16,000 tokens, 32/8 heads of 128: 265 us in the first kernel, 5.2 TB/s (a copy: 5.1), 5 us in the second.  One sequence of 1000, 8/2 heads: 6
+// and 3 us, launches and loads that wait for each other.  Tiles of 16 keys are what a wavefront can have on its way in registers beside the one that it
+// works on, four wavefronts to a SIMD; with sixteen wavefronts to a stretch short caches took longer, and loads past the caches cost 10 %.
+//
 // Visible keys are counted without the gap between the first ones and the window, so that stretches are of one length.
 #include "attention_common.h"
 
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
   }
 }
 
-// The results of the stretches of one query head, joined: two columns per lane, every fourth stretch per wavefront.
+// The results of the stretches of one query head, joined: two columns per lane, every fourth stretch per wavefront.  3 to 5 us, most of it the launch.
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves) void attention_decode_join_kernel(CacheArgs a) {
   __shared__ float weights[kMostSplits];

@@ -18,6 +18,10 @@ namespace {
 // sum of the dS as they were rounded for their product: the weights then add up to nothing, as the true gradient's do, which a row of few keys notices
 // (dq of 5 keys off by 1.55 times what rounding dq alone does, and 1.4 so; for long rows the same, and 15 % of the kernel's time).
 //
+// What bounds it: matrix instructions (four products) and the vector instructions between them, at the clock that the power leaves: 8192 tokens, 32/8 heads of
+// 128, window of 2048, 470 us = 1030 TFLOP/s with the product P K, matrix units busy 55 % of the cycles.  Heads of more than 64 leave no registers for the queries, which
+// are read from LDS again and again, and tiles of 32 keys; of 64, 4 x 2048 tokens, window of 512: 57 us.
+//
 // kGroups: as in the forward kernel, how many groups of 32 queries the four wavefronts have.
 template <typename T, int C, int kGroups>
 __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(AttentionArgs a, int tiles) {
@@ -253,6 +257,10 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
 // to the workspace and attention_join_kernel adds them up in order.
 //
 // kShare: wavefronts of 32 keys each share steps, or have the same 32 and every fourth step; tiles are in one part then.
+//
+// What bounds it: as the dq kernel; of 256 registers 128 are sums (heads of 128), so the keys are read from LDS as the queries are there.  8192 tokens, as above: 530 us = 910
+// TFLOP/s, matrix units busy 45 %, LDS 34 % of the cycles; 4 x 2048: 61 us.  The queries come from behind the L2 (1.6 GB); another order of them, in which
+// workgroups of a die read the same ones, took as long.
 template <typename T, int C, bool kShare>
 __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
   constexpr int D = columns_of_tile(C);
@@ -533,7 +541,7 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
   plain_keys(odd);
 }
 
-// Adds up the parts of tiles that were cut, eight columns of a key per thread, dk and dv.
+// Adds up the parts of tiles that were cut, eight columns of a key per thread, dk and dv.  Bound by the parts: 47 MB in 9 us (2 x 1531 tokens, 12/2 heads of 96).
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, int tiles, int cut_tiles, int first_cut) {
   const int pieces = a.dim / 8;
