@@ -263,7 +263,8 @@ def _attention_function():
             @torch.autograd.function.once_differentiable
             def backward(ctx, d_o):
                 q, k, v, o, lse, *offsets = ctx.saved_tensors
-                d_o = d_o if d_o.stride(-1) == 1 and all(s % 8 == 0 for s in d_o.stride()[:-1]) else d_o.contiguous()
+                if d_o.stride(-1) != 1 or d_o.data_ptr() % 16 or any(s % 8 for s in d_o.stride()[:-1]):
+                    d_o = d_o.clone(memory_format=torch.contiguous_format)
                 return None, *ctx.op.backward(d_o, q, k, v, o, lse, None, None, None, *offsets, *ctx.limits), None, None, None, None
 
         _function = Attention

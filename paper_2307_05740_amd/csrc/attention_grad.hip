@@ -1,7 +1,7 @@
 // Attention under an arrow-shaped mask, gradients (include/arrow_attention.h).
 //
 // The probabilities are computed anew from the scores and the saved log-sums.  Two kernels, each with its sums in registers from
-// the first tile to the last, so that no gradient is added up in memory: one over queries for dq (three products), one over keys for dk
+// the first tile to the last, so that no gradient is added up in memory: one over queries for dq (three products, and a fourth that puts it right), one over keys for dk
 // and dv (four).  That is seven products where five would do; the five would take an addition in memory for every tile's dq, whose
 // order either changes from run to run or has to be enforced.
 #include "attention_common.h"

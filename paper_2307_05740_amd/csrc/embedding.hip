@@ -342,10 +342,9 @@ __device__ __forceinline__ void add_chunk(const SumArgs& a, const T* dY, G* dW, 
 
 constexpr int kTableRows = 8;      // rows of dW that a lane group looks over
 
-// Bound by memory: 16,384 tokens of 32,000 x 4096, bfloat16, 78 us = 5.1 TB/s.
-
 // The first workgroups add up the chunks, `slices` of them per 256 >> lanes_log chunks; the others clear the rows of dW that have no tokens.
 // kNoted: begin[] and end[] say which those are; otherwise they hold what they will for such rows, and a row has tokens only where the sorted ids say so.
+// Bound by memory: 16,384 tokens of 32,000 x 4096, bfloat16, 78 us = 5.1 TB/s.
 template <typename T, typename G, int VEC, bool kNoted>
 __global__ __launch_bounds__(256) void embedding_rows_kernel(SumArgs a, const T* dY, G* dW, int64_t chunks, int chunk_blocks, int slices) {
   const int lane = threadIdx.x & ((1 << a.lanes_log) - 1), in = threadIdx.x >> a.lanes_log, abreast = 256 >> a.lanes_log;

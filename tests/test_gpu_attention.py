@@ -518,3 +518,19 @@ def test_what_is_not_seen_by_workgroups_of_128_queries(torch, Attention, dim, wi
     for h in (0, 239):
         within(torch, "o", o[0, rows, h], want["o"][rows], bound["o"][rows])
         within(torch, "lse", lse[0, h, rows], want["lse"][rows], bound["lse"][rows])
+
+
+def test_gradients_that_lie_anywhere(torch, Attention):
+    """What autograd hands over as the gradient of o: one value for all, a part of a larger tensor at an odd address, transposed."""
+    q, k, v = (normal(torch, s, "bfloat16", 1, 70, 2, 64) for s in (1, 2, 3))
+    op = Attention(30, 2)
+    w = normal(torch, 4, "bfloat16", 1, 70, 2, 64)
+    uses = {"sum": (lambda o: o.sum(), torch.ones_like(w)), "odd": (lambda o: (torch.cat([o[..., :3], o], -1)[..., 3:] * w).sum(), w),
+            "flat": (lambda o: (torch.cat([torch.zeros(3, dtype=o.dtype, device="cuda"), o.flatten()])[3:] * w.flatten()).sum(), w),
+            "across": (lambda o: (o.transpose(1, 3).contiguous() * w.transpose(1, 3).contiguous()).sum(), w)}
+    for name, (use, d_o) in uses.items():
+        x = [t.clone().requires_grad_() for t in (q, k, v)]
+        o = op(*x)
+        use(o).backward()
+        got = dict(zip(("dq", "dk", "dv"), (t.grad[0] for t in x)), o=o[0].detach(), lse=op.forward(q, k, v)[1][0])
+        check_sequence(torch, got, q[0], k[0], v[0], 30, 2, d_o=d_o[0])
