@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
   }
 
   // A tile on its way: of key col, the pieces 4 s + quarter of its row.  Nothing here branches: the loads of one tile are to be on their way while
-  // another's are waited for.  Pieces beyond the row are read as its last one, where zeros of q and unused sums meet them; keys that are not
+  // another's are waited for.  Pieces beyond the row are read as its last one, and cleared or meet unused sums below; keys that are not
   // visible as q, whose scores are masked and whose values are cleared below.
   x8<T> kf[kPer], vf[kPer];
   uint32_t visible = 0;                                          // of the tile's keys, the same in all lanes
@@ -137,6 +137,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
   }
   while (tile < tile1) {
     f32x4 s = (f32x4)(0.f);
+    if (c.dim < D) {                                             // (zeros of q times an infinity are none)
+      const x8<T> z = {};
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) kf[i] = 32 * i + 8 * quarter < c.dim ? kf[i] : z;
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) s = mma16(kf[i], qf[i], s);
     if (visible != 0xffff) {

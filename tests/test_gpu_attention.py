@@ -534,3 +534,23 @@ def test_gradients_that_lie_anywhere(torch, Attention):
         use(o).backward()
         got = dict(zip(("dq", "dk", "dv"), (t.grad[0] for t in x)), o=o[0].detach(), lse=op.forward(q, k, v)[1][0])
         check_sequence(torch, got, q[0], k[0], v[0], 30, 2, d_o=d_o[0])
+
+
+@pytest.mark.parametrize("dim", [40, 64, 80, 128])
+def test_keys_that_their_scores_rule_out(torch, Attention, dim):
+    """A key of minus infinity where queries are positive has no weight, first or last columns alike."""
+    n, at = 90, 40
+    for column in (0, dim - 1):
+        (kp, vp), table, lens, rows = paged(torch, "bfloat16", [n], 16, 1, dim)
+        k, v = rows[0]
+        q = normal(torch, 3, "bfloat16", 1, n, 1, dim)
+        q[..., column] = q[..., column].abs() + 0.5
+        seen = oracle.visible(n, n, 0, 0, "cuda")
+        seen[:, at] = False
+        want, bound = oracle.attention(q[0, :, 0], k[:, 0], v[:, 0], seen=seen)
+        k[at, 0, column] = -math.inf
+        kp[table[0, at // 16], at % 16, 0, column] = -math.inf
+        o, _ = Attention().forward(q, k[None], v[None])
+        within(torch, "o", o[0, :, 0], want["o"], bound["o"])
+        o = Attention().decode(q[:, -1], kp, vp, table, lens, n)
+        within(torch, "o of the last token", o[0], want["o"][-1:], bound["o"][-1:])
