@@ -65,9 +65,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
   const int length = (int)max((int64_t)0, min((int64_t)c.lengths[b], room));
   const int begin = c.window ? max(0, length - c.window) : 0, lead = min(c.sinks, begin);
   const int seen = lead + length - begin;
-  // stretches of whole tiles
-  const int tiles = (seen + kKeys - 1) / kKeys;
-  const int tile0 = (int)((int64_t)tiles * split / a.splits), tile1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+  // stretches of whole tiles, as many for each wavefront
+  const int tiles = (seen + kKeys - 1) / kKeys, rounds = (tiles + kWaves - 1) / kWaves;
+  const int tile0 = kWaves * (int)((int64_t)rounds * split / a.splits), tile1 = min(tiles, kWaves * (int)((int64_t)rounds * (split + 1) / a.splits));
   const int32_t* table = c.table + (int64_t)b * c.columns;
   const char* k_pool = (const char*)a.k_pool + 2 * kv * c.k_head;
   const char* v_pool = (const char*)a.v_pool + 2 * kv * c.v_head;
