@@ -162,11 +162,12 @@ CacheArgs plan(const arrow_cache_t* c) {
   const int64_t rows = std::max<int64_t>(1, (int64_t)c->batch * c->kv_heads * ceil_div(p.group, kHeadTile));
   // Stretches of the visible keys.  A workgroup takes some 14 ns per key where it has the chip to itself, the join 35 ns per stretch, so that the square root
   // of 0.4 `seen` of them take the least time together, and one where another launch is not worth it.  Where there are many rows, so many that the
-  // chip is full: two workgroups to a compute unit where rows see equally many keys, as under a window, and four, to even lengths out, otherwise (us):
+  // chip is full: two workgroups to a compute unit where rows see equally many keys, as under a window, and otherwise, to even lengths out, four, and
+  // stretches of up to 2048 keys (us):
   //   2 rows of 8000 keys: 16 stretches 15.0, 48 11.6, 64 11.4, 128 12.7, 256 18.1;  of 125 keys: 1 6.8, 2 8.4
   //   32 rows of 4000 .. 16,000: 16 38.4, 32 36.8, 64 39.4, 128 46.3;  128 of 500 .. 2000: 1 33.6, 4 22.6, 8 22.4, 16 23.5, 32 29.5
-  //   256 rows, window of 4096: 1 69.4, 2 54.0, 4 63.9, 16 63.2;  128 rows 1 74.2, 2 52.0, 4 55.0, 8 58.8
-  const int64_t full = (p.c.window ? 512 : 1024) / rows, best = (int64_t)std::sqrt(0.4 * (double)seen);
+  //   256 rows, window of 4096: 1 69.4, 2 54.0, 4 63.9, 16 63.2;  128 rows 1 74.2, 2 52.0, 4 55.0, 8 58.8;  256 of 4000 .. 16,000: 4 295, 8 282, 16 280
+  const int64_t full = p.c.window ? 512 / rows : std::max(1024 / rows, ceil_div(seen, 2048)), best = (int64_t)std::sqrt(0.4 * (double)seen);
   // A round of a workgroup's wavefronts is 64 keys: no more stretches than the longest ones' number of rounds needs.
   const int64_t rounds = std::max<int64_t>(1, ceil_div(seen, 64)), most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, full, best, rounds}));
   p.splits = seen <= 192 ? 1 : (int32_t)ceil_div(rounds, ceil_div(rounds, most));
