@@ -26,9 +26,17 @@ namespace {
 //                  512 blocks 27.2 / 16.8 / 16.7, 46.2 / 30.2 / 34.6;  768 blocks 40.3 / 23.2 / 22.5, 70.5 / 44.3 / 41.2
 //   heads of 128:  64 blocks 9.6 / 11.4 / 14.6, 21.2 / 31.1 / 40.1;  128 blocks 17.4 / 11.8 / 15.3, 28.9 / 33.1 / 41.2;  256 blocks 32.6 / 16.2 / 16.4,
 //                  52.6 / 36.1 / 42.3;  384 blocks 49.3 / 25.4 / 23.2, 76.6 / 42.1 / 46.0;  512 blocks 62.9 / 31.0 / 24.8, 100 / 53.0 / 49.9
-int query_groups(int64_t blocks, const AttentionArgs& a) {
+// A tile of keys has nothing to be shared out: 64 keys, 1024 blocks of 64 queries, 19.3 / 9.0 / 8.7, 42.8 / 16.8 / 14.5.  Up to 64 queries never fill four
+// groups, and of up to 32 there are as many workgroups of one group as of four (heads of 64 and of 128, of 20 queries):
+//   300 keys, 256 blocks 7.7 / 7.9 / 8.8, 9.2 / 10.0 / 10.9, 2048 blocks 32.5 / 24.8 / 27.6, 70.4 / 55.9 / 56.4
+//   2000 keys, 256 blocks 17.9 / 25.1 / 33.5, 23.0 / 33.6 / 42.4
+int query_groups(int64_t blocks, int64_t heads, const AttentionArgs& a) {
+  if (a.k_len <= 64) return 4;
   const int64_t seen = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks, a.k_len) : a.k_len;
-  if (blocks <= (a.dim <= 64 ? 128 : 64) * (seen >= 2000 ? 2 : 1)) return 1;
+  const bool twice = seen >= 2000 && (a.dim <= 64 || a.q_len > 64);
+  const int64_t ones = a.q_len <= 64 ? ((int64_t)a.q_len + 31) / 32 * heads : 4 * blocks;
+  if (ones <= (a.dim <= 64 ? 512 : 256) * (twice ? 2 : 1)) return 1;
+  if (a.q_len <= 64) return 2;
   return blocks <= (a.dim <= 64 ? 512 : a.window == 0 && seen >= 1000 ? 384 : 256) ? 2 : 4;
 }
 
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
 template <typename T, int C>
 int forward(const AttentionArgs& a, void* stream) {
   const int64_t heads = (int64_t)a.q_heads * a.batch, tiles = ((int64_t)a.q_len + kQueryTile - 1) / kQueryTile;
-  const int groups = query_groups(tiles * heads, a);
+  const int groups = query_groups(tiles * heads, heads, a);
   const int64_t rows = ((int64_t)a.q_len + 32 * groups - 1) / (32 * groups), blocks = rows * heads;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(256);

@@ -575,11 +575,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 //                  256 blocks 53.4 / 46.0 / 46.8, 85.6 / 77.7 / 83.2;  384 blocks 63.5 / 53.4 / 52.5, 109 / 92.5 / 98.2;  512 blocks 73.5 / 61.5 / 57.5, 124 / 104 / 102
 //   heads of 128:  64 blocks 37.4 / 38.4 / 44.6, 71.3 / 77.4 / 103;  128 blocks 61.1 / 51.3 / 57.4, 91.7 / 89.2 / 113;  256 blocks 92.6 / 63.7 / 64.0,
 //                  154 / 119 / 137;  384 blocks 118 / 76.8 / 76.6, 211 / 150 / 160;  512 blocks 160 / 105 / 98, 254 / 177 / 175
-// Up to 64 keys two, which are all queries of such a sequence as a rule, for what the kernel says of rows of few keys.
+// Up to 64 keys two, which are all queries of such a sequence as a rule, for what the kernel says of rows of few keys.  Up to 64 queries never fill four (300
+// keys, 2048 blocks of 20 queries, 75.0 / 71.1 / 76.2, 156 / 120 / 134).
 int query_groups(int64_t blocks, const AttentionArgs& a) {
   if (a.k_len <= 64) return 2;
   if (blocks <= 64) return 1;
-  return blocks <= (a.window == 0 && a.k_len >= 1000 ? 384 : 256) ? 2 : 4;
+  return a.q_len <= 64 || blocks <= (a.window == 0 && a.k_len >= 1000 ? 384 : 256) ? 2 : 4;
 }
 
 template <typename T, int C>
