@@ -67,6 +67,15 @@ typedef struct arrow_attention_t {
 int arrow_attention_forward(const arrow_attention_t *a, const void *q, const void *k, const void *v, void *o, float *lse, void *stream);
 
 /*
+ * The same with a workspace, in which few queries of many keys have the keys cut over several workgroups.
+ * ws: DEVICE, 256-byte aligned, at least arrow_attention_forward_split_bytes(a), which is 0 where nothing is cut; written, holds nothing
+ * between calls.  Errors: EINVAL, ETOOSMALL, EHIP.
+ */
+size_t arrow_attention_forward_split_bytes(const arrow_attention_t *a);
+int arrow_attention_forward_split(const arrow_attention_t *a, const void *q, const void *k, const void *v, void *o, float *lse, void *ws,
+                                  size_t ws_bytes, void *stream);
+
+/*
  * Gradients of the forward call with the same arguments, for the gradient d_o of its o (lse takes none):
  *     P(i,j) = exp(s(i,j) - lse_i),  dS(i,j) = P(i,j) (<do_i, v_j> - <do_i, o_i>),
  *     dq_i = scale sum_j dS(i,j) k_j,  dk_j = scale sum_i dS(i,j) q_i,  dv_j = sum_i P(i,j) do_i,

@@ -50,7 +50,7 @@ class ArrowAttention:
         mask = (self.device.index, min(self.window, 2**31 - 1), min(self.sinks, 2**31 - 1), -1.0 if scale is None else max(0.0, float(scale)))
         address = lambda name: binding._address(getattr(lib(), name))   # noqa: E731
         if self._call is not None:
-            self._forward = (address("arrow_attention_forward"), *mask)
+            self._forward = (address("arrow_attention_forward_split"), address("arrow_attention_forward_split_bytes"), *mask)
             self._backward = (address("arrow_attention_backward"), address("arrow_attention_workspace_bytes"), *mask)
             self._decode = (address("arrow_attention_decode"), address("arrow_attention_decode_workspace_bytes"), *mask)
 
@@ -138,7 +138,9 @@ class ArrowAttention:
         self._check(q, o=o)
         self._steps(a, "o", o)
         with self._on_device():
-            binding._check(lib().arrow_attention_forward(ctypes.byref(a), _address(q), _address(k), _address(v), _address(o), _address(lse), self._stream()))
+            ws = torch.empty(lib().arrow_attention_forward_split_bytes(ctypes.byref(a)), dtype=torch.uint8, device=q.device)
+            binding._check(lib().arrow_attention_forward_split(ctypes.byref(a), _address(q), _address(k), _address(v), _address(o), _address(lse), _address(ws),
+                                                               ws.numel(), self._stream()))
         return o, lse
 
     def backward(self, d_o, q, k, v, o, lse, dq=None, dk=None, dv=None, q_offsets=None, k_offsets=None, q_len=None, k_len=None):

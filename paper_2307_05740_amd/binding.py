@@ -32,7 +32,7 @@ EXPORTED = [
     "arrow_destroy",
     "csf3_build", "csf3_device_bytes", "csf3_upload", "csf3_workspace_bytes", "csf3_set_workspace",
     "csf3_mttkrp", "csf3_info", "csf3_form", "csf3_set_profiling", "csf3_get_profile", "csf3_last_error", "csf3_destroy",
-    "arrow_attention_forward", "arrow_attention_workspace_bytes", "arrow_attention_backward", "arrow_cache_append",
+    "arrow_attention_forward", "arrow_attention_forward_split_bytes", "arrow_attention_forward_split", "arrow_attention_workspace_bytes", "arrow_attention_backward", "arrow_cache_append",
     "arrow_attention_decode_workspace_bytes", "arrow_attention_decode",
     "arrow_embedding_forward", "arrow_embedding_workspace_bytes", "arrow_embedding_backward",
 ]
@@ -219,6 +219,10 @@ def lib():
                                        ctypes.POINTER(arrow_embedding_t), arrow_strides_t)
     L.arrow_attention_forward.restype = ctypes.c_int
     L.arrow_attention_forward.argtypes = [attention, vp, vp, vp, vp, vp, vp]
+    L.arrow_attention_forward_split_bytes.restype = sz
+    L.arrow_attention_forward_split_bytes.argtypes = [attention]
+    L.arrow_attention_forward_split.restype = ctypes.c_int
+    L.arrow_attention_forward_split.argtypes = [attention, vp, vp, vp, vp, vp, vp, sz, vp]
     L.arrow_attention_workspace_bytes.restype = sz
     L.arrow_attention_workspace_bytes.argtypes = [attention]
     L.arrow_attention_backward.restype = ctypes.c_int

@@ -174,11 +174,13 @@ CacheArgs plan(const arrow_cache_t* c) {
   return p;
 }
 
-}  // namespace
+// Parts of rows in the workspace: their sums, maxima and totals.
+size_t forward_bytes(const AttentionArgs& p) {
+  const int64_t splits = attention_forward_splits(p);
+  return splits > 1 ? align_up((size_t)p.batch * p.q_heads * p.q_len * splits * (p.dim + 2) * 4) : 0;
+}
 
-extern "C" {
-
-int arrow_attention_forward(const arrow_attention_t* a, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
+int forward(const arrow_attention_t* a, const void* q, const void* k, const void* v, void* o, float* lse, bool cut, void* ws, size_t ws_bytes, void* stream) {
   if (int rc = check(a)) return rc;
   const bool ragged = a->q_offsets != nullptr;
   const int64_t nq = tokens_of(a, false), nk = tokens_of(a, true);
@@ -192,7 +194,33 @@ int arrow_attention_forward(const arrow_attention_t* a, const void* q, const voi
   AttentionArgs p = plan(a);
   p.q = operand(q, a->q); p.k = operand(k, a->k); p.v = operand(v, a->v); p.o = operand(o, a->o);
   p.lse = lse;
+  p.splits = 1;
+  if (cut) {
+    const size_t need = forward_bytes(p);
+    if (need && (!ws || (uintptr_t)ws % 256)) return refuse(ARROW_EINVAL, "workspace is NULL or not 256-byte aligned");
+    if (ws_bytes < need) return refuse(ARROW_ETOOSMALL, "workspace of %zu bytes, %zu are needed", ws_bytes, need);
+    p.splits = attention_forward_splits(p);
+    p.parts = (float*)ws;
+  }
   return launched("attention forward", launch_attention_forward(p, a->dtype, stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int arrow_attention_forward(const arrow_attention_t* a, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
+  return forward(a, q, k, v, o, lse, false, nullptr, 0, stream);
+}
+
+size_t arrow_attention_forward_split_bytes(const arrow_attention_t* a) {
+  if (check(a) || tokens_of(a, false) == 0) return 0;
+  return forward_bytes(plan(a));
+}
+
+int arrow_attention_forward_split(const arrow_attention_t* a, const void* q, const void* k, const void* v, void* o, float* lse, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  return forward(a, q, k, v, o, lse, true, ws, ws_bytes, stream);
 }
 
 size_t arrow_attention_workspace_bytes(const arrow_attention_t* a) {

@@ -42,7 +42,7 @@ int query_groups(int64_t blocks, int64_t heads, const AttentionArgs& a) {
 
 // One row of the result in plain steps, the wavefront's lanes over its columns, by the row's own visible keys alone.  Matrix
 // instructions multiply what a query does not see by a probability of 0, and that is no zero where a value there is infinite or NaN:
-// the rows that this may have touched come here.
+// the rows that this may have touched come here, those without any weight (lse = -infinity), whose result is 0, among them.
 template <typename T>
 __device__ __noinline__ void plain_row(const T* q, const char* k, const char* v, T* o, int64_t k_token, int64_t v_token, int dim, int p, int window,
                                        int sinks, float scale, float lse) {
@@ -50,7 +50,7 @@ __device__ __noinline__ void plain_row(const T* q, const char* k, const char* v,
   const bool mine = d < dim;
   const float q0 = mine ? (float)q[d] : 0.f, q1 = mine ? (float)q[d + 1] : 0.f;
   float a0 = 0.f, a1 = 0.f;
-  for (int j = 0; j <= p; ++j) {
+  for (int j = 0; j <= p && lse > minus_infinity(); ++j) {
     if (window && j >= sinks && j <= p - window) { j = p - window; continue; }
     const T* kj = (const T*)(k + 2 * (int64_t)j * k_token);
     const T* vj = (const T*)(v + 2 * (int64_t)j * v_token);
@@ -79,7 +79,9 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   // Workgroups next to each other go to different dies: an item of every sequence and key head in turn, so that a die has the same keys again
   // and again (8192 queries, 32/8 heads of 128: 300 -> 270 us); of one, the longest rows of a triangle first.
-  const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;
+  const int units = a.kv_heads * a.batch, unit = blockIdx.x % units;
+  int item = blockIdx.x / units, split = 0;
+  if constexpr (kGroups == 1) { split = item % a.splits; item /= a.splits; }
   const int g = item % a.group, tile = tiles - 1 - item / a.group;
   const int kv = unit % a.kv_heads, b = unit / a.kv_heads, head = kv * a.group + g;
   const bool ragged = a.q_offsets != nullptr;
@@ -107,6 +109,12 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
 
   const int last = min(first + kRows, sq.count) - 1 + shift;
   const SeenTiles seen = seen_tiles<kStep>(max(first + shift, 0), last, a.window, a.sinks);
+  int begin = 0, end = seen.total;                            // tiles of this workgroup: whole rounds of its wavefronts
+  if constexpr (kGroups == 1) {
+    const int rounds = (seen.total + 3) / 4;
+    begin = 4 * (int)((int64_t)rounds * split / a.splits);
+    end = min(seen.total, 4 * (int)((int64_t)rounds * (split + 1) / a.splits));
+  }
   // of this wavefront's queries
   const int low = mine + shift, high = min(low + 31, sk.count - 1);
 
@@ -125,12 +133,12 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
     lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + 2 * to * kBytes, sharer);
     lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, sharer);
   };
-  const int t0 = kShare ? 0 : wave;
-  if (t0 < seen.total) load(t0, 0);
-  for (int t = t0, now = 0; t < seen.total; t += kTurns, now ^= 1) {
+  const int t0 = begin + (kShare ? 0 : wave);
+  if (t0 < end) load(t0, 0);
+  for (int t = t0, now = 0; t < end; t += kTurns, now ^= 1) {
     if constexpr (kShare) wait_for_tiles();
     else wait_for_own_tiles();
-    if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
+    if (t + kTurns < end) load(t + kTurns, now ^ 1);
     const int skip = kMine < kStep ? part * kMine : 0;        // (keys of the tile that are another wavefront's)
     const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
     const int k0 = seen.at(t) * kStep + skip;
@@ -200,11 +208,11 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
   total = add_halves(total);
   T* o = (T*)rows_of(a.o, ragged, b, sq.first, head);
   const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
-  // 1 / total, 0 for a row that sees nothing; the lanes that hold a result that is not finite though the row's sum is
+  // 1 / total, 0 for a row that sees nothing; the lanes that hold a result that is not finite though the row's sum is not infinite or NaN
   auto over = [](float total) { return total > 0.f || total != total ? 1.f / total : 0.f; };
   auto lse_of = [](float top, float total) { return total == 0.f ? minus_infinity() : (top + __log2f(total)) * kLn2; };
   auto odd_rows = [&](float test, float lse) {
-    const uint64_t odd = __ballot(there && lse - lse == 0.f && test != test);
+    const uint64_t odd = __ballot(there && lse < -minus_infinity() && test != test);
     return (odd | odd >> 32) & 0xffffffffu;
   };
   auto plain_rows = [&](uint64_t odd, float lse) {
@@ -248,8 +256,9 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
       share[w] = __builtin_amdgcn_exp2f(tops[(group + kGroups * w) * 64 + lane] - off);
       total = fmaf(share[w], totals[(group + kGroups * w) * 64 + lane], total);
     }
-    const float by = over(total), lse = lse_of(all, total);
-    if (a.lse && there && half == 0 && part == 0) a.lse[stat] = lse;
+    const bool whole = kGroups > 1 || a.splits == 1;
+    const float by = whole ? over(total) : 1.f, lse = lse_of(all, total);
+    if (whole && a.lse && there && half == 0 && part == 0) a.lse[stat] = lse;
     // a wavefront joins every kParts-th block of 32 columns
     constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
     f32x16 r[kJoined];
@@ -266,6 +275,22 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
 #pragma unroll
       for (int i = 0; i < 16; ++i) { r[n][i] *= by; test = fmaf(r[n][i], 0.f, test); }
     }
+    if (!whole) {
+      const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_len, place = (((int64_t)b * a.q_heads + head) * a.q_len + row) * a.splits + split;
+      if (there && half == 0 && part == 0) {
+        float* to = a.parts + rows * a.splits * a.dim + 2 * place;
+        to[0] = all;
+        to[1] = total;
+      }
+#pragma unroll
+      for (int n = 0; n < kJoined; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int m = part + n * kParts, d = 32 * m + 2 * i + 4 * half;
+          if (m < kBlocks && there && d < a.dim) *(f32x4*)(a.parts + place * a.dim + d) = f32x4{r[n][i], r[n][i + 1], r[n][i + 2], r[n][i + 3]};
+        }
+      return;
+    }
     uint64_t odd = odd_rows(test, lse);
     if (lane == 0) odds[wave] = odd;
     __syncthreads();
@@ -280,16 +305,60 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
   }
 }
 
+// The parts of one row joined, by a wavefront, two columns per lane.
+template <typename T>
+__global__ __launch_bounds__(64) void attention_forward_join_kernel(AttentionArgs a) {
+  const int64_t id = blockIdx.x, unit = id / a.q_len, rows = (int64_t)a.batch * a.q_heads * a.q_len;
+  const int row = (int)(id % a.q_len), head = (int)(unit % a.q_heads), b = (int)(unit / a.q_heads), lane = threadIdx.x, d = 2 * lane;
+  const bool ragged = a.q_offsets != nullptr;
+  const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
+  if (row >= sq.count) return;
+  const bool mine = d < a.dim;
+  const float *from = a.parts + id * a.splits * a.dim + d, *stats = a.parts + rows * a.splits * a.dim + 2 * id * a.splits;
+  const float top = lane < a.splits ? stats[2 * lane] : minus_infinity();
+  float all = top;
+  for (int m = 32; m; m >>= 1) all = fmaxf(all, __shfl_xor(all, m, 64));
+  const float share = __builtin_amdgcn_exp2f(top - (all == minus_infinity() ? 0.f : all));
+  float total = lane < a.splits ? share * stats[2 * lane + 1] : 0.f;
+  for (int m = 32; m; m >>= 1) total += __shfl_xor(total, m, 64);
+  float x0 = 0.f, x1 = 0.f;
+  for (int i = 0; i < a.splits; i += 8) {                     // (shares from a.splits on are 0)
+    float2 x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = mine ? *(const float2*)(from + (int64_t)min(i + j, a.splits - 1) * a.dim) : float2{0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float by = __shfl(share, i + j, 64);
+      x0 = fmaf(by, x[j].x, x0);
+      x1 = fmaf(by, x[j].y, x1);
+    }
+  }
+  const float by = total > 0.f || total != total ? 1.f / total : 0.f, lse = total == 0.f ? minus_infinity() : (all + __log2f(total)) * kLn2;
+  x0 *= by;
+  x1 *= by;
+  T* o = (T*)rows_of(a.o, ragged, b, sq.first, head) + (int64_t)row * a.o.token;
+  if (a.lse && lane == 0) a.lse[ragged ? head * a.q_tokens + sq.first + row : id] = lse;
+  if (lse < -minus_infinity() && __any(x0 - x0 != 0.f || x1 - x1 != 0.f)) {
+    const int kv = head / a.group;
+    plain_row<T>((const T*)rows_of(a.q, ragged, b, sq.first, head) + (int64_t)row * a.q.token, rows_of(a.k, ragged, b, sk.first, kv), rows_of(a.v, ragged, b, sk.first, kv), o,
+                 a.k.token, a.v.token, a.dim, row + sk.count - sq.count, a.window, a.sinks, a.scale, lse);
+  } else if (mine) {
+    o[d] = (T)x0;
+    o[d + 1] = (T)x1;
+  }
+}
+
 template <typename T, int C>
 int forward(const AttentionArgs& a, void* stream) {
   const int64_t heads = (int64_t)a.q_heads * a.batch, tiles = ((int64_t)a.q_len + kQueryTile - 1) / kQueryTile;
   const int groups = query_groups(tiles * heads, heads, a);
-  const int64_t rows = ((int64_t)a.q_len + 32 * groups - 1) / (32 * groups), blocks = rows * heads;
+  const int64_t rows = ((int64_t)a.q_len + 32 * groups - 1) / (32 * groups), blocks = rows * heads * (groups == 1 ? a.splits : 1);
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(256);
   if (groups == 4) attention_forward_kernel<T, C, 4><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
   else if (groups == 2) attention_forward_kernel<T, C, 2><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
   else attention_forward_kernel<T, C, 1><<<grid, block, 0, (hipStream_t)stream>>>(a, (int)rows);
+  if (groups == 1 && a.splits > 1) attention_forward_join_kernel<T><<<dim3((unsigned)(heads * a.q_len)), dim3(64), 0, (hipStream_t)stream>>>(a);
   return (int)hipGetLastError();
 }
 
@@ -299,6 +368,21 @@ int by_columns(const AttentionArgs& a, void* stream) {
 }
 
 }  // namespace
+
+// Keys are cut where workgroups of 32 queries leave the chip empty: as many parts as fill it, of at least four rounds of their wavefronts each (128 keys
+// a round, some 0.8 us).  The join takes 4 us and more with more rows, so that there have to be some keys (us, whole -> cut, heads of 64 and of 128):
+//   16 queries, 4 heads: 1000 keys 10.8 -> 10.9, 13.2 -> 12.7, 1500 13.8 -> 11.1, 17.9 -> 12.9, 5000 33.9 -> 11.6, 41.4 -> 13.4
+//   256 queries, 16 heads: 1500 keys 14.4 -> 15.9, 18.1 -> 19.0, 2000 17.2 -> 16.3, 21.7 -> 21.3, 5000 34.9 -> 22.7, 43.4 -> 31.9
+//   1000 queries, 8 heads of 64: 2000 keys 18.0 -> 20.3, 3000 24.5 -> 24.1, 8000 52.1 -> 42.1
+int attention_forward_splits(const AttentionArgs& a) {
+  const int64_t heads = (int64_t)a.q_heads * a.batch, tiles = ((int64_t)a.q_len + kQueryTile - 1) / kQueryTile;
+  if (heads == 0 || a.q_len == 0 || query_groups(tiles * heads, heads, a) != 1) return 1;
+  const int64_t seen = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks, a.k_len) : a.k_len;
+  const int64_t rows = a.q_len * heads;
+  if (seen < (rows <= 2048 ? 1500 : rows <= 4096 ? 2000 : 3000)) return 1;
+  const int64_t ones = ((int64_t)a.q_len + 31) / 32 * heads, fill = (a.dim <= 64 ? 512 : 256) / ones;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({kMostRowSplits, fill, (seen + 127) / 128 / 4}));
+}
 
 int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream) {
   if (dtype == ARROW_BF16) return by_columns<__bf16>(a, stream);

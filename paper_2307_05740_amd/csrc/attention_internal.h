@@ -21,7 +21,9 @@ struct AttentionArgs {
   const float* lse_in;             // backward
   float* lse;                      // forward, may be null
   float *off, *delta;              // backward, laid out as lse: -lse_i / scale and -sum_j P(i,j) <do_i, v_j>
-  float* parts;                    // backward: sums of the parts of a key tile, dk then dv of each
+  float* parts;                    // backward: sums of the parts of a key tile, dk then dv of each; forward: of the parts of a row, and after them its
+                                   // maximum and total, batch x q_heads x q_len x splits of each
+  int32_t splits;                  // forward: parts that a row's keys are cut into
   const int32_t *q_offsets, *k_offsets;
   int64_t q_tokens, k_tokens;
   int32_t batch, q_heads, kv_heads, group, dim, q_len, k_len, window, sinks;
@@ -40,6 +42,9 @@ struct CacheArgs {
   float* parts;                    // splits x batch x q_heads x (dim + 2)
 };
 
+// Into how many parts the forward call cuts a row's keys where it has a workspace, 1 to kMostRowSplits.
+int attention_forward_splits(const AttentionArgs& a);
+
 // Launchers: 0 or a hipError_t.
 int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream);
 int launch_attention_backward(const AttentionArgs& a, int32_t dtype, void* stream);
@@ -50,6 +55,7 @@ constexpr int kQueryTile = 128;    // queries of a workgroup, forward and dq
 constexpr int kKeyTile = 128;      // keys of a workgroup, dk and dv
 constexpr int kQueryStep = 64;     // queries that it goes through at a time
 constexpr int kMostSplits = 256;   // stretches of a cache
+constexpr int kMostRowSplits = 32; // parts of a row's keys, forward
 constexpr int kHeadTile = 16;      // query heads of a workgroup, single tokens
 
 }  // namespace arrow

@@ -223,25 +223,27 @@ int quietly(F&& call) {
   return rc;
 }
 
-// attention_forward(function, device, window, sinks, scale or -1, q, k, v, o, lse, q_offsets, k_offsets, q_len, k_len)
+// attention_forward(function, of the workspace's size, device, window, sinks, scale or -1, q, k, v, o, lse, q_offsets, k_offsets, q_len, k_len)
 PyObject* attention_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
-  int64_t x[4], len[2];
-  if (!arguments(n_args, 14) || !integers(args, 4, x)) return nullptr;
-  const double scale = PyFloat_AsDouble(args[4]);
+  int64_t x[5], len[2];
+  if (!arguments(n_args, 15) || !integers(args, 5, x)) return nullptr;
+  const double scale = PyFloat_AsDouble(args[5]);
   if (PyErr_Occurred()) return nullptr;
-  if (!lengths(args + 12, 2, len)) return none();
-  return results(x[1], [&](at::Tensor* out, int& rc) {
-    Tensors tensor{x[1]};
-    const at::Tensor *q = tensor(args[5]), *k = tensor(args[6]), *v = tensor(args[7]), *o = tensor(args[8]), *lse = tensor(args[9]);
-    const at::Tensor *q_offsets = tensor(args[10]), *k_offsets = tensor(args[11]);
+  if (!lengths(args + 13, 2, len)) return none();
+  return results(x[2], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[2]};
+    const at::Tensor *q = tensor(args[6]), *k = tensor(args[7]), *v = tensor(args[8]), *o = tensor(args[9]), *lse = tensor(args[10]);
+    const at::Tensor *q_offsets = tensor(args[11]), *k_offsets = tensor(args[12]);
     arrow_attention_t a{};
-    if (!tensor.ok || !describe(a, x[2], x[3], scale, q, k, v, q_offsets, k_offsets, len[0], len[1])) return 0;
+    if (!tensor.ok || !describe(a, x[3], x[4], scale, q, k, v, q_offsets, k_offsets, len[0], len[1])) return 0;
     if ((o && !like(*o, *q)) || (lse && !is_lse(*lse, a))) return 0;
     out[0] = o ? *o : made(q->sizes(), *q, q->scalar_type());
     out[1] = lse ? *lse : a.q_offsets ? made({a.q_heads, a.q_tokens}, *q, at::kFloat) : made({a.batch, a.q_heads, a.q_len}, *q, at::kFloat);
     a.o = steps(out[0]);
-    void *qp = data(*q), *kp = data(*k), *vp = data(*v), *op = data(out[0]), *lp = data(out[1]), *stream = stream_of(x[1]);
-    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_attention_forward)>(x[0])(&a, qp, kp, vp, op, (float*)lp, stream); });
+    const size_t bytes = reinterpret_cast<decltype(&arrow_attention_forward_split_bytes)>(x[1])(&a);
+    const at::Tensor ws = bytes ? made({(int64_t)bytes}, *q, at::kByte) : at::Tensor();
+    void *qp = data(*q), *kp = data(*k), *vp = data(*v), *op = data(out[0]), *lp = data(out[1]), *wp = bytes ? data(ws) : nullptr, *stream = stream_of(x[2]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_attention_forward_split)>(x[0])(&a, qp, kp, vp, op, (float*)lp, wp, bytes, stream); });
     return 2;
   });
 }

@@ -554,3 +554,59 @@ def test_keys_that_their_scores_rule_out(torch, Attention, dim):
         within(torch, "o", o[0, :, 0], want["o"], bound["o"])
         o = Attention().decode(q[:, -1], kp, vp, table, lens, n)
         within(torch, "o of the last token", o[0], want["o"][-1:], bound["o"][-1:])
+
+
+@pytest.mark.parametrize("heads", [1, 60, 240])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_without_keys_next_to_values_that_are_not_finite(torch, Attention, heads, dim):
+    """More queries than keys: the first ones see nothing, their results and gradients are 0 whatever keys and values hold."""
+    q, d_o = (normal(torch, s, "bfloat16", 1, 200, heads, dim) for s in (1, 4))
+    k, v = (normal(torch, s, "bfloat16", 1, 130, 1, dim) for s in (2, 3))
+    k[0, 3], v[0, 3] = math.nan, math.inf
+    got = run(torch, Attention(), q, k, v, d_o)
+    for name in ("o", "dq"):
+        assert bool((got[name][0, :70] == 0).all()), name
+    assert bool((got["lse"][0, :, :70] == -math.inf).all()) and bool(torch.isfinite(got["o"][0, 70:73]).all())
+
+
+# queries, keys, heads, key heads, dim, window, sinks: few queries of many keys
+CUT = [(1, 5000, 4, 2, 128, 0, 0), (16, 9000, 4, 1, 128, 0, 0), (33, 3000, 2, 2, 64, 0, 0), (64, 2500, 3, 3, 80, 2200, 7), (20, 700, 2, 1, 64, 600, 3),
+       (5, 20000, 1, 1, 96, 0, 0), (40, 2100, 1, 1, 128, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("queries,keys,heads,kv,dim,window,sinks", CUT)
+def test_few_queries_of_many_keys(torch, Attention, dtype, queries, keys, heads, kv, dim, window, sinks):
+    """Keys that are cut over several workgroups, also where some sequences of a batch have few or none."""
+    q = normal(torch, 1, dtype, queries, heads, dim, by=2.0)
+    k, v = (normal(torch, s, dtype, keys, kv, dim) for s in (2, 3))
+    op = Attention(window, sinks)
+    got = run(torch, op, q[None], k[None], v[None])
+    check_sequence(torch, {n: t[0] for n, t in got.items()}, q, k, v, window, sinks)
+    again = run(torch, op, q[None], k[None], v[None])
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    lengths = [(queries, keys - 300), (0, 40), (1, 1), (2, 0), (queries, 130)]
+    q_offsets, k_offsets = (torch.tensor([0] + [sum(x[i] for x in lengths[:n + 1]) for n in range(len(lengths))], dtype=torch.int32, device="cuda") for i in (0, 1))
+    nq, nk = (sum(x[i] for x in lengths) for i in (0, 1))
+    q = normal(torch, 1, dtype, nq + 3, heads, dim)
+    k, v = (normal(torch, s, dtype, nk + 3, kv, dim) for s in (2, 3))
+    got = run(torch, op, q, k, v, q_offsets=q_offsets, k_offsets=k_offsets, q_len=queries + 1, k_len=keys)
+    for b in range(len(lengths)):
+        i, j = slice(int(q_offsets[b]), int(q_offsets[b + 1])), slice(int(k_offsets[b]), int(k_offsets[b + 1]))
+        check_sequence(torch, {"o": got["o"][i], "lse": got["lse"][:, i]}, q[i], k[j], v[j], window, sinks)
+    assert bool(torch.isnan(got["o"][nq:]).all())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_few_queries_of_many_keys_of_which_some_are_not_seen(torch, Attention, bad):
+    q = normal(torch, 1, "bfloat16", 1, 40, 2, 128)
+    k, v = (normal(torch, s, "bfloat16", 1, 6000, 2, 128) for s in (2, 3))
+    op = Attention(4000, 4)
+    k[0, 100:1900], v[0, 100:1900] = bad, bad                    # behind all windows
+    k[0, 5990], v[0, 5990] = bad, bad                            # ahead of the first 30
+    got = op.forward(q, k, v)[0]
+    for h in range(2):
+        k2, v2 = torch.where(torch.isfinite(k), k, 0.0), torch.where(torch.isfinite(v), v, 0.0)
+        exact, bound = oracle.attention(q[0, :30, h], k2[0, :5990, h], v2[0, :5990, h], 4000, 4)
+        within(torch, "o", got[0, :30, h], exact["o"], bound["o"])
+    assert not bool(torch.isfinite(got[0, 30:]).any())

@@ -206,3 +206,18 @@ def test_workspaces_of_any_number_of_tokens(L):
         for rows in (1, 2, 32767, 32768, 2**31 - 2):
             e = embedding(tokens=tokens, rows=rows)
             assert L.arrow_embedding_workspace_bytes(ctypes.byref(e)) >= 4 * (rows + 4 * tokens)
+
+
+def test_forward_in_a_workspace(L):
+    """Refusals of the forward call that cuts keys, and what it needs."""
+    few = attention(q_len=16, k_len=9000)
+    need = L.arrow_attention_forward_split_bytes(ctypes.byref(few))
+    assert need > 0 and need % 256 == 0
+    at = (1 * SOME, 2 * SOME, 3 * SOME, 4 * SOME, 5 * SOME)
+    refused(L.arrow_attention_forward_split(ctypes.byref(few), *at, 0, need, 0), "workspace")
+    refused(L.arrow_attention_forward_split(ctypes.byref(few), *at, 6 * SOME + 16, need, 0), "workspace")
+    assert L.arrow_attention_forward_split(ctypes.byref(few), *at, 6 * SOME, need - 1, 0) == binding.ARROW_ETOOSMALL
+    refused(L.arrow_attention_forward_split(None, *at, 0, 0, 0), "NULL")
+    for whole in (attention(q_len=16, k_len=100), attention(q_len=0, k_len=9000), attention(q_len=4000, k_len=4000, window=100)):
+        assert L.arrow_attention_forward_split_bytes(ctypes.byref(whole)) == 0
+    assert L.arrow_attention_forward_split_bytes(None) == 0
