@@ -8,7 +8,7 @@
 // each, or the same 32 queries and every fourth tile, of 32 keys and its own, and join their results in LDS.
 //
 // What bounds it: with heads of 128, matrix instructions and the vector instructions between them (one exponential, one addition, one maximum, one
-// multiply-add and half a conversion per score), at the clock that the card's power leaves: 16,384 tokens, 16/2 heads, window of 4096, 477 us = 1010 TFLOP/s,
+// multiply-add and half a conversion per score), at the clock that the card's power leaves: 16,384 tokens, 16/2 heads, window of 4096, 490 us = 985 TFLOP/s,
 // where a large matrix product reaches 1312.  With heads of 64 the vector instructions: 4 x 2048, 16 heads, window of 512, 33 us = 460 TFLOP/s.  Tiles
 // of 64 keys, because two of keys and two of values (64 KiB) leave room for two workgroups on a compute unit, and each wavefront then has two
 // independent chains of products; 32 queries to a wavefront, because scores, sums and queries of 64 would not fit 256 registers.
