@@ -109,7 +109,7 @@ typedef struct arrow_cache_t {
 
 /*
  * Write `tokens` new keys and values per sequence to its last places, lengths[b] - tokens .. lengths[b] - 1 (places before
- * the first one are left out).  k, v: batch x tokens x kv_heads x dim by their strides.  Errors: EINVAL, EHIP.
+ * the first one, and those that the table has no room for, are left out).  k, v: batch x tokens x kv_heads x dim by their strides.  Errors: EINVAL, EHIP.
  */
 int arrow_cache_append(const arrow_cache_t *c, int32_t tokens, const void *k, const void *v, arrow_strides_t ks, arrow_strides_t vs,
                        void *k_pool, void *v_pool, void *stream);
@@ -117,6 +117,7 @@ int arrow_cache_append(const arrow_cache_t *c, int32_t tokens, const void *k, co
 /*
  * o of one query per sequence, at position lengths[b] - 1.  q, o: batch x q_heads x dim by their strides (token unused).
  * k, v: the new token's key and value (token unused), which the call writes to its place first, or both NULL where they are in the pools.
+ * Of a sequence longer than the table has room for, they are left out: nothing is written, and o is that of the keys that are there.
  * ws: DEVICE, 256-byte aligned, at least arrow_attention_decode_workspace_bytes(c) (which may be 0); written, holds nothing between calls.
  * Errors: EINVAL, ETOOSMALL, EHIP.
  */

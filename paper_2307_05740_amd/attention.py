@@ -215,7 +215,7 @@ class ArrowAttention:
 
     def decode(self, q, k_cache, v_cache, table, lengths, max_len=None, k=None, v=None, o=None):
         """o of one query per sequence, q: (batch, heads, dim), at the last of its lengths[b] positions (0: an idle sequence).  k and v,
-        (batch, key heads, dim): the new token's, written to their place first; without them they are there already.
+        (batch, key heads, dim): the new token's, written to their place first (of a sequence longer than its row of the table, left out); without them they are there already.
         max_len: the longest length; only how the work is split goes by it."""
         if self._call is not None:
             done = self._call.attention_decode(*self._decode, q, k_cache, v_cache, table, lengths, max_len, k, v, o)

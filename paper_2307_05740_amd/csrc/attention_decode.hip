@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
   const int head_tile = id % head_tiles, b = id / head_tiles;
   const int head0 = head_tile * kHeadTile, heads = min(a.group - head0, kHeadTile);
   const int64_t room = (int64_t)c.columns << a.page_log;
-  const int length = (int)max((int64_t)0, min((int64_t)c.lengths[b], room));
+  const int tokens = c.lengths[b], length = (int)max((int64_t)0, min((int64_t)tokens, room));
   const int begin = c.window ? max(0, length - c.window) : 0, lead = min(c.sinks, begin);
   const int seen = lead + length - begin;
   // stretches of whole tiles, as many for each wavefront
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
   const int32_t* table = c.table + (int64_t)b * c.columns;
   const char* k_pool = (const char*)a.k_pool + 2 * kv * c.k_head;
   const char* v_pool = (const char*)a.v_pool + 2 * kv * c.v_head;
-  const bool fresh = a.k.at != nullptr;
+  const bool fresh = a.k.at != nullptr && tokens <= room;        // (a new token beyond the table has no place: the last one is another's)
   const char* k_new = (const char*)a.k.at + 2 * (b * a.k.sequence + kv * a.k.head);
   const char* v_new = (const char*)a.v.at + 2 * (b * a.v.sequence + kv * a.v.head);
 

@@ -610,3 +610,23 @@ def test_few_queries_of_many_keys_of_which_some_are_not_seen(torch, Attention, b
         exact, bound = oracle.attention(q[0, :30, h], k2[0, :5990, h], v2[0, :5990, h], 4000, 4)
         within(torch, "o", got[0, :30, h], exact["o"], bound["o"])
     assert not bool(torch.isfinite(got[0, 30:]).any())
+
+
+@pytest.mark.parametrize("length,window", [(64, 0), (64, 20), (6000, 0)])
+def test_a_new_token_beyond_the_table_is_left_out(torch, Attention, length, window):
+    """The table is full: the last token's key and value stay, and are the ones that count."""
+    page = 16
+    (kp, vp), table, n, rows = paged(torch, "bfloat16", [length, length // 2], page, 2, 64, columns=length // page)
+    q, k, v = normal(torch, 3, "bfloat16", 2, 4, 64), *(normal(torch, s, "bfloat16", 2, 2, 64) for s in (4, 5))
+    half = length // 2                                           # (the other sequence has room)
+    rows[1][0][-1], rows[1][1][-1] = k[1], v[1]
+    want = [p.clone() for p in (kp, vp)]
+    for pool, x in zip(want, (k, v)):
+        pool[table[1, (half - 1) // page], (half - 1) % page] = x[1]
+    op = Attention(window, 2)
+    for more in (length + 1, 2_000_000_000):
+        n[0] = more
+        o = op.decode(q, kp, vp, table, n, length, k=k, v=v)
+        check_tokens(torch, o, q, rows, window, 2)
+        for pool, x in zip((kp, vp), want):
+            assert torch.equal(pool.view(torch.int16), x.view(torch.int16)), "the token was written over another one"
