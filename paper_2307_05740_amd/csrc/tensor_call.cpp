@@ -381,7 +381,7 @@ PyObject* embedding_backward(PyObject*, PyObject* const* args, Py_ssize_t n_args
   return results(x[2], [&](at::Tensor* out, int& rc) {
     Tensors tensor{x[2]};
     const at::Tensor *dY = tensor(args[5]), *ids = tensor(args[6]), *dW = tensor(args[7]);
-    if (!tensor.ok || !dY || !ids || dY->dim() < 2) return 0;
+    if (!tensor.ok || !dY || !ids || dY->dim() < 1) return 0;
     out[0] = dW ? *dW : made({x[3], dY->size(-1)}, *dY, dY->scalar_type());
     arrow_embedding_t e{};
     if ((out[0].scalar_type() != dY->scalar_type() && out[0].scalar_type() != at::kFloat) || !describe(e, x[3], scale, &out[0], ids, dY)) return 0;

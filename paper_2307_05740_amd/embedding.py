@@ -90,7 +90,7 @@ class ArrowEmbedding:
                 return _results(done)
         torch = self._torch
         ids = ids.contiguous()
-        if tuple(dY.shape[:-1]) != tuple(ids.shape) or dY.dim() < 2:
+        if dY.dim() < 1 or tuple(dY.shape[:-1]) != tuple(ids.shape):
             raise ValueError(f"dY {tuple(dY.shape)} of ids {tuple(ids.shape)}")
         flat = dY if dY.dim() == 2 else dY.reshape(math.prod(ids.shape), dY.shape[-1])
         if dW is None:

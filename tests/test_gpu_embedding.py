@@ -169,3 +169,19 @@ def test_few_tokens_of_a_large_table(torch, Embedding, columns):
     for rows in (262_144, 262_145, 300_001):
         dY, ids = normal(torch, 2, "bfloat16", 500, columns), tokens(torch, 3, 500, rows, "text")
         check_grad(torch, Embedding(rows).backward(dY, ids, torch.full((rows, columns), math.nan, dtype=torch.bfloat16, device="cuda")), dY, ids, rows, 1.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_id_without_dimensions(torch, Embedding, dtype):
+    W, dY = normal(torch, 1, dtype, 20, 40), normal(torch, 2, dtype, 40)
+    op, ids = Embedding(20, 2.0), torch.tensor(7, device="cuda")
+    W.requires_grad_()
+    Y = op(W, ids)
+    assert Y.shape == (40,) and torch.equal(Y, 2 * W[7])
+    Y.backward(dY)
+    want = torch.zeros_like(W)
+    want[7] = 2 * dY
+    assert torch.equal(W.grad, want)
+    assert torch.equal(op.backward(dY, ids, dtype=torch.float32), want.float())
+    with pytest.raises(ValueError, match="dY"):
+        op.backward(dY[0], ids)
