@@ -121,7 +121,7 @@ class ArrowAttention:
     def forward(self, q, k, v, o=None, lse=None, q_offsets=None, k_offsets=None, q_len=None, k_len=None):
         """``(o, lse)``.  q: (batch, tokens, heads, dim), k and v: (batch, keys, key heads, dim); or, with int32 offsets of
         batch + 1 values each, (tokens of all sequences, heads, dim), of which no sequence has more than q_len (k_len).
-        lse: float32, (batch, heads, tokens), or (heads, tokens of all sequences)."""
+        lse: float32, (batch, heads, tokens), or (heads, tokens of all sequences).  Results of tokens that no sequence has are not written."""
         if self._call is not None:
             done = self._call.attention_forward(*self._forward, q, k, v, o, lse, q_offsets, k_offsets, q_len, k_len)
             if done is not None:
@@ -144,7 +144,8 @@ class ArrowAttention:
         return o, lse
 
     def backward(self, d_o, q, k, v, o, lse, dq=None, dk=None, dv=None, q_offsets=None, k_offsets=None, q_len=None, k_len=None):
-        """``(dq, dk, dv)`` for the gradient d_o of the o that ``forward`` gave for these arguments together with lse."""
+        """``(dq, dk, dv)`` for the gradient d_o of the o that ``forward`` gave for these arguments together with lse.  Those of tokens that no
+        sequence has are not written."""
         if self._call is not None:
             done = self._call.attention_backward(*self._backward, d_o, q, k, v, o, lse, dq, dk, dv, q_offsets, k_offsets, q_len, k_len)
             if done is not None:
@@ -169,7 +170,7 @@ class ArrowAttention:
         return dq, dk, dv
 
     def __call__(self, q, k, v, q_offsets=None, k_offsets=None, q_len=None, k_len=None):
-        """o as ``forward`` gives it, with its gradient for torch's autograd."""
+        """o as ``forward`` gives it, with its gradient for torch's autograd.  Tokens that no sequence has get zeros in both."""
         return _attention_function().apply(self, q, k, v, q_offsets, k_offsets, q_len, k_len)
 
     # ---- a cache in pages ---------------------------------------------------------------------------------------------
@@ -253,10 +254,14 @@ def _attention_function():
     if _function is None:
         import torch
 
+        def blank(t, q_offsets):
+            """Zeros for the tokens that no sequence of a ragged batch has: what is there goes into products with other gradients."""
+            return torch.zeros(t.shape, dtype=t.dtype, device=t.device) if q_offsets is not None else None
+
         class Attention(torch.autograd.Function):
             @staticmethod
             def forward(ctx, op, q, k, v, *lengths):
-                o, lse = op.forward(q, k, v, None, None, *lengths)
+                o, lse = op.forward(q, k, v, blank(q, lengths[0]), None, *lengths)
                 ctx.save_for_backward(q, k, v, o, lse, *lengths[:2])
                 ctx.op, ctx.limits = op, lengths[2:]
                 return o
@@ -267,7 +272,8 @@ def _attention_function():
                 q, k, v, o, lse, *offsets = ctx.saved_tensors
                 if d_o.stride(-1) != 1 or d_o.data_ptr() % 16 or any(s % 8 for s in d_o.stride()[:-1]):
                     d_o = d_o.clone(memory_format=torch.contiguous_format)
-                return None, *ctx.op.backward(d_o, q, k, v, o, lse, None, None, None, *offsets, *ctx.limits), None, None, None, None
+                grads = (blank(t, offsets[0]) for t in (q, k, v))
+                return None, *ctx.op.backward(d_o, q, k, v, o, lse, *grads, *offsets, *ctx.limits), None, None, None, None
 
         _function = Attention
     return _function

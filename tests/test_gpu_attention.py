@@ -630,3 +630,26 @@ def test_a_new_token_beyond_the_table_is_left_out(torch, Attention, length, wind
         check_tokens(torch, o, q, rows, window, 2)
         for pool, x in zip((kp, vp), want):
             assert torch.equal(pool.view(torch.int16), x.view(torch.int16)), "the token was written over another one"
+
+
+def test_tokens_that_no_sequence_has_take_no_part_in_training(torch, Attention):
+    """Room at the end of a ragged batch, and a sequence cut to q_len and k_len: zeros in o and in the gradients, whatever memory held before."""
+    def junk():
+        return [torch.full((200, 2, 64), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+
+    offsets = torch.tensor([0, 30, 30, 95], dtype=torch.int32, device="cuda")
+    op = Attention(20, 2)
+    for limits, end in (({}, 95), ({"q_len": 40, "k_len": 40}, 70)):
+        x = [normal(torch, s, "bfloat16", 200, 2, 64).requires_grad_() for s in (1, 2, 3)]
+        d_o = normal(torch, 4, "bfloat16", 200, 2, 64)
+        junk()                                                   # (what the allocator hands out next)
+        o = op(*x, offsets, offsets, **limits)
+        junk()
+        o.backward(d_o)
+        got = dict(zip(("dq", "dk", "dv"), (t.grad for t in x)), o=o.detach())
+        for name, t in got.items():
+            assert bool((t[end:] == 0).all()), name
+        lse = op.forward(*(t.detach() for t in x), q_offsets=offsets, k_offsets=offsets, **limits)[1]
+        for of in (slice(0, 30), slice(30, end)):
+            part = {n: t[of] for n, t in got.items()}
+            check_sequence(torch, part | {"lse": lse[:, of]}, *(t.detach()[of] for t in x), 20, 2, d_o=d_o[of])
