@@ -17,7 +17,8 @@
  * Conventions are those of arrow.h: device pointers of the current device, work enqueued on `stream` (a hipStream_t) without
  * waiting, nothing allocated, an arrow_status code and the text in arrow_last_error().  Calls may be captured into a graph.
  * No atomics: results are bitwise reproducible.  Scores, softmax statistics and all sums are held in 32 bits; what goes into a matrix
- * instruction (probabilities, gradients of scores) is rounded to the operands' type first.
+ * instruction (probabilities, gradients of scores) is rounded to the operands' type first; gradients in float16 by the size of d_o, so that small ones
+ * keep its precision.
  */
 #ifndef ARROW_ATTENTION_H
 #define ARROW_ATTENTION_H

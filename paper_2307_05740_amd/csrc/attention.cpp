@@ -124,6 +124,13 @@ size_t rows_bytes(const arrow_attention_t* a) {
   return align_up((size_t)rows * 4);
 }
 
+// Notes of every 32 queries (groups_at of attention_grad.hip).
+size_t notes_bytes(const arrow_attention_t* a) {
+  if (a->dtype != ARROW_F16) return 0;
+  const int64_t groups = a->q_offsets ? (a->q_tokens / 32 + a->batch) * a->q_heads : (int64_t)a->batch * a->q_heads * ceil_div(a->q_len, 32);
+  return align_up((size_t)groups * 4);
+}
+
 int check_cache(const arrow_cache_t* c, const void* k_pool, const void* v_pool) {
   if (!c) return refuse(ARROW_EINVAL, "NULL cache");
   if (int rc = check_heads(c->dtype, c->batch, c->q_heads, c->kv_heads, c->dim, c->window, c->sinks, c->scale)) return rc;
@@ -225,7 +232,7 @@ int arrow_attention_forward_split(const arrow_attention_t* a, const void* q, con
 
 size_t arrow_attention_workspace_bytes(const arrow_attention_t* a) {
   if (check(a)) return 0;
-  return 2 * rows_bytes(a) + align_up((size_t)pairs_of(plan(a)) * 2 * kKeyTile * a->dim * 4);
+  return 2 * rows_bytes(a) + notes_bytes(a) + align_up((size_t)pairs_of(plan(a)) * 2 * kKeyTile * a->dim * 4);
 }
 
 int arrow_attention_backward(const arrow_attention_t* a, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -253,7 +260,8 @@ int arrow_attention_backward(const arrow_attention_t* a, const void* q, const vo
   p.lse_in = lse;
   p.off = (float*)ws;
   p.delta = (float*)((char*)ws + rows_bytes(a));
-  p.parts = (float*)((char*)ws + 2 * rows_bytes(a));
+  p.most = (float*)((char*)ws + 2 * rows_bytes(a));
+  p.parts = (float*)((char*)ws + 2 * rows_bytes(a) + notes_bytes(a));
   return launched("attention backward", launch_attention_backward(p, a->dtype, stream));
 }
 

@@ -4,10 +4,24 @@
 // the first tile to the last, so that no gradient is added up in memory: one over queries for dq (three products, and a fourth that puts it right), one over keys for dk
 // and dv (four).  That is seven products where five would do; the five would take an addition in memory for every tile's dq, whose
 // order either changes from run to run or has to be enforced.
+#include <type_traits>
+
 #include "attention_common.h"
 
 namespace arrow {
 namespace {
+
+// float16 holds nothing below 2^-24, and whole numbers of 2^-24 below 2^-14, which the P and dS of long rows and small gradients do not stay above.  So dS (and P
+// in the dk, dv kernel) are rounded as multiples of a power of two, by the size of d_o: of a row in the dq kernel, of all rows that a key tile's
+// queries are among in the other one, which takes those from the dq kernel's notes, one for 32 queries.
+template <typename T> constexpr bool kScaled = std::is_same<T, _Float16>::value;
+__device__ __forceinline__ float finite_size(float x) { return fabsf(x) < __builtin_inff() ? fabsf(x) : 0.f; }
+// The power of two that brings x into [1, 2), 1 for 0.
+__device__ __forceinline__ float unit_of(float x) { return x > 0.f ? __uint_as_float((254u << 23) - (__float_as_uint(x) & 0x7f800000u)) : 1.f; }
+// Where the notes of a sequence and head begin.
+__device__ __forceinline__ int64_t groups_at(const AttentionArgs& a, bool ragged, int b, int64_t head, int64_t first) {
+  return ragged ? head * (a.q_tokens / 32 + a.batch) + first / 32 + b : ((int64_t)b * a.q_heads + head) * ((a.q_len + 31) / 32);
+}
 
 // dq, and D_i = sum_j P(i,j) <do_i, v_j> for the other kernel.  As the forward kernel: a wavefront holds 32 queries, scores and their gradients
 // are transposed, dS^T is at once the B operand of dQ^T += K^T dS^T.
@@ -61,7 +75,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
   x8<T> qf[kQueriesInLds ? 1 : C / 16], df[C / 16];
   if constexpr (kQueriesInLds)                                   // (waited for with the first tiles)
     Loader<D, kRows, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, room + kQueriesAt, wave);
-  float delta = 0.f;
+  float delta = 0.f, most = 0.f;
 #pragma unroll
   for (int s = 0; s < C / 16; ++s) {
     const int d = 16 * s + 8 * half;
@@ -71,9 +85,24 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
     df[s] = in ? *(const x8<T>*)(d_o + 2 * ((int64_t)row * a.d_o.token + d)) : z;
     const x8<T> of = in ? *(const x8<T>*)(o + 2 * ((int64_t)row * a.o.token + d)) : z;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) delta = fmaf((float)df[s][i], (float)of[i], delta);
+    for (int i = 0; i < 8; ++i) {
+      delta = fmaf((float)df[s][i], (float)of[i], delta);
+      if constexpr (kScaled<T>) most = fmaxf(most, finite_size((float)df[s][i]));
+    }
   }
   delta = add_halves(delta);
+  float larger = 1.f;                                            // that d_o of this row is multiplied by, and taken out of the result again
+  if constexpr (kScaled<T>) {
+    most = max_halves(most);
+    larger = unit_of(most);
+    delta *= larger;
+#pragma unroll
+    for (int s = 0; s < C / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) df[s][i] = (T)((float)df[s][i] * larger);
+    for (int m = 16; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
+    if (lane == 0 && split == 0 && mine < sq.count) a.most[groups_at(a, ragged, b, head, sq.first) + mine / 32] = most;
+  }
   const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
   // of a row that sees nothing, infinity: its probabilities are masked
   const float off = there ? -a.lse_in[stat] / a.scale : 0.f;
@@ -168,7 +197,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
       odd &= odd - 1;
       const T *qr = (const T*)q + (int64_t)at * a.q.token + d, *gr = (const T*)d_o + (int64_t)at * a.d_o.token + d;
       const float q0 = in ? (float)qr[0] : 0.f, q1 = in ? (float)qr[1] : 0.f, g0 = in ? (float)gr[0] : 0.f, g1 = in ? (float)gr[1] : 0.f;
-      const float plus = __shfl(off, r, 64), less = __shfl(delta + rest, r, 64);
+      const float plus = __shfl(off, r, 64), by = __shfl(larger, r, 64), less = __shfl(delta + rest, r, 64);
       float x0 = 0.f, x1 = 0.f;
       for (int j = 0; j <= pr; ++j) {
         if (a.window && j >= a.sinks && j <= pr - a.window) { j = pr - a.window; continue; }
@@ -176,12 +205,12 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
         const float k0 = in ? (float)kj[0] : 0.f, k1 = in ? (float)kj[1] : 0.f;
         float s = q0 * k0 + q1 * k1, e = in ? g0 * (float)vj[0] + g1 * (float)vj[1] : 0.f;
         for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); e += __shfl_xor(e, m, 64); }
-        const float ds = exp2f((s + plus) * c) * (e - less);
+        const float ds = exp2f((s + plus) * c) * (e * by - less);
         x0 = fmaf(ds, k0, x0);
         x1 = fmaf(ds, k1, x1);
       }
       T* to = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)at * a.dq.token + d;
-      if (in) { to[0] = (T)(a.scale * x0); to[1] = (T)(a.scale * x1); }
+      if (in) { to[0] = (T)(a.scale / by * x0); to[1] = (T)(a.scale / by * x1); }
     }
   };
   float test = 0.f;                                           // NaN where a result is not finite
@@ -201,12 +230,13 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
   }
   if (there && half == 0 && split == 0) {
     a.off[stat] = off;
-    a.delta[stat] = -(delta + rest);
+    a.delta[stat] = -(delta + rest) / larger;
   }
+  const float by = a.scale / larger;
 #pragma unroll
   for (int m = 0; m < C / 32; ++m)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[m][i] = a.scale * fmaf(-kept, pk[m][i], acc[m][i]);
+    for (int i = 0; i < 16; ++i) acc[m][i] = by * fmaf(-kept, pk[m][i], acc[m][i]);
   if constexpr (kParts == 1) {
 #pragma unroll
     for (int m = 0; m < C / 32; ++m)
@@ -314,6 +344,15 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
   const int q_steps = end - shift < 0 || first - shift >= sq.count ? 0 : (end - shift) / kQ + 1 - q_begin;
   const int steps = max(q_steps, 0) * a.group;
   const int step0 = (int)((int64_t)steps * part / parts), step1 = (int)((int64_t)steps * (part + 1) / parts);
+  float up = 0.f;                                                // P and dS are rounded 2^up times as large
+  if constexpr (kScaled<T>) {
+    const int from = q_begin * kQ / 32, groups = min((q_begin + max(q_steps, 0)) * (kQ / 32), (sq.count + 31) / 32) - from;
+    float most = 0.f;
+    for (int i = lane; i < groups * a.group; i += 64)
+      most = fmaxf(most, a.most[groups_at(a, ragged, b, kv * a.group + i / groups, sq.first) + from + i % groups]);
+    for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
+    up = __builtin_amdgcn_readfirstlane(min(max(127 - (int)(__float_as_uint(most) >> 23), 0), most > 0.f ? 15 : 0));
+  }
   const float c = a.scale * kLog2e;
 
   const int sharer = kShare ? wave : 0;
@@ -392,7 +431,7 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
       for (int i = 0; i < C / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
       reads_ahead<kKeysInLds ? 16 : 12, C / 16, kKeysInLds ? 2 : 1, C / 16, 1>();   // (eight of those ahead: what the products begin with)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(kScaled<T> ? fmaf(s[i], c, up) : s[i] * c);
       const bool whole = p0 >= low + 31 && q_now + n * 32 + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
       if (!whole) {
         const int ahead = p0 + 4 * half - key;                   // how far the first of this lane's queries is ahead of its key
@@ -476,6 +515,7 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
       }
     }
   };
+  const float back = kScaled<T> ? __builtin_amdgcn_exp2f(-up) : 1.f;
   float test = 0.f;                                              // NaN where a result is not finite
   if constexpr (!kShare) {
     float* sums = (float*)smem;
@@ -498,7 +538,8 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
           x[i] += sums[((w * (C / 32) + wave) * 32 + i) * 64 + lane];
           y[i] += sums[((w * (C / 32) + wave) * 32 + 16 + i) * 64 + lane];
         }
-        x[i] *= a.scale;
+        x[i] *= a.scale * back;
+        y[i] *= back;
         test = fmaf(x[i], 0.f, fmaf(y[i], 0.f, test));
       }
     }
@@ -515,7 +556,8 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
   }
 #pragma unroll
   for (int m = 0; m < C / 32; ++m) {
-    dk[m] *= a.scale;
+    dk[m] *= a.scale * back;
+    if constexpr (kScaled<T>) dv[m] *= back;
 #pragma unroll
     for (int i = 0; i < 16; ++i) test = fmaf(dk[m][i], 0.f, fmaf(dv[m][i], 0.f, test));
   }

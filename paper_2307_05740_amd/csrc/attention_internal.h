@@ -21,6 +21,7 @@ struct AttentionArgs {
   const float* lse_in;             // backward
   float* lse;                      // forward, may be null
   float *off, *delta;              // backward, laid out as lse: -lse_i / scale and -sum_j P(i,j) <do_i, v_j>
+  float* most;                     // backward, float16: the largest |d_o| of every 32 queries, finite ones
   float* parts;                    // backward: sums of the parts of a key tile, dk then dv of each; forward: of the parts of a row, and after them its
                                    // maximum and total, batch x q_heads x q_len x splits of each
   int32_t splits;                  // forward: parts that a row's keys are cut into

@@ -653,3 +653,67 @@ def test_tokens_that_no_sequence_has_take_no_part_in_training(torch, Attention):
         for of in (slice(0, 30), slice(30, end)):
             part = {n: t[of] for n, t in got.items()}
             check_sequence(torch, part | {"lse": lse[:, of]}, *(t.detach()[of] for t in x), 20, 2, d_o=d_o[of])
+
+
+def check_norms(torch, got, q, k, v, window, sinks, d_o):
+    """The gradients of one sequence against 64 bits by their norms.  P and dS are rounded once, relative to themselves, which is u / sqrt(3) of a sum's norm at most
+    where roundings are independent; D adds as much again, and the result is rounded to its type once."""
+    u = oracle.UNIT[q.dtype]
+    heads, kv = q.shape[1], k.shape[1]
+    want = {n: 0 for n in ("dk", "dv")}
+    for h in range(heads):
+        one, _ = oracle.attention(q[:, h], k[:, h * kv // heads], v[:, h * kv // heads], window, sinks, None, d_o[:, h])
+        want["dq"] = one["dq"]
+        for name in ("dk", "dv"):
+            want[name] = want[name] + one[name]
+        of = {"dq": got["dq"][:, h]}
+        if (h + 1) % (heads // kv) == 0:
+            of.update({n: got[n][:, h * kv // heads] for n in ("dk", "dv")})
+        for name, t in of.items():
+            x = want[name]
+            off, result = (float((y.double() - x).norm() / x.norm()) for y in (t, x.to(q.dtype)))
+            assert off <= math.sqrt(result ** 2 + 2 * u * u / 3), (name, h, off, result)
+            if name != "dq":
+                want[name] = 0
+
+
+@pytest.mark.parametrize("size", [0, -6, -10, -12])
+@pytest.mark.parametrize("queries,keys,heads,kv,dim,window,sinks", [(1500, 1500, 1, 1, 64, 0, 0), (1500, 1500, 1, 1, 64, 400, 4), (1100, 1300, 6, 2, 128, 0, 0),
+                                                                    (2100, 2100, 16, 16, 64, 1000, 5), (1000, 1000, 24, 8, 96, 0, 0)])
+def test_small_gradients_in_float16(torch, Attention, queries, keys, heads, kv, dim, window, sinks, size):
+    """Gradients of o of about 2^size over long rows: P dP is below what float16 holds in full."""
+    q, d_o = (normal(torch, s, "float16", queries, heads, dim, by=b) for s, b in ((1, 1.0), (4, 2.0 ** size)))
+    k, v = (normal(torch, s, "float16", keys, kv, dim) for s in (2, 3))
+    got = run(torch, Attention(window, sinks), q[None], k[None], v[None], d_o[None])
+    check_norms(torch, {n: t[0] for n, t in got.items()}, q, k, v, window, sinks, d_o)
+
+
+def test_gradients_of_all_sizes_in_a_ragged_batch(torch, Attention):
+    """Each sequence's gradients are rounded by its own size, however long the others are and wherever it begins."""
+    lengths, sizes = [33, 0, 900, 1, 64, 1003, 95, 31], [-3, 0, -12, 0, -9, 0, -12, -12]
+    starts = [sum(lengths[:i]) for i in range(len(lengths) + 1)]
+    n = starts[-1] + 5
+    q, d_o = (normal(torch, s, "float16", n, 4, 64) for s in (1, 4))
+    k, v = (normal(torch, s, "float16", n, 2, 64) for s in (2, 3))
+    for a, b, size in zip(starts, starts[1:], sizes):
+        d_o[a:b] *= 2.0 ** size
+    offsets = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    for window, sinks in ((0, 0), (200, 3)):
+        got = run(torch, Attention(window, sinks), q, k, v, d_o, q_offsets=offsets, k_offsets=offsets, q_len=1003, k_len=1003)
+        for a, b in zip(starts, starts[1:]):
+            if b - a > 1:
+                of = slice(a, b)
+                check_norms(torch, {x: got[x][of] for x in ("dq", "dk", "dv")}, q[of], k[of], v[of], window, sinks, d_o[of])
+
+
+def test_gradients_of_all_sizes_of_a_float16(torch, Attention):
+    """From the smallest numbers of the type to its largest, in neighbouring rows too, within the bounds."""
+    for low, high in ((-24, -24), (-24, 0), (-14, 15), (4, 15)):
+        g = torch.Generator().manual_seed(8)
+        size = 2.0 ** (low + (high - low) * torch.rand(1, 200, 2, 1, generator=g))
+        q = normal(torch, 1, "float16", 1, 200, 2, 64)
+        k, v = (normal(torch, s, "float16", 1, 200, 1, 64, by=b) for s, b in ((2, 1.0), (3, 2.0 ** -6)))
+        d_o = (torch.randn(1, 200, 2, 64, generator=g).clamp(-1.9, 1.9) * size).half().cuda()
+        for window, sinks in ((0, 0), (40, 2)):
+            got = run(torch, Attention(window, sinks), q, k, v, d_o)
+            check_sequence(torch, {n: t[0] for n, t in got.items()}, q[0], k[0], v[0], window, sinks, d_o=d_o[0])
