@@ -12,7 +12,8 @@
  *
  * over the visible j.  A row without any gives o = 0 and lse = -infinity, and no gradient.  What keys and values hold
  * where a query does not see them, NaN and infinities among it, does not touch its results or its gradient, nor do queries and gradients of
- * results touch those of keys that they do not see; what lies behind a sequence's end is not read.
+ * results touch those of keys that they do not see; what lies behind a sequence's end is not read.  A call in which results are not finite goes through their
+ * tiles a second time.
  *
  * Conventions are those of arrow.h: device pointers of the current device, work enqueued on `stream` (a hipStream_t) without
  * waiting, nothing allocated, an arrow_status code and the text in arrow_last_error().  Calls may be captured into a graph.

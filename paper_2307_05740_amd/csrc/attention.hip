@@ -40,31 +40,9 @@ int query_groups(int64_t blocks, int64_t heads, const AttentionArgs& a) {
   return blocks <= (a.dim <= 64 ? 512 : a.window == 0 && seen >= 1000 ? 384 : 256) ? 2 : 4;
 }
 
-// One row of the result in plain steps, the wavefront's lanes over its columns, by the row's own visible keys alone.  Matrix
-// instructions multiply what a query does not see by a probability of 0, and that is no zero where a value there is infinite or NaN:
-// the rows that this may have touched come here, those without any weight (lse = -infinity), whose result is 0, among them.
-template <typename T>
-__device__ __noinline__ void plain_row(const T* q, const char* k, const char* v, T* o, int64_t k_token, int64_t v_token, int dim, int p, int window,
-                                       int sinks, float scale, float lse) {
-  const int lane = threadIdx.x & 63, d = 2 * lane;
-  const bool mine = d < dim;
-  const float q0 = mine ? (float)q[d] : 0.f, q1 = mine ? (float)q[d + 1] : 0.f;
-  float a0 = 0.f, a1 = 0.f;
-  for (int j = 0; j <= p && lse > minus_infinity(); ++j) {
-    if (window && j >= sinks && j <= p - window) { j = p - window; continue; }
-    const T* kj = (const T*)(k + 2 * (int64_t)j * k_token);
-    const T* vj = (const T*)(v + 2 * (int64_t)j * v_token);
-    float s = mine ? q0 * (float)kj[d] + q1 * (float)kj[d + 1] : 0.f;
-    for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m, 64);
-    const float w = exp2f((s * scale - lse) * kLog2e);
-    if (mine) { a0 += w * (float)vj[d]; a1 += w * (float)vj[d + 1]; }
-  }
-  if (mine) { o[d] = (T)a0; o[d + 1] = (T)a1; }
-}
-
 // kGroups: how many groups of 32 queries the four wavefronts have.
 template <typename T, int C, int kGroups>
-__global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
+__global__ __launch_bounds__(256, kGroups > 1 ? (C <= 64 ? 4 : 2) : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
   constexpr int D = columns_of_tile(C);
   using Tl = Tile<D>;
   constexpr bool kShare = kGroups > 1;                        // tiles
@@ -75,7 +53,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
   // keys and values, two tiles each, of all wavefronts or of each one; joined afterwards: the sums of each, its maxima and totals
   constexpr int kRoom = 4 * kTurns * kBytes;
   static_assert(kParts == 1 || kRoom >= 4 * C * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kRoom + (kParts == 1 ? 0 : 4 * (2 * 64 * 4 + 8))];
+  __shared__ __align__(1024) unsigned char smem[kRoom + (kParts == 1 ? 0 : 4 * 2 * 64 * 4) + 16];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   // Workgroups next to each other go to different dies: an item of every sequence and key head in turn, so that a die has the same keys again
   // and again (8192 queries, 32/8 heads of 128: 300 -> 270 us); of one, the longest rows of a triangle first.
@@ -118,12 +96,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
   // of this wavefront's queries
   const int low = mine + shift, high = min(low + 31, sk.count - 1);
 
-  f32x16 acc[C / 32];
-#pragma unroll
-  for (int m = 0; m < C / 32; ++m) acc[m] = (f32x16)(0.f);
   const float c = a.scale * kLog2e;
-  float top = minus_infinity(), total = 0.f;                  // of c times the scores; of this lane's keys
-
   const int sharer = kShare ? wave : 0;
   const Loader<D, kStep, 4 / kTurns> lk(sharer, lane, a.k.token, a.dim), lv(sharer, lane, a.v.token, a.dim);
   lds_byte* base = (lds_byte*)smem + (kShare ? 0 : wave * 4 * kBytes);
@@ -133,154 +106,159 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
     lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + 2 * to * kBytes, sharer);
     lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, sharer);
   };
-  const int t0 = begin + (kShare ? 0 : wave);
-  if (t0 < end) load(t0, 0);
-  for (int t = t0, now = 0; t < end; t += kTurns, now ^= 1) {
-    if constexpr (kShare) wait_for_tiles();
-    else wait_for_own_tiles();
-    if (t + kTurns < end) load(t + kTurns, now ^ 1);
-    const int skip = kMine < kStep ? part * kMine : 0;        // (keys of the tile that are another wavefront's)
-    const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
-    const int k0 = seen.at(t) * kStep + skip;
-    // no query of this wavefront sees the tile
-    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kMine - 1 <= low - a.window)) continue;
+  // a wavefront joins every kParts-th block of 32 columns; joined_here: the row's keys are all this workgroup's
+  constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
+  const bool joined_here = kGroups > 1 || a.splits == 1;
+  f32x16 r[kJoined];
+  float row_top, row_total, row_lse;
 
-    f32x16 s[kMine / 32];
+  // Matrix instructions multiply what a query does not see by a probability of 0, and that is no zero where a value there is infinite or NaN.  Where a result is not finite though
+  // its row's sum is (so the pass says), the workgroup goes through its tiles again, with care: such values count for those who see them alone.  16,384 tokens, 16/2 heads of
+  // 128, window of 4096: 475 us with finite values, 1580 with an infinity that a quarter of the rows see, 2950 where all see one.
+  auto pass = [&](auto is_careful) -> bool {
+    constexpr bool kCareful = decltype(is_careful)::value;
+    constexpr int kNow = kCareful ? 32 : kMine;                 // keys at a time
+    f32x16 acc[C / 32];
 #pragma unroll
-    for (int n = 0; n < kMine / 32; ++n) s[n] = (f32x16)(0.f);
+    for (int m = 0; m < C / 32; ++m) acc[m] = (f32x16)(0.f);
+    float top = minus_infinity(), total = 0.f;                  // of c times the scores; of this lane's keys
+    const int t0 = begin + (kShare ? 0 : wave);
+    if (t0 < end) load(t0, 0);
+    for (int t = t0, now = 0; t < end; t += kTurns, now ^= 1) {
+      if constexpr (kShare) wait_for_tiles();
+      else wait_for_own_tiles();
+      if (t + kTurns < end) load(t + kTurns, now ^ 1);
+#pragma unroll 1
+      for (int in = 0; in < kMine; in += kNow) {
+        const int skip = (kMine < kStep ? part * kMine : 0) + in; // (keys of the tile that are another wavefront's)
+        const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
+        const int k0 = seen.at(t) * kStep + skip;
+        // no query of this wavefront sees the tile
+        if (k0 > high || (a.window && k0 >= a.sinks && k0 + kNow - 1 <= low - a.window)) continue;
+
+        f32x16 s[kNow / 32];
 #pragma unroll
-    for (int i = 0; i < C / 16; ++i)                          // (in turn: a product waits for the last one on the same sums)
+        for (int n = 0; n < kNow / 32; ++n) s[n] = (f32x16)(0.f);
 #pragma unroll
-      for (int n = 0; n < kMine / 32; ++n) s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
-    reads_ahead<6, (kMine / 32) * (C / 16), 1>();
-    // every query sees every key: nothing to mask
-    const bool whole = k0 + kMine - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kMine <= a.sinks);
-    if (!whole) {
-      const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
-      const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
+        for (int i = 0; i < C / 16; ++i)                          // (in turn: a product waits for the last one on the same sums)
 #pragma unroll
-      for (int n = 0; n < kMine / 32; ++n)
+          for (int n = 0; n < kNow / 32; ++n) s[n] = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), qf[i], s[n]);
+        reads_ahead<6, (kNow / 32) * (C / 16), 1>();
+        // every query sees every key: nothing to mask
+        const bool whole = k0 + kNow - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kNow <= a.sinks);
+        const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
+        const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
+        auto sees = [&](int j, int ago, int sinks) { return bool(((uint32_t)(ago - j) < window) | (j < sinks)); };   // (without branches)
+        if (!whole) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = n * 32 + 8 * (i / 4) + i % 4;
-          const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
-          s[n][i] = visible ? s[n][i] : minus_infinity();
+          for (int n = 0; n < kNow / 32; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool visible = sees(n * 32 + 8 * (i / 4) + i % 4, ago, sinks);
+              s[n][i] = visible ? s[n][i] : minus_infinity();
+            }
         }
-    }
-    float most = s[0][0];
+        float most = s[0][0];
 #pragma unroll
-    for (int n = 0; n < kMine / 32; ++n)
+        for (int n = 0; n < kNow / 32; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
-    most = max_halves(most) * c;
-    // The maximum is only raised where a score is more than 2^8 times the terms' scale: until then they stay within what the sums and
-    // both types hold, and the sums are left as they are.
-    if (__any(most > top + 8.f)) {
-      const float now = most > top + 8.f ? most : top;
-      const float by = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
-      top = now;
-      total *= by;
+          for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
+        most = max_halves(most) * c;
+        // The maximum is only raised where a score is more than 2^8 times the terms' scale: until then they stay within what the sums and
+        // both types hold, and the sums are left as they are.
+        if (__any(most > top + 8.f)) {
+          const float now = most > top + 8.f ? most : top;
+          const float by = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+          top = now;
+          total *= by;
 #pragma unroll
-      for (int m = 0; m < C / 32; ++m) acc[m] *= by;
-    }
-    const float off = top == minus_infinity() ? 0.f : top;
-    x8<T> pf[kMine / 16];
+          for (int m = 0; m < C / 32; ++m) acc[m] *= by;
+        }
+        const float off = top == minus_infinity() ? 0.f : top;
+        x8<T> pf[kNow / 16];
 #pragma unroll
-    for (int n = 0; n < kMine / 32; ++n) {
+        for (int n = 0; n < kNow / 32; ++n) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -off));
-        total += s[n][i];
+          for (int i = 0; i < 16; ++i) {
+            s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -off));
+            total += s[n][i];
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            pf[2 * n + u] = round8<T>(s[n][8 * u], s[n][8 * u + 1], s[n][8 * u + 2], s[n][8 * u + 3], s[n][8 * u + 4], s[n][8 * u + 5],
+                                      s[n][8 * u + 6], s[n][8 * u + 7]);
+        }
+        if constexpr (kCareful) {
+#pragma unroll
+          for (int m = 0; m < C / 32; ++m)
+            add_seen<T, D, kNow / 16, true>(acc[m], vt + my.columns, m, 0, pf,
+                                            [&](int u, int i) { return sees(16 * u + 8 * (i / 4) + i % 4, here(ago), here(sinks)); });
+          continue;
+        }
+#pragma unroll
+        for (int u = 0; u < kNow / 16; ++u)
+#pragma unroll
+          for (int m = 0; m < C / 32; ++m)
+            acc[m] = mma32(read_columns<T, D>(vt + my.columns, m, 16 * u * Tl::kRowBytes), pf[u], acc[m]);
+        reads_ahead<8, (kNow / 16) * (C / 32), 2>();
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        pf[2 * n + u] = round8<T>(s[n][8 * u], s[n][8 * u + 1], s[n][8 * u + 2], s[n][8 * u + 3], s[n][8 * u + 4], s[n][8 * u + 5],
-                                  s[n][8 * u + 6], s[n][8 * u + 7]);
     }
+
+    total = add_halves(total);
+    if constexpr (kParts == 1) {
+      row_top = top;
+      row_total = total;
 #pragma unroll
-    for (int u = 0; u < kMine / 16; ++u)
+      for (int m = 0; m < C / 32; ++m) r[m] = acc[m];
+    } else {
+      float *sums = (float*)smem, *tops = (float*)(smem + kRoom), *totals = tops + 4 * 64;
+      __syncthreads();                                          // the tiles are done with
 #pragma unroll
       for (int m = 0; m < C / 32; ++m)
-        acc[m] = mma32(read_columns<T, D>(vt + my.columns, m, 16 * u * Tl::kRowBytes), pf[u], acc[m]);
-    reads_ahead<8, (kMine / 16) * (C / 32), 2>();
-  }
-
-  total = add_halves(total);
-  T* o = (T*)rows_of(a.o, ragged, b, sq.first, head);
-  const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
-  // 1 / total, 0 for a row that sees nothing; the lanes that hold a result that is not finite though the row's sum is not infinite or NaN
-  auto over = [](float total) { return total > 0.f || total != total ? 1.f / total : 0.f; };
-  auto lse_of = [](float top, float total) { return total == 0.f ? minus_infinity() : (top + __log2f(total)) * kLn2; };
-  auto odd_rows = [&](float test, float lse) {
-    const uint64_t odd = __ballot(there && lse < -minus_infinity() && test != test);
-    return (odd | odd >> 32) & 0xffffffffu;
-  };
-  auto plain_rows = [&](uint64_t odd, float lse) {
-    while (odd) {
-      const int r = __builtin_ctzll(odd), at = mine + r;
-      odd &= odd - 1;
-      plain_row<T>((const T*)q + (int64_t)at * a.q.token, k, v, o + (int64_t)at * a.o.token, a.k.token, a.v.token, a.dim, at + shift, a.window, a.sinks,
-                   a.scale, __shfl(lse, r, 64));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[((wave * (C / 32) + m) * 16 + i) * 64 + lane] = acc[m][i];
+      tops[wave * 64 + lane] = top;
+      totals[wave * 64 + lane] = total;
+      __syncthreads();
+      float all = minus_infinity(), share[kParts];
+#pragma unroll
+      for (int w = 0; w < kParts; ++w) all = fmaxf(all, tops[(group + kGroups * w) * 64 + lane]);
+      const float off = all == minus_infinity() ? 0.f : all;
+      row_top = all;
+      row_total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kParts; ++w) {
+        share[w] = __builtin_amdgcn_exp2f(tops[(group + kGroups * w) * 64 + lane] - off);
+        row_total = fmaf(share[w], totals[(group + kGroups * w) * 64 + lane], row_total);
+      }
+#pragma unroll
+      for (int n = 0; n < kJoined; ++n) {
+        const int m = part + n * kParts;
+        r[n] = (f32x16)(0.f);
+        if (m >= kBlocks) continue;
+#pragma unroll
+        for (int w = 0; w < kParts; ++w)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) r[n][i] = fmaf(share[w], sums[(((group + kGroups * w) * kBlocks + m) * 16 + i) * 64 + lane], r[n][i]);
+      }
     }
-  };
-  if constexpr (kParts == 1) {
-    const float by = over(total), lse = lse_of(top, total);
-    if (a.lse && there && half == 0) a.lse[stat] = lse;
-    float test = 0.f;                                         // NaN where a result is not finite
+    // 1 / total, 0 for a row that sees nothing; parts of rows are left as they are
+    const float by = !joined_here ? 1.f : row_total > 0.f || row_total != row_total ? 1.f / row_total : 0.f;
+    row_lse = row_total == 0.f ? minus_infinity() : (row_top + __log2f(row_total)) * kLn2;
+    float test = 0.f;                                           // NaN where a result is not finite
 #pragma unroll
-    for (int m = 0; m < C / 32; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) { acc[m][i] *= by; test = fmaf(acc[m][i], 0.f, test); }
-    const uint64_t odd = odd_rows(test, lse);
-    // (all lanes take part in the exchange; whether a row is stored is the same in both halves)
-    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, C>(acc, o + (int64_t)row * a.o.token, half, a.dim);
-    plain_rows(odd, lse);
-  } else {
-    float *sums = (float*)smem, *tops = (float*)(smem + kRoom), *totals = tops + 4 * 64;
-    uint64_t* odds = (uint64_t*)(totals + 4 * 64);
-    __syncthreads();                                          // the tiles are done with
-#pragma unroll
-    for (int m = 0; m < C / 32; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sums[((wave * (C / 32) + m) * 16 + i) * 64 + lane] = acc[m][i];
-    tops[wave * 64 + lane] = top;
-    totals[wave * 64 + lane] = total;
-    __syncthreads();
-    float all = minus_infinity(), share[kParts];
-#pragma unroll
-    for (int w = 0; w < kParts; ++w) all = fmaxf(all, tops[(group + kGroups * w) * 64 + lane]);
-    const float off = all == minus_infinity() ? 0.f : all;
-    total = 0.f;
-#pragma unroll
-    for (int w = 0; w < kParts; ++w) {
-      share[w] = __builtin_amdgcn_exp2f(tops[(group + kGroups * w) * 64 + lane] - off);
-      total = fmaf(share[w], totals[(group + kGroups * w) * 64 + lane], total);
-    }
-    const bool whole = kGroups > 1 || a.splits == 1;
-    const float by = whole ? over(total) : 1.f, lse = lse_of(all, total);
-    if (whole && a.lse && there && half == 0 && part == 0) a.lse[stat] = lse;
-    // a wavefront joins every kParts-th block of 32 columns
-    constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
-    f32x16 r[kJoined];
-    float test = 0.f;
-#pragma unroll
-    for (int n = 0; n < kJoined; ++n) {
-      const int m = part + n * kParts;
-      r[n] = (f32x16)(0.f);
-      if (m >= kBlocks) continue;
-#pragma unroll
-      for (int w = 0; w < kParts; ++w)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[n][i] = fmaf(share[w], sums[(((group + kGroups * w) * kBlocks + m) * 16 + i) * 64 + lane], r[n][i]);
+    for (int n = 0; n < kJoined; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) { r[n][i] *= by; test = fmaf(r[n][i], 0.f, test); }
-    }
-    if (!whole) {
+    return there && row_lse < -minus_infinity() && test != test;
+  };
+  auto store = [&] {
+    if (!joined_here) {
       const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_len, place = (((int64_t)b * a.q_heads + head) * a.q_len + row) * a.splits + split;
       if (there && half == 0 && part == 0) {
         float* to = a.parts + rows * a.splits * a.dim + 2 * place;
-        to[0] = all;
-        to[1] = total;
+        to[0] = row_top;
+        to[1] = row_total;
       }
 #pragma unroll
       for (int n = 0; n < kJoined; ++n)
@@ -291,17 +269,21 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_forward_ke
         }
       return;
     }
-    uint64_t odd = odd_rows(test, lse);
-    if (lane == 0) odds[wave] = odd;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kParts; ++w) odd |= odds[group + kGroups * w];
+    const int64_t stat = ragged ? head * a.q_tokens + sq.first + row : ((int64_t)b * a.q_heads + head) * a.q_len + row;
+    if (a.lse && there && half == 0 && part == 0) a.lse[stat] = row_lse;
+    T* o = (T*)rows_of(a.o, ragged, b, sq.first, head) + (int64_t)row * a.o.token;
 #pragma unroll
     for (int n = 0; n < kJoined; ++n) {
       const int m = part + n * kParts;
-      if (m < kBlocks && there && !(odd >> (lane & 31) & 1)) store_block<T>(r[n], m, o + (int64_t)row * a.o.token, half, a.dim);
+      // (all lanes take part in the exchange; whether a row is stored is the same in both halves)
+      if (m < kBlocks && there) store_block<T>(r[n], m, o, half, a.dim);
     }
-    if (part == 0) plain_rows(odd, lse);
+  };
+  const bool again = pass(std::false_type{});
+  store();
+  if (__builtin_expect(any_wave(again, (uint32_t*)(smem + sizeof smem - 16)), 0)) {
+    pass(std::true_type{});
+    store();
   }
 }
 
@@ -311,7 +293,7 @@ __global__ __launch_bounds__(64) void attention_forward_join_kernel(AttentionArg
   const int64_t id = blockIdx.x, unit = id / a.q_len, rows = (int64_t)a.batch * a.q_heads * a.q_len;
   const int row = (int)(id % a.q_len), head = (int)(unit % a.q_heads), b = (int)(unit / a.q_heads), lane = threadIdx.x, d = 2 * lane;
   const bool ragged = a.q_offsets != nullptr;
-  const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
+  const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len);
   if (row >= sq.count) return;
   const bool mine = d < a.dim;
   const float *from = a.parts + id * a.splits * a.dim + d, *stats = a.parts + rows * a.splits * a.dim + 2 * id * a.splits;
@@ -322,10 +304,10 @@ __global__ __launch_bounds__(64) void attention_forward_join_kernel(AttentionArg
   float total = lane < a.splits ? share * stats[2 * lane + 1] : 0.f;
   for (int m = 32; m; m >>= 1) total += __shfl_xor(total, m, 64);
   float x0 = 0.f, x1 = 0.f;
-  for (int i = 0; i < a.splits; i += 8) {                     // (shares from a.splits on are 0)
+  for (int i = 0; i < a.splits; i += 8) {
     float2 x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = mine ? *(const float2*)(from + (int64_t)min(i + j, a.splits - 1) * a.dim) : float2{0.f, 0.f};
+    for (int j = 0; j < 8; ++j) x[j] = mine && i + j < a.splits ? *(const float2*)(from + (int64_t)(i + j) * a.dim) : float2{0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float by = __shfl(share, i + j, 64);
@@ -338,11 +320,7 @@ __global__ __launch_bounds__(64) void attention_forward_join_kernel(AttentionArg
   x1 *= by;
   T* o = (T*)rows_of(a.o, ragged, b, sq.first, head) + (int64_t)row * a.o.token;
   if (a.lse && lane == 0) a.lse[ragged ? head * a.q_tokens + sq.first + row : id] = lse;
-  if (lse < -minus_infinity() && __any(x0 - x0 != 0.f || x1 - x1 != 0.f)) {
-    const int kv = head / a.group;
-    plain_row<T>((const T*)rows_of(a.q, ragged, b, sq.first, head) + (int64_t)row * a.q.token, rows_of(a.k, ragged, b, sk.first, kv), rows_of(a.v, ragged, b, sk.first, kv), o,
-                 a.k.token, a.v.token, a.dim, row + sk.count - sq.count, a.window, a.sinks, a.scale, lse);
-  } else if (mine) {
+  if (mine) {
     o[d] = (T)x0;
     o[d + 1] = (T)x1;
   }

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "attention_internal.h"
 
@@ -138,6 +139,59 @@ __device__ __forceinline__ x8<T> read_columns(uint32_t at, int m, int skip) {
   r.half[0] = lds_transposed((const lds_byte*)(uintptr_t)((at ^ (m << 6)) + skip));
   r.half[1] = lds_transposed((const lds_byte*)(uintptr_t)((at ^ (m << 6 | 32)) + skip + 8 * Tile<D>::kRowBytes));
   return r.all;
+}
+
+// Elements apart: the finite ones, and of the others 1 for infinity, 128 for minus infinity and 129 for NaN: the sum of up to 127 of these says which there are.
+template <typename T> struct Apart { x8<T> finite, other; };
+template <typename T>
+__device__ __forceinline__ Apart<T> apart(x8<T> x) {
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+  constexpr uint16_t infinity = std::is_same<T, __bf16>::value ? 0x7f80 : 0x7c00;
+  union { x8<T> all; u16x8 bits; } u;
+  u.all = x;
+  Apart<T> r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint16_t size = u.bits[i] & 0x7fff;
+    const bool odd = size >= infinity, minus = u.bits[i] >> 15;
+    r.finite[i] = odd ? (T)0.f : x[i];
+    r.other[i] = !odd ? (T)0.f : size > infinity ? (T)129.f : minus ? (T)128.f : (T)1.f;
+  }
+  return r;
+}
+
+// acc += X^T W, where X is 16 kSteps rows of a tile and 32 of its columns, 32 m on.  An element of X that is not finite counts where seen(u, i) says so of the lane's column
+// and the row that element i of operand u has, as itself whatever its weight (kSigned: weights are not negative) or as NaN, and does not elsewhere.  A product with the weights
+// alone would make it NaN everywhere.  (Little is on its way at a time: this is not to take more registers than what it stands beside.)
+template <typename T, int D, int kSteps, bool kSigned, typename F>
+__device__ __forceinline__ void add_seen(f32x16& acc, uint32_t at, int m, int skip, const x8<T>* w, F&& seen) {
+  f32x16 others = (f32x16)(0.f);
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    __builtin_amdgcn_sched_barrier(0);
+    const Apart<T> x = apart<T>(read_columns<T, D>(at, m, skip + 16 * u * Tile<D>::kRowBytes));
+    x8<T> one;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) one[i] = seen(u, i) ? (T)1.f : (T)0.f;
+    acc = mma32(x.finite, w[u], acc);
+    others = mma32(x.other, one, others);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int n = (int)others[i];
+    if (kSigned) acc[i] += (n & 127 ? __builtin_inff() : 0.f) - (n >> 7 ? __builtin_inff() : 0.f);
+    else acc[i] = n ? __builtin_nanf("") : acc[i];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Whether any of the workgroup's four wavefronts says so.  flags: four words that nothing else uses, and are written once.
+__device__ __forceinline__ bool any_wave(bool x, volatile uint32_t* flags) {
+  const bool mine = __any(x);
+  if ((threadIdx.x & 63) == 0) flags[wave_id()] = mine;
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0;
 }
 
 // Copies ROWS rows of an operand into a Tile, straight to LDS, WAVES wavefronts together.  Rows that are not there and columns from `dim` on

@@ -717,3 +717,68 @@ def test_gradients_of_all_sizes_of_a_float16(torch, Attention):
         for window, sinks in ((0, 0), (40, 2)):
             got = run(torch, Attention(window, sinks), q, k, v, d_o)
             check_sequence(torch, {n: t[0] for n, t in got.items()}, q[0], k[0], v[0], window, sinks, d_o=d_o[0])
+
+
+def odd_values(torch, v, at):
+    """v with elements that are not finite, {(key, column): value}."""
+    for (j, d), x in at.items():
+        v[j, :, d] = x
+    return v
+
+
+def want_odd(torch, seen, v):
+    """Where (rows, columns) a result is plus infinity, minus infinity and NaN by the values that each row sees."""
+    see, v = seen.to(v.device).double(), v.double()
+    plus, minus, nan = ((see @ x.double()) > 0 for x in (v == math.inf, v == -math.inf, v.isnan()))
+    nan = nan | (plus & minus)
+    return plus & ~nan, minus & ~nan, nan
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("queries,keys,heads,dim,window,sinks", [(300, 300, 1, 64, 50, 4), (300, 300, 60, 64, 50, 4), (300, 300, 240, 128, 50, 4), (310, 300, 60, 96, 0, 0),
+                                                                 (20, 5000, 2, 64, 0, 0), (40, 6000, 2, 128, 4000, 2), (2100, 2100, 2, 64, 0, 0), (2100, 2100, 16, 128, 600, 70)])
+def test_values_that_are_not_finite_reach_who_sees_them(torch, Attention, dtype, queries, keys, heads, dim, window, sinks):
+    """Infinities of one sign stay, of both make NaN, each in its own column; the rest is within its bounds.  (Scores are small: no weight vanishes.)"""
+    q = normal(torch, 1, dtype, queries, heads, dim, by=0.3)
+    k, v = (normal(torch, s, dtype, keys, 1, dim) for s in (2, 3))
+    half, last = keys // 2, keys - 1
+    odd_values(torch, v, {(half, 3): math.inf, (half + 1, 3): -math.inf, (half + 7, 5): math.nan, (half - 20, 7): -math.inf, (0, 9): math.inf, (last, 11): math.nan,
+                          (last - 2, dim - 1): math.inf, (half, dim - 2): -math.inf})
+    o, lse = Attention(window, sinks).forward(q[None], k[None], v[None])
+    seen = oracle.visible(queries, keys, window, sinks, "cuda")
+    odd = want_odd(torch, seen, v[:, 0])
+    for h in (0, heads - 1):
+        want, bound = oracle.attention(q[:, h], k[:, 0], v[:, 0], window, sinks)
+        got = o[0, :, h].double()
+        for name, x, where in zip(("infinity", "minus infinity", "NaN"), (got == math.inf, got == -math.inf, got.isnan()), odd):
+            assert torch.equal(x, where), (name, h, int((x != where).sum()))
+        finite = ~(odd[0] | odd[1] | odd[2])
+        within(torch, "o", got[finite], want["o"][finite], bound["o"][finite])
+        within(torch, "lse", lse[0, h], want["lse"], bound["lse"])
+
+
+def time_of(torch, call):
+    """The fastest of five, in microseconds."""
+    best = math.inf
+    for _ in range(6):
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        call()
+        end.record()
+        end.synchronize()
+        best = min(best, start.elapsed_time(end) * 1e3)
+    return best
+
+
+@pytest.mark.parametrize("heads,dim,window", [(8, 64, 0), (8, 128, 0), (8, 128, 1024)])
+def test_values_that_are_not_finite_cost_one_pass_more(torch, Attention, heads, dim, window):
+    """A second pass of the same tiles with two products where the first has one, at half as many keys at a time: three to six times a call in all, 12 is room for clocks."""
+    q, k, v = (normal(torch, s, "bfloat16", 1, 4096, heads, dim) for s in (1, 2, 3))
+    op = Attention(window, 4)
+    plain = time_of(torch, lambda: op.forward(q, k, v))
+    v[0, 2] = math.nan                                            # all rows see it
+    every = time_of(torch, lambda: op.forward(q, k, v))
+    v[0, 2] = 0
+    v[0, 1000, :, 5] = math.inf                                   # seen by some
+    some = time_of(torch, lambda: op.forward(q, k, v))
+    assert max(every, some) <= 12 * plain + 50, (plain, every, some)
