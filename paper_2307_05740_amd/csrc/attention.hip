@@ -190,9 +190,11 @@ __global__ __launch_bounds__(256, kGroups > 1 ? (C <= 64 ? 4 : 2) : 1) void atte
         }
         if constexpr (kCareful) {
 #pragma unroll
-          for (int m = 0; m < C / 32; ++m)
-            add_seen<T, D, kNow / 16, true>(acc[m], vt + my.columns, m, 0, pf,
-                                            [&](int u, int i) { return sees(16 * u + 8 * (i / 4) + i % 4, here(ago), here(sinks)); });
+          for (int m = 0; m < C / 32; ++m) {
+            add_finite<T, D, kNow / 16>(acc[m], vt + my.columns, m, pf);
+            add_others<T, D, kNow / 16, true>(acc[m], vt + my.columns, m,
+                                              [&](int u, int i) { return sees(16 * u + 8 * (i / 4) + i % 4, here(ago), here(sinks)); });
+          }
           continue;
         }
 #pragma unroll
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? (C <= 64 ? 4 : 2) : 1) void atte
   };
   const bool again = pass(std::false_type{});
   store();
-  if (__builtin_expect(any_wave(again, (uint32_t*)(smem + sizeof smem - 16)), 0)) {
+  if (__builtin_expect(any_wave(again, (lds_byte*)smem + sizeof smem - 16), 0)) {
     pass(std::true_type{});
     store();
   }

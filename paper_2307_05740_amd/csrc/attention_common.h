@@ -160,38 +160,53 @@ __device__ __forceinline__ Apart<T> apart(x8<T> x) {
   return r;
 }
 
-// acc += X^T W, where X is 16 kSteps rows of a tile and 32 of its columns, 32 m on.  An element of X that is not finite counts where seen(u, i) says so of the lane's column
-// and the row that element i of operand u has, as itself whatever its weight (kSigned: weights are not negative) or as NaN, and does not elsewhere.  A product with the weights
-// alone would make it NaN everywhere.  (Little is on its way at a time: this is not to take more registers than what it stands beside.)
+// Nothing that follows begins before these sums are there.
+__device__ __forceinline__ void one_by_one(f32x16& x) {
+  x = here(x);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// acc += X^T W, where X is 16 kSteps rows of a tile and 32 of its columns, 32 m on, of which elements that are not finite are taken out.
+// (Little is on its way at a time: these are not to take more registers than the products that they stand beside.)
+template <typename T, int D, int kSteps>
+__device__ __forceinline__ void add_finite(f32x16& acc, uint32_t at, int m, const x8<T>* w) {
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    acc = mma32(apart<T>(read_columns<T, D>(at, m, 16 * u * Tile<D>::kRowBytes)).finite, w[u], acc);
+    one_by_one(acc);
+  }
+}
+
+// What was taken out: an element counts where seen(u, i) says so of the lane's column and the row that element i of operand u has, as itself whatever its weight (kSigned:
+// weights are not negative) or as NaN, and does not elsewhere.  A product with the weights would make it NaN everywhere.
 template <typename T, int D, int kSteps, bool kSigned, typename F>
-__device__ __forceinline__ void add_seen(f32x16& acc, uint32_t at, int m, int skip, const x8<T>* w, F&& seen) {
+__device__ __forceinline__ void add_others(f32x16& acc, uint32_t at, int m, F&& seen) {
   f32x16 others = (f32x16)(0.f);
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    __builtin_amdgcn_sched_barrier(0);
-    const Apart<T> x = apart<T>(read_columns<T, D>(at, m, skip + 16 * u * Tile<D>::kRowBytes));
     x8<T> one;
 #pragma unroll
     for (int i = 0; i < 8; ++i) one[i] = seen(u, i) ? (T)1.f : (T)0.f;
-    acc = mma32(x.finite, w[u], acc);
-    others = mma32(x.other, one, others);
+    others = mma32(apart<T>(read_columns<T, D>(at, m, 16 * u * Tile<D>::kRowBytes)).other, one, others);
+    one_by_one(others);
   }
-  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int n = (int)others[i];
     if (kSigned) acc[i] += (n & 127 ? __builtin_inff() : 0.f) - (n >> 7 ? __builtin_inff() : 0.f);
     else acc[i] = n ? __builtin_nanf("") : acc[i];
   }
-  __builtin_amdgcn_sched_barrier(0);
+  one_by_one(acc);
 }
 
-// Whether any of the workgroup's four wavefronts says so.  flags: four words that nothing else uses, and are written once.
-__device__ __forceinline__ bool any_wave(bool x, volatile uint32_t* flags) {
+// Whether any of the workgroup's four wavefronts says so.  flags: four words in LDS that nothing else uses, and are written once.
+__device__ __forceinline__ bool any_wave(bool x, lds_byte* flags) {
+  typedef __attribute__((address_space(3))) uint32_t lds_word;
+  lds_word* at = (lds_word*)flags;
   const bool mine = __any(x);
-  if ((threadIdx.x & 63) == 0) flags[wave_id()] = mine;
+  if ((threadIdx.x & 63) == 0) at[wave_id()] = mine;
   __syncthreads();
-  return __builtin_amdgcn_readfirstlane((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0;
+  return __builtin_amdgcn_readfirstlane((int)(at[0] | at[1] | at[2] | at[3])) != 0;
 }
 
 // Copies ROWS rows of an operand into a Tile, straight to LDS, WAVES wavefronts together.  Rows that are not there and columns from `dim` on
@@ -234,7 +249,8 @@ __device__ __forceinline__ Span span_of(const int32_t* offsets, int b, int64_t t
   first = first < 0 ? 0 : first > tokens ? tokens : first;
   end = end < first ? first : end > tokens ? tokens : end;
   const int64_t n = end - first;
-  return {first, (int)(n < len ? n : len)};
+  // (b is the same in all lanes, and so are these, in scalar registers)
+  return {(int64_t)__builtin_amdgcn_readfirstlane((int)first), __builtin_amdgcn_readfirstlane((int)(n < len ? n : len))};
 }
 __device__ __forceinline__ const char* rows_of(const Operand& m, bool ragged, int b, int64_t first, int64_t head) {
   return (const char*)m.at + 2 * (head * m.head + (ragged ? first * m.token : b * m.sequence));

@@ -18,6 +18,23 @@ template <typename T> constexpr bool kScaled = std::is_same<T, _Float16>::value;
 __device__ __forceinline__ float finite_size(float x) { return fabsf(x) < __builtin_inff() ? fabsf(x) : 0.f; }
 // The power of two that brings x into [1, 2), 1 for 0.
 __device__ __forceinline__ float unit_of(float x) { return x > 0.f ? __uint_as_float((254u << 23) - (__float_as_uint(x) & 0x7f800000u)) : 1.f; }
+// Values of a row or key (this lane's, and those of the lane 32 further on), made smaller by a power of two where they do not fit float16; by which.
+__device__ __forceinline__ float fit(f32x16& x) {
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) most = fmaxf(most, finite_size(x[i]));
+  most = max_halves(most);
+  const float less = most > 0x1p15f ? 0x1p14f * unit_of(most) : 1.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= less;
+  return less;
+}
+// A kernel's arguments, read from memory from here on.
+__device__ __forceinline__ const AttentionArgs& arguments() {
+  auto at = (const __attribute__((address_space(4))) AttentionArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return *(const AttentionArgs*)at;
+}
 // Where the notes of a sequence and head begin.
 __device__ __forceinline__ int64_t groups_at(const AttentionArgs& a, bool ragged, int b, int64_t head, int64_t first) {
   return ragged ? head * (a.q_tokens / 32 + a.batch) + first / 32 + b : ((int64_t)b * a.q_heads + head) * ((a.q_len + 31) / 32);
@@ -48,9 +65,10 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
   constexpr int kTurns = kShare ? 1 : 4, kRows = 32 * kGroups, kParts = 4 / kGroups;
   // k and v, two tiles each, of all wavefronts or of each one, or their sums to be joined; the queries, afterwards the sums of dS to be joined
   constexpr int kQueriesAt = 4 * kTurns * kBytes, kQueriesBytes = kQueriesInLds ? kRows * Tl::kRowBytes : 0;
-  constexpr int kRestBytes = kParts == 1 ? 0 : 2 * 4 * 64 * 4 + 4 * 8;
+  constexpr int kSumBytes = 2 * 4 * 64 * 4, kRestBytes = kParts == 1 ? 0 : kSumBytes + 16, kFlagBytes = kParts == 1 ? 16 : 0;
   static_assert(kParts == 1 || kQueriesAt >= 4 * C * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kQueriesAt + (kQueriesBytes > kRestBytes ? kQueriesBytes : kRestBytes)];
+  constexpr int kEnd = kQueriesAt + (kQueriesBytes > kRestBytes ? kQueriesBytes : kRestBytes);
+  __shared__ __align__(1024) unsigned char smem[kEnd + kFlagBytes];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
   const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;   // as in the forward kernel
   const int g = item % a.group, tile = tiles - 1 - item / a.group;
@@ -73,8 +91,6 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
   lds_byte *room = (lds_byte*)smem, *base = room + (kShare ? 0 : wave * 4 * kBytes);
 
   x8<T> qf[kQueriesInLds ? 1 : C / 16], df[C / 16];
-  if constexpr (kQueriesInLds)                                   // (waited for with the first tiles)
-    Loader<D, kRows, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, room + kQueriesAt, wave);
   float delta = 0.f, most = 0.f;
 #pragma unroll
   for (int s = 0; s < C / 16; ++s) {
@@ -120,163 +136,171 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
     lk.load(k + 2 * (int64_t)k0 * a.k.token, sk.count - k0, base + (2 * to) * kBytes, sharer);
     lv.load(v + 2 * (int64_t)k0 * a.v.token, sk.count - k0, base + (2 * to + 1) * kBytes, sharer);
   };
-  f32x16 acc[C / 32], pk[C / 32];                             // dS K and P K
-#pragma unroll
-  for (int m = 0; m < C / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
-  float rest = 0.f, kept = 0.f;                               // sums of dS of this lane's keys, before and after they are rounded
-  const int t0 = kShare ? 0 : wave;
-  if (t0 < seen.total) load(t0, 0);
-  if constexpr (!kShare && kQueriesInLds) wait_for_tiles();     // (all wavefronts' queries)
-  for (int t = t0, now = 0; t < seen.total; t += kTurns, now ^= 1) {
-    if constexpr (kShare) wait_for_tiles();
-    else wait_for_own_tiles();
-    if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
-    const int skip = kMine < kStep ? split * kMine : 0;
-    const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
-    const uint32_t qt = kQueriesInLds ? here(lds_address(room) + kQueriesAt + group * 32 * Tl::kRowBytes + my.rows) : 0;
-    const int k0 = seen.at(t) * kStep + skip;
-    if (k0 > high || (a.window && k0 >= a.sinks && k0 + kMine - 1 <= low - a.window)) continue;
-    const bool whole = k0 + kMine - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kMine <= a.sinks);
-    const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
-    const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
-#pragma unroll
-    for (int n = 0; n < kMine / 32; ++n) {
-      // the products begin with what is taken off them (which is in one register each, not in 16 ready for that, where those are needed)
-      f32x16 s = (f32x16)(kQueriesInLds ? here(off) : off), e = (f32x16)(kQueriesInLds ? here(-delta) : -delta);
-#pragma unroll
-      for (int i = 0; i < C / 16; ++i)
-        s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt, i, 0) : qf[kQueriesInLds ? 0 : i], s);
-#pragma unroll
-      for (int i = 0; i < C / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
-      reads_ahead<4, C / 16, kQueriesInLds ? 2 : 1, C / 16, 1>();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = n * 32 + 8 * (i / 4) + i % 4;
-          const bool visible = ((uint32_t)(ago - j) < window) | (j < sinks);   // (without branches)
-          s[i] = visible ? s[i] : 0.f;
-          e[i] = visible ? e[i] : 0.f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        e[i] *= s[i];
-        rest += e[i];
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
-        const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
-        if constexpr (kParts > 1) kept = add8(ds, kept);
-#pragma unroll
-        for (int m = 0; m < C / 32; ++m) {
-          const x8<T> kf = read_columns<T, D>(kt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes);
-          acc[m] = mma32(kf, ds, acc[m]);
-          pk[m] = mma32(kf, pf, pk[m]);
-        }
-      }
-      reads_ahead<4, 4 * (C / 32), 1>();
-    }
-  }
+  // a wavefront joins every kParts-th block of 32 columns
+  constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
+  f32x16 r[kJoined];
+  float row_rest;
 
-  rest = add_halves(rest);
-  kept = kParts == 1 ? rest : add_halves(kept);
-  T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
-  // Rows to be done in plain steps, as in the forward kernel: with a result that is not finite, though what they see may be
-  auto odd_rows = [&](float test) {
-    const uint64_t odd = __ballot(there && off == off && delta == delta && test != test);
-    return (odd | odd >> 32) & 0xffffffffu;
-  };
-  auto plain_rows = [&](uint64_t odd) {
-    const int d = 2 * lane;
-    const bool in = d < a.dim;
-    while (odd) {
-      const int r = __builtin_ctzll(odd), at = mine + r, pr = at + shift;
-      odd &= odd - 1;
-      const T *qr = (const T*)q + (int64_t)at * a.q.token + d, *gr = (const T*)d_o + (int64_t)at * a.d_o.token + d;
-      const float q0 = in ? (float)qr[0] : 0.f, q1 = in ? (float)qr[1] : 0.f, g0 = in ? (float)gr[0] : 0.f, g1 = in ? (float)gr[1] : 0.f;
-      const float plus = __shfl(off, r, 64), by = __shfl(larger, r, 64), less = __shfl(delta + rest, r, 64);
-      float x0 = 0.f, x1 = 0.f;
-      for (int j = 0; j <= pr; ++j) {
-        if (a.window && j >= a.sinks && j <= pr - a.window) { j = pr - a.window; continue; }
-        const T *kj = (const T*)k + (int64_t)j * a.k.token + d, *vj = (const T*)v + (int64_t)j * a.v.token + d;
-        const float k0 = in ? (float)kj[0] : 0.f, k1 = in ? (float)kj[1] : 0.f;
-        float s = q0 * k0 + q1 * k1, e = in ? g0 * (float)vj[0] + g1 * (float)vj[1] : 0.f;
-        for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); e += __shfl_xor(e, m, 64); }
-        const float ds = exp2f((s + plus) * c) * (e * by - less);
-        x0 = fmaf(ds, k0, x0);
-        x1 = fmaf(ds, k1, x1);
+  // Twice where a result is not finite though what the row sees may be, as in the forward kernel: the second time elements of keys that are not finite are taken out of the
+  // product, and make NaN of their column for those who see them.  In float16 results are not finite where dS passes 65,504 either: it is rounded as many times smaller there as
+  // it takes.
+  auto pass = [&](auto is_careful) -> bool {
+    constexpr bool kCareful = decltype(is_careful)::value;
+    constexpr int kNow = kCareful ? 32 : kMine;               // keys at a time
+    if constexpr (kQueriesInLds)                              // (waited for with the first tiles)
+      Loader<D, kRows, 4>(wave, lane, a.q.token, a.dim).load(q + 2 * (int64_t)first * a.q.token, sq.count - first, room + kQueriesAt, wave);
+    f32x16 acc[C / 32], pk[C / 32];                           // dS K and P K
+#pragma unroll
+    for (int m = 0; m < C / 32; ++m) { acc[m] = (f32x16)(0.f); pk[m] = (f32x16)(0.f); }
+    float rest = 0.f, kept = 0.f;                             // sums of dS of this lane's keys, before and after they are rounded
+    const int t0 = kShare ? 0 : wave;
+    if (t0 < seen.total) load(t0, 0);
+    if constexpr (!kShare && kQueriesInLds) wait_for_tiles(); // (all wavefronts' queries)
+    for (int t = t0, now = 0; t < seen.total; t += kTurns, now ^= 1) {
+      if constexpr (kShare) wait_for_tiles();
+      else wait_for_own_tiles();
+      if (t + kTurns < seen.total) load(t + kTurns, now ^ 1);
+#pragma unroll 1
+      for (int in = 0; in < kMine; in += kNow) {
+        const int skip = (kMine < kStep ? split * kMine : 0) + in;
+        const uint32_t kt = lds_address(base) + 2 * now * kBytes + skip * Tl::kRowBytes, vt = kt + kBytes;
+        const uint32_t qt = kQueriesInLds ? here(lds_address(room) + kQueriesAt + group * 32 * Tl::kRowBytes + my.rows) : 0;
+        const int k0 = seen.at(t) * kStep + skip;
+        if (k0 > high || (a.window && k0 >= a.sinks && k0 + kNow - 1 <= low - a.window)) continue;
+        const bool whole = k0 + kNow - 1 <= low && (!a.window || k0 > low + 31 - a.window || k0 + kNow <= a.sinks);
+        const int ago = p - k0 - 4 * half, sinks = min(a.sinks - k0 - 4 * half, ago + 1);
+        const uint32_t window = a.window ? (uint32_t)a.window : 0x80000000u;
+        auto sees = [&](int j, int ago, int sinks) { return bool(((uint32_t)(ago - j) < window) | (j < sinks)); };   // (without branches)
+#pragma unroll
+        for (int n = 0; n < kNow / 32; ++n) {
+          // the products begin with what is taken off them (which is in one register each, not in 16 ready for that, where those are needed)
+          f32x16 s = (f32x16)(kQueriesInLds ? here(off) : off), e = (f32x16)(kQueriesInLds ? here(-delta) : -delta);
+#pragma unroll
+          for (int i = 0; i < C / 16; ++i)
+            s = mma32(read_rows<T>(kt + my.rows, i, n * 32 * Tl::kRowBytes), kQueriesInLds ? read_rows<T>(qt, i, 0) : qf[kQueriesInLds ? 0 : i], s);
+#pragma unroll
+          for (int i = 0; i < C / 16; ++i) e = mma32(read_rows<T>(vt + my.rows, i, n * 32 * Tl::kRowBytes), df[i], e);
+          reads_ahead<4, C / 16, kQueriesInLds ? 2 : 1, C / 16, 1>();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool visible = sees(n * 32 + 8 * (i / 4) + i % 4, ago, sinks);
+              s[i] = visible ? s[i] : 0.f;
+              e[i] = visible ? e[i] : 0.f;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            e[i] *= s[i];
+            rest += e[i];
+          }
+          const float less = kCareful && kScaled<T> ? fit(e) : 1.f;
+          x8<T> pf[2], ds[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            pf[u] = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
+            ds[u] = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
+            if constexpr (kParts > 1) kept = kCareful && kScaled<T> ? fmaf(add8(ds[u], 0.f), 1.f / less, kept) : add8(ds[u], kept);
+          }
+          if constexpr (kCareful) {
+            auto seen_of = [&](int u, int i) { return sees(16 * u + 8 * (i / 4) + i % 4, here(ago), here(sinks)); };
+#pragma unroll
+            for (int m = 0; m < C / 32; ++m) add_finite<T, D, 2>(pk[m], kt + my.columns, m, pf);
+#pragma unroll
+            for (int m = 0; m < C / 32; ++m) {
+              if constexpr (kScaled<T>) {
+                f32x16 x = (f32x16)(0.f);
+                add_finite<T, D, 2>(x, kt + my.columns, m, ds);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[m][i] = fmaf(x[i], 1.f / less, acc[m][i]);
+              } else {
+                add_finite<T, D, 2>(acc[m], kt + my.columns, m, ds);
+              }
+              add_others<T, D, 2, false>(acc[m], kt + my.columns, m, seen_of);
+            }
+            continue;
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int m = 0; m < C / 32; ++m) {
+              const x8<T> kf = read_columns<T, D>(kt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes);
+              acc[m] = mma32(kf, ds[u], acc[m]);
+              pk[m] = mma32(kf, pf[u], pk[m]);
+            }
+          reads_ahead<4, 4 * (C / 32), 1>();
+        }
       }
-      T* to = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)at * a.dq.token + d;
-      if (in) { to[0] = (T)(a.scale / by * x0); to[1] = (T)(a.scale / by * x1); }
     }
-  };
-  float test = 0.f;                                           // NaN where a result is not finite
-  uint64_t* odds = (uint64_t*)(smem + kQueriesAt + 2 * 4 * 64 * 4);
-  if constexpr (kParts > 1) {
-    float* rests = (float*)(smem + kQueriesAt);
-    wait_for_tiles();                                           // the tiles and queries are done with, or there and not needed
-    rests[wave * 64 + lane] = rest;
-    rests[(4 + wave) * 64 + lane] = kept;
-    __syncthreads();
-    rest = kept = 0.f;
+
+    rest = add_halves(rest);
+    kept = kParts == 1 ? rest : add_halves(kept);
+    if constexpr (kParts > 1) {
+      float* rests = (float*)(smem + kQueriesAt);
+      wait_for_tiles();                                       // the tiles and queries are done with, or there and not needed
+      rests[wave * 64 + lane] = rest;
+      rests[(4 + wave) * 64 + lane] = kept;
+      __syncthreads();
+      rest = kept = 0.f;
 #pragma unroll
-    for (int w = 0; w < kParts; ++w) {
-      rest += rests[(group + kGroups * w) * 64 + lane];
-      kept += rests[(4 + group + kGroups * w) * 64 + lane];
+      for (int w = 0; w < kParts; ++w) {
+        rest += rests[(group + kGroups * w) * 64 + lane];
+        kept += rests[(4 + group + kGroups * w) * 64 + lane];
+      }
     }
-  }
-  if (there && half == 0 && split == 0) {
-    a.off[stat] = off;
-    a.delta[stat] = -(delta + rest) / larger;
-  }
-  const float by = a.scale / larger;
-#pragma unroll
-  for (int m = 0; m < C / 32; ++m)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[m][i] = by * fmaf(-kept, pk[m][i], acc[m][i]);
-  if constexpr (kParts == 1) {
+    row_rest = rest;
+    const float by = a.scale / larger;
 #pragma unroll
     for (int m = 0; m < C / 32; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) test = fmaf(acc[m][i], 0.f, test);
-    const uint64_t odd = odd_rows(test);
-    if (there && !(odd >> (lane & 31) & 1)) store_columns<T, C>(acc, dq, half, a.dim);
-    plain_rows(odd);
-  } else {
-    float* sums = (float*)smem;
-    constexpr int kBlocks = C / 32, kJoined = (kBlocks + kParts - 1) / kParts;
+      for (int i = 0; i < 16; ++i) acc[m][i] = by * fmaf(-kept, pk[m][i], acc[m][i]);
+    if constexpr (kParts == 1) {
 #pragma unroll
-    for (int m = 0; m < kBlocks; ++m)
+      for (int m = 0; m < kBlocks; ++m) r[m] = acc[m];
+    } else {
+      float* sums = (float*)smem;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sums[((wave * kBlocks + m) * 16 + i) * 64 + lane] = acc[m][i];
-    __syncthreads();
-    f32x16 r[kJoined];                                          // a wavefront joins every kParts-th block of 32 columns
+      for (int m = 0; m < kBlocks; ++m)
 #pragma unroll
-    for (int n = 0; n < kJoined; ++n) {
-      const int m = split + n * kParts;
-      r[n] = (f32x16)(0.f);
-      if (m >= kBlocks) continue;
+        for (int i = 0; i < 16; ++i) sums[((wave * kBlocks + m) * 16 + i) * 64 + lane] = acc[m][i];
+      __syncthreads();
 #pragma unroll
-      for (int w = 0; w < kParts; ++w)
+      for (int n = 0; n < kJoined; ++n) {
+        const int m = split + n * kParts;
+        r[n] = (f32x16)(0.f);
+        if (m >= kBlocks) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) r[n][i] += sums[(((group + kGroups * w) * kBlocks + m) * 16 + i) * 64 + lane];
+        for (int w = 0; w < kParts; ++w)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) r[n][i] += sums[(((group + kGroups * w) * kBlocks + m) * 16 + i) * 64 + lane];
+      }
+    }
+    float test = 0.f;                                         // NaN where a result is not finite
+#pragma unroll
+    for (int n = 0; n < kJoined; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) test = fmaf(r[n][i], 0.f, test);
+    return there && off == off && delta == delta && test != test;
+  };
+  auto store = [&] {
+    if (there && half == 0 && split == 0) {
+      a.off[stat] = off;
+      a.delta[stat] = -(delta + row_rest) / larger;
     }
-    uint64_t odd = odd_rows(test);
-    if (lane == 0) odds[wave] = odd;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kParts; ++w) odd |= odds[group + kGroups * w];
+    T* dq = (T*)rows_of(a.dq, ragged, b, sq.first, head) + (int64_t)row * a.dq.token;
 #pragma unroll
     for (int n = 0; n < kJoined; ++n) {
       const int m = split + n * kParts;
-      if (m < kBlocks && there && !(odd >> (lane & 31) & 1)) store_block<T>(r[n], m, dq, half, a.dim);
+      if (m < kBlocks && there) store_block<T>(r[n], m, dq, half, a.dim);
     }
-    if (split == 0) plain_rows(odd);
+  };
+  const bool again = pass(std::false_type{});
+  store();
+  if (__builtin_expect(any_wave(again, room + (kParts == 1 ? kEnd : kQueriesAt + kSumBytes)), 0)) {
+    pass(std::true_type{});
+    store();
   }
 }
 
@@ -291,18 +315,30 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
 // What bounds it: as the dq kernel; of 256 registers 128 are sums (heads of 128), so the keys are read from LDS as the queries are there.  8192 tokens, as above: 530 us = 910
 // TFLOP/s, matrix units busy 45 %, LDS 34 % of the cycles; 4 x 2048: 61 us.  The queries come from behind the L2 (1.6 GB); another order of them, in which
 // workgroups of a die read the same ones, took as long.
-template <typename T, int C, bool kShare>
-__global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
-  constexpr int D = columns_of_tile(C);
-  using Tl = Tile<D>;
-  constexpr bool kKeysInLds = D > 64;
-  constexpr int kQ = kKeysInLds || !kShare ? 32 : 64, kBytes = kQ * Tl::kRowBytes;   // queries of a step
-  constexpr int kTurns = kShare ? 1 : 4, kKeys = kShare ? kKeyTile : 32;
+//
+// Twice where a result is not finite, as in the dq kernel: the second time (kCareful) elements of queries and of gradients that are not finite are taken out of the products and
+// count for the keys that their queries see.  All gradients, 4096 tokens, 8 heads of 64, no window: 135 us, 496 with an infinity in one gradient of o; 8192 tokens, as above, in
+// float16: 1010 and 4050.
+template <int C, bool kShare>
+struct KeyRoom {                                                 // in LDS
+  static constexpr int D = columns_of_tile(C);
+  static constexpr bool kKeysInLds = D > 64;
+  static constexpr int kQ = kKeysInLds || !kShare ? 32 : 64, kBytes = kQ * Tile<D>::kRowBytes;   // queries of a step
+  static constexpr int kTurns = kShare ? 1 : 4, kKeys = kShare ? kKeyTile : 32;
   // q and do, two tiles each, of all wavefronts or of each one, or their sums to be joined; the keys; what the dq kernel noted of each query, two steps'
-  constexpr int kKeysAt = 4 * kTurns * kBytes, kStatsAt = kKeysAt + (kKeysInLds ? kKeys * Tl::kRowBytes : 0), kStatsBytes = 2 * 2 * 4 * kQ;
+  static constexpr int kKeysAt = 4 * kTurns * kBytes, kStatsAt = kKeysAt + (kKeysInLds ? kKeys * Tile<D>::kRowBytes : 0), kStatsBytes = 2 * 2 * 4 * kQ;
+  static constexpr int kFlagsAt = kStatsAt + kTurns * kStatsBytes, kAll = kFlagsAt + 16;
   static_assert(kShare || kKeysAt >= 4 * 2 * D * 32 * 4, "room for the sums");
-  __shared__ __align__(1024) unsigned char smem[kStatsAt + kTurns * kStatsBytes];
-  const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
+};
+
+// Whether a result of this lane's is not finite.
+template <typename T, int C, bool kShare, bool kCareful>
+__device__ __forceinline__ bool dkv_pass(const AttentionArgs& a, int tiles, unsigned char* smem, int thread) {
+  using Room = KeyRoom<C, kShare>;
+  constexpr int D = Room::D, kQ = Room::kQ, kBytes = Room::kBytes, kTurns = Room::kTurns, kKeys = Room::kKeys, kKeysAt = Room::kKeysAt;
+  constexpr bool kKeysInLds = Room::kKeysInLds;
+  using Tl = Tile<D>;
+  const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), half = lane >> 5;
   // an item of every head and sequence in turn; the longest first, and last the small parts of keys that all queries see
   const int units = a.kv_heads * a.batch, unit = blockIdx.x % units, item = blockIdx.x / units;
   const int kv = unit % a.kv_heads, b = unit / a.kv_heads;
@@ -314,28 +350,28 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
   const bool ragged = a.q_offsets != nullptr;
   const Span sq = span_of(a.q_offsets, b, a.q_tokens, a.q_len), sk = span_of(a.k_offsets, b, a.k_tokens, a.k_len);
   const int first = tile * kKeys;
-  if (first >= sk.count) return;
+  if (first >= sk.count) return false;
   const int shift = sk.count - sq.count;
   const int mine = first + (kShare ? wave * 32 : 0);
   const int key = mine + (lane & 31);
   const bool there = key < sk.count;
   const char* k = rows_of(a.k, ragged, b, sk.first, kv);
   const char* v = rows_of(a.v, ragged, b, sk.first, kv);
-  x8<T> kf[kKeysInLds ? 1 : C / 16], vf[C / 16];
   if constexpr (kKeysInLds)                                      // (waited for with the first step's tiles)
     Loader<D, kKeys, 4>(wave, lane, a.k.token, a.dim).load(k + 2 * (int64_t)first * a.k.token, sk.count - first, (lds_byte*)smem + kKeysAt, wave);
-#pragma unroll
-  for (int s = 0; s < C / 16; ++s) {
-    const int d = 16 * s + 8 * half;
+  // this lane's key and value, columns 16 s + 8 half and on: in registers, or (kCareful) read again and again
+  const char *k_at = k + 2 * ((int64_t)key * a.k.token + 8 * half), *v_at = v + 2 * ((int64_t)key * a.v.token + 8 * half);
+  auto piece = [&](const char* at, int s) {
     const x8<T> z = {};
-    const bool in = there && d < a.dim;
-    if constexpr (!kKeysInLds) kf[s] = in ? *(const x8<T>*)(k + 2 * ((int64_t)key * a.k.token + d)) : z;
-    vf[s] = in ? *(const x8<T>*)(v + 2 * ((int64_t)key * a.v.token + d)) : z;
-  }
-  f32x16 dk[C / 32], dv[C / 32];
+    return there && 16 * s + 8 * half < a.dim ? *(const x8<T>*)(at + 32 * s) : z;
+  };
+  x8<T> kf[kKeysInLds || kCareful ? 1 : C / 16], vf[kCareful ? 1 : C / 16];
+  if constexpr (!kCareful)
 #pragma unroll
-  for (int m = 0; m < C / 32; ++m) { dk[m] = (f32x16)(0.f); dv[m] = (f32x16)(0.f); }
-
+    for (int s = 0; s < C / 16; ++s) {
+      if constexpr (!kKeysInLds) kf[s] = piece(k_at, s);
+      vf[s] = piece(v_at, s);
+    }
   // queries that see one of the tile's keys: positions first .. end
   const int tile_end = min(first + kKeys, sk.count) - 1;
   int end = sk.count - 1;
@@ -348,8 +384,11 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
   if constexpr (kScaled<T>) {
     const int from = q_begin * kQ / 32, groups = min((q_begin + max(q_steps, 0)) * (kQ / 32), (sq.count + 31) / 32) - from;
     float most = 0.f;
-    for (int i = lane; i < groups * a.group; i += 64)
-      most = fmaxf(most, a.most[groups_at(a, ragged, b, kv * a.group + i / groups, sq.first) + from + i % groups]);
+    const AttentionArgs& z = arguments();                        // (what only this needs is in no register later)
+    const float* notes = z.most + groups_at(z, ragged, b, kv * z.group, sq.first) + from;
+    const int64_t step = groups_at(z, ragged, 0, 1, 0) - groups_at(z, ragged, 0, 0, 0);
+    for (int h = 0; h < z.group; ++h, notes += step)
+      for (int i = lane; i < groups; i += 64) most = fmaxf(most, notes[i]);
     for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
     up = __builtin_amdgcn_readfirstlane(min(max(127 - (int)(__float_as_uint(most) >> 23), 0), most > 0.f ? 15 : 0));
   }
@@ -358,10 +397,14 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
   const int sharer = kShare ? wave : 0;
   const Loader<D, kQ, 4 / kTurns> lq(sharer, lane, a.q.token, a.dim), ld(sharer, lane, a.d_o.token, a.dim);
   lds_byte *room = (lds_byte*)smem, *base = room + (kShare ? 0 : wave * 4 * kBytes);
-  lds_byte* stats = room + kStatsAt + (kShare ? 0 : wave * kStatsBytes);
+  lds_byte* stats = room + Room::kStatsAt + (kShare ? 0 : wave * Room::kStatsBytes);
   const TileReads<D> my(lane);
-  // the step that is loaded next: a head's queries from q_next on, and where they lie
   const int64_t q_step = 2 * kQ * a.q.token, d_step = 2 * kQ * a.d_o.token;
+  constexpr int kNow = kCareful ? 32 : kQ;                       // queries at a time
+  f32x16 dk[C / 32], dv[C / 32];
+#pragma unroll
+  for (int m = 0; m < C / 32; ++m) { dk[m] = (f32x16)(0.f); dv[m] = (f32x16)(0.f); }
+  // the step that is loaded next: a head's queries from q_next on, and where they lie
   int head = kv * a.group, q_next = 0;
   const char *q_at = nullptr, *d_at = nullptr;
   int64_t stat_at = 0;
@@ -395,7 +438,7 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
       if (head < (kv + 1) * a.group) begin(from);
     }
   };
-  const int mine0 = step0 + (kShare ? 0 : wave);                 // this wavefront's first step
+  const int mine0 = step0 + (kShare ? 0 : wave);              // this wavefront's first step
   int q_loaded = 0;
   if (mine0 < step1) {
     head += mine0 / q_steps;
@@ -403,124 +446,117 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
     q_loaded = q_next;
     load(0);
   }
-  if constexpr (!kShare) wait_for_tiles();                       // (all wavefronts' keys)
+  if constexpr (!kShare) wait_for_tiles();                    // (all wavefronts' keys)
   for (int t = mine0, now = 0; t < step1; t += kTurns, now ^= 1) {
     if constexpr (kShare) wait_for_tiles();
     else wait_for_own_tiles();
     const int q_now = q_loaded;
     if (t + kTurns < step1) { q_loaded = q_next; load(now ^ 1); }
-    const uint32_t qt = lds_address(base) + (2 * now) * kBytes;
     const uint32_t kt = lds_address(room) + kKeysAt + sharer * 32 * Tl::kRowBytes + my.rows;
-    const uint32_t stat = lds_address(stats) + now * (2 * 4 * kQ) + 16 * half;
-    const int low = mine, high = min(low + 31, sk.count - 1);   // this wavefront's keys
+    auto key_of = [&](int i) {
+      if constexpr (kKeysInLds) return read_rows<T>(kCareful ? here(kt) : kt, i, 0);
+      else if constexpr (kCareful) return piece(here(k_at), i);
+      else return kf[i];
+    };
+    auto value_of = [&](int i) {
+      if constexpr (kCareful) return piece(here(v_at), i);
+      else return vf[i];
+    };
+    const int low = mine, high = min(low + 31, sk.count - 1); // this wavefront's keys
+#pragma unroll 1
+    for (int in = 0; in < kQ; in += kNow) {
+      const uint32_t qt = lds_address(base) + (2 * now) * kBytes + in * Tl::kRowBytes;
+      const uint32_t stat = lds_address(stats) + now * (2 * 4 * kQ) + 16 * half + 4 * in;
 #pragma unroll
-    for (int n = 0; n < kQ / 32; ++n) {
-      const int p0 = q_now + n * 32 + shift;                     // position of the first of 32 queries
-      if (q_now + n * 32 >= sq.count || p0 + 31 < low || (a.window && low >= a.sinks && p0 - a.window >= high)) continue;
-      f32x16 s, e;                                               // the products begin with what is taken off them
+      for (int n = 0; n < kNow / 32; ++n) {
+        const int first_q = q_now + in + n * 32, p0 = first_q + shift;   // the first of 32 queries, and its position
+        if (first_q >= sq.count || p0 + 31 < low || (a.window && low >= a.sinks && p0 - a.window >= high)) continue;
+        f32x16 s, e;                                          // the products begin with what is taken off them
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const f32x4 x = lds_read4(stat + 4 * (n * 32 + 2 * i)), y = lds_read4(stat + 4 * (kQ + n * 32 + 2 * i));
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 x = lds_read4(stat + 4 * (n * 32 + 2 * i)), y = lds_read4(stat + 4 * (kQ + n * 32 + 2 * i));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { s[i + j] = x[j]; e[i + j] = y[j]; }
-      }
+          for (int j = 0; j < 4; ++j) { s[i + j] = x[j]; e[i + j] = y[j]; }
+        }
 #pragma unroll
-      for (int i = 0; i < C / 16; ++i)
-        s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), kKeysInLds ? read_rows<T>(kt, i, 0) : kf[kKeysInLds ? 0 : i], s);
+        for (int i = 0; i < C / 16; ++i) {
+          s = mma32(read_rows<T>(qt + my.rows, i, n * 32 * Tl::kRowBytes), key_of(i), s);
+          if constexpr (kCareful) one_by_one(s);
+        }
 #pragma unroll
-      for (int i = 0; i < C / 16; ++i) e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), vf[i], e);
-      reads_ahead<kKeysInLds ? 16 : 12, C / 16, kKeysInLds ? 2 : 1, C / 16, 1>();   // (eight of those ahead: what the products begin with)
+        for (int i = 0; i < C / 16; ++i) {
+          e = mma32(read_rows<T>(qt + my.rows, i, kBytes + n * 32 * Tl::kRowBytes), value_of(i), e);
+          if constexpr (kCareful) one_by_one(e);
+        }
+        if constexpr (!kCareful) reads_ahead<kKeysInLds ? 16 : 12, C / 16, kKeysInLds ? 2 : 1, C / 16, 1>();   // (eight of those ahead: what the products begin with)
+        const float lift = kScaled<T> ? here(up) : 0.f;          // (in a scalar register otherwise)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(kScaled<T> ? fmaf(s[i], c, up) : s[i] * c);
-      const bool whole = p0 >= low + 31 && q_now + n * 32 + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
-      if (!whole) {
-        const int ahead = p0 + 4 * half - key;                   // how far the first of this lane's queries is ahead of its key
-        const int left = sq.count - (q_now + n * 32 + 4 * half);
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(kScaled<T> ? fmaf(s[i], c, lift) : s[i] * c);
+        const bool whole = p0 >= low + 31 && first_q + 32 <= sq.count && (!a.window || p0 + 31 - a.window < low || low + 32 <= a.sinks);
+        const int ahead = p0 + 4 * half - key;                // how far the first of this lane's queries is ahead of its key
+        const int left = sq.count - (first_q + 4 * half);
         const uint32_t window = a.window && key >= a.sinks ? (uint32_t)a.window : 0x80000000u;
+        auto seen = [&](int j, int ahead) { return bool(((uint32_t)(ahead + j) < window) & (j < left)); };
+        if (!whole) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = 8 * (i / 4) + i % 4;
-          const bool visible = ((uint32_t)(ahead + j) < window) & (j < left);
-          s[i] = visible ? s[i] : 0.f;
-          e[i] = visible ? e[i] : 0.f;
+          for (int i = 0; i < 16; ++i) {
+            const bool visible = seen(8 * (i / 4) + i % 4, ahead);
+            s[i] = visible ? s[i] : 0.f;
+            e[i] = visible ? e[i] : 0.f;
+          }
         }
-      }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) e[i] *= s[i];
+        for (int i = 0; i < 16; ++i) e[i] *= s[i];
+        const float less = kCareful && kScaled<T> ? fit(e) : 1.f;
+        x8<T> pf[2], ds[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const x8<T> pf = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
-        const x8<T> ds = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
-#pragma unroll
-        for (int m = 0; m < C / 32; ++m) {
-          dv[m] = mma32(read_columns<T, D>(qt + my.columns, m, kBytes + (n * 32 + 16 * u) * Tl::kRowBytes), pf, dv[m]);
-          dk[m] = mma32(read_columns<T, D>(qt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes), ds, dk[m]);
+        for (int u = 0; u < 2; ++u) {
+          pf[u] = round8<T>(s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]);
+          ds[u] = round8<T>(e[8 * u], e[8 * u + 1], e[8 * u + 2], e[8 * u + 3], e[8 * u + 4], e[8 * u + 5], e[8 * u + 6], e[8 * u + 7]);
         }
+        if constexpr (kCareful) {
+          auto seen_of = [&](int u, int i) { return seen(16 * u + 8 * (i / 4) + i % 4, here(ahead)); };
+          const uint32_t q_tile = qt + my.columns, d_tile = q_tile + kBytes;
+#pragma unroll
+          for (int m = 0; m < C / 32; ++m) {
+            add_finite<T, D, 2>(dv[m], d_tile, m, pf);
+            add_others<T, D, 2, true>(dv[m], d_tile, m, seen_of);
+          }
+#pragma unroll
+          for (int m = 0; m < C / 32; ++m) {
+            if constexpr (kScaled<T>) {
+              f32x16 x = (f32x16)(0.f);
+              add_finite<T, D, 2>(x, q_tile, m, ds);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) dk[m][i] = fmaf(x[i], 1.f / less, dk[m][i]);
+            } else {
+              add_finite<T, D, 2>(dk[m], q_tile, m, ds);
+            }
+            add_others<T, D, 2, false>(dk[m], q_tile, m, seen_of);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int m = 0; m < C / 32; ++m) {
+            dv[m] = mma32(read_columns<T, D>(qt + my.columns, m, kBytes + (n * 32 + 16 * u) * Tl::kRowBytes), pf[u], dv[m]);
+            dk[m] = mma32(read_columns<T, D>(qt + my.columns, m, (n * 32 + 16 * u) * Tl::kRowBytes), ds[u], dk[m]);
+          }
+        reads_ahead<kKeysInLds ? 8 : 4, 4 * (C / 32), 2>();
       }
-      reads_ahead<kKeysInLds ? 8 : 4, 4 * (C / 32), 2>();
     }
   }
 
-  T *dk_to = (T*)rows_of(a.dk, ragged, b, sk.first, kv), *dv_to = (T*)rows_of(a.dv, ragged, b, sk.first, kv);
-  // parts in the workspace: [sequence, head][item][dk, dv][key][dim]; items of tiles in one part have no place there
-  float* part_to = nullptr;
-  if (parts > 1) part_to = a.parts + part_place(a, tiles, ((int64_t)b * a.kv_heads + kv), tile, part) * 2 * kKeyTile * a.dim + (int64_t)(mine - first) * a.dim;
-  // Keys to be done in plain steps, as rows in the forward kernel: with a result that is not finite, which may come from a query that does
-  // not see them.  A key whose gradients are NaN throughout is done.
-  auto odd_keys = [&](float test) {
-    const uint64_t odd = __ballot(there && test != test);
-    return (odd | odd >> 32) & 0xffffffffu;
-  };
-  auto plain_keys = [&](uint64_t odd) {
-    const int d = 2 * lane;
-    const bool in = d < a.dim;
-    while (odd) {
-      const int r = __builtin_ctzll(odd), j = mine + r;
-      odd &= odd - 1;
-      const T *kj = (const T*)k + (int64_t)j * a.k.token + d, *vj = (const T*)v + (int64_t)j * a.v.token + d;
-      const float k0 = in ? (float)kj[0] : 0.f, k1 = in ? (float)kj[1] : 0.f, v0 = in ? (float)vj[0] : 0.f, v1 = in ? (float)vj[1] : 0.f;
-      float x0 = 0.f, x1 = 0.f, y0 = 0.f, y1 = 0.f;
-      bool done = false;
-      for (int t = step0; t < step1 && !done; ++t) {
-        const int from = (q_begin + t % q_steps) * kQ, h = kv * a.group + t / q_steps;
-        const T *qh = (const T*)rows_of(a.q, ragged, b, sq.first, h) + d, *gh = (const T*)rows_of(a.d_o, ragged, b, sq.first, h) + d;
-        const int64_t stat = ragged ? h * a.q_tokens + sq.first : ((int64_t)b * a.q_heads + h) * a.q_len;
-        for (int i = from; i < min(from + kQ, sq.count) && !done; ++i) {
-          const int p = i + shift;
-          if (j > p || (a.window && j >= a.sinks && j <= p - a.window)) continue;
-          const T *qi = qh + (int64_t)i * a.q.token, *gi = gh + (int64_t)i * a.d_o.token;
-          const float q0 = in ? (float)qi[0] : 0.f, q1 = in ? (float)qi[1] : 0.f, g0 = in ? (float)gi[0] : 0.f, g1 = in ? (float)gi[1] : 0.f;
-          float s = q0 * k0 + q1 * k1, e = g0 * v0 + g1 * v1;
-          for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); e += __shfl_xor(e, m, 64); }
-          const float w = exp2f((s + a.off[stat + i]) * c), ds = w * (e + a.delta[stat + i]);
-          x0 = fmaf(ds, q0, x0);
-          x1 = fmaf(ds, q1, x1);
-          y0 = fmaf(w, g0, y0);
-          y1 = fmaf(w, g1, y1);
-          done = __all(!in || (x0 != x0 && x1 != x1 && y0 != y0 && y1 != y1));
-        }
-      }
-      if (in && parts > 1) {
-        float* to = part_to + (int64_t)r * a.dim + d;
-        to[0] = a.scale * x0;
-        to[1] = a.scale * x1;
-        to[kKeyTile * a.dim] = y0;
-        to[kKeyTile * a.dim + 1] = y1;
-      } else if (in) {
-        T *x = dk_to + (int64_t)j * a.dk.token + d, *y = dv_to + (int64_t)j * a.dv.token + d;
-        x[0] = (T)(a.scale * x0);
-        x[1] = (T)(a.scale * x1);
-        y[0] = (T)y0;
-        y[1] = (T)y1;
-      }
-    }
-  };
-  const float back = kScaled<T> ? __builtin_amdgcn_exp2f(-up) : 1.f;
-  float test = 0.f;                                              // NaN where a result is not finite
-  if constexpr (!kShare) {
+  // what this wavefront has in the end: all columns, or 32 of them of what the four have together
+  constexpr int kBlocks = kShare ? C / 32 : 1;
+  f32x16 dk_sum[kBlocks], dv_sum[kBlocks];
+  if constexpr (kShare) {
+#pragma unroll
+    for (int m = 0; m < C / 32; ++m) { dk_sum[m] = dk[m]; dv_sum[m] = dv[m]; }
+  } else {
     float* sums = (float*)smem;
-    uint64_t* odds = (uint64_t*)(smem + kStatsAt);
-    __syncthreads();                                             // the tiles are done with
+    __syncthreads();                                          // the tiles are done with
 #pragma unroll
     for (int m = 0; m < C / 32; ++m)
 #pragma unroll
@@ -529,58 +565,65 @@ __global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention
         sums[((wave * (C / 32) + m) * 32 + 16 + i) * 64 + lane] = dv[m][i];
       }
     __syncthreads();
-    f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);                 // a wavefront joins 32 columns
+    f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);              // a wavefront joins 32 columns
     if (wave < C / 32) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           x[i] += sums[((w * (C / 32) + wave) * 32 + i) * 64 + lane];
           y[i] += sums[((w * (C / 32) + wave) * 32 + 16 + i) * 64 + lane];
         }
-        x[i] *= a.scale * back;
-        y[i] *= back;
-        test = fmaf(x[i], 0.f, fmaf(y[i], 0.f, test));
-      }
     }
-    uint64_t odd = odd_keys(test);
-    if (lane == 0) odds[wave] = odd;
-    __syncthreads();
-    odd = odds[0] | odds[1] | odds[2] | odds[3];
-    if (wave < C / 32 && there && !(odd >> (lane & 31) & 1)) {
-      store_block<T>(x, wave, dk_to + (int64_t)key * a.dk.token, half, a.dim);
-      store_block<T>(y, wave, dv_to + (int64_t)key * a.dv.token, half, a.dim);
-    }
-    if (wave == 0) plain_keys(odd);
-    return;
+    dk_sum[0] = x;
+    dv_sum[0] = y;
   }
+  const float back = kScaled<T> ? __builtin_amdgcn_exp2f(-up) : 1.f;
+  float test = 0.f;                                           // NaN where a result is not finite
 #pragma unroll
-  for (int m = 0; m < C / 32; ++m) {
-    dk[m] *= a.scale * back;
-    if constexpr (kScaled<T>) dv[m] *= back;
+  for (int m = 0; m < kBlocks; ++m) {
+    dk_sum[m] *= a.scale * back;
+    if constexpr (kScaled<T>) dv_sum[m] *= back;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) test = fmaf(dk[m][i], 0.f, fmaf(dv[m][i], 0.f, test));
+    for (int i = 0; i < 16; ++i) test = fmaf(dk_sum[m][i], 0.f, fmaf(dv_sum[m][i], 0.f, test));
   }
-  const uint64_t odd = odd_keys(test);
-  if (parts == 1) {
-    if (there && !(odd >> (lane & 31) & 1)) {
-      store_columns<T, C>(dk, dk_to + (int64_t)key * a.dk.token, half, a.dim);
-      store_columns<T, C>(dv, dv_to + (int64_t)key * a.dv.token, half, a.dim);
+  T* dk_to = (T*)rows_of(a.dk, ragged, b, sk.first, kv) + (int64_t)key * a.dk.token;
+  T* dv_to = (T*)rows_of(a.dv, ragged, b, sk.first, kv) + (int64_t)key * a.dv.token;
+  if constexpr (!kShare) {
+    if (wave < C / 32 && there) {
+      store_block<T>(dk_sum[0], wave, dk_to, half, a.dim);
+      store_block<T>(dv_sum[0], wave, dv_to, half, a.dim);
     }
-  } else if (!(odd >> (lane & 31) & 1)) {
-    float* to = part_to + (int64_t)(lane & 31) * a.dim;
+  } else if (parts == 1) {
+    if (there) {
+      store_columns<T, C>(dk_sum, dk_to, half, a.dim);
+      store_columns<T, C>(dv_sum, dv_to, half, a.dim);
+    }
+  } else {
+    // parts in the workspace: [sequence, head][item][dk, dv][key][dim]; items of tiles in one part have no place there
+    float* to = a.parts + part_place(a, tiles, ((int64_t)b * a.kv_heads + kv), tile, part) * 2 * kKeyTile * a.dim + (int64_t)(key - first) * a.dim;
 #pragma unroll
     for (int m = 0; m < C / 32; ++m)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int d = 32 * m + 2 * i + 4 * half;
         if (d < a.dim) {
-          *(f32x4*)(to + d) = f32x4{dk[m][i], dk[m][i + 1], dk[m][i + 2], dk[m][i + 3]};
-          *(f32x4*)(to + kKeyTile * a.dim + d) = f32x4{dv[m][i], dv[m][i + 1], dv[m][i + 2], dv[m][i + 3]};
+          *(f32x4*)(to + d) = f32x4{dk_sum[m][i], dk_sum[m][i + 1], dk_sum[m][i + 2], dk_sum[m][i + 3]};
+          *(f32x4*)(to + kKeyTile * a.dim + d) = f32x4{dv_sum[m][i], dv_sum[m][i + 1], dv_sum[m][i + 2], dv_sum[m][i + 3]};
         }
       }
   }
-  plain_keys(odd);
+  return there && test != test;
+}
+
+template <typename T, int C, bool kShare>
+__global__ __launch_bounds__(256, kShare ? (C <= 64 ? 3 : 2) : 1) void attention_dkv_kernel(AttentionArgs a, int tiles) {
+  using Room = KeyRoom<C, kShare>;
+  __shared__ __align__(1024) unsigned char smem[Room::kAll];
+  const bool again = dkv_pass<T, C, kShare, false>(a, tiles, smem, threadIdx.x);
+  if (__builtin_expect(any_wave(again, (lds_byte*)smem + Room::kFlagsAt), 0)) {
+    dkv_pass<T, C, kShare, true>(arguments(), tiles, smem, here((int)threadIdx.x));   // (nothing is kept in registers for this)
+  }
 }
 
 // Adds up the parts of tiles that were cut, eight columns of a key per thread, dk and dv.  Bound by the parts: 47 MB in 9 us (2 x 1531 tokens, 12/2 heads of 96).

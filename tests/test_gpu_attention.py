@@ -782,3 +782,85 @@ def test_values_that_are_not_finite_cost_one_pass_more(torch, Attention, heads, 
     v[0, 1000, :, 5] = math.inf                                   # seen by some
     some = time_of(torch, lambda: op.forward(q, k, v))
     assert max(every, some) <= 12 * plain + 50, (plain, every, some)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,heads,kv,dim,window,sinks", [(300, 2, 1, 64, 50, 4), (300, 60, 20, 96, 0, 0), (1500, 4, 2, 128, 150, 4), (2100, 8, 2, 64, 0, 0), (1100, 16, 16, 64, 300, 3),
+                                                         (900, 96, 32, 128, 256, 70)])
+def test_gradients_next_to_what_is_not_finite(torch, Attention, dtype, n, heads, kv, dim, window, sinks):
+    """As for 300 tokens above, at sizes at which tiles are seen whole, cut into parts, shared by four wavefronts or by none."""
+    q, d_o = (normal(torch, s, dtype, n, heads, dim, by=b) for s, b in ((1, 0.5), (4, 1.0)))
+    k, v = (normal(torch, s, dtype, n, kv, dim) for s in (2, 3))
+    op, at, group = Attention(window, sinks), n // 2, heads // kv
+    seen = oracle.visible(n, n, window, sinks, "cuda")
+    want = [oracle.attention(q[:, h], k[:, -1], v[:, -1], window, sinks, d_o=d_o[:, h]) for h in range(heads - group, heads)]   # of the last key head
+
+    bad_k, bad_v = k.clone(), v.clone()
+    bad_k[at], bad_v[at + 1] = math.nan, math.inf
+    got = run(torch, op, q[None], bad_k[None], bad_v[None], d_o[None])
+    blind = ~seen[:, at] & ~seen[:, at + 1]
+    assert int(blind.sum()) >= n // 2
+    within(torch, "dq", got["dq"][0, :, -1][blind], want[-1][0]["dq"][blind], want[-1][1]["dq"][blind])
+    # (rows that see the infinite value have dS = NaN and the key's gradients with them; the rows that see the NaN key are NaN throughout)
+    assert bool(torch.isnan(got["dq"][0, :, -1][~blind]).all())
+
+    bad_do = d_o.clone()
+    bad_do[at, :, 3], bad_do[at + 5, :, 3], bad_do[at, :, 6], bad_do[n - 1, :, dim - 1] = math.inf, math.inf, -math.inf, math.nan
+    got = run(torch, op, q[None], k[None], v[None], bad_do[None])
+    total, bound = (sum(w[i]["dv"] for w in want) for i in (0, 1))
+    bound = bound + oracle.UNIT[q.dtype] * total.abs()
+    dv = got["dv"][0, :, -1]
+    plain = [d for d in range(dim) if d not in (3, 6, dim - 1)]
+    within(torch, "dv", dv[:, plain], total[:, plain], bound[:, plain])
+    for d, rows in ((3, [at, at + 5]), (6, [at]), (dim - 1, [n - 1])):
+        odd = seen[rows].any(0)
+        assert torch.equal(torch.isfinite(dv[:, d]), ~odd), d
+        within(torch, f"dv, column {d}", dv[~odd][:, d], total[~odd][:, d], bound[~odd][:, d])
+    bad = seen[[at, at + 5, n - 1]].any(0)
+    total, bound = (sum(w[i]["dk"] for w in want) for i in (0, 1))
+    bound = bound + oracle.UNIT[q.dtype] * total.abs()
+    dk = got["dk"][0, :, -1]
+    within(torch, "dk", dk[~bad], total[~bad], bound[~bad])
+    assert not bool(torch.isfinite(dk[bad]).any())
+
+
+@pytest.mark.parametrize("queries,heads,kv,dim,window,sinks", [(200, 2, 1, 64, 0, 0), (200, 2, 1, 128, 40, 2), (300, 60, 20, 64, 0, 0), (300, 90, 30, 96, 60, 3), (40, 4, 4, 64, 0, 0)])
+def test_gradients_of_scores_beyond_float16(torch, Attention, queries, heads, kv, dim, window, sinks):
+    """P (dP - D) of more than 65,504, where the results are not."""
+    q = normal(torch, 1, "float16", queries, heads, dim)
+    k, v = (normal(torch, s, "float16", queries, kv, dim, by=b) for s, b in ((2, 0.25), (3, 12000.0)))
+    v = v.clamp(-60000.0, 60000.0)
+    d_o = torch.where(normal(torch, 4, "float16", queries, heads, dim) < 0, -1.9, 1.9).half()
+    scale = 2.0 ** -4
+    got = run(torch, Attention(window, sinks, scale), q[None], k[None], v[None], d_o[None])
+    got = {n: t[0] for n, t in got.items()}
+    seen, group = oracle.visible(queries, queries, window, sinks, "cuda"), heads // kv
+
+    def largest(h):
+        """|dS| of a head."""
+        g = d_o[:, h].double()
+        p = torch.exp(q[:, h].double() @ k[:, h // group].double().T * scale - got["lse"][h].double()[:, None]) * seen
+        return float((p * (g @ v[:, h // group].double().T - (g * got["o"][:, h].double()).sum(-1, keepdim=True))).abs().max())
+
+    most = [largest(h) for h in range(heads)]
+    assert max(most) > 70000, max(most)
+    for g in sorted({0, kv // 2, kv - 1, most.index(max(most)) // group}):
+        of, at = slice(g * group, (g + 1) * group), slice(g, g + 1)
+        part = {n: got[n][:, of] for n in ("o", "dq")} | {n: got[n][:, at] for n in ("dk", "dv")} | {"lse": got["lse"][of]}
+        check_sequence(torch, part, q[:, of], k[:, at], v[:, at], window, sinks, scale, d_o[:, of])
+
+
+@pytest.mark.parametrize("heads,dim,window", [(8, 64, 0), (8, 128, 1024), (32, 64, 0)])
+def test_gradients_that_are_not_finite_cost_one_pass_more(torch, Attention, heads, dim, window):
+    """As the forward call: three to six times a call, 12 is room for clocks."""
+    q, k, v, d_o = (normal(torch, s, "float16", 1, 4096, heads, dim) for s in (1, 2, 3, 4))
+    op = Attention(window, 4)
+    o, lse = op.forward(q, k, v)
+    plain = time_of(torch, lambda: op.backward(d_o, q, k, v, o, lse))
+    d_o[0, 2000, :, 5] = math.inf                                 # what float16 training with a scaled loss meets
+    one = time_of(torch, lambda: op.backward(d_o, q, k, v, o, lse))
+    d_o[0, 2000, :, 5] = 0
+    v[0, 2, :, 1] = math.inf
+    o, lse = op.forward(q, k, v)
+    value = time_of(torch, lambda: op.backward(d_o, q, k, v, o, lse))
+    assert max(one, value) <= 12 * plain + 50, (plain, one, value)
