@@ -185,3 +185,37 @@ def test_one_id_without_dimensions(torch, Embedding, dtype):
     assert torch.equal(op.backward(dY, ids, dtype=torch.float32), want.float())
     with pytest.raises(ValueError, match="dY"):
         op.backward(dY[0], ids)
+
+
+@pytest.mark.parametrize("n", [65_535, 65_536, 65_537, 200_000, 600_001])
+@pytest.mark.parametrize("rows", [300, 32_000, 70_000, 300_000])
+@pytest.mark.parametrize("kind", ["one", "text", "even"])
+def test_many_tokens(torch, Embedding, n, rows, kind):
+    """Around the number of tokens from which a digit is sorted by three kernels, with ids of one to three digits, and so many that chunks of the sums are longer."""
+    dY, ids = normal(torch, 2, "float32", n, 12), tokens(torch, 3, n, rows, kind)
+    op = Embedding(rows)
+    got = op.backward(dY, ids, torch.full((rows, 12), math.nan, device="cuda"))
+    check_grad(torch, got.cpu(), dY.cpu(), ids.cpu(), rows, 1.0)     # (there: additions of 64 bits to one row contend on a GPU)
+    assert torch.equal(got, op.backward(dY, ids.int()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_tokens_of_wide_rows(torch, Embedding, dtype):
+    rows, n, columns = 5003, 70_001, 1030
+    dY, ids = normal(torch, 2, dtype, n, columns), tokens(torch, 3, n, rows, "text")
+    check_grad(torch, Embedding(rows, 0.5).backward(dY, ids).cpu(), dY.cpu(), ids.cpu(), rows, 0.5)
+
+
+def test_many_tokens_captured(torch, Embedding):
+    rows, n, columns = 40_000, 100_000, 64
+    op = Embedding(rows)
+    dY, ids = normal(torch, 2, "bfloat16", n, columns), tokens(torch, 3, n, rows, "text")
+    op.backward(dY, ids)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dW = op.backward(dY, ids)
+    for seed in (5, 6, 7):
+        ids.copy_(tokens(torch, seed, n, rows, "text"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dW, op.backward(dY, ids))
