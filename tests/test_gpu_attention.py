@@ -864,3 +864,35 @@ def test_gradients_that_are_not_finite_cost_one_pass_more(torch, Attention, head
     o, lse = op.forward(q, k, v)
     value = time_of(torch, lambda: op.backward(d_o, q, k, v, o, lse))
     assert max(one, value) <= 12 * plain + 50, (plain, one, value)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [64, 96, 128])
+@pytest.mark.parametrize("heads,kv", [(4, 2), (8, 4)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 70), (64, 0)])
+def test_long_ragged_batches(torch, Attention, dtype, dim, heads, kv, window, sinks):
+    """Thousands of tokens: workgroups of 64 and of 128 queries and of 128 keys, tiles of keys cut into parts, and sequences without queries, with one, with more
+    queries than keys and the other way round."""
+    import ctypes
+    from paper_2307_05740_amd.binding import lib
+    lengths, keys = [1500, 0, 1, 777, 64, 1031], [1500, 20, 1, 900, 33, 1159]
+    nq, nk = sum(lengths) + 7, sum(keys) + 3
+    q, d_o = (normal(torch, s, dtype, nq, heads, dim) for s in (1, 4))
+    k, v = (normal(torch, s, dtype, nk, kv, dim) for s in (2, 3))
+    ragged = {n: torch.tensor([sum(x[:i]) for i in range(len(x) + 1)], dtype=torch.int32, device="cuda") for n, x in (("q_offsets", lengths), ("k_offsets", keys))}
+    ragged.update(q_len=1500, k_len=1500)
+    op = Attention(window, sinks)
+    if sinks or (window == 0 and kv == 2):                       # (sums of parts are 128 keys of dk and dv in 32 bits)
+        a = op._describe(q, k, v, **ragged)
+        assert lib().arrow_attention_workspace_bytes(ctypes.byref(a)) > 8 * nq * heads + 8 * 128 * dim, "no tile of keys is cut"
+    got = run(torch, op, q, k, v, d_o, **ragged)
+    a = b = 0
+    for n, m in zip(lengths, keys):
+        one = {x: got[x][a:a + n] for x in ("o", "dq")}
+        one.update({x: got[x][b:b + m] for x in ("dk", "dv")}, lse=got["lse"][:, a:a + n])
+        check_sequence(torch, one, q[a:a + n], k[b:b + m], v[b:b + m], window, sinks, d_o=d_o[a:a + n])
+        a, b = a + n, b + m
+    assert bool(got["o"][a:].isnan().all()) and bool(got["dq"][a:].isnan().all()) and bool(got["dk"][b:].isnan().all()), "no sequence's"
+    again = run(torch, op, q, k, v, d_o, **ragged)
+    assert torch.equal(got["lse"][:, :a], again["lse"][:, :a])   # (what lies behind is not written)
+    assert all(torch.equal(got[n].view(torch.int16), again[n].view(torch.int16)) for n in ("o", "dq", "dk", "dv"))
