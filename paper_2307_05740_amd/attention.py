@@ -120,7 +120,8 @@ class ArrowAttention:
 
     def forward(self, q, k, v, o=None, lse=None, q_offsets=None, k_offsets=None, q_len=None, k_len=None):
         """``(o, lse)``.  q: (batch, tokens, heads, dim), k and v: (batch, keys, key heads, dim); or, with int32 offsets of
-        batch + 1 values each, (tokens of all sequences, heads, dim), of which no sequence has more than q_len (k_len).
+        batch + 1 values each, (tokens of all sequences, heads, dim), of which no sequence has more than q_len (k_len); without these the work, and the
+        gradients' workspace, are laid out as if each sequence might have all tokens.
         lse: float32, (batch, heads, tokens), or (heads, tokens of all sequences).  Results of tokens that no sequence has are not written."""
         if self._call is not None:
             done = self._call.attention_forward(*self._forward, q, k, v, o, lse, q_offsets, k_offsets, q_len, k_len)

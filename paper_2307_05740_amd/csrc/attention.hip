@@ -9,7 +9,8 @@
 //
 // What bounds it: with heads of 128, matrix instructions and the vector instructions between them (one exponential, one addition, one maximum, one
 // multiply-add and half a conversion per score), at the clock that the card's power leaves: 16,384 tokens, 16/2 heads, window of 4096, 490 us = 985 TFLOP/s,
-// where a large matrix product reaches 1312.  With heads of 64 the vector instructions: 4 x 2048, 16 heads, window of 512, 33 us = 460 TFLOP/s.  Tiles
+// where a large matrix product reaches 1312.  With heads of 64 how few wavefronts have work: 4 x 2048, 16 heads, window of 512, 30 us = 500 TFLOP/s, 2.3 wavefronts to a SIMD, whose
+// chains of products, maximum, exponentials and products cover each other so far that vector instructions issue in 46 % of the cycles and matrix units run in 20 %.  Tiles
 // of 64 keys, because two of keys and two of values (64 KiB) leave room for two workgroups on a compute unit, and each wavefront then has two
 // independent chains of products; 32 queries to a wavefront, because scores, sums and queries of 64 would not fit 256 registers.
 #include <algorithm>
@@ -40,7 +41,7 @@ int query_groups(int64_t blocks, int64_t heads, const AttentionArgs& a) {
   return blocks <= (a.dim <= 64 ? 512 : a.window == 0 && seen >= 1000 ? 384 : 256) ? 2 : 4;
 }
 
-// kGroups: how many groups of 32 queries the four wavefronts have.
+// kGroups: how many groups of 32 queries the four wavefronts have.  (Four workgroups to a compute unit for heads of 64, 128 registers: so many the first pass takes.)
 template <typename T, int C, int kGroups>
 __global__ __launch_bounds__(256, kGroups > 1 ? (C <= 64 ? 4 : 2) : 1) void attention_forward_kernel(AttentionArgs a, int tiles) {
   constexpr int D = columns_of_tile(C);
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? (C <= 64 ? 4 : 2) : 1) void atte
 
   // Matrix instructions multiply what a query does not see by a probability of 0, and that is no zero where a value there is infinite or NaN.  Where a result is not finite though
   // its row's sum is (so the pass says), the workgroup goes through its tiles again, with care: such values count for those who see them alone.  16,384 tokens, 16/2 heads of
-  // 128, window of 4096: 475 us with finite values, 1580 with an infinity that a quarter of the rows see, 2950 where all see one.
+  // 128, window of 4096: 490 us with finite values, 1780 with an infinity that a quarter of the rows see, 3280 where all see one.
   auto pass = [&](auto is_careful) -> bool {
     constexpr bool kCareful = decltype(is_careful)::value;
     constexpr int kNow = kCareful ? 32 : kMine;                 // keys at a time

@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_decode_join_kernel(Cach
   *(x2<T>*)((T*)a.o.at + b * a.o.sequence + head * a.o.head + d) = r;
 }
 
-// One piece of 16 bytes per thread.
+// One piece of 16 bytes per thread.  Bound by memory: 8 prompts of 2048 tokens, 8 heads of 128, 22 us = 6.2 TB/s (what was just written comes out of the caches; a copy: 5.1).
 template <typename T>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheArgs a) {
   const arrow_cache_t& c = a.c;

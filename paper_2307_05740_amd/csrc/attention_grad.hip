@@ -50,8 +50,8 @@ __device__ __forceinline__ int64_t groups_at(const AttentionArgs& a, bool ragged
 // (dq of 5 keys off by 1.55 times what rounding dq alone does, and 1.4 so; for long rows the same, and 15 % of the kernel's time).
 //
 // What bounds it: matrix instructions (four products) and the vector instructions between them, at the clock that the power leaves: 8192 tokens, 32/8 heads of
-// 128, window of 2048, 470 us = 1030 TFLOP/s with the product P K, matrix units busy 55 % of the cycles.  Heads of more than 64 leave no registers for the queries, which
-// are read from LDS again and again, and tiles of 32 keys; of 64, 4 x 2048 tokens, window of 512: 57 us.
+// 128, window of 2048, 445 us = 1090 TFLOP/s with the product P K, matrix units busy 55 % of the cycles.  Heads of more than 64 leave no registers for the queries, which
+// are read from LDS again and again, and tiles of 32 keys; of 64, 4 x 2048 tokens, window of 512: 52 us, 1.5 wavefronts to a SIMD.
 //
 // kGroups: as in the forward kernel, how many groups of 32 queries the four wavefronts have.
 template <typename T, int C, int kGroups>
@@ -312,8 +312,8 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
 //
 // kShare: wavefronts of 32 keys each share steps, or have the same 32 and every fourth step; tiles are in one part then.
 //
-// What bounds it: as the dq kernel; of 256 registers 128 are sums (heads of 128), so the keys are read from LDS as the queries are there.  8192 tokens, as above: 530 us = 910
-// TFLOP/s, matrix units busy 45 %, LDS 34 % of the cycles; 4 x 2048: 61 us.  The queries come from behind the L2 (1.6 GB); another order of them, in which
+// What bounds it: as the dq kernel; of 256 registers 128 are sums (heads of 128), so the keys are read from LDS as the queries are there.  8192 tokens, as above: 490 us = 980
+// TFLOP/s, matrix units busy 45 %, LDS 34 % of the cycles; 4 x 2048: 55 us, 1.8 wavefronts to a SIMD.  The queries come from behind the L2 (1.7 GB); another order of them, in which
 // workgroups of a die read the same ones, took as long.
 //
 // Twice where a result is not finite, as in the dq kernel: the second time (kCareful) elements of queries and of gradients that are not finite are taken out of the products and

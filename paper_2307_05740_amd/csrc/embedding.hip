@@ -114,7 +114,8 @@ __global__ __launch_bounds__(64) void sort_count_kernel(SortArgs s) {
   for (int i = lane; i < values; i += 64) s.counts[i * s.blocks + blockIdx.x] = n[i];
 }
 
-// Exclusive sums of all counts, in place, one workgroup.
+// Exclusive sums of all counts, in place, one workgroup, each thread a stretch of its own: 131,072 tokens of 32,000 rows, 131,072 counts a digit, 218 us, twice, where the kernels before and
+// after it take 5 and 8 and the sums 284.
 __global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t* counts, int64_t n) {
   __shared__ uint32_t sums[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
