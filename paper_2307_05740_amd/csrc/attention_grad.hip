@@ -12,7 +12,7 @@ namespace arrow {
 namespace {
 
 // float16 holds nothing below 2^-24, and whole numbers of 2^-24 below 2^-14, which the P and dS of long rows and small gradients do not stay above.  So dS (and P
-// in the dk, dv kernel) are rounded as multiples of a power of two, by the size of d_o: of a row in the dq kernel, of all rows that a key tile's
+// in the dk, dv kernel) are rounded as multiples of a power of two, by the size of d_o where that is below 1: of a row in the dq kernel, of all rows that a key tile's
 // queries are among in the other one, which takes those from the dq kernel's notes, one for 32 queries.
 template <typename T> constexpr bool kScaled = std::is_same<T, _Float16>::value;
 __device__ __forceinline__ float finite_size(float x) { return fabsf(x) < __builtin_inff() ? fabsf(x) : 0.f; }
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256, kGroups > 1 ? 2 : 1) void attention_dq_kernel(
   float larger = 1.f;                                            // that d_o of this row is multiplied by, and taken out of the result again
   if constexpr (kScaled<T>) {
     most = max_halves(most);
-    larger = unit_of(most);
+    larger = fmaxf(unit_of(most), 1.f);                          // (never less: what is small beside the largest may be all that counts)
     delta *= larger;
 #pragma unroll
     for (int s = 0; s < C / 16; ++s)

@@ -896,3 +896,13 @@ def test_long_ragged_batches(torch, Attention, dtype, dim, heads, kv, window, si
     again = run(torch, op, q, k, v, d_o, **ragged)
     assert torch.equal(got["lse"][:, :a], again["lse"][:, :a])   # (what lies behind is not written)
     assert all(torch.equal(got[n].view(torch.int16), again[n].view(torch.int16)) for n in ("o", "dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("queries,heads,kv,window", [(700, 2, 1, 0), (700, 24, 8, 200)])
+def test_gradients_of_o_with_a_large_column(torch, Attention, queries, heads, kv, window):
+    """A column of d_o that is large where the values have nothing: the others keep float16's precision."""
+    q, d_o = (normal(torch, s, "float16", queries, heads, 64, by=b) for s, b in ((1, 1.0), (4, 0.3)))
+    k, v = (normal(torch, s, "float16", queries, kv, 64) for s in (2, 3))
+    d_o[..., 5], v[..., 5] = 30000.0, 0.0
+    got = run(torch, Attention(window, 3), q[None], k[None], v[None], d_o[None])
+    check_norms(torch, {n: t[0] for n, t in got.items()}, q, k, v, window, 3, d_o)
