@@ -288,7 +288,7 @@ def _kernels(s):
     if c["top"]:
         out.update(top_logp=r.top_logp, top_ids=r.top_ids)
     if c["op"] == "loss":
-        out["d_logits"] = op.backward(s["d_logp"], s["d_entropy"], s["logits"], s["targets"], r.lse, r.entropy)
+        out["d_logits"] = op.backward(s["d_logp"], s["d_entropy"], s["logits"], s["targets"], r.stats, r.entropy)
     return out
 
 
