@@ -32,7 +32,9 @@ ORACLE_LIB = os.path.join(REPO_DIR, "oracle", "liboracle.so")
 HIP_SOURCES = ["csrc/decompose.cpp", "csrc/layout.cpp", "csrc/abi.cpp", "csrc/kernels.hip", "csrc/sddmm.hip",
                "csrc/csf3.cpp", "csrc/mttkrp.hip", "csrc/probe.hip", "csrc/static_scratch.hip",
                "csrc/attention.cpp", "csrc/attention.hip", "csrc/attention_grad.hip", "csrc/attention_decode.hip",
-               "csrc/embedding.cpp", "csrc/embedding.hip"]
+               "csrc/embedding.cpp", "csrc/embedding.hip",
+               "csrc/rotation.cpp", "csrc/rotation.hip", "csrc/pages.cpp", "csrc/pages.hip",
+               "csrc/packed.cpp", "csrc/packed.hip", "csrc/logprobs.cpp", "csrc/logprobs.hip"]
 
 
 def _run(cmd: list[str]) -> None:

@@ -35,6 +35,10 @@ EXPORTED = [
     "arrow_attention_forward", "arrow_attention_forward_split_bytes", "arrow_attention_forward_split", "arrow_attention_workspace_bytes", "arrow_attention_backward", "arrow_cache_append",
     "arrow_attention_decode_workspace_bytes", "arrow_attention_decode",
     "arrow_embedding_forward", "arrow_embedding_workspace_bytes", "arrow_embedding_backward",
+    "arrow_rotation_forward", "arrow_rotation_workspace_bytes", "arrow_rotation_backward",
+    "arrow_pages_workspace_bytes", "arrow_pages_step",
+    "arrow_packed_append", "arrow_packed_read", "arrow_packed_decode_workspace_bytes", "arrow_packed_decode",
+    "arrow_logprobs_workspace_bytes", "arrow_logprobs_forward", "arrow_logprobs_backward",
 ]
 
 
@@ -115,6 +119,31 @@ class arrow_cache_t(ctypes.Structure):
 class arrow_embedding_t(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "grad_dtype", "id_bytes", "columns")] + \
                [(name, ctypes.c_int64) for name in ("rows", "tokens", "w_stride", "y_stride")] + [("scale", ctypes.c_float)]
+
+
+class arrow_rotation_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("dtype", "weight_dtype", "batch", "tokens", "q_heads", "kv_heads", "dim", "rotary", "interleaved")] + \
+               [("eps", ctypes.c_float), ("position_bytes", ctypes.c_int32), ("positions", ctypes.c_void_p), ("shift", ctypes.c_int64),
+                ("turns", ctypes.c_void_p)] + \
+               [(name, arrow_strides_t) for name in ("q", "k", "q_out", "k_out", "dq", "dk")]
+
+
+class arrow_pages_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "columns", "page", "window", "sinks", "tokens")] + \
+               [("pages", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("rows", ctypes.c_int64)]
+
+
+class arrow_packed_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "batch", "q_heads", "kv_heads", "dim", "window", "sinks")] + \
+               [("scale", ctypes.c_float), ("page", ctypes.c_int32), ("columns", ctypes.c_int32)] + \
+               [(name, ctypes.c_int64) for name in ("pages", "max_len", "page_step", "head_step")] + \
+               [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
+
+
+class arrow_logprobs_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "target_bytes", "top", "vocabulary")] + \
+               [(name, ctypes.c_int64) for name in ("rows", "stride", "d_stride")] + [("scale", ctypes.c_float)]
 
 
 def lib():
@@ -239,6 +268,21 @@ def lib():
     L.arrow_embedding_workspace_bytes.argtypes = [embedding]
     L.arrow_embedding_backward.restype = ctypes.c_int
     L.arrow_embedding_backward.argtypes = [embedding, vp, vp, vp, vp, sz, vp]
+    rotation, pages, packed, logprobs = (ctypes.POINTER(t) for t in (arrow_rotation_t, arrow_pages_t, arrow_packed_t, arrow_logprobs_t))
+    for name, result, arguments in (
+            ("arrow_rotation_forward", ctypes.c_int, [rotation] + [vp] * 7),
+            ("arrow_rotation_workspace_bytes", sz, [rotation]),
+            ("arrow_rotation_backward", ctypes.c_int, [rotation] + [vp] * 11 + [sz, vp]),
+            ("arrow_pages_workspace_bytes", sz, [pages]),
+            ("arrow_pages_step", ctypes.c_int, [pages] + [vp] * 6 + [sz, vp]),
+            ("arrow_packed_append", ctypes.c_int, [packed, i64, vp, vp, st, st, vp, vp, vp]),
+            ("arrow_packed_read", ctypes.c_int, [packed, i64, vp, vp, vp, vp, st, st, vp]),
+            ("arrow_packed_decode_workspace_bytes", sz, [packed]),
+            ("arrow_packed_decode", ctypes.c_int, [packed, vp, st, vp, vp, st, st, vp, vp, st, vp, sz, vp]),
+            ("arrow_logprobs_workspace_bytes", sz, [logprobs]),
+            ("arrow_logprobs_forward", ctypes.c_int, [logprobs] + [vp] * 9 + [sz, vp]),
+            ("arrow_logprobs_backward", ctypes.c_int, [logprobs] + [vp] * 8)):
+        getattr(L, name).restype, getattr(L, name).argtypes = result, arguments
     _lib = L
     return L
 

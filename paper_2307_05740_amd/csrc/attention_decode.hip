@@ -290,6 +290,13 @@ int decode(const CacheArgs& a, void* stream) {
 
 int launch_attention_decode(const CacheArgs& a, void* stream) { return a.c.dtype == ARROW_BF16 ? decode<__bf16>(a, stream) : decode<_Float16>(a, stream); }
 
+int launch_attention_decode_join(const CacheArgs& a, void* stream) {
+  const dim3 rows((unsigned)(a.c.batch * a.c.q_heads)), threads(64 * kWaves);
+  if (a.c.dtype == ARROW_BF16) attention_decode_join_kernel<__bf16><<<rows, threads, 0, (hipStream_t)stream>>>(a);
+  else attention_decode_join_kernel<_Float16><<<rows, threads, 0, (hipStream_t)stream>>>(a);
+  return (int)hipGetLastError();
+}
+
 int launch_cache_append(const CacheArgs& a, void* stream) {
   const int64_t blocks = ((int64_t)a.c.batch * a.tokens * a.c.kv_heads * (a.c.dim / 8) + 255) / 256;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;

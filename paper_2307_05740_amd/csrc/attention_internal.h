@@ -51,6 +51,7 @@ int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream
 int launch_attention_backward(const AttentionArgs& a, int32_t dtype, void* stream);
 int launch_cache_append(const CacheArgs& a, void* stream);
 int launch_attention_decode(const CacheArgs& a, void* stream);
+int launch_attention_decode_join(const CacheArgs& a, void* stream);   // the second of its kernels: c.dtype, batch, q_heads and dim, o, splits and parts
 
 constexpr int kQueryTile = 128;    // queries of a workgroup, forward and dq
 constexpr int kKeyTile = 128;      // keys of a workgroup, dk and dv

@@ -1,0 +1,452 @@
+// Log probabilities of given tokens, entropies, most likely tokens, and the gradient (include/arrow_logprobs.h).
+//
+// What bounds it is memory: the logits are read once (backward: read and written).  A workgroup holds a part of a row in its registers, so that the
+// maximum, the sums relative to it and the largest logits all come from one reading; a second kernel joins the parts of rows that were cut.
+//
+// The largest logits.  Value and index of a logit make one whole number, its key, so that no two are alike and the order is that of the results.  In each
+// wavefront the key that comes `top`-th among its lanes' largest ones is no larger than the `top`-th of all; the largest of the wavefronts' is the border.
+// The few pieces that reach it are read again, and their keys from it on go to a list in LDS, where each is placed by counting those before it.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "attention_common.h"
+#include "logprobs_internal.h"
+
+namespace arrow {
+namespace {
+
+constexpr int kThreads = kScoreThreads, kWaves = kThreads / 64;
+constexpr int kList = 1024;           // keys from the border on that a workgroup has room for
+constexpr float kLeast = -256.f;      // exponents of two below this are 0, and so is their product with it
+
+template <typename T> struct Piece;   // 16 bytes of a row
+template <> struct Piece<float> {
+  static constexpr int kEach = 4;
+  static constexpr uint32_t kNothing = 0xff800000u;
+  static __device__ __forceinline__ float get(const u32x4& r, int i) { return __uint_as_float(r[i]); }
+};
+template <> struct Piece<__bf16> {
+  static constexpr int kEach = 8;
+  static constexpr uint32_t kNothing = 0xff80ff80u;
+  static __device__ __forceinline__ float get(const u32x4& r, int i) { return __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16); }
+};
+template <> struct Piece<_Float16> {
+  static constexpr int kEach = 8;
+  static constexpr uint32_t kNothing = 0xfc00fc00u;
+  static __device__ __forceinline__ float get(const u32x4& r, int i) {
+    union { uint16_t u; _Float16 f; } x;
+    x.u = (uint16_t)(i & 1 ? r[i / 2] >> 16 : r[i / 2]);
+    return (float)x.f;
+  }
+};
+
+// The larger of two; NaN where one is.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// A row's elements: those before the first address that is a multiple of 16, whole pieces, and the rest.
+template <typename T>
+struct Row {
+  const T* at;
+  int head, pieces, rest;
+  __device__ __forceinline__ Row(const T* row, int n) {
+    constexpr int kEach = Piece<T>::kEach;
+    const int off = (int)(((uintptr_t)row & 15) / sizeof(T));
+    at = row;
+    head = off ? min(kEach - off, n) : 0;
+    pieces = (n - head) / kEach;
+    rest = (n - head) % kEach;
+  }
+  __device__ __forceinline__ const u32x4* piece(int i) const { return (const u32x4*)(at + head + (int64_t)i * Piece<T>::kEach); }
+  __device__ __forceinline__ int index(int piece, int i) const { return head + piece * Piece<T>::kEach + i; }
+  // the element beside the pieces that lane `tid` of the first part has, -1: none
+  __device__ __forceinline__ int edge(int tid, int n) const { return tid < head ? tid : tid >= 8 && tid < 8 + rest ? n - rest + tid - 8 : -1; }
+};
+
+// Sums relative to the largest logit: with d = (x - M) scale in exponents of two, s = sum 2^d, w = sum 2^d d.  (The difference comes before the product, so that
+// logits of any size, the type's lowest ones among them, are as exact as they are near to each other.)
+struct Sums {
+  float M, s, w;
+  __device__ __forceinline__ void raise(float to, float c) {       // (to >= M, or NaN)
+    const float d = fmaxf((M - to) * c, kLeast), by = __builtin_amdgcn_exp2f(d);
+    w = by * fmaf(s, d, w);
+    s *= by;
+    M = to;
+  }
+  __device__ __forceinline__ void add(Sums o, float c) {
+    const float to = larger(M, o.M);
+    raise(to, c);
+    o.raise(to, c);
+    s += o.s;
+    w += o.w;
+  }
+};
+
+__device__ __forceinline__ Sums exchanged(const Sums& x, int mask) { return {__shfl_xor(x.M, mask, 64), __shfl_xor(x.s, mask, 64), __shfl_xor(x.w, mask, 64)}; }
+
+// Results of a row from its sums.
+struct Stats {
+  float M, log, entropy;                                           // log: of sum exp(scale (x - M))
+  __device__ __forceinline__ explicit Stats(const Sums& x) : M(x.M) {
+    if (M == minus_infinity()) {
+      log = entropy = 0.f;
+    } else if (!(M < __builtin_inff())) {
+      log = entropy = __builtin_nanf("");
+    } else {
+      const float two = __builtin_amdgcn_logf(x.s);                // (base 2)
+      log = two * kLn2;
+      entropy = (two - x.w / x.s) * kLn2;
+    }
+  }
+  __device__ __forceinline__ float lse(float scale) const { return fmaf(M, scale, log); }
+  __device__ __forceinline__ float of(float logit, float scale) const { return M == minus_infinity() ? M : fmaf(logit - M, scale, -log); }
+};
+
+// Larger logits have larger keys, and of equal ones those of lower indices; 0 is none's.
+__device__ __forceinline__ uint64_t key_of(float x, int index) {
+  uint32_t u = __float_as_uint(x + 0.f);                     // (-0 is 0)
+  u = x != x ? 0xffffffffu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return (uint64_t)u << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return u == 0xffffffffu ? __builtin_nanf("") : __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
+// How many lanes' keys are larger than this one's.
+__device__ __forceinline__ int lanes_before(uint64_t key) {
+  int n = 0;
+#pragma unroll 8
+  for (int i = 0; i < 64; ++i) {
+    const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, i);
+    n += other > key;
+  }
+  return n;
+}
+
+struct Chosen {
+  uint64_t list[kList];
+  uint64_t border[kWaves];
+  uint64_t most[kWaves];
+  int count;
+};
+
+// The border from every lane's largest key (0: it has none); all threads of the workgroup.
+__device__ __forceinline__ uint64_t border_of(uint64_t key, int top, Chosen& c) {
+  if (threadIdx.x == 0) c.count = 0;
+  const uint64_t at = __ballot(lanes_before(key) == top - 1);   // (several lanes without a key have the same place, or none has it)
+  if ((threadIdx.x & 63) == 0) c.border[threadIdx.x >> 6] = 0;
+  if (at && (int)(threadIdx.x & 63) == __builtin_ctzll(at)) c.border[threadIdx.x >> 6] = key;
+  __syncthreads();
+  uint64_t b = c.border[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) b = c.border[w] > b ? c.border[w] : b;
+  return b;
+}
+
+__device__ __forceinline__ void put(uint64_t key, uint64_t border, Chosen& c) {
+  if (key == 0 || key < border) return;
+  const int at = atomicAdd(&c.count, 1);                     // (the order in the list does not matter)
+  if (at < kList) c.list[at] = key;
+}
+
+// The `top` largest keys to out(place, key); where there are fewer, the places behind them get 0.  Where the list has no room, the largest key below the last one is
+// looked for `top` times: below(key) is this thread's largest one.
+template <typename Out, typename Below>
+__device__ __forceinline__ void place(int top, Chosen& c, Out&& out, Below&& below) {
+  __syncthreads();
+  const int n = c.count;
+  if (n <= kList) {
+    for (int i = threadIdx.x; i < max(n, top); i += kThreads) {
+      if (i >= n) { out(i, (uint64_t)0); continue; }
+      const uint64_t key = c.list[i];
+      int before = 0;
+      for (int j = 0; j < n; ++j) before += c.list[j] > key;
+      if (before < top) out(before, key);
+    }
+    return;
+  }
+  uint64_t last = ~(uint64_t)0;
+  for (int i = 0; i < top; ++i) {
+    uint64_t mine = below(last);
+    for (int m = 32; m; m >>= 1) {
+      const uint64_t other = __shfl_xor((unsigned long long)mine, m, 64);
+      mine = other > mine ? other : mine;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) c.most[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) mine = c.most[w] > mine ? c.most[w] : mine;
+    if (threadIdx.x == 0) out(i, mine);
+    last = mine;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ int64_t target_of(const ScoreArgs& p, int64_t row) {
+  return p.a.target_bytes == 4 ? (int64_t)((const int32_t*)p.targets)[row] : ((const int64_t*)p.targets)[row];
+}
+
+template <typename T>
+__device__ __forceinline__ void write_row(const ScoreArgs& p, int64_t row, const Stats& s) {
+  p.lse[row] = s.lse(p.a.scale);
+  p.entropy[row] = s.entropy;
+  *(float2*)(p.stats + 2 * row) = {s.M, s.log};
+  const int64_t t = target_of<T>(p, row);
+  p.logp[row] = t >= 0 && t < p.a.vocabulary ? s.of((float)((const T*)p.logits)[row * p.a.stride + t], p.a.scale) : 0.f;
+}
+
+__device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i, uint64_t key, const Stats& s) {
+  p.top_ids[row * p.a.top + i] = index_of(key);
+  p.top_logp[row * p.a.top + i] = s.of(value_of(key), p.a.scale);
+}
+
+template <typename T, int N, bool kTop>
+__global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
+  using P = Piece<T>;
+  __shared__ Sums waves[kWaves];
+  __shared__ std::conditional_t<kTop, Chosen, int> chosen;
+  const int tid = threadIdx.x, part = (int)(blockIdx.x % (unsigned)p.parts);
+  const int64_t row = blockIdx.x / (unsigned)p.parts;
+  const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
+  const int first = part * p.vectors, end = min(first + p.vectors, r.pieces);
+
+  u32x4 x[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = first + j * kThreads + tid;
+    x[j] = u32x4{P::kNothing, P::kNothing, P::kNothing, P::kNothing};
+    if (i < end) x[j] = *r.piece(i);
+  }
+  const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
+  const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity();
+
+  float most[N], all = beside;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    most[j] = P::get(x[j], 0);
+#pragma unroll
+    for (int i = 1; i < P::kEach; ++i) most[j] = larger(most[j], P::get(x[j], i));
+    all = larger(all, most[j]);
+  }
+  const float mine = all;
+  for (int m = 32; m; m >>= 1) all = larger(all, __shfl_xor(all, m, 64));
+  const float c = p.a.scale * kLog2e;
+  Sums sum{all, 0.f, 0.f};
+  auto count = [&](float v) {
+    const float d = fmaxf((v - sum.M) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
+    sum.s += e;
+    sum.w = fmaf(e, d, sum.w);
+  };
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < P::kEach; ++i) count(P::get(x[j], i));
+  count(beside);
+  for (int m = 32; m; m >>= 1) { sum.s += __shfl_xor(sum.s, m, 64); sum.w += __shfl_xor(sum.w, m, 64); }
+  if ((tid & 63) == 0) waves[tid >> 6] = sum;
+  __syncthreads();
+  sum = waves[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
+  if (p.parts > 1 && tid == 0) *(f32x4*)(p.sums + (row * p.parts + part) * 4) = f32x4{sum.M, sum.s, sum.w, 0.f};
+  const Stats s(sum);
+  if (p.parts == 1 && tid == 0) write_row<T>(p, row, s);
+
+  if constexpr (kTop) {
+    // the lane's largest key: its piece is read again for the index
+    uint64_t key = 0;
+    int at = -1;
+    const float sought = mine;
+    auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
+#pragma unroll
+    for (int j = N - 1; j >= 0; --j)
+      if (first + j * kThreads + tid < end && alike(most[j], sought)) at = first + j * kThreads + tid;
+    if (at >= 0) {
+      const u32x4 v = *r.piece(at);
+#pragma unroll
+      for (int i = P::kEach - 1; i >= 0; --i)
+        if (alike(P::get(v, i), sought)) key = key_of(sought, r.index(at, i));
+    }
+    if (edge >= 0) {
+      const uint64_t k = key_of(beside, edge);
+      key = k > key ? k : key;
+    }
+    const uint64_t border = border_of(key, p.a.top, chosen);
+    if (edge >= 0) put(key_of(beside, edge), border, chosen);
+    uint32_t near = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (first + j * kThreads + tid < end && key_of(most[j], 0) >= border) near |= 1u << j;
+    while (near) {
+      const int i = first + __builtin_ctz(near) * kThreads + tid;
+      near &= near - 1;
+      const u32x4 v = *r.piece(i);
+#pragma unroll
+      for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(i, e)), border, chosen);
+    }
+    place(
+        p.a.top, chosen,
+        [&](int i, uint64_t k) {
+          if (p.parts > 1) p.keys[(row * p.parts + part) * p.a.top + i] = k;
+          else write_top(p, row, i, k, s);
+        },
+        [&](uint64_t last) {
+          uint64_t best = 0;
+          auto look = [&](uint64_t k) { best = k < last && k > best ? k : best; };
+          if (edge >= 0) look(key_of(beside, edge));
+          for (int i = first + tid; i < end; i += kThreads) {
+            const u32x4 v = *r.piece(i);
+#pragma unroll
+            for (int e = 0; e < P::kEach; ++e) look(key_of(P::get(v, e), r.index(i, e)));
+          }
+          return best;
+        });
+  }
+}
+
+// The parts of a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
+  __shared__ Sums waves[kWaves];
+  __shared__ Chosen chosen;
+  const int tid = threadIdx.x, top = p.a.top;
+  const int64_t row = blockIdx.x;
+  const float c = p.a.scale * kLog2e;
+  Sums sum{minus_infinity(), 0.f, 0.f};
+  for (int i = tid; i < p.parts; i += kThreads) {
+    const f32x4 v = *(const f32x4*)(p.sums + (row * p.parts + i) * 4);
+    sum.add({v[0], v[1], v[2]}, c);
+  }
+  for (int m = 32; m; m >>= 1) sum.add(exchanged(sum, m), c);
+  if ((tid & 63) == 0) waves[tid >> 6] = sum;
+  __syncthreads();
+  sum = waves[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
+  const Stats s(sum);
+  if (tid == 0) write_row<T>(p, row, s);
+  if (top == 0) return;
+  const uint64_t* keys = p.keys + row * p.parts * top;
+  const int64_t n = (int64_t)p.parts * top;
+  uint64_t key = 0;
+  for (int i = tid; i < p.parts; i += kThreads) key = keys[(int64_t)i * top] > key ? keys[(int64_t)i * top] : key;
+  const uint64_t border = border_of(key, top, chosen);
+  for (int64_t i = tid; i < n; i += kThreads) put(keys[i], border, chosen);
+  place(
+      top, chosen, [&](int i, uint64_t k) { write_top(p, row, i, k, s); },
+      [&](uint64_t last) {
+        uint64_t best = 0;
+        for (int64_t i = tid; i < n; i += kThreads) best = keys[i] < last && keys[i] > best ? keys[i] : best;
+        return best;
+      });
+}
+
+template <typename T>
+__device__ __forceinline__ void put_value(u32x4& r, int i, float x) {
+  if constexpr (sizeof(T) == 4) {
+    r[i] = __float_as_uint(x);
+  } else {
+    union { T t; uint16_t u; } v;
+    v.t = (T)x;
+    r[i / 2] = i & 1 ? (r[i / 2] & 0xffffu) | (uint32_t)v.u << 16 : v.u;
+  }
+}
+
+constexpr int kGradPieces = 4;        // of a lane
+
+// Gradients: a wavefront has 256 pieces of a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int chunks) {
+  using P = Piece<T>;
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * kWaves + wave_id();
+  const int64_t row = id / chunks;
+  const int chunk = (int)(id - row * chunks);
+  if (row >= p.a.rows) return;
+  const T* in = (const T*)p.logits + row * p.a.stride;
+  T* out = (T*)p.d_logits + row * p.a.d_stride;
+  const int64_t target = target_of<T>(p, row);
+  const bool known = target >= 0 && target < p.a.vocabulary;
+  const int t = known ? (int)target : -1;
+  const float2 stats = *(const float2*)(p.stats + 2 * row);
+  const float most = stats.x, log = stats.y, scale = p.a.scale, g = known && p.d_logp ? p.d_logp[row] * scale : 0.f;
+  const float h = p.d_entropy ? p.d_entropy[row] * scale : 0.f, entropy = p.d_entropy ? p.entropy_in[row] : 0.f;
+  const bool empty = most == minus_infinity();
+  auto grad = [&](float x, int index) {
+    const float d = fmaf(x - most, scale, -log), e = __builtin_amdgcn_exp2f(d * kLog2e);
+    const float y = fmaf(-e, fmaf(h, fmaxf(d, kLeast) + entropy, g), index == t ? g : 0.f);
+    return empty ? 0.f : y;
+  };
+  const Row<T> r(in, p.a.vocabulary);
+  // (pieces of both where the two rows lie alike)
+  const bool alike = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
+  const int first = chunk * 64 * kGradPieces;
+  u32x4 x[kGradPieces];
+#pragma unroll
+  for (int j = 0; j < kGradPieces; ++j) {
+    const int i = first + j * 64 + lane;
+    if (i < r.pieces) x[j] = *r.piece(i);
+  }
+  if (chunk == 0) {
+    const int edge = r.edge(lane, p.a.vocabulary);
+    if (edge >= 0) out[edge] = (T)grad((float)in[edge], edge);
+  }
+#pragma unroll
+  for (int j = 0; j < kGradPieces; ++j) {
+    const int i = first + j * 64 + lane;
+    if (i >= r.pieces) break;
+    u32x4 y = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < P::kEach; ++e) put_value<T>(y, e, grad(P::get(x[j], e), r.index(i, e)));
+    T* to = out + r.index(i, 0);
+    if (alike) {
+      *(u32x4*)to = y;
+    } else {
+#pragma unroll
+      for (int e = 0; e < P::kEach; ++e) to[e] = (T)P::get(y, e);
+    }
+  }
+}
+
+template <typename T, bool kTop>
+int forward(const ScoreArgs& p, hipStream_t s) {
+  const int64_t blocks = p.a.rows * p.parts;
+  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks), block(kThreads);
+  const int n = p.vectors / kThreads;
+  if (n <= 1) score_kernel<T, 1, kTop><<<grid, block, 0, s>>>(p);
+  else if (n <= 2) score_kernel<T, 2, kTop><<<grid, block, 0, s>>>(p);
+  else if (n <= 4) score_kernel<T, 4, kTop><<<grid, block, 0, s>>>(p);
+  else if (n <= 8) score_kernel<T, 8, kTop><<<grid, block, 0, s>>>(p);
+  else score_kernel<T, 16, kTop><<<grid, block, 0, s>>>(p);
+  if (p.parts > 1) score_join_kernel<T><<<dim3((unsigned)p.a.rows), block, 0, s>>>(p);
+  return (int)hipGetLastError();
+}
+
+template <typename T>
+int backward(const ScoreArgs& p, hipStream_t s) {
+  const int chunks = (int)(((int64_t)p.a.vocabulary / Piece<T>::kEach + 64 * kGradPieces) / (64 * kGradPieces));
+  const int64_t blocks = (p.a.rows * chunks + kWaves - 1) / kWaves;
+  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  score_grad_kernel<T><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(p, chunks);
+  return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_score_forward(const ScoreArgs& p, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  const bool top = p.a.top > 0;
+  if (p.a.dtype == ARROW_F32) return top ? forward<float, true>(p, s) : forward<float, false>(p, s);
+  if (p.a.dtype == ARROW_BF16) return top ? forward<__bf16, true>(p, s) : forward<__bf16, false>(p, s);
+  return top ? forward<_Float16, true>(p, s) : forward<_Float16, false>(p, s);
+}
+
+int launch_score_backward(const ScoreArgs& p, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  return p.a.dtype == ARROW_F32 ? backward<float>(p, s) : p.a.dtype == ARROW_BF16 ? backward<__bf16>(p, s) : backward<_Float16>(p, s);
+}
+
+}  // namespace arrow

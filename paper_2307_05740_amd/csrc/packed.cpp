@@ -1,0 +1,151 @@
+// C boundary of the entries of include/arrow_packed.h: checks of the arguments, the plan of a call.
+#include <algorithm>
+#include <cmath>
+
+#include "checks.h"
+#include "packed_internal.h"
+
+namespace {
+
+using namespace arrow;
+
+constexpr int32_t kMostTokens = 1 << 26;    // of a sequence
+
+int check_pool(const arrow_packed_t* c, const void* pool) {
+  if (!c) return refuse(ARROW_EINVAL, "NULL arguments");
+  if (c->dtype != ARROW_BF16 && c->dtype != ARROW_F16) return refuse(ARROW_EINVAL, "dtype %d: a cache in 4 bits takes ARROW_BF16 and ARROW_F16", c->dtype);
+  if (c->kv_heads < 1 || c->kv_heads > 65536) return refuse(ARROW_EINVAL, "kv_heads = %d: 1 .. 65536", c->kv_heads);
+  if (c->dim != 32 && c->dim != 64 && c->dim != 128) return refuse(ARROW_EINVAL, "dim = %d is none of 32, 64, 128", c->dim);
+  if (c->page < 16 || (c->page & (c->page - 1)) || c->page > (1 << 20)) return refuse(ARROW_EINVAL, "page = %d is no power of two from 16 to 2^20", c->page);
+  if (c->pages < 0 || c->pages > 0x7fffffff) return refuse(ARROW_EINVAL, "pages = %lld", (long long)c->pages);
+  if (c->pages == 0) return ARROW_OK;
+  if (int rc = check_pointer("pool", pool, 16)) return rc;
+  const int64_t block = (int64_t)c->page * (c->dim + c->dim / 16);
+  if (c->page_step % 16 || c->head_step % 16 || c->page_step < 0 || c->head_step < 0 || (c->pages > 1 && c->page_step < block) ||
+      (c->kv_heads > 1 && c->head_step < block))
+    return refuse(ARROW_EINVAL, "pool: blocks %lld and %lld bytes apart, multiples of 16 from %lld expected", (long long)c->page_step, (long long)c->head_step,
+                  (long long)block);
+  return ARROW_OK;
+}
+
+int check_rows(const arrow_packed_t* c, const char* name, const void* at, int64_t row, int64_t head, int64_t rows, int32_t heads, bool written) {
+  if (int rc = check_pointer(name, at, 16)) return rc;
+  if (row % 8 || head % 8 || row < 0 || head < 0)
+    return refuse(ARROW_EINVAL, "%s: steps of %lld and %lld elements are not multiples of 8", name, (long long)row, (long long)head);
+  if (written && ((rows > 1 && row < c->dim) || (heads > 1 && head < c->dim))) return refuse(ARROW_EINVAL, "%s is written, and its rows overlap", name);
+  return ARROW_OK;
+}
+
+int check_places(const arrow_packed_t* c, int64_t tokens, const int64_t* slots) {
+  if (tokens < 0 || tokens > 0x7fffffff) return refuse(ARROW_EINVAL, "tokens = %lld: 0 .. 2^31 - 1", (long long)tokens);
+  if (tokens == 0) return ARROW_OK;
+  (void)c;
+  return check_pointer("slots", slots, 8);
+}
+
+PackedArgs plan(const arrow_packed_t* c) {
+  PackedArgs p{};
+  p.c = *c;
+  while ((1 << p.page_log) < c->page) ++p.page_log;
+  return p;
+}
+
+int check_decode(const arrow_packed_t* c) {
+  if (c->batch < 0) return refuse(ARROW_EINVAL, "batch = %d", c->batch);
+  if (c->q_heads < 1 || c->q_heads % c->kv_heads) return refuse(ARROW_EINVAL, "q_heads = %d is no multiple of kv_heads = %d", c->q_heads, c->kv_heads);
+  if (c->window < 0 || c->sinks < 0) return refuse(ARROW_EINVAL, "window = %d, sinks = %d", c->window, c->sinks);
+  if (!(c->scale > 0.f) || !std::isfinite(c->scale)) return refuse(ARROW_EINVAL, "scale = %g is not positive and finite", c->scale);
+  if (c->columns < 0 || (int64_t)c->columns * c->page > kMostTokens)
+    return refuse(ARROW_EINVAL, "columns = %d of %d tokens each: 0 .. %d tokens", c->columns, c->page, kMostTokens);
+  if (c->max_len < 0) return refuse(ARROW_EINVAL, "max_len = %lld", (long long)c->max_len);
+  if (c->batch == 0) return ARROW_OK;
+  if (!c->lengths || (c->columns && !c->table)) return refuse(ARROW_EINVAL, "table or lengths is NULL");
+  if ((uintptr_t)c->lengths % 4 || (uintptr_t)c->table % 4) return refuse(ARROW_EINVAL, "table or lengths is not 4-byte aligned");
+  return ARROW_OK;
+}
+
+PackedArgs plan_decode(const arrow_packed_t* c) {
+  PackedArgs p = plan(c);
+  p.group = c->q_heads / c->kv_heads;
+  const int64_t room = (int64_t)c->columns * c->page;
+  p.c.window = c->window < room ? c->window : 0;     // one as long as any sequence hides nothing
+  p.c.sinks = p.c.window ? (int32_t)std::min<int64_t>(c->sinks, room) : 0;
+  if (c->pages == 0) p.c.columns = 0;
+  int64_t seen = std::min(c->max_len, room);
+  if (p.c.window) seen = std::min(seen, (int64_t)p.c.window + p.c.sinks);
+  const int64_t rows = std::max<int64_t>(1, (int64_t)c->batch * c->kv_heads * ceil_div(p.group, kHeadTile));
+  const int64_t full = p.c.window ? 512 / rows : std::max(1024 / rows, ceil_div(seen, 4096)), best = (int64_t)std::sqrt(0.2 * (double)seen);
+  // A round of a workgroup's wavefronts is 128 keys: no more stretches than the longest ones' number of rounds needs.
+  const int64_t rounds = std::max<int64_t>(1, ceil_div(seen, 128)), most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, full, best, rounds}));
+  p.splits = seen <= 256 ? 1 : (int32_t)ceil_div(rounds, ceil_div(rounds, most));
+  return p;
+}
+
+Operand rows_of(const void* at, const arrow_strides_t& s) { return {at, s.sequence, s.token, s.head}; }
+
+}  // namespace
+
+extern "C" {
+
+int arrow_packed_append(const arrow_packed_t* c, int64_t tokens, const void* k, const void* v, arrow_strides_t ks, arrow_strides_t vs, const int64_t* slots,
+                        void* pool, void* stream) {
+  if (int rc = check_pool(c, pool)) return rc;
+  if (int rc = check_places(c, tokens, slots)) return rc;
+  if (tokens == 0) return ARROW_OK;
+  if (int rc = check_rows(c, "k", k, ks.token, ks.head, tokens, c->kv_heads, false)) return rc;
+  if (int rc = check_rows(c, "v", v, vs.token, vs.head, tokens, c->kv_heads, false)) return rc;
+  if (pool && (k == pool || v == pool)) return refuse(ARROW_EINVAL, "k or v is the pool");
+  if (c->pages == 0) return ARROW_OK;
+  PackedArgs p = plan(c);
+  p.k = rows_of(k, ks); p.v = rows_of(v, vs);
+  p.pool = pool; p.slots = slots; p.tokens = tokens;
+  return launched("packed append", launch_packed_append(p, stream));
+}
+
+int arrow_packed_read(const arrow_packed_t* c, int64_t tokens, const int64_t* slots, const void* pool, void* k, void* v, arrow_strides_t ks, arrow_strides_t vs,
+                      void* stream) {
+  if (int rc = check_pool(c, pool)) return rc;
+  if (int rc = check_places(c, tokens, slots)) return rc;
+  if (tokens == 0) return ARROW_OK;
+  if (int rc = check_rows(c, "k", k, ks.token, ks.head, tokens, c->kv_heads, true)) return rc;
+  if (int rc = check_rows(c, "v", v, vs.token, vs.head, tokens, c->kv_heads, true)) return rc;
+  if (k == v || (pool && (k == pool || v == pool))) return refuse(ARROW_EINVAL, "k or v is the other or the pool");
+  PackedArgs p = plan(c);
+  p.k = rows_of(k, ks); p.v = rows_of(v, vs);
+  p.pool = const_cast<void*>(pool); p.slots = slots; p.tokens = tokens;
+  return launched("packed read", launch_packed_read(p, stream));
+}
+
+size_t arrow_packed_decode_workspace_bytes(const arrow_packed_t* c) {
+  if (!c || c->batch < 1 || c->kv_heads < 1 || c->q_heads < 1 || c->q_heads % c->kv_heads || c->dim < 1 || c->dim > 128 || c->page < 1 || c->page > (1 << 20)) return 0;
+  const PackedArgs p = plan_decode(c);
+  return p.splits == 1 ? 0 : align_up((size_t)p.splits * c->batch * c->q_heads * (c->dim + 2) * 4);
+}
+
+int arrow_packed_decode(const arrow_packed_t* c, const void* q, arrow_strides_t qs, const void* k, const void* v, arrow_strides_t ks, arrow_strides_t vs, void* pool,
+                        void* o, arrow_strides_t os, void* ws, size_t ws_bytes, void* stream) {
+  if (int rc = check_pool(c, pool)) return rc;
+  if (int rc = check_decode(c)) return rc;
+  if (c->batch == 0) return ARROW_OK;
+  if (!k != !v) return refuse(ARROW_EINVAL, "k and v of the new token: both or neither");
+  if (int rc = check_rows(c, "q", q, qs.sequence, qs.head, c->batch, c->q_heads, false)) return rc;
+  if (int rc = check_rows(c, "o", o, os.sequence, os.head, c->batch, c->q_heads, true)) return rc;
+  if (k) {
+    if (int rc = check_rows(c, "k", k, ks.sequence, ks.head, c->batch, c->kv_heads, false)) return rc;
+    if (int rc = check_rows(c, "v", v, vs.sequence, vs.head, c->batch, c->kv_heads, false)) return rc;
+  }
+  if (o == q || o == k || o == v || (pool && o == pool)) return refuse(ARROW_EINVAL, "o is one of the inputs");
+  PackedArgs p = plan_decode(c);
+  if (int rc = check_workspace(ws, ws_bytes, arrow_packed_decode_workspace_bytes(c))) return rc;
+  p.q = rows_of(q, qs); p.o = rows_of(o, os);
+  p.k = rows_of(k, ks); p.v = rows_of(v, vs);
+  p.k.token = ks.sequence; p.v.token = vs.sequence;      // (a token of each sequence)
+  p.pool = pool;
+  p.tokens = c->batch;
+  p.parts = (float*)ws;
+  if (k && c->pages)
+    if (int rc = launched("packed append", launch_packed_append(p, stream))) return rc;
+  return launched("packed decode", launch_packed_decode(p, stream));
+}
+
+}  // extern "C"

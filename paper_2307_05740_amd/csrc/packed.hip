@@ -1,0 +1,437 @@
+// A cache of keys and values in 4 bits: writes, reads, and the attention of one new token per sequence over it (include/arrow_packed.h).
+//
+// What bounds the attention is the cache: every visible key and value is read once, for all query heads that share it.  A workgroup takes the up to 16
+// query heads of a key head and a stretch of the visible keys; its wavefronts take tiles of 32 keys in turn, each with a running maximum and sum of its
+// own, and are joined in LDS; long caches are cut into several stretches, whose results a second kernel joins (attention_decode.hip's).
+//
+// Everything stays in registers.  Scores are computed transposed, keys by heads: a lane holds a quarter of a key's row, whose order within the product is
+// free, so that its 16 bytes are one load.  Of the result a lane holds four keys of a head in each half of a tile, and the products with the values take these
+// eight as they are: the values of four tokens lie together in the cache so that a lane finds its four tokens' eight columns (heads of 128) in 16 bytes, and two
+// bytes permutations turn two tokens' pairs of columns into two columns' pairs of tokens.
+#include "attention_common.h"
+#include "packed_internal.h"
+
+namespace arrow {
+namespace {
+
+constexpr int kWaves = 4;
+
+template <int N> struct Words;
+template <> struct Words<1> { typedef uint32_t type; };
+template <> struct Words<2> { typedef u32x2 type; };
+template <> struct Words<4> { typedef u32x4 type; };
+template <int N> using words = typename Words<N>::type;
+__device__ __forceinline__ uint32_t word(uint32_t w, int) { return w; }
+__device__ __forceinline__ uint32_t word(const u32x2& w, int i) { return w[i]; }
+__device__ __forceinline__ uint32_t word(const u32x4& w, int i) { return w[i]; }
+
+// The two elements of byte B of a word, times a power of two.
+template <int B> __device__ __forceinline__ uint32_t pair_of(uint32_t w, float scale, __bf16) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
+}
+template <int B> __device__ __forceinline__ uint32_t pair_of(uint32_t w, float scale, _Float16) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, B));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pair_at(uint32_t w, float scale, int byte) {       // (a constant, once loops are unrolled)
+  switch (byte) {
+    case 0: return pair_of<0>(w, scale, T{});
+    case 1: return pair_of<1>(w, scale, T{});
+    case 2: return pair_of<2>(w, scale, T{});
+    default: return pair_of<3>(w, scale, T{});
+  }
+}
+template <typename T>
+__device__ __forceinline__ x8<T> eight_of(uint32_t w, float scale) {
+  union { uint32_t u[4]; x8<T> all; } r;
+  r.u[0] = pair_of<0>(w, scale, T{});
+  r.u[1] = pair_of<1>(w, scale, T{});
+  r.u[2] = pair_of<2>(w, scale, T{});
+  r.u[3] = pair_of<3>(w, scale, T{});
+  return r.all;
+}
+
+// A scale's byte as a float: 2^(e - 127), and infinity for 255, which makes NaN of the elements.
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
+
+// Of a block: where codes and scales begin.
+__device__ __forceinline__ int64_t values_at(int page, int dim) { return (int64_t)page * (dim / 2); }
+__device__ __forceinline__ int64_t key_scales_at(int page, int dim) { return (int64_t)page * dim; }
+__device__ __forceinline__ int64_t value_scales_at(int page, int dim) { return (int64_t)page * (dim + dim / 32); }
+
+// ---- writes and reads ----
+// Eight elements a lane, four lanes to a scale.  Four tokens of a head lie in neighbouring lanes, so that what a wavefront writes are whole runs of bytes.
+struct Place {
+  int64_t row, slot;                  // slot -1: none
+  int head, piece;
+  bool in;
+};
+__device__ __forceinline__ Place place_of(const PackedArgs& p, int64_t id) {
+  const arrow_packed_t& c = p.c;
+  const int pieces = c.dim / 8;
+  Place at;
+  at.piece = (int)(id & (pieces - 1));
+  id /= pieces;
+  const int t = (int)(id & 3);
+  id >>= 2;
+  at.head = (int)(id % c.kv_heads);
+  at.row = id / c.kv_heads * 4 + t;
+  at.in = at.row < p.tokens;
+  at.slot = -1;
+  if (!at.in) return at;
+  if (p.slots) {
+    at.slot = p.slots[at.row];
+  } else {                            // the last place of a sequence
+    const int64_t j = (int64_t)c.lengths[at.row] - 1, column = j >> p.page_log;
+    if (j < 0 || column >= c.columns) return at;
+    const int page = c.table[at.row * c.columns + column];
+    at.slot = page < 0 ? -1 : ((int64_t)page << p.page_log) + (j & (c.page - 1));
+  }
+  if (at.slot < 0 || at.slot >> p.page_log >= c.pages) at.slot = -1;
+  return at;
+}
+
+__device__ __forceinline__ uint32_t codes_of(const x8<__bf16>& x, float scale) {
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x2<__bf16>{x[0], x[1]}, scale, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x2<__bf16>{x[2], x[3]}, scale, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x2<__bf16>{x[4], x[5]}, scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x2<__bf16>{x[6], x[7]}, scale, 3);
+}
+__device__ __forceinline__ uint32_t codes_of(const x8<_Float16>& x, float scale) {
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, x2<_Float16>{x[0], x[1]}, scale, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, x2<_Float16>{x[2], x[3]}, scale, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, x2<_Float16>{x[4], x[5]}, scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, x2<_Float16>{x[6], x[7]}, scale, 3);
+}
+
+// Codes of a lane's eight elements and the scale of the 32 ones that its four lanes have.
+template <typename T>
+__device__ __forceinline__ uint32_t pack8(const x8<T>& x, uint32_t* scale) {
+  uint32_t most = 0;                  // (sizes of floats are in the order of their bits, those of NaN last)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint((float)x[i]) & 0x7fffffffu);
+  most = max(most, (uint32_t)__shfl_xor((int)most, 1, 64));
+  most = max(most, (uint32_t)__shfl_xor((int)most, 2, 64));
+  // 1.m 2^(E - 127) <= 7 2^(e - 127): e = E - 2 where 1.m is up to 7/4
+  const int E = (int)(most >> 23), e = E - 2 + ((most & 0x7fffffu) > 0x600000u), limit = std::is_same<T, _Float16>::value ? 140 : 252;
+  *scale = E == 255 ? 255u : (uint32_t)min(max(e, 1), limit);
+  return E == 255 ? 0u : codes_of(x, scale_of(*scale));
+}
+
+// Codes of a token's elements 8 piece .. + 7 to their place among the values.
+template <int D>
+__device__ __forceinline__ void store_values(char* block, int t, int piece, uint32_t codes) {
+  char* at = block + (t >> 2) * (2 * D);
+  if (D == 128) {
+    *(uint32_t*)(at + piece * 16 + (t & 3) * 4) = codes;
+  } else if (D == 64) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(uint16_t*)(at + (2 * piece + i) * 8 + (t & 3) * 2) = (uint16_t)(codes >> (16 * i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(uint8_t*)(at + (4 * piece + i) * 4 + (t & 3)) = (uint8_t)(codes >> (8 * i));
+  }
+}
+template <int D>
+__device__ __forceinline__ uint32_t load_values(const char* block, int t, int piece) {
+  const char* at = block + (t >> 2) * (2 * D);
+  uint32_t codes = 0;
+  if (D == 128) {
+    codes = *(const uint32_t*)(at + piece * 16 + (t & 3) * 4);
+  } else if (D == 64) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) codes |= (uint32_t)*(const uint16_t*)(at + (2 * piece + i) * 8 + (t & 3) * 2) << (16 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) codes |= (uint32_t)*(const uint8_t*)(at + (4 * piece + i) * 4 + (t & 3)) << (8 * i);
+  }
+  return codes;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_append_kernel(PackedArgs p) {
+  const arrow_packed_t& c = p.c;
+  const Place at = place_of(p, (int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (at.slot < 0) return;            // (the four lanes of a scale have one row)
+  const x8<T> k = *(const x8<T>*)((const T*)p.k.at + at.row * p.k.token + at.head * p.k.head + at.piece * 8);
+  const x8<T> v = *(const x8<T>*)((const T*)p.v.at + at.row * p.v.token + at.head * p.v.head + at.piece * 8);
+  const int t = (int)(at.slot & (c.page - 1)), of = at.piece >> 2;
+  char* block = (char*)p.pool + (at.slot >> p.page_log) * c.page_step + at.head * c.head_step;
+  uint32_t ks, vs;
+  const uint32_t kc = pack8<T>(k, &ks), vc = pack8<T>(v, &vs);
+  *(uint32_t*)(block + (int64_t)t * (D / 2) + at.piece * 4) = kc;
+  store_values<D>(block + values_at(c.page, D), t, at.piece, vc);
+  if ((at.piece & 3) == 0) {
+    *(uint8_t*)(block + key_scales_at(c.page, D) + t * (D / 32) + of) = (uint8_t)ks;
+    *(uint8_t*)(block + value_scales_at(c.page, D) + ((t >> 2) * (D / 32) + of) * 4 + (t & 3)) = (uint8_t)vs;
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_read_kernel(PackedArgs p) {
+  const arrow_packed_t& c = p.c;
+  const Place at = place_of(p, (int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (!at.in) return;
+  x8<T> k = {}, v = {};
+  if (at.slot >= 0) {
+    const int t = (int)(at.slot & (c.page - 1)), of = at.piece >> 2;
+    const char* block = (const char*)p.pool + (at.slot >> p.page_log) * c.page_step + at.head * c.head_step;
+    const uint32_t ks = *(const uint8_t*)(block + key_scales_at(c.page, D) + t * (D / 32) + of);
+    const uint32_t vs = *(const uint8_t*)(block + value_scales_at(c.page, D) + ((t >> 2) * (D / 32) + of) * 4 + (t & 3));
+    k = eight_of<T>(*(const uint32_t*)(block + (int64_t)t * (D / 2) + at.piece * 4), scale_of(ks));
+    v = eight_of<T>(load_values<D>(block + values_at(c.page, D), t, at.piece), scale_of(vs));
+  }
+  *(x8<T>*)((T*)const_cast<void*>(p.k.at) + at.row * p.k.token + at.head * p.k.head + at.piece * 8) = k;
+  *(x8<T>*)((T*)const_cast<void*>(p.v.at) + at.row * p.v.token + at.head * p.v.head + at.piece * 8) = v;
+}
+
+// ---- attention ----
+// max / sum over the four lanes that have one l % 16
+__device__ __forceinline__ float max_quarters(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float add_quarters(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return add_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// A tile on its way: of each half, the lane's quarter of key l % 16's row with its scale, and tokens 4 (l / 16) + 0..3 of its columns with theirs.
+template <int D>
+struct Codes {
+  words<D / 32> k[2], v[2];
+  uint32_t ks[2], vs[2];
+  uint32_t visible;                   // keys, the same in all lanes
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArgs a) {
+  constexpr int kSteps = D / 32;      // of the scores' inner dimension
+  constexpr int kColumns = D / 16;    // columns of a lane
+  __shared__ __align__(16) float smem[kWaves * 16 * D + kWaves * 2 * 16];
+  const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
+  const arrow_packed_t& c = a.c;
+  int id = blockIdx.x;
+  const int kv = id % c.kv_heads; id /= c.kv_heads;
+  const int split = id % a.splits; id /= a.splits;
+  const int head_tiles = (a.group + kHeadTile - 1) / kHeadTile;
+  const int head_tile = id % head_tiles, b = id / head_tiles;
+  const int head0 = head_tile * kHeadTile, heads = min(a.group - head0, kHeadTile);
+  const int64_t room = (int64_t)c.columns << a.page_log;
+  const int length = (int)max((int64_t)0, min((int64_t)c.lengths[b], room));
+  const int begin = c.window ? max(0, length - c.window) : 0;
+  // groups of 16 keys (within a page), those that only hide between the first ones and the window left out; tiles of two groups, stretches of whole rounds of the wavefronts
+  const int rest = begin >> 4, lead = min((min(c.sinks, begin) + 15) >> 4, rest), groups = lead + ((length + 15) >> 4) - rest;
+  const int tiles = (groups + 1) >> 1, rounds = (tiles + kWaves - 1) / kWaves;
+  const int tile0 = kWaves * (int)((int64_t)rounds * split / a.splits), tile1 = min(tiles, kWaves * (int)((int64_t)rounds * (split + 1) / a.splits));
+  const int32_t* table = c.table + (int64_t)b * c.columns;
+  const char* pool = (const char*)a.pool + kv * c.head_step;
+
+  // the queries in the order of the keys' quarters
+  x8<T> qf[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const x8<T> z = {};
+    qf[s] = col < heads ? *(const x8<T>*)((const T*)a.q.at + b * a.q.sequence + (int64_t)(kv * a.group + head0 + col) * a.q.head + quarter * (D / 4) + 8 * s) : z;
+  }
+
+  // (nothing here branches: the loads of one tile are to be on their way while another's are waited for; a page that is not there is read as the first one)
+  auto group_at = [&](int g) { return g < lead ? g : g - lead + rest; };
+  auto page_of = [&](int g) { return table[group_at(min(g, groups - 1)) >> (a.page_log - 4)]; };
+  int page[2] = {0, 0};               // of the tile that is loaded next, looked up a tile ahead
+  auto load = [&](int tile) {
+    Codes<D> x;
+    x.visible = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int g = 2 * tile + h, key0 = 16 * group_at(g), slot0 = key0 & (c.page - 1);
+      const bool in = g < groups && page[h] >= 0 && page[h] < c.pages;
+      const char* block = pool + (in ? page[h] : 0) * c.page_step;
+      const int upto = min(16, length - key0), gone = min(16, max(0, begin - key0)), first = min(16, max(0, c.sinks - key0));
+      const uint32_t mask = ((1u << max(0, upto)) - 1) & (~((1u << gone) - 1) | ((1u << first) - 1));
+      x.visible |= (in ? mask & 0xffffu : 0u) << (16 * h);
+      x.k[h] = *(const words<kSteps>*)(block + (slot0 + col) * (D / 2) + quarter * (D / 8));
+      x.ks[h] = *(const uint8_t*)(block + key_scales_at(c.page, D) + (slot0 + col) * (D / 32) + quarter * (D / 4) / 32);
+      x.v[h] = *(const words<kSteps>*)(block + values_at(c.page, D) + (((slot0 >> 2) + quarter) * 16 + col) * (D / 8));
+      x.vs[h] = *(const uint32_t*)(block + value_scales_at(c.page, D) + (((slot0 >> 2) + quarter) * (D / 32) + col * kColumns / 32) * 4);
+      page[h] = page_of(2 * (tile + kWaves) + h);
+    }
+    return x;
+  };
+
+  f32x4 acc[kColumns];
+#pragma unroll
+  for (int m = 0; m < kColumns; ++m) acc[m] = (f32x4)(0.f);
+  const float scale = c.scale * kLog2e;
+  float top = minus_infinity(), total = 0.f;
+
+  int tile = tile0 + wave;
+  Codes<D> next;
+  if (tile < tile1) {
+    page[0] = page_of(2 * tile);
+    page[1] = page_of(2 * tile + 1);
+    next = load(tile);
+  }
+  while (tile < tile1) {
+    const Codes<D> x = next;
+    tile += kWaves;
+    if (tile < tile1) next = load(tile);
+
+    f32x4 s[2] = {(f32x4)(0.f), (f32x4)(0.f)};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float ks = scale_of(x.ks[h]);
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) s[h] = mma16(eight_of<T>(word(x.k[h], i), ks), qf[i], s[h]);
+    }
+    float vs[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      vs[h][0] = __uint_as_float(x.vs[h] << 23 & 0x7f800000u);
+      vs[h][1] = __uint_as_float(x.vs[h] << 15 & 0x7f800000u);
+      vs[h][2] = __uint_as_float(x.vs[h] << 7 & 0x7f800000u);
+      vs[h][3] = __uint_as_float(x.vs[h] >> 1 & 0x7f800000u);
+    }
+    if (x.visible != 0xffffffffu) {   // what is not seen does not count, whatever its scale
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool seen = x.visible >> (16 * h + 4 * quarter + i) & 1;
+          s[h][i] = seen ? s[h][i] : minus_infinity();
+          vs[h][i] = seen ? vs[h][i] : 1.f;
+        }
+    }
+    float most = minus_infinity();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, s[h][i]);
+    most = max_quarters(most) * scale;
+    const float raised = fmaxf(top, most), off = raised == minus_infinity() ? 0.f : raised;
+    if (__any(raised > top)) {
+      const float by = __builtin_amdgcn_exp2f(top - off);
+      total *= by;
+#pragma unroll
+      for (int m = 0; m < kColumns; ++m) acc[m] = acc[m] * by;
+      top = raised;
+    }
+    x8<T> pf;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[h][i], scale, -off));
+        total += e;
+        pf[4 * h + i] = (T)e;
+      }
+#pragma unroll
+    for (int j = 0; j < kColumns / 2; ++j) {
+      union { uint32_t u[4]; x8<T> all; } lo, hi;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 4; t += 2) {
+          const int i = t * (D / 32) + j, n = (t + 1) * (D / 32) + j;          // the bytes of the two tokens
+          const uint32_t one = pair_at<T>(word(x.v[h], i / 4), vs[h][t], i % 4), two = pair_at<T>(word(x.v[h], n / 4), vs[h][t + 1], n % 4);
+          lo.u[2 * h + t / 2] = __builtin_amdgcn_perm(two, one, 0x05040100u);
+          hi.u[2 * h + t / 2] = __builtin_amdgcn_perm(two, one, 0x07060302u);
+        }
+      acc[2 * j] = mma16(lo.all, pf, acc[2 * j]);
+      acc[2 * j + 1] = mma16(hi.all, pf, acc[2 * j + 1]);
+    }
+  }
+  total = add_quarters(total);
+
+  // the wavefronts' results: column d of head h at [d][h], 16 floats to a row
+  float* mine = smem + wave * 16 * D;
+  float *tops = smem + kWaves * 16 * D, *totals = tops + kWaves * 16;
+#pragma unroll
+  for (int m = 0; m < kColumns; ++m)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine[((4 * quarter + i) * kColumns + m) * 16 + col] = acc[m][i];
+  if (quarter == 0) { tops[wave * 16 + col] = top; totals[wave * 16 + col] = total; }
+  __syncthreads();
+  for (int e = threadIdx.x; e < heads * D; e += 64 * kWaves) {
+    const int h = e / D, d = e % D;
+    float all = tops[h];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w * 16 + h]);
+    const float off = all == minus_infinity() ? 0.f : all;
+    float sum = 0.f, weight = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float by = __builtin_amdgcn_exp2f(tops[w * 16 + h] - off);
+      sum = fmaf(by, smem[(w * D + d) * 16 + h], sum);
+      weight = fmaf(by, totals[w * 16 + h], weight);
+    }
+    const int head = kv * a.group + head0 + h;
+    if (a.splits == 1) {
+      ((T*)const_cast<void*>(a.o.at))[b * a.o.sequence + head * a.o.head + d] = (T)(weight > 0.f || weight != weight ? sum / weight : 0.f);
+    } else {
+      float* part = a.parts + ((int64_t)(b * c.q_heads + head) * a.splits + split) * (D + 2);
+      part[d] = sum;
+      if (d == 0) { part[D] = all; part[D + 1] = weight; }
+    }
+  }
+}
+
+template <typename T, int D>
+int decode(const PackedArgs& a, hipStream_t s) {
+  const arrow_packed_t& c = a.c;
+  const int64_t blocks = (int64_t)c.batch * c.kv_heads * a.splits * ((a.group + kHeadTile - 1) / kHeadTile), rows = (int64_t)c.batch * c.q_heads;
+  if (blocks > 0x7fffffff || rows > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  packed_decode_kernel<T, D><<<dim3((unsigned)blocks), dim3(64 * kWaves), 0, s>>>(a);
+  if (a.splits > 1) {
+    CacheArgs j{};
+    j.c.dtype = c.dtype; j.c.batch = c.batch; j.c.q_heads = c.q_heads; j.c.dim = c.dim;
+    j.o = a.o; j.splits = a.splits; j.parts = a.parts;
+    return launch_attention_decode_join(j, s);
+  }
+  return (int)hipGetLastError();
+}
+
+template <typename F>
+int of_kind(const arrow_packed_t& c, F&& f) {
+  if (c.dtype == ARROW_BF16) return c.dim == 128 ? f.template operator()<__bf16, 128>() : c.dim == 64 ? f.template operator()<__bf16, 64>() : f.template operator()<__bf16, 32>();
+  return c.dim == 128 ? f.template operator()<_Float16, 128>() : c.dim == 64 ? f.template operator()<_Float16, 64>() : f.template operator()<_Float16, 32>();
+}
+
+unsigned blocks_of(const PackedArgs& p) {
+  const int64_t n = ((p.tokens + 3) / 4 * 4 * p.c.kv_heads * (p.c.dim / 8) + 255) / 256;
+  return n > 0x7fffffff ? 0 : (unsigned)n;
+}
+
+struct Append {
+  const PackedArgs& p;
+  hipStream_t s;
+  template <typename T, int D> int operator()() const {
+    if (!blocks_of(p)) return (int)hipErrorInvalidConfiguration;
+    packed_append_kernel<T, D><<<dim3(blocks_of(p)), dim3(256), 0, s>>>(p);
+    return (int)hipGetLastError();
+  }
+};
+struct Read {
+  const PackedArgs& p;
+  hipStream_t s;
+  template <typename T, int D> int operator()() const {
+    if (!blocks_of(p)) return (int)hipErrorInvalidConfiguration;
+    packed_read_kernel<T, D><<<dim3(blocks_of(p)), dim3(256), 0, s>>>(p);
+    return (int)hipGetLastError();
+  }
+};
+struct Decode {
+  const PackedArgs& p;
+  hipStream_t s;
+  template <typename T, int D> int operator()() const { return decode<T, D>(p, s); }
+};
+
+}  // namespace
+
+int launch_packed_append(const PackedArgs& p, void* stream) { return of_kind(p.c, Append{p, (hipStream_t)stream}); }
+int launch_packed_read(const PackedArgs& p, void* stream) { return of_kind(p.c, Read{p, (hipStream_t)stream}); }
+int launch_packed_decode(const PackedArgs& p, void* stream) { return of_kind(p.c, Decode{p, (hipStream_t)stream}); }
+
+}  // namespace arrow

@@ -1,0 +1,27 @@
+// What the entries of arrow_packed.h hand to their kernels.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "arrow_packed.h"
+#include "attention_internal.h"
+
+namespace arrow {
+
+struct PackedArgs {
+  arrow_packed_t c;
+  Operand q, k, v, o;
+  void* pool;
+  const int64_t* slots;      // null: the last places of the sequences, by table and lengths
+  int64_t tokens;
+  int32_t group, splits, page_log;
+  float* parts;              // splits x batch x q_heads x (dim + 2)
+};
+
+// Launchers: 0 or a hipError_t.
+int launch_packed_append(const PackedArgs& p, void* stream);
+int launch_packed_read(const PackedArgs& p, void* stream);
+int launch_packed_decode(const PackedArgs& p, void* stream);
+
+}  // namespace arrow

@@ -1,0 +1,119 @@
+// C boundary of the rotation entries (include/arrow_rotation.h): checks of the arguments, the plan of a call.
+#include <algorithm>
+#include <cmath>
+
+#include "checks.h"
+#include "rotation_internal.h"
+
+namespace {
+
+using namespace arrow;
+
+int check(const arrow_rotation_t* a) {
+  if (!a) return refuse(ARROW_EINVAL, "NULL arguments");
+  if (!is_dtype(a->dtype)) return refuse(ARROW_EINVAL, "dtype %d", a->dtype);
+  if (a->weight_dtype != a->dtype && a->weight_dtype != ARROW_F32) return refuse(ARROW_EINVAL, "weight_dtype %d is neither dtype nor ARROW_F32", a->weight_dtype);
+  if (a->batch < 0 || a->tokens < 0 || (int64_t)a->batch * a->tokens > 0x7fffffff) return refuse(ARROW_EINVAL, "batch = %d of tokens = %d", a->batch, a->tokens);
+  if (a->q_heads < 1 || a->kv_heads < 1 || a->q_heads > 65536 || a->kv_heads > 65536)
+    return refuse(ARROW_EINVAL, "q_heads = %d, kv_heads = %d: 1 .. 65536", a->q_heads, a->kv_heads);
+  if (a->dim < 8 || a->dim > 256 || a->dim % 8) return refuse(ARROW_EINVAL, "dim = %d is none of 8, 16, ..., 256", a->dim);
+  if (a->rotary < 0 || a->rotary > a->dim || a->rotary % 16) return refuse(ARROW_EINVAL, "rotary = %d is none of 0, 16, 32, ... up to dim = %d", a->rotary, a->dim);
+  if (a->interleaved != 0 && a->interleaved != 1) return refuse(ARROW_EINVAL, "interleaved = %d", a->interleaved);
+  if (!(a->eps >= 0.f) || !std::isfinite(a->eps)) return refuse(ARROW_EINVAL, "eps = %g is negative or not finite", a->eps);
+  if (a->positions) {
+    if (a->position_bytes != 4 && a->position_bytes != 8) return refuse(ARROW_EINVAL, "position_bytes = %d is neither 4 nor 8", a->position_bytes);
+    if (int rc = check_pointer("positions", a->positions, a->position_bytes)) return rc;
+  }
+  if (a->shift < -((int64_t)1 << 52) || a->shift > (int64_t)1 << 52) return refuse(ARROW_EINVAL, "shift = %lld: within 2^52 of 0", (long long)a->shift);
+  if (a->rotary)
+    if (int rc = check_pointer("turns", a->turns, 8)) return rc;
+  return ARROW_OK;
+}
+
+int check_heads(const arrow_rotation_t* a, const char* name, const void* at, const arrow_strides_t& s, int32_t heads, bool written) {
+  if (int rc = check_pointer(name, at, 16)) return rc;
+  const int step = 16 / size_of(a->dtype);
+  if (s.sequence % step || s.token % step || s.head % step || s.sequence < 0 || s.token < 0 || s.head < 0)
+    return refuse(ARROW_EINVAL, "%s: steps of %lld, %lld, %lld elements: multiples of %d, not negative", name, (long long)s.sequence, (long long)s.token,
+                  (long long)s.head, step);
+  if (written && ((a->tokens > 1 && s.token < a->dim) || (heads > 1 && s.head < a->dim) || (a->batch > 1 && s.sequence < a->dim)))
+    return refuse(ARROW_EINVAL, "%s is written, and its rows overlap", name);
+  return ARROW_OK;
+}
+
+bool same(const arrow_strides_t& a, const arrow_strides_t& b) { return a.sequence == b.sequence && a.token == b.token && a.head == b.head; }
+
+int check_weights(const arrow_rotation_t* a, const char* name, const void* q, const void* k) {
+  if (!q != !k) return refuse(ARROW_EINVAL, "%s of queries and of keys: both or neither", name);
+  const int size = size_of(a->weight_dtype);
+  if ((uintptr_t)q % size || (uintptr_t)k % size) return refuse(ARROW_EINVAL, "%s are not %d-byte aligned", name, size);
+  return ARROW_OK;
+}
+
+RotationArgs plan(const arrow_rotation_t* a, bool backward) {
+  RotationArgs p{};
+  p.a = *a;
+  p.rows = (int64_t)a->batch * a->tokens;
+  while ((16 << p.lanes_log) < a->dim) ++p.lanes_log;
+  // A workgroup's tokens share its angles.  Few tokens: one each.
+  p.per = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kRotationTokens, p.rows / 1024));
+  const int64_t blocks = ceil_div(p.rows, p.per);
+  p.blocks = (int32_t)(backward ? std::min<int64_t>(blocks, kRotationBlocks) : blocks);
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int arrow_rotation_forward(const arrow_rotation_t* a, const void* q, const void* k, const void* wq, const void* wk, void* q_out, void* k_out, void* stream) {
+  if (int rc = check(a)) return rc;
+  if ((int64_t)a->batch * a->tokens == 0) return ARROW_OK;
+  if (int rc = check_weights(a, "weights", wq, wk)) return rc;
+  if (int rc = check_heads(a, "q", q, a->q, a->q_heads, false)) return rc;
+  if (int rc = check_heads(a, "k", k, a->k, a->kv_heads, false)) return rc;
+  if (int rc = check_heads(a, "q_out", q_out, a->q_out, a->q_heads, true)) return rc;
+  if (int rc = check_heads(a, "k_out", k_out, a->k_out, a->kv_heads, true)) return rc;
+  if (q_out == k || k_out == q || q_out == k_out) return refuse(ARROW_EINVAL, "q_out is k or k_out, or k_out is q");
+  if ((q_out == q && !same(a->q, a->q_out)) || (k_out == k && !same(a->k, a->k_out))) return refuse(ARROW_EINVAL, "in place, but with other steps");
+  RotationArgs p = plan(a, false);
+  p.q = q; p.k = k; p.wq = wq; p.wk = wk;
+  p.yq = q_out; p.yk = k_out;
+  p.q_to = a->q_out; p.k_to = a->k_out;
+  return launched("rotation forward", launch_rotation(p, false, stream));
+}
+
+size_t arrow_rotation_workspace_bytes(const arrow_rotation_t* a) {
+  if (check(a)) return 0;
+  return align_up((size_t)plan(a, true).blocks * 2 * a->dim * 4);
+}
+
+int arrow_rotation_backward(const arrow_rotation_t* a, const void* d_q_out, const void* d_k_out, const void* q, const void* k, const void* wq,
+                            const void* wk, void* dq, void* dk, void* dwq, void* dwk, void* ws, size_t ws_bytes, void* stream) {
+  if (int rc = check(a)) return rc;
+  if (int rc = check_weights(a, "weights", wq, wk)) return rc;
+  if (int rc = check_weights(a, "gradients of weights", dwq, dwk)) return rc;
+  if (dwq && dwq == dwk) return refuse(ARROW_EINVAL, "dwq and dwk are the same");
+  RotationArgs p = plan(a, true);
+  if (p.rows) {
+    const struct { const char* name; const void* at; const arrow_strides_t& s; int32_t heads; bool written; } all[] = {
+        {"d_q_out", d_q_out, a->q_out, a->q_heads, false}, {"d_k_out", d_k_out, a->k_out, a->kv_heads, false}, {"q", q, a->q, a->q_heads, false},
+        {"k", k, a->k, a->kv_heads, false}, {"dq", dq, a->dq, a->q_heads, true}, {"dk", dk, a->dk, a->kv_heads, true}};
+    for (auto& m : all)
+      if (int rc = check_heads(a, m.name, m.at, m.s, m.heads, m.written)) return rc;
+    if (dq == dk || dq == k || dk == q || dq == d_k_out || dk == d_q_out || dq == q || dk == k)
+      return refuse(ARROW_EINVAL, "dq or dk is q, k, the other's gradient, or the other");
+    if ((dq == d_q_out && !same(a->dq, a->q_out)) || (dk == d_k_out && !same(a->dk, a->k_out))) return refuse(ARROW_EINVAL, "in place, but with other steps");
+  }
+  if (dwq)
+    if (int rc = check_workspace(ws, ws_bytes, arrow_rotation_workspace_bytes(a))) return rc;
+  if (!p.rows && !dwq) return ARROW_OK;
+  p.q = q; p.k = k; p.wq = wq; p.wk = wk; p.gq = d_q_out; p.gk = d_k_out;
+  p.yq = dq; p.yk = dk;
+  p.q_to = a->dq; p.k_to = a->dk;
+  p.dwq = dwq; p.dwk = dwk;
+  p.parts = (float*)ws;
+  return launched("rotation backward", launch_rotation(p, true, stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,32 @@
+// What the entries of arrow_rotation.h hand to their kernels.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "arrow_rotation.h"
+
+namespace arrow {
+
+constexpr int kRotationThreads = 256;
+constexpr int kRotationTokens = 8;        // of a workgroup at a time, at most
+constexpr int kRotationBlocks = 1024;     // workgroups of a gradient, at most: four to a compute unit; each leaves a sum of the weights' gradients
+
+struct RotationArgs {
+  arrow_rotation_t a;
+  const void *q, *k, *wq, *wk;            // the forward call's
+  const void *gq, *gk;                    // gradients of its results
+  void *yq, *yk;                          // its results, or the gradients of q and k
+  arrow_strides_t q_to, k_to;             // steps of these
+  void *dwq, *dwk;
+  float* parts;                           // blocks x 2 x dim sums of the weights' gradients
+  int64_t rows;                           // tokens of all sequences
+  int32_t per;                            // tokens of a workgroup at a time
+  int32_t blocks;
+  int32_t lanes_log;                      // lanes of a head: a power of two, each has 16 elements
+};
+
+// Launchers: 0 or a hipError_t.
+int launch_rotation(const RotationArgs& p, bool backward, void* stream);
+
+}  // namespace arrow

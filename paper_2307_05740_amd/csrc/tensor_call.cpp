@@ -12,6 +12,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -20,6 +21,10 @@
 
 #include "arrow_attention.h"
 #include "arrow_embedding.h"
+#include "arrow_logprobs.h"
+#include "arrow_packed.h"
+#include "arrow_pages.h"
+#include "arrow_rotation.h"
 
 namespace {
 
@@ -198,7 +203,7 @@ bool lengths(PyObject* const* args, int count, int64_t* out) {
 // What the functions below have in common: None where `call` says so or throws, its error code, or the results.
 template <typename F>
 PyObject* results(int64_t device, F&& call) {
-  at::Tensor out[3];
+  at::Tensor out[6];
   int rc = 0, n = 0;
   try {
     if (c10::hip::current_device() != (c10::DeviceIndex)device) return none();
@@ -393,6 +398,321 @@ PyObject* embedding_backward(PyObject*, PyObject* const* args, Py_ssize_t n_args
   });
 }
 
+// ---- rotation ----
+
+bool steps_fit(const at::Tensor& t) {
+  for (int64_t d = 0; d < t.dim(); ++d)
+    if (!small(t.size(d))) return false;
+  return true;
+}
+
+// q, k, their weights and positions; false for the general way.  values: dim, rotary, interleaved, address of the turns.
+bool describe(arrow_rotation_t& a, const int64_t* values, double eps, const at::Tensor* q, const at::Tensor* k, const at::Tensor* wq, const at::Tensor* wk,
+              const at::Tensor* positions, int64_t shift) {
+  if (!q || !k || !wq != !wk || (q->dim() != 3 && q->dim() != 4) || k->dim() != q->dim() || any_type(*q) < 0 || k->scalar_type() != q->scalar_type()) return false;
+  const int64_t n = q->dim();
+  if (q->size(-1) != values[0] || k->size(-1) != values[0] || k->sizes().slice(0, n - 2) != q->sizes().slice(0, n - 2) || !rows_whole(*q) || !rows_whole(*k)) return false;
+  if (!steps_fit(*q) || !steps_fit(*k)) return false;
+  a.dtype = a.weight_dtype = any_type(*q);
+  for (auto* t : {wq, wk})
+    if (t) {
+      if (t->dim() != 1 || t->size(0) != values[0] || !rows_whole(*t) || t->scalar_type() != wq->scalar_type()) return false;
+      if (t->scalar_type() != q->scalar_type() && t->scalar_type() != at::kFloat) return false;
+      a.weight_dtype = any_type(*t);
+    }
+  if (positions) {
+    if ((positions->scalar_type() != at::kInt && positions->scalar_type() != at::kLong) || positions->sizes() != q->sizes().slice(0, n - 2) || !positions->is_contiguous())
+      return false;
+    a.positions = positions->const_data_ptr();
+    a.position_bytes = positions->scalar_type() == at::kLong ? 8 : 4;
+  }
+  a.batch = (int32_t)(n == 4 ? q->size(0) : 1);
+  a.tokens = (int32_t)q->size(n - 3);
+  a.q_heads = (int32_t)q->size(-2); a.kv_heads = (int32_t)k->size(-2);
+  a.dim = (int32_t)values[0]; a.rotary = (int32_t)values[1]; a.interleaved = (int32_t)values[2];
+  a.eps = (float)eps; a.shift = shift;
+  a.turns = a.rotary ? reinterpret_cast<const double*>(values[3]) : nullptr;
+  a.q = steps(*q); a.k = steps(*k);
+  return true;
+}
+
+// rotation_forward(function, device, dim, rotary, interleaved, turns, eps, q, k, q_weight, k_weight, positions, shift, q_out, k_out)
+PyObject* rotation_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[6], shift;
+  if (!arguments(n_args, 15) || !integers(args, 6, x)) return nullptr;
+  const double eps = PyFloat_AsDouble(args[6]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!integers(args + 12, 1, &shift)) { PyErr_Clear(); return none(); }
+  return results(x[1], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[1]};
+    const at::Tensor *q = tensor(args[7]), *k = tensor(args[8]), *wq = tensor(args[9]), *wk = tensor(args[10]), *positions = tensor(args[11]);
+    const at::Tensor *qo = tensor(args[13]), *ko = tensor(args[14]);
+    arrow_rotation_t a{};
+    if (!tensor.ok || !describe(a, x + 2, eps, q, k, wq, wk, positions, shift) || (qo && !like(*qo, *q)) || (ko && !like(*ko, *k))) return 0;
+    out[0] = qo ? *qo : made(q->sizes(), *q, q->scalar_type());
+    out[1] = ko ? *ko : made(k->sizes(), *k, q->scalar_type());
+    a.q_out = steps(out[0]); a.k_out = steps(out[1]);
+    void *qp = data(*q), *kp = data(*k), *wqp = wq ? data(*wq) : nullptr, *wkp = wk ? data(*wk) : nullptr, *op = data(out[0]), *okp = data(out[1]);
+    void* stream = stream_of(x[1]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_rotation_forward)>(x[0])(&a, qp, kp, wqp, wkp, op, okp, stream); });
+    return 2;
+  });
+}
+
+// rotation_backward(function, of the workspace's size, device, dim, rotary, interleaved, turns, eps, d_q, d_k, q, k, q_weight, k_weight, positions, shift, dq, dk)
+PyObject* rotation_backward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[7], shift;
+  if (!arguments(n_args, 18) || !integers(args, 7, x)) return nullptr;
+  const double eps = PyFloat_AsDouble(args[7]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!integers(args + 15, 1, &shift)) { PyErr_Clear(); return none(); }
+  return results(x[2], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[2]};
+    const at::Tensor *gq = tensor(args[8]), *gk = tensor(args[9]), *q = tensor(args[10]), *k = tensor(args[11]), *wq = tensor(args[12]), *wk = tensor(args[13]);
+    const at::Tensor *positions = tensor(args[14]), *dq = tensor(args[16]), *dk = tensor(args[17]);
+    arrow_rotation_t a{};
+    if (!tensor.ok || !describe(a, x + 3, eps, q, k, wq, wk, positions, shift) || !gq || !gk || !like(*gq, *q) || !like(*gk, *k)) return 0;
+    if ((dq && !like(*dq, *q)) || (dk && !like(*dk, *k))) return 0;
+    out[0] = dq ? *dq : made(q->sizes(), *q, q->scalar_type());
+    out[1] = dk ? *dk : made(k->sizes(), *k, q->scalar_type());
+    a.q_out = steps(*gq); a.k_out = steps(*gk); a.dq = steps(out[0]); a.dk = steps(out[1]);
+    at::Tensor ws;
+    size_t bytes = 0;
+    if (wq) {
+      out[2] = made(wq->sizes(), *wq, wq->scalar_type());
+      out[3] = made(wk->sizes(), *wk, wk->scalar_type());
+      bytes = reinterpret_cast<decltype(&arrow_rotation_workspace_bytes)>(x[1])(&a);
+      ws = made({(int64_t)bytes}, *q, at::kByte);
+    }
+    void *gqp = data(*gq), *gkp = data(*gk), *qp = data(*q), *kp = data(*k), *dqp = data(out[0]), *dkp = data(out[1]);
+    void *wqp = wq ? data(*wq) : nullptr, *wkp = wk ? data(*wk) : nullptr, *dwqp = wq ? data(out[2]) : nullptr, *dwkp = wq ? data(out[3]) : nullptr;
+    void *wp = bytes ? data(ws) : nullptr, *stream = stream_of(x[2]);
+    rc = quietly([&] {
+      return reinterpret_cast<decltype(&arrow_rotation_backward)>(x[0])(&a, gqp, gkp, qp, kp, wqp, wkp, dqp, dkp, dwqp, dwkp, wp, bytes, stream);
+    });
+    return wq ? 4 : 2;
+  });
+}
+
+// ---- pages ----
+
+bool ints(const at::Tensor* t, at::ScalarType type, at::IntArrayRef shape) {
+  return t && t->scalar_type() == type && t->sizes() == shape && t->is_contiguous();
+}
+
+// pages_step(function, of the workspace's size, device, pages, page, window, sinks, table, held, free, lengths, tokens, offsets, slots)
+PyObject* pages_step(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[7], tokens;
+  if (!arguments(n_args, 14) || !integers(args, 7, x)) return nullptr;
+  if (!integers(args + 11, 1, &tokens)) { PyErr_Clear(); return none(); }
+  return results(x[2], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[2]};
+    const at::Tensor *table = tensor(args[7]), *held = tensor(args[8]), *list = tensor(args[9]), *lengths = tensor(args[10]), *offsets = tensor(args[12]);
+    const at::Tensor* slots = tensor(args[13]);
+    if (!tensor.ok || !small(tokens) || !table || table->dim() != 2 || !ints(table, at::kInt, table->sizes()) || !steps_fit(*table)) return 0;
+    const int64_t batch = table->size(0);
+    if (!ints(held, at::kInt, {batch}) || !ints(list, at::kInt, {1 + x[3]}) || !ints(lengths, at::kInt, {batch}) || (offsets && !ints(offsets, at::kInt, {batch + 1})))
+      return 0;
+    const at::DimVector shape = offsets ? at::DimVector{tokens} : at::DimVector{batch, tokens};
+    if (slots && !ints(slots, at::kLong, shape)) return 0;
+    out[0] = slots ? *slots : made(shape, *table, at::kLong);
+    arrow_pages_t a{};
+    a.batch = (int32_t)batch; a.columns = (int32_t)table->size(1); a.page = (int32_t)std::min<int64_t>(x[4], 0x7fffffff); a.pages = x[3];
+    a.window = (int32_t)x[5]; a.sinks = (int32_t)x[6];
+    if (offsets) { a.offsets = offsets->const_data_ptr<int32_t>(); a.rows = tokens; }
+    else a.tokens = (int32_t)tokens;
+    const size_t bytes = reinterpret_cast<decltype(&arrow_pages_workspace_bytes)>(x[1])(&a);
+    const at::Tensor ws = bytes ? made({(int64_t)bytes}, *table, at::kByte) : at::Tensor();
+    auto address = [](const at::Tensor* t) { return static_cast<int32_t*>(data(*t)); };
+    int32_t *tp = address(table), *hp = address(held), *fp = address(list), *lp = address(lengths);
+    void *sp = data(out[0]), *wp = bytes ? data(ws) : nullptr, *stream = stream_of(x[2]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_pages_step)>(x[0])(&a, lp, hp, tp, fp, static_cast<int64_t*>(sp), wp, bytes, stream); });
+    return 1;
+  });
+}
+
+// ---- the cache in 4 bits ----
+
+bool describe(arrow_packed_t& c, const at::Tensor* pool, int64_t dim, at::ScalarType type) {
+  if (!pool || (dim != 32 && dim != 64 && dim != 128) || (type != at::kBFloat16 && type != at::kHalf)) return false;
+  const int64_t size = dim + dim / 16;
+  if (pool->scalar_type() != at::kByte || pool->dim() != 3 || pool->size(2) % size || !rows_whole(*pool) || !steps_fit(*pool)) return false;
+  auto step = [&](int64_t d) { return pool->size(d) > 1 ? pool->stride(d) : 0; };
+  c.dtype = type == at::kBFloat16 ? ARROW_BF16 : ARROW_F16;
+  c.pages = pool->size(0); c.kv_heads = (int32_t)pool->size(1); c.page = (int32_t)(pool->size(2) / size); c.dim = (int32_t)dim;
+  c.page_step = step(0); c.head_step = step(1);
+  return true;
+}
+
+// Steps of (rows, heads, dim).
+arrow_strides_t row_steps(const at::Tensor* t) {
+  if (!t) return {};
+  const int64_t row = t->size(0) > 1 ? t->stride(0) : 0;
+  return {row, row, t->size(1) > 1 ? t->stride(1) : 0};
+}
+
+bool is_rows(const at::Tensor* t, at::IntArrayRef shape, at::ScalarType type) {
+  return t && t->scalar_type() == type && t->sizes() == shape && (t->stride(-1) == 1 || t->numel() == 0);
+}
+
+// packed_append(function, device, k, v, pool, slots): the pool
+PyObject* packed_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[2];
+  if (!arguments(n_args, 6) || !integers(args, 2, x)) return nullptr;
+  return results(x[1], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[1]};
+    const at::Tensor *k = tensor(args[2]), *v = tensor(args[3]), *pool = tensor(args[4]), *slots = tensor(args[5]);
+    arrow_packed_t c{};
+    if (!tensor.ok || !k || !v || k->dim() != 3 || !describe(c, pool, k->size(2), k->scalar_type())) return 0;
+    if (!slots || slots->dim() != 1 || !ints(slots, at::kLong, slots->sizes())) return 0;
+    const int64_t shape[] = {slots->size(0), c.kv_heads, c.dim};
+    if (!is_rows(k, shape, k->scalar_type()) || !is_rows(v, shape, k->scalar_type())) return 0;
+    out[0] = *pool;
+    const arrow_strides_t ks = row_steps(k), vs = row_steps(v);
+    void *kp = data(*k), *vp = data(*v), *pp = data(*pool), *sp = data(*slots), *stream = stream_of(x[1]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_packed_append)>(x[0])(&c, shape[0], kp, vp, ks, vs, (const int64_t*)sp, pp, stream); });
+    return 1;
+  });
+}
+
+// packed_read(function, device, pool, slots, dim, dtype, k, v)
+PyObject* packed_read(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[2], dim;
+  if (!arguments(n_args, 8) || !integers(args, 2, x)) return nullptr;
+  if (!integers(args + 4, 1, &dim)) { PyErr_Clear(); return none(); }
+  if (!THPDtype_Check(args[5])) return none();
+  const at::ScalarType type = reinterpret_cast<THPDtype*>(args[5])->scalar_type;
+  return results(x[1], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[1]};
+    const at::Tensor *pool = tensor(args[2]), *slots = tensor(args[3]), *k = tensor(args[6]), *v = tensor(args[7]);
+    arrow_packed_t c{};
+    if (!tensor.ok || !describe(c, pool, dim, type) || !slots || slots->dim() != 1 || !ints(slots, at::kLong, slots->sizes())) return 0;
+    const int64_t shape[] = {slots->size(0), c.kv_heads, c.dim};
+    if ((k && !is_rows(k, shape, type)) || (v && !is_rows(v, shape, type))) return 0;
+    out[0] = k ? *k : made(shape, *pool, type);
+    out[1] = v ? *v : made(shape, *pool, type);
+    const arrow_strides_t ks = row_steps(&out[0]), vs = row_steps(&out[1]);
+    void *kp = data(out[0]), *vp = data(out[1]), *pp = data(*pool), *sp = data(*slots), *stream = stream_of(x[1]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_packed_read)>(x[0])(&c, shape[0], (const int64_t*)sp, pp, kp, vp, ks, vs, stream); });
+    return 2;
+  });
+}
+
+// packed_decode(function, of the workspace's size, device, window, sinks, scale or -1, q, pool, table, lengths, max_len, k, v, o)
+PyObject* packed_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[5], max_len;
+  if (!arguments(n_args, 14) || !integers(args, 5, x)) return nullptr;
+  const double scale = PyFloat_AsDouble(args[5]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!lengths(args + 10, 1, &max_len)) return none();
+  return results(x[2], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[2]};
+    const at::Tensor *q = tensor(args[6]), *pool = tensor(args[7]), *table = tensor(args[8]), *n = tensor(args[9]);
+    const at::Tensor *k = tensor(args[11]), *v = tensor(args[12]), *o = tensor(args[13]);
+    arrow_packed_t c{};
+    if (!tensor.ok || !q || !table || !n || !k != !v || q->dim() != 3 || !describe(c, pool, q->size(2), q->scalar_type())) return 0;
+    if (table->dim() != 2 || !ints(table, at::kInt, table->sizes()) || !ints(n, at::kInt, {q->size(0)}) || table->size(0) != q->size(0)) return 0;
+    const int64_t own[] = {q->size(0), c.kv_heads, c.dim};
+    if (!is_rows(q, q->sizes(), q->scalar_type()) || (o && !is_rows(o, q->sizes(), q->scalar_type()))) return 0;
+    if ((k && !is_rows(k, own, q->scalar_type())) || (v && !is_rows(v, own, q->scalar_type())) || !steps_fit(*table) || !steps_fit(*q)) return 0;
+    c.batch = (int32_t)table->size(0); c.columns = (int32_t)table->size(1);
+    c.q_heads = (int32_t)q->size(1);
+    c.window = (int32_t)x[3]; c.sinks = (int32_t)x[4];
+    c.scale = (float)(scale >= 0 ? scale : 1.0 / std::sqrt((double)c.dim));
+    c.max_len = max_len >= 0 ? max_len : (int64_t)c.columns * c.page;
+    c.table = table->const_data_ptr<int32_t>(); c.lengths = n->const_data_ptr<int32_t>();
+    out[0] = o ? *o : made(q->sizes(), *q, q->scalar_type());
+    const arrow_strides_t qs = row_steps(q), ks = row_steps(k), vs = row_steps(v), os = row_steps(&out[0]);
+    const size_t bytes = reinterpret_cast<decltype(&arrow_packed_decode_workspace_bytes)>(x[1])(&c);
+    const at::Tensor ws = bytes ? made({(int64_t)bytes}, *q, at::kByte) : at::Tensor();
+    void *qp = data(*q), *kp = k ? data(*k) : nullptr, *vp = v ? data(*v) : nullptr, *pp = data(*pool), *op = data(out[0]);
+    void *wp = bytes ? data(ws) : nullptr, *stream = stream_of(x[2]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_packed_decode)>(x[0])(&c, qp, qs, kp, vp, ks, vs, pp, op, os, wp, bytes, stream); });
+    return 1;
+  });
+}
+
+// ---- log probabilities ----
+
+// Logits (or their gradient) as rows that lie evenly apart; 0: not so.
+int64_t row_step(const at::Tensor& t, int64_t rows) {
+  const int64_t n = t.size(-1);
+  if (!rows_whole(t)) return 0;
+  if (rows <= 1) return n;
+  if (t.dim() == 2) return t.stride(0);
+  return t.is_contiguous() ? n : 0;
+}
+
+bool describe(arrow_logprobs_t& a, const at::Tensor* logits, const at::Tensor* targets, double scale) {
+  if (!logits || !targets || any_type(*logits) < 0 || logits->dim() < 1 || logits->dim() != targets->dim() + 1) return false;
+  if ((targets->scalar_type() != at::kInt && targets->scalar_type() != at::kLong) || !targets->is_contiguous()) return false;
+  if (logits->sizes().slice(0, targets->dim()) != targets->sizes() || logits->size(-1) < 1 || logits->size(-1) > (1 << 30)) return false;
+  a.dtype = any_type(*logits);
+  a.target_bytes = targets->scalar_type() == at::kLong ? 8 : 4;
+  a.vocabulary = (int32_t)logits->size(-1);
+  a.rows = targets->numel();
+  a.stride = row_step(*logits, a.rows);
+  a.scale = (float)scale;
+  return a.stride != 0;
+}
+
+// logprobs_forward(function, of the workspace's size, device, scale, logits, targets, top): logp, entropy, lse, stats and, with top, top_logp, top_ids
+PyObject* logprobs_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[3], top;
+  if (!arguments(n_args, 7) || !integers(args, 3, x)) return nullptr;
+  const double scale = PyFloat_AsDouble(args[3]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!integers(args + 6, 1, &top)) { PyErr_Clear(); return none(); }
+  return results(x[2], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[2]};
+    const at::Tensor *logits = tensor(args[4]), *targets = tensor(args[5]);
+    arrow_logprobs_t a{};
+    if (!tensor.ok || !describe(a, logits, targets, scale) || top < 0 || top > 32 || top > a.vocabulary) return 0;
+    a.top = (int32_t)top;
+    for (int i = 0; i < 3; ++i) out[i] = made(targets->sizes(), *logits, at::kFloat);
+    out[3] = made(with(targets->sizes(), 2), *logits, at::kFloat);
+    if (top) {
+      out[4] = made(with(targets->sizes(), top), *logits, at::kFloat);
+      out[5] = made(with(targets->sizes(), top), *logits, at::kLong);
+    }
+    const size_t bytes = reinterpret_cast<decltype(&arrow_logprobs_workspace_bytes)>(x[1])(&a);
+    const at::Tensor ws = bytes ? made({(int64_t)bytes}, *logits, at::kByte) : at::Tensor();
+    float* p[5] = {};
+    for (int i = 0; i < (top ? 5 : 4); ++i) p[i] = static_cast<float*>(data(out[i]));
+    void *xp = data(*logits), *tp = data(*targets), *ip = top ? data(out[5]) : nullptr, *wp = bytes ? data(ws) : nullptr, *stream = stream_of(x[2]);
+    rc = quietly([&] {
+      return reinterpret_cast<decltype(&arrow_logprobs_forward)>(x[0])(&a, xp, tp, p[0], p[1], p[2], p[3], p[4], static_cast<int64_t*>(ip), wp, bytes, stream);
+    });
+    return top ? 6 : 4;
+  });
+}
+
+// logprobs_backward(function, device, scale, d_logp, d_entropy, logits, targets, stats, entropy, d_logits)
+PyObject* logprobs_backward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  int64_t x[2];
+  if (!arguments(n_args, 10) || !integers(args, 2, x)) return nullptr;
+  const double scale = PyFloat_AsDouble(args[2]);
+  if (PyErr_Occurred()) return nullptr;
+  return results(x[1], [&](at::Tensor* out, int& rc) {
+    Tensors tensor{x[1]};
+    const at::Tensor *d_logp = tensor(args[3]), *d_entropy = tensor(args[4]), *logits = tensor(args[5]), *targets = tensor(args[6]), *stats = tensor(args[7]);
+    const at::Tensor *entropy = tensor(args[8]), *to = tensor(args[9]);
+    arrow_logprobs_t a{};
+    if (!tensor.ok || !describe(a, logits, targets, scale) || (d_entropy && !entropy) || !ints(stats, at::kFloat, with(targets->sizes(), 2))) return 0;
+    for (auto* t : {d_logp, d_entropy, entropy})
+      if (t && !ints(t, at::kFloat, targets->sizes())) return 0;
+    if (to && (to->scalar_type() != logits->scalar_type() || to->sizes() != logits->sizes())) return 0;
+    out[0] = to ? *to : made(logits->sizes(), *logits, logits->scalar_type());
+    a.d_stride = row_step(out[0], a.rows);
+    if (a.d_stride == 0) return 0;
+    auto address = [](const at::Tensor* t) { return t ? static_cast<const float*>(t->const_data_ptr()) : nullptr; };
+    const float *gp = address(d_logp), *hp = address(d_entropy), *sp = address(stats), *ep = address(entropy);
+    void *xp = data(*logits), *tp = data(*targets), *op = data(out[0]), *stream = stream_of(x[1]);
+    rc = quietly([&] { return reinterpret_cast<decltype(&arrow_logprobs_backward)>(x[0])(&a, gp, hp, xp, tp, sp, ep, op, stream); });
+    return 1;
+  });
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -401,7 +721,11 @@ PyMethodDef method(const char* name) {
 PyMethodDef methods[] = {method<spmm>("spmm"), method<sddmm>("sddmm"), method<mttkrp>("mttkrp"),
                          method<attention_forward>("attention_forward"), method<attention_backward>("attention_backward"),
                          method<attention_decode>("attention_decode"), method<embedding_forward>("embedding_forward"),
-                         method<embedding_backward>("embedding_backward"), {nullptr, nullptr, 0, nullptr}};
+                         method<embedding_backward>("embedding_backward"),
+                         method<rotation_forward>("rotation_forward"), method<rotation_backward>("rotation_backward"),
+                         method<pages_step>("pages_step"), method<packed_append>("packed_append"), method<packed_read>("packed_read"),
+                         method<packed_decode>("packed_decode"), method<logprobs_forward>("logprobs_forward"),
+                         method<logprobs_backward>("logprobs_backward"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "tensor_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,175 @@
+"""Page tables and slot maps against a simulation on lists: every number has to be the same."""
+import random
+
+import pytest
+
+from oracle import operators_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: these tests need a real MI355X")
+    return torch
+
+
+@pytest.fixture(scope="module")
+def Pages(torch):
+    from paper_2307_05740_amd.pages import ArrowPages
+    return ArrowPages
+
+
+class Both:
+    """The operator and the simulation, side by side."""
+
+    def __init__(self, torch, Pages, pages, page, window, sinks, batch, columns):
+        self.torch = torch
+        self.op = Pages(pages, page, window, sinks)
+        self.table, self.held, self.free = self.op.state(batch, columns)
+        self.sim = oracle.Pages(pages, page, window, sinks, batch, columns)
+
+    def ints(self, x, dtype="int32"):
+        return self.torch.tensor(x, dtype=getattr(self.torch, dtype), device="cuda")
+
+    def compare(self):
+        assert self.table.tolist() == self.sim.table
+        assert self.held.tolist() == self.sim.held
+        free = self.free.tolist()
+        assert free[0] == len(self.sim.stack) and free[1:1 + free[0]] == self.sim.stack
+
+    def step(self, lengths, tokens):
+        """`tokens` new ones of each sequence."""
+        want = self.sim.step(lengths, [tokens] * len(lengths))
+        got = self.op.step(self.table, self.held, self.free, self.ints(lengths), tokens)
+        assert (got is None) == (tokens == 0)
+        if tokens:
+            assert got.tolist() == want
+        self.compare()
+
+    def ragged(self, lengths, fresh, before=0, behind=0):
+        """New tokens of each sequence, with rows that none has before and behind them."""
+        want = self.sim.step(lengths, fresh)
+        offsets = [before]
+        for n in fresh:
+            offsets.append(offsets[-1] + n)
+        total = offsets[-1] + behind
+        got = self.op.step(self.table, self.held, self.free, self.ints(lengths), total, self.ints(offsets), self.torch.full((total,), 77, device="cuda"))
+        flat = [-1] * before + [s for own in want for s in own] + [-1] * behind
+        assert (got.tolist() if total else []) == flat
+        self.compare()
+
+
+@pytest.mark.parametrize("page", [1, 16, 64])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (40, 4), (100, 70), (64, 200), (5000, 3)])
+@pytest.mark.parametrize("batch", [1, 7, 70])
+def test_a_life_of_sequences(torch, Pages, page, window, sinks, batch):
+    """Sequences that come, grow by a token, by drafts that are taken back, by prompts, and go, in a pool that runs out now and then."""
+    rng = random.Random(page * 1000 + window + batch)
+    columns = -(-600 // page)
+    both = Both(torch, Pages, max(4, batch * columns // 3), page, window, sinks, batch, columns)
+    lengths = [0] * batch
+    for turn in range(12):
+        kind = rng.choice(("one", "drafts", "prompts", "end", "ragged"))
+        if kind == "one":
+            lengths = [n + 1 if n else 0 for n in lengths]
+            both.step(lengths, 1)
+        elif kind == "drafts":
+            more = rng.randint(2, 9)
+            both.step([n + more for n in lengths], more)
+            lengths = [n + rng.randint(0, more) for n in lengths]
+            both.step(lengths, 0)
+        elif kind == "prompts":
+            fresh = [rng.randint(0, 300) if n == 0 or rng.random() < 0.3 else 0 for n in lengths]
+            lengths = [min(600, n + f) for n, f in zip(lengths, fresh)]
+            both.ragged(lengths, fresh, rng.randint(0, 3), rng.randint(0, 3))
+        elif kind == "end":
+            lengths = [0 if rng.random() < 0.4 else n for n in lengths]
+            both.step(lengths, 0)
+        else:
+            fresh = [rng.randint(0, 40) for _ in lengths]
+            lengths = [n + f for n, f in zip(lengths, fresh)]     # (some beyond the table's row)
+            both.ragged(lengths, fresh)
+    both.step([0] * batch, 0)
+
+
+@pytest.mark.parametrize("batch,most", [(1, 9000), (3, 20000), (1024, 9), (1025, 9), (1300, 40), (5000, 3), (200, 2000)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (33, 20)])
+def test_steps_of_one_launch_and_of_several(torch, Pages, batch, most, window, sinks):
+    rng = random.Random(batch)
+    page = 16
+    lengths = [rng.randint(0, most) for _ in range(batch)]
+    both = Both(torch, Pages, sum(-(-n // page) for n in lengths) + batch, page, window, sinks, batch, -(-most // page) + 1)
+    both.ragged(lengths, lengths, 2, 5)
+    lengths = [n + 1 for n in lengths]
+    both.step(lengths, 1)
+    lengths = [n + rng.randint(-min(3, n), 9) for n in lengths]
+    both.step(lengths, 9)
+    both.step([0 if rng.random() < 0.5 else n for n in lengths], 0)
+    both.step([0] * batch, 0)
+    free = both.free.tolist()                                     # (all pages, in the order that they came back in)
+    assert free[0] == both.op.pages and sorted(free[1:]) == list(range(both.op.pages))
+
+
+def test_there_and_back(torch, Pages):
+    """The list is as it was, in order too."""
+    both = Both(torch, Pages, 500, 16, 0, 0, 8, 100)
+    lengths = [100, 3, 0, 77, 160, 16, 15, 17]
+    both.ragged(lengths, lengths)
+    table, free = both.table.clone(), both.free.clone()
+    for more in (1, 5, 40):
+        both.step([n + more for n in lengths], more)
+        both.step(lengths, 0)
+        assert torch.equal(both.table, table) and torch.equal(both.free, free)
+
+
+def test_numbers_out_of_range(torch, Pages):
+    """Lengths, entries and a list that are not what they should be are cut to what there is: nothing outside is touched."""
+    op = Pages(20, 16)
+    room = torch.full((3, 6 + 2), 77, dtype=torch.int32, device="cuda")
+    table = torch.full((3, 6), -1, dtype=torch.int32, device="cuda")
+    held = torch.tensor([2**31 - 1, -7, 40], dtype=torch.int32, device="cuda")
+    table[0] = torch.tensor([5, 99, -3, 6, 2**31 - 1, 7])
+    free = torch.tensor([1000] + list(range(20)), dtype=torch.int32, device="cuda")
+    n = torch.tensor([-2**31, 2**31 - 1, 30], dtype=torch.int32, device="cuda")
+    slots = op.step(table, held, free, n, 3)
+    assert bool((slots[:2] == -1).all()) and 0 <= int(free[0]) <= 20
+    assert bool((table[0] == -1).all()) and held.tolist() == n.tolist()
+    for offsets in ([-5, 3, 2**31 - 1, 9], [9, 2, 1, 0], [100, 100, 100, 100]):
+        got = op.step(table, held, free, torch.tensor([10, 20, 30], dtype=torch.int32, device="cuda"), 7, torch.tensor(offsets, dtype=torch.int32, device="cuda"))
+        assert got.shape == (7,) and bool((got >= -1).all()) and bool((got < 20 * 16).all())
+    assert bool((room == 77).all())
+
+
+def test_captured(torch, Pages):
+    """A graph of a token for each sequence, replayed, beside eager steps of the same."""
+    both = Both(torch, Pages, 400, 16, 48, 4, 5, 60)
+    lengths = [30, 0, 47, 100, 16]
+    both.ragged(lengths, lengths)
+    other = [t.clone() for t in (both.table, both.held, both.free)]
+    n, slots = both.ints(lengths), torch.zeros(5, 1, dtype=torch.int64, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        n += 1
+        both.op.step(both.table, both.held, both.free, n, 1, slots=slots)
+    for _ in range(70):
+        graph.replay()
+        lengths = [x + 1 for x in lengths]
+        got = both.op.step(*other, both.ints(lengths), 1)
+        assert slots.tolist() == got.tolist() == both.sim.step(lengths, [1] * 5)
+        both.compare()
+
+
+def test_nothing_to_do(torch, Pages):
+    op = Pages(10, 16)
+    table, held, free = op.state(0, 5)
+    assert op.step(table, held, free, held.clone(), 0) is None
+    assert op.step(table, held, free, held.clone(), 4).shape == (0, 4)
+    assert op.step(table, held, free, held.clone(), 3, torch.zeros(1, dtype=torch.int32, device="cuda")).tolist() == [-1, -1, -1]
+    table, held, free = op.state(3, 0)
+    assert op.step(table, held, free, torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda"), 1).tolist() == [[-1]] * 3
+    none = Pages(0, 16)
+    table, held, free = none.state(2, 3)
+    assert none.step(table, held, free, torch.tensor([5, 0], dtype=torch.int32, device="cuda"), 1).tolist() == [[-1]] * 2 and int(free[0]) == 0
