@@ -88,15 +88,10 @@ __device__ __forceinline__ Sums exchanged(const Sums& x, int mask) { return {__s
 struct Stats {
   float M, log, entropy;                                           // log: of sum exp(scale (x - M))
   __device__ __forceinline__ explicit Stats(const Sums& x) : M(x.M) {
-    if (M == minus_infinity()) {
-      log = entropy = 0.f;
-    } else if (!(M < __builtin_inff())) {
-      log = entropy = __builtin_nanf("");
-    } else {
-      const float two = __builtin_amdgcn_logf(x.s);                // (base 2)
-      log = two * kLn2;
-      entropy = (two - x.w / x.s) * kLn2;
-    }
+    const bool empty = M == minus_infinity(), odd = !(M < __builtin_inff());
+    const float two = __builtin_amdgcn_logf(x.s), nan = __builtin_nanf("");       // (base 2)
+    log = empty ? 0.f : odd ? nan : two * kLn2;
+    entropy = empty ? 0.f : odd ? nan : (two - x.w / x.s) * kLn2;
   }
   __device__ __forceinline__ float lse(float scale) const { return fmaf(M, scale, log); }
   __device__ __forceinline__ float of(float logit, float scale) const { return M == minus_infinity() ? M : fmaf(logit - M, scale, -log); }
@@ -202,22 +197,51 @@ __device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i
   p.top_logp[row * p.a.top + i] = s.of(value_of(key), p.a.scale);
 }
 
+// Sums of a lane's logits.  Relative to R = M c rounded, c = scale log2 e, a product and a sum are one instruction; what R is off by is taken out of the sums at the end.
+// kForm 0: that.  1: the same with exponents cut off, for pieces that are filled up with -infinity, and rows that have some: 0 times an infinity is none.
+// 2: differences from M itself, where M c is so large that R is off by too much.
+struct LaneSums {
+  float M, c, R, s = 0.f, w = 0.f;
+  __device__ __forceinline__ LaneSums(float most, float by) : M(most), c(by), R(most * by) {}
+  template <int kForm>
+  __device__ __forceinline__ void add(float x) {
+    float d = kForm == 2 ? (x - M) * c : fmaf(x, c, -R);
+    if (kForm) d = fmaxf(d, kLeast);
+    const float e = __builtin_amdgcn_exp2f(d);
+    s += e;
+    w = fmaf(e, d, w);
+  }
+  template <int kForm, typename T>
+  __device__ __forceinline__ void add(const u32x4& x) {
+#pragma unroll
+    for (int i = 0; i < Piece<T>::kEach; ++i) add<kForm>(Piece<T>::get(x, i));
+  }
+  __device__ __forceinline__ bool plain() const { return fabsf(R) < 1048576.f; }     // (R is off by less than 1/16; not NaN, nor infinite)
+  // of the wavefront
+  __device__ __forceinline__ Sums joined() {
+    for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); w += __shfl_xor(w, m, 64); }
+    const float off = plain() ? fmaf(M, c, -R) : 0.f, by = __builtin_amdgcn_exp2f(-off);
+    return {M, s * by, fmaf(-off, s, w) * by};
+  }
+};
+
+// N pieces a lane.
 template <typename T, int N, bool kTop>
 __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   using P = Piece<T>;
   __shared__ Sums waves[kWaves];
   __shared__ std::conditional_t<kTop, Chosen, int> chosen;
-  const int tid = threadIdx.x, part = (int)(blockIdx.x % (unsigned)p.parts);
+  const int tid = threadIdx.x, part = (int)(blockIdx.x % (unsigned)p.parts), lead = 64 * wave_id();
   const int64_t row = blockIdx.x / (unsigned)p.parts;
   const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
-  const int first = part * p.vectors, end = min(first + p.vectors, r.pieces);
+  const int first = part * p.vectors, pieces = min(p.vectors, r.pieces - first);      // (of this part; may be none)
+  const u32x4* at = r.piece(first);
 
   u32x4 x[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int i = first + j * kThreads + tid;
     x[j] = u32x4{P::kNothing, P::kNothing, P::kNothing, P::kNothing};
-    if (i < end) x[j] = *r.piece(i);
+    if (j * kThreads + tid < pieces) x[j] = at[j * kThreads + tid];
   }
   const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
   const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity();
@@ -233,21 +257,31 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   const float mine = all;
   for (int m = 32; m; m >>= 1) all = larger(all, __shfl_xor(all, m, 64));
   const float c = p.a.scale * kLog2e;
-  Sums sum{all, 0.f, 0.f};
-  auto count = [&](float v) {
-    const float d = fmaxf((v - sum.M) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
-    sum.s += e;
-    sum.w = fmaf(e, d, sum.w);
-  };
+  LaneSums lane(all, c);
+  if (lane.plain()) {
 #pragma unroll
-  for (int j = 0; j < N; ++j)
+    for (int j = 0; j < N; ++j) {
+      const int end = pieces - j * kThreads - lead;       // (of this wavefront's 64 pieces)
+      x[j] = here(x[j]);                                  // (not kept as 32-bit numbers from above)
+      if (end >= 64) lane.template add<0, T>(x[j]);
+      else if (end > 0) lane.template add<1, T>(x[j]);
+    }
+    if (edge >= 0) lane.template add<1>(beside);
+    if (__any(lane.w != lane.w)) {                        // (a logit of -infinity)
+      lane.s = lane.w = 0.f;
 #pragma unroll
-    for (int i = 0; i < P::kEach; ++i) count(P::get(x[j], i));
-  count(beside);
-  for (int m = 32; m; m >>= 1) { sum.s += __shfl_xor(sum.s, m, 64); sum.w += __shfl_xor(sum.w, m, 64); }
-  if ((tid & 63) == 0) waves[tid >> 6] = sum;
+      for (int j = 0; j < N; ++j) lane.template add<1, T>(here(x[j]));
+      lane.template add<1>(beside);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) lane.template add<2, T>(here(x[j]));
+    lane.template add<2>(beside);
+  }
+  const Sums of_wave = lane.joined();
+  if ((tid & 63) == 0) waves[tid >> 6] = of_wave;
   __syncthreads();
-  sum = waves[0];
+  Sums sum = waves[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
   if (p.parts > 1 && tid == 0) *(f32x4*)(p.sums + (row * p.parts + part) * 4) = f32x4{sum.M, sum.s, sum.w, 0.f};
@@ -255,36 +289,44 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   if (p.parts == 1 && tid == 0) write_row<T>(p, row, s);
 
   if constexpr (kTop) {
-    // the lane's largest key: its piece is read again for the index
+    // the lane's largest key: its piece is taken, or read again, for the index
+    constexpr bool kHeld = N <= 2;
     uint64_t key = 0;
-    int at = -1;
-    const float sought = mine;
     auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
-#pragma unroll
-    for (int j = N - 1; j >= 0; --j)
-      if (first + j * kThreads + tid < end && alike(most[j], sought)) at = first + j * kThreads + tid;
-    if (at >= 0) {
-      const u32x4 v = *r.piece(at);
+    auto look = [&](const u32x4& v, int piece) {
 #pragma unroll
       for (int i = P::kEach - 1; i >= 0; --i)
-        if (alike(P::get(v, i), sought)) key = key_of(sought, r.index(at, i));
-    }
+        if (alike(P::get(v, i), mine)) key = key_of(mine, r.index(piece, i));
+    };
+    int found = -1;
+#pragma unroll
+    for (int j = N - 1; j >= 0; --j)
+      if (j * kThreads + tid < pieces && alike(most[j], mine)) {
+        if (kHeld) look(x[j], first + j * kThreads + tid);
+        else found = j * kThreads + tid;
+      }
+    if (!kHeld && found >= 0) look(at[found], first + found);
     if (edge >= 0) {
       const uint64_t k = key_of(beside, edge);
       key = k > key ? k : key;
     }
     const uint64_t border = border_of(key, p.a.top, chosen);
     if (edge >= 0) put(key_of(beside, edge), border, chosen);
+    auto put_all = [&](const u32x4& v, int piece) {
+#pragma unroll
+      for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(piece, e)), border, chosen);
+    };
     uint32_t near = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (first + j * kThreads + tid < end && key_of(most[j], 0) >= border) near |= 1u << j;
+      if (j * kThreads + tid < pieces && key_of(most[j], 0) >= border) {
+        if (kHeld) put_all(x[j], first + j * kThreads + tid);
+        else near |= 1u << j;
+      }
     while (near) {
-      const int i = first + __builtin_ctz(near) * kThreads + tid;
+      const int i = __builtin_ctz(near) * kThreads + tid;
       near &= near - 1;
-      const u32x4 v = *r.piece(i);
-#pragma unroll
-      for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(i, e)), border, chosen);
+      put_all(at[i], first + i);
     }
     place(
         p.a.top, chosen,
@@ -294,12 +336,12 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
         },
         [&](uint64_t last) {
           uint64_t best = 0;
-          auto look = [&](uint64_t k) { best = k < last && k > best ? k : best; };
-          if (edge >= 0) look(key_of(beside, edge));
-          for (int i = first + tid; i < end; i += kThreads) {
-            const u32x4 v = *r.piece(i);
+          auto next = [&](uint64_t k) { best = k < last && k > best ? k : best; };
+          if (edge >= 0) next(key_of(beside, edge));
+          for (int i = tid; i < pieces; i += kThreads) {
+            const u32x4 v = at[i];
 #pragma unroll
-            for (int e = 0; e < P::kEach; ++e) look(key_of(P::get(v, e), r.index(i, e)));
+            for (int e = 0; e < P::kEach; ++e) next(key_of(P::get(v, e), r.index(first + i, e)));
           }
           return best;
         });
