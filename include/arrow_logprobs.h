@@ -37,7 +37,7 @@ typedef struct arrow_logprobs_t {
 } arrow_logprobs_t;
 
 /*
- * logp, entropy, lse: fp32, rows each.  stats: fp32, rows x 2, 8-byte aligned, for the gradient: the largest logit, and lse less scale times that.  top_logp (fp32), top_ids (int64): rows x top, contiguous; NULL where top is 0.
+ * logp, entropy, lse: fp32, rows each.  stats: fp32, rows x 2, 8-byte aligned, for the gradient: a logit near the largest, and lse less scale times that.  top_logp (fp32), top_ids (int64): rows x top, contiguous; NULL where top is 0.
  * ws: DEVICE, 256-byte aligned, at least arrow_logprobs_workspace_bytes(a), which is 0 where rows are not cut; written, holds nothing between calls.
  * Errors: EINVAL, ETOOSMALL, EHIP.
  */

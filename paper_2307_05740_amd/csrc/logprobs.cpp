@@ -8,10 +8,10 @@
 namespace arrow {
 
 void plan_score(ScoreArgs& p) {
-  // Pieces of 16 bytes that a row reaches into, at any address.  A workgroup holds a part of a row in its registers; where there are few rows, they are cut
-  // further, down to a piece per lane.
+  // Pieces of 16 bytes that a row reaches into, at any address.  With most likely tokens a workgroup holds a part of a row in its registers; where there are few rows,
+  // they are cut further, down to a piece per lane.
   const int64_t each = 16 / size_of(p.a.dtype), pieces = ceil_div((int64_t)p.a.vocabulary, each) + 1;
-  const int64_t least = ceil_div(pieces, kScoreThreads * kMostVectors), most = ceil_div(pieces, kScoreThreads);
+  const int64_t least = p.a.top ? ceil_div(pieces, kScoreThreads * kMostVectors) : ceil_div(pieces, kMostPieces), most = ceil_div(pieces, kScoreThreads);
   const int64_t wanted = std::max<int64_t>(least, std::min<int64_t>(most, 512 / std::max<int64_t>(1, p.a.rows)));
   const int64_t rounds = ceil_div(pieces, wanted * kScoreThreads);           // pieces per lane
   p.parts = (int32_t)ceil_div(pieces, rounds * kScoreThreads);

@@ -63,7 +63,7 @@ struct Row {
   __device__ __forceinline__ int edge(int tid, int n) const { return tid < head ? tid : tid >= 8 && tid < 8 + rest ? n - rest + tid - 8 : -1; }
 };
 
-// Sums relative to the largest logit: with d = (x - M) scale in exponents of two, s = sum 2^d, w = sum 2^d d.  (The difference comes before the product, so that
+// Sums relative to a logit M near the largest: with d = (x - M) scale in exponents of two, s = sum 2^d, w = sum 2^d d.  (The difference comes before the product, so that
 // logits of any size, the type's lowest ones among them, are as exact as they are near to each other.)
 struct Sums {
   float M, s, w;
@@ -109,15 +109,23 @@ __device__ __forceinline__ float value_of(uint64_t key) {
   return u == 0xffffffffu ? __builtin_nanf("") : __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-// How many lanes' keys are larger than this one's.
-__device__ __forceinline__ int lanes_before(uint64_t key) {
-  int n = 0;
-#pragma unroll 8
-  for (int i = 0; i < 64; ++i) {
-    const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, i);
-    n += other > key;
+// The largest number that `count` or more of these lanes' are at least, from bit `bits` - 1 on below `base`; 0 bits more than there are lanes' numbers leave base.
+__device__ __forceinline__ uint32_t nth_of(uint32_t x, uint64_t lanes, int count, uint32_t base, int bits) {
+  for (int b = bits - 1; b >= 0; --b) {
+    const uint32_t more = base | 1u << b;
+    base = __popcll(__ballot(x >= more) & lanes) >= count ? more : base;
   }
-  return n;
+  return base;
+}
+
+// The key that comes `count`-th among the lanes', 0 where there are fewer.  Indices have `bits` bits.
+__device__ __forceinline__ uint64_t nth_key(uint64_t key, int count, int bits) {
+  const uint32_t high = (uint32_t)(key >> 32), low = (uint32_t)key;
+  const uint32_t value = nth_of(high, ~(uint64_t)0, count, 0, 32);
+  if (value == 0) return 0;
+  const uint64_t tied = __ballot(high == value);
+  const int rest = count - __popcll(__ballot(high > value));
+  return (uint64_t)value << 32 | nth_of(low, tied, rest, ~0u << bits, bits);
 }
 
 struct Chosen {
@@ -128,17 +136,19 @@ struct Chosen {
 };
 
 // The border from every lane's largest key (0: it has none); all threads of the workgroup.
-__device__ __forceinline__ uint64_t border_of(uint64_t key, int top, Chosen& c) {
+__device__ __forceinline__ uint64_t border_of(uint64_t key, int top, int bits, Chosen& c) {
   if (threadIdx.x == 0) c.count = 0;
-  const uint64_t at = __ballot(lanes_before(key) == top - 1);   // (several lanes without a key have the same place, or none has it)
-  if ((threadIdx.x & 63) == 0) c.border[threadIdx.x >> 6] = 0;
-  if (at && (int)(threadIdx.x & 63) == __builtin_ctzll(at)) c.border[threadIdx.x >> 6] = key;
+  const uint64_t mine = nth_key(key, top, bits);
+  if ((threadIdx.x & 63) == 0) c.border[threadIdx.x >> 6] = mine;
   __syncthreads();
   uint64_t b = c.border[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) b = c.border[w] > b ? c.border[w] : b;
   return b;
 }
+
+// Bits of an index.
+__device__ __forceinline__ int index_bits(int vocabulary) { return 32 - __clz(vocabulary - 1 | 1); }
 
 __device__ __forceinline__ void put(uint64_t key, uint64_t border, Chosen& c) {
   if (key == 0 || key < border) return;
@@ -197,41 +207,138 @@ __device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i
   p.top_logp[row * p.a.top + i] = s.of(value_of(key), p.a.scale);
 }
 
-// Sums of a lane's logits.  Relative to R = M c rounded, c = scale log2 e, a product and a sum are one instruction; what R is off by is taken out of the sums at the end.
-// kForm 0: that.  1: the same with exponents cut off, for pieces that are filled up with -infinity, and rows that have some: 0 times an infinity is none.
-// 2: differences from M itself, where M c is so large that R is off by too much.
+// Sums of a lane's logits, as they come.  Relative to R = M c rounded, c = scale log2 e, a product and a sum are one instruction; what R is off by is taken out of
+// the sums at the end.  M is raised when a piece exceeds it by 2^8.  A logit of -infinity makes w NaN, as 0 times an infinity is: then, and where others are not finite or
+// too large, the wavefront goes through its pieces again, with exponents that are cut off.
 struct LaneSums {
-  float M, c, R, s = 0.f, w = 0.f;
-  __device__ __forceinline__ LaneSums(float most, float by) : M(most), c(by), R(most * by) {}
-  template <int kForm>
+  float M = -__builtin_inff(), c, R = 0.f, s = 0.f, w = 0.f;
+  __device__ __forceinline__ explicit LaneSums(float by) : c(by) {}
+  __device__ __forceinline__ void start(float most) { M = most; R = M * c; }
   __device__ __forceinline__ void add(float x) {
-    float d = kForm == 2 ? (x - M) * c : fmaf(x, c, -R);
-    if (kForm) d = fmaxf(d, kLeast);
-    const float e = __builtin_amdgcn_exp2f(d);
+    const float d = fmaf(x, c, -R), e = __builtin_amdgcn_exp2f(d);
     s += e;
     w = fmaf(e, d, w);
   }
-  template <int kForm, typename T>
-  __device__ __forceinline__ void add(const u32x4& x) {
-#pragma unroll
-    for (int i = 0; i < Piece<T>::kEach; ++i) add<kForm>(Piece<T>::get(x, i));
+  // (differences from M itself, for any M)
+  __device__ __forceinline__ void add_any(float x) {
+    const float d = fmaxf((x - M) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
+    s += e;
+    w = fmaf(e, d, w);
   }
-  __device__ __forceinline__ bool plain() const { return fabsf(R) < 1048576.f; }     // (R is off by less than 1/16; not NaN, nor infinite)
-  // of the wavefront
-  __device__ __forceinline__ Sums joined() {
-    for (int m = 32; m; m >>= 1) { s += __shfl_xor(s, m, 64); w += __shfl_xor(w, m, 64); }
-    const float off = plain() ? fmaf(M, c, -R) : 0.f, by = __builtin_amdgcn_exp2f(-off);
+  __device__ __forceinline__ bool exceeded(float most) const { return fmaf(most, c, -R) > 8.f; }
+  __device__ __forceinline__ void raise(float most) {
+    const float before = R;
+    start(most);
+    const float d = before - R, by = __builtin_amdgcn_exp2f(d);
+    w = by * fmaf(s, d, w);
+    s *= by;
+  }
+  // whether the sums are not what they should be: a logit that is not finite, or so large that R is off by too much (here by less than 1/16)
+  __device__ __forceinline__ bool failed() const { return !(fabsf(w) < __builtin_inff() && fabsf(R) < 1048576.f); }
+  __device__ __forceinline__ Sums exact() const {
+    const float off = M == minus_infinity() ? 0.f : fmaf(M, c, -R), by = __builtin_amdgcn_exp2f(-off);
     return {M, s * by, fmaf(-off, s, w) * by};
   }
 };
 
-// N pieces a lane.
-template <typename T, int N, bool kTop>
+// The sums of a wavefront, in all lanes.
+__device__ __forceinline__ Sums of_wave(Sums x, float c) {
+  float most = x.M;
+  for (int m = 32; m; m >>= 1) most = larger(most, __shfl_xor(most, m, 64));
+  x.raise(most, c);
+  for (int m = 32; m; m >>= 1) { x.s += __shfl_xor(x.s, m, 64); x.w += __shfl_xor(x.w, m, 64); }
+  return x;
+}
+
+// A part of a row, of any length: a lane has four pieces on their way.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
+  using P = Piece<T>;
+  constexpr int kAhead = 4;
+  __shared__ Sums waves[kWaves];
+  const int tid = threadIdx.x, part = (int)(blockIdx.x % (unsigned)p.parts);
+  const int64_t row = blockIdx.x / (unsigned)p.parts;
+  const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
+  const int first = part * p.vectors, pieces = min(p.vectors, r.pieces - first);      // (of this part; may be none)
+  const u32x4* at = r.piece(first);
+
+  const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
+  const float c = p.a.scale * kLog2e, beside = edge >= 0 ? (float)r.at[edge] : 0.f;
+  LaneSums lane(c);
+  auto add = [&](const u32x4& v) {
+    float most = P::get(v, 0);
+#pragma unroll
+    for (int e = 1; e < P::kEach; ++e) most = larger(most, P::get(v, e));
+    if (lane.exceeded(most)) lane.raise(most);
+#pragma unroll
+    for (int e = 0; e < P::kEach; ++e) lane.add(P::get(v, e));
+  };
+  // rounds of all lanes: nothing but the sums branches, and loads beyond the last round read it again
+  const int rounds = pieces / kThreads;
+  if (rounds > 0) {
+    auto load = [&](int j) { return at[min(j, rounds - 1) * kThreads + tid]; };
+    u32x4 x[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) x[j] = load(j);
+    lane.start(P::get(x[0], 0));
+    int j = 0;
+    for (; j + kAhead <= rounds; j += kAhead)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const u32x4 v = x[i];
+        x[i] = load(j + i + kAhead);
+        add(v);
+      }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (j + i < rounds) add(x[i]);
+  }
+  if (rounds * kThreads + tid < pieces) {
+    const u32x4 v = at[rounds * kThreads + tid];
+    if (rounds == 0) lane.start(P::get(v, 0));
+    add(v);
+  }
+  if (edge >= 0) {
+    if (tid >= pieces) lane.start(beside);
+    else if (lane.exceeded(beside)) lane.raise(beside);
+    lane.add(beside);
+  }
+  Sums lane_sums = lane.exact();
+  if (__any(lane.failed())) {
+    float most = edge >= 0 ? beside : minus_infinity();
+    for (int i = tid; i < pieces; i += kThreads) {
+      const u32x4 v = at[i];
+#pragma unroll
+      for (int e = 0; e < P::kEach; ++e) most = larger(most, P::get(v, e));
+    }
+    lane = LaneSums(c);
+    lane.M = most;
+    if (edge >= 0) lane.add_any(beside);
+    for (int i = tid; i < pieces; i += kThreads) {
+      const u32x4 v = at[i];
+#pragma unroll
+      for (int e = 0; e < P::kEach; ++e) lane.add_any(P::get(v, e));
+    }
+    lane_sums = {lane.M, lane.s, lane.w};
+  }
+  const Sums wave_sums = of_wave(lane_sums, c);
+  if ((tid & 63) == 0) waves[tid >> 6] = wave_sums;
+  __syncthreads();
+  if (tid) return;
+  Sums sum = waves[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
+  if (p.parts > 1) *(f32x4*)(p.sums + (row * p.parts + part) * 4) = f32x4{sum.M, sum.s, sum.w, 0.f};
+  else write_row<T>(p, row, Stats(sum));
+}
+
+// The same with the largest logits: a lane holds its N pieces.
+template <typename T, int N>
 __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   using P = Piece<T>;
   __shared__ Sums waves[kWaves];
-  __shared__ std::conditional_t<kTop, Chosen, int> chosen;
-  const int tid = threadIdx.x, part = (int)(blockIdx.x % (unsigned)p.parts), lead = 64 * wave_id();
+  __shared__ Chosen chosen;
+  const int tid = threadIdx.x, part = (int)(blockIdx.x % (unsigned)p.parts);
   const int64_t row = blockIdx.x / (unsigned)p.parts;
   const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
   const int first = part * p.vectors, pieces = min(p.vectors, r.pieces - first);      // (of this part; may be none)
@@ -246,40 +353,41 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
   const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity();
 
-  float most[N], all = beside;
+  // (the sums of a piece begin when it has come)
+  const float c = p.a.scale * kLog2e;
+  LaneSums lane(c);
+  float most[N], mine = beside;
+  if (edge >= 0) { lane.start(beside); lane.add(beside); }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
+    most[j] = minus_infinity();
+    if (j * kThreads + tid >= pieces) continue;
     most[j] = P::get(x[j], 0);
 #pragma unroll
     for (int i = 1; i < P::kEach; ++i) most[j] = larger(most[j], P::get(x[j], i));
-    all = larger(all, most[j]);
+    mine = larger(mine, most[j]);
+    if (j == 0 && edge < 0) lane.start(most[j]);
+    else if (lane.exceeded(most[j])) lane.raise(most[j]);
+#pragma unroll
+    for (int i = 0; i < P::kEach; ++i) lane.add(P::get(x[j], i));
   }
-  const float mine = all;
-  for (int m = 32; m; m >>= 1) all = larger(all, __shfl_xor(all, m, 64));
-  const float c = p.a.scale * kLog2e;
-  LaneSums lane(all, c);
-  if (lane.plain()) {
+  Sums lane_sums = lane.exact();
+  if (__any(lane.failed())) {
+    float all = mine;
+    for (int m = 32; m; m >>= 1) all = larger(all, __shfl_xor(all, m, 64));
+    lane = LaneSums(c);
+    lane.M = all;
+    lane.add_any(beside);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int end = pieces - j * kThreads - lead;       // (of this wavefront's 64 pieces)
-      x[j] = here(x[j]);                                  // (not kept as 32-bit numbers from above)
-      if (end >= 64) lane.template add<0, T>(x[j]);
-      else if (end > 0) lane.template add<1, T>(x[j]);
-    }
-    if (edge >= 0) lane.template add<1>(beside);
-    if (__any(lane.w != lane.w)) {                        // (a logit of -infinity)
-      lane.s = lane.w = 0.f;
+      const u32x4 again = here(x[j]);                     // (not kept as 32-bit numbers from above)
 #pragma unroll
-      for (int j = 0; j < N; ++j) lane.template add<1, T>(here(x[j]));
-      lane.template add<1>(beside);
+      for (int i = 0; i < P::kEach; ++i) lane.add_any(P::get(again, i));
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j) lane.template add<2, T>(here(x[j]));
-    lane.template add<2>(beside);
+    lane_sums = {lane.M, lane.s, lane.w};
   }
-  const Sums of_wave = lane.joined();
-  if ((tid & 63) == 0) waves[tid >> 6] = of_wave;
+  const Sums wave_sums = of_wave(lane_sums, c);
+  if ((tid & 63) == 0) waves[tid >> 6] = wave_sums;
   __syncthreads();
   Sums sum = waves[0];
 #pragma unroll
@@ -288,64 +396,63 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   const Stats s(sum);
   if (p.parts == 1 && tid == 0) write_row<T>(p, row, s);
 
-  if constexpr (kTop) {
-    // the lane's largest key: its piece is taken, or read again, for the index
-    constexpr bool kHeld = N <= 2;
-    uint64_t key = 0;
-    auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
-    auto look = [&](const u32x4& v, int piece) {
+  // the lane's largest key: its piece is taken, or read again, for the index
+  constexpr bool kHeld = N <= 2;
+  uint64_t key = 0;
+  auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
+  auto look = [&](const u32x4& v, int piece) {
 #pragma unroll
-      for (int i = P::kEach - 1; i >= 0; --i)
-        if (alike(P::get(v, i), mine)) key = key_of(mine, r.index(piece, i));
-    };
-    int found = -1;
+    for (int i = P::kEach - 1; i >= 0; --i)
+      if (alike(P::get(v, i), mine)) key = key_of(mine, r.index(piece, i));
+  };
+  int found = -1;
 #pragma unroll
-    for (int j = N - 1; j >= 0; --j)
-      if (j * kThreads + tid < pieces && alike(most[j], mine)) {
-        if (kHeld) look(x[j], first + j * kThreads + tid);
-        else found = j * kThreads + tid;
-      }
-    if (!kHeld && found >= 0) look(at[found], first + found);
-    if (edge >= 0) {
-      const uint64_t k = key_of(beside, edge);
-      key = k > key ? k : key;
+  for (int j = N - 1; j >= 0; --j)
+    if (j * kThreads + tid < pieces && alike(most[j], mine)) {
+      if (kHeld) look(x[j], first + j * kThreads + tid);
+      else found = j * kThreads + tid;
     }
-    const uint64_t border = border_of(key, p.a.top, chosen);
-    if (edge >= 0) put(key_of(beside, edge), border, chosen);
-    auto put_all = [&](const u32x4& v, int piece) {
-#pragma unroll
-      for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(piece, e)), border, chosen);
-    };
-    uint32_t near = 0;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j * kThreads + tid < pieces && key_of(most[j], 0) >= border) {
-        if (kHeld) put_all(x[j], first + j * kThreads + tid);
-        else near |= 1u << j;
-      }
-    while (near) {
-      const int i = __builtin_ctz(near) * kThreads + tid;
-      near &= near - 1;
-      put_all(at[i], first + i);
-    }
-    place(
-        p.a.top, chosen,
-        [&](int i, uint64_t k) {
-          if (p.parts > 1) p.keys[(row * p.parts + part) * p.a.top + i] = k;
-          else write_top(p, row, i, k, s);
-        },
-        [&](uint64_t last) {
-          uint64_t best = 0;
-          auto next = [&](uint64_t k) { best = k < last && k > best ? k : best; };
-          if (edge >= 0) next(key_of(beside, edge));
-          for (int i = tid; i < pieces; i += kThreads) {
-            const u32x4 v = at[i];
-#pragma unroll
-            for (int e = 0; e < P::kEach; ++e) next(key_of(P::get(v, e), r.index(first + i, e)));
-          }
-          return best;
-        });
+  if (!kHeld && found >= 0) look(at[found], first + found);
+  if (edge >= 0) {
+    const uint64_t k = key_of(beside, edge);
+    key = k > key ? k : key;
   }
+  const uint64_t border = border_of(key, p.a.top, index_bits(p.a.vocabulary), chosen);
+  if (edge >= 0) put(key_of(beside, edge), border, chosen);
+  auto put_all = [&](const u32x4& v, int piece) {
+#pragma unroll
+    for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(piece, e)), border, chosen);
+  };
+  const float least = value_of(border);                   // (0 stands for a number below all others)
+  uint32_t near = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (j * kThreads + tid < pieces && (border == 0 || !(most[j] < least))) {
+      if (kHeld) put_all(x[j], first + j * kThreads + tid);
+      else near |= 1u << j;
+    }
+  while (near) {
+    const int i = __builtin_ctz(near) * kThreads + tid;
+    near &= near - 1;
+    put_all(at[i], first + i);
+  }
+  place(
+      p.a.top, chosen,
+      [&](int i, uint64_t k) {
+        if (p.parts > 1) p.keys[(row * p.parts + part) * p.a.top + i] = k;
+        else write_top(p, row, i, k, s);
+      },
+      [&](uint64_t last) {
+        uint64_t best = 0;
+        auto next = [&](uint64_t k) { best = k < last && k > best ? k : best; };
+        if (edge >= 0) next(key_of(beside, edge));
+        for (int i = tid; i < pieces; i += kThreads) {
+          const u32x4 v = at[i];
+#pragma unroll
+          for (int e = 0; e < P::kEach; ++e) next(key_of(P::get(v, e), r.index(first + i, e)));
+        }
+        return best;
+      });
 }
 
 // The parts of a row.
@@ -374,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
   const int64_t n = (int64_t)p.parts * top;
   uint64_t key = 0;
   for (int i = tid; i < p.parts; i += kThreads) key = keys[(int64_t)i * top] > key ? keys[(int64_t)i * top] : key;
-  const uint64_t border = border_of(key, top, chosen);
+  const uint64_t border = border_of(key, top, index_bits(p.a.vocabulary), chosen);
   for (int64_t i = tid; i < n; i += kThreads) put(keys[i], border, chosen);
   place(
       top, chosen, [&](int i, uint64_t k) { write_top(p, row, i, k, s); },
@@ -452,17 +559,18 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int c
   }
 }
 
-template <typename T, bool kTop>
+template <typename T>
 int forward(const ScoreArgs& p, hipStream_t s) {
   const int64_t blocks = p.a.rows * p.parts;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(kThreads);
   const int n = p.vectors / kThreads;
-  if (n <= 1) score_kernel<T, 1, kTop><<<grid, block, 0, s>>>(p);
-  else if (n <= 2) score_kernel<T, 2, kTop><<<grid, block, 0, s>>>(p);
-  else if (n <= 4) score_kernel<T, 4, kTop><<<grid, block, 0, s>>>(p);
-  else if (n <= 8) score_kernel<T, 8, kTop><<<grid, block, 0, s>>>(p);
-  else score_kernel<T, 16, kTop><<<grid, block, 0, s>>>(p);
+  if (p.a.top == 0) score_sums_kernel<T><<<grid, block, 0, s>>>(p);
+  else if (n <= 1) score_kernel<T, 1><<<grid, block, 0, s>>>(p);
+  else if (n <= 2) score_kernel<T, 2><<<grid, block, 0, s>>>(p);
+  else if (n <= 4) score_kernel<T, 4><<<grid, block, 0, s>>>(p);
+  else if (n <= 8) score_kernel<T, 8><<<grid, block, 0, s>>>(p);
+  else score_kernel<T, 16><<<grid, block, 0, s>>>(p);
   if (p.parts > 1) score_join_kernel<T><<<dim3((unsigned)p.a.rows), block, 0, s>>>(p);
   return (int)hipGetLastError();
 }
@@ -480,10 +588,7 @@ int backward(const ScoreArgs& p, hipStream_t s) {
 
 int launch_score_forward(const ScoreArgs& p, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  const bool top = p.a.top > 0;
-  if (p.a.dtype == ARROW_F32) return top ? forward<float, true>(p, s) : forward<float, false>(p, s);
-  if (p.a.dtype == ARROW_BF16) return top ? forward<__bf16, true>(p, s) : forward<__bf16, false>(p, s);
-  return top ? forward<_Float16, true>(p, s) : forward<_Float16, false>(p, s);
+  return p.a.dtype == ARROW_F32 ? forward<float>(p, s) : p.a.dtype == ARROW_BF16 ? forward<__bf16>(p, s) : forward<_Float16>(p, s);
 }
 
 int launch_score_backward(const ScoreArgs& p, void* stream) {

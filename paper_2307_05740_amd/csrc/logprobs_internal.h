@@ -11,6 +11,7 @@ namespace arrow {
 constexpr int kScoreThreads = 256;
 constexpr int kMostTop = 32;
 constexpr int kMostVectors = 16;       // pieces of 16 bytes of a row that a lane holds
+constexpr int64_t kMostPieces = 1 << 26; // of a part of a row that is not held
 
 struct ScoreArgs {
   arrow_logprobs_t a;
