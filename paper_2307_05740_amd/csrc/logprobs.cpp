@@ -12,7 +12,8 @@ void plan_score(ScoreArgs& p) {
   // they are cut further, down to a piece per lane.
   const int64_t each = 16 / size_of(p.a.dtype), pieces = ceil_div((int64_t)p.a.vocabulary, each) + 1;
   const int64_t least = p.a.top ? ceil_div(pieces, kScoreThreads * kMostVectors) : ceil_div(pieces, kMostPieces), most = ceil_div(pieces, kScoreThreads);
-  const int64_t wanted = std::max<int64_t>(least, std::min<int64_t>(most, 512 / std::max<int64_t>(1, p.a.rows)));
+  const int64_t limit = p.a.top ? 64 : 128;       // (of lists that are joined)
+  const int64_t wanted = std::max<int64_t>(least, std::min<int64_t>({most, limit, 512 / std::max<int64_t>(1, p.a.rows)}));
   const int64_t rounds = ceil_div(pieces, wanted * kScoreThreads);           // pieces per lane
   p.parts = (int32_t)ceil_div(pieces, rounds * kScoreThreads);
   p.vectors = (int32_t)(rounds * kScoreThreads);

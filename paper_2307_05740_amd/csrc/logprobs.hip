@@ -11,6 +11,7 @@
 #include <cstdint>
 
 #include "attention_common.h"
+#include "lanes.h"
 #include "logprobs_internal.h"
 
 namespace arrow {
@@ -81,8 +82,6 @@ struct Sums {
     w += o.w;
   }
 };
-
-__device__ __forceinline__ Sums exchanged(const Sums& x, int mask) { return {__shfl_xor(x.M, mask, 64), __shfl_xor(x.s, mask, 64), __shfl_xor(x.w, mask, 64)}; }
 
 // Results of a row from its sums.
 struct Stats {
@@ -167,6 +166,7 @@ __device__ __forceinline__ void place(int top, Chosen& c, Out&& out, Below&& bel
       if (i >= n) { out(i, (uint64_t)0); continue; }
       const uint64_t key = c.list[i];
       int before = 0;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) before += c.list[j] > key;
       if (before < top) out(before, key);
     }
@@ -188,18 +188,27 @@ __device__ __forceinline__ void place(int top, Chosen& c, Out&& out, Below&& bel
   }
 }
 
-template <typename T>
 __device__ __forceinline__ int64_t target_of(const ScoreArgs& p, int64_t row) {
   return p.a.target_bytes == 4 ? (int64_t)((const int32_t*)p.targets)[row] : ((const int64_t*)p.targets)[row];
 }
 
-template <typename T>
-__device__ __forceinline__ void write_row(const ScoreArgs& p, int64_t row, const Stats& s) {
+// A row's target and its logit, looked up before the rest of the row is there.
+struct Target {
+  bool known;
+  float logit;
+  template <typename T>
+  __device__ __forceinline__ Target(const ScoreArgs& p, int64_t row, const T*) {
+    const int64_t t = target_of(p, row);
+    known = t >= 0 && t < p.a.vocabulary;
+    logit = (float)((const T*)p.logits)[row * p.a.stride + (known ? t : 0)];
+  }
+};
+
+__device__ __forceinline__ void write_row(const ScoreArgs& p, int64_t row, const Stats& s, const Target& t) {
   p.lse[row] = s.lse(p.a.scale);
   p.entropy[row] = s.entropy;
   *(float2*)(p.stats + 2 * row) = {s.M, s.log};
-  const int64_t t = target_of<T>(p, row);
-  p.logp[row] = t >= 0 && t < p.a.vocabulary ? s.of((float)((const T*)p.logits)[row * p.a.stride + t], p.a.scale) : 0.f;
+  p.logp[row] = t.known ? s.of(t.logit, p.a.scale) : 0.f;
 }
 
 __device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i, uint64_t key, const Stats& s) {
@@ -243,10 +252,9 @@ struct LaneSums {
 
 // The sums of a wavefront, in all lanes.
 __device__ __forceinline__ Sums of_wave(Sums x, float c) {
-  float most = x.M;
-  for (int m = 32; m; m >>= 1) most = larger(most, __shfl_xor(most, m, 64));
-  x.raise(most, c);
-  for (int m = 32; m; m >>= 1) { x.s += __shfl_xor(x.s, m, 64); x.w += __shfl_xor(x.w, m, 64); }
+  x.raise(over_lanes(x.M, 6, larger), c);
+  x.s = sum_of_lanes(x.s, 6);
+  x.w = sum_of_lanes(x.w, 6);
   return x;
 }
 
@@ -261,6 +269,7 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
   const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
   const int first = part * p.vectors, pieces = min(p.vectors, r.pieces - first);      // (of this part; may be none)
   const u32x4* at = r.piece(first);
+  const Target target(p, row, (const T*)nullptr);
 
   const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
   const float c = p.a.scale * kLog2e, beside = edge >= 0 ? (float)r.at[edge] : 0.f;
@@ -329,7 +338,7 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
   if (p.parts > 1) *(f32x4*)(p.sums + (row * p.parts + part) * 4) = f32x4{sum.M, sum.s, sum.w, 0.f};
-  else write_row<T>(p, row, Stats(sum));
+  else write_row(p, row, Stats(sum), target);
 }
 
 // The same with the largest logits: a lane holds its N pieces.
@@ -343,6 +352,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
   const int first = part * p.vectors, pieces = min(p.vectors, r.pieces - first);      // (of this part; may be none)
   const u32x4* at = r.piece(first);
+  const Target target(p, row, (const T*)nullptr);
 
   u32x4 x[N];
 #pragma unroll
@@ -373,10 +383,8 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   }
   Sums lane_sums = lane.exact();
   if (__any(lane.failed())) {
-    float all = mine;
-    for (int m = 32; m; m >>= 1) all = larger(all, __shfl_xor(all, m, 64));
     lane = LaneSums(c);
-    lane.M = all;
+    lane.M = over_lanes(mine, 6, larger);
     lane.add_any(beside);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -394,16 +402,17 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
   if (p.parts > 1 && tid == 0) *(f32x4*)(p.sums + (row * p.parts + part) * 4) = f32x4{sum.M, sum.s, sum.w, 0.f};
   const Stats s(sum);
-  if (p.parts == 1 && tid == 0) write_row<T>(p, row, s);
+  if (p.parts == 1 && tid == 0) write_row(p, row, s, target);
 
   // the lane's largest key: its piece is taken, or read again, for the index
-  constexpr bool kHeld = N <= 2;
+  constexpr bool kHeld = N <= 4;
   uint64_t key = 0;
   auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
   auto look = [&](const u32x4& v, int piece) {
+    int at = 0;
 #pragma unroll
-    for (int i = P::kEach - 1; i >= 0; --i)
-      if (alike(P::get(v, i), mine)) key = key_of(mine, r.index(piece, i));
+    for (int i = P::kEach - 1; i >= 0; --i) at = alike(P::get(v, i), mine) ? i : at;
+    key = key_of(mine, r.index(piece, at));
   };
   int found = -1;
 #pragma unroll
@@ -419,15 +428,16 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   }
   const uint64_t border = border_of(key, p.a.top, index_bits(p.a.vocabulary), chosen);
   if (edge >= 0) put(key_of(beside, edge), border, chosen);
+  const float least = border ? value_of(border) : minus_infinity();
   auto put_all = [&](const u32x4& v, int piece) {
 #pragma unroll
-    for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(piece, e)), border, chosen);
+    for (int e = 0; e < P::kEach; ++e)
+      if (!(P::get(v, e) < least)) put(key_of(P::get(v, e), r.index(piece, e)), border, chosen);
   };
-  const float least = value_of(border);                   // (0 stands for a number below all others)
   uint32_t near = 0;
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (j * kThreads + tid < pieces && (border == 0 || !(most[j] < least))) {
+    if (j * kThreads + tid < pieces && !(most[j] < least)) {
       if (kHeld) put_all(x[j], first + j * kThreads + tid);
       else near |= 1u << j;
     }
@@ -455,34 +465,40 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
       });
 }
 
-// The parts of a row.
+// The parts of a row.  All loads that others do not wait for come first.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
+  constexpr int kHeld = 4;
   __shared__ Sums waves[kWaves];
   __shared__ Chosen chosen;
   const int tid = threadIdx.x, top = p.a.top;
-  const int64_t row = blockIdx.x;
+  const int64_t row = blockIdx.x, n = (int64_t)p.parts * top;
   const float c = p.a.scale * kLog2e;
+  const uint64_t* keys = p.keys + row * n;
+  uint64_t held[kHeld], key = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = i * kThreads + tid < n ? keys[i * kThreads + tid] : 0;
+  if (top)
+    for (int i = tid; i < p.parts; i += kThreads) key = max(key, keys[(int64_t)i * top]);
+  const Target target(p, row, (const T*)nullptr);
   Sums sum{minus_infinity(), 0.f, 0.f};
   for (int i = tid; i < p.parts; i += kThreads) {
     const f32x4 v = *(const f32x4*)(p.sums + (row * p.parts + i) * 4);
     sum.add({v[0], v[1], v[2]}, c);
   }
-  for (int m = 32; m; m >>= 1) sum.add(exchanged(sum, m), c);
+  sum = of_wave(sum, c);
   if ((tid & 63) == 0) waves[tid >> 6] = sum;
   __syncthreads();
   sum = waves[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) sum.add(waves[w], c);
   const Stats s(sum);
-  if (tid == 0) write_row<T>(p, row, s);
+  if (tid == 0) write_row(p, row, s, target);
   if (top == 0) return;
-  const uint64_t* keys = p.keys + row * p.parts * top;
-  const int64_t n = (int64_t)p.parts * top;
-  uint64_t key = 0;
-  for (int i = tid; i < p.parts; i += kThreads) key = keys[(int64_t)i * top] > key ? keys[(int64_t)i * top] : key;
   const uint64_t border = border_of(key, top, index_bits(p.a.vocabulary), chosen);
-  for (int64_t i = tid; i < n; i += kThreads) put(keys[i], border, chosen);
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) put(held[i], border, chosen);
+  for (int64_t i = kHeld * kThreads + tid; i < n; i += kThreads) put(keys[i], border, chosen);
   place(
       top, chosen, [&](int i, uint64_t k) { write_top(p, row, i, k, s); },
       [&](uint64_t last) {
@@ -490,6 +506,21 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
         for (int64_t i = tid; i < n; i += kThreads) best = keys[i] < last && keys[i] > best ? keys[i] : best;
         return best;
       });
+}
+
+// The same without tokens, of few parts: a row to a lane.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void score_join_rows_kernel(ScoreArgs p) {
+  const int64_t row = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (row >= p.a.rows) return;
+  const float c = p.a.scale * kLog2e;
+  const Target target(p, row, (const T*)nullptr);
+  Sums sum{minus_infinity(), 0.f, 0.f};
+  for (int i = 0; i < p.parts; ++i) {
+    const f32x4 v = *(const f32x4*)(p.sums + (row * p.parts + i) * 4);
+    sum.add({v[0], v[1], v[2]}, c);
+  }
+  write_row(p, row, Stats(sum), target);
 }
 
 template <typename T>
@@ -516,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int c
   if (row >= p.a.rows) return;
   const T* in = (const T*)p.logits + row * p.a.stride;
   T* out = (T*)p.d_logits + row * p.a.d_stride;
-  const int64_t target = target_of<T>(p, row);
+  const int64_t target = target_of(p, row);
   const bool known = target >= 0 && target < p.a.vocabulary;
   const int t = known ? (int)target : -1;
   const float2 stats = *(const float2*)(p.stats + 2 * row);
@@ -571,7 +602,8 @@ int forward(const ScoreArgs& p, hipStream_t s) {
   else if (n <= 4) score_kernel<T, 4><<<grid, block, 0, s>>>(p);
   else if (n <= 8) score_kernel<T, 8><<<grid, block, 0, s>>>(p);
   else score_kernel<T, 16><<<grid, block, 0, s>>>(p);
-  if (p.parts > 1) score_join_kernel<T><<<dim3((unsigned)p.a.rows), block, 0, s>>>(p);
+  if (p.parts > 1 && p.parts <= 8 && p.a.top == 0) score_join_rows_kernel<T><<<dim3((unsigned)((p.a.rows + kThreads - 1) / kThreads)), block, 0, s>>>(p);
+  else if (p.parts > 1) score_join_kernel<T><<<dim3((unsigned)p.a.rows), block, 0, s>>>(p);
   return (int)hipGetLastError();
 }
 

@@ -8,6 +8,7 @@
 #include <cstdint>
 
 #include "attention_common.h"
+#include "lanes.h"
 #include "rotation_internal.h"
 
 namespace arrow {
@@ -43,12 +44,6 @@ __device__ __forceinline__ void store8(T* at, const Eight& v) {
 }
 
 __device__ __forceinline__ Eight zeros() { return {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}}; }
-
-// Sum over the 2^log lanes of a head, in all of them.
-__device__ __forceinline__ float add_lanes(float x, int log) {
-  for (int m = 1; m < 1 << log; m <<= 1) x += __shfl_xor(x, m, 64);
-  return x;
-}
 
 // The turn of a pair at a position, as cosine and sine.  The product in 64 bits is off by 2^-53 of itself, at a position of 2^31 by 2^-22 of a turn.
 __device__ __forceinline__ float2 turned(double turns, int64_t position) {
@@ -157,7 +152,7 @@ __global__ __launch_bounds__(kThreads) void rotation_kernel(RotationArgs p) {
         float square = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) square = fmaf(xa.x[j], xa.x[j], fmaf(xb.x[j], xb.x[j], square));
-        const float r = 1.f / sqrtf(add_lanes(square, p.lanes_log) / (float)a.dim + a.eps);
+        const float r = 1.f / sqrtf(sum_of_lanes(square, p.lanes_log) / (float)a.dim + a.eps);
         const float2* cs = angles + t * half + lane.pair;
         if constexpr (!kBack) {
 #pragma unroll
@@ -174,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void rotation_kernel(RotationArgs p) {
             sum[which][1].x[j] += db;
             mean = fmaf(wa.x[j], da, fmaf(wb.x[j], db, mean));
           }
-          mean = add_lanes(mean, p.lanes_log) / (float)a.dim;
+          mean = sum_of_lanes(mean, p.lanes_log) / (float)a.dim;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             xa.x[j] = r * (wa.x[j] * ga.x[j] - xa.x[j] * mean);
