@@ -50,15 +50,34 @@ int check_weights(const arrow_rotation_t* a, const char* name, const void* q, co
   return ARROW_OK;
 }
 
+bool follow(const arrow_rotation_t* a, const arrow_strides_t& s) { return a->batch <= 1 || s.sequence == a->tokens * s.token; }
+
 RotationArgs plan(const arrow_rotation_t* a, bool backward) {
   RotationArgs p{};
   p.a = *a;
-  p.rows = (int64_t)a->batch * a->tokens;
+  p.sequences = a->batch;
+  p.length = a->tokens;
+  if (a->tokens == 1 && a->batch > 1) {               // (tokens that are sequences' only ones)
+    for (auto* s : {&p.a.q, &p.a.k, &p.a.q_out, &p.a.k_out, &p.a.dq, &p.a.dk}) s->token = s->sequence;
+    p.sequences = 1;
+    p.length = a->batch;
+  } else if (follow(a, a->q) && follow(a, a->k) && follow(a, a->q_out) && follow(a, a->k_out) && (!backward || (follow(a, a->dq) && follow(a, a->dk)))) {
+    p.sequences = std::min(a->batch, 1);
+    p.length = a->batch * a->tokens;
+  }
   while ((16 << p.lanes_log) < a->dim) ++p.lanes_log;
   // A workgroup's tokens share its angles.  Few tokens: one each.
-  p.per = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kRotationTokens, p.rows / 1024));
-  const int64_t blocks = ceil_div(p.rows, p.per);
-  p.blocks = (int32_t)(backward ? std::min<int64_t>(blocks, kRotationBlocks) : blocks);
+  p.per = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kRotationTokens, (int64_t)p.sequences * p.length / 1024));
+  p.tiles = (int32_t)ceil_div(p.length, p.per);
+  p.all_tiles = p.sequences * p.tiles;
+  if (!backward) {
+    p.blocks = p.all_tiles;
+    return p;
+  }
+  // Queries and keys have workgroups by their heads.
+  const int32_t q = (int32_t)std::max<int64_t>(1, kRotationBlocks * (int64_t)a->q_heads / (a->q_heads + a->kv_heads));
+  p.q_blocks = std::min(p.all_tiles, std::min(q, kRotationBlocks - 1));
+  p.blocks = p.q_blocks + std::min(p.all_tiles, std::max(1, kRotationBlocks - q));
   return p;
 }
 
@@ -79,13 +98,13 @@ int arrow_rotation_forward(const arrow_rotation_t* a, const void* q, const void*
   RotationArgs p = plan(a, false);
   p.q = q; p.k = k; p.wq = wq; p.wk = wk;
   p.yq = q_out; p.yk = k_out;
-  p.q_to = a->q_out; p.k_to = a->k_out;
+  p.q_to = p.a.q_out; p.k_to = p.a.k_out;
   return launched("rotation forward", launch_rotation(p, false, stream));
 }
 
 size_t arrow_rotation_workspace_bytes(const arrow_rotation_t* a) {
   if (check(a)) return 0;
-  return align_up((size_t)plan(a, true).blocks * 2 * a->dim * 4);
+  return align_up((size_t)plan(a, true).blocks * a->dim * 4);
 }
 
 int arrow_rotation_backward(const arrow_rotation_t* a, const void* d_q_out, const void* d_k_out, const void* q, const void* k, const void* wq,
@@ -95,7 +114,8 @@ int arrow_rotation_backward(const arrow_rotation_t* a, const void* d_q_out, cons
   if (int rc = check_weights(a, "gradients of weights", dwq, dwk)) return rc;
   if (dwq && dwq == dwk) return refuse(ARROW_EINVAL, "dwq and dwk are the same");
   RotationArgs p = plan(a, true);
-  if (p.rows) {
+  const bool some = (int64_t)a->batch * a->tokens > 0;
+  if (some) {
     const struct { const char* name; const void* at; const arrow_strides_t& s; int32_t heads; bool written; } all[] = {
         {"d_q_out", d_q_out, a->q_out, a->q_heads, false}, {"d_k_out", d_k_out, a->k_out, a->kv_heads, false}, {"q", q, a->q, a->q_heads, false},
         {"k", k, a->k, a->kv_heads, false}, {"dq", dq, a->dq, a->q_heads, true}, {"dk", dk, a->dk, a->kv_heads, true}};
@@ -107,10 +127,10 @@ int arrow_rotation_backward(const arrow_rotation_t* a, const void* d_q_out, cons
   }
   if (dwq)
     if (int rc = check_workspace(ws, ws_bytes, arrow_rotation_workspace_bytes(a))) return rc;
-  if (!p.rows && !dwq) return ARROW_OK;
+  if (!some && !dwq) return ARROW_OK;
   p.q = q; p.k = k; p.wq = wq; p.wk = wk; p.gq = d_q_out; p.gk = d_k_out;
   p.yq = dq; p.yk = dk;
-  p.q_to = a->dq; p.k_to = a->dk;
+  p.q_to = p.a.dq; p.k_to = p.a.dk;
   p.dwq = dwq; p.dwk = dwk;
   p.parts = (float*)ws;
   return launched("rotation backward", launch_rotation(p, true, stream));

@@ -18,19 +18,24 @@ constexpr int kThreads = kRotationThreads;
 
 struct Eight { float x[8]; };
 
+// Eight elements as they lie in memory.
+template <typename T> struct Raw { x8<T> v; };
+template <> struct Raw<float> { f32x4 v[2]; };
+
 template <typename T>
-__device__ __forceinline__ Eight load8(const T* at) {
-  Eight r;
-  if constexpr (sizeof(T) == 4) {
-    const f32x4 a = *(const f32x4*)at, b = *(const f32x4*)(at + 4);
+__device__ __forceinline__ Raw<T> raw8(const T* at) {
+  if constexpr (sizeof(T) == 4) return {{*(const f32x4*)at, *(const f32x4*)(at + 4)}};
+  else return {*(const x8<T>*)at};
+}
+template <typename T>
+__device__ __forceinline__ Eight wide(const Raw<T>& r, bool in) {
+  Eight e;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { r.x[i] = a[i]; r.x[4 + i] = b[i]; }
-  } else {
-    const x8<T> a = *(const x8<T>*)at;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.x[i] = (float)a[i];
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (sizeof(T) == 4) e.x[i] = in ? r.v[i / 4][i % 4] : 0.f;
+    else e.x[i] = in ? (float)r.v[i] : 0.f;
   }
-  return r;
+  return e;
 }
 
 template <typename T>
@@ -40,6 +45,19 @@ __device__ __forceinline__ void store8(T* at, const Eight& v) {
     *(f32x4*)(at + 4) = f32x4{v.x[4], v.x[5], v.x[6], v.x[7]};
   } else {
     *(x8<T>*)at = round8<T>(v.x[0], v.x[1], v.x[2], v.x[3], v.x[4], v.x[5], v.x[6], v.x[7]);
+  }
+}
+
+// The same, and what was made of it before is not kept in registers.
+template <typename T>
+__device__ __forceinline__ Raw<T> again(const Raw<T>& r) {
+  if constexpr (sizeof(T) == 4) {
+    return {{here(r.v[0]), here(r.v[1])}};
+  } else {
+    union { x8<T> v; u32x4 u; } x;
+    x.v = r.v;
+    x.u = here(x.u);
+    return {x.v};
   }
 }
 
@@ -54,37 +72,33 @@ __device__ __forceinline__ float2 turned(double turns, int64_t position) {
 }
 
 // The pairs of the lane's two pieces, rotated by (cos, sin), or back.
-template <bool kBack>
-__device__ __forceinline__ void rotate(Eight& a, Eight& b, const float2* cs, bool interleaved) {
-  float2 t[8];
+template <bool kBack, bool kInterleaved>
+__device__ __forceinline__ void rotate(Eight& a, Eight& b, const float2* cs) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const f32x4 two = *(const f32x4*)(cs + 2 * i);
-    t[2 * i] = {two[0], kBack ? -two[1] : two[1]};
-    t[2 * i + 1] = {two[2], kBack ? -two[3] : two[3]};
-  }
-  if (interleaved) {
+  for (int i = 0; i < 8; i += 2) {
+    const f32x4 two = *(const f32x4*)(cs + i);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      Eight& p = i < 4 ? a : b;
-      const int d = 2 * (i & 3);
-      const float x = p.x[d], y = p.x[d + 1];
-      p.x[d] = x * t[i].x - y * t[i].y;
-      p.x[d + 1] = y * t[i].x + x * t[i].y;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = a.x[i], y = b.x[i];
-      a.x[i] = x * t[i].x - y * t[i].y;
-      b.x[i] = y * t[i].x + x * t[i].y;
+    for (int k = 0; k < 2; ++k) {
+      const float c = two[2 * k], s = kBack ? -two[2 * k + 1] : two[2 * k + 1];
+      if constexpr (kInterleaved) {
+        Eight& p = i < 4 ? a : b;
+        const int d = 2 * ((i + k) & 3);
+        const float x = p.x[d], y = p.x[d + 1];
+        p.x[d] = x * c - y * s;
+        p.x[d + 1] = y * c + x * s;
+      } else {
+        const float x = a.x[i + k], y = b.x[i + k];
+        a.x[i + k] = x * c - y * s;
+        b.x[i + k] = y * c + x * s;
+      }
     }
   }
 }
 
 // What a lane does at any head: where its two pieces lie, and its pairs' turns.
 struct Lane {
-  int first, second;        // elements, -1: a piece that is not there
+  int first, second;        // elements
+  bool has_first, has_second;
   bool turns;
   int pair;                 // the first of its eight
   __device__ __forceinline__ Lane(const arrow_rotation_t& a, int u) {
@@ -99,132 +113,203 @@ struct Lane {
       x = rotated + 2 * (u - rotated / 2);
       y = x + 1;
     }
-    first = x < pieces ? 8 * x : -1;
-    second = y < pieces ? 8 * y : -1;
+    has_first = x < pieces;
+    has_second = y < pieces;
+    first = has_first ? 8 * x : 0;           // (a piece that is not there is read as the first one)
+    second = has_second ? 8 * y : 0;
   }
 };
 
-template <typename T, typename W, bool kBack>
+// Some tokens of one sequence.
+struct Tokens {
+  uint32_t b, at;           // the sequence, and the first of them in it
+  int count;
+  __device__ __forceinline__ Tokens(const RotationArgs& p, uint32_t tile) {
+    b = tile / (uint32_t)p.tiles;
+    at = (tile - b * p.tiles) * p.per;
+    count = min(p.per, p.length - (int)at);
+  }
+};
+
+// Their heads, of queries or keys (kKeys): 2^n lanes each, the next one's elements on their way while one is worked on.
+template <typename T, bool kBack, bool kKeys, bool kInterleaved>
+__device__ __forceinline__ void rotate_heads(const RotationArgs& p, const Lane& lane, const Tokens& of, const float2* angles, const float* w, Eight* sum) {
+  const arrow_rotation_t& a = p.a;
+  const int heads = kKeys ? a.kv_heads : a.q_heads, half = a.rotary / 2, n = of.count * heads, step = kThreads >> p.lanes_log;
+  const arrow_strides_t& from = kKeys ? a.k : a.q;
+  const arrow_strides_t& to = kKeys ? p.k_to : p.q_to;
+  const arrow_strides_t& grad = kKeys ? a.k_out : a.q_out;
+  const T* x = (const T*)(kKeys ? p.k : p.q) + of.b * from.sequence + of.at * from.token;
+  const T* g = kBack ? (const T*)(kKeys ? p.gk : p.gq) + of.b * grad.sequence + of.at * grad.token : nullptr;
+  T* y = (T*)(kKeys ? p.yk : p.yq) + of.b * to.sequence + of.at * to.token;
+  struct Pieces { Raw<T> xa, xb, ga, gb; };
+  auto load = [&](int t, int head) {
+    const T* at = x + t * from.token + head * from.head;
+    Pieces r;
+    r.xa = raw8(at + lane.first);
+    r.xb = raw8(at + lane.second);
+    if constexpr (kBack) {
+      at = g + t * grad.token + head * grad.head;
+      r.ga = raw8(at + lane.first);
+      r.gb = raw8(at + lane.second);
+    }
+    return r;
+  };
+  // head i of token t, and `step` heads further on each time
+  int i = threadIdx.x >> p.lanes_log;
+  if (i >= n) return;
+  int t = (uint32_t)i / (uint32_t)heads, head = i - t * heads;
+  const int step_t = step / heads, step_head = step - step_t * heads;
+  Pieces next = load(t, head);
+  while (true) {
+    const Pieces now = next;
+    const int now_t = t, now_head = head;
+    i += step;
+    const bool more = i < n;
+    head += step_head;
+    t += step_t;
+    if (head >= heads) { head -= heads; ++t; }
+    if (!more) { t = now_t; head = now_head; }
+    next = load(t, head);
+    Eight xa = wide<T>(now.xa, lane.has_first), xb = wide<T>(now.xb, lane.has_second);
+    float square = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) square = fmaf(xa.x[j], xa.x[j], fmaf(xb.x[j], xb.x[j], square));
+    const float r = 1.f / sqrtf(sum_of_lanes(square, p.lanes_log) / (float)a.dim + a.eps);
+    const float2* cs = angles + now_t * half + lane.pair;
+    if constexpr (!kBack) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { xa.x[j] *= r * w[lane.first + j]; xb.x[j] *= r * w[lane.second + j]; }
+      if (lane.turns) rotate<false, kInterleaved>(xa, xb, cs);
+    } else {
+      Eight ga = wide<T>(now.ga, lane.has_first), gb = wide<T>(now.gb, lane.has_second);
+      if (lane.turns) rotate<true, kInterleaved>(ga, gb, cs);
+      __builtin_amdgcn_sched_barrier(0);          // (the weights are not loaded before the angles are done with)
+      xa = wide<T>(again(now.xa), lane.has_first);
+      xb = wide<T>(again(now.xb), lane.has_second);
+      float mean = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        xa.x[j] *= r; xb.x[j] *= r;               // n
+        sum[0].x[j] = fmaf(ga.x[j], xa.x[j], sum[0].x[j]);
+        sum[1].x[j] = fmaf(gb.x[j], xb.x[j], sum[1].x[j]);
+        ga.x[j] *= w[lane.first + j];
+        gb.x[j] *= w[lane.second + j];
+        mean = fmaf(ga.x[j], xa.x[j], fmaf(gb.x[j], xb.x[j], mean));
+      }
+      mean = sum_of_lanes(mean, p.lanes_log) / (float)a.dim;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        xa.x[j] = r * (ga.x[j] - xa.x[j] * mean);
+        xb.x[j] = r * (gb.x[j] - xb.x[j] * mean);
+      }
+    }
+    T* at = y + now_t * to.token + now_head * to.head;
+    if (lane.has_first) store8(at + lane.first, xa);
+    if (lane.has_second) store8(at + lane.second, xb);
+    if (!more) return;
+  }
+}
+
+// Their angles, `half` each.
+__device__ __forceinline__ void find_angles(const RotationArgs& p, const Tokens& of, float2* angles) {
+  const arrow_rotation_t& a = p.a;
+  const int half = a.rotary / 2;
+  for (int i = threadIdx.x; i < of.count * half; i += kThreads) {
+    const uint32_t t = (uint32_t)i / (uint32_t)half, pair = i - t * half, row = of.b * p.length + of.at + t;
+    const int64_t position = !a.positions ? row % (uint32_t)a.tokens : a.position_bytes == 4 ? ((const int32_t*)a.positions)[row] : ((const int64_t*)a.positions)[row];
+    angles[i] = turned(a.turns[pair], position + a.shift);
+  }
+}
+
+template <typename W>
+__device__ __forceinline__ void find_weights(const RotationArgs& p, bool keys, float* weights) {
+  const W* w = (const W*)(keys ? p.wk : p.wq);
+  for (int d = threadIdx.x; d < p.a.dim; d += kThreads) weights[d] = w ? (float)w[d] : 1.f;
+}
+
+template <typename T, typename W, bool kInterleaved>
 __global__ __launch_bounds__(kThreads) void rotation_kernel(RotationArgs p) {
   __shared__ __align__(16) float2 angles[kRotationTokens * 128];
-  __shared__ __align__(16) float weights[2 * 256];
-  __shared__ __align__(16) float sums[kBack ? kThreads * 16 : 1];
-  const arrow_rotation_t& a = p.a;
-  const int tid = threadIdx.x, lanes = 1 << p.lanes_log, groups = kThreads >> p.lanes_log, group = tid >> p.lanes_log, half = a.rotary / 2;
-  const Lane lane(a, tid & (lanes - 1));
-  for (int i = tid; i < 2 * a.dim; i += kThreads) {
-    const int d = i < a.dim ? i : i - a.dim;
-    const W* w = (const W*)(i < a.dim ? p.wq : p.wk);
-    weights[i] = w ? (float)w[d] : 1.f;
-  }
-  Eight sum[2][2] = {{zeros(), zeros()}, {zeros(), zeros()}};
+  __shared__ __align__(16) float weights[2][256];
+  const Lane lane(p.a, threadIdx.x & ((1 << p.lanes_log) - 1));
+  const Tokens of(p, blockIdx.x);
+  find_weights<W>(p, false, weights[0]);
+  find_weights<W>(p, true, weights[1]);
+  find_angles(p, of, angles);
+  __syncthreads();
+  rotate_heads<T, false, false, kInterleaved>(p, lane, of, angles, weights[0], nullptr);
+  rotate_heads<T, false, true, kInterleaved>(p, lane, of, angles, weights[1], nullptr);
+}
 
-  for (int64_t token0 = (int64_t)blockIdx.x * p.per; token0 < p.rows; token0 += (int64_t)gridDim.x * p.per) {
-    const int tokens = (int)min((int64_t)p.per, p.rows - token0);
+// Gradients: a workgroup has queries or keys, so that it holds the sums of one weight's gradient only.
+template <typename T, typename W, bool kKeys, bool kInterleaved>
+__device__ __forceinline__ void rotate_back(const RotationArgs& p, uint32_t block, uint32_t blocks, float2* angles, float* weights, float* sums) {
+  const int lanes = 1 << p.lanes_log, groups = kThreads >> p.lanes_log;
+  const Lane lane(p.a, threadIdx.x & (lanes - 1));
+  find_weights<W>(p, kKeys, weights);
+  Eight sum[2] = {zeros(), zeros()};
+  for (uint32_t tile = block; tile < (uint32_t)p.all_tiles; tile += blocks) {
+    const Tokens of(p, tile);
     __syncthreads();                                  // (the angles of the tokens before are done with)
-    for (int i = tid; i < tokens * half; i += kThreads) {
-      const int t = i / half, pair = i - t * half;
-      const int64_t row = token0 + t;
-      const int64_t position = !a.positions ? row % a.tokens : a.position_bytes == 4 ? ((const int32_t*)a.positions)[row] : ((const int64_t*)a.positions)[row];
-      angles[t * half + pair] = turned(a.turns[pair], position + a.shift);
-    }
+    find_angles(p, of, angles);
     __syncthreads();
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {         // queries, then keys
-      const int heads = which ? a.kv_heads : a.q_heads;
-      const arrow_strides_t& from = which ? a.k : a.q;
-      const arrow_strides_t& to = which ? p.k_to : p.q_to;
-      const arrow_strides_t& grad = which ? a.k_out : a.q_out;
-      const float* w = weights + which * a.dim;
-      for (int i = group; i < tokens * heads; i += groups) {
-        const int t = i / heads, head = i - t * heads;
-        const int64_t row = token0 + t, b = row / a.tokens, at = row - b * a.tokens;
-        const T* x = (const T*)(which ? p.k : p.q) + b * from.sequence + at * from.token + head * from.head;
-        T* y = (T*)(which ? p.yk : p.yq) + b * to.sequence + at * to.token + head * to.head;
-        Eight xa = zeros(), xb = zeros(), wa = zeros(), wb = zeros(), ga = zeros(), gb = zeros();
-        if (lane.first >= 0) { xa = load8(x + lane.first); wa = load8(w + lane.first); }
-        if (lane.second >= 0) { xb = load8(x + lane.second); wb = load8(w + lane.second); }
-        if constexpr (kBack) {
-          const T* g = (const T*)(which ? p.gk : p.gq) + b * grad.sequence + at * grad.token + head * grad.head;
-          if (lane.first >= 0) ga = load8(g + lane.first);
-          if (lane.second >= 0) gb = load8(g + lane.second);
-        }
-        float square = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) square = fmaf(xa.x[j], xa.x[j], fmaf(xb.x[j], xb.x[j], square));
-        const float r = 1.f / sqrtf(sum_of_lanes(square, p.lanes_log) / (float)a.dim + a.eps);
-        const float2* cs = angles + t * half + lane.pair;
-        if constexpr (!kBack) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) { xa.x[j] *= r * wa.x[j]; xb.x[j] *= r * wb.x[j]; }
-          if (lane.turns) rotate<false>(xa, xb, cs, a.interleaved);
-        } else {
-          if (lane.turns) rotate<true>(ga, gb, cs, a.interleaved);
-          float mean = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            xa.x[j] *= r; xb.x[j] *= r;               // n
-            const float da = ga.x[j] * xa.x[j], db = gb.x[j] * xb.x[j];
-            sum[which][0].x[j] += da;
-            sum[which][1].x[j] += db;
-            mean = fmaf(wa.x[j], da, fmaf(wb.x[j], db, mean));
-          }
-          mean = sum_of_lanes(mean, p.lanes_log) / (float)a.dim;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            xa.x[j] = r * (wa.x[j] * ga.x[j] - xa.x[j] * mean);
-            xb.x[j] = r * (wb.x[j] * gb.x[j] - xb.x[j] * mean);
-          }
-        }
-        if (lane.first >= 0) store8(y + lane.first, xa);
-        if (lane.second >= 0) store8(y + lane.second, xb);
-      }
-    }
+    rotate_heads<T, true, kKeys, kInterleaved>(p, lane, of, angles, weights, sum);
   }
+  if (!p.dwq) return;
+  // the groups' sums of an element, one after the other
+  float* mine = sums + (threadIdx.x >> p.lanes_log) * lanes * 16;
+  if (lane.has_first) store8(mine + lane.first, sum[0]);
+  if (lane.has_second) store8(mine + lane.second, sum[1]);
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.a.dim; d += kThreads) {
+    float all = 0.f;
+    for (int i = 0; i < groups; ++i) all += sums[i * lanes * 16 + d];
+    p.parts[(int64_t)blockIdx.x * p.a.dim + d] = all;
+  }
+}
 
-  if constexpr (kBack) {
-    if (!p.dwq) return;
-    // the groups' sums of an element, one after the other
-    for (int which = 0; which < 2; ++which) {
-      __syncthreads();
-      float* mine = sums + group * lanes * 16;
-      if (lane.first >= 0) store8(mine + lane.first, sum[which][0]);
-      if (lane.second >= 0) store8(mine + lane.second, sum[which][1]);
-      __syncthreads();
-      for (int d = tid; d < a.dim; d += kThreads) {
-        float all = 0.f;
-        for (int i = 0; i < groups; ++i) all += sums[i * lanes * 16 + d];
-        p.parts[((int64_t)blockIdx.x * 2 + which) * a.dim + d] = all;
-      }
-    }
-  }
+template <typename T, typename W, bool kInterleaved>
+__global__ __launch_bounds__(kThreads, 4) void rotation_grad_kernel(RotationArgs p) {
+  __shared__ __align__(16) float2 angles[kRotationTokens * 128];
+  __shared__ __align__(16) float weights[256];
+  __shared__ __align__(16) float sums[kThreads * 16];
+  const uint32_t block = blockIdx.x, q_blocks = p.q_blocks;
+  if (block < q_blocks) rotate_back<T, W, false, kInterleaved>(p, block, q_blocks, angles, weights, sums);
+  else rotate_back<T, W, true, kInterleaved>(p, block - q_blocks, gridDim.x - q_blocks, angles, weights, sums);
 }
 
 // The workgroups' sums of the weights' gradients, 16 elements to a workgroup.
 template <typename W>
 __global__ __launch_bounds__(kThreads) void rotation_join_kernel(RotationArgs p) {
   __shared__ float sums[kThreads];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4, columns = 2 * p.a.dim;
+  const bool keys = blockIdx.y;
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
+  const int first = keys ? p.q_blocks : 0, end = keys ? p.blocks : p.q_blocks;
   float all = 0.f;
-#pragma unroll 4
-  for (int i = part; i < p.blocks; i += kThreads / 16) all += p.parts[(int64_t)i * columns + c];
+  if (c < p.a.dim) {
+#pragma unroll 8
+    for (int i = first + part; i < end; i += kThreads / 16) all += p.parts[(int64_t)i * p.a.dim + c];
+  }
   sums[threadIdx.x] = all;
   __syncthreads();
-  if (threadIdx.x >= 16) return;
+  if (threadIdx.x >= 16 || c >= p.a.dim) return;
   for (int i = 1; i < kThreads / 16; ++i) all += sums[i * 16 + threadIdx.x];
-  W* to = (W*)(c < p.a.dim ? p.dwq : p.dwk);
-  to[c < p.a.dim ? c : c - p.a.dim] = (W)all;
+  ((W*)(keys ? p.dwk : p.dwq))[c] = (W)all;
 }
 
+template <typename T, typename W, bool kInterleaved>
+int launch(const RotationArgs& p, bool backward, hipStream_t s) {
+  if (p.blocks) {
+    if (backward) rotation_grad_kernel<T, W, kInterleaved><<<dim3((unsigned)p.blocks), dim3(kThreads), 0, s>>>(p);
+    else rotation_kernel<T, W, kInterleaved><<<dim3((unsigned)p.blocks), dim3(kThreads), 0, s>>>(p);
+  }
+  if (backward && p.dwq) rotation_join_kernel<W><<<dim3((unsigned)((p.a.dim + 15) / 16), 2), dim3(kThreads), 0, s>>>(p);
+  return (int)hipGetLastError();
+}
 template <typename T, typename W>
 int launch(const RotationArgs& p, bool backward, void* stream) {
-  hipStream_t s = (hipStream_t)stream;
-  if (p.blocks) {
-    if (backward) rotation_kernel<T, W, true><<<dim3((unsigned)p.blocks), dim3(kThreads), 0, s>>>(p);
-    else rotation_kernel<T, W, false><<<dim3((unsigned)p.blocks), dim3(kThreads), 0, s>>>(p);
-  }
-  if (backward && p.dwq) rotation_join_kernel<W><<<dim3((unsigned)(2 * p.a.dim / 16)), dim3(kThreads), 0, s>>>(p);
-  return (int)hipGetLastError();
+  return p.a.interleaved ? launch<T, W, true>(p, backward, (hipStream_t)stream) : launch<T, W, false>(p, backward, (hipStream_t)stream);
 }
 
 }  // namespace

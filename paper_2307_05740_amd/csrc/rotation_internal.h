@@ -10,7 +10,7 @@ namespace arrow {
 
 constexpr int kRotationThreads = 256;
 constexpr int kRotationTokens = 8;        // of a workgroup at a time, at most
-constexpr int kRotationBlocks = 1024;     // workgroups of a gradient, at most: four to a compute unit; each leaves a sum of the weights' gradients
+constexpr int kRotationBlocks = 1024;     // workgroups of a gradient, at most: four to a compute unit; each leaves a sum of a weight's gradient
 
 struct RotationArgs {
   arrow_rotation_t a;
@@ -19,10 +19,10 @@ struct RotationArgs {
   void *yq, *yk;                          // its results, or the gradients of q and k
   arrow_strides_t q_to, k_to;             // steps of these
   void *dwq, *dwk;
-  float* parts;                           // blocks x 2 x dim sums of the weights' gradients
-  int64_t rows;                           // tokens of all sequences
-  int32_t per;                            // tokens of a workgroup at a time
-  int32_t blocks;
+  float* parts;                           // blocks x dim sums of the weights' gradients
+  int32_t sequences, length;              // and tokens of each: one of all where sequences follow each other
+  int32_t per, tiles, all_tiles;          // tokens of a workgroup at a time; such tiles of a sequence, and of all
+  int32_t blocks, q_blocks;               // workgroups; of a gradient, those that have queries: the first ones
   int32_t lanes_log;                      // lanes of a head: a power of two, each has 16 elements
 };
 
