@@ -66,8 +66,9 @@ RotationArgs plan(const arrow_rotation_t* a, bool backward) {
     p.length = a->batch * a->tokens;
   }
   while ((16 << p.lanes_log) < a->dim) ++p.lanes_log;
-  // A workgroup's tokens share its angles.  Few tokens: one each.
-  p.per = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kRotationTokens, (int64_t)p.sequences * p.length / 1024));
+  // A workgroup's tokens share its angles.  Few tokens: as many as have a head for each of its groups of lanes.
+  const int64_t heads = a->q_heads + a->kv_heads, groups = kRotationThreads >> p.lanes_log;
+  p.per = (int32_t)std::max<int64_t>({1, std::min<int64_t>(kRotationTokens, groups / heads), std::min<int64_t>(kRotationTokens, (int64_t)p.sequences * p.length / 1024)});
   p.tiles = (int32_t)ceil_div(p.length, p.per);
   p.all_tiles = p.sequences * p.tiles;
   if (!backward) {

@@ -131,36 +131,49 @@ struct Tokens {
   }
 };
 
-// Their heads, of queries or keys (kKeys): 2^n lanes each, the next one's elements on their way while one is worked on.
+// Their heads, of queries or keys (kKeys): 2^n lanes each, the next one's elements on their way while one is worked on, the first ones' from the start.
 template <typename T, bool kBack, bool kKeys, bool kInterleaved>
-__device__ __forceinline__ void rotate_heads(const RotationArgs& p, const Lane& lane, const Tokens& of, const float2* angles, const float* w, Eight* sum) {
-  const arrow_rotation_t& a = p.a;
-  const int heads = kKeys ? a.kv_heads : a.q_heads, half = a.rotary / 2, n = of.count * heads, step = kThreads >> p.lanes_log;
-  const arrow_strides_t& from = kKeys ? a.k : a.q;
-  const arrow_strides_t& to = kKeys ? p.k_to : p.q_to;
-  const arrow_strides_t& grad = kKeys ? a.k_out : a.q_out;
-  const T* x = (const T*)(kKeys ? p.k : p.q) + of.b * from.sequence + of.at * from.token;
-  const T* g = kBack ? (const T*)(kKeys ? p.gk : p.gq) + of.b * grad.sequence + of.at * grad.token : nullptr;
-  T* y = (T*)(kKeys ? p.yk : p.yq) + of.b * to.sequence + of.at * to.token;
+struct Heads {
   struct Pieces { Raw<T> xa, xb, ga, gb; };
-  auto load = [&](int t, int head) {
+  const RotationArgs& p;
+  const Lane& lane;
+  const arrow_strides_t &from, &to, &grad;
+  const T *x, *g;
+  T* y;
+  int heads, n, i, t, head;           // head i of n: of token t
+  Pieces next;
+
+  __device__ __forceinline__ Heads(const RotationArgs& args, const Lane& l, const Tokens& of)
+      : p(args), lane(l), from(kKeys ? args.a.k : args.a.q), to(kKeys ? args.k_to : args.q_to), grad(kKeys ? args.a.k_out : args.a.q_out) {
+    heads = kKeys ? p.a.kv_heads : p.a.q_heads;
+    n = of.count * heads;
+    x = (const T*)(kKeys ? p.k : p.q) + of.b * from.sequence + of.at * from.token;
+    g = kBack ? (const T*)(kKeys ? p.gk : p.gq) + of.b * grad.sequence + of.at * grad.token : nullptr;
+    y = (T*)(kKeys ? p.yk : p.yq) + of.b * to.sequence + of.at * to.token;
+    i = threadIdx.x >> p.lanes_log;
+    const int j = min(i, n - 1);
+    t = (uint32_t)j / (uint32_t)heads;
+    head = j - t * heads;
+    load();
+  }
+  __device__ __forceinline__ void load() {
     const T* at = x + t * from.token + head * from.head;
-    Pieces r;
-    r.xa = raw8(at + lane.first);
-    r.xb = raw8(at + lane.second);
+    next.xa = raw8(at + lane.first);
+    next.xb = raw8(at + lane.second);
     if constexpr (kBack) {
       at = g + t * grad.token + head * grad.head;
-      r.ga = raw8(at + lane.first);
-      r.gb = raw8(at + lane.second);
+      next.ga = raw8(at + lane.first);
+      next.gb = raw8(at + lane.second);
     }
-    return r;
-  };
-  // head i of token t, and `step` heads further on each time
-  int i = threadIdx.x >> p.lanes_log;
+  }
+  __device__ __forceinline__ void run(const float2* angles, const float* w, Eight* sum);
+};
+
+template <typename T, bool kBack, bool kKeys, bool kInterleaved>
+__device__ __forceinline__ void Heads<T, kBack, kKeys, kInterleaved>::run(const float2* angles, const float* w, Eight* sum) {
   if (i >= n) return;
-  int t = (uint32_t)i / (uint32_t)heads, head = i - t * heads;
-  const int step_t = step / heads, step_head = step - step_t * heads;
-  Pieces next = load(t, head);
+  const arrow_rotation_t& a = p.a;
+  const int half = a.rotary / 2, step = kThreads >> p.lanes_log, step_t = step / heads, step_head = step - step_t * heads;
   while (true) {
     const Pieces now = next;
     const int now_t = t, now_head = head;
@@ -170,7 +183,7 @@ __device__ __forceinline__ void rotate_heads(const RotationArgs& p, const Lane& 
     t += step_t;
     if (head >= heads) { head -= heads; ++t; }
     if (!more) { t = now_t; head = now_head; }
-    next = load(t, head);
+    load();
     Eight xa = wide<T>(now.xa, lane.has_first), xb = wide<T>(now.xb, lane.has_second);
     float square = 0.f;
 #pragma unroll
@@ -234,12 +247,14 @@ __global__ __launch_bounds__(kThreads) void rotation_kernel(RotationArgs p) {
   __shared__ __align__(16) float weights[2][256];
   const Lane lane(p.a, threadIdx.x & ((1 << p.lanes_log) - 1));
   const Tokens of(p, blockIdx.x);
+  Heads<T, false, false, kInterleaved> queries(p, lane, of);
+  Heads<T, false, true, kInterleaved> keys(p, lane, of);
   find_weights<W>(p, false, weights[0]);
   find_weights<W>(p, true, weights[1]);
   find_angles(p, of, angles);
   __syncthreads();
-  rotate_heads<T, false, false, kInterleaved>(p, lane, of, angles, weights[0], nullptr);
-  rotate_heads<T, false, true, kInterleaved>(p, lane, of, angles, weights[1], nullptr);
+  queries.run(angles, weights[0], nullptr);
+  keys.run(angles, weights[1], nullptr);
 }
 
 // Gradients: a workgroup has queries or keys, so that it holds the sums of one weight's gradient only.
@@ -251,10 +266,11 @@ __device__ __forceinline__ void rotate_back(const RotationArgs& p, uint32_t bloc
   Eight sum[2] = {zeros(), zeros()};
   for (uint32_t tile = block; tile < (uint32_t)p.all_tiles; tile += blocks) {
     const Tokens of(p, tile);
+    Heads<T, true, kKeys, kInterleaved> heads(p, lane, of);
     __syncthreads();                                  // (the angles of the tokens before are done with)
     find_angles(p, of, angles);
     __syncthreads();
-    rotate_heads<T, true, kKeys, kInterleaved>(p, lane, of, angles, weights, sum);
+    heads.run(angles, weights, sum);
   }
   if (!p.dwq) return;
   // the groups' sums of an element, one after the other
@@ -270,7 +286,7 @@ __device__ __forceinline__ void rotate_back(const RotationArgs& p, uint32_t bloc
 }
 
 template <typename T, typename W, bool kInterleaved>
-__global__ __launch_bounds__(kThreads, 4) void rotation_grad_kernel(RotationArgs p) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) void rotation_grad_kernel(RotationArgs p) {
   __shared__ __align__(16) float2 angles[kRotationTokens * 128];
   __shared__ __align__(16) float weights[256];
   __shared__ __align__(16) float sums[kThreads * 16];
