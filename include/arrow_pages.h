@@ -28,7 +28,7 @@ extern "C" {
 
 typedef struct arrow_pages_t {
   int32_t batch;         /* sequences                                                                                   */
-  int32_t columns;       /* of the table; columns * page is at most 2^26                                                */
+  int32_t columns;       /* of the table; columns * page is at most 2^26, batch * columns 2^31 - 1                       */
   int32_t page;          /* tokens of a page, T: a power of two                                                         */
   int32_t window, sinks; /* of the mask                                                                                 */
   int32_t tokens;        /* new tokens of each sequence; not used with offsets                                          */

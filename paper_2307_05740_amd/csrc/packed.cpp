@@ -74,7 +74,20 @@ PackedArgs plan_decode(const arrow_packed_t* c) {
   int64_t seen = std::min(c->max_len, room);
   if (p.c.window) seen = std::min(seen, (int64_t)p.c.window + p.c.sinks);
   const int64_t rows = std::max<int64_t>(1, (int64_t)c->batch * c->kv_heads * ceil_div(p.group, kHeadTile));
-  const int64_t full = p.c.window ? 512 / rows : std::max(1024 / rows, ceil_div(seen, 4096)), best = (int64_t)std::sqrt(0.2 * (double)seen);
+  // Stretches of the visible keys, each a workgroup; more than one take another launch, for their join.  One where that is not worth it; the square root of a tenth of
+  // `seen` where there are few rows; and two workgroups to a compute unit where there are many, or stretches of up to 6000 keys where lengths differ (us):
+  //   2 rows of 1000 keys: 1 stretch 9.9, 4 8.4, 8 8.0, 16 7.8, 64 9.2;  of 200, heads of 64: 1 4.9, 2 7.6
+  //   8 rows of 60,000: 16 33.1, 32 21.9, 64 20.1, 128 23.4;  32 of 1000 .. 4000: 4 13.1, 8 10.6, 16 10.4, 32 12.1
+  //   128 rows of 500 .. 2000: 1 16.4, 4 12.7, 8 13.2, 16 16.5;  512 of 125 .. 500: 1 9.8, 2 14.8;  256 of 4000 .. 16,000: 2 84, 3 79, 8 81
+  const int64_t full = std::max(512 / rows, p.c.window ? 0 : ceil_div(seen, 6000)), best = (int64_t)std::sqrt(0.1 * (double)seen);
+  p.waves = 4;
+  // Many rows under a window see equally many keys, so that workgroups of eight wavefronts fill the chip without a join (256 rows of 4096 keys: heads of 64, four wavefronts in
+  // one stretch 27.9, two 24.6, eight in one 20.7; heads of 128, 34.2, 30.1, 26.4).
+  if (p.c.window && rows >= 192 && rows <= 768 && seen > 256) {
+    p.waves = 8;
+    p.splits = 1;
+    return p;
+  }
   // A round of a workgroup's wavefronts is 128 keys: no more stretches than the longest ones' number of rounds needs.
   const int64_t rounds = std::max<int64_t>(1, ceil_div(seen, 128)), most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, full, best, rounds}));
   p.splits = seen <= 256 ? 1 : (int32_t)ceil_div(rounds, ceil_div(rounds, most));

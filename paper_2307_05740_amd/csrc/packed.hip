@@ -14,7 +14,6 @@
 namespace arrow {
 namespace {
 
-constexpr int kWaves = 4;
 
 template <int N> struct Words;
 template <> struct Words<1> { typedef uint32_t type; };
@@ -206,10 +205,11 @@ struct Codes {
   uint32_t visible;                   // keys, the same in all lanes
 };
 
-template <typename T, int D>
+template <typename T, int D, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArgs a) {
   constexpr int kSteps = D / 32;      // of the scores' inner dimension
   constexpr int kColumns = D / 16;    // columns of a lane
+  constexpr int kAhead = D == 128 ? 1 : 2;   // tiles on their way
   __shared__ __align__(16) float smem[kWaves * 16 * D + kWaves * 2 * 16];
   const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
   const arrow_packed_t& c = a.c;
@@ -219,8 +219,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
   const int head_tiles = (a.group + kHeadTile - 1) / kHeadTile;
   const int head_tile = id % head_tiles, b = id / head_tiles;
   const int head0 = head_tile * kHeadTile, heads = min(a.group - head0, kHeadTile);
-  const int64_t room = (int64_t)c.columns << a.page_log;
-  const int length = (int)max((int64_t)0, min((int64_t)c.lengths[b], room));
+  // (columns << page_log is at most 2^26.  All that follows to the first load is the same in all lanes, and said to be so where the compiler loses sight of it.)
+  const int length = __builtin_amdgcn_readfirstlane(max(0, min(c.lengths[b], c.columns << a.page_log)));
   const int begin = c.window ? max(0, length - c.window) : 0;
   // groups of 16 keys (within a page), those that only hide between the first ones and the window left out; tiles of two groups, stretches of whole rounds of the wavefronts
   const int rest = begin >> 4, lead = min((min(c.sinks, begin) + 15) >> 4, rest), groups = lead + ((length + 15) >> 4) - rest;
@@ -241,23 +241,34 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
   auto group_at = [&](int g) { return g < lead ? g : g - lead + rest; };
   auto page_of = [&](int g) { return table[group_at(min(g, groups - 1)) >> (a.page_log - 4)]; };
   int page[2] = {0, 0};               // of the tile that is loaded next, looked up a tile ahead
-  auto load = [&](int tile) {
+  auto find_pages = [&](int tile) {
+    page[0] = page_of(2 * tile);
+    page[1] = page_of(2 * tile + 1);
+  };
+  // (what a lane adds to its wavefront's addresses: of its quarter of key l % 16, of tokens 4 (l / 16) + 0..3, and of their scales)
+  const uint32_t of_key = col * (D / 2) + quarter * (D / 8), of_value = (quarter * 16 + col) * (D / 8);
+  const uint32_t of_key_scale = col * (D / 32) + quarter * (D / 4) / 32, of_value_scale = (quarter * (D / 32) + col * kColumns / 32) * 4;
+  auto load = [&](int tile, int after) {
     Codes<D> x;
     x.visible = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int g = 2 * tile + h, key0 = 16 * group_at(g), slot0 = key0 & (c.page - 1);
-      const bool in = g < groups && page[h] >= 0 && page[h] < c.pages;
-      const char* block = pool + (in ? page[h] : 0) * c.page_step;
-      const int upto = min(16, length - key0), gone = min(16, max(0, begin - key0)), first = min(16, max(0, c.sinks - key0));
-      const uint32_t mask = ((1u << max(0, upto)) - 1) & (~((1u << gone) - 1) | ((1u << first) - 1));
-      x.visible |= (in ? mask & 0xffffu : 0u) << (16 * h);
-      x.k[h] = *(const words<kSteps>*)(block + (slot0 + col) * (D / 2) + quarter * (D / 8));
-      x.ks[h] = *(const uint8_t*)(block + key_scales_at(c.page, D) + (slot0 + col) * (D / 32) + quarter * (D / 4) / 32);
-      x.v[h] = *(const words<kSteps>*)(block + values_at(c.page, D) + (((slot0 >> 2) + quarter) * 16 + col) * (D / 8));
-      x.vs[h] = *(const uint32_t*)(block + value_scales_at(c.page, D) + (((slot0 >> 2) + quarter) * (D / 32) + col * kColumns / 32) * 4);
-      page[h] = page_of(2 * (tile + kWaves) + h);
+      const bool in = g < groups && (uint32_t)page[h] < (uint32_t)c.pages;
+      const char* block = pool + (uint32_t)__builtin_amdgcn_readfirstlane(in ? page[h] : 0) * c.page_step;
+      const char *codes = block + slot0 * (D / 2), *scales = block + c.page * D + slot0 * (D / 32);
+      x.k[h] = *(const words<kSteps>*)(codes + of_key);
+      x.ks[h] = *(const uint8_t*)(scales + of_key_scale);
+      x.v[h] = *(const words<kSteps>*)(codes + c.page * (D / 2) + of_value);
+      x.vs[h] = *(const uint32_t*)(scales + c.page * (D / 32) + of_value_scale);
+      uint32_t mask = 0xffff;
+      if (key0 < begin || key0 + 16 > length) {       // at an edge of what is seen
+        const int upto = min(16, length - key0), gone = min(16, max(0, begin - key0)), first = min(16, max(0, c.sinks - key0));
+        mask = ((1u << max(0, upto)) - 1) & (~((1u << gone) - 1) | ((1u << first) - 1)) & 0xffff;
+      }
+      x.visible |= (in ? mask : 0u) << (16 * h);
     }
+    find_pages(after);
     return x;
   };
 
@@ -267,18 +278,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
   const float scale = c.scale * kLog2e;
   float top = minus_infinity(), total = 0.f;
 
-  int tile = tile0 + wave;
-  Codes<D> next;
-  if (tile < tile1) {
-    page[0] = page_of(2 * tile);
-    page[1] = page_of(2 * tile + 1);
-    next = load(tile);
-  }
-  while (tile < tile1) {
-    const Codes<D> x = next;
-    tile += kWaves;
-    if (tile < tile1) next = load(tile);
-
+  auto work = [&](const Codes<D>& x) {
     f32x4 s[2] = {(f32x4)(0.f), (f32x4)(0.f)};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -342,6 +342,24 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
       acc[2 * j] = mma16(lo.all, pf, acc[2 * j]);
       acc[2 * j + 1] = mma16(hi.all, pf, acc[2 * j + 1]);
     }
+  };
+  // (tiles beyond the last one are the last one again: loads that are always there can be told apart when one of them is waited for)
+  int tile = tile0 + wave;
+  if (tile < tile1) {
+    const int last = tile + (tile1 - 1 - tile) / kWaves * kWaves;
+    Codes<D> next[kAhead];
+    find_pages(tile);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) next[u] = load(min(tile + u * kWaves, last), min(tile + (u + 1) * kWaves, last));
+    while (tile <= last) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const Codes<D> x = next[u];
+        next[u] = load(min(tile + kAhead * kWaves, last), min(tile + (kAhead + 1) * kWaves, last));
+        if (tile <= last) work(x);
+        tile += kWaves;
+      }
+    }
   }
   total = add_quarters(total);
 
@@ -383,7 +401,8 @@ int decode(const PackedArgs& a, hipStream_t s) {
   const arrow_packed_t& c = a.c;
   const int64_t blocks = (int64_t)c.batch * c.kv_heads * a.splits * ((a.group + kHeadTile - 1) / kHeadTile), rows = (int64_t)c.batch * c.q_heads;
   if (blocks > 0x7fffffff || rows > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
-  packed_decode_kernel<T, D><<<dim3((unsigned)blocks), dim3(64 * kWaves), 0, s>>>(a);
+  if (a.waves == 4) packed_decode_kernel<T, D, 4><<<dim3((unsigned)blocks), dim3(64 * 4), 0, s>>>(a);
+  else packed_decode_kernel<T, D, 8><<<dim3((unsigned)blocks), dim3(64 * 8), 0, s>>>(a);
   if (a.splits > 1) {
     CacheArgs j{};
     j.c.dtype = c.dtype; j.c.batch = c.batch; j.c.q_heads = c.q_heads; j.c.dim = c.dim;

@@ -16,6 +16,7 @@ struct PackedArgs {
   const int64_t* slots;      // null: the last places of the sequences, by table and lengths
   int64_t tokens;
   int32_t group, splits, page_log;
+  int32_t waves;             // of a workgroup: 4 or 8
   float* parts;              // splits x batch x q_heads x (dim + 2)
 };
 

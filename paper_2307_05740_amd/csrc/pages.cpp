@@ -14,6 +14,7 @@ int check(const arrow_pages_t* a) {
   if (a->page < 1 || (a->page & (a->page - 1)) || a->page > (1 << 20)) return refuse(ARROW_EINVAL, "page = %d is no power of two up to 2^20", a->page);
   if (a->columns < 0 || (int64_t)a->columns * a->page > (1 << 26))
     return refuse(ARROW_EINVAL, "columns = %d of %d tokens each: 0 .. 2^26 tokens", a->columns, a->page);
+  if ((int64_t)a->batch * a->columns > 0x7fffffff) return refuse(ARROW_EINVAL, "a table of %d x %d entries: 2^31 - 1 at most", a->batch, a->columns);
   if (a->window < 0 || a->sinks < 0) return refuse(ARROW_EINVAL, "window = %d, sinks = %d", a->window, a->sinks);
   if (a->pages < 0 || a->pages > (1 << 30)) return refuse(ARROW_EINVAL, "pages = %lld: 0 .. 2^30", (long long)a->pages);
   if (a->offsets ? a->rows < 0 || a->rows > 0x7fffffff : a->tokens < 0 || (int64_t)a->tokens * a->batch > 0x7fffffff)
@@ -26,7 +27,7 @@ PagesArgs plan(const arrow_pages_t* a) {
   p.a = *a;
   while ((1 << p.page_log) < a->page) ++p.page_log;
   p.rows = a->offsets ? a->rows : (int64_t)a->batch * a->tokens;
-  p.one = a->batch <= kPagesBatch && p.rows <= kPagesWork;
+  p.one = a->batch <= kPagesBatch && p.rows <= kPagesRows && (int64_t)a->batch * a->columns <= kPagesEntries;
   return p;
 }
 

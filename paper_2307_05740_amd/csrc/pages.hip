@@ -13,8 +13,6 @@
 namespace arrow {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-
 // Columns that a sequence of `length` tokens needs: 0 .. lead - 1 and rest .. end - 1.
 struct Needed {
   int lead, rest, end;
@@ -61,7 +59,7 @@ struct Runs {
 struct Fresh {
   int64_t first;
   int count, position;
-  __device__ __forceinline__ Fresh(const PagesArgs& p, int b) {
+  __device__ __forceinline__ Fresh(const PagesArgs& p, int b, int now) {
     if (p.a.offsets) {
       first = max((int64_t)0, min((int64_t)p.a.offsets[b], p.rows));
       count = (int)(max(first, min((int64_t)p.a.offsets[b + 1], p.rows)) - first);
@@ -69,14 +67,15 @@ struct Fresh {
       first = (int64_t)b * p.a.tokens;
       count = p.a.tokens;
     }
-    position = (int)max((int64_t)-0x40000000, (int64_t)p.lengths[b] - count);
+    position = (int)max((int64_t)-0x40000000, (int64_t)now - count);
   }
   __device__ __forceinline__ int column(const PagesArgs& p) const { return (max(0, min(position, 1 << 30)) + p.a.page - 1) >> p.page_log; }   // the first that begins with one
 };
 
-__device__ __forceinline__ Runs given_of(const PagesArgs& p, int b, int before) { return Runs(Needed(p, before), Needed(p, p.lengths[b]), 0); }
-__device__ __forceinline__ Runs taken_of(const PagesArgs& p, int b, int before) {
-  return Runs(Needed(p, p.lengths[b]), Needed(p, before), Fresh(p, b).column(p));
+// (lengths of before and now)
+__device__ __forceinline__ Runs given_of(const PagesArgs& p, int before, int now) { return Runs(Needed(p, before), Needed(p, now), 0); }
+__device__ __forceinline__ Runs taken_of(const PagesArgs& p, int b, int before, int now) {
+  return Runs(Needed(p, now), Needed(p, before), Fresh(p, b, now).column(p));
 }
 __device__ __forceinline__ int list_size(const PagesArgs& p) { return max(0, min(p.list[0], (int)p.a.pages)); }
 
@@ -131,61 +130,139 @@ __device__ __forceinline__ int64_t slot_of(const PagesArgs& p, int position, int
   return position < 0 || page < 0 || page >= p.a.pages ? -1 : ((int64_t)page << p.page_log) + (position & (p.a.page - 1));
 }
 
-// Sums of x over the threads before this one, and over all of them.
-__device__ __forceinline__ int before_me(int x, int* all, int* room) {
+// The slot of row `row`, one of sequence b's: from the list, or from the table where its column is no new one.
+__device__ __forceinline__ int64_t slot_at(const PagesArgs& p, int b, int64_t row, int before, int now, int first, int size) {
+  const Fresh f(p, b, now);
+  if (row < f.first || row >= f.first + f.count) return -1;
+  const int position = f.position + (int)(row - f.first), column = position >> p.page_log;
+  if (position < 0 || column >= p.a.columns) return -1;
+  const int at = taken_of(p, b, before, now).place(column);
+  return slot_of(p, position, at >= 0 ? page_taken(p, first + at, size) : p.table[(int64_t)b * p.a.columns + column]);
+}
+
+// Sums of x over the threads before this one, and over all of them: two numbers in one.
+template <int kThreads>
+__device__ __forceinline__ uint64_t before_me(uint64_t x, uint64_t* all, uint64_t* room) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int sum = x;
+  uint64_t sum = x;
+#pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    const int y = __shfl_up(sum, m, 64);
+    const uint64_t y = __shfl_up((unsigned long long)sum, m, 64);
     if (lane >= m) sum += y;
   }
   __syncthreads();
   if (lane == 63) room[wave] = sum;
   __syncthreads();
-  int first = 0, total = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) first += room[w];
-    total += room[w];
+  uint64_t first = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    const uint64_t y = room[w];
+    if (w < wave) first += y;
+    total += y;
   }
   *all = total;
   return first + sum - x;
 }
 
+// The last of n rising numbers that is at most x, of those from `low` on (which is).
+__device__ __forceinline__ int last_upto(const int* numbers, int low, int n, int x) {
+  int high = n - 1;
+  while (low < high) {
+    const int mid = (low + high + 1) >> 1;
+    if (numbers[mid] <= x) low = mid;
+    else high = mid - 1;
+  }
+  return low;
+}
+
+// A step in one workgroup.  Columns that change are numbered through all sequences, so that the threads share them evenly; a page that is given back is read
+// once and put where it goes if all the others are there, too, which is nearly always so.  Where some are not, they are counted first.
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
-  __shared__ int given[kPagesBatch], taken[kPagesBatch], room[kWaves];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), batch = p.a.batch;
+  constexpr int kAhead = 4, kWaves = kThreads / 64;
+  __shared__ int before[kPagesBatch], now[kPagesBatch], given[kPagesBatch], taken[kPagesBatch];
+  __shared__ uint64_t room[kWaves];
+  const int tid = threadIdx.x, batch = p.a.batch, columns = p.a.columns;
   const int size0 = list_size(p);
-  for (int b = wave; b < batch; b += kWaves) {
-    const int before = p.held[b], n = count_given(p, b, given_of(p, b, before));
-    if ((tid & 63) == 0) { given[b] = n; taken[b] = taken_of(p, b, before).total(); }
+  // (one sequence a thread, or several one after the other)
+  const int each = (batch + kThreads - 1) / kThreads, b0 = min(batch, tid * each), b1 = min(batch, b0 + each);
+  uint64_t mine = 0, all;
+  for (int b = b0; b < b1; ++b) {
+    const int held = p.held[b], length = p.lengths[b];
+    before[b] = held;
+    now[b] = length;
+    given[b] = given_of(p, held, length).total();
+    taken[b] = taken_of(p, b, held, length).total();
+    mine += (uint64_t)given[b] << 32 | (uint32_t)taken[b];
+  }
+  uint64_t first = before_me<kThreads>(mine, &all, room);
+  for (int b = b0; b < b1; ++b) {
+    const uint64_t x = (uint64_t)given[b] << 32 | (uint32_t)taken[b];
+    given[b] = (int)(first >> 32);
+    taken[b] = (int)first;
+    first += x;
   }
   __syncthreads();
-  int gives = 0, takes = 0;
-  const int mine = tid < batch ? given[tid] : 0, mine_too = tid < batch ? taken[tid] : 0;
-  const int first = before_me(mine, &gives, room), first_too = before_me(mine_too, &takes, room);
-  if (tid < batch) { given[tid] = first; taken[tid] = first_too; }
-  __syncthreads();
-  const int size = min(size0 + gives, (int)p.a.pages);
+  int gives = (int)(all >> 32);
+  const int takes = (int)all, columns_given = gives;
   if (gives) {
-    for (int b = wave; b < batch; b += kWaves) give(p, b, given_of(p, b, p.held[b]), given[b], size0, gives);
-    __syncthreads();
-  }
-  if (takes) {
-    for (int b = wave; b < batch; b += kWaves) take(p, b, taken_of(p, b, p.held[b]), taken[b], size);
-    __syncthreads();
-  }
-  if (p.a.offsets) {                        // what no sequence has, then what one has
-    for (int64_t i = tid; i < p.rows; i += kThreads) p.slots[i] = -1;
-    __syncthreads();
-  }
-  for (int b = p.rows ? wave : batch; b < batch; b += kWaves) {
-    const Fresh f(p, b);
-    for (int i = tid & 63; i < f.count; i += 64) {
-      const int position = f.position + i, column = position >> p.page_log;
-      p.slots[f.first + i] = slot_of(p, position, position >= 0 && column < p.a.columns ? p.table[(int64_t)b * p.a.columns + column] : -1);
+    bool hole = false;
+    for (int i0 = tid; i0 < columns_given; i0 += kAhead * kThreads) {
+      int page[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads;
+        if (i >= columns_given) continue;
+        const int b = last_upto(given, 0, batch, i);
+        page[j] = p.table[(int64_t)b * columns + given_of(p, before[b], now[b]).column(i - given[b])];
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads, at = size0 + gives - 1 - i;
+        if (i >= columns_given) continue;
+        hole = hole || page[j] < 0 || page[j] >= p.a.pages;
+        if (at < p.a.pages) p.list[1 + at] = page[j];            // (behind the list's end until it is said to be longer)
+      }
     }
+    if (__syncthreads_or(hole)) {
+      const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+      for (int b = wave; b < batch; b += kWaves) {
+        const int n = count_given(p, b, given_of(p, before[b], now[b]));
+        if ((tid & 63) == 0) given[b] = n;
+      }
+      __syncthreads();
+      mine = 0;
+      for (int b = b0; b < b1; ++b) mine += given[b];
+      first = before_me<kThreads>(mine, &all, room);
+      for (int b = b0; b < b1; ++b) {
+        const int n = given[b];
+        given[b] = (int)first;
+        first += n;
+      }
+      gives = (int)all;
+      __syncthreads();
+      for (int b = wave; b < batch; b += kWaves) give(p, b, given_of(p, before[b], now[b]), given[b], size0, gives);
+    } else {
+      for (int i = tid; i < columns_given; i += kThreads) {
+        const int b = last_upto(given, 0, batch, i);
+        p.table[(int64_t)b * columns + given_of(p, before[b], now[b]).column(i - given[b])] = -1;
+      }
+    }
+    __syncthreads();
   }
-  for (int b = tid; b < batch; b += kThreads) p.held[b] = p.lengths[b];
+  const int size = min(size0 + gives, (int)p.a.pages);
+  for (int i = tid; i < takes; i += kThreads) {
+    const int b = last_upto(taken, 0, batch, i);
+    p.table[(int64_t)b * columns + taken_of(p, b, before[b], now[b]).column(i - taken[b])] = page_taken(p, i, size);
+  }
+  // (a slot's page is looked for in the list where it is a new one: nothing here waits for the table)
+  for (int row = tid; row < p.rows; row += kThreads) {
+    int b;
+    if (p.a.offsets) b = p.a.offsets[0] > row ? -1 : last_upto(p.a.offsets, 0, batch, row);
+    else b = row / p.a.tokens;
+    p.slots[row] = b < 0 || b >= batch ? -1 : slot_at(p, b, row, before[b], now[b], taken[b], size);
+  }
+  for (int b = b0; b < b1; ++b) p.held[b] = now[b];
   if (tid == 0) p.list[0] = max(0, size - takes);
 }
 
@@ -193,30 +270,31 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
 __global__ __launch_bounds__(256) void pages_count_kernel(PagesArgs p) {
   const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (b >= p.a.batch) return;
-  const int before = p.held[b], n = count_given(p, b, given_of(p, b, before));
+  const int before = p.held[b], n = count_given(p, b, given_of(p, before, p.lengths[b]));
   if (threadIdx.x & 63) return;
   p.before[b] = before;
   p.given[b] = n;
-  p.taken[b] = taken_of(p, b, before).total();
+  p.taken[b] = taken_of(p, b, before, p.lengths[b]).total();
 }
 
-__global__ __launch_bounds__(kThreads) void pages_sum_kernel(PagesArgs p) {
-  __shared__ int room[kWaves];
-  int gives = 0, takes = 0;
-  for (int b0 = 0; b0 < p.a.batch; b0 += kThreads) {
+constexpr int kSumThreads = 1024;
+
+__global__ __launch_bounds__(kSumThreads) void pages_sum_kernel(PagesArgs p) {
+  __shared__ uint64_t room[kSumThreads / 64];
+  uint64_t sum = 0;                          // what is given back, and taken
+  for (int b0 = 0; b0 < p.a.batch; b0 += kSumThreads) {
     const int b = b0 + threadIdx.x;
-    int all, all_too;
-    const int first = before_me(b < p.a.batch ? p.given[b] : 0, &all, room), first_too = before_me(b < p.a.batch ? p.taken[b] : 0, &all_too, room);
+    uint64_t all;
+    const uint64_t first = sum + before_me<kSumThreads>(b < p.a.batch ? (uint64_t)p.given[b] << 32 | (uint32_t)p.taken[b] : 0, &all, room);
     if (b < p.a.batch) {
-      p.given[b] = gives + first;
-      p.taken[b] = takes + first_too;
+      p.given[b] = (int)(first >> 32);
+      p.taken[b] = (int)first;
       p.held[b] = p.lengths[b];
     }
-    gives += all;
-    takes += all_too;
+    sum += all;
   }
   if (threadIdx.x) return;
-  const int size0 = list_size(p), size = min(size0 + gives, (int)p.a.pages);
+  const int gives = (int)(sum >> 32), takes = (int)sum, size0 = list_size(p), size = min(size0 + gives, (int)p.a.pages);
   p.sizes[0] = size0;
   p.sizes[1] = gives;
   p.sizes[2] = size;
@@ -226,43 +304,44 @@ __global__ __launch_bounds__(kThreads) void pages_sum_kernel(PagesArgs p) {
 __global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p) {
   const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (b >= p.a.batch) return;
-  give(p, b, given_of(p, b, p.before[b]), p.given[b], p.sizes[0], p.sizes[1]);
+  give(p, b, given_of(p, p.before[b], p.lengths[b]), p.given[b], p.sizes[0], p.sizes[1]);
 }
 
 // Takes and slots: neither waits for the other, as a slot's page is found in the list where it is a new one.
+constexpr int kRowsEach = 8;
+
 __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_blocks) {
-  const int size = p.sizes[2];
+  __shared__ int counts[2][4];
+  const int size = p.sizes[2], tid = threadIdx.x, batch = p.a.batch;
   if ((int)blockIdx.x < take_blocks) {
-    const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    if (b < p.a.batch) take(p, b, taken_of(p, b, p.before[b]), p.taken[b], size);
+    const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (b < batch) take(p, b, taken_of(p, b, p.before[b], p.lengths[b]), p.taken[b], size);
     return;
   }
-  const int64_t row = (int64_t)(blockIdx.x - take_blocks) * 256 + threadIdx.x;
-  if (row >= p.rows) return;
-  int b;
-  if (p.a.offsets) {                        // the last sequence that begins at or before the row
-    int low = 0, high = p.a.batch;
-    while (low < high) {
-      const int mid = (low + high) >> 1;
-      if (p.a.offsets[mid] <= row) low = mid + 1;
-      else high = mid;
+  const int64_t row0 = (int64_t)(blockIdx.x - take_blocks) * (256 * kRowsEach), last = min(row0 + 256 * kRowsEach, p.rows) - 1;
+  int low = 0, high = 0;                     // sequences that the first and the last row may be of
+  if (p.a.offsets) {
+    for (int b = tid; b < batch; b += 256) {
+      const int first = p.a.offsets[b];
+      low += first <= row0;
+      high += first <= last;
     }
-    b = low - 1;
-  } else {
-    b = (int)(row / p.a.tokens);
+    for (int m = 32; m; m >>= 1) { low += __shfl_xor(low, m, 64); high += __shfl_xor(high, m, 64); }
+    if ((tid & 63) == 0) { counts[0][tid >> 6] = low; counts[1][tid >> 6] = high; }
+    __syncthreads();
+    low = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
+    high = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
   }
-  int64_t slot = -1;
-  if (b >= 0) {
-    const Fresh f(p, b);
-    if (row >= f.first && row < f.first + f.count) {
-      const int position = f.position + (int)(row - f.first), column = position >> p.page_log;
-      if (position >= 0 && column < p.a.columns) {
-        const int at = taken_of(p, b, p.before[b]).place(column);
-        slot = slot_of(p, position, at >= 0 ? page_taken(p, p.taken[b] + at, size) : p.table[(int64_t)b * p.a.columns + column]);
-      }
-    }
+#pragma unroll
+  for (int j = 0; j < kRowsEach; ++j) {
+    const int64_t row = row0 + j * 256 + tid;
+    if (row >= p.rows) return;
+    int b;
+    if (!p.a.offsets) b = (int)(row / p.a.tokens);
+    else if (high == 0 || (low == 0 && p.a.offsets[0] > row)) b = -1;
+    else b = last_upto(p.a.offsets, max(0, low - 1), high, (int)row);
+    p.slots[row] = b < 0 || b >= batch ? -1 : slot_at(p, b, row, p.before[b], p.lengths[b], p.taken[b], size);
   }
-  p.slots[row] = slot;
 }
 
 }  // namespace
@@ -270,14 +349,17 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
 int launch_pages_step(const PagesArgs& p, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (p.one) {
-    pages_step_kernel<<<dim3(1), dim3(kThreads), 0, s>>>(p);
+    // (fewer threads wait less for each other)
+    if (p.a.batch <= 256 && p.rows <= 2048) pages_step_kernel<256><<<dim3(1), dim3(256), 0, s>>>(p);
+    else pages_step_kernel<1024><<<dim3(1), dim3(1024), 0, s>>>(p);
     return (int)hipGetLastError();
   }
-  const unsigned fours = (unsigned)((p.a.batch + 3) / 4), rows = (unsigned)((p.rows + 255) / 256);
+  const unsigned fours = (unsigned)((p.a.batch + 3) / 4), rows = (unsigned)((p.rows + 256 * kRowsEach - 1) / (256 * kRowsEach));
   if (fours) pages_count_kernel<<<dim3(fours), dim3(256), 0, s>>>(p);
-  pages_sum_kernel<<<dim3(1), dim3(kThreads), 0, s>>>(p);
+  pages_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, s>>>(p);
   if (fours) pages_give_kernel<<<dim3(fours), dim3(256), 0, s>>>(p);
-  if (fours + rows) pages_take_kernel<<<dim3(fours + rows), dim3(256), 0, s>>>(p, (int)fours);
+  // (without new tokens nothing is taken)
+  if (rows) pages_take_kernel<<<dim3(fours + rows), dim3(256), 0, s>>>(p, (int)fours);
   return (int)hipGetLastError();
 }
 

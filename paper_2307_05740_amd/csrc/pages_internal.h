@@ -9,7 +9,8 @@
 namespace arrow {
 
 constexpr int kPagesBatch = 1024;          // sequences of a step in one launch, at most
-constexpr int64_t kPagesWork = 8192;       // new tokens of one
+constexpr int64_t kPagesRows = 8192;       // new tokens of one, at most
+constexpr int64_t kPagesEntries = 65536;   // and entries of its table
 
 struct PagesArgs {
   arrow_pages_t a;

@@ -188,6 +188,20 @@ def test_long_caches_in_stretches(torch, Packed, dtype, window, sinks):
 
 
 @pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("batch,kv", [(48, 4), (200, 1), (47, 4), (193, 4)])
+def test_many_rows_under_a_window(torch, Packed, dim, batch, kv):
+    """Around the numbers of rows that have workgroups of eight wavefronts."""
+    op = Packed(300, 5)
+    g = torch.Generator().manual_seed(batch)
+    lengths = torch.randint(0, 900, (batch,), generator=g).tolist()
+    pool, table, n, keys, values = filled(torch, op, TYPES[batch % 2], lengths, 32, kv, dim)
+    q = normal(torch, 3, TYPES[batch % 2], batch, 2 * kv, dim, by=2.0)
+    o = op.decode(q, pool, table, n, 900)
+    part = slice(0, batch, 5)
+    check(torch, op, o[part], q[part], keys[part], values[part])
+
+
+@pytest.mark.parametrize("dim", [32, 64, 128])
 def test_new_tokens(torch, Packed, dim):
     """k and v go to their place first; those without one (an idle sequence, a page that is not there, a row of the table that is too short) nowhere."""
     op, page = Packed(), 16
