@@ -268,79 +268,143 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
 
 // ---- larger steps ----
 __global__ __launch_bounds__(256) void pages_count_kernel(PagesArgs p) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.sizes[0] = list_size(p);
   const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (b >= p.a.batch) return;
-  const int before = p.held[b], n = count_given(p, b, given_of(p, before, p.lengths[b]));
+  const int before = p.held[b], now = p.lengths[b], n = count_given(p, b, given_of(p, before, now));
   if (threadIdx.x & 63) return;
   p.before[b] = before;
   p.given[b] = n;
-  p.taken[b] = taken_of(p, b, before, p.lengths[b]).total();
+  p.taken[b] = taken_of(p, b, before, now).total();
+}
+
+// What is given back and taken in all, and before each sequence.  Of up to kPagesBatch sequences every workgroup adds them up for itself, into LDS; of more one has done so, in place.
+struct Sums {
+  const int *given, *taken;
+  int size0, gives, takes;
+  __device__ __forceinline__ int size(const PagesArgs& p) const { return min(size0 + gives, (int)p.a.pages); }
+};
+
+template <int kThreads>
+__device__ __forceinline__ Sums add_up(const PagesArgs& p, int* given, int* taken, uint64_t* room) {
+  const int batch = p.a.batch, each = (batch + kThreads - 1) / kThreads, b0 = min(batch, (int)threadIdx.x * each), b1 = min(batch, b0 + each);
+  uint64_t mine = 0, all;
+  for (int b = b0; b < b1; ++b) mine += (uint64_t)p.given[b] << 32 | (uint32_t)p.taken[b];
+  uint64_t first = before_me<kThreads>(mine, &all, room);
+  for (int b = b0; b < b1; ++b) {
+    const uint64_t x = (uint64_t)p.given[b] << 32 | (uint32_t)p.taken[b];
+    given[b] = (int)(first >> 32);
+    taken[b] = (int)first;
+    first += x;
+  }
+  __syncthreads();
+  return {given, taken, p.sizes[0], (int)(all >> 32), (int)all};
 }
 
 constexpr int kSumThreads = 1024;
 
 __global__ __launch_bounds__(kSumThreads) void pages_sum_kernel(PagesArgs p) {
   __shared__ uint64_t room[kSumThreads / 64];
-  uint64_t sum = 0;                          // what is given back, and taken
-  for (int b0 = 0; b0 < p.a.batch; b0 += kSumThreads) {
-    const int b = b0 + threadIdx.x;
-    uint64_t all;
-    const uint64_t first = sum + before_me<kSumThreads>(b < p.a.batch ? (uint64_t)p.given[b] << 32 | (uint32_t)p.taken[b] : 0, &all, room);
-    if (b < p.a.batch) {
-      p.given[b] = (int)(first >> 32);
-      p.taken[b] = (int)first;
-      p.held[b] = p.lengths[b];
-    }
-    sum += all;
-  }
+  const Sums s = add_up<kSumThreads>(p, p.given, p.taken, room);
   if (threadIdx.x) return;
-  const int gives = (int)(sum >> 32), takes = (int)sum, size0 = list_size(p), size = min(size0 + gives, (int)p.a.pages);
-  p.sizes[0] = size0;
-  p.sizes[1] = gives;
-  p.sizes[2] = size;
-  p.list[0] = max(0, size - takes);
+  p.sizes[1] = s.gives;
+  p.sizes[2] = s.takes;
 }
 
-__global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p) {
+struct Room {
+  int given[kPagesBatch], taken[kPagesBatch];
+  uint64_t sums[4];
+};
+__device__ __forceinline__ Sums sums_of(const PagesArgs& p, Room& room) {
+  if (p.a.batch <= kPagesBatch) return add_up<256>(p, room.given, room.taken, room.sums);
+  return {p.given, p.taken, p.sizes[0], p.sizes[1], p.sizes[2]};
+}
+
+// The state after the step, by the last kernel's first workgroups.
+__device__ __forceinline__ void finish(const PagesArgs& p, const Sums& s, int block, int blocks) {
+  for (int b = block * 256 + threadIdx.x; b < p.a.batch; b += blocks * 256) p.held[b] = p.lengths[b];
+  if (block == 0 && threadIdx.x == 0) p.list[0] = max(0, s.size(p) - s.takes);
+}
+
+__global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p, bool last) {
+  __shared__ Room room;
+  const Sums s = sums_of(p, room);
   const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  if (b >= p.a.batch) return;
-  give(p, b, given_of(p, p.before[b], p.lengths[b]), p.given[b], p.sizes[0], p.sizes[1]);
+  if (b < p.a.batch) give(p, b, given_of(p, p.before[b], p.lengths[b]), s.given[b], s.size0, s.gives);
+  if (last) finish(p, s, blockIdx.x, gridDim.x);
 }
 
 // Takes and slots: neither waits for the other, as a slot's page is found in the list where it is a new one.
 constexpr int kRowsEach = 8;
 
 __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_blocks) {
+  __shared__ Room room;
   __shared__ int counts[2][4];
-  const int size = p.sizes[2], tid = threadIdx.x, batch = p.a.batch;
-  if ((int)blockIdx.x < take_blocks) {
-    const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (b < batch) take(p, b, taken_of(p, b, p.before[b], p.lengths[b]), p.taken[b], size);
-    return;
-  }
-  const int64_t row0 = (int64_t)(blockIdx.x - take_blocks) * (256 * kRowsEach), last = min(row0 + 256 * kRowsEach, p.rows) - 1;
-  int low = 0, high = 0;                     // sequences that the first and the last row may be of
-  if (p.a.offsets) {
+  const int tid = threadIdx.x, batch = p.a.batch;
+  // (offsets are on their way while the sums are added up)
+  const int64_t row0 = (int64_t)((int)blockIdx.x - take_blocks) * (256 * kRowsEach), last = min(row0 + 256 * kRowsEach, p.rows) - 1;
+  int low = 0, high = 0;                     // the sequences that the first and the last row may be of
+  if (p.a.offsets)
     for (int b = tid; b < batch; b += 256) {
       const int first = p.a.offsets[b];
       low += first <= row0;
       high += first <= last;
     }
+  const Sums s = sums_of(p, room);
+  const int size = s.size(p);
+  if ((int)blockIdx.x < take_blocks) {
+    const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (b < batch) take(p, b, taken_of(p, b, p.before[b], p.lengths[b]), s.taken[b], size);
+    finish(p, s, blockIdx.x, take_blocks);
+    return;
+  }
+  if (p.a.offsets) {
     for (int m = 32; m; m >>= 1) { low += __shfl_xor(low, m, 64); high += __shfl_xor(high, m, 64); }
     if ((tid & 63) == 0) { counts[0][tid >> 6] = low; counts[1][tid >> 6] = high; }
     __syncthreads();
-    low = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
-    high = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
+    low = __builtin_amdgcn_readfirstlane(counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3]) - 1;
+    high = __builtin_amdgcn_readfirstlane(counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3]) - 1;
+  } else {
+    low = (int)(row0 / p.a.tokens);
+    high = (int)(last / p.a.tokens);
   }
+  if (high - low <= 4) {
+    // few sequences: one after the other, with what they have in common worked out once
+    int64_t done = row0;                     // (rows up to there are written)
+    for (int b = max(low, 0); b <= high; ++b) {
+      const int now = p.lengths[b], before = p.before[b], first = s.taken[b];
+      const Fresh f(p, b, now);
+      const Runs runs = taken_of(p, b, before, now);
+      const int64_t begin = max(done, f.first), end = min(last + 1, f.first + f.count);
+      for (int64_t row = done + tid; row < min(begin, last + 1); row += 256) p.slots[row] = -1;
+      int page[kRowsEach], position[kRowsEach];
 #pragma unroll
-  for (int j = 0; j < kRowsEach; ++j) {
-    const int64_t row = row0 + j * 256 + tid;
-    if (row >= p.rows) return;
+      for (int j = 0; j < kRowsEach; ++j) {
+        const int64_t row = begin + j * 256 + tid;
+        page[j] = position[j] = -1;
+        if (row >= end) continue;
+        position[j] = f.position + (int)(row - f.first);
+        const int column = position[j] >> p.page_log;
+        if (position[j] < 0 || column >= p.a.columns) continue;
+        const int at = runs.place(column);
+        const int32_t* where = at < 0 ? p.table + (int64_t)b * p.a.columns + column : first + at < size ? p.list + size - first - at : nullptr;
+        if (where) page[j] = *where;
+      }
+#pragma unroll
+      for (int j = 0; j < kRowsEach; ++j) {
+        const int64_t row = begin + j * 256 + tid;
+        if (row < end) p.slots[row] = slot_of(p, position[j], page[j]);
+      }
+      done = max(done, end);
+    }
+    for (int64_t row = done + tid; row <= last; row += 256) p.slots[row] = -1;
+    return;
+  }
+  for (int64_t row = row0 + tid; row <= last; row += 256) {
     int b;
     if (!p.a.offsets) b = (int)(row / p.a.tokens);
-    else if (high == 0 || (low == 0 && p.a.offsets[0] > row)) b = -1;
-    else b = last_upto(p.a.offsets, max(0, low - 1), high, (int)row);
-    p.slots[row] = b < 0 || b >= batch ? -1 : slot_at(p, b, row, p.before[b], p.lengths[b], p.taken[b], size);
+    else b = low < 0 && p.a.offsets[0] > row ? -1 : last_upto(p.a.offsets, max(0, low), high + 1, (int)row);
+    p.slots[row] = b < 0 ? -1 : slot_at(p, b, row, p.before[b], p.lengths[b], s.taken[b], size);
   }
 }
 
@@ -356,8 +420,8 @@ int launch_pages_step(const PagesArgs& p, void* stream) {
   }
   const unsigned fours = (unsigned)((p.a.batch + 3) / 4), rows = (unsigned)((p.rows + 256 * kRowsEach - 1) / (256 * kRowsEach));
   if (fours) pages_count_kernel<<<dim3(fours), dim3(256), 0, s>>>(p);
-  pages_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, s>>>(p);
-  if (fours) pages_give_kernel<<<dim3(fours), dim3(256), 0, s>>>(p);
+  if (p.a.batch > kPagesBatch) pages_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, s>>>(p);
+  if (fours) pages_give_kernel<<<dim3(fours), dim3(256), 0, s>>>(p, rows == 0);
   // (without new tokens nothing is taken)
   if (rows) pages_take_kernel<<<dim3(fours + rows), dim3(256), 0, s>>>(p, (int)fours);
   return (int)hipGetLastError();
