@@ -12,6 +12,14 @@ void plan_score(ScoreArgs& p) {
   // they are cut further, down to a piece per lane.
   const int64_t each = 16 / size_of(p.a.dtype), pieces = ceil_div((int64_t)p.a.vocabulary, each) + 1;
   const int64_t least = p.a.top ? ceil_div(pieces, kScoreThreads * kMostVectors) : ceil_div(pieces, kMostPieces), most = ceil_div(pieces, kScoreThreads);
+  // Rows of few pieces have 16 lanes or a wavefront each, where there are enough of them for longer ones.  (Tokens on top are looked for among those that lanes have as their
+  // largest: there have to be some more lanes than tokens.)
+  p.parts = 1;
+  p.lanes = pieces <= 16 * 4 && p.a.top <= 8 ? 16 : pieces <= 64 * 4 || (pieces <= 64 * 8 && p.a.rows >= 512) ? 64 : 0;
+  if (p.lanes) {
+    p.vectors = (int32_t)(ceil_div(pieces, p.lanes) * p.lanes);
+    return;
+  }
   const int64_t limit = p.a.top ? 64 : 128;       // (of lists that are joined)
   const int64_t wanted = std::max<int64_t>(least, std::min<int64_t>({most, limit, 512 / std::max<int64_t>(1, p.a.rows)}));
   const int64_t rounds = ceil_div(pieces, wanted * kScoreThreads);           // pieces per lane

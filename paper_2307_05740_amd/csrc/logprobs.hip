@@ -8,6 +8,7 @@
 // The few pieces that reach it are read again, and their keys from it on go to a list in LDS, where each is placed by counting those before it.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "attention_common.h"
@@ -108,23 +109,34 @@ __device__ __forceinline__ float value_of(uint64_t key) {
   return u == 0xffffffffu ? __builtin_nanf("") : __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-// The largest number that `count` or more of these lanes' are at least, from bit `bits` - 1 on below `base`; 0 bits more than there are lanes' numbers leave base.
+// The largest number that `count` or more of these lanes' are at least, from bit `bits` - 1 on below `base`; or, where that many are, the first that is found with no
+// more than these above it.  `lanes` and so the result may differ from lane to lane.
 __device__ __forceinline__ uint32_t nth_of(uint32_t x, uint64_t lanes, int count, uint32_t base, int bits) {
+  bool done = false;
   for (int b = bits - 1; b >= 0; --b) {
     const uint32_t more = base | 1u << b;
-    base = __popcll(__ballot(x >= more) & lanes) >= count ? more : base;
+    // (lanes' own numbers are compared with their own group's)
+    const int n = __popcll(__ballot(x >= more) & lanes);
+    base = !done && n >= count ? more : base;
+    done = done || n == count;
+    if (__all(done)) break;
   }
   return base;
 }
 
-// The key that comes `count`-th among the lanes', 0 where there are fewer.  Indices have `bits` bits.
-__device__ __forceinline__ uint64_t nth_key(uint64_t key, int count, int bits) {
+// A number that the `count`-th of the lanes' keys is at least, as near to it as is worth it; 0 where there are fewer.  Indices have `bits` bits.
+__device__ __forceinline__ uint64_t nth_key(uint64_t key, uint64_t lanes, int count, int bits) {
   const uint32_t high = (uint32_t)(key >> 32), low = (uint32_t)key;
-  const uint32_t value = nth_of(high, ~(uint64_t)0, count, 0, 32);
-  if (value == 0) return 0;
-  const uint64_t tied = __ballot(high == value);
-  const int rest = count - __popcll(__ballot(high > value));
-  return (uint64_t)value << 32 | nth_of(low, tied, rest, ~0u << bits, bits);
+  const uint32_t value = nth_of(high, lanes, count, 0, 32);
+  const int above = __popcll(__ballot(high >= value) & lanes);
+  // (several lanes have the value that the count-th has: those of the lowest indices)
+  uint32_t index = 0;
+  if (__any(value && above > count)) {
+    const uint64_t tied = __ballot(high == value) & lanes;
+    index = nth_of(low, tied, count - (above - __popcll(tied)), ~0u << bits, bits);
+    index = above > count ? index : 0;
+  }
+  return value ? (uint64_t)value << 32 | index : 0;
 }
 
 struct Chosen {
@@ -137,7 +149,7 @@ struct Chosen {
 // The border from every lane's largest key (0: it has none); all threads of the workgroup.
 __device__ __forceinline__ uint64_t border_of(uint64_t key, int top, int bits, Chosen& c) {
   if (threadIdx.x == 0) c.count = 0;
-  const uint64_t mine = nth_key(key, top, bits);
+  const uint64_t mine = nth_key(key, ~(uint64_t)0, top, bits);
   if ((threadIdx.x & 63) == 0) c.border[threadIdx.x >> 6] = mine;
   __syncthreads();
   uint64_t b = c.border[0];
@@ -465,6 +477,139 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
       });
 }
 
+// Rows of few pieces: L lanes each, of which each holds N pieces; nothing is cut, and the rows of a wavefront have nothing to do with each other.
+template <int L>
+struct ChosenOfRows {
+  static constexpr int kRows = kThreads / L, kRoom = kList / kRows;
+  uint64_t list[kRows][kRoom];
+  int count[kRows];
+};
+
+template <typename T, int L, int N, bool kTop>
+__global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
+  using P = Piece<T>;
+  constexpr int kLog = L == 16 ? 4 : 6, kRows = kThreads / L;
+  __shared__ std::conditional_t<kTop, ChosenOfRows<L>, int> chosen;
+  const int sub = threadIdx.x & (L - 1), mine_of = threadIdx.x / L;
+  const int64_t at_row = (int64_t)blockIdx.x * kRows + mine_of, row = min(at_row, p.a.rows - 1);     // (rows that are not there are the last one again)
+  const bool there = at_row < p.a.rows;
+  const uint64_t lanes = L == 64 ? ~(uint64_t)0 : (uint64_t)0xffff << (threadIdx.x & 48);
+  const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
+  const u32x4* at = r.piece(0);
+  const Target target(p, row, (const T*)nullptr);
+  u32x4 x[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    x[j] = u32x4{P::kNothing, P::kNothing, P::kNothing, P::kNothing};
+    if (j * L + sub < r.pieces) x[j] = at[j * L + sub];
+  }
+  const int edge = r.edge(sub, p.a.vocabulary);
+  const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity(), c = p.a.scale * kLog2e;
+  LaneSums lane(c);
+  float most[N], mine = beside;
+  if (edge >= 0) { lane.start(beside); lane.add(beside); }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    most[j] = minus_infinity();
+    if (j * L + sub >= r.pieces) continue;
+    most[j] = P::get(x[j], 0);
+#pragma unroll
+    for (int i = 1; i < P::kEach; ++i) most[j] = larger(most[j], P::get(x[j], i));
+    mine = larger(mine, most[j]);
+    if (j == 0 && edge < 0) lane.start(most[j]);
+    else if (lane.exceeded(most[j])) lane.raise(most[j]);
+#pragma unroll
+    for (int i = 0; i < P::kEach; ++i) lane.add(P::get(x[j], i));
+  }
+  Sums lane_sums = lane.exact();
+  const bool failed = (__ballot(lane.failed()) & lanes) != 0;
+  if (failed) {
+    lane = LaneSums(c);
+    lane.M = over_lanes(mine, kLog, larger);               // (all lanes of a row are here)
+    lane.add_any(beside);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const u32x4 again = here(x[j]);
+#pragma unroll
+      for (int i = 0; i < P::kEach; ++i) lane.add_any(P::get(again, i));
+    }
+    lane_sums = {lane.M, lane.s, lane.w};
+  }
+  Sums sum = lane_sums;
+  sum.raise(over_lanes(sum.M, kLog, larger), c);
+  sum.s = sum_of_lanes(sum.s, kLog);
+  sum.w = sum_of_lanes(sum.w, kLog);
+  const Stats s(sum);
+  if (there && sub == 0) write_row(p, row, s, target);
+
+  if constexpr (kTop) {
+    const int top = p.a.top;
+    uint64_t* list = chosen.list[mine_of];
+    if (sub == 0) chosen.count[mine_of] = 0;
+    auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
+    uint64_t key = edge >= 0 ? key_of(beside, edge) : 0;
+    int found = -1;
+    u32x4 piece = x[0];
+#pragma unroll
+    for (int j = N - 1; j >= 0; --j)
+      if (j * L + sub < r.pieces && alike(most[j], mine)) {
+        found = j * L + sub;
+        piece = x[j];
+      }
+    if (found >= 0) {
+      int e = 0;
+#pragma unroll
+      for (int i = P::kEach - 1; i >= 0; --i) e = alike(P::get(piece, i), mine) ? i : e;
+      key = max(key, key_of(mine, r.index(found, e)));
+    }
+    const uint64_t border = nth_key(key, lanes, top, index_bits(p.a.vocabulary));
+    const float least = border ? value_of(border) : minus_infinity();
+    __syncthreads();
+    auto keep = [&](float v, int index) {
+      if (v < least) return;
+      const uint64_t k = key_of(v, index);
+      if (k < border) return;
+      const int to = atomicAdd(&chosen.count[mine_of], 1);   // (the order in the list does not matter)
+      if (to < ChosenOfRows<L>::kRoom) list[to] = k;
+    };
+    if (edge >= 0) keep(beside, edge);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j * L + sub < r.pieces && !(most[j] < least)) {
+#pragma unroll
+        for (int e = 0; e < P::kEach; ++e) keep(P::get(x[j], e), r.index(j * L + sub, e));
+      }
+    __syncthreads();
+    const int n = chosen.count[mine_of];
+    if (n <= ChosenOfRows<L>::kRoom) {
+      for (int i = sub; i < n; i += L) {
+        const uint64_t k = list[i];
+        int before = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) before += list[j] > k;
+        if (there && before < top) write_top(p, row, before, k, s);
+      }
+    } else {
+      // no room: the largest key below the last one, `top` times
+      uint64_t last = ~(uint64_t)0;
+      for (int i = 0; i < top; ++i) {
+        uint64_t best = 0;
+        auto next = [&](uint64_t k) { best = k < last && k > best ? k : best; };
+        if (edge >= 0) next(key_of(beside, edge));
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j * L + sub < r.pieces) {
+#pragma unroll
+            for (int e = 0; e < P::kEach; ++e) next(key_of(P::get(x[j], e), r.index(j * L + sub, e)));
+          }
+        for (int m = L / 2; m; m >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, m, 64));
+        if (there && sub == 0) write_top(p, row, i, best, s);
+        last = best;
+      }
+    }
+  }
+}
+
 // The parts of a row.  All loads that others do not wait for come first.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
@@ -536,12 +681,12 @@ __device__ __forceinline__ void put_value(u32x4& r, int i, float x) {
 
 constexpr int kGradPieces = 4;        // of a lane
 
-// Gradients: a wavefront has 256 pieces of a row.
-template <typename T>
+// Gradients: L lanes have four pieces each of a row.
+template <typename T, int L>
 __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int chunks) {
   using P = Piece<T>;
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * kWaves + wave_id();
+  const int lane = threadIdx.x & (L - 1);
+  const int64_t id = (int64_t)blockIdx.x * (kThreads / L) + (L == 64 ? wave_id() : (int)(threadIdx.x / L));
   const int64_t row = id / chunks;
   const int chunk = (int)(id - row * chunks);
   if (row >= p.a.rows) return;
@@ -562,11 +707,11 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int c
   const Row<T> r(in, p.a.vocabulary);
   // (pieces of both where the two rows lie alike)
   const bool alike = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
-  const int first = chunk * 64 * kGradPieces;
+  const int first = chunk * L * kGradPieces;
   u32x4 x[kGradPieces];
 #pragma unroll
   for (int j = 0; j < kGradPieces; ++j) {
-    const int i = first + j * 64 + lane;
+    const int i = first + j * L + lane;
     if (i < r.pieces) x[j] = *r.piece(i);
   }
   if (chunk == 0) {
@@ -575,7 +720,7 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int c
   }
 #pragma unroll
   for (int j = 0; j < kGradPieces; ++j) {
-    const int i = first + j * 64 + lane;
+    const int i = first + j * L + lane;
     if (i >= r.pieces) break;
     u32x4 y = {0, 0, 0, 0};
 #pragma unroll
@@ -590,8 +735,25 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int c
   }
 }
 
+template <typename T, bool kTop>
+int rows(const ScoreArgs& p, hipStream_t s) {
+  const int lanes = p.lanes, n = p.vectors / lanes;
+  const dim3 grid((unsigned)((p.a.rows + kThreads / lanes - 1) / (kThreads / lanes))), block(kThreads);
+  if (lanes == 16) {
+    if (n <= 1) score_rows_kernel<T, 16, 1, kTop><<<grid, block, 0, s>>>(p);
+    else if (n <= 2) score_rows_kernel<T, 16, 2, kTop><<<grid, block, 0, s>>>(p);
+    else score_rows_kernel<T, 16, 4, kTop><<<grid, block, 0, s>>>(p);
+  } else {
+    if (n <= 2) score_rows_kernel<T, 64, 2, kTop><<<grid, block, 0, s>>>(p);
+    else if (n <= 4) score_rows_kernel<T, 64, 4, kTop><<<grid, block, 0, s>>>(p);
+    else score_rows_kernel<T, 64, 8, kTop><<<grid, block, 0, s>>>(p);
+  }
+  return (int)hipGetLastError();
+}
+
 template <typename T>
 int forward(const ScoreArgs& p, hipStream_t s) {
+  if (p.lanes) return p.a.top ? rows<T, true>(p, s) : rows<T, false>(p, s);
   const int64_t blocks = p.a.rows * p.parts;
   if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(kThreads);
@@ -607,13 +769,18 @@ int forward(const ScoreArgs& p, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
+template <typename T, int L>
+int backward(const ScoreArgs& p, hipStream_t s) {
+  const int chunks = (int)std::max<int64_t>(1, ((int64_t)p.a.vocabulary / Piece<T>::kEach + L * kGradPieces - 1) / (L * kGradPieces));
+  const int64_t blocks = (p.a.rows * chunks + kThreads / L - 1) / (kThreads / L);
+  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  score_grad_kernel<T, L><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(p, chunks);
+  return (int)hipGetLastError();
+}
+// (rows of up to 64 pieces by 16 lanes)
 template <typename T>
 int backward(const ScoreArgs& p, hipStream_t s) {
-  const int chunks = (int)(((int64_t)p.a.vocabulary / Piece<T>::kEach + 64 * kGradPieces) / (64 * kGradPieces));
-  const int64_t blocks = (p.a.rows * chunks + kWaves - 1) / kWaves;
-  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
-  score_grad_kernel<T><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(p, chunks);
-  return (int)hipGetLastError();
+  return p.a.vocabulary / Piece<T>::kEach <= 16 * kGradPieces ? backward<T, 16>(p, s) : backward<T, 64>(p, s);
 }
 
 }  // namespace

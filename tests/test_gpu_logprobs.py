@@ -121,6 +121,36 @@ def test_more_keys_than_a_list_has_room_for(torch, LogProbs, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [300, 500, 1000, 1800, 4000, 10000, 40000])
+@pytest.mark.parametrize("rows", [2, 600])
+def test_large_logits_in_few_lanes(torch, LogProbs, dtype, n, rows):
+    """One lane less than there are tokens on top has all the large logits, of 16, 64 or 256: far more than there is room for reach the border."""
+    each = 128 // torch.finfo(getattr(torch, dtype)).bits
+    piece = torch.arange(n) // each
+    for top in (2, 8, 32):
+        x = torch.rand(rows, n, generator=torch.Generator().manual_seed(top))
+        for row, lanes in enumerate((16, 64, 256)):
+            x[row::3, piece % lanes < top - 1] += 2.0
+        y = x.to(getattr(torch, dtype)).cuda()
+        check(torch, LogProbs(), y, targets_of(torch, 2, rows, n), top, grads=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 15, 16, 17, 511, 512, 513])
+@pytest.mark.parametrize("n", [5, 248, 256, 263, 400, 505, 511, 520, 1030, 2040, 4080, 4090])
+def test_short_rows(torch, LogProbs, dtype, rows, n):
+    """Several rows to a wavefront, or one; numbers of rows that leave places empty; a row does not depend on its neighbours."""
+    x, t = normal(torch, n, dtype, rows, n, by=2.0), targets_of(torch, 2, rows, n)
+    x[rows // 2, n // 2:] = -math.inf
+    r = check(torch, LogProbs(0.9), x, t, 4)
+    y = normal(torch, n + 1, dtype, rows, n)
+    y[rows - 1], y[::3, n // 3], y[::3, 0] = x[rows - 1], -math.inf, x[::3, 0]
+    y[rows - 1] = x[rows - 1]
+    again = LogProbs(0.9).forward(y, t, 4)
+    assert all(torch.equal(a[rows - 1], b[rows - 1]) for a, b in zip(again, r))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [50, 33000])
 def test_masked_and_odd_logits(torch, LogProbs, dtype, n):
     """-infinity and the type's lowest value as masks, of a few tokens, all but a few, and all; infinities and NaN; targets among them."""
