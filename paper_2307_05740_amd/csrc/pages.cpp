@@ -27,7 +27,9 @@ PagesArgs plan(const arrow_pages_t* a) {
   p.a = *a;
   while ((1 << p.page_log) < a->page) ++p.page_log;
   p.rows = a->offsets ? a->rows : (int64_t)a->batch * a->tokens;
-  p.one = a->batch <= kPagesBatch && p.rows <= kPagesRows && (int64_t)a->batch * a->columns <= kPagesEntries;
+  const bool small = a->batch <= kPagesBatch && (int64_t)a->batch * a->columns <= kPagesEntries;
+  p.one = small && p.rows <= kPagesRows;
+  p.two = small && !p.one;
   return p;
 }
 
@@ -37,7 +39,7 @@ size_t each_bytes(const arrow_pages_t* a) { return align_up((size_t)a->batch * 4
 
 extern "C" {
 
-size_t arrow_pages_workspace_bytes(const arrow_pages_t* a) { return check(a) || plan(a).one ? 0 : 3 * each_bytes(a) + 256; }
+size_t arrow_pages_workspace_bytes(const arrow_pages_t* a) { return check(a) || plan(a).one ? 0 : 4 * each_bytes(a) + 256; }
 
 int arrow_pages_step(const arrow_pages_t* a, const int32_t* lengths, int32_t* held, int32_t* table, int32_t* list, int64_t* slots, void* ws, size_t ws_bytes,
                      void* stream) {
@@ -59,7 +61,8 @@ int arrow_pages_step(const arrow_pages_t* a, const int32_t* lengths, int32_t* he
     p.before = (int32_t*)ws;
     p.given = (int32_t*)((char*)ws + each_bytes(a));
     p.taken = (int32_t*)((char*)ws + 2 * each_bytes(a));
-    p.sizes = (int32_t*)((char*)ws + 3 * each_bytes(a));
+    p.first = (int32_t*)((char*)ws + 3 * each_bytes(a));
+    p.sizes = (int32_t*)((char*)ws + 4 * each_bytes(a));
   }
   return launched("pages step", launch_pages_step(p, stream));
 }

@@ -2,8 +2,8 @@
 //
 // What a step has to touch is little: the entries of columns that change, a page of the list for each, and the slots.  What is needed of a row of the table is two
 // runs of columns, the first ones and those of the window, so that what changes are up to three runs, found from the two lengths without looking at the table.
-// Small steps, such as that of a token for each sequence, are one launch of one workgroup, bound by the loads and barriers that follow each other; larger ones
-// four: count, add up, give back, take.
+// Small steps, such as that of a token for each sequence, are one launch of one workgroup, bound by the loads and barriers that follow each other; of more new tokens a
+// second launch takes the pages and writes the slots; steps of large tables count, give back and take in a launch each.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -59,10 +59,12 @@ struct Runs {
 struct Fresh {
   int64_t first;
   int count, position;
-  __device__ __forceinline__ Fresh(const PagesArgs& p, int b, int now) {
+  __device__ __forceinline__ Fresh(const PagesArgs& p, int b, int now) : Fresh(p, b, now, p.a.offsets ? p.a.offsets + b : nullptr) {}
+  // (offsets: this sequence's and the next one's)
+  __device__ __forceinline__ Fresh(const PagesArgs& p, int b, int now, const int* offsets) {
     if (p.a.offsets) {
-      first = max((int64_t)0, min((int64_t)p.a.offsets[b], p.rows));
-      count = (int)(max(first, min((int64_t)p.a.offsets[b + 1], p.rows)) - first);
+      first = max((int64_t)0, min((int64_t)offsets[0], p.rows));
+      count = (int)(max(first, min((int64_t)offsets[1], p.rows)) - first);
     } else {
       first = (int64_t)b * p.a.tokens;
       count = p.a.tokens;
@@ -74,9 +76,8 @@ struct Fresh {
 
 // (lengths of before and now)
 __device__ __forceinline__ Runs given_of(const PagesArgs& p, int before, int now) { return Runs(Needed(p, before), Needed(p, now), 0); }
-__device__ __forceinline__ Runs taken_of(const PagesArgs& p, int b, int before, int now) {
-  return Runs(Needed(p, now), Needed(p, before), Fresh(p, b, now).column(p));
-}
+__device__ __forceinline__ Runs taken_of(const PagesArgs& p, const Fresh& f, int before, int now) { return Runs(Needed(p, now), Needed(p, before), f.column(p)); }
+__device__ __forceinline__ Runs taken_of(const PagesArgs& p, int b, int before, int now) { return taken_of(p, Fresh(p, b, now), before, now); }
 __device__ __forceinline__ int list_size(const PagesArgs& p) { return max(0, min(p.list[0], (int)p.a.pages)); }
 
 // f(column, page or -1) for the columns of runs, 64 at a time, four of those on their way together; a wavefront.
@@ -131,12 +132,11 @@ __device__ __forceinline__ int64_t slot_of(const PagesArgs& p, int position, int
 }
 
 // The slot of row `row`, one of sequence b's: from the list, or from the table where its column is no new one.
-__device__ __forceinline__ int64_t slot_at(const PagesArgs& p, int b, int64_t row, int before, int now, int first, int size) {
-  const Fresh f(p, b, now);
+__device__ __forceinline__ int64_t slot_at(const PagesArgs& p, const Fresh& f, int b, int64_t row, int before, int now, int first, int size) {
   if (row < f.first || row >= f.first + f.count) return -1;
   const int position = f.position + (int)(row - f.first), column = position >> p.page_log;
   if (position < 0 || column >= p.a.columns) return -1;
-  const int at = taken_of(p, b, before, now).place(column);
+  const int at = taken_of(p, f, before, now).place(column);
   return slot_of(p, position, at >= 0 ? page_taken(p, first + at, size) : p.table[(int64_t)b * p.a.columns + column]);
 }
 
@@ -180,12 +180,14 @@ __device__ __forceinline__ int last_upto(const int* numbers, int low, int n, int
 template <int kThreads>
 __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
   constexpr int kAhead = 4, kWaves = kThreads / 64;
-  __shared__ int before[kPagesBatch], now[kPagesBatch], given[kPagesBatch], taken[kPagesBatch];
+  __shared__ int before[kPagesBatch], now[kPagesBatch], given[kPagesBatch], taken[kPagesBatch], offsets[kPagesBatch + 1];
   __shared__ uint64_t room[kWaves];
   const int tid = threadIdx.x, batch = p.a.batch, columns = p.a.columns;
   const int size0 = list_size(p);
   // (one sequence a thread, or several one after the other)
   const int each = (batch + kThreads - 1) / kThreads, b0 = min(batch, tid * each), b1 = min(batch, b0 + each);
+  if (p.a.offsets)
+    for (int b = tid; b <= batch; b += kThreads) offsets[b] = p.a.offsets[b];
   uint64_t mine = 0, all;
   for (int b = b0; b < b1; ++b) {
     const int held = p.held[b], length = p.lengths[b];
@@ -251,6 +253,21 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
     __syncthreads();
   }
   const int size = min(size0 + gives, (int)p.a.pages);
+  if (p.two) {
+    // (what is taken, and the slots, are another kernel's)
+    for (int b = b0; b < b1; ++b) {
+      p.before[b] = before[b];
+      p.taken[b] = taken[b];
+      p.held[b] = now[b];
+    }
+    if (tid == 0) {
+      p.sizes[0] = size0;
+      p.sizes[1] = gives;
+      p.sizes[2] = takes;
+      p.list[0] = max(0, size - takes);
+    }
+    return;
+  }
   for (int i = tid; i < takes; i += kThreads) {
     const int b = last_upto(taken, 0, batch, i);
     p.table[(int64_t)b * columns + taken_of(p, b, before[b], now[b]).column(i - taken[b])] = page_taken(p, i, size);
@@ -258,9 +275,9 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
   // (a slot's page is looked for in the list where it is a new one: nothing here waits for the table)
   for (int row = tid; row < p.rows; row += kThreads) {
     int b;
-    if (p.a.offsets) b = p.a.offsets[0] > row ? -1 : last_upto(p.a.offsets, 0, batch, row);
+    if (p.a.offsets) b = batch == 0 || offsets[0] > row ? -1 : last_upto(offsets, 0, batch, row);
     else b = row / p.a.tokens;
-    p.slots[row] = b < 0 || b >= batch ? -1 : slot_at(p, b, row, before[b], now[b], taken[b], size);
+    p.slots[row] = b < 0 ? -1 : slot_at(p, Fresh(p, b, now[b], offsets + b), b, row, before[b], now[b], taken[b], size);
   }
   for (int b = b0; b < b1; ++b) p.held[b] = now[b];
   if (tid == 0) p.list[0] = max(0, size - takes);
@@ -278,7 +295,8 @@ __global__ __launch_bounds__(256) void pages_count_kernel(PagesArgs p) {
   p.taken[b] = taken_of(p, b, before, now).total();
 }
 
-// What is given back and taken in all, and before each sequence.  Of up to kPagesBatch sequences every workgroup adds them up for itself, into LDS; of more one has done so, in place.
+// What is given back and taken in all, and before each sequence.  Of up to kPagesBatch sequences every workgroup that gives back adds them up for itself, into LDS, and the first one
+// writes them down for what follows; of more one has done so, in place.
 struct Sums {
   const int *given, *taken;
   int size0, gives, takes;
@@ -315,10 +333,6 @@ struct Room {
   int given[kPagesBatch], taken[kPagesBatch];
   uint64_t sums[4];
 };
-__device__ __forceinline__ Sums sums_of(const PagesArgs& p, Room& room) {
-  if (p.a.batch <= kPagesBatch) return add_up<256>(p, room.given, room.taken, room.sums);
-  return {p.given, p.taken, p.sizes[0], p.sizes[1], p.sizes[2]};
-}
 
 // The state after the step, by the last kernel's first workgroups.
 __device__ __forceinline__ void finish(const PagesArgs& p, const Sums& s, int block, int blocks) {
@@ -328,7 +342,12 @@ __device__ __forceinline__ void finish(const PagesArgs& p, const Sums& s, int bl
 
 __global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p, bool last) {
   __shared__ Room room;
-  const Sums s = sums_of(p, room);
+  const bool few = p.a.batch <= kPagesBatch;
+  const Sums s = few ? add_up<256>(p, room.given, room.taken, room.sums) : Sums{p.given, p.taken, p.sizes[0], p.sizes[1], p.sizes[2]};
+  if (few && !last && blockIdx.x == 0) {
+    for (int b = threadIdx.x; b < p.a.batch; b += 256) p.first[b] = s.taken[b];
+    if (threadIdx.x == 0) { p.sizes[1] = s.gives; p.sizes[2] = s.takes; }
+  }
   const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (b < p.a.batch) give(p, b, given_of(p, p.before[b], p.lengths[b]), s.given[b], s.size0, s.gives);
   if (last) finish(p, s, blockIdx.x, gridDim.x);
@@ -338,24 +357,23 @@ __global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p, bool last)
 constexpr int kRowsEach = 8;
 
 __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_blocks) {
-  __shared__ Room room;
   __shared__ int counts[2][4];
   const int tid = threadIdx.x, batch = p.a.batch;
-  // (offsets are on their way while the sums are added up)
+  const int* first = p.a.batch <= kPagesBatch && !p.two ? p.first : p.taken;
   const int64_t row0 = (int64_t)((int)blockIdx.x - take_blocks) * (256 * kRowsEach), last = min(row0 + 256 * kRowsEach, p.rows) - 1;
   int low = 0, high = 0;                     // the sequences that the first and the last row may be of
   if (p.a.offsets)
     for (int b = tid; b < batch; b += 256) {
-      const int first = p.a.offsets[b];
-      low += first <= row0;
-      high += first <= last;
+      const int begin = p.a.offsets[b];
+      low += begin <= row0;
+      high += begin <= last;
     }
-  const Sums s = sums_of(p, room);
+  const Sums s{nullptr, nullptr, p.sizes[0], p.sizes[1], p.sizes[2]};
   const int size = s.size(p);
   if ((int)blockIdx.x < take_blocks) {
     const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (b < batch) take(p, b, taken_of(p, b, p.before[b], p.lengths[b]), s.taken[b], size);
-    finish(p, s, blockIdx.x, take_blocks);
+    if (b < batch) take(p, b, taken_of(p, b, p.before[b], p.lengths[b]), first[b], size);
+    if (!p.two) finish(p, s, blockIdx.x, take_blocks);
     return;
   }
   if (p.a.offsets) {
@@ -372,9 +390,9 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
     // few sequences: one after the other, with what they have in common worked out once
     int64_t done = row0;                     // (rows up to there are written)
     for (int b = max(low, 0); b <= high; ++b) {
-      const int now = p.lengths[b], before = p.before[b], first = s.taken[b];
+      const int now = p.lengths[b], before = p.before[b], taken = first[b];
       const Fresh f(p, b, now);
-      const Runs runs = taken_of(p, b, before, now);
+      const Runs runs = taken_of(p, f, before, now);
       const int64_t begin = max(done, f.first), end = min(last + 1, f.first + f.count);
       for (int64_t row = done + tid; row < min(begin, last + 1); row += 256) p.slots[row] = -1;
       int page[kRowsEach], position[kRowsEach];
@@ -387,7 +405,7 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
         const int column = position[j] >> p.page_log;
         if (position[j] < 0 || column >= p.a.columns) continue;
         const int at = runs.place(column);
-        const int32_t* where = at < 0 ? p.table + (int64_t)b * p.a.columns + column : first + at < size ? p.list + size - first - at : nullptr;
+        const int32_t* where = at < 0 ? p.table + (int64_t)b * p.a.columns + column : taken + at < size ? p.list + size - taken - at : nullptr;
         if (where) page[j] = *where;
       }
 #pragma unroll
@@ -404,7 +422,7 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
     int b;
     if (!p.a.offsets) b = (int)(row / p.a.tokens);
     else b = low < 0 && p.a.offsets[0] > row ? -1 : last_upto(p.a.offsets, max(0, low), high + 1, (int)row);
-    p.slots[row] = b < 0 ? -1 : slot_at(p, b, row, p.before[b], p.lengths[b], s.taken[b], size);
+    p.slots[row] = b < 0 ? -1 : slot_at(p, Fresh(p, b, p.lengths[b]), b, row, p.before[b], p.lengths[b], first[b], size);
   }
 }
 
@@ -419,6 +437,11 @@ int launch_pages_step(const PagesArgs& p, void* stream) {
     return (int)hipGetLastError();
   }
   const unsigned fours = (unsigned)((p.a.batch + 3) / 4), rows = (unsigned)((p.rows + 256 * kRowsEach - 1) / (256 * kRowsEach));
+  if (p.two) {
+    pages_step_kernel<1024><<<dim3(1), dim3(1024), 0, s>>>(p);
+    pages_take_kernel<<<dim3(fours + rows), dim3(256), 0, s>>>(p, (int)fours);
+    return (int)hipGetLastError();
+  }
   if (fours) pages_count_kernel<<<dim3(fours), dim3(256), 0, s>>>(p);
   if (p.a.batch > kPagesBatch) pages_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, s>>>(p);
   if (fours) pages_give_kernel<<<dim3(fours), dim3(256), 0, s>>>(p, rows == 0);
