@@ -735,10 +735,14 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(ScoreArgs p, int c
   }
 }
 
+constexpr int64_t kMostBlocks = 0xffffffff / kThreads;      // (a launch has less than 2^32 threads)
+
 template <typename T, bool kTop>
 int rows(const ScoreArgs& p, hipStream_t s) {
   const int lanes = p.lanes, n = p.vectors / lanes;
-  const dim3 grid((unsigned)((p.a.rows + kThreads / lanes - 1) / (kThreads / lanes))), block(kThreads);
+  const int64_t blocks = (p.a.rows + kThreads / lanes - 1) / (kThreads / lanes);
+  if (blocks > kMostBlocks) return (int)hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks), block(kThreads);
   if (lanes == 16) {
     if (n <= 1) score_rows_kernel<T, 16, 1, kTop><<<grid, block, 0, s>>>(p);
     else if (n <= 2) score_rows_kernel<T, 16, 2, kTop><<<grid, block, 0, s>>>(p);
@@ -755,7 +759,7 @@ template <typename T>
 int forward(const ScoreArgs& p, hipStream_t s) {
   if (p.lanes) return p.a.top ? rows<T, true>(p, s) : rows<T, false>(p, s);
   const int64_t blocks = p.a.rows * p.parts;
-  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  if (blocks > kMostBlocks) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(kThreads);
   const int n = p.vectors / kThreads;
   if (p.a.top == 0) score_sums_kernel<T><<<grid, block, 0, s>>>(p);
@@ -773,7 +777,7 @@ template <typename T, int L>
 int backward(const ScoreArgs& p, hipStream_t s) {
   const int chunks = (int)std::max<int64_t>(1, ((int64_t)p.a.vocabulary / Piece<T>::kEach + L * kGradPieces - 1) / (L * kGradPieces));
   const int64_t blocks = (p.a.rows * chunks + kThreads / L - 1) / (kThreads / L);
-  if (blocks > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  if (blocks > kMostBlocks) return (int)hipErrorInvalidConfiguration;
   score_grad_kernel<T, L><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(p, chunks);
   return (int)hipGetLastError();
 }

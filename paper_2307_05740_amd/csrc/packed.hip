@@ -400,7 +400,7 @@ template <typename T, int D>
 int decode(const PackedArgs& a, hipStream_t s) {
   const arrow_packed_t& c = a.c;
   const int64_t blocks = (int64_t)c.batch * c.kv_heads * a.splits * ((a.group + kHeadTile - 1) / kHeadTile), rows = (int64_t)c.batch * c.q_heads;
-  if (blocks > 0x7fffffff || rows > 0x7fffffff) return (int)hipErrorInvalidConfiguration;
+  if (blocks * 64 * a.waves > 0xffffffff || rows * 256 > 0xffffffff) return (int)hipErrorInvalidConfiguration;   // (a launch has less than 2^32 threads)
   if (a.waves == 4) packed_decode_kernel<T, D, 4><<<dim3((unsigned)blocks), dim3(64 * 4), 0, s>>>(a);
   else packed_decode_kernel<T, D, 8><<<dim3((unsigned)blocks), dim3(64 * 8), 0, s>>>(a);
   if (a.splits > 1) {
@@ -420,7 +420,7 @@ int of_kind(const arrow_packed_t& c, F&& f) {
 
 unsigned blocks_of(const PackedArgs& p) {
   const int64_t n = ((p.tokens + 3) / 4 * 4 * p.c.kv_heads * (p.c.dim / 8) + 255) / 256;
-  return n > 0x7fffffff ? 0 : (unsigned)n;
+  return n * 256 > 0xffffffff ? 0 : (unsigned)n;
 }
 
 struct Append {

@@ -72,7 +72,7 @@ RotationArgs plan(const arrow_rotation_t* a, bool backward) {
   p.tiles = (int32_t)ceil_div(p.length, p.per);
   p.all_tiles = p.sequences * p.tiles;
   if (!backward) {
-    p.blocks = p.all_tiles;
+    p.blocks = std::min(p.all_tiles, 1 << 23);       // (a launch has less than 2^32 threads)
     return p;
   }
   // Queries and keys have workgroups by their heads.

@@ -246,15 +246,21 @@ __global__ __launch_bounds__(kThreads) void rotation_kernel(RotationArgs p) {
   __shared__ __align__(16) float2 angles[kRotationTokens * 128];
   __shared__ __align__(16) float weights[2][256];
   const Lane lane(p.a, threadIdx.x & ((1 << p.lanes_log) - 1));
-  const Tokens of(p, blockIdx.x);
-  Heads<T, false, false, kInterleaved> queries(p, lane, of);
-  Heads<T, false, true, kInterleaved> keys(p, lane, of);
-  find_weights<W>(p, false, weights[0]);
-  find_weights<W>(p, true, weights[1]);
-  find_angles(p, of, angles);
-  __syncthreads();
-  queries.run(angles, weights[0], nullptr);
-  keys.run(angles, weights[1], nullptr);
+  for (uint32_t tile = blockIdx.x; tile < (uint32_t)p.all_tiles; tile += gridDim.x) {
+    const Tokens of(p, tile);
+    Heads<T, false, false, kInterleaved> queries(p, lane, of);
+    Heads<T, false, true, kInterleaved> keys(p, lane, of);
+    if (tile == blockIdx.x) {
+      find_weights<W>(p, false, weights[0]);
+      find_weights<W>(p, true, weights[1]);
+    } else {
+      __syncthreads();                                // (the angles of the tokens before are done with)
+    }
+    find_angles(p, of, angles);
+    __syncthreads();
+    queries.run(angles, weights[0], nullptr);
+    keys.run(angles, weights[1], nullptr);
+  }
 }
 
 // Gradients: a workgroup has queries or keys, so that it holds the sums of one weight's gradient only.
