@@ -68,10 +68,8 @@ def packed(x):
     x = x.double().unflatten(-1, (-1, 32))
     size = x.abs().amax(-1, keepdim=True)
     bad = ~torch.isfinite(size)
-    e = torch.full_like(size, -126.0)
-    for k in range(-126, 126):                                    # the smallest power of two that size is at most seven times of
-        e = torch.where((e == k) & (size > 7.0 * 2.0 ** k), k + 1.0, e)
-    step = torch.exp2(e).clamp(max=most)
+    part, e = torch.frexp(torch.where(bad, 0.0, size))            # size = part 2^e, 1/2 <= part < 1: the smallest power of two that it is at most seven times of
+    step = torch.exp2((e - torch.where(part <= 0.875, 3, 2)).double()).clamp(2.0 ** -126, most)
     y = x.abs() / step
     best, gap = torch.zeros_like(y), torch.full_like(y, math.inf)
     for i in (0, 2, 4, 6, 1, 3, 5, 7):                            # (even codes first: of two at one distance they are taken)
