@@ -9,7 +9,7 @@
 //
 // The calls on sequences (attention, embedding) return their results instead, the error code, or None for the general way.
 #include <Python.h>
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -141,7 +141,8 @@ struct Tensors {
 int half_type(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? ARROW_BF16 : t.scalar_type() == at::kHalf ? ARROW_F16 : -1; }
 bool rows_whole(const at::Tensor& t) { return t.size(-1) <= 1 || t.stride(-1) == 1; }
 bool like(const at::Tensor& t, const at::Tensor& other) { return t.scalar_type() == other.scalar_type() && t.sizes() == other.sizes() && rows_whole(t); }
-at::Tensor made(at::IntArrayRef sizes, const at::Tensor& on, at::ScalarType type) { return at::empty(sizes, on.options().dtype(type)); }
+// (without torch's dispatcher: 0.47 us instead of 0.70, which a call takes up to seven times)
+at::Tensor made(at::IntArrayRef sizes, const at::Tensor& on, at::ScalarType type) { return at::detail::empty_cuda(sizes, type, on.device(), std::nullopt); }
 void* data(const at::Tensor& t) { return t.data_ptr(); }
 
 // Steps between sequences, tokens and heads of (sequences, tokens, heads, dim) or (tokens, heads, dim); one that is never taken counts as none.
@@ -656,6 +657,14 @@ bool describe(arrow_logprobs_t& a, const at::Tensor* logits, const at::Tensor* t
   return a.stride != 0;
 }
 
+// A contiguous tensor in the memory of another one of the same type.
+at::Tensor part_of(const at::Tensor& all, int64_t offset, at::IntArrayRef sizes) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+  t.unsafeGetTensorImpl()->set_storage_offset(offset);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+  return t;
+}
+
 // logprobs_forward(function, of the workspace's size, device, scale, logits, targets, top): logp, entropy, lse, stats and, with top, top_logp, top_ids
 PyObject* logprobs_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   int64_t x[3], top;
@@ -669,8 +678,10 @@ PyObject* logprobs_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) 
     arrow_logprobs_t a{};
     if (!tensor.ok || !describe(a, logits, targets, scale) || top < 0 || top > 32 || top > a.vocabulary) return 0;
     a.top = (int32_t)top;
-    for (int i = 0; i < 3; ++i) out[i] = made(targets->sizes(), *logits, at::kFloat);
-    out[3] = made(with(targets->sizes(), 2), *logits, at::kFloat);
+    // (a few numbers of each row, in one piece of memory)
+    const at::Tensor all = made({std::max<int64_t>(1, 5 * a.rows)}, *logits, at::kFloat);
+    out[3] = part_of(all, 0, with(targets->sizes(), 2));
+    for (int i = 0; i < 3; ++i) out[i] = part_of(all, (2 + i) * a.rows, targets->sizes());
     if (top) {
       out[4] = made(with(targets->sizes(), top), *logits, at::kFloat);
       out[5] = made(with(targets->sizes(), top), *logits, at::kLong);
