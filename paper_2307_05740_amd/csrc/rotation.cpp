@@ -1,6 +1,7 @@
 // C boundary of the rotation entries (include/arrow_rotation.h): checks of the arguments, the plan of a call.
 #include <algorithm>
 #include <cmath>
+#include <numeric>
 
 #include "checks.h"
 #include "rotation_internal.h"
@@ -52,6 +53,27 @@ int check_weights(const arrow_rotation_t* a, const char* name, const void* q, co
 
 bool follow(const arrow_rotation_t* a, const arrow_strides_t& s) { return a->batch <= 1 || s.sequence == a->tokens * s.token; }
 
+// Tokens of a workgroup at a time, which share its angles: up to eight rounds of its groups of lanes, as even a share of all as that leaves, but enough for one round, and where a
+// round is of whole tokens, a multiple of them.  At most 4096 angles, 32 KiB; us for 1.3e8 elements (gradients: 0.67e8, with the forward call):
+//   up to 8 tokens, and 1024 angles: heads 32/8 of 128 110 (148), 8/2 of 64 128 (268), 4/1 of 128 140 (297), 2/1 of 256 147 (257)
+//   2048 angles: 109 (142), 107 (163), 115 (191), 132 (211);  4096: 107 (142), 107 (163), 115 (183), 128 (199)
+//   4 rounds instead of 8: 107 (141), 114 (163), 123 (184), 131 (198);  16, with 2048 angles: 117 (145), 110 (166), 114 (191), 130 (211)
+RotationTiles tiles_of(const RotationArgs& p, int64_t heads, int64_t blocks) {
+  const int64_t groups = kRotationThreads >> p.lanes_log, tokens = (int64_t)p.sequences * p.length, angles = p.a.rotary / 2;
+  const int64_t fit = std::min<int64_t>(kRotationTokens, angles ? kRotationAngles / angles : kRotationTokens);
+  const int64_t some = std::max<int64_t>(1, std::min(fit, groups / heads)), unit = groups / std::gcd(groups, heads);
+  int64_t most = std::min(fit, std::max(some, 8 * groups / heads));
+  if (unit <= most) most = most / unit * unit;
+  const int64_t rounds = std::max<int64_t>(1, ceil_div(tokens, most * blocks));
+  int64_t per = std::min(most, std::max(some, ceil_div(tokens, rounds * blocks)));
+  if (unit <= per) per = ceil_div(per, unit) * unit;
+  RotationTiles t;
+  t.per = (int32_t)per;
+  t.tiles = (int32_t)ceil_div(p.length, per);
+  t.all = p.sequences * t.tiles;
+  return t;
+}
+
 RotationArgs plan(const arrow_rotation_t* a, bool backward) {
   RotationArgs p{};
   p.a = *a;
@@ -66,19 +88,17 @@ RotationArgs plan(const arrow_rotation_t* a, bool backward) {
     p.length = a->batch * a->tokens;
   }
   while ((16 << p.lanes_log) < a->dim) ++p.lanes_log;
-  // A workgroup's tokens share its angles.  Few tokens: as many as have a head for each of its groups of lanes.
-  const int64_t heads = a->q_heads + a->kv_heads, groups = kRotationThreads >> p.lanes_log;
-  p.per = (int32_t)std::max<int64_t>({1, std::min<int64_t>(kRotationTokens, groups / heads), std::min<int64_t>(kRotationTokens, (int64_t)p.sequences * p.length / 1024)});
-  p.tiles = (int32_t)ceil_div(p.length, p.per);
-  p.all_tiles = p.sequences * p.tiles;
   if (!backward) {
-    p.blocks = std::min(p.all_tiles, 1 << 23);       // (a launch has less than 2^32 threads)
+    p.tiles[0] = tiles_of(p, a->q_heads + a->kv_heads, 1024);
+    p.blocks = std::min(p.tiles[0].all, 1 << 23);    // (a launch has less than 2^32 threads)
     return p;
   }
   // Queries and keys have workgroups by their heads.
-  const int32_t q = (int32_t)std::max<int64_t>(1, kRotationBlocks * (int64_t)a->q_heads / (a->q_heads + a->kv_heads));
-  p.q_blocks = std::min(p.all_tiles, std::min(q, kRotationBlocks - 1));
-  p.blocks = p.q_blocks + std::min(p.all_tiles, std::max(1, kRotationBlocks - q));
+  const int32_t q = std::min(kRotationBlocks - 1, std::max(1, (int32_t)(kRotationBlocks * (int64_t)a->q_heads / (a->q_heads + a->kv_heads))));
+  p.tiles[0] = tiles_of(p, a->q_heads, q);
+  p.tiles[1] = tiles_of(p, a->kv_heads, kRotationBlocks - q);
+  p.q_blocks = std::min(p.tiles[0].all, q);
+  p.blocks = p.q_blocks + std::min(p.tiles[1].all, kRotationBlocks - q);
   return p;
 }
 

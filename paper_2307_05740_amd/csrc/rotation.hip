@@ -124,10 +124,10 @@ struct Lane {
 struct Tokens {
   uint32_t b, at;           // the sequence, and the first of them in it
   int count;
-  __device__ __forceinline__ Tokens(const RotationArgs& p, uint32_t tile) {
-    b = tile / (uint32_t)p.tiles;
-    at = (tile - b * p.tiles) * p.per;
-    count = min(p.per, p.length - (int)at);
+  __device__ __forceinline__ Tokens(const RotationArgs& p, const RotationTiles& tiles, uint32_t tile) {
+    b = tile / (uint32_t)tiles.tiles;
+    at = (tile - b * tiles.tiles) * tiles.per;
+    count = min(tiles.per, p.length - (int)at);
   }
 };
 
@@ -243,11 +243,11 @@ __device__ __forceinline__ void find_weights(const RotationArgs& p, bool keys, f
 
 template <typename T, typename W, bool kInterleaved>
 __global__ __launch_bounds__(kThreads) void rotation_kernel(RotationArgs p) {
-  __shared__ __align__(16) float2 angles[kRotationTokens * 128];
+  __shared__ __align__(16) float2 angles[kRotationAngles];
   __shared__ __align__(16) float weights[2][256];
   const Lane lane(p.a, threadIdx.x & ((1 << p.lanes_log) - 1));
-  for (uint32_t tile = blockIdx.x; tile < (uint32_t)p.all_tiles; tile += gridDim.x) {
-    const Tokens of(p, tile);
+  for (uint32_t tile = blockIdx.x; tile < (uint32_t)p.tiles[0].all; tile += gridDim.x) {
+    const Tokens of(p, p.tiles[0], tile);
     Heads<T, false, false, kInterleaved> queries(p, lane, of);
     Heads<T, false, true, kInterleaved> keys(p, lane, of);
     if (tile == blockIdx.x) {
@@ -270,8 +270,8 @@ __device__ __forceinline__ void rotate_back(const RotationArgs& p, uint32_t bloc
   const Lane lane(p.a, threadIdx.x & (lanes - 1));
   find_weights<W>(p, kKeys, weights);
   Eight sum[2] = {zeros(), zeros()};
-  for (uint32_t tile = block; tile < (uint32_t)p.all_tiles; tile += blocks) {
-    const Tokens of(p, tile);
+  for (uint32_t tile = block; tile < (uint32_t)p.tiles[kKeys].all; tile += blocks) {
+    const Tokens of(p, p.tiles[kKeys], tile);
     Heads<T, true, kKeys, kInterleaved> heads(p, lane, of);
     __syncthreads();                                  // (the angles of the tokens before are done with)
     find_angles(p, of, angles);
@@ -280,6 +280,7 @@ __device__ __forceinline__ void rotate_back(const RotationArgs& p, uint32_t bloc
   }
   if (!p.dwq) return;
   // the groups' sums of an element, one after the other
+  __syncthreads();
   float* mine = sums + (threadIdx.x >> p.lanes_log) * lanes * 16;
   if (lane.has_first) store8(mine + lane.first, sum[0]);
   if (lane.has_second) store8(mine + lane.second, sum[1]);
@@ -293,9 +294,10 @@ __device__ __forceinline__ void rotate_back(const RotationArgs& p, uint32_t bloc
 
 template <typename T, typename W, bool kInterleaved>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) void rotation_grad_kernel(RotationArgs p) {
-  __shared__ __align__(16) float2 angles[kRotationTokens * 128];
+  static_assert(sizeof(float2) * kRotationAngles >= sizeof(float) * kThreads * 16, "the sums have the angles' place");
+  __shared__ __align__(16) float2 angles[kRotationAngles];
   __shared__ __align__(16) float weights[256];
-  __shared__ __align__(16) float sums[kThreads * 16];
+  float* sums = (float*)angles;
   const uint32_t block = blockIdx.x, q_blocks = p.q_blocks;
   if (block < q_blocks) rotate_back<T, W, false, kInterleaved>(p, block, q_blocks, angles, weights, sums);
   else rotate_back<T, W, true, kInterleaved>(p, block - q_blocks, gridDim.x - q_blocks, angles, weights, sums);

@@ -9,8 +9,14 @@
 namespace arrow {
 
 constexpr int kRotationThreads = 256;
-constexpr int kRotationTokens = 8;        // of a workgroup at a time, at most
+constexpr int kRotationAngles = 4096;     // of a workgroup at a time, at most: tokens x rotary / 2
+constexpr int kRotationTokens = 64;       // and tokens
 constexpr int kRotationBlocks = 1024;     // workgroups of a gradient, at most: four to a compute unit; each leaves a sum of a weight's gradient
+
+// Tokens that a workgroup has at a time, such tiles of a sequence, and of all.
+struct RotationTiles {
+  int32_t per, tiles, all;
+};
 
 struct RotationArgs {
   arrow_rotation_t a;
@@ -21,7 +27,7 @@ struct RotationArgs {
   void *dwq, *dwk;
   float* parts;                           // blocks x dim sums of the weights' gradients
   int32_t sequences, length;              // and tokens of each: one of all where sequences follow each other
-  int32_t per, tiles, all_tiles;          // tokens of a workgroup at a time; such tiles of a sequence, and of all
+  RotationTiles tiles[2];                 // forward: [0]; of a gradient, those of queries and of keys
   int32_t blocks, q_blocks;               // workgroups; of a gradient, those that have queries: the first ones
   int32_t lanes_log;                      // lanes of a head: a power of two, each has 16 elements
 };

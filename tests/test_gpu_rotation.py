@@ -86,6 +86,18 @@ def test_numbers_of_tokens(torch, Rotation, tokens, heads, kv):
     check(torch, op, q, k, wq, wk, gq=gq, gk=gk)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("heads,kv,dim,rotary", [(1, 1, 256, 256), (2, 1, 128, 128), (3, 1, 96, 96), (6, 3, 80, 32), (16, 1, 8, 0), (70, 2, 32, 32)])
+@pytest.mark.parametrize("batch,tokens", [(3, 1031), (40, 97), (2, 4000)])
+def test_tokens_of_workgroups(torch, Rotation, interleaved, heads, kv, dim, rotary, batch, tokens):
+    """Many tokens of a few heads and few ones of many, in sequences that follow each other or lie apart, so that they end inside what a workgroup has at a time."""
+    op = Rotation(dim, rotary=rotary, interleaved=interleaved)
+    for room in (0, 1):
+        (q, gq), (k, gk) = ([normal(torch, s, "bfloat16", batch, tokens + room, h, dim)[:, :tokens] for s in seeds] for h, seeds in ((heads, (1, 2)), (kv, (3, 4))))
+        wq, wk = (1 + 0.3 * normal(torch, s, "float32", dim) for s in (5, 6))
+        check(torch, op, q, k, wq, wk, gq=gq, gk=gk)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("kind", ["int32", "int64"])
 def test_positions(torch, Rotation, dtype, kind):
