@@ -361,12 +361,12 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
   const int tid = threadIdx.x, batch = p.a.batch;
   const int* first = p.a.batch <= kPagesBatch && !p.two ? p.first : p.taken;
   const int64_t row0 = (int64_t)((int)blockIdx.x - take_blocks) * (256 * kRowsEach), last = min(row0 + 256 * kRowsEach, p.rows) - 1;
-  int low = 0, high = 0;                     // the sequences that the first and the last row may be of
+  int low = 0, high = 0;                     // the sequences that the first and the last row may be of: those of this wavefront's that begin up to there
   if (p.a.offsets)
-    for (int b = tid; b < batch; b += 256) {
-      const int begin = p.a.offsets[b];
-      low += begin <= row0;
-      high += begin <= last;
+    for (int b0 = 0; b0 < batch; b0 += 256) {
+      const int begin = b0 + tid < batch ? p.a.offsets[b0 + tid] : 0x7fffffff;
+      low += __popcll(__ballot(begin <= row0));
+      high += __popcll(__ballot(begin <= last));
     }
   const Sums s{nullptr, nullptr, p.sizes[0], p.sizes[1], p.sizes[2]};
   const int size = s.size(p);
@@ -377,7 +377,6 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
     return;
   }
   if (p.a.offsets) {
-    for (int m = 32; m; m >>= 1) { low += __shfl_xor(low, m, 64); high += __shfl_xor(high, m, 64); }
     if ((tid & 63) == 0) { counts[0][tid >> 6] = low; counts[1][tid >> 6] = high; }
     __syncthreads();
     low = __builtin_amdgcn_readfirstlane(counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3]) - 1;
