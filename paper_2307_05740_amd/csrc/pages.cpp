@@ -27,13 +27,15 @@ PagesArgs plan(const arrow_pages_t* a) {
   p.a = *a;
   while ((1 << p.page_log) < a->page) ++p.page_log;
   p.rows = a->offsets ? a->rows : (int64_t)a->batch * a->tokens;
-  const bool small = a->batch <= kPagesBatch && (int64_t)a->batch * a->columns <= kPagesEntries;
-  p.one = small && p.rows <= kPagesRows;
-  p.two = small && !p.one;
+  const int64_t entries = (int64_t)a->batch * a->columns;
+  p.one = a->batch <= kPagesBatch && p.rows <= kPagesRows && entries <= (p.rows ? kPagesEntries : kPagesBack);
+  p.two = !p.one && a->batch <= kPagesBatch && entries <= kPagesFew;
+  p.chunk = p.two ? std::max(1, a->columns) : 1024;
+  p.chunks = (int32_t)std::max<int64_t>(1, ceil_div(a->columns, p.chunk));
   return p;
 }
 
-size_t each_bytes(const arrow_pages_t* a) { return align_up((size_t)a->batch * 4); }
+size_t each_bytes(const arrow_pages_t* a) { return align_up((size_t)a->batch * plan(a).chunks * 4); }
 
 }  // namespace
 

@@ -80,12 +80,20 @@ __device__ __forceinline__ Runs taken_of(const PagesArgs& p, const Fresh& f, int
 __device__ __forceinline__ Runs taken_of(const PagesArgs& p, int b, int before, int now) { return taken_of(p, Fresh(p, b, now), before, now); }
 __device__ __forceinline__ int list_size(const PagesArgs& p) { return max(0, min(p.list[0], (int)p.a.pages)); }
 
-// f(column, page or -1) for the columns of runs, 64 at a time, four of those on their way together; a wavefront.
+// Columns first .. end - 1 of those that change.
+struct Part {
+  int first, end;
+  __device__ __forceinline__ Part(const Runs& r) : first(0), end(r.total()) {}
+  __device__ __forceinline__ Part(const PagesArgs& p, const Runs& r, int chunk) : first(chunk * p.chunk), end(min(r.total(), first + p.chunk)) {}
+  __device__ __forceinline__ int count() const { return max(0, end - first); }
+};
+
+// f(column, page or -1) for some columns of runs, 64 at a time, four of those on their way together; a wavefront.
 template <typename F>
-__device__ __forceinline__ void each_entry(const PagesArgs& p, int b, const Runs& r, F&& f) {
-  const int lane = threadIdx.x & 63, n = r.total();
+__device__ __forceinline__ void each_entry(const PagesArgs& p, int b, const Runs& r, const Part& part, F&& f) {
+  const int lane = threadIdx.x & 63, n = part.end;
   const int32_t* row = p.table + (int64_t)b * p.a.columns;
-  for (int i0 = 0; i0 < n; i0 += 256) {
+  for (int i0 = part.first; i0 < n; i0 += 256) {
     int page[4], column[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -100,16 +108,16 @@ __device__ __forceinline__ void each_entry(const PagesArgs& p, int b, const Runs
   }
 }
 
-__device__ __forceinline__ int count_given(const PagesArgs& p, int b, const Runs& r) {
+__device__ __forceinline__ int count_given(const PagesArgs& p, int b, const Runs& r, const Part& part) {
   int n = 0;
-  each_entry(p, b, r, [&](int, int page) { n += __popcll(__ballot(page >= 0)); });
+  each_entry(p, b, r, part, [&](int, int page) { n += __popcll(__ballot(page >= 0)); });
   return n;
 }
 
-// The pages of a sequence to the list: `first` have gone there before it, the last of all to place `size`.
-__device__ __forceinline__ void give(const PagesArgs& p, int b, const Runs& r, int first, int size, int all) {
+// Pages of a sequence to the list: `first` have gone there before them, the last of all to place `size`.
+__device__ __forceinline__ void give(const PagesArgs& p, int b, const Runs& r, const Part& part, int first, int size, int all) {
   const uint64_t below = ((uint64_t)1 << (threadIdx.x & 63)) - 1;
-  each_entry(p, b, r, [&](int column, int page) {
+  each_entry(p, b, r, part, [&](int column, int page) {
     const uint64_t there = __ballot(page >= 0);
     const int at = size + all - 1 - first - __popcll(there & below);
     first += __popcll(there);
@@ -121,9 +129,8 @@ __device__ __forceinline__ void give(const PagesArgs& p, int b, const Runs& r, i
 // The i-th page that is taken from a list of `size`.
 __device__ __forceinline__ int page_taken(const PagesArgs& p, int i, int size) { return i < size ? p.list[size - i] : -1; }
 
-__device__ __forceinline__ void take(const PagesArgs& p, int b, const Runs& r, int first, int size) {
-  const int n = r.total();
-  for (int i = threadIdx.x & 63; i < n; i += 64) p.table[(int64_t)b * p.a.columns + r.column(i)] = page_taken(p, first + i, size);
+__device__ __forceinline__ void take(const PagesArgs& p, int b, const Runs& r, const Part& part, int first, int size) {
+  for (int i = part.first + (threadIdx.x & 63); i < part.end; i += 64) p.table[(int64_t)b * p.a.columns + r.column(i)] = page_taken(p, first + i - part.first, size);
 }
 
 // A slot from its position and its column's page.
@@ -207,9 +214,40 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
   __syncthreads();
   int gives = (int)(all >> 32);
   const int takes = (int)all, columns_given = gives;
+  // f(i, its sequence, its column) for the i-th columns that give their pages back, i0 + 64 j; most often they are all of one sequence
+  const auto some_given = [&](int i0, auto&& f) {
+    const int low = last_upto(given, 0, batch, i0), high = last_upto(given, low, batch, min(i0 + 64 * kAhead, columns_given) - 1), lane = tid & 63;
+    if (low == high) {
+      const int b = __builtin_amdgcn_readfirstlane(low);
+      const Runs r = given_of(p, before[b], now[b]);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) f(j, i0 + 64 * j + lane, b, r.column(i0 + 64 * j + lane - given[b]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = min(i0 + 64 * j + lane, columns_given - 1), b = last_upto(given, low, high + 1, i);
+        f(j, i0 + 64 * j + lane, b, given_of(p, before[b], now[b]).column(i - given[b]));
+      }
+    }
+  };
+  const int wave0 = __builtin_amdgcn_readfirstlane(tid >> 6) * (64 * kAhead);
+  const bool many = columns_given > kAhead * kThreads;
   if (gives) {
     bool hole = false;
-    for (int i0 = tid; i0 < columns_given; i0 += kAhead * kThreads) {
+    if (many) {
+      for (int i0 = wave0; i0 < columns_given; i0 += kAhead * kThreads) {
+        int page[kAhead];
+        some_given(i0, [&](int j, int i, int b, int column) { page[j] = i < columns_given ? p.table[(int64_t)b * columns + column] : 0; });
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int i = i0 + 64 * j + (tid & 63), at = size0 + gives - 1 - i;
+          if (i >= columns_given) continue;
+          hole = hole || page[j] < 0 || page[j] >= p.a.pages;
+          if (at < p.a.pages) p.list[1 + at] = page[j];
+        }
+      }
+    }
+    for (int i0 = many ? columns_given : tid; i0 < columns_given; i0 += kAhead * kThreads) {
       int page[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -229,7 +267,8 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
     if (__syncthreads_or(hole)) {
       const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
       for (int b = wave; b < batch; b += kWaves) {
-        const int n = count_given(p, b, given_of(p, before[b], now[b]));
+        const Runs r = given_of(p, before[b], now[b]);
+        const int n = count_given(p, b, r, r);
         if ((tid & 63) == 0) given[b] = n;
       }
       __syncthreads();
@@ -243,9 +282,15 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
       }
       gives = (int)all;
       __syncthreads();
-      for (int b = wave; b < batch; b += kWaves) give(p, b, given_of(p, before[b], now[b]), given[b], size0, gives);
+      for (int b = wave; b < batch; b += kWaves) {
+        const Runs r = given_of(p, before[b], now[b]);
+        give(p, b, r, r, given[b], size0, gives);
+      }
     } else {
-      for (int i = tid; i < columns_given; i += kThreads) {
+      if (many)
+        for (int i0 = wave0; i0 < columns_given; i0 += kAhead * kThreads)
+          some_given(i0, [&](int, int i, int b, int column) { if (i < columns_given) p.table[(int64_t)b * columns + column] = -1; });
+      for (int i = many ? columns_given : tid; i < columns_given; i += kThreads) {
         const int b = last_upto(given, 0, batch, i);
         p.table[(int64_t)b * columns + given_of(p, before[b], now[b]).column(i - given[b])] = -1;
       }
@@ -284,18 +329,32 @@ __global__ __launch_bounds__(kThreads) void pages_step_kernel(PagesArgs p) {
 }
 
 // ---- larger steps ----
+// A unit of the work is up to p.chunk of the columns that change of a sequence, for a wavefront.
+struct Unit {
+  int at, b, chunk;
+  bool in;
+  __device__ __forceinline__ explicit Unit(const PagesArgs& p) {
+    at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    b = p.chunks == 1 ? at : (uint32_t)at / (uint32_t)p.chunks;
+    chunk = at - b * p.chunks;
+    in = b < p.a.batch;
+  }
+};
+
 __global__ __launch_bounds__(256) void pages_count_kernel(PagesArgs p) {
   if (blockIdx.x == 0 && threadIdx.x == 0) p.sizes[0] = list_size(p);
-  const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  if (b >= p.a.batch) return;
-  const int before = p.held[b], now = p.lengths[b], n = count_given(p, b, given_of(p, before, now));
+  const Unit u(p);
+  if (!u.in) return;
+  const int before = p.held[u.b], now = p.lengths[u.b];
+  const Runs given = given_of(p, before, now);
+  const int n = count_given(p, u.b, given, Part(p, given, u.chunk));
   if (threadIdx.x & 63) return;
-  p.before[b] = before;
-  p.given[b] = n;
-  p.taken[b] = taken_of(p, b, before, now).total();
+  if (u.chunk == 0) p.before[u.b] = before;
+  p.given[u.at] = n;
+  p.taken[u.at] = Part(p, taken_of(p, u.b, before, now), u.chunk).count();
 }
 
-// What is given back and taken in all, and before each sequence.  Of up to kPagesBatch sequences every workgroup that gives back adds them up for itself, into LDS, and the first one
+// What is given back and taken in all, and before each unit.  Of up to kPagesBatch units every workgroup that gives back adds them up for itself, into LDS, and the first one
 // writes them down for what follows; of more one has done so, in place.
 struct Sums {
   const int *given, *taken;
@@ -305,7 +364,7 @@ struct Sums {
 
 template <int kThreads>
 __device__ __forceinline__ Sums add_up(const PagesArgs& p, int* given, int* taken, uint64_t* room) {
-  const int batch = p.a.batch, each = (batch + kThreads - 1) / kThreads, b0 = min(batch, (int)threadIdx.x * each), b1 = min(batch, b0 + each);
+  const int units = p.a.batch * p.chunks, each = (units + kThreads - 1) / kThreads, b0 = min(units, (int)threadIdx.x * each), b1 = min(units, b0 + each);
   uint64_t mine = 0, all;
   for (int b = b0; b < b1; ++b) mine += (uint64_t)p.given[b] << 32 | (uint32_t)p.taken[b];
   uint64_t first = before_me<kThreads>(mine, &all, room);
@@ -342,14 +401,18 @@ __device__ __forceinline__ void finish(const PagesArgs& p, const Sums& s, int bl
 
 __global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p, bool last) {
   __shared__ Room room;
-  const bool few = p.a.batch <= kPagesBatch;
+  const int units = p.a.batch * p.chunks;
+  const bool few = units <= kPagesBatch;
   const Sums s = few ? add_up<256>(p, room.given, room.taken, room.sums) : Sums{p.given, p.taken, p.sizes[0], p.sizes[1], p.sizes[2]};
   if (few && !last && blockIdx.x == 0) {
-    for (int b = threadIdx.x; b < p.a.batch; b += 256) p.first[b] = s.taken[b];
+    for (int i = threadIdx.x; i < units; i += 256) p.first[i] = s.taken[i];
     if (threadIdx.x == 0) { p.sizes[1] = s.gives; p.sizes[2] = s.takes; }
   }
-  const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  if (b < p.a.batch) give(p, b, given_of(p, p.before[b], p.lengths[b]), s.given[b], s.size0, s.gives);
+  const Unit u(p);
+  if (u.in) {
+    const Runs r = given_of(p, p.before[u.b], p.lengths[u.b]);
+    give(p, u.b, r, Part(p, r, u.chunk), s.given[u.at], s.size0, s.gives);
+  }
   if (last) finish(p, s, blockIdx.x, gridDim.x);
 }
 
@@ -359,7 +422,7 @@ constexpr int kRowsEach = 8;
 __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_blocks) {
   __shared__ int counts[2][4];
   const int tid = threadIdx.x, batch = p.a.batch;
-  const int* first = p.a.batch <= kPagesBatch && !p.two ? p.first : p.taken;
+  const int* first = p.a.batch * p.chunks <= kPagesBatch && !p.two ? p.first : p.taken;
   const int64_t row0 = (int64_t)((int)blockIdx.x - take_blocks) * (256 * kRowsEach), last = min(row0 + 256 * kRowsEach, p.rows) - 1;
   int low = 0, high = 0;                     // the sequences that the first and the last row may be of: those of this wavefront's that begin up to there
   if (p.a.offsets)
@@ -371,8 +434,11 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
   const Sums s{nullptr, nullptr, p.sizes[0], p.sizes[1], p.sizes[2]};
   const int size = s.size(p);
   if ((int)blockIdx.x < take_blocks) {
-    const int b = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (b < batch) take(p, b, taken_of(p, b, p.before[b], p.lengths[b]), first[b], size);
+    const Unit u(p);
+    if (u.in) {
+      const Runs r = taken_of(p, u.b, p.before[u.b], p.lengths[u.b]);
+      take(p, u.b, r, Part(p, r, u.chunk), first[u.at], size);
+    }
     if (!p.two) finish(p, s, blockIdx.x, take_blocks);
     return;
   }
@@ -389,7 +455,7 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
     // few sequences: one after the other, with what they have in common worked out once
     int64_t done = row0;                     // (rows up to there are written)
     for (int b = max(low, 0); b <= high; ++b) {
-      const int now = p.lengths[b], before = p.before[b], taken = first[b];
+      const int now = p.lengths[b], before = p.before[b], taken = first[b * p.chunks];
       const Fresh f(p, b, now);
       const Runs runs = taken_of(p, f, before, now);
       const int64_t begin = max(done, f.first), end = min(last + 1, f.first + f.count);
@@ -421,7 +487,7 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
     int b;
     if (!p.a.offsets) b = (int)(row / p.a.tokens);
     else b = low < 0 && p.a.offsets[0] > row ? -1 : last_upto(p.a.offsets, max(0, low), high + 1, (int)row);
-    p.slots[row] = b < 0 ? -1 : slot_at(p, Fresh(p, b, p.lengths[b]), b, row, p.before[b], p.lengths[b], first[b], size);
+    p.slots[row] = b < 0 ? -1 : slot_at(p, Fresh(p, b, p.lengths[b]), b, row, p.before[b], p.lengths[b], first[b * p.chunks], size);
   }
 }
 
@@ -430,19 +496,20 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
 int launch_pages_step(const PagesArgs& p, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (p.one) {
-    // (fewer threads wait less for each other)
-    if (p.a.batch <= 256 && p.rows <= 2048) pages_step_kernel<256><<<dim3(1), dim3(256), 0, s>>>(p);
+    // Fewer threads wait less for each other: four new tokens and back, us a pass with 256 and 1024 threads, 4 sequences 8.2, 8.5, 32 8.1, 9.0, 256 10.7, 9.7.  Where all of 16,384
+    // pages go at once they take longer: 17 and 23 us more for 4 and 32.
+    if (p.a.batch <= 128 && p.rows <= 2048 && (int64_t)p.a.batch * p.a.columns <= 16384) pages_step_kernel<256><<<dim3(1), dim3(256), 0, s>>>(p);
     else pages_step_kernel<1024><<<dim3(1), dim3(1024), 0, s>>>(p);
     return (int)hipGetLastError();
   }
-  const unsigned fours = (unsigned)((p.a.batch + 3) / 4), rows = (unsigned)((p.rows + 256 * kRowsEach - 1) / (256 * kRowsEach));
+  const unsigned fours = (unsigned)(((int64_t)p.a.batch * p.chunks + 3) / 4), rows = (unsigned)((p.rows + 256 * kRowsEach - 1) / (256 * kRowsEach));
   if (p.two) {
     pages_step_kernel<1024><<<dim3(1), dim3(1024), 0, s>>>(p);
     pages_take_kernel<<<dim3(fours + rows), dim3(256), 0, s>>>(p, (int)fours);
     return (int)hipGetLastError();
   }
   if (fours) pages_count_kernel<<<dim3(fours), dim3(256), 0, s>>>(p);
-  if (p.a.batch > kPagesBatch) pages_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, s>>>(p);
+  if ((int64_t)p.a.batch * p.chunks > kPagesBatch) pages_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, s>>>(p);
   if (fours) pages_give_kernel<<<dim3(fours), dim3(256), 0, s>>>(p, rows == 0);
   // (without new tokens nothing is taken)
   if (rows) pages_take_kernel<<<dim3(fours + rows), dim3(256), 0, s>>>(p, (int)fours);

@@ -113,6 +113,23 @@ def test_steps_of_one_launch_and_of_several(torch, Pages, batch, most, window, s
     assert free[0] == both.op.pages and sorted(free[1:]) == list(range(both.op.pages))
 
 
+@pytest.mark.parametrize("batch,columns", [(1, 2048), (1, 5000), (3, 5461), (7, 2341), (130, 100), (1, 30000), (40, 2100), (600, 1100)])
+@pytest.mark.parametrize("short", [False, True])
+def test_long_rows_come_and_go(torch, Pages, batch, columns, short):
+    """Rows of more columns than one wavefront goes through, and pages of many rows that one workgroup gives back, with a pool for all and one that leaves holes."""
+    rng = random.Random(batch)
+    page, room = 2, 2 * columns
+    lengths = [rng.randint(room // 2, room) for _ in range(batch)]
+    if batch == 3:
+        lengths = [2 * 1024, 2 * 1024 + 1, 2 * 4096]              # (at and beyond the ends of what a wavefront has)
+    pages = sum(-(-n // page) for n in lengths)
+    both = Both(torch, Pages, pages * 3 // 4 if short else pages, page, 0, 0, batch, columns)
+    both.ragged(lengths, lengths, 1, 1)
+    both.step([n // 3 if rng.random() < 0.5 else n for n in lengths], 0)
+    both.step([min(room, n + 1) for n in lengths], 1)
+    both.step([0] * batch, 0)
+
+
 def test_there_and_back(torch, Pages):
     """The list is as it was, in order too."""
     both = Both(torch, Pages, 500, 16, 0, 0, 8, 100)
