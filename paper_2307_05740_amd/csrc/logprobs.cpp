@@ -8,20 +8,24 @@
 namespace arrow {
 
 void plan_score(ScoreArgs& p) {
-  // Pieces of 16 bytes that a row reaches into, at any address.  With most likely tokens a workgroup holds a part of a row in its registers; where there are few rows,
-  // they are cut further, down to a piece per lane.
+  // Pieces of 16 bytes that a row reaches into, at any address.
   const int64_t each = 16 / size_of(p.a.dtype), pieces = ceil_div((int64_t)p.a.vocabulary, each) + 1;
-  const int64_t least = p.a.top ? ceil_div(pieces, kScoreThreads * kMostVectors) : ceil_div(pieces, kMostPieces), most = ceil_div(pieces, kScoreThreads);
-  // Rows of few pieces have 16 lanes or a wavefront each, where there are enough of them for longer ones.  (Tokens on top are looked for among those that lanes have as their
-  // largest: there have to be some more lanes than tokens.)
+  // Rows of few pieces have 16 lanes or a wavefront each.  (Tokens on top are looked for among those that lanes have as their largest: there have to be some more lanes than
+  // tokens.)  A wavefront and a workgroup, us, bfloat16: rows of 5675 with the 20 best, 2048 of them 12.2 24.3, 20,000 57.8 140; of 8100 with 5, one 7.7 11.8 (in two launches), 9668 35.2 58.0;
+  // without any, of 5675, 4096 12.0 12.0, 20,000 41.4 52.6, of 8100, 2048 10.5 9.0, 20,000 59.0 60.0.
   p.parts = 1;
-  p.lanes = pieces <= 16 * 4 && p.a.top <= 8 ? 16 : pieces <= 64 * 4 || (pieces <= 64 * 8 && p.a.rows >= 512) ? 64 : 0;
+  p.lanes = pieces <= 16 * 4 && p.a.top <= 8 ? 16 : pieces <= 64 * (p.a.top ? 16 : p.a.rows >= 4096 ? 12 : 8) ? 64 : 0;
   if (p.lanes) {
     p.vectors = (int32_t)(ceil_div(pieces, p.lanes) * p.lanes);
     return;
   }
+  // With most likely tokens a workgroup holds its pieces in registers.  Longer rows are cut, and where there are few of them, so are rows that would take longer than the second
+  // launch that joins parts.  One part and several, us, bfloat16, 6 rows: of 18,065 without tokens 5.3 8.3, with 5 8.6 11.8, with 32 9.4 20.9; of 65,000 without any 7.2 8.1; of 110,000 10.1 9.1;
+  // of 157,065 13.3 9.1.  512 workgroups in all: 24 rows of 110,000 with 5, parts for 64, 128, ... 2048 workgroups, 16.6, 16.1, 15.5, 15.1, 15.2, 16.7; 93 of 500,000 without any 47, 47, 28, 20, 21, 21.
+  const int64_t one = kScoreThreads * (p.a.top ? kMostVectors : 48);
+  const int64_t least = p.a.top ? ceil_div(pieces, one) : ceil_div(pieces, kMostPieces), most = ceil_div(pieces, kScoreThreads);
   const int64_t limit = p.a.top ? 64 : 128;       // (of lists that are joined)
-  const int64_t wanted = std::max<int64_t>(least, std::min<int64_t>({most, limit, 512 / std::max<int64_t>(1, p.a.rows)}));
+  const int64_t wanted = pieces <= one ? 1 : std::max<int64_t>(least, std::min<int64_t>({most, limit, 512 / std::max<int64_t>(1, p.a.rows)}));
   const int64_t rounds = ceil_div(pieces, wanted * kScoreThreads);           // pieces per lane
   p.parts = (int32_t)ceil_div(pieces, rounds * kScoreThreads);
   p.vectors = (int32_t)(rounds * kScoreThreads);

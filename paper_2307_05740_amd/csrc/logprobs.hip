@@ -3,9 +3,9 @@
 // What bounds it is memory: the logits are read once (backward: read and written).  A workgroup holds a part of a row in its registers, so that the
 // maximum, the sums relative to it and the largest logits all come from one reading; a second kernel joins the parts of rows that were cut.
 //
-// The largest logits.  Value and index of a logit make one whole number, its key, so that no two are alike and the order is that of the results.  In each
-// wavefront the key that comes `top`-th among its lanes' largest ones is no larger than the `top`-th of all; the largest of the wavefronts' is the border.
-// The few pieces that reach it are read again, and their keys from it on go to a list in LDS, where each is placed by counting those before it.
+// The largest logits.  Value and index of a logit make one whole number, its key, so that no two are alike and the order is that of the results.  The value that comes `top`-th
+// among the lanes' largest ones (a search by bits, counting lanes by ballots) is no larger than the `top`-th of all: the border.  The few pieces that reach it are read again, and their keys
+// from it on go to a list in LDS, where each is placed by counting those before it.  If so many are alike that the list has no room, the border is found again as a key.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,20 +22,29 @@ constexpr int kThreads = kScoreThreads, kWaves = kThreads / 64;
 constexpr int kList = 1024;           // keys from the border on that a workgroup has room for
 constexpr float kLeast = -256.f;      // exponents of two below this are 0, and so is their product with it
 
-template <typename T> struct Piece;   // 16 bytes of a row
+__device__ __forceinline__ uint32_t word_of(const u32x4& r, int i) { return i < 2 ? (i == 0 ? r[0] : r[1]) : i == 2 ? r[2] : r[3]; }
+
+template <typename T> struct Piece;   // 16 bytes of a row; an element of it (`any` takes numbers that are no constants)
 template <> struct Piece<float> {
   static constexpr int kEach = 4;
   static constexpr uint32_t kNothing = 0xff800000u;
+  static __device__ __forceinline__ float any(const u32x4& r, int i) { return __uint_as_float(word_of(r, i)); }
   static __device__ __forceinline__ float get(const u32x4& r, int i) { return __uint_as_float(r[i]); }
 };
 template <> struct Piece<__bf16> {
   static constexpr int kEach = 8;
   static constexpr uint32_t kNothing = 0xff80ff80u;
+  static __device__ __forceinline__ float any(const u32x4& r, int i) { return __uint_as_float(word_of(r, i >> 1) >> (16 * (i & 1)) << 16); }
   static __device__ __forceinline__ float get(const u32x4& r, int i) { return __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16); }
 };
 template <> struct Piece<_Float16> {
   static constexpr int kEach = 8;
   static constexpr uint32_t kNothing = 0xfc00fc00u;
+  static __device__ __forceinline__ float any(const u32x4& r, int i) {
+    union { uint16_t u; _Float16 f; } x;
+    x.u = (uint16_t)(word_of(r, i >> 1) >> (16 * (i & 1)));
+    return (float)x.f;
+  }
   static __device__ __forceinline__ float get(const u32x4& r, int i) {
     union { uint16_t u; _Float16 f; } x;
     x.u = (uint16_t)(i & 1 ? r[i / 2] >> 16 : r[i / 2]);
@@ -124,6 +133,21 @@ __device__ __forceinline__ uint32_t nth_of(uint32_t x, uint64_t lanes, int count
   return base;
 }
 
+// The same over several numbers of each lane, of 32 bits.
+template <int M>
+__device__ __forceinline__ uint32_t nth_of_all(const uint32_t (&x)[M], int count) {
+  uint32_t base = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t more = base | 1u << b;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) n += __popcll(__ballot(x[i] >= more));
+    if (n >= count) base = more;
+    if (n == count) break;
+  }
+  return base;
+}
+
 // A number that the `count`-th of the lanes' keys is at least, as near to it as is worth it; 0 where there are fewer.  Indices have `bits` bits.
 __device__ __forceinline__ uint64_t nth_key(uint64_t key, uint64_t lanes, int count, int bits) {
   const uint32_t high = (uint32_t)(key >> 32), low = (uint32_t)key;
@@ -140,7 +164,9 @@ __device__ __forceinline__ uint64_t nth_key(uint64_t key, uint64_t lanes, int co
 }
 
 struct Chosen {
-  uint64_t list[kList];
+  uint64_t list[kList];               // (or a wavefront's in each quarter of it)
+  uint32_t values[kThreads];
+  int counts[kWaves];
   uint64_t border[kWaves];
   uint64_t most[kWaves];
   int count;
@@ -200,6 +226,32 @@ __device__ __forceinline__ void place(int top, Chosen& c, Out&& out, Below&& bel
   }
 }
 
+// The `top` largest keys of the wavefronts' quarters of the list to out(place, key), 0 where there are fewer; all threads, after a barrier.
+template <typename Out>
+__device__ __forceinline__ void rank_all(int top, const Chosen& chosen, Out&& out) {
+  constexpr int kRoom = kList / kWaves;
+  int counts[kWaves], n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    counts[w] = __builtin_amdgcn_readfirstlane(chosen.counts[w]);
+    n += counts[w];
+  }
+  for (int i = threadIdx.x; i < max(n, top); i += kThreads) {
+    if (i >= n) { out(i, (uint64_t)0); continue; }
+    int of = i, before = 0;
+    const uint64_t* mine = chosen.list;
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w)
+      if (mine == chosen.list + w * kRoom && of >= counts[w]) { of -= counts[w]; mine += kRoom; }
+    const uint64_t key = mine[of];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+#pragma unroll 4
+      for (int j = 0; j < counts[w]; ++j) before += chosen.list[w * kRoom + j] > key;
+    if (before < top) out(before, key);
+  }
+}
+
 __device__ __forceinline__ int64_t target_of(const ScoreArgs& p, int64_t row) {
   return p.a.target_bytes == 4 ? (int64_t)((const int32_t*)p.targets)[row] : ((const int64_t*)p.targets)[row];
 }
@@ -223,10 +275,11 @@ __device__ __forceinline__ void write_row(const ScoreArgs& p, int64_t row, const
   p.logp[row] = t.known ? s.of(t.logit, p.a.scale) : 0.f;
 }
 
-__device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i, uint64_t key, const Stats& s) {
-  p.top_ids[row * p.a.top + i] = index_of(key);
-  p.top_logp[row * p.a.top + i] = s.of(value_of(key), p.a.scale);
+__device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i, int id, float logit, const Stats& s) {
+  p.top_ids[row * p.a.top + i] = id;
+  p.top_logp[row * p.a.top + i] = s.of(logit, p.a.scale);
 }
+__device__ __forceinline__ void write_top(const ScoreArgs& p, int64_t row, int i, uint64_t key, const Stats& s) { write_top(p, row, i, index_of(key), value_of(key), s); }
 
 // Sums of a lane's logits, as they come.  Relative to R = M c rounded, c = scale log2 e, a product and a sum are one instruction; what R is off by is taken out of
 // the sums at the end.  M is raised when a piece exceeds it by 2^8.  A logit of -infinity makes w NaN, as 0 times an infinity is: then, and where others are not finite or
@@ -268,6 +321,100 @@ __device__ __forceinline__ Sums of_wave(Sums x, float c) {
   x.s = sum_of_lanes(x.s, 6);
   x.w = sum_of_lanes(x.w, 6);
   return x;
+}
+
+// Keys of any row, and of rows of at most 2^16 logits of a type of 16 bits: 16 bits of value and 16 of index.
+struct LongKey {
+  typedef uint64_t type;
+  static constexpr int kIndexBits = 32;
+  static __device__ __forceinline__ uint64_t of(float x, int index) { return key_of(x, index); }
+  static __device__ __forceinline__ int index(uint64_t key) { return index_of(key); }
+  static __device__ __forceinline__ float value(uint64_t key) { return value_of(key); }
+};
+template <typename T>
+struct Key {
+  typedef uint32_t type;
+  static constexpr int kIndexBits = 16;
+  static __device__ __forceinline__ uint32_t of(float x, int index) {
+    union { T t; uint16_t u; } v;
+    v.t = (T)(x + 0.f);                                      // (exact; -0 is 0)
+    const uint32_t u = x != x ? 0xffffu : v.u & 0x8000u ? ~v.u & 0xffffu : v.u | 0x8000u;
+    return u << 16 | (~index & 0xffff);
+  }
+  static __device__ __forceinline__ int index(uint32_t key) { return ~key & 0xffff; }
+  static __device__ __forceinline__ float value(uint32_t key) {
+    const uint32_t u = key >> 16;
+    union { uint16_t u; T t; } v;
+    v.u = (uint16_t)(u & 0x8000u ? u ^ 0x8000u : ~u);
+    return u == 0xffffu ? __builtin_nanf("") : (float)v.t;
+  }
+};
+template <>
+struct Key<float> : LongKey {};
+
+// Keys from the border on of a wavefront's lanes, to a list; how many they are (the list has the first of them).  `lanes` are those of this lane's row.  A lane holds the N pieces
+// j * kStep + sub of `pieces` at `at`, the first of which is the row's piece `first`, knows the largest element of each (`most`), and may have one element beside
+// them (`edge`).  It takes its pieces that reach the border one after the other, and of those their elements that do, so that a wavefront works on as many of either as the lane with
+// most of them has.  They are counted off by ballots: nothing waits for LDS.
+template <typename T, typename Of, int N, int kStep>
+__device__ __forceinline__ int collect(typename Of::type border, const Row<T>& r, const u32x4* at, int first, int pieces, int sub, const u32x4 (&x)[N], const float (&most)[N],
+                                       int edge, float beside, uint64_t lanes, typename Of::type* list, int room) {
+  using P = Piece<T>;
+  using K = typename Of::type;
+  const uint64_t below = lanes & (((uint64_t)1 << (threadIdx.x & 63)) - 1);
+  const float least = border >> Of::kIndexBits ? Of::value(border) : minus_infinity();
+  int n = 0;
+  auto keep = [&](bool has, float v, int index) {
+    const K k = Of::of(v, index);
+    const bool in = has && k >= border;
+    const uint64_t all = __ballot(in);
+    const int to = n + __popcll(all & below);
+    if (in && to < room) list[to] = k;
+    n += __popcll(all & lanes);
+  };
+  if (__any(edge >= 0)) keep(edge >= 0, beside, edge);
+  uint32_t near = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) near |= j * kStep + sub < pieces && !(most[j] < least) ? 1u << j : 0u;
+  while (__any(near)) {
+    const bool has = near;
+    const int j = has ? __builtin_ctz(near) : 0, piece = j * kStep + sub;
+    near &= near - 1;
+    u32x4 v = x[0];
+    if constexpr (N == 2) v = j ? x[1] : v;
+    else if (N > 2 && has) v = at[piece];                    // (a choice of more registers costs more, and holds them)
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < P::kEach; ++e) bits |= !(P::get(v, e) < least) ? 1u << e : 0u;
+    bits = has ? bits : 0;
+    while (__any(bits)) {
+      const int e = bits ? __builtin_ctz(bits) : 0;
+      keep(bits, P::any(v, e), r.index(first + piece, e));
+      bits &= bits - 1;
+    }
+  }
+  return n;
+}
+
+// The key of a lane's largest element, 0: it has none.
+template <typename T, typename Of, int N, int kStep>
+__device__ __forceinline__ typename Of::type largest_key(const Row<T>& r, const u32x4* at, int first, int pieces, int sub, const float (&most)[N], float mine, int edge,
+                                                         float beside) {
+  using P = Piece<T>;
+  auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
+  typename Of::type key = edge >= 0 ? Of::of(beside, edge) : 0;
+  int found = -1;
+#pragma unroll
+  for (int j = N - 1; j >= 0; --j)
+    if (j * kStep + sub < pieces && alike(most[j], mine)) found = j * kStep + sub;
+  if (found >= 0) {
+    const u32x4 piece = at[found];
+    int e = 0;
+#pragma unroll
+    for (int i = P::kEach - 1; i >= 0; --i) e = alike(P::get(piece, i), mine) ? i : e;
+    key = max(key, Of::of(mine, r.index(first + found, e)));
+  }
+  return key;
 }
 
 // A part of a row, of any length: a lane has four pieces on their way.
@@ -408,6 +555,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   }
   const Sums wave_sums = of_wave(lane_sums, c);
   if ((tid & 63) == 0) waves[tid >> 6] = wave_sums;
+  chosen.values[tid] = edge >= 0 || tid < pieces ? (uint32_t)(key_of(mine, 0) >> 32) : 0;
   __syncthreads();
   Sums sum = waves[0];
 #pragma unroll
@@ -415,55 +563,34 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   if (p.parts > 1 && tid == 0) *(f32x4*)(p.sums + (row * p.parts + part) * 4) = f32x4{sum.M, sum.s, sum.w, 0.f};
   const Stats s(sum);
   if (p.parts == 1 && tid == 0) write_row(p, row, s, target);
+  auto out = [&](int i, uint64_t k) {
+    if (p.parts > 1) p.keys[(row * p.parts + part) * p.a.top + i] = k;
+    else write_top(p, row, i, k, s);
+  };
 
-  // the lane's largest key: its piece is taken, or read again, for the index
-  constexpr bool kHeld = N <= 4;
-  uint64_t key = 0;
-  auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
-  auto look = [&](const u32x4& v, int piece) {
-    int at = 0;
+  // Every wavefront looks for the border by itself, and has a quarter of the list.
+  constexpr int kRoom = kList / kWaves;
+  const int top = p.a.top, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t values[kWaves];
 #pragma unroll
-    for (int i = P::kEach - 1; i >= 0; --i) at = alike(P::get(v, i), mine) ? i : at;
-    key = key_of(mine, r.index(piece, at));
-  };
-  int found = -1;
-#pragma unroll
-  for (int j = N - 1; j >= 0; --j)
-    if (j * kThreads + tid < pieces && alike(most[j], mine)) {
-      if (kHeld) look(x[j], first + j * kThreads + tid);
-      else found = j * kThreads + tid;
-    }
-  if (!kHeld && found >= 0) look(at[found], first + found);
-  if (edge >= 0) {
-    const uint64_t k = key_of(beside, edge);
-    key = k > key ? k : key;
+  for (int w = 0; w < kWaves; ++w) values[w] = chosen.values[w * 64 + (tid & 63)];
+  const uint64_t border = (uint64_t)nth_of_all(values, top) << 32;
+  const int count = collect<T, LongKey, N, kThreads>(border, r, at, first, pieces, tid, x, most, edge, beside, ~(uint64_t)0, chosen.list + wave * kRoom, kRoom);
+  if ((tid & 63) == 0) chosen.counts[wave] = count;
+  if (!__syncthreads_or(count > kRoom)) {
+    rank_all(top, chosen, out);
+    return;
   }
-  const uint64_t border = border_of(key, p.a.top, index_bits(p.a.vocabulary), chosen);
-  if (edge >= 0) put(key_of(beside, edge), border, chosen);
-  const float least = border ? value_of(border) : minus_infinity();
-  auto put_all = [&](const u32x4& v, int piece) {
+  // many are alike: the border is a value and an index, and all share the list
+  const uint64_t key = largest_key<T, LongKey, N, kThreads>(r, at, first, pieces, tid, most, mine, edge, beside), exact = border_of(key, top, index_bits(p.a.vocabulary), chosen);
+  if (edge >= 0) put(key_of(beside, edge), exact, chosen);
+  for (int i = tid; i < pieces; i += kThreads) {
+    const u32x4 v = at[i];
 #pragma unroll
-    for (int e = 0; e < P::kEach; ++e)
-      if (!(P::get(v, e) < least)) put(key_of(P::get(v, e), r.index(piece, e)), border, chosen);
-  };
-  uint32_t near = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (j * kThreads + tid < pieces && !(most[j] < least)) {
-      if (kHeld) put_all(x[j], first + j * kThreads + tid);
-      else near |= 1u << j;
-    }
-  while (near) {
-    const int i = __builtin_ctz(near) * kThreads + tid;
-    near &= near - 1;
-    put_all(at[i], first + i);
+    for (int e = 0; e < P::kEach; ++e) put(key_of(P::get(v, e), r.index(first + i, e)), exact, chosen);
   }
   place(
-      p.a.top, chosen,
-      [&](int i, uint64_t k) {
-        if (p.parts > 1) p.keys[(row * p.parts + part) * p.a.top + i] = k;
-        else write_top(p, row, i, k, s);
-      },
+      top, chosen, out,
       [&](uint64_t last) {
         uint64_t best = 0;
         auto next = [&](uint64_t k) { best = k < last && k > best ? k : best; };
@@ -478,18 +605,20 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
 }
 
 // Rows of few pieces: L lanes each, of which each holds N pieces; nothing is cut, and the rows of a wavefront have nothing to do with each other.
-template <int L>
+__device__ __forceinline__ uint32_t other_lane(uint32_t x, int m) { return (uint32_t)__shfl_xor((int)x, m, 64); }
+__device__ __forceinline__ uint64_t other_lane(uint64_t x, int m) { return __shfl_xor((unsigned long long)x, m, 64); }
+
+template <typename K, int L>
 struct ChosenOfRows {
   static constexpr int kRows = kThreads / L, kRoom = kList / kRows;
-  uint64_t list[kRows][kRoom];
-  int count[kRows];
+  K list[kRows][kRoom];
 };
 
 template <typename T, int L, int N, bool kTop>
 __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
   using P = Piece<T>;
   constexpr int kLog = L == 16 ? 4 : 6, kRows = kThreads / L;
-  __shared__ std::conditional_t<kTop, ChosenOfRows<L>, int> chosen;
+  __shared__ std::conditional_t<kTop, ChosenOfRows<typename Key<T>::type, L>, int> chosen;
   const int sub = threadIdx.x & (L - 1), mine_of = threadIdx.x / L;
   const int64_t at_row = (int64_t)blockIdx.x * kRows + mine_of, row = min(at_row, p.a.rows - 1);     // (rows that are not there are the last one again)
   const bool there = at_row < p.a.rows;
@@ -543,88 +672,69 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
   if (there && sub == 0) write_row(p, row, s, target);
 
   if constexpr (kTop) {
+    using Of = Key<T>;
+    using K = typename Of::type;
+    constexpr int kRoom = ChosenOfRows<K, L>::kRoom;
     const int top = p.a.top;
-    uint64_t* list = chosen.list[mine_of];
-    if (sub == 0) chosen.count[mine_of] = 0;
-    auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
-    uint64_t key = edge >= 0 ? key_of(beside, edge) : 0;
-    int found = -1;
-    u32x4 piece = x[0];
-#pragma unroll
-    for (int j = N - 1; j >= 0; --j)
-      if (j * L + sub < r.pieces && alike(most[j], mine)) {
-        found = j * L + sub;
-        piece = x[j];
-      }
-    if (found >= 0) {
-      int e = 0;
-#pragma unroll
-      for (int i = P::kEach - 1; i >= 0; --i) e = alike(P::get(piece, i), mine) ? i : e;
-      key = max(key, key_of(mine, r.index(found, e)));
-    }
-    const uint64_t border = nth_key(key, lanes, top, index_bits(p.a.vocabulary));
-    const float least = border ? value_of(border) : minus_infinity();
-    __syncthreads();
-    auto keep = [&](float v, int index) {
-      if (v < least) return;
-      const uint64_t k = key_of(v, index);
-      if (k < border) return;
-      const int to = atomicAdd(&chosen.count[mine_of], 1);   // (the order in the list does not matter)
-      if (to < ChosenOfRows<L>::kRoom) list[to] = k;
+    K* list = chosen.list[mine_of];
+    auto reach = [&](K border) {
+      const int n = collect<T, Of, N, L>(border, r, at, 0, r.pieces, sub, x, most, edge, beside, lanes, list, kRoom);
+      // (a wavefront's own accesses of LDS keep their order)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      return n;
     };
-    if (edge >= 0) keep(beside, edge);
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j * L + sub < r.pieces && !(most[j] < least)) {
-#pragma unroll
-        for (int e = 0; e < P::kEach; ++e) keep(P::get(x[j], e), r.index(j * L + sub, e));
-      }
-    __syncthreads();
-    const int n = chosen.count[mine_of];
-    if (n <= ChosenOfRows<L>::kRoom) {
+    // As many lanes as there are tokens have a value from the border on.
+    const uint32_t value = edge >= 0 || sub < r.pieces ? (uint32_t)(Of::of(mine, 0) >> Of::kIndexBits) : 0;
+    int n = reach((K)nth_of(value, lanes, top, 0, Of::kIndexBits) << Of::kIndexBits);
+    if (__any(n > kRoom)) {
+      // many are alike: the border is a value and an index
+      const K key = largest_key<T, Of, N, L>(r, at, 0, r.pieces, sub, most, mine, edge, beside);
+      if constexpr (sizeof(K) == 4) n = reach(nth_of(key, lanes, top, 0, 32));
+      else n = reach(nth_key(key, lanes, top, index_bits(p.a.vocabulary)));
+    }
+    if (n <= kRoom) {
       for (int i = sub; i < n; i += L) {
-        const uint64_t k = list[i];
+        const K k = list[i];
         int before = 0;
 #pragma unroll 8
         for (int j = 0; j < n; ++j) before += list[j] > k;
-        if (there && before < top) write_top(p, row, before, k, s);
+        if (there && before < top) write_top(p, row, before, Of::index(k), Of::value(k), s);
       }
     } else {
       // no room: the largest key below the last one, `top` times
-      uint64_t last = ~(uint64_t)0;
+      K last = ~(K)0;
       for (int i = 0; i < top; ++i) {
-        uint64_t best = 0;
-        auto next = [&](uint64_t k) { best = k < last && k > best ? k : best; };
-        if (edge >= 0) next(key_of(beside, edge));
+        K best = 0;
+        auto next = [&](K k) { best = k < last && k > best ? k : best; };
+        if (edge >= 0) next(Of::of(beside, edge));
+        for (int j = sub; j < r.pieces; j += L) {
+          const u32x4 v = at[j];
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j * L + sub < r.pieces) {
-#pragma unroll
-            for (int e = 0; e < P::kEach; ++e) next(key_of(P::get(x[j], e), r.index(j * L + sub, e)));
-          }
-        for (int m = L / 2; m; m >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, m, 64));
-        if (there && sub == 0) write_top(p, row, i, best, s);
+          for (int e = 0; e < P::kEach; ++e) next(Of::of(P::get(v, e), r.index(j, e)));
+        }
+        for (int m = L / 2; m; m >>= 1) best = max(best, other_lane(best, m));
+        if (there && sub == 0) write_top(p, row, i, Of::index(best), Of::value(best), s);
         last = best;
       }
     }
   }
 }
 
-// The parts of a row.  All loads that others do not wait for come first.
+// The parts of a row.  All loads that others do not wait for come first.  Of up to 2048 keys each thread holds some, and the border comes from the threads' largest ones, as above;
+// of more, from those of the parts.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
-  constexpr int kHeld = 4;
+  constexpr int kHeld = 8, kRoom = kList / kWaves;
   __shared__ Sums waves[kWaves];
   __shared__ Chosen chosen;
-  const int tid = threadIdx.x, top = p.a.top;
+  const int tid = threadIdx.x, top = p.a.top, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x, n = (int64_t)p.parts * top;
   const float c = p.a.scale * kLog2e;
   const uint64_t* keys = p.keys + row * n;
-  uint64_t held[kHeld], key = 0;
+  uint64_t held[kHeld], most = 0;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) held[i] = i * kThreads + tid < n ? keys[i * kThreads + tid] : 0;
-  if (top)
-    for (int i = tid; i < p.parts; i += kThreads) key = max(key, keys[(int64_t)i * top]);
   const Target target(p, row, (const T*)nullptr);
   Sums sum{minus_infinity(), 0.f, 0.f};
   for (int i = tid; i < p.parts; i += kThreads) {
@@ -632,7 +742,10 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
     sum.add({v[0], v[1], v[2]}, c);
   }
   sum = of_wave(sum, c);
-  if ((tid & 63) == 0) waves[tid >> 6] = sum;
+  if ((tid & 63) == 0) waves[wave] = sum;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) most = max(most, held[i]);
+  chosen.values[tid] = (uint32_t)(most >> 32);
   __syncthreads();
   sum = waves[0];
 #pragma unroll
@@ -640,17 +753,36 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
   const Stats s(sum);
   if (tid == 0) write_row(p, row, s, target);
   if (top == 0) return;
-  const uint64_t border = border_of(key, top, index_bits(p.a.vocabulary), chosen);
+  auto out = [&](int i, uint64_t k) { write_top(p, row, i, k, s); };
+  if (n <= kHeld * kThreads) {
+    uint32_t values[kWaves];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) put(held[i], border, chosen);
-  for (int64_t i = kHeld * kThreads + tid; i < n; i += kThreads) put(keys[i], border, chosen);
-  place(
-      top, chosen, [&](int i, uint64_t k) { write_top(p, row, i, k, s); },
-      [&](uint64_t last) {
-        uint64_t best = 0;
-        for (int64_t i = tid; i < n; i += kThreads) best = keys[i] < last && keys[i] > best ? keys[i] : best;
-        return best;
-      });
+    for (int w = 0; w < kWaves; ++w) values[w] = chosen.values[w * 64 + (tid & 63)];
+    const uint64_t border = (uint64_t)nth_of_all(values, top) << 32, below = ((uint64_t)1 << (tid & 63)) - 1;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const uint64_t all = __ballot(held[i] && held[i] >= border);
+      const int to = count + __popcll(all & below);
+      if (held[i] && held[i] >= border && to < kRoom) chosen.list[wave * kRoom + to] = held[i];
+      count += __popcll(all);
+    }
+    if ((tid & 63) == 0) chosen.counts[wave] = count;
+    if (!__syncthreads_or(count > kRoom)) {
+      rank_all(top, chosen, out);
+      return;
+    }
+  }
+  // more keys, or many of one value
+  uint64_t key = 0;
+  for (int i = tid; i < p.parts; i += kThreads) key = max(key, keys[(int64_t)i * top]);
+  const uint64_t border = border_of(key, top, index_bits(p.a.vocabulary), chosen);
+  for (int64_t i = tid; i < n; i += kThreads) put(keys[i], border, chosen);
+  place(top, chosen, out, [&](uint64_t last) {
+    uint64_t best = 0;
+    for (int64_t i = tid; i < n; i += kThreads) best = keys[i] < last && keys[i] > best ? keys[i] : best;
+    return best;
+  });
 }
 
 // The same without tokens, of few parts: a row to a lane.
@@ -750,7 +882,8 @@ int rows(const ScoreArgs& p, hipStream_t s) {
   } else {
     if (n <= 2) score_rows_kernel<T, 64, 2, kTop><<<grid, block, 0, s>>>(p);
     else if (n <= 4) score_rows_kernel<T, 64, 4, kTop><<<grid, block, 0, s>>>(p);
-    else score_rows_kernel<T, 64, 8, kTop><<<grid, block, 0, s>>>(p);
+    else if (n <= 8) score_rows_kernel<T, 64, 8, kTop><<<grid, block, 0, s>>>(p);
+    else score_rows_kernel<T, 64, 16, kTop><<<grid, block, 0, s>>>(p);
   }
   return (int)hipGetLastError();
 }

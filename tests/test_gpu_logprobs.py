@@ -89,6 +89,31 @@ def test_numbers_of_rows(torch, LogProbs, rows, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pieces,rows", [(256, 3), (512, 5), (513, 5), (768, 4097), (769, 4097), (768, 30), (1024, 9), (1025, 9), (4096, 3), (4097, 3), (12288, 2), (12289, 2), (30000, 2)])
+def test_edges_of_the_kernels(torch, LogProbs, dtype, pieces, rows):
+    """Rows of that many pieces of 16 bytes, less one element, and of one element more, with and without most likely tokens."""
+    each = 128 // torch.finfo(getattr(torch, dtype)).bits
+    for n in ((pieces - 1) * each, (pieces - 1) * each + 1):
+        x, t = normal(torch, n, dtype, rows, n, by=2.0), targets_of(torch, 2, rows, n)
+        check(torch, LogProbs(1.1), x, t, 20 if rows < 4000 else 3, grads=False)
+        check(torch, LogProbs(1.1), x, t, grads=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [300_000, 2_200_000])
+def test_many_parts(torch, LogProbs, dtype, n):
+    """More keys than the workgroup that joins parts holds; all logits alike; the largest ones in one part, and as one lane's keys."""
+    x = torch.zeros(4, n, device="cuda")
+    x[0] = torch.randn(n, generator=torch.Generator().manual_seed(n)).cuda()
+    x[1, n // 2:n // 2 + 40] = 1.0
+    x[2, ::n // 31] = 2.0
+    x[3] = x[0].abs().round()
+    x = x.to(getattr(torch, dtype))
+    for top in (1, 20, 32):
+        check(torch, LogProbs(), x, targets_of(torch, 2, 4, n), top, grads=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [40, 3000, 40000])
 def test_order_of_logits_that_are_alike(torch, LogProbs, dtype, n):
     """All alike; few different ones; in falling and rising order; all large ones where one lane of a workgroup has them."""
