@@ -10,11 +10,15 @@ namespace arrow {
 void plan_score(ScoreArgs& p) {
   // Pieces of 16 bytes that a row reaches into, at any address.
   const int64_t each = 16 / size_of(p.a.dtype), pieces = ceil_div((int64_t)p.a.vocabulary, each) + 1;
-  // Rows of few pieces have 16 lanes or a wavefront each.  (Tokens on top are looked for among those that lanes have as their largest: there have to be some more lanes than
+  // Rows of few pieces have 16 lanes, 32 or a wavefront each.  (Tokens on top are looked for among those that lanes have as their largest: there have to be some more lanes than
   // tokens.)  A wavefront and a workgroup, us, bfloat16: rows of 5675 with the 20 best, 2048 of them 12.2 24.3, 20,000 57.8 140; of 8100 with 5, one 7.7 11.8 (in two launches), 9668 35.2 58.0;
   // without any, of 5675, 4096 12.0 12.0, 20,000 41.4 52.6, of 8100, 2048 10.5 9.0, 20,000 59.0 60.0.
+  // 16 lanes, 32, and 64, 65,536 rows: of 472 without tokens 12.5 14.2 19.8, with 5 25.2 31.9 41.2, with 12 37.1 37.8 44.5, with 20 - 47.5 48.1; of 952 21.7 20.8 25.4, 33.7 38.5 45.9,
+  // 47.8 46.0 51.7, - 58.0 58.6;  of 232 with 20 - 39.6 52.5.
   p.parts = 1;
-  p.lanes = pieces <= 16 * 4 && p.a.top <= 8 ? 16 : pieces <= 64 * (p.a.top ? 16 : p.a.rows >= 4096 ? 12 : 8) ? 64 : 0;
+  if (p.a.top <= 8 && pieces <= 128) p.lanes = 16;
+  else if ((p.a.top <= 16 && pieces >= 24 && pieces <= 128) || (p.a.top <= 20 && pieces >= 28 && pieces <= 64)) p.lanes = 32;
+  else p.lanes = pieces <= 64 * (p.a.top ? 16 : p.a.rows >= 4096 ? 12 : 8) ? 64 : 0;
   if (p.lanes) {
     p.vectors = (int32_t)(ceil_div(pieces, p.lanes) * p.lanes);
     return;

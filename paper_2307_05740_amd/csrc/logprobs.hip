@@ -617,12 +617,12 @@ struct ChosenOfRows {
 template <typename T, int L, int N, bool kTop>
 __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
   using P = Piece<T>;
-  constexpr int kLog = L == 16 ? 4 : 6, kRows = kThreads / L;
+  constexpr int kLog = L == 16 ? 4 : L == 32 ? 5 : 6, kRows = kThreads / L;
   __shared__ std::conditional_t<kTop, ChosenOfRows<typename Key<T>::type, L>, int> chosen;
   const int sub = threadIdx.x & (L - 1), mine_of = threadIdx.x / L;
   const int64_t at_row = (int64_t)blockIdx.x * kRows + mine_of, row = min(at_row, p.a.rows - 1);     // (rows that are not there are the last one again)
   const bool there = at_row < p.a.rows;
-  const uint64_t lanes = L == 64 ? ~(uint64_t)0 : (uint64_t)0xffff << (threadIdx.x & 48);
+  const uint64_t lanes = L == 64 ? ~(uint64_t)0 : (((uint64_t)1 << (L & 63)) - 1) << (threadIdx.x & (64 - L));
   const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
   const u32x4* at = r.piece(0);
   const Target target(p, row, (const T*)nullptr);
@@ -692,6 +692,28 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
       const K key = largest_key<T, Of, N, L>(r, at, 0, r.pieces, sub, most, mine, edge, beside);
       if constexpr (sizeof(K) == 4) n = reach(nth_of(key, lanes, top, 0, 32));
       else n = reach(nth_key(key, lanes, top, index_bits(p.a.vocabulary)));
+    }
+    if (L == 64 && n > 64 && n <= kRoom) {
+      // (a few lanes have many of them: those from the list's own `top`-th on, by the first 32 bits of their keys)
+      constexpr int kEach = kRoom / 64;
+      K k[kEach];
+      uint32_t high[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        k[i] = 64 * i + sub < n ? list[64 * i + sub] : 0;
+        high[i] = (uint32_t)(k[i] >> (8 * sizeof(K) - 32));
+      }
+      const uint32_t border = nth_of_all(high, top);
+      n = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const bool in = k[i] && high[i] >= border;
+        const uint64_t all = __ballot(in);
+        if (in) list[n + __popcll(all & (((uint64_t)1 << sub) - 1))] = k[i];
+        n += __popcll(all);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
     if (n <= kRoom) {
       for (int i = sub; i < n; i += L) {
@@ -878,7 +900,12 @@ int rows(const ScoreArgs& p, hipStream_t s) {
   if (lanes == 16) {
     if (n <= 1) score_rows_kernel<T, 16, 1, kTop><<<grid, block, 0, s>>>(p);
     else if (n <= 2) score_rows_kernel<T, 16, 2, kTop><<<grid, block, 0, s>>>(p);
-    else score_rows_kernel<T, 16, 4, kTop><<<grid, block, 0, s>>>(p);
+    else if (n <= 4) score_rows_kernel<T, 16, 4, kTop><<<grid, block, 0, s>>>(p);
+    else score_rows_kernel<T, 16, 8, kTop><<<grid, block, 0, s>>>(p);
+  } else if (lanes == 32) {
+    if (n <= 1) score_rows_kernel<T, 32, 1, kTop><<<grid, block, 0, s>>>(p);
+    else if (n <= 2) score_rows_kernel<T, 32, 2, kTop><<<grid, block, 0, s>>>(p);
+    else score_rows_kernel<T, 32, 4, kTop><<<grid, block, 0, s>>>(p);
   } else {
     if (n <= 2) score_rows_kernel<T, 64, 2, kTop><<<grid, block, 0, s>>>(p);
     else if (n <= 4) score_rows_kernel<T, 64, 4, kTop><<<grid, block, 0, s>>>(p);

@@ -89,14 +89,14 @@ def test_numbers_of_rows(torch, LogProbs, rows, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("pieces,rows", [(256, 3), (512, 5), (513, 5), (768, 4097), (769, 4097), (768, 30), (1024, 9), (1025, 9), (4096, 3), (4097, 3), (12288, 2), (12289, 2), (30000, 2)])
+@pytest.mark.parametrize("pieces,rows", [(2, 70), (23, 9), (24, 9), (28, 33), (64, 70), (65, 70), (128, 9), (129, 70), (256, 3), (512, 5), (513, 5), (768, 4097), (769, 4097), (768, 30), (1024, 9), (1025, 9), (4096, 3), (4097, 3), (12288, 2), (12289, 2), (30000, 2)])
 def test_edges_of_the_kernels(torch, LogProbs, dtype, pieces, rows):
     """Rows of that many pieces of 16 bytes, less one element, and of one element more, with and without most likely tokens."""
     each = 128 // torch.finfo(getattr(torch, dtype)).bits
     for n in ((pieces - 1) * each, (pieces - 1) * each + 1):
         x, t = normal(torch, n, dtype, rows, n, by=2.0), targets_of(torch, 2, rows, n)
-        check(torch, LogProbs(1.1), x, t, 20 if rows < 4000 else 3, grads=False)
-        check(torch, LogProbs(1.1), x, t, grads=False)
+        for top in (0, 3, 8, 9, 16, 17, 20, 21, 32) if pieces < 200 else (0, 20) if rows < 4000 else (0, 3):
+            check(torch, LogProbs(1.1), x, t, min(n, top), grads=False)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
