@@ -6,6 +6,10 @@
 // The largest logits.  Value and index of a logit make one whole number, its key, so that no two are alike and the order is that of the results.  The value that comes `top`-th
 // among the lanes' largest ones (a search by bits, counting lanes by ballots) is no larger than the `top`-th of all: the border.  The few pieces that reach it are read again, and their keys
 // from it on go to a list in LDS, where each is placed by counting those before it.  If so many are alike that the list has no room, the border is found again as a key.
+//
+// Measured: 8192 rows of 32,000 in bfloat16 with the five best 109 us (97 on changing inputs), 4.8 TB/s of 524 MB (a 1 GiB copy: 5.1), vector instructions in 85 % of the cycles, some twelve
+// for a logit and a hundred for a row's border; 4095 of 50,257 without any, and their gradient: 110 and 134 us, 3.8 and 6.2 TB/s (the gradient's writes go on under the next
+// forward call), 243 together for 242 of the floor; 4 rows of 128,001 in float32 with the twenty best 7.1 us and 5.7 for the join, launches and barriers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -417,7 +421,7 @@ __device__ __forceinline__ typename Of::type largest_key(const Row<T>& r, const 
   return key;
 }
 
-// A part of a row, of any length: a lane has four pieces on their way.
+// A part of a row, of any length: a lane has four pieces on their way.  Six wavefronts to a SIMD; held to eight, it spills.
 template <typename T>
 __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
   using P = Piece<T>;

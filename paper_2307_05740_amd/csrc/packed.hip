@@ -7,13 +7,17 @@
 // Everything stays in registers.  Scores are computed transposed, keys by heads: a lane holds a quarter of a key's row, whose order within the product is
 // free, so that its 16 bytes are one load.  Of the result a lane holds four keys of a head in each half of a tile, and the products with the values take these
 // eight as they are: the values of four tokens lie together in the cache so that a lane finds its four tokens' eight columns (heads of 128) in 16 bytes, and two
-// bytes permutations turn two tokens' pairs of columns into two columns' pairs of tokens.
+// permutations of bytes turn two tokens' pairs of columns into two columns' pairs of tokens.
+//
+// Measured: 32 rows of up to 16,000 keys, 32/8 heads of 128, 366 MB in 80 us with the join, 4.6 TB/s (a 1 GiB copy: 5.1), matrix units busy in 11 % of the cycles and vector
+// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 39 %; 64 rows under a window of 4096, 16/4 heads of 64, 20 us, 3.5 TB/s, where a wavefront has
+// 16 tiles in all; one row of 1000 keys 5.4 us and 3.7 for the join, which are launches and four loads that wait for each other.  Tried for groups of up to 4 heads: four blocks of
+// 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax: 22 us for those 64 rows, and 173 for the 32 with heads of 128, which spill.
 #include "attention_common.h"
 #include "packed_internal.h"
 
 namespace arrow {
 namespace {
-
 
 template <int N> struct Words;
 template <> struct Words<1> { typedef uint32_t type; };
@@ -59,7 +63,8 @@ __device__ __forceinline__ int64_t key_scales_at(int page, int dim) { return (in
 __device__ __forceinline__ int64_t value_scales_at(int page, int dim) { return (int64_t)page * (dim + dim / 32); }
 
 // ---- writes and reads ----
-// Eight elements a lane, four lanes to a scale.  Four tokens of a head lie in neighbouring lanes, so that what a wavefront writes are whole runs of bytes.
+// Eight elements a lane, four lanes to a scale.  Four tokens of a head lie in neighbouring lanes, so that what a wavefront writes are whole runs of bytes.  Bound by memory:
+// 16,384 tokens of 8 heads of 128 are written in 17.5 us, 5.0 TB/s, and read in 15.6, 5.7.
 struct Place {
   int64_t row, slot;                  // slot -1: none
   int head, piece;

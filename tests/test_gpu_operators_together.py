@@ -175,6 +175,97 @@ def test_on_another_stream(torch):
     assert torch.equal(d, score.backward(s.logp, s.entropy, x, t, s.stats, s.entropy))
 
 
+def test_two_streams_and_two_graphs_at_once(torch):
+    """The same objects called on two streams that do not wait for each other, and captured twice: calls share no memory."""
+    from paper_2307_05740_amd.logprobs import ArrowLogProbs
+    from paper_2307_05740_amd.packed import ArrowPackedAttention
+    from paper_2307_05740_amd.rotation import ArrowRotation
+    rotate, score, attend = ArrowRotation(128), ArrowLogProbs(), ArrowPackedAttention()
+    pool = attend.pool(300, 16, 2, 128)
+    slots = torch.arange(300 * 16, device="cuda")
+    attend.append(normal(torch, 1, "bfloat16", 4800, 2, 128), normal(torch, 2, "bfloat16", 4800, 2, 128), pool, slots)
+    table, lengths = torch.arange(300, dtype=torch.int32, device="cuda").view(1, 300), torch.tensor([4800], dtype=torch.int32, device="cuda")
+    weights = [1 + 0.3 * normal(torch, s, "float32", 128) for s in (3, 4)]
+
+    def inputs(seed):
+        q, k = normal(torch, seed, "bfloat16", 700, 8, 128), normal(torch, seed + 1, "bfloat16", 700, 2, 128)
+        return q, k, normal(torch, seed + 2, "float32", 3, 200_000), torch.arange(3, device="cuda")
+
+    def work(q, k, x, t):
+        y = rotate.forward(q, k, *weights)
+        back = rotate.backward(*y, q, k, *weights)
+        r = score.forward(x, t, 20)
+        return (*y, *back, *r, score.backward(r.logp, r.entropy, x, t, r.stats, r.entropy), attend.decode(q[:1], pool, table, lengths))
+
+    ins = [inputs(10), inputs(20)]
+    want = [work(*i) for i in ins]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ins]
+    got = [[], []]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(work(*ins[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for run in got[i] for a, b in zip(run, want[i]))
+    del got
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in ins], []
+    for graph, i in zip(graphs, ins):
+        with torch.cuda.graph(graph):
+            outs.append(work(*i))
+    for turn in range(6):
+        for out in outs:
+            for o in out:
+                o.zero_()
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        eager = work(*ins[turn % 2])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, want[turn % 2]))
+        for i in (0, 1):
+            assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
+
+
+def test_gradients_of_broadcast_operands(torch):
+    """Heads and tokens that are one in memory, gradients whose elements have one address, weights that queries and keys share."""
+    from paper_2307_05740_amd.logprobs import ArrowLogProbs
+    from paper_2307_05740_amd.rotation import ArrowRotation
+    rotate, score = ArrowRotation(64), ArrowLogProbs()
+    x, w = normal(torch, 1, "float32", 1, 9, 1, 64).requires_grad_(), (1 + 0.2 * normal(torch, 2, "float32", 64)).requires_grad_()
+    q, k = rotate(x.expand(3, 9, 4, 64), x.expand(3, 9, 1, 64), w, w)
+    (q.sum() + (k * 2).sum()).backward()
+    one = x.detach()
+    gq, gk = torch.ones(3, 9, 4, 64, device="cuda"), torch.full((3, 9, 1, 64), 2.0, device="cuda")
+    dq, dk, dwq, dwk = rotate.backward(gq, gk, one.expand(3, 9, 4, 64).contiguous(), one.expand(3, 9, 1, 64).contiguous(), w.detach(), w.detach())
+    torch.testing.assert_close(x.grad, dq.sum((0, 2), keepdim=True) + dk.sum((0, 2), keepdim=True), rtol=2.0 ** -18, atol=2.0 ** -18)     # (fifteen numbers near one, in other orders)
+    # the same 108 and 27 terms, in an order that goes by how sequences lie: each sum is off by at most its number of terms times 2^-24 of the sizes' sum, and a term is
+    # a normed element times one of a pair of ones, or twos, that is turned
+    n = (one.double() / (one.double().square().mean(-1, keepdim=True) + 1e-6).sqrt()).abs().sum((0, 1, 2)) * 2 ** 0.5
+    assert bool(((w.grad.double() - (dwq + dwk)).abs() <= 2 * 2.0 ** -24 * (109 * 12 * n + 28 * 3 * 2 * n + 2 * (12 + 6) * n)).all())
+    rows = normal(torch, 3, "bfloat16", 7, 50).requires_grad_()
+    logp, entropy = score(rows, torch.arange(7, device="cuda"))
+    entropy.sum().backward()
+    r = score.forward(rows.detach(), torch.arange(7, device="cuda"))
+    assert torch.equal(rows.grad, score.backward(None, torch.ones(7, device="cuda"), rows.detach(), torch.arange(7, device="cuda"), r.stats, r.entropy))
+    with pytest.raises(RuntimeError):
+        score.forward(rows.detach()[:1].expand(7, 50), torch.arange(7, device="cuda"))       # rows that lie upon each other are refused
+
+
+def test_in_inference_mode(torch):
+    from paper_2307_05740_amd.logprobs import ArrowLogProbs
+    from paper_2307_05740_amd.rotation import ArrowRotation
+    x, q = normal(torch, 1, "bfloat16", 5, 333), normal(torch, 2, "bfloat16", 6, 3, 32)
+    with torch.inference_mode():
+        r, y = ArrowLogProbs().forward(x, torch.arange(5, device="cuda"), 3), ArrowRotation(32).forward(q, q.clone())
+        assert r.logp.is_inference() and y[0].is_inference()
+        r.logp.add_(1)
+    s, z = ArrowLogProbs().forward(x, torch.arange(5, device="cuda"), 3), ArrowRotation(32).forward(q, q.clone())
+    assert torch.equal(r.logp, s.logp + 1) and torch.equal(r.lse, s.lse) and torch.equal(r.top_ids, s.top_ids) and torch.equal(y[0], z[0])
+
+
 def test_by_the_general_way(torch):
     """Devices without a number, subclasses of tensors and strided targets go by the classes' own checks, to the same results."""
     from paper_2307_05740_amd.logprobs import ArrowLogProbs
