@@ -9,10 +9,11 @@
 // eight as they are: the values of four tokens lie together in the cache so that a lane finds its four tokens' eight columns (heads of 128) in 16 bytes, and two
 // permutations of bytes turn two tokens' pairs of columns into two columns' pairs of tokens.
 //
-// Measured: 32 rows of up to 16,000 keys, 32/8 heads of 128, 366 MB in 80 us with the join, 4.6 TB/s (a 1 GiB copy: 5.1), matrix units busy in 11 % of the cycles and vector
-// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 39 %; 64 rows under a window of 4096, 16/4 heads of 64, 20 us, 3.5 TB/s, where a wavefront has
-// 16 tiles in all; one row of 1000 keys 5.4 us and 3.7 for the join, which are launches and four loads that wait for each other.  Tried for groups of up to 4 heads: four blocks of
-// 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax: 22 us for those 64 rows, and 173 for the 32 with heads of 128, which spill.
+// Measured: 32 rows of up to 16,000 keys, 32/8 heads of 128, 366 MB in 78 us with the join, 4.7 TB/s (a 1 GiB copy: 5.1), matrix units busy in 11 % of the cycles and vector
+// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 39 %; 64 rows under a window of 4096, 16/4 heads of 64, 19 us, 3.8 TB/s, where a wavefront has
+// 16 tiles in all, one of two on its SIMD: some 150 vector and 65 scalar instructions each, and the waits between them; one row of 1000 keys 5.4 us and 3.7 for the join, which are
+// launches and four loads that wait for each other.  Tried for the window: four blocks of 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax
+// (22 us, and spills with heads of 128); tiles of 64 keys (24, spills); twice as many tiles on their way (22).
 #include "attention_common.h"
 #include "packed_internal.h"
 
@@ -210,7 +211,7 @@ struct Codes {
   uint32_t visible;                   // keys, the same in all lanes
 };
 
-template <typename T, int D, int kWaves>
+template <typename T, int D, int kWaves, bool kPairs>
 __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArgs a) {
   constexpr int kSteps = D / 32;      // of the scores' inner dimension
   constexpr int kColumns = D / 16;    // columns of a lane
@@ -227,9 +228,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
   // (columns << page_log is at most 2^26.  All that follows to the first load is the same in all lanes, and said to be so where the compiler loses sight of it.)
   const int length = __builtin_amdgcn_readfirstlane(max(0, min(c.lengths[b], c.columns << a.page_log)));
   const int begin = c.window ? max(0, length - c.window) : 0;
-  // groups of 16 keys (within a page), those that only hide between the first ones and the window left out; tiles of two groups, stretches of whole rounds of the wavefronts
-  const int rest = begin >> 4, lead = min((min(c.sinks, begin) + 15) >> 4, rest), groups = lead + ((length + 15) >> 4) - rest;
-  const int tiles = (groups + 1) >> 1, rounds = (tiles + kWaves - 1) / kWaves;
+  // groups of 16 keys, or of 32 (within a page), those that only hide between the first ones and the window left out; tiles of 32 keys, stretches of whole rounds of the wavefronts
+  constexpr int kLog = kPairs ? 5 : 4, kGroups = kPairs ? 1 : 2, kKeys = 1 << kLog;
+  const int rest = begin >> kLog, lead = min((min(c.sinks, begin) + kKeys - 1) >> kLog, rest), groups = lead + ((length + kKeys - 1) >> kLog) - rest;
+  const int tiles = (groups + kGroups - 1) / kGroups, rounds = (tiles + kWaves - 1) / kWaves;
   const int tile0 = kWaves * (int)((int64_t)rounds * split / a.splits), tile1 = min(tiles, kWaves * (int)((int64_t)rounds * (split + 1) / a.splits));
   const int32_t* table = c.table + (int64_t)b * c.columns;
   const char* pool = (const char*)a.pool + kv * c.head_step;
@@ -244,11 +246,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
 
   // (nothing here branches: the loads of one tile are to be on their way while another's are waited for; a page that is not there is read as the first one)
   auto group_at = [&](int g) { return g < lead ? g : g - lead + rest; };
-  auto page_of = [&](int g) { return table[group_at(min(g, groups - 1)) >> (a.page_log - 4)]; };
-  int page[2] = {0, 0};               // of the tile that is loaded next, looked up a tile ahead
+  auto page_of = [&](int g) { return table[group_at(min(g, groups - 1)) >> (a.page_log - kLog)]; };
+  int page[kGroups] = {};             // of the tile that is loaded next, looked up a tile ahead
   auto find_pages = [&](int tile) {
-    page[0] = page_of(2 * tile);
-    page[1] = page_of(2 * tile + 1);
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) page[h] = page_of(kGroups * tile + h);
   };
   // (what a lane adds to its wavefront's addresses: of its quarter of key l % 16, of tokens 4 (l / 16) + 0..3, and of their scales)
   const uint32_t of_key = col * (D / 2) + quarter * (D / 8), of_value = (quarter * 16 + col) * (D / 8);
@@ -257,19 +259,25 @@ __global__ __launch_bounds__(64 * kWaves, 4) void packed_decode_kernel(PackedArg
     Codes<D> x;
     x.visible = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int g = 2 * tile + h, key0 = 16 * group_at(g), slot0 = key0 & (c.page - 1);
+    for (int h = 0; h < kGroups; ++h) {
+      const int g = kGroups * tile + h, key0 = kKeys * group_at(g), slot0 = key0 & (c.page - 1);
       const bool in = g < groups && (uint32_t)page[h] < (uint32_t)c.pages;
       const char* block = pool + (uint32_t)__builtin_amdgcn_readfirstlane(in ? page[h] : 0) * c.page_step;
       const char *codes = block + slot0 * (D / 2), *scales = block + c.page * D + slot0 * (D / 32);
-      x.k[h] = *(const words<kSteps>*)(codes + of_key);
-      x.ks[h] = *(const uint8_t*)(scales + of_key_scale);
-      x.v[h] = *(const words<kSteps>*)(codes + c.page * (D / 2) + of_value);
-      x.vs[h] = *(const uint32_t*)(scales + c.page * (D / 32) + of_value_scale);
-      uint32_t mask = 0xffff;
-      if (key0 < begin || key0 + 16 > length) {       // at an edge of what is seen
-        const int upto = min(16, length - key0), gone = min(16, max(0, begin - key0)), first = min(16, max(0, c.sinks - key0));
-        mask = ((1u << max(0, upto)) - 1) & (~((1u << gone) - 1) | ((1u << first) - 1)) & 0xffff;
+      const char *values = codes + c.page * (D / 2), *value_scales = scales + c.page * (D / 32);
+#pragma unroll
+      for (int i = h; i < h + 2 / kGroups; ++i) {           // (sixteen keys are 8 D bytes of codes and D / 2 of scales further)
+        const int of = i - h;
+        x.k[i] = *(const words<kSteps>*)(codes + of * 8 * D + of_key);
+        x.ks[i] = *(const uint8_t*)(scales + of * (D / 2) + of_key_scale);
+        x.v[i] = *(const words<kSteps>*)(values + of * 8 * D + of_value);
+        x.vs[i] = *(const uint32_t*)(value_scales + of * (D / 2) + of_value_scale);
+      }
+      constexpr uint32_t kAll = kPairs ? 0xffffffffu : 0xffffu;
+      uint32_t mask = kAll;
+      if (key0 < begin || key0 + kKeys > length) {          // at an edge of what is seen
+        const auto below = [](int n) { return n >= 32 ? ~0u : (1u << max(0, n)) - 1; };
+        mask = below(length - key0) & (~below(begin - key0) | below(c.sinks - key0)) & kAll;
       }
       x.visible |= (in ? mask : 0u) << (16 * h);
     }
@@ -406,8 +414,11 @@ int decode(const PackedArgs& a, hipStream_t s) {
   const arrow_packed_t& c = a.c;
   const int64_t blocks = (int64_t)c.batch * c.kv_heads * a.splits * ((a.group + kHeadTile - 1) / kHeadTile), rows = (int64_t)c.batch * c.q_heads;
   if (blocks * 64 * a.waves > 0xffffffff || rows * 256 > 0xffffffff) return (int)hipErrorInvalidConfiguration;   // (a launch has less than 2^32 threads)
-  if (a.waves == 4) packed_decode_kernel<T, D, 4><<<dim3((unsigned)blocks), dim3(64 * 4), 0, s>>>(a);
-  else packed_decode_kernel<T, D, 8><<<dim3((unsigned)blocks), dim3(64 * 8), 0, s>>>(a);
+  // Pages of 32 tokens or more have a tile in one of them: half the work on addresses and edges, which is scalar but takes turns with the rest (64 rows under a window of 4096, heads of 64
+  // 20.9 us as for pages of 16, 19.1; 54 rows of up to 12,700 keys, 6/2 heads of 128, 35.2 and 32.2).
+  const auto launch = [&](auto* kernel) { kernel<<<dim3((unsigned)blocks), dim3(64 * a.waves), 0, s>>>(a); };
+  if (a.waves == 4) launch(c.page >= 32 ? packed_decode_kernel<T, D, 4, true> : packed_decode_kernel<T, D, 4, false>);
+  else launch(c.page >= 32 ? packed_decode_kernel<T, D, 8, true> : packed_decode_kernel<T, D, 8, false>);
   if (a.splits > 1) {
     CacheArgs j{};
     j.c.dtype = c.dtype; j.c.batch = c.batch; j.c.q_heads = c.q_heads; j.c.dim = c.dim;
