@@ -74,23 +74,30 @@ PackedArgs plan_decode(const arrow_packed_t* c) {
   int64_t seen = std::min(c->max_len, room);
   if (p.c.window) seen = std::min(seen, (int64_t)p.c.window + p.c.sinks);
   const int64_t rows = std::max<int64_t>(1, (int64_t)c->batch * c->kv_heads * ceil_div(p.group, kHeadTile));
-  // Stretches of the visible keys, each a workgroup; more than one take another launch, for their join.  One where that is not worth it; the square root of a tenth of
-  // `seen` where there are few rows; and two workgroups to a compute unit where there are many, or stretches of up to 6000 keys where lengths differ (us):
-  //   2 rows of 1000 keys: 1 stretch 9.9, 4 8.4, 8 8.0, 16 7.8, 64 9.2;  of 200, heads of 64: 1 4.9, 2 7.6
-  //   8 rows of 60,000: 16 33.1, 32 21.9, 64 20.1, 128 23.4;  32 of 1000 .. 4000: 4 13.1, 8 10.6, 16 10.4, 32 12.1
-  //   128 rows of 500 .. 2000: 1 16.4, 4 12.7, 8 13.2, 16 16.5;  512 of 125 .. 500: 1 9.8, 2 14.8;  256 of 4000 .. 16,000: 2 84, 3 79, 8 81
-  const int64_t full = std::max(512 / rows, p.c.window ? 0 : ceil_div(seen, 6000)), best = (int64_t)std::sqrt(0.1 * (double)seen);
+  // Stretches of the visible keys, each a workgroup of four wavefronts; more than one take another launch, for their join.
+  const bool equal = p.c.window != 0;               // (sequences see equally many keys)
   p.waves = 4;
-  // Many rows under a window see equally many keys, so that workgroups of eight wavefronts fill the chip without a join (256 rows of 4096 keys: heads of 64, four wavefronts in
-  // one stretch 27.9, two 24.6, eight in one 20.7; heads of 128, 34.2, 30.1, 26.4).
-  if (p.c.window && rows >= 192 && rows <= 768 && seen > 256) {
+  p.splits = 1;
+  if (seen <= 512) return p;                        // (2 to 256 rows of up to 400 keys: 6.7 to 8.8 us, in two stretches 9.7 to 11.4)
+  // One stretch, of eight wavefronts where these and not workgroups are what fills the chip; us, one stretch of four wavefronts, of eight, and the best of several of four:
+  //   heads of 64, 128 rows of up to 1000 keys 9.0 8.5 9.8, of 2000 14 12.0 11.5; 256 of 2000 14 12.0 15, of 4000 26 19 21; 512 of 4000 34 29 32, of 8000 59 48 45; 1024 of 1000 17 21 26
+  //   heads of 128, 2 rows of 1000 10.0 9.6 8.4; 160 of 1500 - 12.3 13.6, of 5000 - 28.2 23.9; 256 of 4000 31 24 26; 1024 of 8000 142 140 147
+  //   under a window of 4096, 256 rows, heads of 64 28 20.7 24.6, of 128 34 26.4 30.1
+  const bool eight = seen <= 1024 ? rows < 512 && (rows >= 64 || c->dim <= 64) : equal ? rows >= 192 && rows <= 768 : rows >= 160 && rows <= 768 && seen <= (rows < 192 ? 2000 : 6000);
+  if (eight) {
     p.waves = 8;
-    p.splits = 1;
     return p;
   }
-  // A round of a workgroup's wavefronts is 128 keys: no more stretches than the longest ones' number of rounds needs.
-  const int64_t rounds = std::max<int64_t>(1, ceil_div(seen, 128)), most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, full, best, rounds}));
-  p.splits = seen <= 256 ? 1 : (int32_t)ceil_div(rounds, ceil_div(rounds, most));
+  if (rows >= 512 && (equal || seen <= (rows > 768 ? 12000 : 6000))) return p;
+  // Several: as many as give two workgroups to a compute unit; where lengths differ, of about 1000 keys each, and 2000 beyond eight, or where there are many rows, 2500, and 6000
+  // beyond four; at most the square root of a tenth of `seen`, which is what their join is worth for few rows; no more than there are rounds of 128 keys.
+  //   128 rows of up to 16,000 keys, heads of 64, 4 stretches 34.5, 8 26.0; of 128, 41.7, 33.2; 256 of 8000, heads of 64, 2 36, 4 30, 8 30; 512 of 16,000, 3 99, 4 92, 8 95, of 30,000 5 165, 15 171
+  //   8 rows of 60,000, heads of 128, 16 33.1, 32 21.9, 64 20.1, 128 23.4;  2 of 1000, 4 8.4, 8 8.0, 16 7.8, 64 9.2
+  const int64_t even = equal ? 1 : rows > 768 ? ceil_div(seen, 4000) : rows >= 384 ? std::max(std::min<int64_t>(4, ceil_div(seen, 2500)), ceil_div(seen, 6000))
+                                                                                    : std::max(std::min<int64_t>(8, seen / 1000), ceil_div(seen, 2000));
+  const int64_t rounds = ceil_div(seen, 128), best = (int64_t)std::sqrt(0.1 * (double)seen);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, std::max(512 / rows, even), best, rounds}));
+  p.splits = (int32_t)ceil_div(rounds, ceil_div(rounds, most));
   return p;
 }
 

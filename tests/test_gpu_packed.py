@@ -187,6 +187,24 @@ def test_long_caches_in_stretches(torch, Packed, dtype, window, sinks):
     assert all(torch.equal(o, op.decode(q, pool, table, n)) for _ in range(3))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("batch,kv", [(1, 2), (7, 8), (8, 8), (19, 8), (20, 8), (24, 8), (48, 8), (64, 8), (96, 8), (97, 8)])
+@pytest.mark.parametrize("longest", [512, 513, 1024, 1025, 2000, 2001, 6000, 6001, 12001, 30000])
+def test_splits_by_rows_and_lengths(torch, Packed, dim, batch, kv, longest):
+    """Around the numbers of rows and keys from which the keys are cut otherwise: how they are goes by the longest length that is named, not by those that there are."""
+    op = Packed()
+    g = torch.Generator().manual_seed(batch)
+    lengths = torch.randint(0, 300, (batch,), generator=g).tolist()
+    lengths[0] = 1100
+    pool, table, n, keys, values = filled(torch, op, TYPES[batch % 2], lengths, 32, kv, dim)
+    wide = torch.full((batch, 1000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    q = normal(torch, 3, TYPES[batch % 2], batch, 2 * kv, dim, by=2.0)
+    o = op.decode(q, pool, wide, n, longest)
+    part = slice(0, batch, 9)
+    check(torch, op, o[part], q[part], keys[part], values[part])
+
+
 @pytest.mark.parametrize("dim", [32, 64, 128])
 @pytest.mark.parametrize("batch,kv", [(48, 4), (200, 1), (47, 4), (193, 4)])
 def test_many_rows_under_a_window(torch, Packed, dim, batch, kv):
