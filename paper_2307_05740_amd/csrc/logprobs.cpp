@@ -19,6 +19,14 @@ void plan_score(ScoreArgs& p) {
   if (p.a.top <= 8 && pieces <= 128) p.lanes = 16;
   else if ((p.a.top <= 16 && pieces >= 24 && pieces <= 128) || (p.a.top <= 20 && pieces >= 28 && pieces <= 64)) p.lanes = 32;
   else p.lanes = pieces <= 64 * (p.a.top ? 16 : p.a.rows >= 4096 ? 12 : 8) ? 64 : 0;
+  // More tokens than there are lanes with pieces, or nearly as many, leave no border to look for: lanes have single logits then.  (65,536 rows, pieces and logits: of 40 with 20 70.8 33.5;
+  // of 150 with 12 51.6 41.3, with 32 91.6 48.8; of 200 with 12 31.5 42.6, with 20 55.8 46.0.)
+  if (p.a.top > 8 && (pieces < 24 || 2 * pieces < 3 * p.a.top)) {
+    p.single = true;
+    p.lanes = 64;
+    p.vectors = (int32_t)(ceil_div(p.a.vocabulary, 64) * 64);
+    return;
+  }
   if (p.lanes) {
     p.vectors = (int32_t)(ceil_div(pieces, p.lanes) * p.lanes);
     return;

@@ -59,23 +59,31 @@ template <> struct Piece<_Float16> {
 // The larger of two; NaN where one is.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
+// One element as a piece, for rows of so few that pieces of 16 bytes leave most lanes without any.
+template <typename T> struct One : Piece<T> { static constexpr int kEach = 1; };
+
 // A row's elements: those before the first address that is a multiple of 16, whole pieces, and the rest.
-template <typename T>
+template <typename T, typename P = Piece<T>>
 struct Row {
   const T* at;
   int head, pieces, rest;
   __device__ __forceinline__ Row(const T* row, int n) {
-    constexpr int kEach = Piece<T>::kEach;
+    constexpr int kEach = P::kEach;
     const int off = (int)(((uintptr_t)row & 15) / sizeof(T));
     at = row;
-    head = off ? min(kEach - off, n) : 0;
+    head = kEach > 1 && off ? min(kEach - off, n) : 0;
     pieces = (n - head) / kEach;
     rest = (n - head) % kEach;
   }
-  __device__ __forceinline__ const u32x4* piece(int i) const { return (const u32x4*)(at + head + (int64_t)i * Piece<T>::kEach); }
-  __device__ __forceinline__ int index(int piece, int i) const { return head + piece * Piece<T>::kEach + i; }
+  __device__ __forceinline__ const u32x4* piece(int i) const { return (const u32x4*)(at + head + (int64_t)i * P::kEach); }
+  __device__ __forceinline__ u32x4 load(int i) const {
+    if constexpr (P::kEach > 1) return *piece(i);
+    else if constexpr (sizeof(T) == 4) return u32x4{((const uint32_t*)at)[i], 0, 0, 0};
+    else return u32x4{((const uint16_t*)at)[i], 0, 0, 0};
+  }
+  __device__ __forceinline__ int index(int piece, int i) const { return head + piece * P::kEach + i; }
   // the element beside the pieces that lane `tid` of the first part has, -1: none
-  __device__ __forceinline__ int edge(int tid, int n) const { return tid < head ? tid : tid >= 8 && tid < 8 + rest ? n - rest + tid - 8 : -1; }
+  __device__ __forceinline__ int edge(int tid, int n) const { return P::kEach == 1 ? -1 : tid < head ? tid : tid >= 8 && tid < 8 + rest ? n - rest + tid - 8 : -1; }
 };
 
 // Sums relative to a logit M near the largest: with d = (x - M) scale in exponents of two, s = sum 2^d, w = sum 2^d d.  (The difference comes before the product, so that
@@ -357,13 +365,12 @@ template <>
 struct Key<float> : LongKey {};
 
 // Keys from the border on of a wavefront's lanes, to a list; how many they are (the list has the first of them).  `lanes` are those of this lane's row.  A lane holds the N pieces
-// j * kStep + sub of `pieces` at `at`, the first of which is the row's piece `first`, knows the largest element of each (`most`), and may have one element beside
+// j * kStep + sub of `pieces`, the first of which is the row's piece `first`, knows the largest element of each (`most`), and may have one element beside
 // them (`edge`).  It takes its pieces that reach the border one after the other, and of those their elements that do, so that a wavefront works on as many of either as the lane with
 // most of them has.  They are counted off by ballots: nothing waits for LDS.
-template <typename T, typename Of, int N, int kStep>
-__device__ __forceinline__ int collect(typename Of::type border, const Row<T>& r, const u32x4* at, int first, int pieces, int sub, const u32x4 (&x)[N], const float (&most)[N],
+template <typename T, typename P, typename Of, int N, int kStep>
+__device__ __forceinline__ int collect(typename Of::type border, const Row<T, P>& r, int first, int pieces, int sub, const u32x4 (&x)[N], const float (&most)[N],
                                        int edge, float beside, uint64_t lanes, typename Of::type* list, int room) {
-  using P = Piece<T>;
   using K = typename Of::type;
   const uint64_t below = lanes & (((uint64_t)1 << (threadIdx.x & 63)) - 1);
   const float least = border >> Of::kIndexBits ? Of::value(border) : minus_infinity();
@@ -386,7 +393,7 @@ __device__ __forceinline__ int collect(typename Of::type border, const Row<T>& r
     near &= near - 1;
     u32x4 v = x[0];
     if constexpr (N == 2) v = j ? x[1] : v;
-    else if (N > 2 && has) v = at[piece];                    // (a choice of more registers costs more, and holds them)
+    else if (N > 2 && has) v = r.load(first + piece);                    // (a choice of more registers costs more, and holds them)
     uint32_t bits = 0;
 #pragma unroll
     for (int e = 0; e < P::kEach; ++e) bits |= !(P::get(v, e) < least) ? 1u << e : 0u;
@@ -401,10 +408,9 @@ __device__ __forceinline__ int collect(typename Of::type border, const Row<T>& r
 }
 
 // The key of a lane's largest element, 0: it has none.
-template <typename T, typename Of, int N, int kStep>
-__device__ __forceinline__ typename Of::type largest_key(const Row<T>& r, const u32x4* at, int first, int pieces, int sub, const float (&most)[N], float mine, int edge,
+template <typename T, typename P, typename Of, int N, int kStep>
+__device__ __forceinline__ typename Of::type largest_key(const Row<T, P>& r, int first, int pieces, int sub, const float (&most)[N], float mine, int edge,
                                                          float beside) {
-  using P = Piece<T>;
   auto alike = [](float a, float b) { return a == b || (a != a && b != b); };
   typename Of::type key = edge >= 0 ? Of::of(beside, edge) : 0;
   int found = -1;
@@ -412,7 +418,7 @@ __device__ __forceinline__ typename Of::type largest_key(const Row<T>& r, const 
   for (int j = N - 1; j >= 0; --j)
     if (j * kStep + sub < pieces && alike(most[j], mine)) found = j * kStep + sub;
   if (found >= 0) {
-    const u32x4 piece = at[found];
+    const u32x4 piece = r.load(first + found);
     int e = 0;
 #pragma unroll
     for (int i = P::kEach - 1; i >= 0; --i) e = alike(P::get(piece, i), mine) ? i : e;
@@ -579,14 +585,14 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) values[w] = chosen.values[w * 64 + (tid & 63)];
   const uint64_t border = (uint64_t)nth_of_all(values, top) << 32;
-  const int count = collect<T, LongKey, N, kThreads>(border, r, at, first, pieces, tid, x, most, edge, beside, ~(uint64_t)0, chosen.list + wave * kRoom, kRoom);
+  const int count = collect<T, P, LongKey, N, kThreads>(border, r, first, pieces, tid, x, most, edge, beside, ~(uint64_t)0, chosen.list + wave * kRoom, kRoom);
   if ((tid & 63) == 0) chosen.counts[wave] = count;
   if (!__syncthreads_or(count > kRoom)) {
     rank_all(top, chosen, out);
     return;
   }
   // many are alike: the border is a value and an index, and all share the list
-  const uint64_t key = largest_key<T, LongKey, N, kThreads>(r, at, first, pieces, tid, most, mine, edge, beside), exact = border_of(key, top, index_bits(p.a.vocabulary), chosen);
+  const uint64_t key = largest_key<T, P, LongKey, N, kThreads>(r, first, pieces, tid, most, mine, edge, beside), exact = border_of(key, top, index_bits(p.a.vocabulary), chosen);
   if (edge >= 0) put(key_of(beside, edge), exact, chosen);
   for (int i = tid; i < pieces; i += kThreads) {
     const u32x4 v = at[i];
@@ -618,23 +624,21 @@ struct ChosenOfRows {
   K list[kRows][kRoom];
 };
 
-template <typename T, int L, int N, bool kTop>
+template <typename T, int L, int N, bool kTop, typename P = Piece<T>>
 __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
-  using P = Piece<T>;
   constexpr int kLog = L == 16 ? 4 : L == 32 ? 5 : 6, kRows = kThreads / L;
   __shared__ std::conditional_t<kTop, ChosenOfRows<typename Key<T>::type, L>, int> chosen;
   const int sub = threadIdx.x & (L - 1), mine_of = threadIdx.x / L;
   const int64_t at_row = (int64_t)blockIdx.x * kRows + mine_of, row = min(at_row, p.a.rows - 1);     // (rows that are not there are the last one again)
   const bool there = at_row < p.a.rows;
   const uint64_t lanes = L == 64 ? ~(uint64_t)0 : (((uint64_t)1 << (L & 63)) - 1) << (threadIdx.x & (64 - L));
-  const Row<T> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
-  const u32x4* at = r.piece(0);
+  const Row<T, P> r((const T*)p.logits + row * p.a.stride, p.a.vocabulary);
   const Target target(p, row, (const T*)nullptr);
   u32x4 x[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     x[j] = u32x4{P::kNothing, P::kNothing, P::kNothing, P::kNothing};
-    if (j * L + sub < r.pieces) x[j] = at[j * L + sub];
+    if (j * L + sub < r.pieces) x[j] = r.load(j * L + sub);
   }
   const int edge = r.edge(sub, p.a.vocabulary);
   const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity(), c = p.a.scale * kLog2e;
@@ -682,7 +686,7 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
     const int top = p.a.top;
     K* list = chosen.list[mine_of];
     auto reach = [&](K border) {
-      const int n = collect<T, Of, N, L>(border, r, at, 0, r.pieces, sub, x, most, edge, beside, lanes, list, kRoom);
+      const int n = collect<T, P, Of, N, L>(border, r, 0, r.pieces, sub, x, most, edge, beside, lanes, list, kRoom);
       // (a wavefront's own accesses of LDS keep their order)
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -693,7 +697,7 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
     int n = reach((K)nth_of(value, lanes, top, 0, Of::kIndexBits) << Of::kIndexBits);
     if (__any(n > kRoom)) {
       // many are alike: the border is a value and an index
-      const K key = largest_key<T, Of, N, L>(r, at, 0, r.pieces, sub, most, mine, edge, beside);
+      const K key = largest_key<T, P, Of, N, L>(r, 0, r.pieces, sub, most, mine, edge, beside);
       if constexpr (sizeof(K) == 4) n = reach(nth_of(key, lanes, top, 0, 32));
       else n = reach(nth_key(key, lanes, top, index_bits(p.a.vocabulary)));
     }
@@ -735,7 +739,7 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
         auto next = [&](K k) { best = k < last && k > best ? k : best; };
         if (edge >= 0) next(Of::of(beside, edge));
         for (int j = sub; j < r.pieces; j += L) {
-          const u32x4 v = at[j];
+          const u32x4 v = r.load(j);
 #pragma unroll
           for (int e = 0; e < P::kEach; ++e) next(Of::of(P::get(v, e), r.index(j, e)));
         }
@@ -910,6 +914,10 @@ int rows(const ScoreArgs& p, hipStream_t s) {
     if (n <= 1) score_rows_kernel<T, 32, 1, kTop><<<grid, block, 0, s>>>(p);
     else if (n <= 2) score_rows_kernel<T, 32, 2, kTop><<<grid, block, 0, s>>>(p);
     else score_rows_kernel<T, 32, 4, kTop><<<grid, block, 0, s>>>(p);
+  } else if (kTop && p.single) {
+    if (n <= 2) score_rows_kernel<T, 64, 2, true, One<T>><<<grid, block, 0, s>>>(p);
+    else if (n <= 4) score_rows_kernel<T, 64, 4, true, One<T>><<<grid, block, 0, s>>>(p);
+    else score_rows_kernel<T, 64, 8, true, One<T>><<<grid, block, 0, s>>>(p);
   } else {
     if (n <= 2) score_rows_kernel<T, 64, 2, kTop><<<grid, block, 0, s>>>(p);
     else if (n <= 4) score_rows_kernel<T, 64, 4, kTop><<<grid, block, 0, s>>>(p);

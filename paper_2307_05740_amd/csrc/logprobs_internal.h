@@ -23,6 +23,7 @@ struct ScoreArgs {
   int32_t parts;                       // that a row is cut into
   int32_t vectors;                     // pieces of 16 bytes of a part: parts x vectors cover a row whatever its first address
   int32_t lanes;                       // that have a row: 16, 32 or 64, or 0 for workgroups, which parts have
+  bool single;                         // of 64 lanes: a logit is a piece
   float* sums;                         // rows x parts x 4: the largest logit, the sums relative to it, 0; where rows are cut
   uint64_t* keys;                      // rows x parts x top, falling
 };

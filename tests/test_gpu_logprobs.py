@@ -100,6 +100,17 @@ def test_edges_of_the_kernels(torch, LogProbs, dtype, pieces, rows):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [9, 16, 31, 32, 33, 63, 64, 65, 91, 92, 93, 127, 128, 129, 183, 184, 185, 191, 192, 193, 255, 256, 257, 370, 376, 400])
+def test_few_logits_and_many_tokens(torch, LogProbs, dtype, n):
+    """Rows of which a lane has single logits, and of nearly as many that it has pieces of: any address, logits that are alike, masked ones."""
+    x = normal(torch, n, dtype, 37, n, by=2.0)
+    x[1::4] = x[1::4].round()
+    x[2, n // 2:], x[3] = -math.inf, 0
+    for top in (1, 8, 9, 12, 20, 32):
+        check(torch, LogProbs(0.8), x, targets_of(torch, 2, 37, n), min(n, top), grads=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [300_000, 2_200_000])
 def test_many_parts(torch, LogProbs, dtype, n):
     """More keys than the workgroup that joins parts holds; all logits alike; the largest ones in one part, and as one lane's keys."""
