@@ -10,7 +10,7 @@
 // permutations of bytes turn two tokens' pairs of columns into two columns' pairs of tokens.
 //
 // Measured: 32 rows of up to 16,000 keys, 32/8 heads of 128, 366 MB in 78 us with the join, 4.7 TB/s (a 1 GiB copy: 5.1), matrix units busy in 11 % of the cycles and vector
-// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 39 %; 64 rows under a window of 4096, 16/4 heads of 64, 19 us, 3.8 TB/s, where a wavefront has
+// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 39 %; 64 rows under a window of 4096, 16/4 heads of 64, 18 us on changing inputs, 4.1 TB/s, where a wavefront has
 // 16 tiles in all, one of two on its SIMD: some 150 vector and 65 scalar instructions each, and the waits between them; one row of 1000 keys 5.4 us and 3.7 for the join, which are
 // launches and four loads that wait for each other.  Tried for the window: four blocks of 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax
 // (22 us, and spills with heads of 128); tiles of 64 keys (24, spills); twice as many tiles on their way (22).
