@@ -145,11 +145,25 @@ __device__ __forceinline__ uint32_t nth_of(uint32_t x, uint64_t lanes, int count
   return base;
 }
 
-// The same over several numbers of each lane, of 32 bits.
+// The same over several numbers of each lane, of 32 bits.  The highest bits that all have alike are not searched (4372 rows of 20,450 with five, 44.4 us with them, 42.8; rows of a
+// wavefront have more to do than to wait, and take 1 to 10 % longer so).
 template <int M>
 __device__ __forceinline__ uint32_t nth_of_all(const uint32_t (&x)[M], int count) {
-  uint32_t base = 0;
-  for (int b = 31; b >= 0; --b) {
+  uint32_t most = x[0], least = x[0];
+#pragma unroll
+  for (int i = 1; i < M; ++i) {
+    most = max(most, x[i]);
+    least = min(least, x[i]);
+  }
+  const auto over = [](uint32_t x, auto&& f) {
+    return (uint32_t)__builtin_amdgcn_readfirstlane(
+        __float_as_int(over_lanes(__uint_as_float(x), 6, [&](float a, float b) { return __uint_as_float(f(__float_as_uint(a), __float_as_uint(b))); })));
+  };
+  most = over(most, [](uint32_t a, uint32_t b) { return max(a, b); });
+  least = over(least, [](uint32_t a, uint32_t b) { return min(a, b); });
+  const int bits = most == least ? 0 : 32 - __clz((int)(most ^ least));
+  uint32_t base = bits > 31 ? 0 : most >> bits << bits;
+  for (int b = bits - 1; b >= 0; --b) {
     const uint32_t more = base | 1u << b;
     int n = 0;
 #pragma unroll
