@@ -145,24 +145,28 @@ __device__ __forceinline__ uint32_t nth_of(uint32_t x, uint64_t lanes, int count
   return base;
 }
 
-// The same over several numbers of each lane, of 32 bits.  The highest bits that all have alike are not searched (4372 rows of 20,450 with five, 44.4 us with them, 42.8; rows of a
-// wavefront have more to do than to wait, and take 1 to 10 % longer so).
-template <int M>
+// The same over several numbers of each lane, of 32 bits.  Numbers that are all there have their highest bits alike, which are not searched then (kAll): 4372 rows of 20,450 with five
+// tokens 44.4 -> 42.8 us, 64 of 32,000 with twenty 10.5 -> 10.3; parts of few pieces 0.2 to 0.4 us more; rows of a wavefront, which have more to do than to wait, 1 to 10 %.
+template <bool kAll, int M>
 __device__ __forceinline__ uint32_t nth_of_all(const uint32_t (&x)[M], int count) {
-  uint32_t most = x[0], least = x[0];
+  uint32_t base = 0;
+  int bits = 32;
+  if constexpr (kAll) {
+    uint32_t most = x[0], least = x[0];
 #pragma unroll
-  for (int i = 1; i < M; ++i) {
-    most = max(most, x[i]);
-    least = min(least, x[i]);
+    for (int i = 1; i < M; ++i) {
+      most = max(most, x[i]);
+      least = min(least, x[i]);
+    }
+    const auto over = [](uint32_t x, auto&& f) {
+      return (uint32_t)__builtin_amdgcn_readfirstlane(
+          __float_as_int(over_lanes(__uint_as_float(x), 6, [&](float a, float b) { return __uint_as_float(f(__float_as_uint(a), __float_as_uint(b))); })));
+    };
+    most = over(most, [](uint32_t a, uint32_t b) { return max(a, b); });
+    least = over(least, [](uint32_t a, uint32_t b) { return min(a, b); });
+    bits = most == least ? 0 : 32 - __clz((int)(most ^ least));
+    base = bits > 31 ? 0 : most >> bits << bits;
   }
-  const auto over = [](uint32_t x, auto&& f) {
-    return (uint32_t)__builtin_amdgcn_readfirstlane(
-        __float_as_int(over_lanes(__uint_as_float(x), 6, [&](float a, float b) { return __uint_as_float(f(__float_as_uint(a), __float_as_uint(b))); })));
-  };
-  most = over(most, [](uint32_t a, uint32_t b) { return max(a, b); });
-  least = over(least, [](uint32_t a, uint32_t b) { return min(a, b); });
-  const int bits = most == least ? 0 : 32 - __clz((int)(most ^ least));
-  uint32_t base = bits > 31 ? 0 : most >> bits << bits;
   for (int b = bits - 1; b >= 0; --b) {
     const uint32_t more = base | 1u << b;
     int n = 0;
@@ -598,7 +602,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   uint32_t values[kWaves];
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) values[w] = chosen.values[w * 64 + (tid & 63)];
-  const uint64_t border = (uint64_t)nth_of_all(values, top) << 32;
+  const uint64_t border = (uint64_t)nth_of_all<(N >= 8)>(values, top) << 32;
   const int count = collect<T, P, LongKey, N, kThreads>(border, r, first, pieces, tid, x, most, edge, beside, ~(uint64_t)0, chosen.list + wave * kRoom, kRoom);
   if ((tid & 63) == 0) chosen.counts[wave] = count;
   if (!__syncthreads_or(count > kRoom)) {
@@ -725,7 +729,7 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
         k[i] = 64 * i + sub < n ? list[64 * i + sub] : 0;
         high[i] = (uint32_t)(k[i] >> (8 * sizeof(K) - 32));
       }
-      const uint32_t border = nth_of_all(high, top);
+      const uint32_t border = nth_of_all<false>(high, top);
       n = 0;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
@@ -802,7 +806,7 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
     uint32_t values[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) values[w] = chosen.values[w * 64 + (tid & 63)];
-    const uint64_t border = (uint64_t)nth_of_all(values, top) << 32, below = ((uint64_t)1 << (tid & 63)) - 1;
+    const uint64_t border = (uint64_t)nth_of_all<false>(values, top) << 32, below = ((uint64_t)1 << (tid & 63)) - 1;
     int count = 0;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
