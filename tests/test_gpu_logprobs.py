@@ -211,6 +211,20 @@ def test_masked_and_odd_logits(torch, LogProbs, dtype, n):
     check(torch, LogProbs(), x[:, :49], t.clamp(max=48), 32)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [30, 100, 700, 3001, 40000])
+def test_order_of_the_smallest_numbers(torch, LogProbs, dtype, n):
+    """Logits below the type's normal numbers, of either sign, among zeros: none of them is taken for a zero."""
+    least = torch.finfo(getattr(torch, dtype)).smallest_normal * torch.finfo(getattr(torch, dtype)).eps
+    steps = torch.randint(-60, 61, (4, n), generator=torch.Generator().manual_seed(n)).double()
+    steps[1] = steps[1].clamp(max=0)
+    steps[2, 3:] = 0
+    x = (steps * least).to(getattr(torch, dtype)).cuda()
+    assert bool((x.double().cpu() == steps * least).all())
+    for top in (3, 9, 30):
+        check(torch, LogProbs(), x, targets_of(torch, 2, 4, n), top, grads=False)
+
+
 def test_large_logits(torch, LogProbs):
     """Differences count, whatever the size of the logits."""
     x = normal(torch, 1, "float32", 6, 3000) + torch.tensor([0.0, 1e3, -1e3, 1e5, 1e30, -3e38], device="cuda")[:, None]
