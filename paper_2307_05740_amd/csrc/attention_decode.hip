@@ -216,34 +216,58 @@ __global__ __launch_bounds__(64 * kWaves, 4) void attention_decode_kernel(CacheA
 
 // The results of the stretches of one query head, joined: two columns per lane, every fourth stretch per wavefront.  3 to 5 us, most of it the launch.
 template <typename T>
-__global__ __launch_bounds__(64 * kWaves) void attention_decode_join_kernel(CacheArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void attention_decode_join_kernel(DecodeJoinArgs a) {
+  constexpr int kAhead = 4;
   __shared__ float weights[kMostSplits];
   __shared__ float2 sums[kWaves][64];
-  const arrow_cache_t& c = a.c;
-  const int row = blockIdx.x, b = row / c.q_heads, head = row % c.q_heads, step = c.dim + 2, lane = threadIdx.x & 63, wave = wave_id(), d = 2 * lane;
+  const int row = blockIdx.x, b = row / a.q_heads, head = row % a.q_heads, step = a.dim + 2, lane = threadIdx.x & 63, wave = wave_id(), d = 2 * lane;
   const float* from = a.parts + (int64_t)row * a.splits * step;
+  // (all maxima and totals, and the columns of the first stretches, are on their way before one of them is waited for)
+  float2 stats[kMostSplits / 64], ahead[kAhead];
+#pragma unroll
+  for (int k = 0; k < kMostSplits / 64; ++k) {
+    const int i = lane + 64 * k;
+    stats[k] = float2{minus_infinity(), 0.f};
+    if (i < a.splits) stats[k] = *(const float2*)(from + (int64_t)i * step + a.dim);
+  }
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int i = wave + k * kWaves;
+    ahead[k] = i < a.splits && d < a.dim ? *(const float2*)(from + (int64_t)i * step + d) : float2{0.f, 0.f};
+  }
   float all = minus_infinity();
-  for (int i = lane; i < a.splits; i += 64) all = fmaxf(all, from[(int64_t)i * step + c.dim]);
+#pragma unroll
+  for (int k = 0; k < kMostSplits / 64; ++k) all = fmaxf(all, stats[k].x);
   for (int m = 32; m; m >>= 1) all = fmaxf(all, __shfl_xor(all, m, 64));
   const float off = all == minus_infinity() ? 0.f : all;
   float total = 0.f;
-  for (int i = lane; i < a.splits; i += 64) {
-    const float by = __builtin_amdgcn_exp2f(from[(int64_t)i * step + c.dim] - off);
+#pragma unroll
+  for (int k = 0; k < kMostSplits / 64; ++k) {
+    const int i = lane + 64 * k;
+    if (i >= a.splits) break;
+    const float by = __builtin_amdgcn_exp2f(stats[k].x - off);
     if (wave == 0) weights[i] = by;
-    total = fmaf(by, from[(int64_t)i * step + c.dim + 1], total);
+    total = fmaf(by, stats[k].y, total);
   }
   for (int m = 32; m; m >>= 1) total += __shfl_xor(total, m, 64);
   __syncthreads();
   float2 sum = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int i = wave + k * kWaves;
+    if (i >= a.splits) break;
+    sum.x = fmaf(weights[i], ahead[k].x, sum.x);
+    sum.y = fmaf(weights[i], ahead[k].y, sum.y);
+  }
 #pragma unroll 4
-  for (int i = wave; i < a.splits; i += kWaves) {
-    const float2 x = d < c.dim ? *(const float2*)(from + (int64_t)i * step + d) : float2{0.f, 0.f};
+  for (int i = wave + kAhead * kWaves; i < a.splits; i += kWaves) {
+    const float2 x = d < a.dim ? *(const float2*)(from + (int64_t)i * step + d) : float2{0.f, 0.f};
     sum.x = fmaf(weights[i], x.x, sum.x);
     sum.y = fmaf(weights[i], x.y, sum.y);
   }
   sums[wave][lane] = sum;
   __syncthreads();
-  if (wave > 0 || d >= c.dim) return;
+  if (wave > 0 || d >= a.dim) return;
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) { sum.x += sums[w][lane].x; sum.y += sums[w][lane].y; }
   const float over = total > 0.f || total != total ? 1.f / total : 0.f;
@@ -282,7 +306,7 @@ int decode(const CacheArgs& a, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (c.dim <= 64) attention_decode_kernel<T, 64><<<dim3((unsigned)blocks), dim3(64 * kWaves), 0, s>>>(a);
   else attention_decode_kernel<T, 128><<<dim3((unsigned)blocks), dim3(64 * kWaves), 0, s>>>(a);
-  if (a.splits > 1) attention_decode_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kWaves), 0, s>>>(a);
+  if (a.splits > 1) attention_decode_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kWaves), 0, s>>>({a.o, a.parts, a.splits, c.q_heads, c.dim});
   return (int)hipGetLastError();
 }
 
@@ -290,10 +314,10 @@ int decode(const CacheArgs& a, void* stream) {
 
 int launch_attention_decode(const CacheArgs& a, void* stream) { return a.c.dtype == ARROW_BF16 ? decode<__bf16>(a, stream) : decode<_Float16>(a, stream); }
 
-int launch_attention_decode_join(const CacheArgs& a, void* stream) {
-  const dim3 rows((unsigned)(a.c.batch * a.c.q_heads)), threads(64 * kWaves);
-  if (a.c.dtype == ARROW_BF16) attention_decode_join_kernel<__bf16><<<rows, threads, 0, (hipStream_t)stream>>>(a);
-  else attention_decode_join_kernel<_Float16><<<rows, threads, 0, (hipStream_t)stream>>>(a);
+int launch_attention_decode_join(const DecodeJoinArgs& a, int32_t dtype, int64_t rows, void* stream) {
+  const dim3 grid((unsigned)rows), threads(64 * kWaves);
+  if (dtype == ARROW_BF16) attention_decode_join_kernel<__bf16><<<grid, threads, 0, (hipStream_t)stream>>>(a);
+  else attention_decode_join_kernel<_Float16><<<grid, threads, 0, (hipStream_t)stream>>>(a);
   return (int)hipGetLastError();
 }
 

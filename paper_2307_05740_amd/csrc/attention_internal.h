@@ -43,6 +43,13 @@ struct CacheArgs {
   float* parts;                    // splits x batch x q_heads x (dim + 2)
 };
 
+// Stretches of a cache, joined: rows of batch x q_heads.  (Of its own: a launch whose arguments are below 128 bytes takes the host half a microsecond less than one of 300.)
+struct DecodeJoinArgs {
+  Operand o;
+  const float* parts;              // rows x splits x (dim + 2): sums, maximum, total
+  int32_t splits, q_heads, dim;
+};
+
 // Into how many parts the forward call cuts a row's keys where it has a workspace, 1 to kMostRowSplits.
 int attention_forward_splits(const AttentionArgs& a);
 
@@ -51,7 +58,7 @@ int launch_attention_forward(const AttentionArgs& a, int32_t dtype, void* stream
 int launch_attention_backward(const AttentionArgs& a, int32_t dtype, void* stream);
 int launch_cache_append(const CacheArgs& a, void* stream);
 int launch_attention_decode(const CacheArgs& a, void* stream);
-int launch_attention_decode_join(const CacheArgs& a, void* stream);   // the second of its kernels: c.dtype, batch, q_heads and dim, o, splits and parts
+int launch_attention_decode_join(const DecodeJoinArgs& a, int32_t dtype, int64_t rows, void* stream);   // the second of its kernels
 
 constexpr int kQueryTile = 128;    // queries of a workgroup, forward and dq
 constexpr int kKeyTile = 128;      // keys of a workgroup, dk and dv

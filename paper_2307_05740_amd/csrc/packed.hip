@@ -419,12 +419,7 @@ int decode(const PackedArgs& a, hipStream_t s) {
   const auto launch = [&](auto* kernel) { kernel<<<dim3((unsigned)blocks), dim3(64 * a.waves), 0, s>>>(a); };
   if (a.waves == 4) launch(c.page >= 32 ? packed_decode_kernel<T, D, 4, true> : packed_decode_kernel<T, D, 4, false>);
   else launch(c.page >= 32 ? packed_decode_kernel<T, D, 8, true> : packed_decode_kernel<T, D, 8, false>);
-  if (a.splits > 1) {
-    CacheArgs j{};
-    j.c.dtype = c.dtype; j.c.batch = c.batch; j.c.q_heads = c.q_heads; j.c.dim = c.dim;
-    j.o = a.o; j.splits = a.splits; j.parts = a.parts;
-    return launch_attention_decode_join(j, s);
-  }
+  if (a.splits > 1) return launch_attention_decode_join({a.o, a.parts, a.splits, c.q_heads, c.dim}, c.dtype, rows, s);
   return (int)hipGetLastError();
 }
 
