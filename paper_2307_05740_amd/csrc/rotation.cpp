@@ -88,6 +88,8 @@ RotationArgs plan(const arrow_rotation_t* a, bool backward) {
     p.length = a->batch * a->tokens;
   }
   while ((16 << p.lanes_log) < a->dim) ++p.lanes_log;
+  p.whole = (16 << p.lanes_log) == a->dim;
+  p.share = 1.f / (float)a->dim;
   if (!backward) {
     p.tiles[0] = tiles_of(p, a->q_heads + a->kv_heads, 1024);
     p.blocks = std::min(p.tiles[0].all, 1 << 23);    // (a launch has less than 2^32 threads)

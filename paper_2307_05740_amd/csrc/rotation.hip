@@ -31,13 +31,22 @@ __device__ __forceinline__ Raw<T> raw8(const T* at) {
   if constexpr (sizeof(T) == 4) return {{*(const f32x4*)at, *(const f32x4*)(at + 4)}};
   else return {*(const x8<T>*)at};
 }
+// Zeros where the piece is not there.
 template <typename T>
-__device__ __forceinline__ Eight wide(const Raw<T>& r, bool in) {
+__device__ __forceinline__ Raw<T> only(const Raw<T>& r, bool in) {
+  union { Raw<T> r; uint32_t u[sizeof(Raw<T>) / 4]; } x;
+  x.r = r;
+#pragma unroll
+  for (auto& u : x.u) u = in ? u : 0;
+  return x.r;
+}
+template <typename T>
+__device__ __forceinline__ Eight wide(const Raw<T>& r) {
   Eight e;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if constexpr (sizeof(T) == 4) e.x[i] = in ? r.v[i / 4][i % 4] : 0.f;
-    else e.x[i] = in ? (float)r.v[i] : 0.f;
+    if constexpr (sizeof(T) == 4) e.x[i] = r.v[i / 4][i % 4];
+    else e.x[i] = (float)r.v[i];
   }
   return e;
 }
@@ -179,7 +188,7 @@ __device__ __forceinline__ void Heads<T, kBack, kKeys, kInterleaved>::run(const 
   const arrow_rotation_t& a = p.a;
   const int half = a.rotary / 2, step = kThreads >> p.lanes_log, step_t = step / heads, step_head = step - step_t * heads;
   while (true) {
-    const Pieces now = next;
+    Pieces now = next;
     const int now_t = t, now_head = head;
     i += step;
     const bool more = i < n;
@@ -188,22 +197,30 @@ __device__ __forceinline__ void Heads<T, kBack, kKeys, kInterleaved>::run(const 
     if (head >= heads) { head -= heads; ++t; }
     if (!more) { t = now_t; head = now_head; }
     load();
-    Eight xa = wide<T>(now.xa, lane.has_first), xb = wide<T>(now.xb, lane.has_second);
+    if (!p.whole) {
+      now.xa = only(now.xa, lane.has_first);
+      now.xb = only(now.xb, lane.has_second);
+      if constexpr (kBack) {
+        now.ga = only(now.ga, lane.has_first);
+        now.gb = only(now.gb, lane.has_second);
+      }
+    }
+    Eight xa = wide<T>(now.xa), xb = wide<T>(now.xb);
     float square = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) square = fmaf(xa.x[j], xa.x[j], fmaf(xb.x[j], xb.x[j], square));
-    const float r = 1.f / sqrtf(sum_of_lanes(square, p.lanes_log) / (float)a.dim + a.eps);
+    const float r = rsqrtf(fmaf(sum_of_lanes(square, p.lanes_log), p.share, a.eps));
     const float2* cs = angles + now_t * half + lane.pair;
     if constexpr (!kBack) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) { xa.x[j] *= r * w[lane.first + j]; xb.x[j] *= r * w[lane.second + j]; }
       if (lane.turns) rotate<false, kInterleaved>(xa, xb, cs);
     } else {
-      Eight ga = wide<T>(now.ga, lane.has_first), gb = wide<T>(now.gb, lane.has_second);
+      Eight ga = wide<T>(now.ga), gb = wide<T>(now.gb);
       if (lane.turns) rotate<true, kInterleaved>(ga, gb, cs);
       __builtin_amdgcn_sched_barrier(0);          // (the weights are not loaded before the angles are done with)
-      xa = wide<T>(again(now.xa), lane.has_first);
-      xb = wide<T>(again(now.xb), lane.has_second);
+      xa = wide<T>(again(now.xa));
+      xb = wide<T>(again(now.xb));
       float mean = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -214,7 +231,7 @@ __device__ __forceinline__ void Heads<T, kBack, kKeys, kInterleaved>::run(const 
         gb.x[j] *= w[lane.second + j];
         mean = fmaf(ga.x[j], xa.x[j], fmaf(gb.x[j], xb.x[j], mean));
       }
-      mean = sum_of_lanes(mean, p.lanes_log) / (float)a.dim;
+      mean = sum_of_lanes(mean, p.lanes_log) * p.share;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         xa.x[j] = r * (ga.x[j] - xa.x[j] * mean);

@@ -30,6 +30,8 @@ struct RotationArgs {
   RotationTiles tiles[2];                 // forward: [0]; of a gradient, those of queries and of keys
   int32_t blocks, q_blocks;               // workgroups; of a gradient, those that have queries: the first ones
   int32_t lanes_log;                      // lanes of a head: a power of two, each has 16 elements
+  bool whole;                             // all of them have them
+  float share;                            // 1 / dim
 };
 
 // Launchers: 0 or a hipError_t.
