@@ -31,11 +31,14 @@ void plan_score(ScoreArgs& p) {
     p.vectors = (int32_t)(ceil_div(pieces, p.lanes) * p.lanes);
     return;
   }
-  // With most likely tokens a workgroup holds its pieces in registers.  Longer rows are cut, and where there are few of them, so are rows that would take longer than the second
-  // launch that joins parts.  One part and several, us, bfloat16, 6 rows: of 18,065 without tokens 5.3 8.3, with 5 8.6 11.8, with 32 9.4 20.9; of 65,000 without any 7.2 8.1; of 110,000 10.1 9.1;
-  // of 157,065 13.3 9.1.  512 workgroups in all: 24 rows of 110,000 with 5, parts for 64, 128, ... 2048 workgroups, 16.6, 16.1, 15.5, 15.1, 15.2, 16.7; 93 of 500,000 without any 47, 47, 28, 20, 21, 21.
+  // With most likely tokens a workgroup holds its pieces in registers, up to 32 to a lane.  Longer rows are cut, into parts of up to 16 to a lane, and where there are few of them, so
+  // are rows without tokens that would take longer than the second launch that joins parts.  One part and several, us, bfloat16:
+  //   6 rows of 18,065 without tokens 5.3 8.3, with 5 8.6 11.8, with 32 9.4 20.9; of 65,000 without any 7.2 8.1; of 110,000 10.1 9.1; of 157,065 13.3 9.1
+  //   with 5, 85 rows of 33,000 10.7 14.7, 4000 60 85; 85 of 50,257 12.0 16.0, 4000 98.6 102.9; 85 of 65,000 13.7 16.3, 4000 115.2 114.7; 48 to a lane, 300 of 66,000 28.4 22.5
+  //   parts of 16 and 32 to a lane, 2000 rows of 128,001 with 5 114 126
+  // 512 workgroups in all: 24 rows of 110,000 with 5, parts for 64, 128, ... 2048 workgroups, 16.6, 16.1, 15.5, 15.1, 15.2, 16.7; 93 of 500,000 without any 47, 47, 28, 20, 21, 21.
   const int64_t one = kScoreThreads * (p.a.top ? kMostVectors : 48);
-  const int64_t least = p.a.top ? ceil_div(pieces, one) : ceil_div(pieces, kMostPieces), most = ceil_div(pieces, kScoreThreads);
+  const int64_t least = ceil_div(pieces, p.a.top ? kScoreThreads * kPartVectors : kMostPieces), most = ceil_div(pieces, kScoreThreads);
   const int64_t limit = p.a.top ? 64 : 128;       // (of lists that are joined)
   const int64_t wanted = pieces <= one ? 1 : std::max<int64_t>(least, std::min<int64_t>({most, limit, 512 / std::max<int64_t>(1, p.a.rows)}));
   const int64_t rounds = ceil_div(pieces, wanted * kScoreThreads);           // pieces per lane

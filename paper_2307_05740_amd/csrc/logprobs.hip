@@ -957,7 +957,9 @@ int forward(const ScoreArgs& p, hipStream_t s) {
   else if (n <= 2) score_kernel<T, 2><<<grid, block, 0, s>>>(p);
   else if (n <= 4) score_kernel<T, 4><<<grid, block, 0, s>>>(p);
   else if (n <= 8) score_kernel<T, 8><<<grid, block, 0, s>>>(p);
-  else score_kernel<T, 16><<<grid, block, 0, s>>>(p);
+  else if (n <= 16) score_kernel<T, 16><<<grid, block, 0, s>>>(p);
+  else if (n <= 24) score_kernel<T, 24><<<grid, block, 0, s>>>(p);
+  else score_kernel<T, 32><<<grid, block, 0, s>>>(p);
   if (p.parts > 1 && p.parts <= 8 && p.a.top == 0) score_join_rows_kernel<T><<<dim3((unsigned)((p.a.rows + kThreads - 1) / kThreads)), block, 0, s>>>(p);
   else if (p.parts > 1) score_join_kernel<T><<<dim3((unsigned)p.a.rows), block, 0, s>>>(p);
   return (int)hipGetLastError();

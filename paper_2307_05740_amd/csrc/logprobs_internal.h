@@ -10,7 +10,8 @@ namespace arrow {
 
 constexpr int kScoreThreads = 256;
 constexpr int kMostTop = 32;
-constexpr int kMostVectors = 16;       // pieces of 16 bytes of a row that a lane holds
+constexpr int kMostVectors = 32;       // pieces of 16 bytes of a whole row that a lane of a workgroup holds
+constexpr int kPartVectors = 16;       // and of a part of one
 constexpr int64_t kMostPieces = 1 << 26; // of a part of a row that is not held
 
 struct ScoreArgs {

@@ -89,7 +89,7 @@ def test_numbers_of_rows(torch, LogProbs, rows, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("pieces,rows", [(2, 70), (23, 9), (24, 9), (28, 33), (64, 70), (65, 70), (128, 9), (129, 70), (256, 3), (512, 5), (513, 5), (768, 4097), (769, 4097), (768, 30), (1024, 9), (1025, 9), (4096, 3), (4097, 3), (12288, 2), (12289, 2), (30000, 2)])
+@pytest.mark.parametrize("pieces,rows", [(2, 70), (23, 9), (24, 9), (28, 33), (64, 70), (65, 70), (128, 9), (129, 70), (256, 3), (512, 5), (513, 5), (768, 4097), (769, 4097), (768, 30), (1024, 9), (1025, 9), (4096, 3), (4097, 3), (6144, 3), (6145, 3), (8192, 3), (8193, 2), (12287, 2), (12288, 2), (12289, 2), (30000, 2)])
 def test_edges_of_the_kernels(torch, LogProbs, dtype, pieces, rows):
     """Rows of that many pieces of 16 bytes, less one element, and of one element more, with and without most likely tokens."""
     each = 128 // torch.finfo(getattr(torch, dtype)).bits
