@@ -498,9 +498,10 @@ __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_b
 int launch_pages_step(const PagesArgs& p, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (p.one) {
-    // Fewer threads wait less for each other: four new tokens and back, us a pass with 256 and 1024 threads, 4 sequences 8.2, 8.5, 32 8.1, 9.0, 256 10.7, 9.7.  Where all of 16,384
-    // pages go at once they take longer: 17 and 23 us more for 4 and 32.
-    if (p.a.batch <= 128 && p.rows <= 2048 && (int64_t)p.a.batch * p.a.columns <= 16384) pages_step_kernel<256><<<dim3(1), dim3(256), 0, s>>>(p);
+    // Fewer threads wait less for each other: four new tokens and back, us a pass with 256 and 1024 threads, 4 sequences 8.2, 8.5, 32 8.1, 9.0, 256 10.7, 9.7.  Where all pages of a table
+    // go they take longer: prompts and back, the way back with 256 and 1024, 4 sequences of 4000 pages 21 18, of 16,000 40 26, 64 of 4000 33 23, of 16,000 58 30.  So steps without new
+    // tokens have 1024.
+    if (p.rows > 0 && p.a.batch <= 128 && p.rows <= 2048 && (int64_t)p.a.batch * p.a.columns <= 16384) pages_step_kernel<256><<<dim3(1), dim3(256), 0, s>>>(p);
     else pages_step_kernel<1024><<<dim3(1), dim3(1024), 0, s>>>(p);
     return (int)hipGetLastError();
   }
