@@ -14,7 +14,7 @@
  *
  * Conventions are those of arrow.h: device pointers of the current device, work enqueued on `stream` (a hipStream_t) without waiting, nothing
  * allocated, an arrow_status code and the text in arrow_last_error().  Calls may be captured into a graph.  Scores, softmax statistics and all sums are held in 32
- * bits; probabilities are rounded to the operands' type, elements of the cache are exact in it.  No atomics: results are bitwise reproducible.
+ * bits; a probability goes into the product as two numbers of the operands' type, off by 2^-16 (float16: 2^-22) of itself, elements of the cache are exact in that type.  No atomics: results are bitwise reproducible.
  */
 #ifndef ARROW_PACKED_H
 #define ARROW_PACKED_H

@@ -3,7 +3,7 @@ result in a type of unit roundoff u (bfloat16 2^-8, float16 2^-11) that holds sc
 
 Bounds.  A score in 32 bits is off by at most e_s = (dim + 16) 2^-24 scale sum_d |q_d k_d|, and so is a probability, relative to itself, before
 it is rounded; sums of n terms are off by n 2^-24 of the terms' magnitudes.  With h = max e_s + (n + 64) 2^-24:
-  o:   (P |V|) (2 u + h): once for P, once for o;
+  o:   (P |V|) (2 u + h): once for P, once for o; where P is off by `p_unit` of itself instead, (P |V|) (p_unit + h) (1 + u) + u |o|;
   dv:  (P^T |dO|) (2 u + h);
   dS = P (dP - D) is rounded once; D = <dO, o> takes the rounded o, off by E_o (the bound above):
        E_S = P (|dP - D| (u + h) + <|dO|, E_o> + h (|dO| |V|^T + <|dO|, |o|>)),
@@ -31,7 +31,7 @@ def _clean(x):
     return torch.where(torch.isfinite(x), x, 0.0)
 
 
-def attention(q, k, v, window=0, sinks=0, scale=None, d_o=None, seen=None):
+def attention(q, k, v, window=0, sinks=0, scale=None, d_o=None, seen=None, p_unit=None):
     """One head: q (n, d), k and v (m, d), all of one type.  Results and bounds: dicts of o, lse and, with d_o, dq, dk, dv.
     What is not seen does not count, whatever it holds."""
     n, m, d = q.shape[0], k.shape[0], q.shape[1]
@@ -52,7 +52,8 @@ def attention(q, k, v, window=0, sinks=0, scale=None, d_o=None, seen=None):
     h = e_s + (m + 64) * 2.0 ** -24
     see = seen.double()
     # (a running maximum may be up to 2^8 below the final one; its terms are never below 1 at their largest)
-    b_o = (p @ v.abs()) * (2 * u + h) + tiny * (see @ v.abs()) + 2 * tiny
+    b_o = (p @ v.abs()) * (2 * u + h) if p_unit is None else (p @ v.abs()) * (p_unit + h) * (1 + u) + u * o.abs()
+    b_o = b_o + tiny * (see @ v.abs()) + 2 * tiny
     got = {"o": o, "lse": lse}
     bound = {"o": b_o, "lse": e_s[:, 0] + 2.0 ** -20 * (1 + torch.where(torch.isfinite(lse), lse.abs(), 0.0))}
     if d_o is not None:

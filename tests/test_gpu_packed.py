@@ -332,3 +332,20 @@ def test_offsets_beyond_32_bits(torch, Packed):
     same(torch, keys, oracle.packed(k))
     q = normal(torch, 3, "bfloat16", 1, 8, dim)
     check(torch, op, op.decode(q, pool, table, torch.tensor([1000], dtype=torch.int32, device="cuda")), q, [keys], [values])
+
+
+@pytest.mark.parametrize("dtype,p_unit", [("bfloat16", 2.0 ** -16), ("float16", 2.0 ** -22)])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 7)])
+def test_probabilities_are_not_rounded_to_the_type(torch, Packed, dtype, p_unit, dim, window, sinks):
+    """What they are off by goes with their own two numbers, not with one of the type: values that cancel each other show it."""
+    op = Packed(window, sinks)
+    pool, table, n, keys, values = filled(torch, op, dtype, [2, 3, 7, 16, 33, 70, 200, 1500], 16, 2, dim)
+    q = normal(torch, 3, dtype, 8, 6, dim)
+    for longest in (1500, None):
+        o = op.decode(q, pool, table, n, longest)
+        for b in range(8):
+            for h in range(6):
+                want, bound = attention_oracle.attention(q[b, h][None], keys[b][:, h // 3], values[b][:, h // 3], window, sinks, p_unit=p_unit)
+                off = (o[b, h].double() - want["o"][0]).abs()
+                assert bool((off <= bound["o"][0]).all()), (b, h, float((off / bound["o"][0].clamp(min=1e-300)).max()))
