@@ -43,7 +43,8 @@ typedef struct arrow_rotation_t {
 } arrow_rotation_t;
 
 /*
- * q_out, k_out: y of q and k.  wq, wk: DEVICE, dim weights each, or both NULL for ones.  q_out may be q where their steps are the same, and k_out k.
+ * q_out, k_out: y of q and k.  wq, wk: DEVICE, dim weights each, or both NULL for ones.  q_out may be q where their steps are the same, and k_out k; otherwise what is
+ * written overlaps nothing (views of one tensor with the same steps, such as queries and keys of one projection, lie apart where their elements do).
  * Errors: EINVAL, EHIP.
  */
 int arrow_rotation_forward(const arrow_rotation_t *a, const void *q, const void *k, const void *wq, const void *wk, void *q_out, void *k_out, void *stream);

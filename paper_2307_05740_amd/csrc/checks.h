@@ -4,9 +4,11 @@
 
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <initializer_list>
 
 #include "arrow.h"
 #include "arrow_attention.h"
@@ -51,6 +53,70 @@ namespace {
 [[maybe_unused]] bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+// Rows of `row` bytes at every sum of some steps (in bytes, not negative), each taken 0 .. count - 1 times.
+struct Rows {
+  struct Step { int64_t count, bytes; };
+  uintptr_t at;
+  int64_t row;
+  int n = 0;
+  bool repeat = false;                       // a step of nothing
+  Step steps[3];                             // the longest first
+  int64_t reach;                             // bytes from the first to the last one
+  Rows(const void* p, int64_t bytes, std::initializer_list<Step> all = {}) : at((uintptr_t)p), row(bytes) {
+    for (auto& s : all)
+      if (s.count > 1) {
+        if (s.bytes > 0) steps[n++] = s;
+        else repeat = true;
+      }
+    std::sort(steps, steps + n, [](const Step& a, const Step& b) { return a.bytes > b.bytes; });
+    reach = extent(0);
+  }
+  int64_t count(int i, int64_t step) const { return i < n && steps[i].bytes == step ? steps[i].count : 1; }
+  // the same of the steps from the i-th on (large ones are cut: what follows only compares)
+  int64_t extent(int i) const {
+    constexpr int64_t kMost = (int64_t)1 << 60;
+    int64_t all = std::min(row, kMost);
+    for (; i < n; ++i) {
+      int64_t x;
+      if (__builtin_mul_overflow(steps[i].count - 1, steps[i].bytes, &x)) x = kMost;
+      all += std::min(x, kMost);
+    }
+    return all;
+  }
+  // whether no two rows have a byte in common, where each step is as long as what the shorter ones reach over (others are taken to have)
+  bool distinct() const {
+    for (int i = 0; i < n; ++i)
+      if (steps[i].bytes < extent(i + 1)) return false;
+    return !repeat;
+  }
+};
+
+// Whether no row of `a`, of its steps from the i-th on, has a byte in common with one of `b`, from the j-th on, which begin `off` bytes behind them.  Exact where what is shorter than the
+// longest step does not reach beyond it in either, as in views of one tensor; others that reach into each other are taken to overlap.
+[[maybe_unused]] bool apart(const Rows& a, int i, const Rows& b, int j, int64_t off) {
+  if (off >= a.extent(i) || off <= -b.extent(j)) return true;
+  const int64_t step = std::max(i < a.n ? a.steps[i].bytes : 0, j < b.n ? b.steps[j].bytes : 0);
+  if (step == 0) return false;
+  const int64_t na = a.count(i, step), nb = b.count(j, step);
+  if (i < a.n && a.steps[i].bytes == step) ++i;
+  if (j < b.n && b.steps[j].bytes == step) ++j;
+  const int64_t ea = a.extent(i), eb = b.extent(j);
+  if (ea > step || eb > step) return false;
+  // of the distances off + t step between what is left of the two, those that are near enough
+  const int64_t rest = off % step, whole = off / step;      // (t + whole is -2 .. 2 then)
+  for (int64_t t = -2; t <= 2; ++t) {
+    const int64_t by = rest + t * step;
+    if (by >= ea || by <= -eb || t - whole < 1 - na || t - whole > nb - 1) continue;
+    if (!apart(a, i, b, j, by)) return false;
+  }
+  return true;
+}
+[[maybe_unused]] bool apart(const Rows& a, const Rows& b) {
+  if (!a.at || !b.at || a.row <= 0 || b.row <= 0) return true;
+  const int64_t off = (int64_t)(b.at - a.at);
+  return off >= a.reach || off <= -b.reach || apart(a, 0, b, 0, off);
 }
 
 }  // namespace

@@ -31,14 +31,20 @@ int check(const arrow_rotation_t* a) {
   return ARROW_OK;
 }
 
+Rows rows_of(const arrow_rotation_t* a, const void* at, const arrow_strides_t& s, int32_t heads) {
+  const int64_t size = size_of(a->dtype);
+  return {at, a->dim * size, {{a->batch, s.sequence * size}, {a->tokens, s.token * size}, {heads, s.head * size}}};
+}
+
 int check_heads(const arrow_rotation_t* a, const char* name, const void* at, const arrow_strides_t& s, int32_t heads, bool written) {
   if (int rc = check_pointer(name, at, 16)) return rc;
   const int step = 16 / size_of(a->dtype);
   if (s.sequence % step || s.token % step || s.head % step || s.sequence < 0 || s.token < 0 || s.head < 0)
     return refuse(ARROW_EINVAL, "%s: steps of %lld, %lld, %lld elements: multiples of %d, not negative", name, (long long)s.sequence, (long long)s.token,
                   (long long)s.head, step);
-  if (written && ((a->tokens > 1 && s.token < a->dim) || (heads > 1 && s.head < a->dim) || (a->batch > 1 && s.sequence < a->dim)))
-    return refuse(ARROW_EINVAL, "%s is written, and its rows overlap", name);
+  for (int64_t step : {s.sequence, s.token, s.head})
+    if (step > (int64_t)1 << 56) return refuse(ARROW_EINVAL, "%s: a step of %lld elements", name, (long long)step);
+  if (written && !rows_of(a, at, s, heads).distinct()) return refuse(ARROW_EINVAL, "%s is written, and its rows overlap", name);
   return ARROW_OK;
 }
 
@@ -50,6 +56,27 @@ int check_weights(const arrow_rotation_t* a, const char* name, const void* q, co
   if ((uintptr_t)q % size || (uintptr_t)k % size) return refuse(ARROW_EINVAL, "%s are not %d-byte aligned", name, size);
   return ARROW_OK;
 }
+
+// Operands of a call; `in_place`: of the one that it may lie on with the same steps (-1: none).
+struct Part {
+  const char* name;
+  Rows rows;
+  bool written;
+  int in_place;
+};
+template <size_t N>
+int check_apart(const Part (&all)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < N; ++j) {
+      const Part &m = all[i], &o = all[j];
+      if (i == j || !m.written || (o.written && j < i) || (m.in_place == (int)j && m.rows.at == o.rows.at)) continue;
+      if (!apart(m.rows, o.rows)) return refuse(ARROW_EINVAL, "%s is written, and overlaps %s", m.name, o.name);
+    }
+  return ARROW_OK;
+}
+Rows weights_of(const arrow_rotation_t* a, const void* at) { return {at, (int64_t)a->dim * size_of(a->weight_dtype)}; }
+Rows positions_of(const arrow_rotation_t* a) { return {a->positions, a->batch * (int64_t)a->tokens * a->position_bytes}; }
+Rows turns_of(const arrow_rotation_t* a) { return {a->rotary ? a->turns : nullptr, (int64_t)a->rotary * 4}; }
 
 bool follow(const arrow_rotation_t* a, const arrow_strides_t& s) { return a->batch <= 1 || s.sequence == a->tokens * s.token; }
 
@@ -118,6 +145,10 @@ int arrow_rotation_forward(const arrow_rotation_t* a, const void* q, const void*
   if (int rc = check_heads(a, "k_out", k_out, a->k_out, a->kv_heads, true)) return rc;
   if (q_out == k || k_out == q || q_out == k_out) return refuse(ARROW_EINVAL, "q_out is k or k_out, or k_out is q");
   if ((q_out == q && !same(a->q, a->q_out)) || (k_out == k && !same(a->k, a->k_out))) return refuse(ARROW_EINVAL, "in place, but with other steps");
+  const Part all[] = {{"q", rows_of(a, q, a->q, a->q_heads), false, -1}, {"k", rows_of(a, k, a->k, a->kv_heads), false, -1},
+                      {"q_out", rows_of(a, q_out, a->q_out, a->q_heads), true, 0}, {"k_out", rows_of(a, k_out, a->k_out, a->kv_heads), true, 1},
+                      {"a weight", weights_of(a, wq), false, -1}, {"a weight", weights_of(a, wk), false, -1}, {"positions", positions_of(a), false, -1}, {"turns", turns_of(a), false, -1}};
+  if (int rc = check_apart(all)) return rc;
   RotationArgs p = plan(a, false);
   p.q = q; p.k = k; p.wq = wq; p.wk = wk;
   p.yq = q_out; p.yk = k_out;
@@ -135,7 +166,7 @@ int arrow_rotation_backward(const arrow_rotation_t* a, const void* d_q_out, cons
   if (int rc = check(a)) return rc;
   if (int rc = check_weights(a, "weights", wq, wk)) return rc;
   if (int rc = check_weights(a, "gradients of weights", dwq, dwk)) return rc;
-  if (dwq && dwq == dwk) return refuse(ARROW_EINVAL, "dwq and dwk are the same");
+  if (dwq && !apart(weights_of(a, dwq), weights_of(a, dwk))) return refuse(ARROW_EINVAL, "dwq and dwk are the same, or overlap");
   RotationArgs p = plan(a, true);
   const bool some = (int64_t)a->batch * a->tokens > 0;
   if (some) {
@@ -147,6 +178,13 @@ int arrow_rotation_backward(const arrow_rotation_t* a, const void* d_q_out, cons
     if (dq == dk || dq == k || dk == q || dq == d_k_out || dk == d_q_out || dq == q || dk == k)
       return refuse(ARROW_EINVAL, "dq or dk is q, k, the other's gradient, or the other");
     if ((dq == d_q_out && !same(a->dq, a->q_out)) || (dk == d_k_out && !same(a->dk, a->k_out))) return refuse(ARROW_EINVAL, "in place, but with other steps");
+    const Part parts[] = {{"d_q_out", rows_of(a, d_q_out, a->q_out, a->q_heads), false, -1}, {"d_k_out", rows_of(a, d_k_out, a->k_out, a->kv_heads), false, -1},
+                          {"q", rows_of(a, q, a->q, a->q_heads), false, -1}, {"k", rows_of(a, k, a->k, a->kv_heads), false, -1},
+                          {"dq", rows_of(a, dq, a->dq, a->q_heads), true, 0}, {"dk", rows_of(a, dk, a->dk, a->kv_heads), true, 1},
+                          {"a weight", weights_of(a, wq), false, -1}, {"a weight", weights_of(a, wk), false, -1}, {"positions", positions_of(a), false, -1},
+                          {"turns", turns_of(a), false, -1}, {"dwq", weights_of(a, dwq), true, -1}, {"dwk", weights_of(a, dwk), true, -1},
+                          {"the workspace", {dwq ? ws : nullptr, (int64_t)arrow_rotation_workspace_bytes(a)}, true, -1}};
+    if (int rc = check_apart(parts)) return rc;
   }
   if (dwq)
     if (int rc = check_workspace(ws, ws_bytes, arrow_rotation_workspace_bytes(a))) return rc;

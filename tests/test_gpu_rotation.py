@@ -237,3 +237,30 @@ def test_offsets_beyond_32_bits(torch, Rotation):
         want, bound = oracle.rotation(q[part], None, p, op.turns, 256, dy=y[part])
         within(torch, "y", y[part], want["y"], bound["y"])
         within(torch, "dx", dq[part], want["dx"], bound["dx"])
+
+
+def test_views_of_one_tensor(torch, Rotation):
+    """What is written may lie between what is read, element by element of the outer dimensions: projections with all heads, heads in turn, results in one tensor."""
+    op, g = Rotation(64), torch.Generator().manual_seed(1)
+    wq, wk = (torch.rand(64, generator=g).cuda() + 0.5 for _ in range(2))
+    for batch, tokens in ((3, 5), (1, 7), (4, 1), (1, 1)):
+        x = torch.randn(batch, tokens, 6, 64, generator=g).bfloat16().cuda()
+        d = torch.randn(batch, tokens, 6, 64, generator=g).bfloat16().cuda()
+        for split in (lambda t: (t[:, :, :4], t[:, :, 4:]), lambda t: (t[:, :, ::2], t[:, :, 1::2]), lambda t: (t[:, :, 1:3], t[:, :, 5:])):
+            q, k = split(x)
+            want = op.forward(q.contiguous(), k.contiguous(), wq, wk)
+            grads = op.backward(split(d)[0].contiguous(), split(d)[1].contiguous(), q.contiguous(), k.contiguous(), wq, wk)
+            out, dx = torch.zeros_like(x), torch.zeros_like(x)
+            got = op.forward(q, k, wq, wk, q_out=split(out)[0], k_out=split(out)[1])
+            back = op.backward(*split(d), q, k, wq, wk, dq=split(dx)[0], dk=split(dx)[1])
+            assert all(torch.equal(a, b) for a, b in zip((*got, *back[:2]), (*want, *grads[:2])))
+            both, again = x.clone(), d.clone()
+            op.forward(*split(both), wq, wk, q_out=split(both)[0], k_out=split(both)[1])
+            op.backward(*split(again), q, k, wq, wk, dq=split(again)[0], dk=split(again)[1])
+            assert all(torch.equal(a, b) for a, b in zip((*split(both), *split(again)), (*want, *grads[:2])))
+            rest = [h for h in range(6) if not any(torch.equal(x[:, :, h], s[:, :, i]) for s in (q, k) for i in range(s.shape[2]))]
+            assert torch.equal(both[:, :, rest], x[:, :, rest]) and torch.equal(again[:, :, rest], d[:, :, rest])
+            # queries and their results in the two halves of every row of one tensor
+            pair = torch.cat([q, torch.zeros_like(q)], 2)
+            op.forward(pair[:, :, :q.shape[2]], k, wq, wk, q_out=pair[:, :, q.shape[2]:])
+            assert torch.equal(pair[:, :, q.shape[2]:], want[0]) and torch.equal(pair[:, :, :q.shape[2]], q)

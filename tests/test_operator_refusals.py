@@ -280,3 +280,33 @@ def test_classes_refuse_before_any_call():
     a = ArrowPackedAttention(device="cpu")
     with pytest.raises(ValueError, match="cpu"):
         a.read(a.pool(2, 16, 1, 64), t, 64, torch.bfloat16)
+
+
+# ---- what is written lies apart from all else ----
+def steps(*s):
+    return binding.arrow_strides_t(*s)
+
+
+@pytest.mark.parametrize("change,at", [
+    ({"q_out": steps(2048, 64, 64)}, {}),                                     # (token t, head h + 1) is (token t + 1, head h)
+    ({"k_out": steps(64, 64, 512)}, {}), ({"q_out": steps(256, 256, 64)}, {}), ({"q_out": steps(2048, 128, 64)}, {}),
+    ({}, {"qo": SOME + 512}), ({}, {"qo": 2 * SOME + 256}), ({}, {"ko": SOME + 1024}), ({}, {"ko": 2 * SOME - 256}), ({}, {"ko": 3 * SOME + 128}), ({}, {"qo": 4 * SOME - 128}),
+    ({}, {"qo": 5 * SOME - 1024}), ({"positions": 8 * SOME, "position_bytes": 8}, {"qo": 8 * SOME}), ({"turns": 8 * SOME}, {"ko": 8 * SOME + 128}),
+    # views of one tensor: queries from head 0 on, keys from 4 on; a head too early
+    ({name: steps(8 * 512, 512, 64) for name in ("q", "k", "q_out", "k_out")}, {"q": SOME, "qo": SOME, "k": SOME + 3 * 128, "ko": SOME + 3 * 128}),
+    ({name: steps(8 * 512, 512, 64) for name in ("q", "k", "q_out", "k_out")}, {"q": SOME, "qo": SOME, "k": SOME + 4 * 128 + 512, "ko": SOME + 7 * 128}),
+])
+def test_rotation_refuses_what_overlaps(L, change, at):
+    p = dict(dict(q=SOME, k=2 * SOME, wq=5 * SOME, wk=6 * SOME, qo=3 * SOME, ko=4 * SOME), **at)
+    refused(L.arrow_rotation_forward(ctypes.byref(rotation(**change)), *p.values(), 0), "overlap")
+
+
+@pytest.mark.parametrize("change,at", [
+    ({"dq": steps(2048, 64, 64)}, {}), ({"dk": steps(64, 64, 512)}, {}), ({}, {"dq": SOME + 512}), ({}, {"dq": 2 * SOME - 16}), ({}, {"dk": 2 * SOME + 256}), ({}, {"dq": 3 * SOME + 256}),
+    ({}, {"dk": 4 * SOME + 256}), ({}, {"dk": 7 * SOME + 256}), ({}, {"dwq": 7 * SOME + 64}), ({}, {"dwk": 5 * SOME + 64}), ({}, {"dwq": 10 * SOME + 128}), ({}, {"dwk": SOME}),
+    ({}, {"ws": 4 * SOME}), ({}, {"dwq": 16 * SOME + 256}), ({"positions": 8 * SOME, "position_bytes": 4}, {}),
+])
+def test_rotation_gradients_refuse_what_overlaps(L, change, at):
+    a = rotation(**change)
+    p = dict(dict(gq=SOME, gk=2 * SOME, q=3 * SOME, k=4 * SOME, wq=5 * SOME, wk=6 * SOME, dq=7 * SOME, dk=8 * SOME, dwq=9 * SOME, dwk=10 * SOME, ws=16 * SOME), **at)
+    refused(L.arrow_rotation_backward(ctypes.byref(a), *p.values(), L.arrow_rotation_workspace_bytes(ctypes.byref(a)), 0), "overlap")
