@@ -46,7 +46,8 @@ typedef struct arrow_packed_t {
 
 /*
  * Write `tokens` rows, k and v: tokens x kv_heads x dim by their strides (sequence unused), to the places slots[i] = page * T + token (DEVICE, int64), and read them from there.
- * Slots outside the pool are places that are not there: nothing is written for them, and zeros are read.  Two rows written to one place leave parts of both.
+ * Slots outside the pool are places that are not there: nothing is written for them, and zeros are read.  Two rows written to one place leave parts of both.  What is written, here
+ * and below, overlaps neither itself nor another operand.
  * Errors: EINVAL, EHIP.
  */
 int arrow_packed_append(const arrow_packed_t *c, int64_t tokens, const void *k, const void *v, arrow_strides_t ks, arrow_strides_t vs, const int64_t *slots,

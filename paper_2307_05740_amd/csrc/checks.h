@@ -8,7 +8,6 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
-#include <initializer_list>
 
 #include "arrow.h"
 #include "arrow_attention.h"
@@ -57,43 +56,52 @@ namespace {
 
 // Rows of `row` bytes at every sum of some steps (in bytes, not negative), each taken 0 .. count - 1 times.
 struct Rows {
+  static constexpr int64_t kMost = (int64_t)1 << 60;         // (larger reaches are cut: they are only compared)
   struct Step { int64_t count, bytes; };
   uintptr_t at;
-  int64_t row;
+  int64_t row, reach;                        // reach: bytes from the first to the last one
   int n = 0;
   bool repeat = false;                       // a step of nothing
-  Step steps[3];                             // the longest first
-  int64_t reach;                             // bytes from the first to the last one
-  Rows(const void* p, int64_t bytes, std::initializer_list<Step> all = {}) : at((uintptr_t)p), row(bytes) {
-    for (auto& s : all)
-      if (s.count > 1) {
-        if (s.bytes > 0) steps[n++] = s;
-        else repeat = true;
-      }
-    std::sort(steps, steps + n, [](const Step& a, const Step& b) { return a.bytes > b.bytes; });
-    reach = extent(0);
+  Step steps[3];
+  Rows(const void* p, int64_t bytes) : at((uintptr_t)p), row(std::min(bytes, kMost)), reach(row) {}
+  Rows(const void* p, int64_t bytes, Step a, Step b, Step c = {1, 0}) : Rows(p, bytes) {
+    add(a);
+    add(b);
+    add(c);
   }
-  int64_t count(int i, int64_t step) const { return i < n && steps[i].bytes == step ? steps[i].count : 1; }
-  // the same of the steps from the i-th on (large ones are cut: what follows only compares)
+  void add(const Step& s) {
+    if (s.count <= 1) return;
+    if (s.bytes <= 0) { repeat = true; return; }
+    reach += across(s);
+    steps[n++] = s;
+  }
+  static int64_t across(const Step& s) {
+    int64_t x;
+    return __builtin_mul_overflow(s.count - 1, s.bytes, &x) ? kMost : std::min(x, kMost);
+  }
+  // the same with the longest step first
+  Rows sorted() const {
+    Rows r = *this;
+    std::sort(r.steps, r.steps + n, [](const Step& a, const Step& b) { return a.bytes > b.bytes; });
+    return r;
+  }
+  // (sorted:) bytes from the first to the last one of the steps from the i-th on
   int64_t extent(int i) const {
-    constexpr int64_t kMost = (int64_t)1 << 60;
-    int64_t all = std::min(row, kMost);
-    for (; i < n; ++i) {
-      int64_t x;
-      if (__builtin_mul_overflow(steps[i].count - 1, steps[i].bytes, &x)) x = kMost;
-      all += std::min(x, kMost);
-    }
+    int64_t all = row;
+    for (; i < n; ++i) all += across(steps[i]);
     return all;
   }
+  int64_t count(int i, int64_t step) const { return i < n && steps[i].bytes == step ? steps[i].count : 1; }
   // whether no two rows have a byte in common, where each step is as long as what the shorter ones reach over (others are taken to have)
   bool distinct() const {
+    const Rows r = sorted();
     for (int i = 0; i < n; ++i)
-      if (steps[i].bytes < extent(i + 1)) return false;
+      if (r.steps[i].bytes < r.extent(i + 1)) return false;
     return !repeat;
   }
 };
 
-// Whether no row of `a`, of its steps from the i-th on, has a byte in common with one of `b`, from the j-th on, which begin `off` bytes behind them.  Exact where what is shorter than the
+// Whether no row of `a` (both are sorted), of its steps from the i-th on, has a byte in common with one of `b`, from the j-th on, which begin `off` bytes behind them.  Exact where what is shorter than the
 // longest step does not reach beyond it in either, as in views of one tensor; others that reach into each other are taken to overlap.
 [[maybe_unused]] bool apart(const Rows& a, int i, const Rows& b, int j, int64_t off) {
   if (off >= a.extent(i) || off <= -b.extent(j)) return true;
@@ -116,7 +124,25 @@ struct Rows {
 [[maybe_unused]] bool apart(const Rows& a, const Rows& b) {
   if (!a.at || !b.at || a.row <= 0 || b.row <= 0) return true;
   const int64_t off = (int64_t)(b.at - a.at);
-  return off >= a.reach || off <= -b.reach || apart(a, 0, b, 0, off);
+  return off >= a.reach || off <= -b.reach || apart(a.sorted(), 0, b.sorted(), 0, off);
+}
+
+// Operands of a call; `in_place`: of the one that it may lie on with the same steps (-1: none).
+struct Part {
+  const char* name;
+  Rows rows;
+  bool written;
+  int in_place;
+};
+template <size_t N>
+[[maybe_unused]] int check_apart(const Part (&all)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < N; ++j) {
+      const Part &m = all[i], &o = all[j];
+      if (i == j || !m.written || (o.written && j < i) || (m.in_place == (int)j && m.rows.at == o.rows.at)) continue;
+      if (!apart(m.rows, o.rows)) return refuse(ARROW_EINVAL, "%s is written, and overlaps %s", m.name, o.name);
+    }
+  return ARROW_OK;
 }
 
 }  // namespace

@@ -11,6 +11,12 @@ using namespace arrow;
 
 constexpr int32_t kMostTokens = 1 << 26;    // of a sequence
 
+constexpr int64_t kMostStep = (int64_t)1 << 56;
+
+Rows pool_of(const arrow_packed_t* c, const void* pool) {
+  return {c->pages ? pool : nullptr, (int64_t)c->page * (c->dim + c->dim / 16), {c->pages, c->page_step}, {c->kv_heads, c->head_step}};
+}
+
 int check_pool(const arrow_packed_t* c, const void* pool) {
   if (!c) return refuse(ARROW_EINVAL, "NULL arguments");
   if (c->dtype != ARROW_BF16 && c->dtype != ARROW_F16) return refuse(ARROW_EINVAL, "dtype %d: a cache in 4 bits takes ARROW_BF16 and ARROW_F16", c->dtype);
@@ -21,18 +27,19 @@ int check_pool(const arrow_packed_t* c, const void* pool) {
   if (c->pages == 0) return ARROW_OK;
   if (int rc = check_pointer("pool", pool, 16)) return rc;
   const int64_t block = (int64_t)c->page * (c->dim + c->dim / 16);
-  if (c->page_step % 16 || c->head_step % 16 || c->page_step < 0 || c->head_step < 0 || (c->pages > 1 && c->page_step < block) ||
-      (c->kv_heads > 1 && c->head_step < block))
-    return refuse(ARROW_EINVAL, "pool: blocks %lld and %lld bytes apart, multiples of 16 from %lld expected", (long long)c->page_step, (long long)c->head_step,
-                  (long long)block);
+  if (c->page_step % 16 || c->head_step % 16 || c->page_step < 0 || c->head_step < 0 || c->page_step > kMostStep || c->head_step > kMostStep || !pool_of(c, pool).distinct())
+    return refuse(ARROW_EINVAL, "pool: blocks %lld and %lld bytes apart, multiples of 16 from %lld expected that do not overlap", (long long)c->page_step,
+                  (long long)c->head_step, (long long)block);
   return ARROW_OK;
 }
 
+Rows rows_of(const arrow_packed_t* c, const void* at, int64_t row, int64_t head, int64_t rows, int32_t heads) { return {at, c->dim * 2, {rows, row * 2}, {heads, head * 2}}; }
+
 int check_rows(const arrow_packed_t* c, const char* name, const void* at, int64_t row, int64_t head, int64_t rows, int32_t heads, bool written) {
   if (int rc = check_pointer(name, at, 16)) return rc;
-  if (row % 8 || head % 8 || row < 0 || head < 0)
+  if (row % 8 || head % 8 || row < 0 || head < 0 || row > kMostStep || head > kMostStep)
     return refuse(ARROW_EINVAL, "%s: steps of %lld and %lld elements are not multiples of 8", name, (long long)row, (long long)head);
-  if (written && ((rows > 1 && row < c->dim) || (heads > 1 && head < c->dim))) return refuse(ARROW_EINVAL, "%s is written, and its rows overlap", name);
+  if (written && !rows_of(c, at, row, head, rows, heads).distinct()) return refuse(ARROW_EINVAL, "%s is written, and its rows overlap", name);
   return ARROW_OK;
 }
 
@@ -101,7 +108,7 @@ PackedArgs plan_decode(const arrow_packed_t* c) {
   return p;
 }
 
-Operand rows_of(const void* at, const arrow_strides_t& s) { return {at, s.sequence, s.token, s.head}; }
+Operand operand(const void* at, const arrow_strides_t& s) { return {at, s.sequence, s.token, s.head}; }
 
 }  // namespace
 
@@ -116,8 +123,11 @@ int arrow_packed_append(const arrow_packed_t* c, int64_t tokens, const void* k, 
   if (int rc = check_rows(c, "v", v, vs.token, vs.head, tokens, c->kv_heads, false)) return rc;
   if (pool && (k == pool || v == pool)) return refuse(ARROW_EINVAL, "k or v is the pool");
   if (c->pages == 0) return ARROW_OK;
+  const Part all[] = {{"the pool", pool_of(c, pool), true, -1}, {"k", rows_of(c, k, ks.token, ks.head, tokens, c->kv_heads), false, -1},
+                      {"v", rows_of(c, v, vs.token, vs.head, tokens, c->kv_heads), false, -1}, {"slots", {slots, tokens * 8}, false, -1}};
+  if (int rc = check_apart(all)) return rc;
   PackedArgs p = plan(c);
-  p.k = rows_of(k, ks); p.v = rows_of(v, vs);
+  p.k = operand(k, ks); p.v = operand(v, vs);
   p.pool = pool; p.slots = slots; p.tokens = tokens;
   return launched("packed append", launch_packed_append(p, stream));
 }
@@ -130,8 +140,11 @@ int arrow_packed_read(const arrow_packed_t* c, int64_t tokens, const int64_t* sl
   if (int rc = check_rows(c, "k", k, ks.token, ks.head, tokens, c->kv_heads, true)) return rc;
   if (int rc = check_rows(c, "v", v, vs.token, vs.head, tokens, c->kv_heads, true)) return rc;
   if (k == v || (pool && (k == pool || v == pool))) return refuse(ARROW_EINVAL, "k or v is the other or the pool");
+  const Part all[] = {{"the pool", pool_of(c, pool), false, -1}, {"k", rows_of(c, k, ks.token, ks.head, tokens, c->kv_heads), true, -1},
+                      {"v", rows_of(c, v, vs.token, vs.head, tokens, c->kv_heads), true, -1}, {"slots", {slots, tokens * 8}, false, -1}};
+  if (int rc = check_apart(all)) return rc;
   PackedArgs p = plan(c);
-  p.k = rows_of(k, ks); p.v = rows_of(v, vs);
+  p.k = operand(k, ks); p.v = operand(v, vs);
   p.pool = const_cast<void*>(pool); p.slots = slots; p.tokens = tokens;
   return launched("packed read", launch_packed_read(p, stream));
 }
@@ -156,9 +169,15 @@ int arrow_packed_decode(const arrow_packed_t* c, const void* q, arrow_strides_t 
   }
   if (o == q || o == k || o == v || (pool && o == pool)) return refuse(ARROW_EINVAL, "o is one of the inputs");
   PackedArgs p = plan_decode(c);
-  if (int rc = check_workspace(ws, ws_bytes, arrow_packed_decode_workspace_bytes(c))) return rc;
-  p.q = rows_of(q, qs); p.o = rows_of(o, os);
-  p.k = rows_of(k, ks); p.v = rows_of(v, vs);
+  const size_t need = arrow_packed_decode_workspace_bytes(c);
+  if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
+  const Part all[] = {{"o", rows_of(c, o, os.sequence, os.head, c->batch, c->q_heads), true, -1}, {"the pool", pool_of(c, pool), k != nullptr, -1},
+                      {"the workspace", {need ? ws : nullptr, (int64_t)need}, true, -1}, {"q", rows_of(c, q, qs.sequence, qs.head, c->batch, c->q_heads), false, -1},
+                      {"k", rows_of(c, k, ks.sequence, ks.head, c->batch, c->kv_heads), false, -1}, {"v", rows_of(c, v, vs.sequence, vs.head, c->batch, c->kv_heads), false, -1},
+                      {"table", {c->table, (int64_t)c->batch * c->columns * 4}, false, -1}, {"lengths", {c->lengths, (int64_t)c->batch * 4}, false, -1}};
+  if (int rc = check_apart(all)) return rc;
+  p.q = operand(q, qs); p.o = operand(o, os);
+  p.k = operand(k, ks); p.v = operand(v, vs);
   p.k.token = ks.sequence; p.v.token = vs.sequence;      // (a token of each sequence)
   p.pool = pool;
   p.tokens = c->batch;

@@ -33,7 +33,7 @@ int check(const arrow_rotation_t* a) {
 
 Rows rows_of(const arrow_rotation_t* a, const void* at, const arrow_strides_t& s, int32_t heads) {
   const int64_t size = size_of(a->dtype);
-  return {at, a->dim * size, {{a->batch, s.sequence * size}, {a->tokens, s.token * size}, {heads, s.head * size}}};
+  return {at, a->dim * size, {a->batch, s.sequence * size}, {a->tokens, s.token * size}, {heads, s.head * size}};
 }
 
 int check_heads(const arrow_rotation_t* a, const char* name, const void* at, const arrow_strides_t& s, int32_t heads, bool written) {
@@ -57,23 +57,6 @@ int check_weights(const arrow_rotation_t* a, const char* name, const void* q, co
   return ARROW_OK;
 }
 
-// Operands of a call; `in_place`: of the one that it may lie on with the same steps (-1: none).
-struct Part {
-  const char* name;
-  Rows rows;
-  bool written;
-  int in_place;
-};
-template <size_t N>
-int check_apart(const Part (&all)[N]) {
-  for (size_t i = 0; i < N; ++i)
-    for (size_t j = 0; j < N; ++j) {
-      const Part &m = all[i], &o = all[j];
-      if (i == j || !m.written || (o.written && j < i) || (m.in_place == (int)j && m.rows.at == o.rows.at)) continue;
-      if (!apart(m.rows, o.rows)) return refuse(ARROW_EINVAL, "%s is written, and overlaps %s", m.name, o.name);
-    }
-  return ARROW_OK;
-}
 Rows weights_of(const arrow_rotation_t* a, const void* at) { return {at, (int64_t)a->dim * size_of(a->weight_dtype)}; }
 Rows positions_of(const arrow_rotation_t* a) { return {a->positions, a->batch * (int64_t)a->tokens * a->position_bytes}; }
 Rows turns_of(const arrow_rotation_t* a) { return {a->rotary ? a->turns : nullptr, (int64_t)a->rotary * 4}; }

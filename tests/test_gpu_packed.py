@@ -349,3 +349,20 @@ def test_probabilities_are_not_rounded_to_the_type(torch, Packed, dtype, p_unit,
                 want, bound = attention_oracle.attention(q[b, h][None], keys[b][:, h // 3], values[b][:, h // 3], window, sinks, p_unit=p_unit)
                 off = (o[b, h].double() - want["o"][0]).abs()
                 assert bool((off <= bound["o"][0]).all()), (b, h, float((off / bound["o"][0].clamp(min=1e-300)).max()))
+
+
+def test_views_of_one_tensor(torch, Packed):
+    """Queries, the new token's key and value, and results as views of one tensor; keys and values read into one."""
+    op, page = Packed(), 16
+    pool, table, n, keys, values = filled(torch, op, "bfloat16", [40, 1, 700], page, 2, 64)
+    x = normal(torch, 3, "bfloat16", 3, 4 + 2 + 2 + 4, 64)
+    q, k, v, o = x.split((4, 2, 2, 4), 1)
+    got = op.decode(q, pool, table, n, k=k, v=v, o=o)
+    assert got.data_ptr() == o.data_ptr()
+    want = op.decode(q.contiguous(), pool, table, n)
+    assert torch.equal(o, want)
+    slots = torch.tensor([int(table[2, 3]) * page + 5, int(table[0, 0]) * page, -1], device="cuda")
+    both = torch.full((3, 5, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    op.read(pool, slots, 64, torch.bfloat16, both[:, ::2][:, :2], both[:, 1::2])
+    k, v = op.read(pool, slots, 64, torch.bfloat16)
+    assert torch.equal(both[:, ::2][:, :2], k) and torch.equal(both[:, 1::2], v) and bool((both[:, 4] == 7).all())

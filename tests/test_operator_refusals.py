@@ -310,3 +310,35 @@ def test_rotation_gradients_refuse_what_overlaps(L, change, at):
     a = rotation(**change)
     p = dict(dict(gq=SOME, gk=2 * SOME, q=3 * SOME, k=4 * SOME, wq=5 * SOME, wk=6 * SOME, dq=7 * SOME, dk=8 * SOME, dwq=9 * SOME, dwk=10 * SOME, ws=16 * SOME), **at)
     refused(L.arrow_rotation_backward(ctypes.byref(a), *p.values(), L.arrow_rotation_workspace_bytes(ctypes.byref(a)), 0), "overlap")
+
+
+TALL = steps(256, 256, 64)           # rows of four heads
+
+
+@pytest.mark.parametrize("change,at", [
+    ({"page_step": 1088, "head_step": 1088}, {}), ({"page_step": 1088, "head_step": 2176}, {}), ({}, {"ks": steps(0, 64, 64)}), ({}, {"vs": steps(0, 64, 128)}),
+    ({}, {"k": 2 * SOME + 128}), ({}, {"k": 4 * SOME + 1088}), ({}, {"v": 4 * SOME - 128}), ({}, {"slots": SOME + 8}), ({}, {"ks": TALL, "vs": TALL, "v": SOME + 128}),
+    ({"head_step": 4096, "page_step": 8192}, {"k": 4 * SOME + 4096 + 1024}),
+])
+def test_packed_read_refuses_what_overlaps(L, change, at):
+    p = dict(dict(slots=3 * SOME, pool=4 * SOME, k=SOME, v=2 * SOME, ks=ROWS, vs=ROWS), **at)
+    refused(L.arrow_packed_read(ctypes.byref(packed(**change)), 3, *p.values(), 0), "pool: blocks" if "pool" not in at and change.get("page_step") == 1088 else "overlap")
+
+
+@pytest.mark.parametrize("change,at", [({}, {"k": 4 * SOME + 1088}), ({}, {"v": 4 * SOME - 128}), ({}, {"slots": 4 * SOME + 16}), ({}, {"slots": 4 * SOME - 16})])
+def test_packed_append_refuses_what_overlaps(L, change, at):
+    p = dict(dict(k=SOME, v=2 * SOME, ks=ROWS, vs=ROWS, slots=3 * SOME, pool=4 * SOME), **at)
+    refused(L.arrow_packed_append(ctypes.byref(packed(**change)), 3, *p.values(), 0), "overlap")
+
+
+@pytest.mark.parametrize("change,at", [
+    ({}, {"os": steps(64, 0, 64)}), ({}, {"os": steps(128, 0, 64)}), ({}, {"o": SOME + 512}), ({}, {"o": SOME - 512}), ({}, {"o": 2 * SOME + 256}), ({}, {"o": 3 * SOME - 256}),
+    ({}, {"o": 4 * SOME + 1088}), ({}, {"k": 4 * SOME + 1088}), ({}, {"v": 4 * SOME + 16}), ({"table": 5 * SOME + 4}, {}), ({"lengths": 4 * SOME + 4}, {}),
+    ({"columns": 100, "max_len": 1600, "batch": 1}, {"ws": 4 * SOME}), ({"columns": 100, "max_len": 1600, "batch": 1}, {"ws": SOME}),
+])
+def test_packed_decode_refuses_what_overlaps(L, change, at):
+    c = packed(**dict({"table": 6 * SOME, "lengths": 7 * SOME}, **change))
+    st = steps(256, 0, 64)
+    p = dict(dict(q=SOME, qs=st, k=2 * SOME, v=3 * SOME, ks=ROWS, vs=ROWS, pool=4 * SOME, o=5 * SOME, os=st, ws=16 * SOME), **at)
+    assert "ws" not in at or L.arrow_packed_decode_workspace_bytes(ctypes.byref(c)) > 0
+    refused(L.arrow_packed_decode(ctypes.byref(c), *p.values(), 1 << 30, 0), "overlap")
