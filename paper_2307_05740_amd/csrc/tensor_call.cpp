@@ -657,14 +657,6 @@ bool describe(arrow_logprobs_t& a, const at::Tensor* logits, const at::Tensor* t
   return a.stride != 0;
 }
 
-// A contiguous tensor in the memory of another one of the same type.
-at::Tensor part_of(const at::Tensor& all, int64_t offset, at::IntArrayRef sizes) {
-  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
-  t.unsafeGetTensorImpl()->set_storage_offset(offset);
-  t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
-  return t;
-}
-
 // logprobs_forward(function, of the workspace's size, device, scale, logits, targets, top): logp, entropy, lse, stats and, with top, top_logp, top_ids
 PyObject* logprobs_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   int64_t x[3], top;
@@ -678,10 +670,8 @@ PyObject* logprobs_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) 
     arrow_logprobs_t a{};
     if (!tensor.ok || !describe(a, logits, targets, scale) || top < 0 || top > 32 || top > a.vocabulary) return 0;
     a.top = (int32_t)top;
-    // (a few numbers of each row, in one piece of memory)
-    const at::Tensor all = made({std::max<int64_t>(1, 5 * a.rows)}, *logits, at::kFloat);
-    out[3] = part_of(all, 0, with(targets->sizes(), 2));
-    for (int i = 0; i < 3; ++i) out[i] = part_of(all, (2 + i) * a.rows, targets->sizes());
+    for (int i = 0; i < 3; ++i) out[i] = made(targets->sizes(), *logits, at::kFloat);
+    out[3] = made(with(targets->sizes(), 2), *logits, at::kFloat);
     if (top) {
       out[4] = made(with(targets->sizes(), top), *logits, at::kFloat);
       out[5] = made(with(targets->sizes(), top), *logits, at::kLong);
