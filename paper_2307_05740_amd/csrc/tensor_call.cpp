@@ -9,7 +9,11 @@
 //
 // The calls on sequences (attention, embedding) return their results instead, the error code, or None for the general way.
 #include <Python.h>
+#include <ATen/Context.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <ATen/ops/empty.h>
+#include <ATen/record_function.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -141,8 +145,16 @@ struct Tensors {
 int half_type(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? ARROW_BF16 : t.scalar_type() == at::kHalf ? ARROW_F16 : -1; }
 bool rows_whole(const at::Tensor& t) { return t.size(-1) <= 1 || t.stride(-1) == 1; }
 bool like(const at::Tensor& t, const at::Tensor& other) { return t.scalar_type() == other.scalar_type() && t.sizes() == other.sizes() && rows_whole(t); }
-// (without torch's dispatcher: 0.47 us instead of 0.70, which a call takes up to seven times)
-at::Tensor made(at::IntArrayRef sizes, const at::Tensor& on, at::ScalarType type) { return at::detail::empty_cuda(sizes, type, on.device(), std::nullopt); }
+// Whether someone looks at allocations, or wants them filled: dispatch modes and the like, profilers, deterministic algorithms.
+bool watched() {
+  if (!(c10::impl::tls_local_dispatch_key_set().included_ - c10::default_included_set).empty() || at::hasCallbacks()) return true;
+  const at::Context& context = at::globalContext();
+  return context.deterministicAlgorithms() && context.deterministicFillUninitializedMemory();
+}
+// (without torch's dispatcher where nobody does: 0.47 us instead of 0.70, which a call takes up to seven times)
+at::Tensor made(at::IntArrayRef sizes, const at::Tensor& on, at::ScalarType type) {
+  return watched() ? at::empty(sizes, on.options().dtype(type)) : at::detail::empty_cuda(sizes, type, on.device(), std::nullopt);
+}
 void* data(const at::Tensor& t) { return t.data_ptr(); }
 
 // Steps between sequences, tokens and heads of (sequences, tokens, heads, dim) or (tokens, heads, dim); one that is never taken counts as none.

@@ -1,4 +1,4 @@
-"""What calls on tensors return stands by itself."""
+"""What calls on tensors have to do with torch beside the tensors: who watches allocations sees theirs, and what torch fills it fills for them; what they return stands by itself."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +59,46 @@ def test_results_stand_by_themselves(torch):
         assert len(out) == made, name
         assert len({t.untyped_storage().data_ptr() for t in out}) == made, name
         assert all(t.storage_offset() == 0 and t.untyped_storage().nbytes() == t.numel() * t.element_size() for t in out), name
+
+
+def test_who_watches_allocations_sees_them(torch):
+    """Dispatch modes and profilers, for every call."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Seen(TorchDispatchMode):
+        def __init__(self):
+            super().__init__()
+            self.empties = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            self.empties += func is torch.ops.aten.empty.memory_format
+            return func(*args, **(kwargs or {}))
+
+    for name, (call, made) in calls(torch).items():
+        call()
+        with Seen() as seen:
+            call()
+        assert seen.empties >= made, (name, seen.empties)
+        with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CPU]) as prof:
+            call()
+        assert sum(e.count for e in prof.key_averages() if e.key == "aten::empty") >= made, name
+
+
+def test_deterministic_algorithms_fill_what_is_not_written(torch):
+    """Results of tokens that no sequence has are left as they are: NaN where torch fills new memory."""
+    from paper_2307_05740_amd.attention import ArrowAttention
+    op, x = ArrowAttention(), torch.ones(64, 2, 64, dtype=torch.bfloat16, device="cuda")
+    offsets = torch.tensor([0, 16, 40], dtype=torch.int32, device="cuda")
+    want, _ = op.forward(x, x, x, q_offsets=offsets, k_offsets=offsets)
+    for _ in range(4):
+        torch.full_like(x, 5.0)                    # (memory that the next results have is not NaN by itself)
+        torch.full((2, 64), 5.0, device="cuda")
+    before = torch.are_deterministic_algorithms_enabled()
+    torch.use_deterministic_algorithms(True)
+    try:
+        o, lse = op.forward(x, x, x, q_offsets=offsets, k_offsets=offsets)
+        grads = op.backward(x, x, x, x, o.nan_to_num(), lse.nan_to_num(), q_offsets=offsets, k_offsets=offsets)
+    finally:
+        torch.use_deterministic_algorithms(before)
+    assert torch.equal(o[:40], want[:40]) and bool(o[40:].isnan().all()) and bool(lse[:, 40:].isnan().all())
+    assert all(bool(g[:40].isfinite().all()) and bool(g[40:].isnan().all()) for g in grads)
