@@ -3,7 +3,8 @@ rounding may do to a result in a type of unit roundoff u that holds everything e
 
 Rotation.  The mean of `dim` squares and its root are off by less than h = (dim + 12) e, relative; an angle by a = 2 pi (2^-25 + 2^-51 |turns|) + 8 e, from the
 product in 64 bits, its rounding to 32 and the functions of it.  A rotated pair is off by (|x| + |y|) (h + a).
-Log probabilities.  With d = scale (x - max): exp d is off by (4 |d| + 8) e, relative, and sums of n terms, added up in some 300 steps, by 512 e more.
+Log probabilities.  With d = scale (x - max): exp d is off by (4 |d| + 8) e, relative, and sums, which a lane adds up in at most 256 steps and their sums in 128,
+and some 60 more join, by 512 e more.
 """
 from __future__ import annotations
 

@@ -38,7 +38,7 @@ void plan_score(ScoreArgs& p) {
   //   parts of 16 and 32 to a lane, 2000 rows of 128,001 with 5 114 126
   // 512 workgroups in all: 24 rows of 110,000 with 5, parts for 64, 128, ... 2048 workgroups, 16.6, 16.1, 15.5, 15.1, 15.2, 16.7; 93 of 500,000 without any 47, 47, 28, 20, 21, 21.
   const int64_t one = kScoreThreads * (p.a.top ? kMostVectors : 48);
-  const int64_t least = ceil_div(pieces, p.a.top ? kScoreThreads * kPartVectors : kMostPieces), most = ceil_div(pieces, kScoreThreads);
+  const int64_t least = ceil_div(pieces, kScoreThreads * (p.a.top ? kPartVectors : kSumVectors * kMostSums)), most = ceil_div(pieces, kScoreThreads);
   const int64_t limit = p.a.top ? 64 : 128;       // (of lists that are joined)
   const int64_t wanted = pieces <= one ? 1 : std::max<int64_t>(least, std::min<int64_t>({most, limit, 512 / std::max<int64_t>(1, p.a.rows)}));
   const int64_t rounds = ceil_div(pieces, wanted * kScoreThreads);           // pieces per lane

@@ -345,6 +345,24 @@ struct LaneSums {
   }
 };
 
+// The same of many logits: what has been added up so far is put aside now and then, so that small terms are not lost in it one by one.
+struct LongSums : LaneSums {
+  float s_all = 0.f, w_all = 0.f;
+  using LaneSums::LaneSums;
+  __device__ __forceinline__ void aside() {
+    s_all += s;
+    w_all += w;
+    s = w = 0.f;
+  }
+  __device__ __forceinline__ void raise(float most) {
+    const float before = R;
+    LaneSums::raise(most);
+    const float d = before - R, by = __builtin_amdgcn_exp2f(d);
+    w_all = by * fmaf(s_all, d, w_all);
+    s_all *= by;
+  }
+};
+
 // The sums of a wavefront, in all lanes.
 __device__ __forceinline__ Sums of_wave(Sums x, float c) {
   x.raise(over_lanes(x.M, 6, larger), c);
@@ -460,7 +478,7 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
 
   const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
   const float c = p.a.scale * kLog2e, beside = edge >= 0 ? (float)r.at[edge] : 0.f;
-  LaneSums lane(c);
+  LongSums lane(c);
   auto add = [&](const u32x4& v) {
     float most = P::get(v, 0);
 #pragma unroll
@@ -484,6 +502,7 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
         const u32x4 v = x[i];
         x[i] = load(j + i + kAhead);
         add(v);
+        if (i == kAhead - 1 && (j & (kSumVectors - 1)) == kSumVectors - kAhead) lane.aside();
       }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
@@ -499,6 +518,9 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
     else if (lane.exceeded(beside)) lane.raise(beside);
     lane.add(beside);
   }
+  lane.aside();
+  lane.s = lane.s_all;
+  lane.w = lane.w_all;
   Sums lane_sums = lane.exact();
   if (__any(lane.failed())) {
     float most = edge >= 0 ? beside : minus_infinity();
@@ -507,15 +529,17 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
 #pragma unroll
       for (int e = 0; e < P::kEach; ++e) most = larger(most, P::get(v, e));
     }
-    lane = LaneSums(c);
+    lane = LongSums(c);
     lane.M = most;
     if (edge >= 0) lane.add_any(beside);
     for (int i = tid; i < pieces; i += kThreads) {
       const u32x4 v = at[i];
 #pragma unroll
       for (int e = 0; e < P::kEach; ++e) lane.add_any(P::get(v, e));
+      if (i / kThreads % kSumVectors == kSumVectors - 1) lane.aside();
     }
-    lane_sums = {lane.M, lane.s, lane.w};
+    lane.aside();
+    lane_sums = {lane.M, lane.s_all, lane.w_all};
   }
   const Sums wave_sums = of_wave(lane_sums, c);
   if ((tid & 63) == 0) waves[tid >> 6] = wave_sums;

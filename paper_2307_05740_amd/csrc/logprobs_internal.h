@@ -12,7 +12,9 @@ constexpr int kScoreThreads = 256;
 constexpr int kMostTop = 32;
 constexpr int kMostVectors = 32;       // pieces of 16 bytes of a whole row that a lane of a workgroup holds
 constexpr int kPartVectors = 16;       // and of a part of one
-constexpr int64_t kMostPieces = 1 << 26; // of a part of a row that is not held
+// A lane's sums have no more than so many steps, which is what they are as exact as: up to 256 logits one after the other, and of these sums up to 128.
+constexpr int kSumVectors = 32;        // pieces, of a part that is not held, to a sum
+constexpr int kMostSums = 128;         // and sums of a part
 
 struct ScoreArgs {
   arrow_logprobs_t a;

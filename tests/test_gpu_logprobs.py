@@ -331,3 +331,34 @@ def test_offsets_beyond_32_bits(torch, LogProbs):
     assert torch.equal(r.top_ids[at], want["top_ids"])
     d = op.backward(g, None, x, t, r.stats, d_logits=x)
     within(torch, "d_logits", d[at], want["d_logits"], bound["d_logits"])
+
+
+@pytest.mark.parametrize("dtype,n,low", [("bfloat16", 1 << 20, -16.75), ("float16", 1 << 20, -16.75), ("float32", 1 << 19, -16.7), ("float16", 200_003, -16.75)])
+def test_long_sums_of_small_terms(torch, LogProbs, dtype, n, low):
+    """Many rows of many logits that are each less than half a step of a sum of 32 bits which begins with 1: one after the other they would all be lost."""
+    op, rows = LogProbs(), 512
+    x = torch.full((rows, n), low, dtype=getattr(torch, dtype), device="cuda")
+    each = 16 // x.element_size()
+    x[:, :256 * each:each] = 0.0
+    x += torch.arange(rows, device="cuda", dtype=x.dtype)[:, None] % 4
+    t = torch.arange(rows, device="cuda") % n
+    for part, masked in ((slice(0, None), False), (slice(0, 3), False), (slice(0, None), True)):
+        if masked:                          # (a token of every lane that cannot be, for which it adds up everything again)
+            x[:, 256 * each + 1:512 * each + 1:each] = -math.inf
+        r = op.forward(x[part], t[part])
+        some = torch.arange(x[part].shape[0], device="cuda")[::200]
+        want, bound = oracle.logprobs(x[some], t[some])
+        for name in ("logp", "entropy", "lse"):
+            within(torch, name, getattr(r, name)[some], want[name], bound[name])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_of_200000(torch, LogProbs, dtype):
+    op = LogProbs()
+    x, t = normal(torch, 1, dtype, 520, 200_000, by=3.0), targets_of(torch, 2, 520, 200_000)
+    r = op.forward(x, t)
+    d = op.backward(torch.ones_like(r.logp), None, x, t, r.stats)
+    for some in (slice(0, 8), slice(512, 520)):
+        want, bound = oracle.logprobs(x[some], t[some], 1.0, 0, torch.ones(8, device="cuda"), None)
+        for name, got in (("logp", r.logp), ("entropy", r.entropy), ("lse", r.lse), ("d_logits", d)):
+            within(torch, name, got[some], want[name], bound[name])
