@@ -945,7 +945,6 @@ template <typename T, bool kTop>
 int rows(const ScoreArgs& p, hipStream_t s) {
   const int lanes = p.lanes, n = p.vectors / lanes;
   const int64_t blocks = (p.a.rows + kThreads / lanes - 1) / (kThreads / lanes);
-  if (blocks > kMostBlocks) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(kThreads);
   if (lanes == 16) {
     if (n <= 1) score_rows_kernel<T, 16, 1, kTop><<<grid, block, 0, s>>>(p);
@@ -973,7 +972,6 @@ template <typename T>
 int forward(const ScoreArgs& p, hipStream_t s) {
   if (p.lanes) return p.a.top ? rows<T, true>(p, s) : rows<T, false>(p, s);
   const int64_t blocks = p.a.rows * p.parts;
-  if (blocks > kMostBlocks) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(kThreads);
   const int n = p.vectors / kThreads;
   if (p.a.top == 0) score_sums_kernel<T><<<grid, block, 0, s>>>(p);
@@ -989,30 +987,66 @@ int forward(const ScoreArgs& p, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
+// Gradients: 16 lanes where rows have up to 64 pieces, and 64; workgroups' worth of pieces to a row.
+template <typename T>
+int grad_lanes(const ScoreArgs& p) { return p.a.vocabulary / Piece<T>::kEach <= 16 * kGradPieces ? 16 : 64; }
+template <typename T>
+int64_t grad_chunks(const ScoreArgs& p) {
+  const int64_t each = grad_lanes<T>(p) * kGradPieces;
+  return std::max<int64_t>(1, (p.a.vocabulary / Piece<T>::kEach + each - 1) / each);
+}
 template <typename T, int L>
 int backward(const ScoreArgs& p, hipStream_t s) {
-  const int chunks = (int)std::max<int64_t>(1, ((int64_t)p.a.vocabulary / Piece<T>::kEach + L * kGradPieces - 1) / (L * kGradPieces));
-  const int64_t blocks = (p.a.rows * chunks + kThreads / L - 1) / (kThreads / L);
-  if (blocks > kMostBlocks) return (int)hipErrorInvalidConfiguration;
-  score_grad_kernel<T, L><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(p, chunks);
+  const int64_t chunks = grad_chunks<T>(p), blocks = (p.a.rows * chunks + kThreads / L - 1) / (kThreads / L);
+  score_grad_kernel<T, L><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(p, (int)chunks);
   return (int)hipGetLastError();
 }
-// (rows of up to 64 pieces by 16 lanes)
+
+// A call's rows from one on.
+ScoreArgs rows_from(const ScoreArgs& p, int64_t first, int64_t rows, int64_t size) {
+  ScoreArgs q = p;
+  const auto by = [&](auto*& at, int64_t each) { at = at ? at + first * each : at; };
+  const auto bytes = [&](auto* at, int64_t each) { return at ? decltype(at)((uintptr_t)at + first * each) : at; };
+  q.a.rows = rows;
+  q.logits = bytes(p.logits, p.a.stride * size);
+  q.targets = bytes(p.targets, p.a.target_bytes);
+  q.d_logits = bytes(p.d_logits, p.a.d_stride * size);
+  by(q.d_logp, 1); by(q.d_entropy, 1); by(q.entropy_in, 1);
+  by(q.logp, 1); by(q.entropy, 1); by(q.lse, 1); by(q.stats, 2);
+  by(q.top_logp, p.a.top); by(q.top_ids, p.a.top);
+  by(q.sums, 4 * p.parts); by(q.keys, (int64_t)p.parts * p.a.top);
+  return q;
+}
+
+// In as many launches as have `most` rows each: nearly always one.
+template <typename F>
+int in_turn(const ScoreArgs& p, int64_t most, int64_t size, F&& f) {
+  if (p.a.rows <= most) return f(p);
+  for (int64_t first = 0; first < p.a.rows; first += most)
+    if (int rc = f(rows_from(p, first, std::min(most, p.a.rows - first), size))) return rc;
+  return 0;
+}
+
 template <typename T>
-int backward(const ScoreArgs& p, hipStream_t s) {
-  return p.a.vocabulary / Piece<T>::kEach <= 16 * kGradPieces ? backward<T, 16>(p, s) : backward<T, 64>(p, s);
+int forward_all(const ScoreArgs& p, void* stream) {
+  return in_turn(p, p.lanes ? kMostBlocks * (kThreads / p.lanes) : kMostBlocks / p.parts, sizeof(T), [&](const ScoreArgs& q) { return forward<T>(q, (hipStream_t)stream); });
+}
+template <typename T>
+int backward_all(const ScoreArgs& p, void* stream) {
+  const int lanes = grad_lanes<T>(p);
+  return in_turn(p, kMostBlocks * (kThreads / lanes) / grad_chunks<T>(p), sizeof(T), [&](const ScoreArgs& q) {
+    return lanes == 16 ? backward<T, 16>(q, (hipStream_t)stream) : backward<T, 64>(q, (hipStream_t)stream);
+  });
 }
 
 }  // namespace
 
 int launch_score_forward(const ScoreArgs& p, void* stream) {
-  hipStream_t s = (hipStream_t)stream;
-  return p.a.dtype == ARROW_F32 ? forward<float>(p, s) : p.a.dtype == ARROW_BF16 ? forward<__bf16>(p, s) : forward<_Float16>(p, s);
+  return p.a.dtype == ARROW_F32 ? forward_all<float>(p, stream) : p.a.dtype == ARROW_BF16 ? forward_all<__bf16>(p, stream) : forward_all<_Float16>(p, stream);
 }
 
 int launch_score_backward(const ScoreArgs& p, void* stream) {
-  hipStream_t s = (hipStream_t)stream;
-  return p.a.dtype == ARROW_F32 ? backward<float>(p, s) : p.a.dtype == ARROW_BF16 ? backward<__bf16>(p, s) : backward<_Float16>(p, s);
+  return p.a.dtype == ARROW_F32 ? backward_all<float>(p, stream) : p.a.dtype == ARROW_BF16 ? backward_all<__bf16>(p, stream) : backward_all<_Float16>(p, stream);
 }
 
 }  // namespace arrow

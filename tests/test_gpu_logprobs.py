@@ -362,3 +362,17 @@ def test_many_rows_of_200000(torch, LogProbs, dtype):
         want, bound = oracle.logprobs(x[some], t[some], 1.0, 0, torch.ones(8, device="cuda"), None)
         for name, got in (("logp", r.logp), ("entropy", r.entropy), ("lse", r.lse), ("d_logits", d)):
             within(torch, name, got[some], want[name], bound[name])
+
+
+@pytest.mark.parametrize("n,top,border,rows", [(17, 9, 67_108_860, 67_108_911), (5, 0, 268_435_440, 268_435_471)])
+def test_more_rows_than_a_launch_has(torch, LogProbs, n, top, border, rows):
+    """67,108,860 rows of a wavefront each are the most that a launch has, or 268,435,440 of 16 lanes."""
+    op, g = LogProbs(), torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((rows, n), generator=g, device="cuda", dtype=torch.float16)
+    t = (torch.arange(rows, device="cuda", dtype=torch.int32) * 7) % (n + 1)
+    r = op.forward(x, t, top)
+    d = op.backward(r.logp, r.entropy, x, t, r.stats, r.entropy)
+    for at in (slice(0, 9), slice(border - 7, border + 9), slice(rows - 9, rows)):
+        want = op.forward(x[at], t[at], top)
+        assert all(torch.equal(a[at], b) for a, b in zip(r, want) if a is not None), at
+        assert torch.equal(d[at], op.backward(r.logp[at], r.entropy[at], x[at], t[at], r.stats[at], r.entropy[at])), at
