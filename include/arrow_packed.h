@@ -57,7 +57,7 @@ int arrow_packed_read(const arrow_packed_t *c, int64_t tokens, const int64_t *sl
 
 /*
  * o of one query per sequence, at position lengths[b] - 1, as arrow_attention_decode has it.  k, v: the new token's key and value (token step unused), which are
- * written to their place first, or both NULL where they are in the pool.  A page that is not there, or an idle sequence, is as there.
+ * written to their place first, or both NULL where they are in the pool.  batch * q_heads is at most 2^24 - 1.  A page that is not there, or an idle sequence, is as there.
  * ws: DEVICE, 256-byte aligned, at least arrow_packed_decode_workspace_bytes(c) (which may be 0); written, holds nothing between calls.
  * Errors: EINVAL, ETOOSMALL, EHIP.
  */

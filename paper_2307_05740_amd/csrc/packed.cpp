@@ -60,6 +60,7 @@ PackedArgs plan(const arrow_packed_t* c) {
 int check_decode(const arrow_packed_t* c) {
   if (c->batch < 0) return refuse(ARROW_EINVAL, "batch = %d", c->batch);
   if (c->q_heads < 1 || c->q_heads % c->kv_heads) return refuse(ARROW_EINVAL, "q_heads = %d is no multiple of kv_heads = %d", c->q_heads, c->kv_heads);
+  if ((int64_t)c->batch * c->q_heads > kMostBlocks) return refuse(ARROW_EINVAL, "batch = %d with q_heads = %d: 2^24 - 1 rows at most", c->batch, c->q_heads);
   if (c->window < 0 || c->sinks < 0) return refuse(ARROW_EINVAL, "window = %d, sinks = %d", c->window, c->sinks);
   if (!(c->scale > 0.f) || !std::isfinite(c->scale)) return refuse(ARROW_EINVAL, "scale = %g is not positive and finite", c->scale);
   if (c->columns < 0 || (int64_t)c->columns * c->page > kMostTokens)
@@ -103,7 +104,7 @@ PackedArgs plan_decode(const arrow_packed_t* c) {
   const int64_t even = equal ? 1 : rows > 768 ? ceil_div(seen, 4000) : rows >= 384 ? std::max(std::min<int64_t>(4, ceil_div(seen, 2500)), ceil_div(seen, 6000))
                                                                                     : std::max(std::min<int64_t>(8, seen / 1000), ceil_div(seen, 2000));
   const int64_t rounds = ceil_div(seen, 128), best = (int64_t)std::sqrt(0.1 * (double)seen);
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, std::max(512 / rows, even), best, rounds}));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({kMostSplits, std::max(512 / rows, even), best, rounds, kMostBlocks / rows}));
   p.splits = (int32_t)ceil_div(rounds, ceil_div(rounds, most));
   return p;
 }

@@ -14,6 +14,8 @@
 // 16 tiles in all, one of two on its SIMD: some 150 vector and 65 scalar instructions each, and the waits between them; one row of 1000 keys 5.4 us and 3.7 for the join, which are
 // launches and four loads that wait for each other.  Tried for the window: four blocks of 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax
 // (22 us, and spills with heads of 128); tiles of 64 keys (24, spills); twice as many tiles on their way (22).
+#include <algorithm>
+
 #include "attention_common.h"
 #include "packed_internal.h"
 
@@ -435,7 +437,6 @@ template <typename T, int D>
 int decode(const PackedArgs& a, hipStream_t s) {
   const arrow_packed_t& c = a.c;
   const int64_t blocks = (int64_t)c.batch * c.kv_heads * a.splits * ((a.group + kHeadTile - 1) / kHeadTile), rows = (int64_t)c.batch * c.q_heads;
-  if (blocks * 64 * a.waves > 0xffffffff || rows * 256 > 0xffffffff) return (int)hipErrorInvalidConfiguration;   // (a launch has less than 2^32 threads)
   // Pages of 32 tokens or more have a tile in one of them: half the work on addresses and edges, which is scalar but takes turns with the rest (64 rows under a window of 4096, heads of 64
   // 20.9 us as for pages of 16, 19.1; 54 rows of up to 12,700 keys, 6/2 heads of 128, 35.2 and 32.2).
   const auto launch = [&](auto* kernel) { kernel<<<dim3((unsigned)blocks), dim3(64 * a.waves), 0, s>>>(a); };
@@ -451,27 +452,34 @@ int of_kind(const arrow_packed_t& c, F&& f) {
   return c.dim == 128 ? f.template operator()<_Float16, 128>() : c.dim == 64 ? f.template operator()<_Float16, 64>() : f.template operator()<_Float16, 32>();
 }
 
-unsigned blocks_of(const PackedArgs& p) {
-  const int64_t n = ((p.tokens + 3) / 4 * 4 * p.c.kv_heads * (p.c.dim / 8) + 255) / 256;
-  return n * 256 > 0xffffffff ? 0 : (unsigned)n;
+// Writes and reads, in as many launches as it takes: nearly always one.
+template <typename F>
+int in_turn(const PackedArgs& p, F&& launch) {
+  const int64_t pieces = (int64_t)p.c.kv_heads * (p.c.dim / 8), most = kMostBlocks * 256 / pieces / 4 * 4;
+  for (int64_t first = 0; first < p.tokens; first += most) {
+    PackedArgs q = p;
+    q.tokens = std::min(most, p.tokens - first);
+    q.slots = p.slots ? p.slots + first : nullptr;           // (the last places of sequences are fewer than a launch has)
+    q.k.at = (const char*)p.k.at + first * p.k.token * 2;
+    q.v.at = (const char*)p.v.at + first * p.v.token * 2;
+    launch(q, dim3((unsigned)(((q.tokens + 3) / 4 * 4 * pieces + 255) / 256)));
+    if (const hipError_t rc = hipGetLastError()) return (int)rc;
+  }
+  return 0;
 }
 
 struct Append {
   const PackedArgs& p;
   hipStream_t s;
   template <typename T, int D> int operator()() const {
-    if (!blocks_of(p)) return (int)hipErrorInvalidConfiguration;
-    packed_append_kernel<T, D><<<dim3(blocks_of(p)), dim3(256), 0, s>>>(p);
-    return (int)hipGetLastError();
+    return in_turn(p, [&](const PackedArgs& q, dim3 grid) { packed_append_kernel<T, D><<<grid, dim3(256), 0, s>>>(q); });
   }
 };
 struct Read {
   const PackedArgs& p;
   hipStream_t s;
   template <typename T, int D> int operator()() const {
-    if (!blocks_of(p)) return (int)hipErrorInvalidConfiguration;
-    packed_read_kernel<T, D><<<dim3(blocks_of(p)), dim3(256), 0, s>>>(p);
-    return (int)hipGetLastError();
+    return in_turn(p, [&](const PackedArgs& q, dim3 grid) { packed_read_kernel<T, D><<<grid, dim3(256), 0, s>>>(q); });
   }
 };
 struct Decode {

@@ -9,6 +9,8 @@
 
 namespace arrow {
 
+constexpr int64_t kMostBlocks = 0xffffffff / 256;    // workgroups of 256: a launch has less than 2^32 threads
+
 struct PackedArgs {
   arrow_packed_t c;
   Operand q, k, v, o;

@@ -366,3 +366,26 @@ def test_views_of_one_tensor(torch, Packed):
     op.read(pool, slots, 64, torch.bfloat16, both[:, ::2][:, :2], both[:, 1::2])
     k, v = op.read(pool, slots, 64, torch.bfloat16)
     assert torch.equal(both[:, ::2][:, :2], k) and torch.equal(both[:, 1::2], v) and bool((both[:, 4] == 7).all())
+
+
+def test_more_tokens_than_a_launch_has(torch, Packed):
+    """33,554,428 tokens of 8 heads of 128 are the most that a launch writes or reads.  (Keys and values that overlap are 0.5 GB; what is read is 69 GB each.)"""
+    op, page, kv, dim, n, border = Packed(), 16, 8, 128, 33_554_500, 33_554_428
+    x = normal(torch, 1, "bfloat16", 1 << 20).repeat(-(-(n * 8 + kv * dim + 64) // (1 << 20)))
+    k, v = x.as_strided((n, kv, dim), (8, dim, 1)), x.as_strided((n, kv, dim), (8, dim, 1), 64)
+    slots = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    some = torch.cat([torch.arange(5), torch.arange(border - 6, border + 9), torch.arange(n - 5, n)]).cuda()
+    slots[some] = torch.randperm(2 * page, generator=torch.Generator().manual_seed(1))[:len(some)].cuda()
+    pool, want = op.pool(2, page, kv, dim), op.pool(2, page, kv, dim)
+    op.append(k, v, pool, slots)
+    op.append(k[some], v[some], want, slots[some])
+    assert torch.equal(pool, want)
+    if torch.cuda.mem_get_info()[0] < 160 * 2**30:
+        pytest.skip("the card has not the 138 GB of keys and values")
+    got = op.read(pool, slots, dim, torch.bfloat16)
+    for a, b in zip(got, op.read(pool, slots[some], dim, torch.bfloat16)):
+        assert torch.equal(a[some], b)
+    for at in (slice(1000, 2000), slice(border + 100, None), slice(border - 1000, border - 6)):
+        assert not any(bool(a[at][slots[at] < 0].any()) for a in got)
+    del got
+    torch.cuda.empty_cache()

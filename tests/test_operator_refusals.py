@@ -342,3 +342,18 @@ def test_packed_decode_refuses_what_overlaps(L, change, at):
     p = dict(dict(q=SOME, qs=st, k=2 * SOME, v=3 * SOME, ks=ROWS, vs=ROWS, pool=4 * SOME, o=5 * SOME, os=st, ws=16 * SOME), **at)
     assert "ws" not in at or L.arrow_packed_decode_workspace_bytes(ctypes.byref(c)) > 0
     refused(L.arrow_packed_decode(ctypes.byref(c), *p.values(), 1 << 30, 0), "overlap")
+
+
+@pytest.mark.parametrize("change", [{"batch": 1 << 22}, {"batch": 1 << 30}, {"batch": 1, "q_heads": 1 << 24}])
+def test_packed_decode_refuses_more_rows_than_a_launch_has(L, change):
+    """By name, before the new token's key and value are written."""
+    c, st = packed(**dict({"table": 1 << 44, "lengths": 1 << 45}, **change)), steps(0, 0, 64)
+    os = steps(64 * c.q_heads, 0, 64)
+    refused(L.arrow_packed_decode(ctypes.byref(c), SOME, st, 2 * SOME, 3 * SOME, steps(0, 0, 64), steps(0, 0, 64), 4 * SOME, 1 << 46, os, 1 << 47, 1 << 40, 0), "2^24 - 1 rows")
+
+
+def test_packed_decode_cuts_no_more_stretches_than_a_launch_has(L):
+    c = packed(batch=(1 << 18) - 1, q_heads=64, kv_heads=1, columns=1 << 22, max_len=1 << 26)
+    need = L.arrow_packed_decode_workspace_bytes(ctypes.byref(c))
+    rows = c.batch * 4                                            # (of sixteen heads)
+    assert need // (c.batch * 64 * 66 * 4) * rows * 256 < 1 << 32
