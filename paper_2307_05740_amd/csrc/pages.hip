@@ -70,7 +70,7 @@ struct Fresh {
       first = (int64_t)b * p.a.tokens;
       count = p.a.tokens;
     }
-    position = (int)max((int64_t)-0x40000000, (int64_t)now - count);
+    position = (int)max((int64_t)-0x80000000ll, (int64_t)now - count);
   }
   __device__ __forceinline__ int column(const PagesArgs& p) const { return (max(0, min(position, 1 << 30)) + p.a.page - 1) >> p.page_log; }   // the first that begins with one
 };

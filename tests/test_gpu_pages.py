@@ -190,3 +190,18 @@ def test_nothing_to_do(torch, Pages):
     none = Pages(0, 16)
     table, held, free = none.state(2, 3)
     assert none.step(table, held, free, torch.tensor([5, 0], dtype=torch.int32, device="cuda"), 1).tolist() == [[-1]] * 2 and int(free[0]) == 0
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_more_new_tokens_than_2_to_the_30(torch, Pages, ragged):
+    """Of a step that names far more new tokens than the sequence has, its own are the last ones.  (Slots of 8.6 GB.)"""
+    op, n = Pages(8, 16), 2**30 + 64
+    table, held, free = op.state(1, 4)
+    length = torch.tensor([40], dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, n], dtype=torch.int32, device="cuda") if ragged else None
+    slots = op.step(table, held, free, length, n, offsets).flatten()
+    assert slots[-40:].tolist() == list(range(40)) and bool((slots[:-40] == -1).all())
+    assert table.tolist() == [[0, 1, 2, -1]] and held.tolist() == [40] and free[:6].tolist() == [5, 7, 6, 5, 4, 3]
+    for length in (-5, -2**31):
+        slots = op.step(table, held, free, torch.tensor([length], dtype=torch.int32, device="cuda"), n, offsets)
+        assert bool((slots == -1).all()) and int(free[0]) == 8
