@@ -56,6 +56,9 @@ template <> struct Piece<_Float16> {
   }
 };
 
+// The scale for exponents of two.  (Finite: the largest logit's difference from itself times an infinity is no number.)
+__device__ __forceinline__ float exponents(float scale) { return fminf(scale * kLog2e, 3.402823466e38f); }
+
 // The larger of two; NaN where one is.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
@@ -477,7 +480,7 @@ __global__ __launch_bounds__(kThreads, 6) void score_sums_kernel(ScoreArgs p) {
   const Target target(p, row, (const T*)nullptr);
 
   const int edge = part == 0 ? r.edge(tid, p.a.vocabulary) : -1;
-  const float c = p.a.scale * kLog2e, beside = edge >= 0 ? (float)r.at[edge] : 0.f;
+  const float c = exponents(p.a.scale), beside = edge >= 0 ? (float)r.at[edge] : 0.f;
   LongSums lane(c);
   auto add = [&](const u32x4& v) {
     float most = P::get(v, 0);
@@ -575,7 +578,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs p) {
   const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity();
 
   // (the sums of a piece begin when it has come)
-  const float c = p.a.scale * kLog2e;
+  const float c = exponents(p.a.scale);
   LaneSums lane(c);
   float most[N], mine = beside;
   if (edge >= 0) { lane.start(beside); lane.add(beside); }
@@ -683,7 +686,7 @@ __global__ __launch_bounds__(kThreads) void score_rows_kernel(ScoreArgs p) {
     if (j * L + sub < r.pieces) x[j] = r.load(j * L + sub);
   }
   const int edge = r.edge(sub, p.a.vocabulary);
-  const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity(), c = p.a.scale * kLog2e;
+  const float beside = edge >= 0 ? (float)r.at[edge] : minus_infinity(), c = exponents(p.a.scale);
   LaneSums lane(c);
   float most[N], mine = beside;
   if (edge >= 0) { lane.start(beside); lane.add(beside); }
@@ -802,7 +805,7 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs p) {
   __shared__ Chosen chosen;
   const int tid = threadIdx.x, top = p.a.top, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x, n = (int64_t)p.parts * top;
-  const float c = p.a.scale * kLog2e;
+  const float c = exponents(p.a.scale);
   const uint64_t* keys = p.keys + row * n;
   uint64_t held[kHeld], most = 0;
 #pragma unroll
@@ -862,7 +865,7 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void score_join_rows_kernel(ScoreArgs p) {
   const int64_t row = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   if (row >= p.a.rows) return;
-  const float c = p.a.scale * kLog2e;
+  const float c = exponents(p.a.scale);
   const Target target(p, row, (const T*)nullptr);
   Sums sum{minus_infinity(), 0.f, 0.f};
   for (int i = 0; i < p.parts; ++i) {

@@ -376,3 +376,24 @@ def test_more_rows_than_a_launch_has(torch, LogProbs, n, top, border, rows):
         want = op.forward(x[at], t[at], top)
         assert all(torch.equal(a[at], b) for a, b in zip(r, want) if a is not None), at
         assert torch.equal(d[at], op.backward(r.logp[at], r.entropy[at], x[at], t[at], r.stats[at], r.entropy[at])), at
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,top", [(9, 0), (9, 5), (40, 20), (700, 3), (5000, 0), (9000, 4), (70_000, 0), (140_000, 2)])
+def test_the_largest_scales(torch, LogProbs, dtype, n, top):
+    """A temperature of next to nothing: whatever is on top has all of the probability."""
+    for scale in (2.0e38, 3.0e38):
+        op = LogProbs(scale)
+        x = -torch.randint(0, 2, (6, n), generator=torch.Generator().manual_seed(n)).to(getattr(torch, dtype)).cuda()
+        x[:, n // 2] = 0
+        x[0, :] = -1
+        x[0, 1] = 0
+        t = torch.tensor([1, 0, n // 2, 3, n - 1, 2], device="cuda")
+        want, bound = oracle.logprobs(x, t, op.scale, top, torch.ones(6, device="cuda"), None)
+        r = op.forward(x, t, top)
+        for name in ("logp", "entropy", "lse"):
+            within(torch, name, getattr(r, name), want[name], bound[name])
+        if top:
+            assert torch.equal(r.top_ids, want["top_ids"])
+            within(torch, "top_logp", r.top_logp, want["top_logp"], bound["top_logp"])
+        within(torch, "d_logits", op.backward(torch.ones(6, device="cuda"), None, x, t, r.stats), want["d_logits"], bound["d_logits"])
