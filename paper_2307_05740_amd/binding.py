@@ -96,11 +96,23 @@ class csf3_info_t(ctypes.Structure):
 ARROW_F32, ARROW_BF16, ARROW_F16 = 0, 1, 2
 
 
+class _Checked(ctypes.Structure):
+    """Whole numbers that a field has no room for are refused; ctypes would keep their lowest bits."""
+
+    def __setattr__(self, name, value):
+        kind = dict(self._fields_).get(name)
+        if kind in (ctypes.c_int32, ctypes.c_int64):
+            most = 1 << (8 * ctypes.sizeof(kind) - 1)
+            if not -most <= value < most:
+                raise ValueError(f"{name} = {value}: {-most} .. {most - 1}")
+        super().__setattr__(name, value)
+
+
 class arrow_strides_t(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int64) for name in ("sequence", "token", "head")]
 
 
-class arrow_attention_t(ctypes.Structure):
+class arrow_attention_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in
                 ("dtype", "batch", "q_heads", "kv_heads", "dim", "q_len", "k_len", "window", "sinks")] + \
                [("scale", ctypes.c_float), ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
@@ -108,7 +120,7 @@ class arrow_attention_t(ctypes.Structure):
                [(name, arrow_strides_t) for name in ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")]
 
 
-class arrow_cache_t(ctypes.Structure):
+class arrow_cache_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "batch", "q_heads", "kv_heads", "dim", "window", "sinks")] + \
                [("scale", ctypes.c_float), ("page", ctypes.c_int32), ("columns", ctypes.c_int32)] + \
                [(name, ctypes.c_int64) for name in
@@ -116,12 +128,12 @@ class arrow_cache_t(ctypes.Structure):
                [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
 
 
-class arrow_embedding_t(ctypes.Structure):
+class arrow_embedding_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "grad_dtype", "id_bytes", "columns")] + \
                [(name, ctypes.c_int64) for name in ("rows", "tokens", "w_stride", "y_stride")] + [("scale", ctypes.c_float)]
 
 
-class arrow_rotation_t(ctypes.Structure):
+class arrow_rotation_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in
                 ("dtype", "weight_dtype", "batch", "tokens", "q_heads", "kv_heads", "dim", "rotary", "interleaved")] + \
                [("eps", ctypes.c_float), ("position_bytes", ctypes.c_int32), ("positions", ctypes.c_void_p), ("shift", ctypes.c_int64),
@@ -129,19 +141,19 @@ class arrow_rotation_t(ctypes.Structure):
                [(name, arrow_strides_t) for name in ("q", "k", "q_out", "k_out", "dq", "dk")]
 
 
-class arrow_pages_t(ctypes.Structure):
+class arrow_pages_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in ("batch", "columns", "page", "window", "sinks", "tokens")] + \
                [("pages", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("rows", ctypes.c_int64)]
 
 
-class arrow_packed_t(ctypes.Structure):
+class arrow_packed_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "batch", "q_heads", "kv_heads", "dim", "window", "sinks")] + \
                [("scale", ctypes.c_float), ("page", ctypes.c_int32), ("columns", ctypes.c_int32)] + \
                [(name, ctypes.c_int64) for name in ("pages", "max_len", "page_step", "head_step")] + \
                [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
 
 
-class arrow_logprobs_t(ctypes.Structure):
+class arrow_logprobs_t(_Checked):
     _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "target_bytes", "top", "vocabulary")] + \
                [(name, ctypes.c_int64) for name in ("rows", "stride", "d_stride")] + [("scale", ctypes.c_float)]
 

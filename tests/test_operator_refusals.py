@@ -357,3 +357,21 @@ def test_packed_decode_cuts_no_more_stretches_than_a_launch_has(L):
     need = L.arrow_packed_decode_workspace_bytes(ctypes.byref(c))
     rows = c.batch * 4                                            # (of sixteen heads)
     assert need // (c.batch * 64 * 66 * 4) * rows * 256 < 1 << 32
+
+
+@pytest.mark.parametrize("kind", [binding.arrow_attention_t, binding.arrow_cache_t, binding.arrow_embedding_t, binding.arrow_rotation_t, binding.arrow_pages_t, binding.arrow_packed_t,
+                                  binding.arrow_logprobs_t])
+def test_numbers_that_a_field_has_no_room_for(kind):
+    """A table of 2^32 + 4 columns is none of four."""
+    a = kind()
+    for name, of in kind._fields_:
+        if of in (ctypes.c_int32, ctypes.c_int64):
+            most = 1 << (8 * ctypes.sizeof(of) - 1)
+            for value in (most, 2 * most + 4, -most - 1):
+                with pytest.raises(ValueError, match=name):
+                    setattr(a, name, value)
+                with pytest.raises(ValueError, match=name):
+                    kind(**{name: value})
+            for value in (most - 1, -most, 4):
+                setattr(a, name, value)
+                assert getattr(a, name) == value
