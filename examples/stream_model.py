@@ -124,7 +124,7 @@ class PackedCaches:
         self.pages, self.attend = ArrowPages(pages, page, window, sinks, device=DEV), ArrowPackedAttention(window, sinks, device=DEV)
         self.pools = [self.attend.pool(pages, page, model.kv_heads, model.dim) for _ in model.qkv]
         self.table, self.held, self.free = self.pages.state(batch, columns)
-        self.lengths, self.slots = torch.zeros(batch, dtype=torch.int32, device=DEV), None
+        self.lengths, self.length, self.slots = torch.zeros(batch, dtype=torch.int32, device=DEV), 0, None
 
     def append(self, layer, k, v):
         self.attend.append(k.flatten(0, 1), v.flatten(0, 1), self.pools[layer], self.slots)
@@ -133,7 +133,7 @@ class PackedCaches:
         return self.attend.decode(q, self.pools[layer], self.table, self.lengths, k=k, v=v)
 
     def grow(self, length):
-        more = length - int(self.lengths[0])
+        more, self.length = length - self.length, length
         self.lengths.fill_(length)
         self.slots = self.pages.step(self.table, self.held, self.free, self.lengths, more).flatten()
 

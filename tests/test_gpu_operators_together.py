@@ -351,3 +351,47 @@ def test_the_example(torch):
     ids, _ = example.serve(model, 120, bits=16)
     again, _ = example.serve(model, 120, bits=4)
     assert ids.shape == again.shape == (3, 120)
+
+
+def example_of():
+    spec = importlib.util.spec_from_file_location("stream_model", os.path.join(ROOT, "examples", "stream_model.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    return example
+
+
+def test_the_example_hands_out_pages_without_waiting(torch):
+    """Nothing comes back to the host for a token."""
+    example = example_of()
+    caches = example.PackedCaches(example.StreamModel(positions=True), 3, columns=10, pages=20)
+    caches.grow(3)
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        for length in (40, 41, 42, 60):
+            caches.grow(length)
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    assert caches.held.tolist() == [60] * 3 and caches.slots.shape == (3 * 18,)
+
+
+def test_the_example_has_the_same_cache_in_4_bits(torch):
+    """A server's two caches, the one in 16 bits of what the one in 4 keeps, page by page as they are given back and used again: attention over either is within what rounding does."""
+    example = example_of()
+    model = example.StreamModel()
+    args = dict(batch=3, columns=12, pages=3 * (model.attend.window // 16 + 4))
+    wide, narrow = example.Caches(model, **args), example.PackedCaches(model, **args)
+    for caches in (wide, narrow):
+        caches.grow(40)
+    rounded = lambda x: oracle.packed(x).to(x.dtype)   # noqa: E731
+    for layer in range(2):
+        k, v = (normal(torch, 10 * layer + i, "bfloat16", 3, 40, model.kv_heads, model.dim) for i in range(2))
+        wide.append(layer, rounded(k), rounded(v))
+        narrow.append(layer, k, v)
+    for length in range(41, 180):
+        for caches in (wide, narrow):
+            caches.grow(length)
+        for layer in range(2):
+            q, k, v = (normal(torch, 1000 * layer + 10 * length + i, "bfloat16", 3, heads, model.dim) for i, heads in enumerate((model.heads, model.kv_heads, model.kv_heads)))
+            got, want = narrow.decode(layer, q, k, v), wide.decode(layer, q, rounded(k), rounded(v))
+            # each is off by 2 u of sum p |v| at most, and by less than 2^-16 of it for scores and sums; no value is larger than 6
+            assert bool(((got.double() - want.double()).abs() <= 6 * (4 * 2.0 ** -8 + 2.0 ** -15)).all()), (length, layer)
