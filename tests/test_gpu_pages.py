@@ -205,3 +205,39 @@ def test_more_new_tokens_than_2_to_the_30(torch, Pages, ragged):
     for length in (-5, -2**31):
         slots = op.step(table, held, free, torch.tensor([length], dtype=torch.int32, device="cuda"), n, offsets)
         assert bool((slots == -1).all()) and int(free[0]) == 8
+
+
+@pytest.mark.parametrize("batch,columns,tokens", [(1, 4, 3), (5, 40, 1), (100, 100, 20), (1000, 60, 8), (60, 30, 200), (1000, 2, 40), (1100, 30, 3), (700, 700, 2), (3, 30_000, 5), (2000, 40, 0), (9, 20, 0)])
+def test_nothing_outside_is_touched(torch, Pages, batch, columns, tokens):
+    """State, lengths, offsets and slots as pieces of one tensor each with numbers between them, and any numbers in them, in one launch, two and several."""
+    g = random.Random(batch)
+    op, pages, gap = Pages(batch * columns // 2 + 3, 16, g.choice((0, 100)), 5), batch * columns // 2 + 3, 37
+    sizes = {"table": batch * columns, "held": batch, "free": 1 + pages, "lengths": batch, "offsets": batch + 1}
+
+    def any_of(n, low, high):
+        x = torch.randint(low, high, (n,), generator=torch.Generator().manual_seed(g.randrange(2**31)))
+        wild = torch.tensor([-2**31, -1, 2**31 - 1, 1 << 26, columns * 16, 0])[torch.randint(0, 6, (n,), generator=torch.Generator().manual_seed(g.randrange(2**31)))]
+        return torch.where(torch.rand(n, generator=torch.Generator().manual_seed(g.randrange(2**31))) < 0.2, wild, x).int()
+
+    for ragged in (False, True):
+        rows = batch * tokens
+        room = torch.full((sum(sizes.values()) + gap * (len(sizes) + 1),), 1234567, dtype=torch.int32, device="cuda")
+        places = torch.full((rows + 2 * gap,), 1234567, dtype=torch.int64, device="cuda")
+        part, own, at = {}, torch.zeros_like(room, dtype=torch.bool), gap
+        for name, n in sizes.items():
+            part[name], own[at:at + n] = room[at:at + n], True
+            at += n + gap
+        for _ in range(3):
+            part["table"].copy_(any_of(batch * columns, -2, pages + 2))
+            part["held"].copy_(any_of(batch, 0, columns * 16))
+            part["free"].copy_(any_of(1 + pages, 0, pages))
+            part["lengths"].copy_(any_of(batch, 0, columns * 16))
+            part["offsets"].copy_(any_of(batch + 1, 0, rows + 1).sort()[0] if g.random() < 0.5 else any_of(batch + 1, 0, rows + 1))
+            keep = {name: part[name].clone() for name in ("lengths", "offsets")}
+            slots = places[gap:gap + rows]
+            op.step(part["table"].view(batch, columns), part["held"], part["free"], part["lengths"], rows if ragged else tokens, part["offsets"] if ragged else None,
+                    slots if ragged else slots.view(batch, tokens))
+            assert bool((room[~own] == 1234567).all()) and bool((places[:gap] == 1234567).all()) and bool((places[gap + rows:] == 1234567).all())
+            assert all(torch.equal(part[name], x) for name, x in keep.items()) and torch.equal(part["held"], part["lengths"])
+            assert 0 <= int(part["free"][0]) <= pages
+            assert bool(((slots >= -1) & (slots < pages * 16)).all())
