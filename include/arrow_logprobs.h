@@ -7,7 +7,7 @@
  *
  * and the `top` largest logits in falling order, of equal ones the lower index first: their indices j and scale x_j - lse.  A target outside
  * 0 .. vocabulary - 1 (padding) has logp = 0 and no gradient of logp.  Logits of -infinity are tokens that cannot be: p = 0.  A row of nothing else has lse =
- * logp = -infinity (of its top, too), H = 0 and no gradient; one with NaN or +infinity has NaN in lse, logp, H, top_logp and its gradient.  NaN counts as the largest
+ * logp = -infinity (of its top, too), H = 0 and no gradient; one with NaN or +infinity has NaN in lse, logp (but of padding), H, top_logp and its gradient.  NaN counts as the largest
  * logit.
  *
  * Conventions are those of arrow.h: device pointers of the current device, work enqueued on `stream` (a hipStream_t) without waiting, nothing

@@ -4,7 +4,8 @@
  * A row of `dim` elements becomes codes of 4 bits and a scale for every 32 of them (the microscaled form e2m1 with scales e8m0): a code is a sign (its highest bit)
  * and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 in that order, a scale the byte e for 2^(e - 127), an element their product.  Written, the scale is the
  * smallest power of two of which no element's size is more than seven times, within 2^-126 .. 2^125 (float16: up to 2^13), the code the nearest one, of two the one whose
- * lowest bit is 0, and 6 for all above: no element is further off than half of the largest step.  Elements that are not finite make their 32 ones NaN (e = 255).
+ * lowest bit is 0, and 6 for all above: no element is further off than half of the largest step, unless that scale was cut (of the type's largest elements one may be off by nearly
+ * all of it: 65504 in float16 becomes 49152).  Elements that are not finite make their 32 ones NaN (e = 255).
  *
  * The block of a page of T tokens and one head, (dim + dim/16) T bytes:
  *     keys' codes     T x dim/2                       byte i of a row holds elements 2 i (low half) and 2 i + 1

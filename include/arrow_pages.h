@@ -40,7 +40,8 @@ typedef struct arrow_pages_t {
 /*
  * lengths: DEVICE, int32, batch: the new lengths.  State, DEVICE, int32: held, batch; table, batch x columns; list, 1 + pages.
  * slots: DEVICE, int64: batch x tokens, or rows with offsets; every one is written (-1 for rows that no sequence has).  NULL where there are none.
- * Lengths are cut to 0 .. columns * T, steps of offsets to 0 .. rows.
+ * What columns a sequence needs goes by its length cut to 0 .. columns * T; `held` keeps the length itself, and new tokens' places count from it: those beyond the table have none.
+ * Steps of offsets are cut to 0 .. rows.
  * ws: DEVICE, 256-byte aligned, at least arrow_pages_workspace_bytes(a); written, holds nothing between calls.
  * Errors: EINVAL, ETOOSMALL, EHIP.
  */

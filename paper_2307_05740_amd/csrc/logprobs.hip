@@ -7,9 +7,11 @@
 // among the lanes' largest ones (a search by bits, counting lanes by ballots) is no larger than the `top`-th of all: the border.  The few pieces that reach it are read again, and their keys
 // from it on go to a list in LDS, where each is placed by counting those before it.  If so many are alike that the list has no room, the border is found again as a key.
 //
-// Measured: 8192 rows of 32,000 in bfloat16 with the five best 109 us (97 on changing inputs), 4.8 TB/s of 524 MB (a 1 GiB copy: 5.1), vector instructions in 85 % of the cycles, some twelve
-// for a logit and a hundred for a row's border; 4095 of 50,257 without any, and their gradient: 110 and 134 us, 3.8 and 6.2 TB/s (the gradient's writes go on under the next
-// forward call), 243 together for 242 of the floor; 4 rows of 128,001 in float32 with the twenty best 7.1 us and 5.7 for the join, launches and barriers.
+// Measured: 8192 rows of 32,000 in bfloat16 with the five best 112 us by itself, 4.7 TB/s of 524 MB, vector instructions in 83 % of the cycles, some twelve for a logit and a hundred for
+// a row's border; 96 a call of several in a row, whose first workgroups fill what the last ones of the call before leave (5.5 TB/s: reads alone are faster than a copy, 5.1);
+// 4095 of 50,257 without any, and their gradient: 110 and 135 us, 3.8 and 6.2 TB/s (the gradient's writes go on under the next forward call; forward calls alone 74), 243 together for 242 of
+// the floor, in float32 145 and 296; 4 rows of 128,001 in float32 with the twenty best 7.3 us and 5.7 for the join, launches and barriers.  With a third or nine tenths of the
+// logits masked by -infinity 4095 of 50,257 take 180 us and 8192 of 32,000 134, as every wavefront adds up its pieces again.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

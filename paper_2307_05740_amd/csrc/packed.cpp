@@ -83,7 +83,7 @@ PackedArgs plan_decode(const arrow_packed_t* c) {
   if (p.c.window) seen = std::min(seen, (int64_t)p.c.window + p.c.sinks);
   const int64_t rows = std::max<int64_t>(1, (int64_t)c->batch * c->kv_heads * ceil_div(p.group, kHeadTile));
   // Stretches of the visible keys, each a workgroup of four wavefronts; more than one take another launch, for their join.
-  const bool equal = p.c.window != 0;               // (sequences see equally many keys)
+  const bool equal = p.c.window != 0;               // (sequences that are longer than it see equally many keys; of those that are not, lengths are not known here)
   p.waves = 4;
   p.splits = 1;
   if (seen <= 512) return p;                        // (2 to 256 rows of up to 400 keys: 6.7 to 8.8 us, in two stretches 9.7 to 11.4)

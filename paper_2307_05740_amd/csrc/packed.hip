@@ -9,10 +9,11 @@
 // eight as they are: the values of four tokens lie together in the cache so that a lane finds its four tokens' eight columns (heads of 128) in 16 bytes, and two
 // permutations of bytes turn two tokens' pairs of columns into two columns' pairs of tokens.
 //
-// Measured: 32 rows of up to 16,000 keys, 32/8 heads of 128, 366 MB in 78 us with the join, 4.7 TB/s (a 1 GiB copy: 5.1), matrix units busy in 11 % of the cycles and vector
-// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 39 %; 64 rows under a window of 4096, 16/4 heads of 64, 18 us on changing inputs, 4.1 TB/s, where a wavefront has
-// 16 tiles in all, one of two on its SIMD: some 150 vector and 65 scalar instructions each, and the waits between them; one row of 1000 keys 5.4 us and 3.7 for the join, which are
-// launches and four loads that wait for each other.  Tried for the window: four blocks of 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax
+// Measured: 32 rows of up to 16,000 keys, 32/8 heads of 128, 366 MB in 80 us, 4.6 TB/s (a 1 GiB copy: 5.1), matrix units busy in 16 % of the cycles and vector
+// instructions, most of them conversions and the softmax of 16 columns of which 4 are heads, in 49 %, and 5 us for the join, which mostly goes on beside the next call; 64 rows under a window of
+// 4096, 16/4 heads of 64, 18.7 us on changing inputs, 3.9 TB/s, where a wavefront has 16 tiles in all, one of two on its SIMD: some 170 vector and 65 scalar instructions each, and the
+// waits between them; one row of 1000 keys 5.5 us and 3.1 for the join, which are launches and four loads that wait for each other.  A new token's key and value are written by a launch of
+// their own, 3.8 us more of any of these.  Tried for the window: four blocks of 16 keys to a tile, whose four heads fill the 16 columns, for a quarter of the softmax
 // (22 us, and spills with heads of 128); tiles of 64 keys (24, spills); twice as many tiles on their way (22).
 #include <algorithm>
 
@@ -84,7 +85,7 @@ __device__ __forceinline__ int64_t value_scales_at(int page, int dim) { return (
 
 // ---- writes and reads ----
 // Eight elements a lane, four lanes to a scale.  Four tokens of a head lie in neighbouring lanes, so that what a wavefront writes are whole runs of bytes.  Bound by memory:
-// 16,384 tokens of 8 heads of 128 are written in 17.5 us, 5.0 TB/s, and read in 15.6, 5.7.
+// 16,384 tokens of 8 heads of 128 are written in 16.9 us, 5.2 TB/s, and read in 15.3, 5.8.
 struct Place {
   int64_t row, slot;                  // slot -1: none
   int head, piece;

@@ -2,9 +2,9 @@
 //
 // What a step has to touch is little: the entries of columns that change, a page of the list for each, and the slots.  What is needed of a row of the table is two
 // runs of columns, the first ones and those of the window, so that what changes are up to three runs, found from the two lengths without looking at the table.
-// Small steps, such as that of a token for each sequence, are one launch of one workgroup, bound by the loads and barriers that follow each other (64 sequences, 3.7 us, the
+// Small steps, such as that of a token for each sequence, are one launch of one workgroup, bound by the loads and barriers that follow each other (64 sequences, 3.6 us there and 4.5 back, the
 // launch with them); of more new tokens a second launch takes the pages and writes the slots; steps of large tables count, give back and take in a launch each (256 prompts of up to
-// 16,000 tokens: 3.0, 4.0 and 12.2 us, of which the slots' 20 MB are 4; and 3.0 and 4.0 for their end).  The rules are with their numbers in pages_internal.h.
+// 16,000 tokens: 2.8, 3.7 and 12.0 us, of which the slots' 20 MB are 4; and 2.8 and 3.7 for their end).  The rules are with their numbers in pages_internal.h.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(256) void pages_give_kernel(PagesArgs p, bool last)
 }
 
 // Takes and slots: neither waits for the other, as a slot's page is found in the list where it is a new one.  What bounds it is a wavefront's chain of loads (offsets, the
-// sequence's lengths, the list or table: 6.6 us of the 12.2 above); eight rows of a lane share it.
+// sequence's lengths, the list or table: 6.6 us of the 12.0 above); eight rows of a lane share it.
 constexpr int kRowsEach = 8;
 
 __global__ __launch_bounds__(256) void pages_take_kernel(PagesArgs p, int take_blocks) {

@@ -5,8 +5,8 @@
 // takes some tokens with all their heads, whose angles it computes once, into LDS: with 40 heads of 128 they are a fortieth of the work, but with three of 256 a third
 // (tiles_of in rotation.cpp has the times).
 //
-// Measured with 4 x 4096 tokens of 32/8 heads of 128 in bfloat16: forward 64 us, 5.2 TB/s of what it has to move (a 1 GiB copy: 5.1), vector instructions issue in 56 % of the cycles;
-// gradients 111 us, 4.5 TB/s, 53 %, and 5 us for the join of the weights' gradients; a few tokens 5.1 us, which is a launch.
+// Measured with 4 x 4096 tokens of 32/8 heads of 128 in bfloat16: forward 64 us, 5.2 TB/s of what it has to move (a 1 GiB copy: 5.1), vector instructions issue in 44 % of the cycles;
+// gradients 110 us, 4.6 TB/s, 43 %, and 5 us for the join of the weights' gradients (in float32 131 and 207 together); a few tokens 5.2 us, which is a launch.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
