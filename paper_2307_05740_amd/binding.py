@@ -99,12 +99,14 @@ ARROW_F32, ARROW_BF16, ARROW_F16 = 0, 1, 2
 class _Checked(ctypes.Structure):
     """Whole numbers that a field has no room for are refused; ctypes would keep their lowest bits."""
 
+    def __init_subclass__(cls, **kw):
+        super().__init_subclass__(**kw)
+        cls._most = {name: 1 << (8 * ctypes.sizeof(kind) - 1) for name, kind in cls._fields_ if kind in (ctypes.c_int32, ctypes.c_int64)}
+
     def __setattr__(self, name, value):
-        kind = dict(self._fields_).get(name)
-        if kind in (ctypes.c_int32, ctypes.c_int64):
-            most = 1 << (8 * ctypes.sizeof(kind) - 1)
-            if not -most <= value < most:
-                raise ValueError(f"{name} = {value}: {-most} .. {most - 1}")
+        most = self._most.get(name)
+        if most is not None and not -most <= value < most:
+            raise ValueError(f"{name} = {value}: {-most} .. {most - 1}")
         super().__setattr__(name, value)
 
 
